@@ -19,7 +19,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libparaanya.so")
 
-SOURCES = ["paraanya.cpp", "paraanya_parareal.cpp", "host_common.cpp", "k_solver.hip", "k_epsnet.hip", "k_parareal.hip"]
+SOURCES = ["paraanya.cpp", "paraanya_parareal.cpp", "host_common.cpp", "k_solver.hip", "k_epsnet.hip", "k_parareal.hip",
+           "paraanya_ops.cpp", "k_norm.hip", "k_cross.hip", "k_lora.hip"]
 ARCH = "gfx950"
 
 
@@ -33,7 +34,7 @@ def hipcc() -> str:
 def command(out: str = LIB) -> list:
     srcs = [os.path.join(CSRC, s) for s in SOURCES]
     return [hipcc(), f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-shared",
-            "-x", "hip", "-Wall", "-Wshadow", "-Werror=shadow", "-fvisibility=hidden", "-Wno-unused-command-line-argument",
+            "-x", "hip", "-Wall", "-Wshadow", "-Werror=shadow", "-fvisibility=hidden", "-parallel-jobs=8", "-Wno-unused-command-line-argument",
             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
             "-I", INCLUDE, "-I", CSRC, *srcs, "-o", out]
 

@@ -1,0 +1,331 @@
+"""Operators of a text-conditioned noise network (the C ABI in include/paraanya_ops.h): layer norm,
+cross attention to a prompt encoder's states, a shared projection with the low-rank adapters of many
+requests.
+
+Argument marshalling only, as in :mod:`binding`: every product and sum runs in the library's HIP
+kernels. Tensors lie on the current device; kernels run on torch's current stream, outputs and
+workspaces come from torch's allocator on that stream. :func:`layer_norm` and
+:func:`cross_attention` take part in autograd; the ``*_forward`` and ``*_backward`` functions do not.
+"""
+from __future__ import annotations
+
+import ctypes as C
+import math
+
+import torch
+
+from . import binding as B
+
+PA_F32, PA_BF16, PA_F16 = 0, 1, 2
+PA_MASK_NONE, PA_MASK_BOOL, PA_MASK_ADD = 0, 1, 2
+PA_NORM_MAX_COLS = 1 << 20
+PA_LORA_MAX_RANK = 128
+HEAD_DIM_MAX = 128
+
+EXPORTED = ("paraanya_layer_norm", "paraanya_layer_norm_backward", "paraanya_layer_norm_backward_workspace",
+            "paraanya_cross_attention", "paraanya_cross_attention_workspace",
+            "paraanya_cross_attention_backward", "paraanya_cross_attention_backward_workspace",
+            "paraanya_lora_linear", "paraanya_lora_linear_workspace")
+
+_DTYPE = {torch.float32: PA_F32, torch.bfloat16: PA_BF16, torch.float16: PA_F16}
+
+
+class Norm(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("dtype", C.c_int32), ("param_dtype", C.c_int32),
+                ("eps", C.c_double), ("x_stride", C.c_int64), ("y_stride", C.c_int64), ("dx_stride", C.c_int64)]
+
+
+class Cross(C.Structure):
+    _fields_ = [("batch", C.c_int64), ("q_len", C.c_int64), ("kv_len", C.c_int64), ("q_heads", C.c_int32),
+                ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_double),
+                ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3),
+                ("o_stride", C.c_int64 * 3), ("kv_lens", C.c_void_p), ("mask", C.c_void_p),
+                ("mask_kind", C.c_int32), ("pad", C.c_int32), ("mask_stride", C.c_int64)]
+
+
+class CrossGrad(C.Structure):
+    _fields_ = [("do_stride", C.c_int64 * 3), ("dq_stride", C.c_int64 * 3), ("dk_stride", C.c_int64 * 3),
+                ("dv_stride", C.c_int64 * 3)]
+
+
+class Lora(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("in_features", C.c_int32), ("out_features", C.c_int32), ("rank", C.c_int32),
+                ("adapters", C.c_int32), ("requests", C.c_int32), ("dtype", C.c_int32), ("x_stride", C.c_int64),
+                ("w_stride", C.c_int64), ("y_stride", C.c_int64), ("offsets", C.c_void_p), ("ids", C.c_void_p),
+                ("scales", C.c_void_p)]
+
+
+_LIB = None
+
+
+def _library():
+    global _LIB
+    if _LIB is None:
+        lib = B.load_library()
+        P, Z = C.c_void_p, C.c_size_t
+        lib.paraanya_layer_norm.argtypes = [P, P, P, P, P, P, P, P]
+        lib.paraanya_layer_norm_backward.argtypes = [P, P, P, P, P, P, P, P, P, P, Z, P]
+        lib.paraanya_cross_attention.argtypes = [P, P, P, P, P, P, P, Z, P]
+        lib.paraanya_cross_attention_backward.argtypes = [P, P, P, P, P, P, P, P, P, P, P, P, Z, P]
+        lib.paraanya_lora_linear.argtypes = [P, P, P, P, P, P, P, P, Z, P]
+        for name in EXPORTED:
+            f = getattr(lib, name)
+            f.restype = C.c_int
+            if name.endswith("_workspace"):
+                f.argtypes = [P, C.POINTER(Z)]
+        _LIB = lib
+    return _LIB
+
+
+def _on_device(*tensors):
+    """The current stream's handle, once every tensor given is on the current device."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and not (t.is_cuda and t.get_device() == dev):
+            raise ValueError(f"expected tensors on the current CUDA device {dev}")
+    return torch.cuda.current_stream(dev).cuda_stream
+
+
+def _workspace(query, p, like):
+    """(tensor or None, bytes) of the scratch memory that a call with these sizes needs."""
+    n = C.c_size_t(0)
+    B._check(query(C.byref(p), C.byref(n)))
+    return (torch.empty(n.value, dtype=torch.uint8, device=like.device) if n.value else None), n.value
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+# ------------------------------------------------------------------ layer norm
+def _rows(t, N):
+    """A [rows, N] view of t (a copy where its strides allow no view)."""
+    t = t.reshape(-1, N)
+    return t if t.stride(1) == 1 and (t.shape[0] < 2 or t.stride(0) >= N) else t.contiguous()
+
+
+def _stride(t):
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _norm_args(x, weight, bias):
+    if x.dtype not in _DTYPE:
+        raise ValueError(f"layer norm of {x.dtype} is not built")
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError("layer norm needs at least one column")
+    pt = x.dtype
+    for t, name in ((weight, "weight"), (bias, "bias")):
+        if t is None:
+            continue
+        if t.shape != x.shape[-1:] or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous with {x.shape[-1]} elements")
+        if t.dtype not in (x.dtype, torch.float32):
+            raise ValueError(f"{name} must have x's type or float32")
+        pt = t.dtype
+    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+        raise ValueError("weight and bias must have one type")
+    return pt
+
+
+def layer_norm_forward(x, weight=None, bias=None, eps=1e-5):
+    """(y, mean, rstd) of the norm over x's last dimension; mean and rstd are fp32, one per row."""
+    pt = _norm_args(x, weight, bias)
+    st = _on_device(x, weight, bias)
+    N = x.shape[-1]
+    x2 = _rows(x, N)
+    M = x2.shape[0]
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    mean, rstd = torch.empty((2, M), dtype=torch.float32, device=x.device)
+    p = Norm(M, N, _DTYPE[x.dtype], _DTYPE[pt], eps, _stride(x2), N, N)
+    B._check(_library().paraanya_layer_norm(C.byref(p), x2.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(),
+                                            mean.data_ptr(), rstd.data_ptr(), st))
+    return y, mean, rstd
+
+
+def layer_norm_backward(dy, x, mean, rstd, weight=None, *, param_dtype=None):
+    """(dx, dweight, dbias) from the forward pass's x, mean and rstd. dweight and dbias have
+    weight's type (``param_dtype``, or x's, without a weight)."""
+    if weight is not None:
+        param_dtype = weight.dtype
+    elif param_dtype is None:
+        param_dtype = x.dtype
+    _norm_args(x, weight, None)
+    if param_dtype not in (x.dtype, torch.float32):
+        raise ValueError("param_dtype must be x's type or float32")
+    if dy.shape != x.shape or dy.dtype != x.dtype:
+        raise ValueError("dy must have x's shape and type")
+    N = x.shape[-1]
+    x2, dy2 = _rows(x, N), _rows(dy, N)
+    M = x2.shape[0]
+    for t in (mean, rstd):
+        if t.dtype != torch.float32 or t.numel() != M or not t.is_contiguous():
+            raise ValueError(f"mean and rstd must be contiguous float32 tensors of {M} elements")
+    st = _on_device(x, dy, mean, rstd, weight)
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    dw, db = torch.empty((2, N), dtype=param_dtype, device=x.device)
+    p = Norm(M, N, _DTYPE[x.dtype], _DTYPE[param_dtype], 0.0, _stride(x2), _stride(dy2), N)
+    lib = _library()
+    ws, n = _workspace(lib.paraanya_layer_norm_backward_workspace, p, x)
+    B._check(lib.paraanya_layer_norm_backward(C.byref(p), dy2.data_ptr(), x2.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+                                              _ptr(weight), dx.data_ptr(), dw.data_ptr(), db.data_ptr(), _ptr(ws), n, st))
+    return dx, dw, db
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps):
+        y, mean, rstd = layer_norm_forward(x, weight, bias, eps)
+        ctx.save_for_backward(x, weight, mean, rstd)
+        ctx.param_dtype = None if bias is None else bias.dtype
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, weight, mean, rstd = ctx.saved_tensors
+        dx, dw, db = layer_norm_backward(dy, x, mean, rstd, weight, param_dtype=ctx.param_dtype)
+        need = ctx.needs_input_grad
+        return dx if need[0] else None, dw if need[1] else None, db if need[2] else None, None
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5):
+    """The norm over x's last dimension, differentiable in x, weight and bias."""
+    return _LayerNorm.apply(x, weight, bias, eps)
+
+
+# ------------------------------------------------------------------ cross attention
+def _heads(t, name):
+    """t [batch, tokens, heads, head_dim] with consecutive head elements (a copy otherwise)."""
+    if t.dim() != 4:
+        raise ValueError(f"{name} must have the shape [batch, tokens, heads, head_dim]")
+    return t if t.stride(3) == 1 or t.shape[3] == 1 else t.contiguous()
+
+
+def _cross_args(q, k, v, kv_lens, mask, scale, o_stride):
+    if q.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError(f"cross attention of {q.dtype} is not built")
+    if k.dtype != q.dtype or v.dtype != q.dtype:
+        raise ValueError("q, k and v must have one type")
+    Bn, Lq, Hq, D = q.shape
+    Lk, Hk = k.shape[1], k.shape[2]
+    if k.shape != (Bn, Lk, Hk, D) or v.shape != k.shape:
+        raise ValueError("k and v must have one shape, and q's batch and head_dim")
+    if Hk < 1 or Hq % Hk:
+        raise ValueError("q's heads must be a multiple of k's")
+    p = Cross(Bn, Lq, Lk, Hq, Hk, D, _DTYPE[q.dtype], 1.0 / math.sqrt(D) if scale is None else scale,
+              q.stride()[:3], k.stride()[:3], v.stride()[:3], o_stride)
+    if kv_lens is not None:
+        if kv_lens.dtype != torch.int32 or kv_lens.shape != (Bn,) or not kv_lens.is_contiguous():
+            raise ValueError(f"kv_lens must be a contiguous int32 tensor of {Bn} elements")
+        p.kv_lens = kv_lens.data_ptr()
+    if mask is not None:
+        if mask.dtype not in (torch.bool, torch.uint8, torch.float32) or mask.shape != (Bn, Lk):
+            raise ValueError(f"mask must be a bool, uint8 or float32 tensor of [{Bn}, {Lk}]")
+        if mask.stride(1) != 1 and Lk > 1:
+            raise ValueError("a mask row's elements must be consecutive")
+        p.mask = mask.data_ptr()
+        p.mask_kind = PA_MASK_ADD if mask.dtype == torch.float32 else PA_MASK_BOOL
+        p.mask_stride = mask.stride(0)
+    return p
+
+
+def cross_attention_forward(q, k, v, *, kv_lens=None, mask=None, scale=None):
+    """(o, stats): softmax(scale q k^T + mask) v per head.
+
+    q [batch, q_len, q_heads, head_dim], k and v [batch, kv_len, kv_heads, head_dim] in bf16 or fp16, of
+    any strides with consecutive head elements (a stride of 0 repeats); q_heads a multiple of kv_heads.
+    ``kv_lens`` (int32, [batch]) is each sample's number of states; ``mask`` [batch, kv_len] admits keys
+    (bool or uint8) or is added to their scores (float32, -inf hides a key). ``scale`` defaults to
+    1 / sqrt(head_dim). stats [batch, q_heads, q_len, 2] is what the backward pass needs (the largest
+    score and the logarithm of the sum of exponentials past it; their sum is the log-sum-exp)."""
+    q, k, v = _heads(q, "q"), _heads(k, "k"), _heads(v, "v")
+    o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    st = _on_device(q, k, v, kv_lens, mask)
+    p = _cross_args(q, k, v, kv_lens, mask, scale, o.stride()[:3])
+    stats = torch.empty((q.shape[0], q.shape[2], q.shape[1], 2), dtype=torch.float32, device=q.device)
+    lib = _library()
+    ws, n = _workspace(lib.paraanya_cross_attention_workspace, p, q)
+    B._check(lib.paraanya_cross_attention(C.byref(p), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
+                                          stats.data_ptr(), _ptr(ws), n, st))
+    return o, stats
+
+
+def cross_attention_backward(do, q, k, v, o, stats, *, kv_lens=None, mask=None, scale=None):
+    """(dq, dk, dv) from the forward pass's inputs and results. A gradient has its input's full shape,
+    also where the input repeats memory (an expanded tensor)."""
+    q, k, v, o, do = _heads(q, "q"), _heads(k, "k"), _heads(v, "v"), _heads(o, "o"), _heads(do, "do")
+    if o.shape != q.shape or do.shape != q.shape or o.dtype != q.dtype or do.dtype != q.dtype:
+        raise ValueError("o and do must have q's shape and type")
+    if stats.dtype != torch.float32 or stats.shape != (q.shape[0], q.shape[2], q.shape[1], 2) or not stats.is_contiguous():
+        raise ValueError("stats must be the forward pass's")
+    st = _on_device(q, k, v, o, do, stats, kv_lens, mask)
+    p = _cross_args(q, k, v, kv_lens, mask, scale, o.stride()[:3])
+    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    dk = torch.empty(k.shape, dtype=q.dtype, device=q.device)
+    dv = torch.empty(v.shape, dtype=q.dtype, device=q.device)
+    g = CrossGrad(do.stride()[:3], dq.stride()[:3], dk.stride()[:3], dv.stride()[:3])
+    lib = _library()
+    ws, n = _workspace(lib.paraanya_cross_attention_backward_workspace, p, q)
+    B._check(lib.paraanya_cross_attention_backward(C.byref(p), C.byref(g), do.data_ptr(), q.data_ptr(), k.data_ptr(),
+                                                   v.data_ptr(), o.data_ptr(), stats.data_ptr(), dq.data_ptr(),
+                                                   dk.data_ptr(), dv.data_ptr(), _ptr(ws), n, st))
+    return dq, dk, dv
+
+
+class _CrossAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, kv_lens, mask, scale):
+        o, stats = cross_attention_forward(q, k, v, kv_lens=kv_lens, mask=mask, scale=scale)
+        ctx.save_for_backward(q, k, v, o, stats, kv_lens, mask)
+        ctx.scale = scale
+        return o
+
+    @staticmethod
+    def backward(ctx, do):
+        q, k, v, o, stats, kv_lens, mask = ctx.saved_tensors
+        dq, dk, dv = cross_attention_backward(do, q, k, v, o, stats, kv_lens=kv_lens, mask=mask, scale=ctx.scale)
+        return dq, dk, dv, None, None, None
+
+
+def cross_attention(q, k, v, *, kv_lens=None, mask=None, scale=None):
+    """:func:`cross_attention_forward`'s o, differentiable in q, k and v."""
+    return _CrossAttention.apply(q, k, v, kv_lens, mask, scale)
+
+
+# ------------------------------------------------------------------ projection with adapters
+def lora_linear(x, weight, a, b, offsets, ids, *, scales=None, bias=None):
+    """x W^T + bias + scales[i] (x A_i^T) B_i^T with the adapter i of each row's request.
+
+    x [rows, K], weight [N, K] (row strides of their own), bias [N], a [adapters, R, K] and
+    b [adapters, N, R] in bf16 or fp16. Request r is rows offsets[r] .. offsets[r + 1] - 1 and uses
+    adapter ids[r] (none if negative); offsets (requests + 1) and ids are int32 tensors on the
+    device, scales float32 ([adapters], 1 if absent). No gradients: an inference operator."""
+    if x.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError(f"lora linear of {x.dtype} is not built")
+    for t in (weight, a, b) + (() if bias is None else (bias,)):
+        if t.dtype != x.dtype:
+            raise ValueError("x, weight, a, b and bias must have one type")
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, a, b, bias, scales)):
+        raise ValueError("lora linear has no gradients: call it under torch.no_grad()")
+    if x.dim() != 2 or weight.dim() != 2 or a.dim() != 3 or b.dim() != 3:
+        raise ValueError("expected x [rows, K], weight [N, K], a [adapters, R, K] and b [adapters, N, R]")
+    (M, K), N, (E, R) = x.shape, weight.shape[0], a.shape[:2]
+    if weight.shape[1] != K or a.shape[2] != K or b.shape != (E, N, R) or (bias is not None and bias.shape != (N,)):
+        raise ValueError("x, weight, a, b and bias do not fit together")
+    n = ids.numel()
+    for t, count, name in ((offsets, n + 1, "offsets"), (ids, n, "ids")):
+        if t.dtype != torch.int32 or t.dim() != 1 or t.numel() != count or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous int32 tensor of {count} elements")
+    if scales is not None and (scales.dtype != torch.float32 or scales.shape != (E,) or not scales.is_contiguous()):
+        raise ValueError(f"scales must be a contiguous float32 tensor of {E} elements")
+    if not (a.is_contiguous() and b.is_contiguous() and (bias is None or bias.is_contiguous())):
+        raise ValueError("a, b and bias must be contiguous")
+    x, weight = (t if t.stride(1) == 1 and (t.shape[0] < 2 or t.stride(0) >= K) else t.contiguous() for t in (x, weight))
+    st = _on_device(x, weight, a, b, offsets, ids, scales, bias)
+    y = torch.empty((M, N), dtype=x.dtype, device=x.device)
+    p = Lora(M, K, N, R, E, n, _DTYPE[x.dtype], _stride(x), _stride(weight), N, offsets.data_ptr(), ids.data_ptr(),
+             _ptr(scales))
+    lib = _library()
+    ws, size = _workspace(lib.paraanya_lora_linear_workspace, p, x)
+    B._check(lib.paraanya_lora_linear(C.byref(p), x.data_ptr(), weight.data_ptr(), _ptr(bias), a.data_ptr(), b.data_ptr(),
+                                      y.data_ptr(), _ptr(ws), size, st))
+    return y

@@ -1,0 +1,492 @@
+"""The operators of include/paraanya_ops.h on the device against their definitions in 64 bits
+(tests/ops_reference.py), at the sizes, strides, masks and types where they can go wrong."""
+import math
+
+import pytest
+import torch
+
+import ops_reference as R
+from paper_2609_36522_amd import binding as B
+from paper_2609_36522_amd import ops
+
+pytestmark = pytest.mark.gpu
+
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+
+
+@pytest.fixture(autouse=True)
+def _lib(gpu_lib):
+    return gpu_lib
+
+
+def _gen(seed=0):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def _randn(g, *s, dtype=F32, f=1.0):
+    return (f * torch.randn(s, generator=g, device="cuda")).to(dtype)
+
+
+# ------------------------------------------------------------------ layer norm
+def _norm_case(M, N, dt, pt=None, seed=0, affine="wb"):
+    g = _gen(seed)
+    x = (_randn(g, M, N) * (0.5 + torch.rand(N, generator=g, device="cuda")) + 0.5 * _randn(g, N)).to(dt)
+    w = (1 + _randn(g, N, f=0.3)).to(pt or dt) if "w" in affine else None
+    b = _randn(g, N, dtype=pt or dt) if "b" in affine else None
+    return x, w, b, _randn(g, M, N, dtype=dt)
+
+
+def _check_norm(x, w, b, dy, eps=1e-5):
+    y, mean, rstd = ops.layer_norm_forward(x, w, b, eps)
+    dx, dw, db = ops.layer_norm_backward(dy, x, mean, rstd, w, param_dtype=None if b is None else b.dtype)
+    N = x.shape[-1]
+    ref = R.layer_norm(x.reshape(-1, N), w if w is not None or b is None else torch.ones(N, device="cuda", dtype=b.dtype), b, eps,
+                       dy.reshape(-1, N))
+    for name, got in (("y", y.reshape(-1, N)), ("dx", dx.reshape(-1, N)), ("dw", dw), ("db", db)):
+        R.check(got, *ref[name], f"{name} of {tuple(x.shape)} {x.dtype}")
+
+
+@pytest.mark.parametrize("dt", [F32, BF16, F16], ids=["f32", "bf16", "f16"])
+@pytest.mark.parametrize("M,N", [(1, 1), (3, 7), (1, 8), (5, 63), (4, 64), (2, 65), (9, 511), (3, 512), (7, 513),
+                                 (33, 1024), (2, 1025), (6, 1333), (5, 2048), (3, 2049), (4, 4096), (2, 4097), (3, 8192),
+                                 (2, 8193), (2, 20001), (2500, 96), (2100, 2056)])
+def test_layer_norm(M, N, dt):
+    _check_norm(*_norm_case(M, N, dt))
+
+
+@pytest.mark.parametrize("affine", ["", "w", "b", "wb"])
+@pytest.mark.parametrize("dt", [BF16, F16], ids=["bf16", "f16"])
+@pytest.mark.parametrize("N", [40, 3000, 9000])
+def test_layer_norm_parameters_in_32_bits(N, dt, affine):
+    _check_norm(*_norm_case(6, N, dt, F32, affine=affine))
+
+
+@pytest.mark.parametrize("N", [50, 1027, 5000])
+def test_layer_norm_strides_and_alignment(N):
+    """Rows apart, rows that start at any element, several leading dimensions."""
+    x, w, b, dy = _norm_case(12, N + 3, BF16)
+    w, b = w[:N].contiguous(), b[:N].contiguous()
+    _check_norm(x[:, 1:N + 1], w, b, dy[:, 3:N + 3])
+    _check_norm(x[:, :N].reshape(3, 4, N), w, b, dy[:, :N].reshape(3, 4, N))
+
+
+def test_layer_norm_offset_far_beyond_its_spread():
+    """A mean of 1000 times the deviation: squares are taken of differences."""
+    x, w, b, dy = _norm_case(8, 1024, F32)
+    _check_norm(x * 1e-2 + 10.0, w, b, dy)
+
+
+def test_layer_norm_constant_rows_and_no_rows():
+    x = torch.full((3, 100), 2.5, device="cuda")
+    y, mean, rstd = ops.layer_norm_forward(x, None, None, 1e-5)
+    assert torch.equal(y, torch.zeros_like(y)) and torch.equal(mean, x[:, 0].contiguous())
+    e = torch.empty((0, 100), device="cuda")
+    y, mean, rstd = ops.layer_norm_forward(e)
+    assert y.shape == (0, 100) and mean.numel() == 0
+    dx, dw, db = ops.layer_norm_backward(e, e, mean, rstd)
+    assert dx.shape == (0, 100) and not dw.any() and not db.any()
+
+
+def test_layer_norm_not_a_number_stays_in_its_row():
+    x, w, b, dy = _norm_case(9, 700, BF16)
+    x[4, 13] = math.nan
+    y, mean, rstd = ops.layer_norm_forward(x, w, b)
+    bad = torch.isnan(y).any(1)
+    assert bad.tolist() == [i == 4 for i in range(9)] and bool(torch.isnan(y[4]).all())
+    dx, _, db = ops.layer_norm_backward(dy, x, mean, rstd, w)
+    assert torch.isnan(dx).any(1).tolist() == [i == 4 for i in range(9)] and not bool(torch.isnan(db).any())
+
+
+def test_layer_norm_gradient_against_differences():
+    """The slope of sum(dy * y) along random directions, in fp32: a central difference with step h has
+    an error of h^2 times the third derivative and of the outputs' rounding over h."""
+    g = _gen(3)
+    M, N, h = 16, 333, 1e-2
+    x, w, b, dy = _norm_case(M, N, F32, seed=3)
+    y, mean, rstd = ops.layer_norm_forward(x, w, b)
+    dx, dw, db = ops.layer_norm_backward(dy, x, mean, rstd, w)
+    for which, grad in ((0, dx), (1, dw), (2, db)):
+        args = [x, w, b]
+        e = _randn(g, *args[which].shape)
+        up, dn = list(args), list(args)
+        up[which], dn[which] = args[which] + h * e, args[which] - h * e
+        f = [(ops.layer_norm_forward(*a)[0].double() * dy.double()).sum() for a in (up, dn)]
+        got = float((f[0] - f[1]) / (2 * h))
+        want = float((grad.double() * e.double()).sum())
+        noise = 64 * R.U32 * float((y.double() * dy.double()).abs().square().sum().sqrt()) / h
+        assert abs(got - want) <= noise + 2 * h * h * float(grad.double().norm() * e.double().norm()) / math.sqrt(N), (which, got, want)
+
+
+def test_layer_norm_in_autograd():
+    x, w, b, dy = _norm_case(10, 257, BF16)
+    leaves = [t.clone().requires_grad_(True) for t in (x, w, b)]
+    ops.layer_norm(*leaves, 1e-5).backward(dy)
+    y, mean, rstd = ops.layer_norm_forward(x, w, b, 1e-5)
+    for leaf, want in zip(leaves, ops.layer_norm_backward(dy, x, mean, rstd, w)):
+        assert torch.equal(leaf.grad, want)
+
+
+# ------------------------------------------------------------------ cross attention
+def _cross_case(B_, Lq, Hq, Hk, Lk, D, dt, seed=0, sharp=1.5):
+    g = _gen(seed)
+    return (_randn(g, B_, Lq, Hq, D, dtype=dt, f=sharp), _randn(g, B_, Lk, Hk, D, dtype=dt), _randn(g, B_, Lk, Hk, D, dtype=dt),
+            _randn(g, B_, Lq, Hq, D, dtype=dt))
+
+
+def _check_cross(q, k, v, do, **kw):
+    o, stats = ops.cross_attention_forward(q, k, v, **kw)
+    grads = ops.cross_attention_backward(do, q, k, v, o, stats, **kw)
+    ref = R.cross_attention(q, k, v, do, **kw)
+    what = f"{tuple(q.shape)} over {tuple(k.shape)} {q.dtype}"
+    for name, got in zip(("o", "dq", "dk", "dv"), (o, *grads)):
+        R.check(got, *ref[name], f"{name} of {what}")
+    lse, bound = ref["lse"]
+    seen = lse > -math.inf
+    assert torch.equal(stats.sum(-1) > -math.inf, seen)
+    R.check(torch.where(seen, stats.sum(-1).double(), 0.0), torch.where(seen, lse, 0.0), bound, f"log-sum-exp of {what}")
+
+
+LENGTHS = [(1, 1), (1, 5), (3, 1), (2, 31), (31, 32), (32, 33), (33, 64), (5, 77), (64, 77), (127, 96), (128, 128), (129, 129),
+           (130, 160), (1, 300), (7, 511), (40, 700), (260, 257)]
+
+
+@pytest.mark.parametrize("dt", [BF16, F16], ids=["bf16", "f16"])
+@pytest.mark.parametrize("Lq,Lk", LENGTHS)
+def test_cross_attention_lengths(Lq, Lk, dt):
+    _check_cross(*_cross_case(2, Lq, 3, 3, Lk, 64, dt))
+
+
+@pytest.mark.parametrize("D", [1, 7, 8, 16, 31, 32, 33, 40, 63, 64, 65, 72, 80, 96, 120, 127, 128])
+@pytest.mark.parametrize("Lq,Lk", [(37, 45), (70, 200)])
+def test_cross_attention_head_widths(D, Lq, Lk):
+    _check_cross(*_cross_case(1, Lq, 2, 2, Lk, D, BF16 if D % 2 else F16))
+
+
+@pytest.mark.parametrize("Hq,Hk", [(4, 1), (6, 2), (8, 8), (32, 4), (40, 1)])
+@pytest.mark.parametrize("Lq,Lk", [(1, 90), (17, 140), (50, 33)])
+def test_cross_attention_shared_heads(Hq, Hk, Lq, Lk):
+    _check_cross(*_cross_case(2, Lq, Hq, Hk, Lk, 48, BF16))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Lq", [1, 9, 45])
+def test_cross_attention_long_states_split(Lq, D):
+    """Few rows over long states: the keys are split over blocks and joined."""
+    _check_cross(*_cross_case(1, Lq, 2, 1, 5003, D, F16))
+
+
+@pytest.mark.parametrize("Lq", [1, 20, 150])
+@pytest.mark.parametrize("Lk", [60, 400])
+def test_cross_attention_sample_lengths(Lq, Lk):
+    """Lengths of zero, one, a tile's border and out of range (clamped), with infinities and NaN past them."""
+    lens = torch.tensor([0, 1, 32, Lk // 2 + 1, Lk, Lk + 9, -3], dtype=torch.int32, device="cuda")
+    q, k, v, do = _cross_case(7, Lq, 2, 2, Lk, 64, BF16)
+    for b, n in enumerate(lens.clamp(0, Lk).tolist()):
+        k[b, n:], v[b, n:] = math.nan, math.inf
+    _check_cross(q, k, v, do, kv_lens=lens)
+
+
+@pytest.mark.parametrize("kind", ["bool", "uint8", "add"])
+@pytest.mark.parametrize("Lq,Lk,Hq,Hk", [(1, 70, 4, 2), (40, 77, 2, 2), (140, 333, 4, 1)])
+def test_cross_attention_masks(kind, Lq, Lk, Hq, Hk):
+    """Masks with rows that admit nothing, one key, only the last; NaN and infinities in masked places."""
+    g = _gen(5)
+    keep = torch.rand((6, Lk), generator=g, device="cuda") < 0.6
+    keep[0] = False
+    keep[1] = False
+    keep[1, 3] = True
+    keep[2] = False
+    keep[2, Lk - 1] = True
+    keep[3] = True
+    q, k, v, do = _cross_case(6, Lq, Hq, Hk, Lk, 64, F16)
+    k[~keep] = math.nan
+    v[~keep] = -math.inf
+    mask = keep
+    if kind == "uint8":
+        mask = keep.to(torch.uint8) * 3
+    if kind == "add":
+        mask = torch.where(keep, _randn(g, 6, Lk), -math.inf)
+    _check_cross(q, k, v, do, mask=mask)
+    lens = torch.tensor([Lk, Lk, Lk - 1, 33, 0, Lk], dtype=torch.int32, device="cuda")
+    k[3, 33:], v[4] = math.inf, math.nan
+    _check_cross(q, k, v, do, mask=mask, kv_lens=lens)
+
+
+@pytest.mark.parametrize("Lq,Lk", [(1, 60), (40, 77), (40, 300)])
+@pytest.mark.parametrize("dt", [BF16, F16], ids=["bf16", "f16"])
+def test_cross_attention_masks_of_the_lowest_value(Lq, Lk, dt):
+    """fp32's lowest value, the 16-bit types' and -1e4 hide a key beside an ordinary one; a row that has
+    nothing else takes their average (the score is lost beside fp32's lowest value)."""
+    q, k, v, do = _cross_case(5, Lq, 2, 2, Lk, 64, dt)
+    mask = torch.zeros(5, Lk, device="cuda")
+    low = torch.finfo(F32).min
+    mask[0, ::2] = low
+    mask[1] = low
+    mask[2, 5:] = torch.finfo(dt).min
+    mask[3, ::3] = -1e4
+    mask[4] = low
+    mask[4, 7:] = -math.inf
+    _check_cross(q, k, v, do, mask=mask)
+
+
+def test_cross_attention_shared_mask_row_and_repeated_states():
+    """One prompt for many latents: k, v and the mask repeat (strides of 0)."""
+    q, k, v, do = _cross_case(5, 70, 3, 3, 91, 64, BF16)
+    k, v = k[:1].expand(5, -1, -1, -1), v[:1].expand(5, -1, -1, -1)
+    mask = (torch.rand((1, 91), generator=_gen(1), device="cuda") < 0.7).expand(5, -1)
+    _check_cross(q, k, v, do, mask=mask)
+    # Through autograd the shared states receive the sum over the latents.
+    leaf = k[:1].clone().requires_grad_(True)
+    ops.cross_attention(q, leaf.expand(5, -1, -1, -1), v, mask=mask).backward(do)
+    o, stats = ops.cross_attention_forward(q, k, v, mask=mask)
+    dk = ops.cross_attention_backward(do, q, k, v, o, stats, mask=mask)[1]
+    R.check(leaf.grad, dk.double().sum(0, keepdim=True), 5 * R.U[BF16] * dk.double().abs().sum(0, keepdim=True), "shared k")
+
+
+def test_cross_attention_strides_and_alignment():
+    """Heads before tokens, heads inside a packed projection, rows that start at any element."""
+    q, k, v, do = _cross_case(2, 50, 4, 4, 130, 40, BF16)
+
+    def heads_first(t):
+        return t.permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3)
+
+    _check_cross(heads_first(q), heads_first(k), heads_first(v), heads_first(do))
+    packed = torch.cat((k, v), 3)
+    _check_cross(q, packed[..., :40], packed[..., 40:], do)
+    wide = torch.zeros(2, 130, 4, 43, dtype=BF16, device="cuda")
+    wide[..., 1:41] = k
+    _check_cross(q, wide[..., 1:41], v, do)
+    _check_cross(q[:, ::2], k[:, ::3], v[:, ::3], do[:, ::2])
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.3, 3.0])
+def test_cross_attention_scales(scale):
+    _check_cross(*_cross_case(1, 45, 2, 2, 99, 32, F16, sharp=0.5), scale=scale)
+    _check_cross(*_cross_case(1, 2, 2, 2, 300, 32, F16, sharp=0.5), scale=scale)
+
+
+def test_cross_attention_large_scores():
+    """Scores of hundreds: one key takes all the weight."""
+    _check_cross(*_cross_case(1, 40, 2, 2, 200, 64, BF16, sharp=60.0))
+
+
+def test_cross_attention_no_queries_or_no_states():
+    q, k, v, do = _cross_case(2, 4, 2, 2, 9, 64, BF16)
+    o, stats = ops.cross_attention_forward(q, k[:, :0], v[:, :0])
+    assert not o.any() and bool((stats == -math.inf).all())
+    dq, dk, dv = ops.cross_attention_backward(do, q, k[:, :0], v[:, :0], o, stats)
+    assert not dq.any() and dk.numel() == 0
+    o, stats = ops.cross_attention_forward(q[:, :0], k, v)
+    dq, dk, dv = ops.cross_attention_backward(do[:, :0], q[:, :0], k, v, o, stats)
+    assert o.numel() == 0 and not dk.any() and not dv.any()
+
+
+def test_cross_attention_not_a_number_where_it_is_seen():
+    q, k, v, do = _cross_case(2, 40, 1, 1, 100, 64, BF16)
+    v[0, 50, 0, 3] = math.nan
+    o, _ = ops.cross_attention_forward(q, k, v)
+    assert bool(torch.isnan(o[0, :, 0, 3]).all()) and not bool(torch.isnan(o[1]).any())
+    k[1, 7] = math.inf
+    o, _ = ops.cross_attention_forward(q, k, v)
+    assert bool(torch.isnan(o[1]).any())
+
+
+def test_cross_attention_gradient_against_differences():
+    """The slope of sum(do * o) in fp64 along random directions, from fp16 outputs: the difference's
+    noise is the outputs' independent rounding over the step."""
+    g = _gen(11)
+    q, k, v, do = _cross_case(1, 64, 2, 1, 90, 32, F16, seed=11, sharp=1.0)
+    o, stats = ops.cross_attention_forward(q, k, v)
+    grads = ops.cross_attention_backward(do, q, k, v, o, stats)
+    noise = 2 * R.U[F16] * float((o.double() * do.double()).square().sum().sqrt())
+    for which in range(3):
+        e = _randn(g, *(q, k, v)[which].shape, dtype=F16, f=0.0625)
+        up, dn = [q, k, v], [q, k, v]
+        up[which], dn[which] = up[which] + e, dn[which] - e
+        step = (up[which].double() - dn[which].double())          # as rounded
+        f = [(ops.cross_attention_forward(*a)[0].double() * do.double()).sum() for a in (up, dn)]
+        got, want = float(f[0] - f[1]), float((grads[which].double() * step).sum())
+        scale = float(grads[which].double().norm() * step.norm()) / math.sqrt(step.numel())
+        assert abs(got - want) <= 6 * noise + 0.1 * scale * 4, (which, got, want, noise, scale)
+
+
+def test_cross_attention_in_autograd():
+    q, k, v, do = _cross_case(2, 33, 4, 2, 77, 64, F16)
+    lens = torch.tensor([77, 30], dtype=torch.int32, device="cuda")
+    leaves = [t.clone().requires_grad_(True) for t in (q, k, v)]
+    ops.cross_attention(*leaves, kv_lens=lens).backward(do)
+    o, stats = ops.cross_attention_forward(q, k, v, kv_lens=lens)
+    for leaf, want in zip(leaves, ops.cross_attention_backward(do, q, k, v, o, stats, kv_lens=lens)):
+        assert torch.equal(leaf.grad, want)
+
+
+def test_cross_attention_offsets_past_32_bits():
+    """Strides that put the last sample and the last token more than 2^32 elements from the first."""
+    Lk, D = 70, 64
+    big = torch.empty((1 << 32) + (1 << 20), dtype=BF16, device="cuda")
+    k = big.as_strided((2, Lk, 1, D), ((1 << 31), (1 << 31) // 69, D, 1))
+    q, kk, v, do = _cross_case(2, 5, 1, 1, Lk, D, BF16)
+    k.copy_(kk)
+    _check_cross(q, k, v, do)
+
+
+# ------------------------------------------------------------------ projection with adapters
+def _lora_case(M, K, N, Rk, E, dt, seed=0):
+    g = _gen(seed)
+    return (_randn(g, M, K, dtype=dt), _randn(g, N, K, dtype=dt, f=K ** -0.5), _randn(g, E, Rk, K, dtype=dt, f=K ** -0.5),
+            _randn(g, E, N, Rk, dtype=dt, f=Rk ** -0.5), 0.5 + torch.rand(E, generator=g, device="cuda"), _randn(g, N, dtype=dt))
+
+
+def _check_lora(x, w, a, b, off, ids, scales=None, bias=None):
+    o = torch.tensor(off, dtype=torch.int32, device="cuda")
+    i = torch.tensor(ids, dtype=torch.int32, device="cuda")
+    y = ops.lora_linear(x, w, a, b, o, i, scales=scales, bias=bias)
+    R.check(y, *R.lora_linear(x, w, a, b, off, ids, scales, bias), f"y of {tuple(x.shape)} x {tuple(w.shape)} {x.dtype}")
+
+
+@pytest.mark.parametrize("dt", [BF16, F16], ids=["bf16", "f16"])
+@pytest.mark.parametrize("M,K,N", [(1, 1, 1), (1, 64, 32), (3, 40, 33), (8, 1024, 96), (31, 100, 70), (32, 333, 64), (33, 65, 31),
+                                   (64, 512, 200), (65, 96, 129), (128, 128, 128), (200, 1030, 77), (300, 72, 260),
+                                   (1000, 520, 390), (1300, 264, 513), (4200, 136, 264)])
+@pytest.mark.parametrize("Rk", [1, 8, 20, 64, 128])
+def test_lora_linear(M, K, N, Rk, dt):
+    x, w, a, b, s, bias = _lora_case(M, K, N, Rk, 3, dt)
+    cuts = [0, M // 5, M // 5, M // 3, M - M // 4, M]
+    _check_lora(x, w, a, b, cuts, [2, 0, -1, 1, 0], s, bias)
+
+
+@pytest.mark.parametrize("M", [24, 64, 100, 700])
+def test_lora_linear_a_request_per_row(M):
+    x, w, a, b, s, bias = _lora_case(M, 264, 136, 16, 11, BF16)
+    _check_lora(x, w, a, b, list(range(M + 1)), [i % 13 - 1 for i in range(M)], s, bias)
+
+
+@pytest.mark.parametrize("M", [20, 500])
+def test_lora_linear_requests_at_the_edges(M):
+    """No request, rows before the first and past the last, offsets and ids out of range, no adapters."""
+    x, w, a, b, s, bias = _lora_case(M, 130, 100, 12, 4, F16)
+    _check_lora(x, w, a, b, [0], [], s, bias)
+    _check_lora(x, w, a, b, [3, 9, M - 2], [1, 3], None, None)
+    _check_lora(x, w, a, b, [-5, 7, 7, M + 40], [1, 0, 2], s, None)
+    _check_lora(x, w, a, b, [0, 5, M], [4, -7], s, bias)
+    _check_lora(x, w, a[:0], b[:0], [0, M], [0], s[:0], bias)
+    y = ops.lora_linear(x[:0], w, a, b, torch.zeros(2, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"))
+    assert y.shape == (0, 100)
+
+
+@pytest.mark.parametrize("M", [9, 333])
+def test_lora_linear_strides_and_alignment(M):
+    x, w, a, b, s, bias = _lora_case(M, 203, 150, 9, 2, BF16)
+    _check_lora(x[:, 3:131], w[:, 1:129], a[:, :, :128].contiguous(), b, [0, M // 2, M], [1, 0], s, bias)
+    _check_lora(x[::2], w[::3], a, b[:, ::3].contiguous(), [0, M // 4], [1], s, None)
+
+
+@pytest.mark.parametrize("M", [5, 300])
+def test_lora_linear_not_a_number_stays_in_its_row(M):
+    """An adapter or a row that is not finite changes no row of another request."""
+    x, w, a, b, s, bias = _lora_case(M, 64, 96, 16, 2, BF16)
+    a[1] = math.nan
+    off = torch.tensor([0, M // 2, M], dtype=torch.int32, device="cuda")
+    y = ops.lora_linear(x, w, a, b, off, torch.tensor([0, 1], dtype=torch.int32, device="cuda"), scales=s, bias=bias)
+    bad = torch.isnan(y).any(1)
+    assert not bool(bad[:M // 2].any()) and bool(bad[M // 2:].all())
+
+
+# ------------------------------------------------------------------ all
+def test_results_repeat_bit_for_bit_and_on_another_stream():
+    q, k, v, do = _cross_case(2, 300, 4, 2, 77, 64, BF16)
+    x, w, b, dy = _norm_case(3000, 513, BF16)
+    lx, lw, la, lb, ls, lbias = _lora_case(500, 264, 300, 16, 3, BF16)
+    off = torch.tensor([0, 100, 350, 500], dtype=torch.int32, device="cuda")
+    ids = torch.tensor([2, 0, 1], dtype=torch.int32, device="cuda")
+
+    def run():
+        o, st = ops.cross_attention_forward(q, k, v)
+        y, mean, rstd = ops.layer_norm_forward(x, w, b)
+        return (o, st, *ops.cross_attention_backward(do, q, k, v, o, st), y, *ops.layer_norm_backward(dy, x, mean, rstd, w),
+                ops.lora_linear(lx, lw, la, lb, off, ids, scales=ls, bias=lbias))
+
+    want = run()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        assert all(torch.equal(g, t) for g, t in zip(run(), want))
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        other = run()
+    s.synchronize()
+    assert all(torch.equal(g, t) for g, t in zip(other, want))
+
+
+def test_operators_in_a_graph():
+    """Captured once, replayed with new inputs, with the program's own work between."""
+    q, k, v, do = _cross_case(1, 3, 4, 2, 2000, 64, BF16)
+    x, w, b, dy = _norm_case(40, 264, BF16)
+    lx, lw, la, lb, ls, _ = _lora_case(40, 264, 128, 16, 3, BF16)
+    off = torch.tensor([0, 10, 40], dtype=torch.int32, device="cuda")
+    ids = torch.tensor([2, 0], dtype=torch.int32, device="cuda")
+
+    def run():
+        o, st = ops.cross_attention_forward(q, k, v)
+        y, mean, rstd = ops.layer_norm_forward(x, w, b)
+        return (o, *ops.cross_attention_backward(do, q, k, v, o, st), y, *ops.layer_norm_backward(dy, x, mean, rstd, w),
+                ops.lora_linear(lx, lw, la, lb, off, ids, scales=ls))
+
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = run()
+    for turn in range(4):
+        g = _gen(100 + turn)
+        for t in (q, k, v, do, x, dy, lx):
+            t.copy_(torch.randn(t.shape, generator=g, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in outs]
+        for a, e in zip(got, run()):
+            assert torch.equal(a, e), turn
+
+
+def test_refusals_on_the_device():
+    q, k, v, do = _cross_case(1, 4, 2, 2, 9, 64, BF16)
+    with pytest.raises(ValueError):
+        ops.cross_attention_forward(q.float(), k.float(), v.float())
+    with pytest.raises(ValueError):
+        ops.cross_attention_forward(q, k.half(), v)
+    with pytest.raises(ValueError):
+        ops.cross_attention_forward(q, k[:, :, :1], v)
+    with pytest.raises(ValueError):
+        ops.cross_attention_forward(q[:, :, :1], k, v)
+    with pytest.raises(ValueError):
+        ops.cross_attention_forward(q, k, v, mask=torch.ones(1, 8, device="cuda"))
+    with pytest.raises(ValueError):
+        ops.cross_attention_forward(q, k, v, kv_lens=torch.ones(1, dtype=torch.int64, device="cuda"))
+    with pytest.raises(ValueError):
+        ops.cross_attention_forward(q.cpu(), k, v)
+    wide = torch.zeros(1, 4, 2, 160, dtype=BF16, device="cuda")
+    with pytest.raises(B.PAError) as ei:
+        ops.cross_attention_forward(wide, wide, wide)
+    assert ei.value.code == B.PA_ERR_UNSUPPORTED
+    x, w, b, dy = _norm_case(4, 32, BF16)
+    with pytest.raises(ValueError):
+        ops.layer_norm_forward(x, w[:16], b)
+    with pytest.raises(ValueError):
+        ops.layer_norm_forward(x, w.half(), b)
+    with pytest.raises(ValueError):
+        ops.layer_norm_forward(x.int())
+    with pytest.raises(B.PAError) as ei:
+        ops.layer_norm_forward(x, w, b, eps=-1.0)
+    assert ei.value.code == B.PA_ERR_INVALID_ARG
+    lx, lw, la, lb, ls, bias = _lora_case(4, 32, 16, 8, 2, BF16)
+    off = torch.tensor([0, 4], dtype=torch.int32, device="cuda")
+    ids = torch.zeros(1, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        ops.lora_linear(lx, lw, la, lb[:, :, :4], off, ids)
+    with pytest.raises(ValueError):
+        ops.lora_linear(lx, lw, la, lb, off[:1], ids)
+    with pytest.raises(ValueError):
+        ops.lora_linear(lx.requires_grad_(True), lw, la, lb, off, ids)
+    big = torch.zeros(2, 200, 32, dtype=BF16, device="cuda")
+    with pytest.raises(B.PAError) as ei:
+        ops.lora_linear(lx.detach(), lw, big, torch.zeros(2, 16, 200, dtype=BF16, device="cuda"), off, ids)
+    assert ei.value.code == B.PA_ERR_UNSUPPORTED
