@@ -44,50 +44,64 @@ __device__ __forceinline__ float key_bias(const CrossDev& d, int b, int key) {
 }
 
 // A tile of ROWS rows on its way from memory to LDS: each thread holds some of its 16-byte pieces.
-template <class T, int DP, int ROWS>
+// Rows lie `stride` elements apart. Without RAGGED (head_dim a multiple of 8, strides below
+// kBufferStride) a piece is one buffer load whose offset within the tile fits 32 bits and is the same
+// for every tile; pieces and rows that do not exist get an offset out of the buffer's range, which reads
+// as zero. RAGGED takes any head_dim and stride.
+constexpr int64_t kBufferStride = 1 << 23;
+constexpr uint32_t kBufferBytes = 0x7fffffff, kNowhere = 0x80000000;
+
+template <class T, int DP, int ROWS, bool RAGGED>
 struct Stage {
     static constexpr int kPieces = ROWS * (DP / 8) / kThreads, kPerRow = DP / 8;
-    Pack8<T> r[kPieces];
+    uint4 r[kPieces];
+    uint32_t off;
 
-    __device__ __forceinline__ static int row(int i) { return ((int)threadIdx.x + i * kThreads) / kPerRow; }
+    __device__ __forceinline__ static int row(int i) { return (int)threadIdx.x / kPerRow + i * (kThreads / kPerRow); }
     __device__ __forceinline__ static int piece() { return (int)threadIdx.x % kPerRow; }
 
-    // at(row) is the address of a row's first element, or null for a row of zeros.
-    template <class F>
-    __device__ __forceinline__ void load(int dim, F at) {
+    __device__ __forceinline__ Stage(int dim, int64_t stride)
+        : off(piece() * 8 < dim ? (uint32_t)(row(0) * (int)stride + piece() * 8) * 2 : kNowhere) {}
+
+    // rows of the tile at `base` exist.
+    __device__ __forceinline__ void load(const T* base, int64_t stride, int rows, int dim) {
+        if constexpr (RAGGED) {
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const T* p = at(row(i));
-            r[i] = load8(p + piece() * 8, p ? dim - piece() * 8 : 0);
+            for (int i = 0; i < kPieces; ++i)
+                r[i] = __builtin_bit_cast(uint4, load8(base + row(i) * stride, piece() * 8, dim, row(i) < rows));
+        } else {
+            const __amdgpu_buffer_rsrc_t src = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, kBufferBytes, 0x00020000);
+            const int step = (kThreads / kPerRow) * (int)stride * 2;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i)
+                r[i] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(src, row(i) < rows ? off : kNowhere, i * step, 0));
         }
-    }
-    __device__ __forceinline__ void zero(int i) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) r[i].v[j] = (T)0.0f;
     }
     __device__ __forceinline__ void store(T* tile) const {
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i)
-            *reinterpret_cast<uint4*>(tile + piece_at<DP>(row(i), piece())) = __builtin_bit_cast(uint4, r[i]);
+        for (int i = 0; i < kPieces; ++i) *reinterpret_cast<uint4*>(tile + piece_at<DP>(row(i), piece())) = r[i];
     }
 };
 
 // Keys and values of a tile, zeros where a key is not visible (0 weight times an infinity or a NaN
 // would not be 0), and with MASKED the keys' biases.
-template <class T, int DP, int KEYS, bool MASKED>
+template <class T, int DP, int KEYS, bool MASKED, bool RAGGED>
 struct KvStage {
-    Stage<T, DP, KEYS> k, v;
-    float bias, seen[Stage<T, DP, KEYS>::kPieces];
+    typedef Stage<T, DP, KEYS, RAGGED> S;
+    S k, v;
+    float bias, seen[MASKED ? S::kPieces : 1];
+
+    __device__ __forceinline__ KvStage(const CrossDev& d) : k(d.dim, d.ks[1]), v(d.dim, d.vs[1]) {}
 
     __device__ __forceinline__ void load(const CrossDev& d, const T* kb, const T* vb, int b, int k0, int kend) {
-        k.load(d.dim, [&](int r) { return k0 + r < kend ? kb + (int64_t)(k0 + r) * d.ks[1] : nullptr; });
-        v.load(d.dim, [&](int r) { return k0 + r < kend ? vb + (int64_t)(k0 + r) * d.vs[1] : nullptr; });
+        k.load(kb + k0 * d.ks[1], d.ks[1], kend - k0, d.dim);
+        v.load(vb + k0 * d.vs[1], d.vs[1], kend - k0, d.dim);
         if constexpr (MASKED) {
             const int key = k0 + (int)threadIdx.x;
             bias = (int)threadIdx.x < KEYS && key < kend ? key_bias(d, b, key) : -INFINITY;
 #pragma unroll
-            for (int i = 0; i < Stage<T, DP, KEYS>::kPieces; ++i) {
-                const int kk = k0 + Stage<T, DP, KEYS>::row(i);
+            for (int i = 0; i < S::kPieces; ++i) {
+                const int kk = k0 + S::row(i);
                 seen[i] = kk < kend ? key_bias(d, b, kk) : 0.0f;
             }
         }
@@ -95,12 +109,8 @@ struct KvStage {
     __device__ __forceinline__ void store(T* kt, T* vt, float* bt) {
         if constexpr (MASKED) {
 #pragma unroll
-            for (int i = 0; i < Stage<T, DP, KEYS>::kPieces; ++i) {
-                if (seen[i] == -INFINITY) {
-                    k.zero(i);
-                    v.zero(i);
-                }
-            }
+            for (int i = 0; i < S::kPieces; ++i)
+                if (seen[i] == -INFINITY) k.r[i] = v.r[i] = make_uint4(0, 0, 0, 0);
             if ((int)threadIdx.x < KEYS) bt[threadIdx.x] = bias;
         }
         k.store(kt);
@@ -108,8 +118,24 @@ struct KvStage {
     }
 };
 
+// B operands of one row for all reduction steps: elements 16 ks + 8 half .. of the row at p.
+template <class T, int DP, bool RAGGED>
+__device__ __forceinline__ void load_row(typename Vec<T>::v8 (&out)[DP / 16], const T* p, int dim, int half, bool valid) {
+#pragma unroll
+    for (int ks = 0; ks < DP / 16; ++ks) {
+        const int at = ks * 16 + half * 8;
+        if constexpr (RAGGED) {
+            out[ks] = __builtin_bit_cast(typename Vec<T>::v8, load8(p, at, dim, valid));
+        } else {
+            uint4 r = make_uint4(0, 0, 0, 0);
+            if (valid && at < dim) r = __builtin_bit_cast(uint4, *reinterpret_cast<const Pack8<T>*>(p + at));
+            out[ks] = __builtin_bit_cast(typename Vec<T>::v8, r);
+        }
+    }
+}
+
 // Stores a transposed accumulator (lane = row of the output) times f to the row at `out`.
-template <class T, int DP>
+template <class T, int DP, bool RAGGED>
 __device__ __forceinline__ void store_row(T* out, int dim, const f32x16* acc, float f, int half, bool valid) {
 #pragma unroll
     for (int db = 0; db < DP / 32; ++db) {
@@ -117,7 +143,11 @@ __device__ __forceinline__ void store_row(T* out, int dim, const f32x16* acc, fl
         for (int j = 0; j < 2; ++j) {
             const Pack8<T> p = gather8<T>(acc[db], j, f);   // every lane takes part in the exchange
             const int c = db * 32 + j * 16 + half * 8;
-            if (valid) store8(out + c, p, dim - c);
+            if constexpr (RAGGED) {
+                if (valid) store8(out + c, p, dim - c);
+            } else {
+                if (valid && c < dim) *reinterpret_cast<Pack8<T>*>(out + c) = p;
+            }
         }
     }
 }
@@ -151,7 +181,7 @@ __device__ __forceinline__ int64_t stat_at(const CrossDev& d, int b, RowAt r) {
 // ------------------------------------------------------------------ forward
 // KW = 1: four waves of 32 rows share tiles of 64 keys. KW = 4 (at most 32 rows): the four waves
 // take 32 keys each of a 128-key tile for the same rows and are joined at the end.
-template <class T, int DP, int KW, bool MASKED>
+template <class T, int DP, int KW, bool MASKED, bool RAGGED>
 __global__ __launch_bounds__(kThreads, 2) void k_cross_fwd(CrossDev d) {
     constexpr int KEYS = KW == 1 ? 64 : 128, ROWS = KW == 1 ? 128 : 32, NT = KW == 1 ? 2 : 1;
     typedef typename Vec<T>::v8 v8;
@@ -175,9 +205,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_fwd(CrossDev d) {
 
     const T* qp = static_cast<const T*>(d.q) + b * d.qs[0] + ra.token * d.qs[1] + ra.head * d.qs[2];
     v8 q[DP / 16];
-#pragma unroll
-    for (int ks = 0; ks < DP / 16; ++ks)
-        q[ks] = __builtin_bit_cast(v8, load8(qp + ks * 16 + half * 8, valid ? d.dim - ks * 16 - half * 8 : 0));
+    load_row<T, DP, RAGGED>(q, qp, d.dim, half, valid);
 
     const int klen = sample_keys(d, b);
     const int kbeg = split * d.split_keys;
@@ -192,7 +220,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_fwd(CrossDev d) {
     for (int i = 0; i < DP / 32; ++i) acc[i] = f32x16{};
     float m = -INFINITY, l = 0.0f;
 
-    KvStage<T, DP, KEYS, MASKED> st;
+    KvStage<T, DP, KEYS, MASKED, RAGGED> st(d);
     if (kbeg < kend) st.load(d, kb, vb, b, kbeg, kend);
     for (int k0 = kbeg; k0 < kend; k0 += KEYS) {
         __syncthreads();
@@ -266,7 +294,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_fwd(CrossDev d) {
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;      // no key seen: acc is 0
         if (d.splits == 1) {
             T* op = static_cast<T*>(d.o) + b * d.os[0] + ra.token * d.os[1] + ra.head * d.os[2];
-            store_row<T, DP>(op, d.dim, acc, inv, half, valid);
+            store_row<T, DP, RAGGED>(op, d.dim, acc, inv, half, valid);
             if (d.stats && valid && half == 0) {
                 float* sp = d.stats + stat_at(d, b, ra) * 2;
                 sp[0] = m_nat;
@@ -372,8 +400,8 @@ __global__ __launch_bounds__(kThreads) void k_cross_delta(CrossDev d) {
     // Tokens outermost, as the tensors usually lie.
     const int h = (int)(at % d.q_heads);
     const int64_t bt = at / d.q_heads, t = bt % d.q_len, b = bt / d.q_len;
-    const Pack8<T> po = load8(static_cast<const T*>(d.o) + b * d.os[0] + t * d.os[1] + h * d.os[2] + c, d.dim - c);
-    const Pack8<T> pd = load8(static_cast<const T*>(d.d_o) + b * d.dos[0] + t * d.dos[1] + h * d.dos[2] + c, d.dim - c);
+    const Pack8<T> po = load8(static_cast<const T*>(d.o) + b * d.os[0] + t * d.os[1] + h * d.os[2], c, d.dim);
+    const Pack8<T> pd = load8(static_cast<const T*>(d.d_o) + b * d.dos[0] + t * d.dos[1] + h * d.dos[2], c, d.dim);
     float s = 0.0f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) s += (float)po.v[e] * (float)pd.v[e];
@@ -398,7 +426,7 @@ __device__ __forceinline__ float weight(float s, float scale, float f, float bia
 }
 
 // dq: the forward pass's tiling; a lane owns a row, K and V tiles pass by.
-template <class T, int DP, bool MASKED>
+template <class T, int DP, bool MASKED, bool RAGGED>
 __global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
     constexpr int KEYS = 64, ROWS = 128;
     typedef typename Vec<T>::v8 v8;
@@ -422,12 +450,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
     const T* qp = static_cast<const T*>(d.q) + b * d.qs[0] + ra.token * d.qs[1] + ra.head * d.qs[2];
     const T* dp = static_cast<const T*>(d.d_o) + b * d.dos[0] + ra.token * d.dos[1] + ra.head * d.dos[2];
     v8 q[DP / 16], g[DP / 16];
-#pragma unroll
-    for (int ks = 0; ks < DP / 16; ++ks) {
-        const int n = valid ? d.dim - ks * 16 - half * 8 : 0;
-        q[ks] = __builtin_bit_cast(v8, load8(qp + ks * 16 + half * 8, n));
-        g[ks] = __builtin_bit_cast(v8, load8(dp + ks * 16 + half * 8, n));
-    }
+    load_row<T, DP, RAGGED>(q, qp, d.dim, half, valid);
+    load_row<T, DP, RAGGED>(g, dp, d.dim, half, valid);
     float hi, lo;
     row_stats<MASKED>(d, sat, hi, lo);
     const float delta = d.delta[sat], f = d.scale * kLog2e;
@@ -441,7 +465,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i) acc[i] = f32x16{};
 
-    KvStage<T, DP, KEYS, MASKED> st;
+    KvStage<T, DP, KEYS, MASKED, RAGGED> st(d);
     if (kbeg < kend) st.load(d, kb, vb, b, kbeg, kend);
     for (int k0 = kbeg; k0 < kend; k0 += KEYS) {
         __syncthreads();
@@ -474,7 +498,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
     }
     if (d.splits == 1) {
         T* out = static_cast<T*>(d.dq) + b * d.dqs[0] + ra.token * d.dqs[1] + ra.head * d.dqs[2];
-        store_row<T, DP>(out, d.dim, acc, d.scale, half, valid);
+        store_row<T, DP, RAGGED>(out, d.dim, acc, d.scale, half, valid);
     } else if (valid) {
         const int64_t at = ((int64_t)split * d.batch * d.kv_heads + bh) * d.rows + row;
         store_row_f32<DP>(d.part + at * d.dim, d.dim, acc, half);
@@ -482,7 +506,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
 }
 
 // dk, dv: a wave owns 32 keys (K and V in registers), tiles of 32 rows of q and do pass by.
-template <class T, int DP, bool MASKED>
+template <class T, int DP, bool MASKED, bool RAGGED>
 __global__ __launch_bounds__(kThreads, 1) void k_cross_dkv(CrossDev d) {
     constexpr int KEYS = 128, ROWS = 32;
     typedef typename Vec<T>::v8 v8;
@@ -509,38 +533,30 @@ __global__ __launch_bounds__(kThreads, 1) void k_cross_dkv(CrossDev d) {
     const T* kp = static_cast<const T*>(d.k) + b * d.ks[0] + key * d.ks[1] + hk * d.ks[2];
     const T* vp = static_cast<const T*>(d.v) + b * d.vs[0] + key * d.vs[1] + hk * d.vs[2];
     v8 kr[DP / 16], vr[DP / 16];
-#pragma unroll
-    for (int ks = 0; ks < DP / 16; ++ks) {
-        const int n = seen ? d.dim - ks * 16 - half * 8 : 0;
-        kr[ks] = __builtin_bit_cast(v8, load8(kp + ks * 16 + half * 8, n));
-        vr[ks] = __builtin_bit_cast(v8, load8(vp + ks * 16 + half * 8, n));
-    }
+    load_row<T, DP, RAGGED>(kr, kp, d.dim, half, seen);
+    load_row<T, DP, RAGGED>(vr, vp, d.dim, half, seen);
     f32x16 ak[DP / 32], av[DP / 32];
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i) ak[i] = av[i] = f32x16{};
     const float f = d.scale * kLog2e;
 
-    const int rbeg = split * d.split_rows;
-    const int rend = tile * KEYS >= klen ? rbeg : d.rows < rbeg + d.split_rows ? d.rows : rbeg + d.split_rows;
-    const T* qb = static_cast<const T*>(d.q) + b * d.qs[0];
-    const T* gb = static_cast<const T*>(d.d_o) + b * d.dos[0];
-    Stage<T, DP, ROWS> sq, sg;
+    // Tiles of 32 tokens of one query head; the heads of the group one after the other.
+    const int head_tiles = (d.q_len + ROWS - 1) / ROWS;
+    const int tbeg = split * d.split_tiles;
+    int tend = d.group * head_tiles;
+    if (tend > tbeg + d.split_tiles) tend = tbeg + d.split_tiles;
+    if (tile * KEYS >= klen) tend = tbeg;
+    const T* qb = static_cast<const T*>(d.q) + b * d.qs[0] + (int64_t)hk * d.group * d.qs[2];
+    const T* gb = static_cast<const T*>(d.d_o) + b * d.dos[0] + (int64_t)hk * d.group * d.dos[2];
+    Stage<T, DP, ROWS, RAGGED> sq(d.dim, d.qs[1]), sg(d.dim, d.dos[1]);
     float s_hi = 0.0f, s_lo = 0.0f, s_delta = 0.0f;
-    auto load = [&](int r0) {
-        sq.load(d.dim, [&](int r) -> const T* {
-            if (r0 + r >= rend) return nullptr;
-            const RowAt a = row_at(d, hk, r0 + r);
-            return qb + a.token * d.qs[1] + a.head * d.qs[2];
-        });
-        sg.load(d.dim, [&](int r) -> const T* {
-            if (r0 + r >= rend) return nullptr;
-            const RowAt a = row_at(d, hk, r0 + r);
-            return gb + a.token * d.dos[1] + a.head * d.dos[2];
-        });
+    auto load = [&](int t) {
+        const int g = t / head_tiles, r0 = (t - g * head_tiles) * ROWS, rows = d.q_len - r0;
+        sq.load(qb + g * d.qs[2] + r0 * d.qs[1], d.qs[1], rows, d.dim);
+        sg.load(gb + g * d.dos[2] + r0 * d.dos[1], d.dos[1], rows, d.dim);
         if (threadIdx.x < ROWS) {
-            const int r = r0 + threadIdx.x;
-            if (r < rend) {
-                const int64_t at = stat_at(d, b, row_at(d, hk, r));
+            if ((int)threadIdx.x < rows) {
+                const int64_t at = stat_at(d, b, {r0 + (int)threadIdx.x, hk * d.group + g});
                 row_stats<MASKED>(d, at, s_hi, s_lo);
                 s_delta = d.delta[at];
             } else {
@@ -550,8 +566,8 @@ __global__ __launch_bounds__(kThreads, 1) void k_cross_dkv(CrossDev d) {
             }
         }
     };
-    if (rbeg < rend) load(rbeg);
-    for (int r0 = rbeg; r0 < rend; r0 += ROWS) {
+    if (tbeg < tend) load(tbeg);
+    for (int it = tbeg; it < tend; ++it) {
         __syncthreads();
         sq.store(qt);
         sg.store(gt);
@@ -561,7 +577,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_cross_dkv(CrossDev d) {
             stat[2][threadIdx.x] = s_delta;
         }
         __syncthreads();
-        if (r0 + ROWS < rend) load(r0 + ROWS);
+        if (it + 1 < tend) load(it + 1);
         f32x16 s = f32x16{}, e = f32x16{};
 #pragma unroll
         for (int ks = 0; ks < DP / 16; ++ks) {
@@ -590,8 +606,8 @@ __global__ __launch_bounds__(kThreads, 1) void k_cross_dkv(CrossDev d) {
     if (d.row_splits == 1) {
         T* ok = static_cast<T*>(d.dk) + b * d.dks[0] + key * d.dks[1] + hk * d.dks[2];
         T* ov = static_cast<T*>(d.dv) + b * d.dvs[0] + key * d.dvs[1] + hk * d.dvs[2];
-        store_row<T, DP>(ok, d.dim, ak, d.scale, half, valid);
-        store_row<T, DP>(ov, d.dim, av, 1.0f, half, valid);
+        store_row<T, DP, RAGGED>(ok, d.dim, ak, d.scale, half, valid);
+        store_row<T, DP, RAGGED>(ov, d.dim, av, 1.0f, half, valid);
     } else if (valid) {
         const int64_t at = ((int64_t)split * d.batch * d.kv_heads + bh) * d.kv_len + key;
         store_row_f32<DP>(d.part_dk + at * d.dim, d.dim, ak, half);
@@ -628,18 +644,18 @@ bool masked(const CrossDev& d) { return d.mask_kind != PA_MASK_NONE || !(d.scale
 
 unsigned blocks_for(int64_t n) { return (unsigned)((n + kThreads - 1) / kThreads); }
 
-template <class T, int DP, bool MASKED>
+template <class T, int DP, bool MASKED, bool RAGGED>
 hipError_t forward(const CrossDev& d, hipStream_t st) {
     const int64_t bh = (int64_t)d.batch * d.kv_heads;
-    if (d.rows <= 32) k_cross_fwd<T, DP, 4, MASKED><<<(unsigned)(d.splits * bh), kThreads, 0, st>>>(d);
-    else k_cross_fwd<T, DP, 1, MASKED><<<(unsigned)((d.rows + 127) / 128 * d.splits * bh), kThreads, 0, st>>>(d);
+    if (d.rows <= 32) k_cross_fwd<T, DP, 4, MASKED, RAGGED><<<(unsigned)(d.splits * bh), kThreads, 0, st>>>(d);
+    else k_cross_fwd<T, DP, 1, MASKED, RAGGED><<<(unsigned)((d.rows + 127) / 128 * d.splits * bh), kThreads, 0, st>>>(d);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || d.splits == 1) return e;
     k_cross_join<T><<<(unsigned)((bh * d.rows + 3) / 4), kThreads, 0, st>>>(d);
     return hipGetLastError();
 }
 
-template <class T, int DP, bool MASKED>
+template <class T, int DP, bool MASKED, bool RAGGED>
 hipError_t backward(const CrossDev& d, hipStream_t st) {
     const int64_t bh = (int64_t)d.batch * d.kv_heads;
     hipError_t e = hipSuccess;
@@ -648,7 +664,7 @@ hipError_t backward(const CrossDev& d, hipStream_t st) {
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (d.dq && d.rows > 0) {
-        k_cross_dq<T, DP, MASKED><<<(unsigned)((d.rows + 127) / 128 * d.splits * bh), kThreads, 0, st>>>(d);
+        k_cross_dq<T, DP, MASKED, RAGGED><<<(unsigned)((d.rows + 127) / 128 * d.splits * bh), kThreads, 0, st>>>(d);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         if (d.splits > 1) {
             k_cross_sum<T, 0><<<blocks_for(bh * d.rows * d.dim), kThreads, 0, st>>>(d);
@@ -656,7 +672,7 @@ hipError_t backward(const CrossDev& d, hipStream_t st) {
         }
     }
     if (d.dk && d.kv_len > 0) {
-        k_cross_dkv<T, DP, MASKED><<<(unsigned)((d.kv_len + 127) / 128 * d.row_splits * bh), kThreads, 0, st>>>(d);
+        k_cross_dkv<T, DP, MASKED, RAGGED><<<(unsigned)((d.kv_len + 127) / 128 * d.row_splits * bh), kThreads, 0, st>>>(d);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         if (d.row_splits > 1) {
             k_cross_sum<T, 1><<<blocks_for(bh * d.kv_len * d.dim), kThreads, 0, st>>>(d);
@@ -668,16 +684,23 @@ hipError_t backward(const CrossDev& d, hipStream_t st) {
     return e;
 }
 
+bool ragged(const CrossDev& d) {
+    for (const int64_t* p : {d.qs, d.ks, d.vs, d.os, d.dos, d.dqs, d.dks, d.dvs})
+        if (p[1] >= kBufferStride) return true;
+    return d.dim % 8 != 0;
+}
+
 template <class F>
 hipError_t dispatch(const CrossDev& d, int dtype, F f) {
-    const bool wide = d.dim > 64, m = masked(d);
-    auto with = [&](auto t) {
-        if (wide) return m ? f(t, std::integral_constant<int, 128>{}, std::true_type{})
-                           : f(t, std::integral_constant<int, 128>{}, std::false_type{});
-        return m ? f(t, std::integral_constant<int, 64>{}, std::true_type{})
-                 : f(t, std::integral_constant<int, 64>{}, std::false_type{});
+    const bool m = masked(d), r = ragged(d);
+    auto with = [&](auto t, auto dp) {
+        if (m) return r ? f(t, dp, std::true_type{}, std::true_type{}) : f(t, dp, std::true_type{}, std::false_type{});
+        return r ? f(t, dp, std::false_type{}, std::true_type{}) : f(t, dp, std::false_type{}, std::false_type{});
     };
-    return dtype == PA_BF16 ? with((__bf16)0) : with((_Float16)0);
+    auto wide = [&](auto t) {
+        return d.dim > 64 ? with(t, std::integral_constant<int, 128>{}) : with(t, std::integral_constant<int, 64>{});
+    };
+    return dtype == PA_BF16 ? wide((__bf16)0) : wide((_Float16)0);
 }
 
 }  // namespace
@@ -699,18 +722,18 @@ void cross_plan(CrossDev& d, bool backward_pass) {
     const int64_t bh = (int64_t)d.batch * d.kv_heads;
     if (!backward_pass && d.rows <= 32) split(bh, d.kv_len, 128, d.splits, d.split_keys);
     else split((d.rows + 127) / 128 * bh, d.kv_len, 64, d.splits, d.split_keys);
-    split((d.kv_len + 127) / 128 * bh, d.rows, 32, d.row_splits, d.split_rows);
+    split((d.kv_len + 127) / 128 * bh, (int64_t)d.group * ((d.q_len + 31) / 32), 1, d.row_splits, d.split_tiles);
 }
 
 hipError_t cross_forward(const CrossDev& d, int dtype, hipStream_t st) {
-    return dispatch(d, dtype, [&](auto t, auto dp, auto m) {
-        return forward<decltype(t), decltype(dp)::value, decltype(m)::value>(d, st);
+    return dispatch(d, dtype, [&](auto t, auto dp, auto m, auto r) {
+        return forward<decltype(t), decltype(dp)::value, decltype(m)::value, decltype(r)::value>(d, st);
     });
 }
 
 hipError_t cross_backward(const CrossDev& d, int dtype, hipStream_t st) {
-    return dispatch(d, dtype, [&](auto t, auto dp, auto m) {
-        return backward<decltype(t), decltype(dp)::value, decltype(m)::value>(d, st);
+    return dispatch(d, dtype, [&](auto t, auto dp, auto m, auto r) {
+        return backward<decltype(t), decltype(dp)::value, decltype(m)::value, decltype(r)::value>(d, st);
     });
 }
 

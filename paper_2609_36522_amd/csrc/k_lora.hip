@@ -64,11 +64,11 @@ __global__ __launch_bounds__(kThreads) void k_lora_down(LoraDev d) {
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks) {
                 const int k = k0 + ks * 16 + half * 8;
-                const v8 xv = __builtin_bit_cast(v8, load8(x + k, valid ? K - k : 0));
+                const v8 xv = __builtin_bit_cast(v8, load8(x, k, K, valid));
 #pragma unroll
                 for (int n = 0; n < NR; ++n) {
                     const int r = n * 32 + (lane & 31);
-                    const v8 av = __builtin_bit_cast(v8, load8(a + (int64_t)r * K + k, r < d.rank ? K - k : 0));
+                    const v8 av = __builtin_bit_cast(v8, load8(a + (int64_t)r * K, k, K, r < d.rank));
                     acc[n] = mma(av, xv, acc[n]);
                 }
             }
@@ -108,12 +108,12 @@ __device__ __forceinline__ void add_adapters(const LoraDev& d, int f0, int r0, i
             for (int j = 0; j < NX; ++j) {
                 const int row = r0 + j * 32 + (lane & 31);
                 const bool mine = row >= beg && row < end;
-                tv[j] = __builtin_bit_cast(v8, load8(static_cast<const T*>(d.t) + (int64_t)row * d.rank_pad + k, mine ? 8 : 0));
+                tv[j] = __builtin_bit_cast(v8, load8(static_cast<const T*>(d.t) + (int64_t)row * d.rank_pad, k, d.rank_pad, mine));
             }
 #pragma unroll
             for (int m = 0; m < NM; ++m) {
                 const int f = f0 + m * 32 + (lane & 31);
-                const v8 bv = __builtin_bit_cast(v8, load8(b + (int64_t)f * d.rank + k, f < d.out ? d.rank - k : 0));
+                const v8 bv = __builtin_bit_cast(v8, load8(b + (int64_t)f * d.rank, k, d.rank, f < d.out));
 #pragma unroll
                 for (int j = 0; j < NX; ++j) acc[m][j] = mma(bv, tv[j], acc[m][j]);
             }
@@ -169,8 +169,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_lora_tile(LoraDev d) {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const int c = threadIdx.x + i * kThreads, row = c >> 3, k = k0 + (c & 7) * 8;
-            pw[i] = load8(static_cast<const T*>(d.w) + (int64_t)(f0 + row) * d.w_stride + k, f0 + row < d.out ? K - k : 0);
-            px[i] = load8(static_cast<const T*>(d.x) + (int64_t)(r0 + row) * d.x_stride + k, r0 + row < d.rows ? K - k : 0);
+            pw[i] = load8(static_cast<const T*>(d.w) + (int64_t)(f0 + row) * d.w_stride, k, K, f0 + row < d.out);
+            px[i] = load8(static_cast<const T*>(d.x) + (int64_t)(r0 + row) * d.x_stride, k, K, r0 + row < d.rows);
         }
     };
     f32x16 acc[2][2];
@@ -225,8 +225,8 @@ __global__ __launch_bounds__(kThreads) void k_lora_rows(LoraDev d) {
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) {
             const int k = k0 + ks * 16 + half * 8;
-            const v8 wv = __builtin_bit_cast(v8, load8(wp + k, f < d.out ? K - k : 0));
-            const v8 xv = __builtin_bit_cast(v8, load8(xp + k, row < d.rows ? K - k : 0));
+            const v8 wv = __builtin_bit_cast(v8, load8(wp, k, K, f < d.out));
+            const v8 xv = __builtin_bit_cast(v8, load8(xp, k, K, row < d.rows));
             acc[0][0] = mma(wv, xv, acc[0][0]);
         }
     }

@@ -46,7 +46,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_fwd(NormDev d) {
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int col = (c * TPR + t) * 8;
-        const Pack8<T> p = load8(x + col, N - col);
+        const Pack8<T> p = load8(x, col, N);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             v[c][i] = (float)p.v[i];
@@ -77,8 +77,8 @@ __global__ __launch_bounds__(kThreads) void k_norm_fwd(NormDev d) {
         const int col = (c * TPR + t) * 8, n = N - col;
         if (n <= 0) continue;
         Pack8<W> pw, pb;
-        if (w) pw = load8(w + col, n);
-        if (b) pb = load8(b + col, n);
+        if (w) pw = load8(w, col, N);
+        if (b) pb = load8(b, col, N);
         Pack8<T> o;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -104,14 +104,14 @@ __global__ __launch_bounds__(kThreads) void k_norm_fwd_long(NormDev d) {
     const float n_f = (float)N;
     float s = 0.0f;
     for (int col = threadIdx.x * 8; col < N; col += kThreads * 8) {
-        const Pack8<T> p = load8(x + col, N - col);
+        const Pack8<T> p = load8(x, col, N);
 #pragma unroll
         for (int i = 0; i < 8; ++i) s += (float)p.v[i];
     }
     const float mean = row_sum<4>(s, red[0]) / n_f;
     float q = 0.0f;
     for (int col = threadIdx.x * 8; col < N; col += kThreads * 8) {
-        const Pack8<T> p = load8(x + col, N - col);
+        const Pack8<T> p = load8(x, col, N);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float e = (float)p.v[i] - mean;
@@ -125,10 +125,10 @@ __global__ __launch_bounds__(kThreads) void k_norm_fwd_long(NormDev d) {
     }
     for (int col = threadIdx.x * 8; col < N; col += kThreads * 8) {
         const int n = N - col;
-        const Pack8<T> p = load8(x + col, n);
+        const Pack8<T> p = load8(x, col, N);
         Pack8<W> pw, pb;
-        if (w) pw = load8(w + col, n);
-        if (b) pb = load8(b + col, n);
+        if (w) pw = load8(w, col, N);
+        if (b) pb = load8(b, col, N);
         Pack8<T> o;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -163,15 +163,15 @@ __global__ __launch_bounds__(kThreads) void k_norm_bwd(NormDev d) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * TPR + t) * 8;
-            px[c] = load8(x + col, N - col);
-            pd[c] = load8(dy + col, N - col);
+            px[c] = load8(x, col, N);
+            pd[c] = load8(dy, col, N);
         }
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * TPR + t) * 8;
             Pack8<W> pw;
-            if (w) pw = load8(w + col, N - col);
+            if (w) pw = load8(w, col, N);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float dyi = (float)pd[c].v[i];          // 0 past the row
@@ -192,7 +192,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_bwd(NormDev d) {
             const int col = (c * TPR + t) * 8, n = N - col;
             if (n <= 0) continue;
             Pack8<W> pw;
-            if (w) pw = load8(w + col, n);
+            if (w) pw = load8(w, col, N);
             Pack8<T> o;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -249,9 +249,9 @@ __global__ __launch_bounds__(kThreads) void k_norm_bwd_long_dx(NormDev d) {
     const float mean = d.mean[row], rstd = d.rstd[row], n_f = (float)N;
     float s1 = 0.0f, s2 = 0.0f;
     for (int col = threadIdx.x * 8; col < N; col += kThreads * 8) {
-        const Pack8<T> px = load8(x + col, N - col), pd = load8(dy + col, N - col);
+        const Pack8<T> px = load8(x, col, N), pd = load8(dy, col, N);
         Pack8<W> pw;
-        if (w) pw = load8(w + col, N - col);
+        if (w) pw = load8(w, col, N);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float gi = (float)pd.v[i] * (w ? (float)pw.v[i] : 1.0f);
@@ -263,9 +263,9 @@ __global__ __launch_bounds__(kThreads) void k_norm_bwd_long_dx(NormDev d) {
     s2 = row_sum<4>(s2, red[1]) / n_f;
     for (int col = threadIdx.x * 8; col < N; col += kThreads * 8) {
         const int n = N - col;
-        const Pack8<T> px = load8(x + col, n), pd = load8(dy + col, n);
+        const Pack8<T> px = load8(x, col, N), pd = load8(dy, col, N);
         Pack8<W> pw;
-        if (w) pw = load8(w + col, n);
+        if (w) pw = load8(w, col, N);
         Pack8<T> o;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -285,8 +285,8 @@ __global__ __launch_bounds__(kThreads) void k_norm_bwd_long_dw(NormDev d) {
     float aw[8] = {}, ab[8] = {};
     for (int64_t row = blockIdx.x; row < d.rows; row += gridDim.x) {
         const float mean = d.mean[row], rstd = d.rstd[row];
-        const Pack8<T> px = load8(static_cast<const T*>(d.x) + row * d.x_stride + col, n);
-        const Pack8<T> pd = load8(static_cast<const T*>(d.dy) + row * d.y_stride + col, n);
+        const Pack8<T> px = load8(static_cast<const T*>(d.x) + row * d.x_stride, col, N);
+        const Pack8<T> pd = load8(static_cast<const T*>(d.dy) + row * d.y_stride, col, N);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float dyi = (float)pd.v[i];

@@ -30,7 +30,7 @@ struct CrossDev {
     int q_len, kv_len, dim;
     int rows;                        // q_len * group: rows that share a kv head, row = token * group + head in group
     int splits, split_keys;          // forward, dq: key ranges of split_keys keys (a multiple of the key tile)
-    int row_splits, split_rows;      // dk, dv: row ranges of split_rows rows (a multiple of the row tile)
+    int row_splits, split_tiles;     // dk, dv: ranges of split_tiles tiles of 32 tokens of a query head
     float scale;
     int64_t mask_stride;
     int64_t qs[3], ks[3], vs[3], os[3], dos[3], dqs[3], dks[3], dvs[3];   // batch, token, head

@@ -20,15 +20,43 @@ struct __attribute__((packed, aligned(sizeof(T)))) Pack8 {
     T v[8];
 };
 
-// n of the eight elements at p exist; the others read as zero.
+// r moved down by n elements (0 .. 7), zeros behind.
 template <class T>
-__device__ __forceinline__ Pack8<T> load8(const T* p, int n) {
-    Pack8<T> r;
-    if (n >= 8) {
-        r = *reinterpret_cast<const Pack8<T>*>(p);
+__device__ __forceinline__ Pack8<T> shift8(Pack8<T> r, int n) {
+    if constexpr (sizeof(T) == 2) {
+        typedef unsigned long long u64;
+        struct Two { u64 lo, hi; };
+        Two t = __builtin_bit_cast(Two, r);
+        if (n & 4) t = {t.hi, 0};
+        const int b = (n & 3) * 16;
+        t.lo = (t.lo >> b) | ((t.hi << 1) << (63 - b));
+        t.hi >>= b;
+        return __builtin_bit_cast(Pack8<T>, t);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) r.v[i] = i < n ? p[i] : (T)0.0f;
+        for (int k = 4; k >= 1; k >>= 1)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (n & k) r.v[i] = i + k < 8 ? r.v[i + k < 8 ? i + k : 7] : (T)0.0f;
+        return r;
+    }
+}
+
+// Elements at .. at + 7 of a row of len elements, zeros past its end and in an invalid row. A piece
+// that reaches past the end is read as the row's last eight elements and moved down, so that no
+// element outside the row is touched and the load stays one access. len is the same in all lanes.
+template <class T>
+__device__ __forceinline__ Pack8<T> load8(const T* row, int at, int len, bool valid = true) {
+    Pack8<T> r;
+    const int n = valid ? len - at : 0;
+    if (len >= 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.v[i] = (T)0.0f;
+        if (n > 0) r = *reinterpret_cast<const Pack8<T>*>(row + (n >= 8 ? at : len - 8));
+        if (len & 7) r = shift8(r, n > 0 && n < 8 ? 8 - n : 0);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.v[i] = i < n ? row[at + i] : (T)0.0f;
     }
     return r;
 }
