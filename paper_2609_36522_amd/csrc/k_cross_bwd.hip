@@ -1,0 +1,330 @@
+// Cross attention, backward, for gfx950 (layout and products: pa_cross.h).
+//
+// dq tiles the work as the forward pass does (a block owns rows, keys pass by: three products a tile),
+// dk and dv the other way round (a wave owns 32 keys, rows pass by: four products a tile). The scores are
+// computed in both; no atomics, so results do not depend on the order of blocks.
+#include "pa_cross.h"
+
+namespace pa {
+
+namespace {
+
+// delta = sum of do * o over a head: 16 lanes per row of [batch][q_heads][q_len].
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_cross_delta(CrossDev d) {
+    const int64_t n = (int64_t)d.batch * d.q_heads * d.q_len;
+    const int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+    const int64_t at = i < n ? i : n - 1;
+    const int c = (threadIdx.x & 15) * 8;
+    // Tokens outermost, as the tensors usually lie.
+    const int h = (int)(at % d.q_heads);
+    const int64_t bt = at / d.q_heads, t = bt % d.q_len, b = bt / d.q_len;
+    const Pack8<T> po = load8(static_cast<const T*>(d.o) + b * d.os[0] + t * d.os[1] + h * d.os[2], c, d.dim);
+    const Pack8<T> pd = load8(static_cast<const T*>(d.d_o) + b * d.dos[0] + t * d.dos[1] + h * d.dos[2], c, d.dim);
+    float s = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s += (float)po.v[e] * (float)pd.v[e];
+#pragma unroll
+    for (int off = 8; off >= 1; off >>= 1) s += __shfl_xor(s, off, 64);
+    if (i < n && (threadIdx.x & 15) == 0) d.delta[(b * d.q_heads + h) * d.q_len + t] = s;
+}
+
+// A row's statistics as the backward pass uses them: without a mask hi = log2 of the sum of all
+// weights (lo unused), with one the maximum and the logarithm apart. A row that sees no key has
+// weights 0 whatever its scores.
+template <bool MASKED>
+__device__ __forceinline__ void row_stats(const CrossDev& d, int64_t at, float& hi, float& lo) {
+    const float m = d.stats[at * 2], ll = d.stats[at * 2 + 1];
+    const bool empty = ll == -INFINITY;
+    hi = MASKED ? (empty ? 0.0f : m) : (empty ? INFINITY : (m + ll) * kLog2e);
+    lo = empty ? INFINITY : ll;
+}
+template <bool MASKED>
+__device__ __forceinline__ float weight(float s, float scale, float f, float bias, float hi, float lo) {
+    return __builtin_amdgcn_exp2f(MASKED ? ((fmaf(s, scale, bias) - hi) - lo) * kLog2e : fmaf(s, f, -hi));
+}
+
+// dq: the forward pass's tiling; a lane owns a row, K and V tiles pass by. Writes delta for the rows of its
+// tile on the way (the first key range does).
+template <class T, int KS, bool MASKED, bool RAGGED>
+__global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
+    constexpr int DP = KS <= 4 ? 64 : 128, DB = (KS + 1) / 2, KEYS = 64, ROWS = 128;
+    typedef typename Vec<T>::v8 v8;
+    __shared__ __align__(16) T tiles[2][2][KEYS * DP];
+    __shared__ __align__(16) float bias[2][MASKED ? KEYS : 4];
+
+    const int row_tiles = (d.rows + ROWS - 1) / ROWS;
+    int id = xcd_order(blockIdx.x, gridDim.x);
+    const int tile = id % row_tiles;
+    id /= row_tiles;
+    const int split = id % d.splits, bh = id / d.splits;
+    const int b = bh / d.kv_heads, hk = bh - b * d.kv_heads;
+    const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6;
+    const int row = tile * ROWS + w * 32 + (lane & 31);
+    const bool valid = row < d.rows;
+    const RowAt ra = row_at(d, hk, valid ? row : 0);
+    const int64_t sat = stat_at(d, b, ra);
+
+    const int klen = sample_keys(d, b);
+    const int kbeg = split * d.split_keys;
+    const int kend = klen < kbeg + d.split_keys ? klen : kbeg + d.split_keys;
+    const T* kb = static_cast<const T*>(d.k) + b * d.ks[0] + hk * d.ks[2];
+    const T* vb = static_cast<const T*>(d.v) + b * d.vs[0] + hk * d.vs[2];
+    KvStage<T, DP, KEYS, MASKED, kKvKind<MASKED, RAGGED>> st(d);
+    if (kbeg < kend) st.load(d, kb, vb, b, kbeg, kend, tiles[0][0], tiles[0][1]);
+
+    v8 q[KS], g[KS];
+    load_row<T, KS, RAGGED>(g, static_cast<const T*>(d.d_o) + b * d.dos[0] + ra.token * d.dos[1] + ra.head * d.dos[2], d.dim, half, valid);
+    load_row<T, KS, RAGGED>(q, static_cast<const T*>(d.o) + b * d.os[0] + ra.token * d.os[1] + ra.head * d.os[2], d.dim, half, valid);
+    float delta = 0.0f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) delta = fmaf((float)g[ks][i], (float)q[ks][i], delta);
+    delta += __shfl_xor(delta, 32, 64);
+    if (split == 0 && valid && half == 0) d.delta[sat] = delta;
+    load_row<T, KS, RAGGED>(q, static_cast<const T*>(d.q) + b * d.qs[0] + ra.token * d.qs[1] + ra.head * d.qs[2], d.dim, half, valid);
+    float hi, lo;
+    row_stats<MASKED>(d, sat, hi, lo);
+    const float f = d.scale * kLog2e;
+    f32x16 acc[DB];
+#pragma unroll
+    for (int i = 0; i < DB; ++i) acc[i] = f32x16{};
+
+    if (kbeg < kend) st.arrive(tiles[0][0], tiles[0][1], bias[0]);
+    __syncthreads();
+    int p = 0;
+    for (int k0 = kbeg; k0 < kend; k0 += KEYS, p ^= 1) {
+        const T* kt = tiles[p][0];
+        const T* vt = tiles[p][1];
+        if (k0 + KEYS < kend) st.load(d, kb, vb, b, k0 + KEYS, kend, tiles[p ^ 1][0], tiles[p ^ 1][1]);
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+            f32x16 s = f32x16{}, e = f32x16{};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                s = mma(read_rows<T, DP>(kt, nt * 32 + (lane & 31), ks, half), q[ks], s);
+                e = mma(read_rows<T, DP>(vt, nt * 32 + (lane & 31), ks, half), g[ks], e);
+            }
+            const bool border = !MASKED && k0 + nt * 32 + 32 > kend;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int key = nt * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
+                float x = weight<MASKED>(s[r], d.scale, f, MASKED ? bias[p][key] : 0.0f, hi, lo);
+                if (border && k0 + key >= kend) x = 0.0f;
+                s[r] = x * (e[r] - delta);
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const v8 ds = pack<T>(s, t);
+#pragma unroll
+                for (int db = 0; db < DB; ++db) acc[db] = mma(read_cols<T, DP>(kt, nt * 32 + t * 16, db, lane), ds, acc[db]);
+            }
+        }
+        if (k0 + KEYS < kend) st.arrive(tiles[p ^ 1][0], tiles[p ^ 1][1], bias[p ^ 1]);
+        __syncthreads();
+    }
+    if (d.splits == 1) {
+        T* out = static_cast<T*>(d.dq) + b * d.dqs[0] + ra.token * d.dqs[1] + ra.head * d.dqs[2];
+        store_row<T, DB, RAGGED>(out, d.dim, acc, d.scale, half, valid);
+    } else if (valid) {
+        const int64_t at = ((int64_t)split * d.batch * d.kv_heads + bh) * d.rows + row;
+        store_row_f32<DB>(d.part + at * d.dim, d.dim, acc, half);
+    }
+}
+
+// dk, dv: a wave owns 32 keys (K and V in registers), tiles of 32 tokens of one query head pass by, double
+// buffered; the heads of the group one after the other.
+template <class T, int KS, bool MASKED, bool RAGGED>
+__global__ __launch_bounds__(kThreads, KS <= 6 ? 2 : 1) void k_cross_dkv(CrossDev d) {
+    constexpr int DP = KS <= 4 ? 64 : 128, DB = (KS + 1) / 2, KEYS = 128, ROWS = 32;
+    constexpr int KIND = RAGGED ? kRagged : kDirect;
+    typedef typename Vec<T>::v8 v8;
+    __shared__ __align__(16) T tiles[2][2][ROWS * DP];       // [parity][q, do]
+    __shared__ __align__(16) float stat[2][3][ROWS];         // hi, lo, delta
+
+    const int key_tiles = (d.kv_len + KEYS - 1) / KEYS;
+    int id = xcd_order(blockIdx.x, gridDim.x);
+    const int tile = id % key_tiles;
+    id /= key_tiles;
+    const int split = id % d.row_splits, bh = id / d.row_splits;
+    const int b = bh / d.kv_heads, hk = bh - b * d.kv_heads;
+    const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6;
+    const int key = tile * KEYS + w * 32 + (lane & 31);
+    const int klen = sample_keys(d, b);
+
+    const int head_tiles = (d.q_len + ROWS - 1) / ROWS;
+    const int tbeg = split * d.split_tiles;
+    int tend = d.group * head_tiles;
+    if (tend > tbeg + d.split_tiles) tend = tbeg + d.split_tiles;
+    if (tile * KEYS >= klen) tend = tbeg;
+    const T* qb = static_cast<const T*>(d.q) + b * d.qs[0] + (int64_t)hk * d.group * d.qs[2];
+    const T* gb = static_cast<const T*>(d.d_o) + b * d.dos[0] + (int64_t)hk * d.group * d.dos[2];
+    Stage<T, DP, ROWS, KIND> sq(d.dim, d.qs[1]), sg(d.dim, d.dos[1]);
+    float s_hi = 0.0f, s_lo = 0.0f, s_delta = 0.0f;
+    auto load = [&](int it, int p) {
+        const int gh = it / head_tiles, r0 = (it - gh * head_tiles) * ROWS, rows = d.q_len - r0;
+        sq.load(qb + gh * d.qs[2] + r0 * d.qs[1], d.qs[1], rows, d.dim, tiles[p][0]);
+        sg.load(gb + gh * d.dos[2] + r0 * d.dos[1], d.dos[1], rows, d.dim, tiles[p][1]);
+        if (threadIdx.x < ROWS) {
+            if ((int)threadIdx.x < rows) {
+                const int64_t at = stat_at(d, b, {r0 + (int)threadIdx.x, hk * d.group + gh});
+                row_stats<MASKED>(d, at, s_hi, s_lo);
+                s_delta = d.delta[at];
+            } else {
+                s_hi = MASKED ? 0.0f : INFINITY;
+                s_lo = INFINITY;
+                s_delta = 0.0f;
+            }
+        }
+    };
+    auto arrive = [&](int p) {
+        sq.arrive(tiles[p][0]);
+        sg.arrive(tiles[p][1]);
+        if (threadIdx.x < ROWS) {
+            stat[p][0][threadIdx.x] = s_hi;
+            stat[p][1][threadIdx.x] = s_lo;
+            stat[p][2][threadIdx.x] = s_delta;
+        }
+    };
+    if (tbeg < tend) load(tbeg, 0);
+
+    bool seen = key < klen;
+    float bias = 0.0f;
+    if (MASKED && seen) {
+        bias = key_bias(d, b, key);
+        seen = bias != -INFINITY;
+    }
+    v8 kr[KS], vr[KS];
+    load_row<T, KS, RAGGED>(kr, static_cast<const T*>(d.k) + b * d.ks[0] + key * d.ks[1] + hk * d.ks[2], d.dim, half, seen);
+    load_row<T, KS, RAGGED>(vr, static_cast<const T*>(d.v) + b * d.vs[0] + key * d.vs[1] + hk * d.vs[2], d.dim, half, seen);
+    f32x16 ak[DB], av[DB];
+#pragma unroll
+    for (int i = 0; i < DB; ++i) ak[i] = av[i] = f32x16{};
+    const float f = d.scale * kLog2e;
+
+    if (tbeg < tend) arrive(0);
+    __syncthreads();
+    int p = 0;
+    for (int it = tbeg; it < tend; ++it, p ^= 1) {
+        if (it + 1 < tend) load(it + 1, p ^ 1);
+        const T* qt = tiles[p][0];
+        const T* gt = tiles[p][1];
+        f32x16 s = f32x16{}, e = f32x16{};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            s = mma(read_rows<T, DP>(qt, lane & 31, ks, half), kr[ks], s);
+            e = mma(read_rows<T, DP>(gt, lane & 31, ks, half), vr[ks], e);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int rr = 8 * (r >> 2) + 4 * half + (r & 3);
+            float x = weight<MASKED>(s[r], d.scale, f, bias, stat[p][0][rr], MASKED ? stat[p][1][rr] : 0.0f);
+            if (!seen) x = 0.0f;
+            s[r] = x;
+            e[r] = seen ? x * (e[r] - stat[p][2][rr]) : 0.0f;
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const v8 pw = pack<T>(s, t), ds = pack<T>(e, t);
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+                av[db] = mma(read_cols<T, DP>(gt, t * 16, db, lane), pw, av[db]);
+                ak[db] = mma(read_cols<T, DP>(qt, t * 16, db, lane), ds, ak[db]);
+            }
+        }
+        if (it + 1 < tend) arrive(p ^ 1);
+        __syncthreads();
+    }
+    const bool valid = key < d.kv_len;
+    if (d.row_splits == 1) {
+        T* ok = static_cast<T*>(d.dk) + b * d.dks[0] + key * d.dks[1] + hk * d.dks[2];
+        T* ov = static_cast<T*>(d.dv) + b * d.dvs[0] + key * d.dvs[1] + hk * d.dvs[2];
+        store_row<T, DB, RAGGED>(ok, d.dim, ak, d.scale, half, valid);
+        store_row<T, DB, RAGGED>(ov, d.dim, av, 1.0f, half, valid);
+    } else if (valid) {
+        const int64_t at = ((int64_t)split * d.batch * d.kv_heads + bh) * d.kv_len + key;
+        store_row_f32<DB>(d.part_dk + at * d.dim, d.dim, ak, half);
+        store_row_f32<DB>(d.part_dv + at * d.dim, d.dim, av, half);
+    }
+}
+
+// Sums of the key ranges' dq (KIND 0) or the row ranges' dk, dv (1, 2), in a fixed order.
+template <class T, int KIND>
+__global__ __launch_bounds__(kThreads) void k_cross_sum(CrossDev d) {
+    const int rows = KIND == 0 ? d.rows : d.kv_len, n_part = KIND == 0 ? d.splits : d.row_splits;
+    const int64_t n = (int64_t)d.batch * d.kv_heads * rows * d.dim;
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (i >= n) return;
+    const float* part = KIND == 0 ? d.part : KIND == 1 ? d.part_dk : d.part_dv;
+    float s = 0.0f;
+    for (int k = 0; k < n_part; ++k) s += part[k * n + i];
+    const int c = (int)(i % d.dim);
+    const int64_t r = i / d.dim, bh = r / rows, b = bh / d.kv_heads;
+    const int hk = (int)(bh - b * d.kv_heads), row = (int)(r - bh * rows);
+    if constexpr (KIND == 0) {
+        const RowAt a = row_at(d, hk, row);
+        static_cast<T*>(d.dq)[b * d.dqs[0] + a.token * d.dqs[1] + a.head * d.dqs[2] + c] = (T)(s * d.scale);
+    } else if constexpr (KIND == 1) {
+        static_cast<T*>(d.dk)[b * d.dks[0] + row * d.dks[1] + hk * d.dks[2] + c] = (T)(s * d.scale);
+    } else {
+        static_cast<T*>(d.dv)[b * d.dvs[0] + row * d.dvs[1] + hk * d.dvs[2] + c] = (T)s;
+    }
+}
+
+template <class T, int KS, bool MASKED, bool RAGGED>
+hipError_t backward(const CrossDev& d, hipStream_t st) {
+    const int64_t bh = (int64_t)d.batch * d.kv_heads;
+    hipError_t e = hipSuccess;
+    if (d.dq && d.rows > 0) {
+        k_cross_dq<T, KS, MASKED, RAGGED><<<(unsigned)((d.rows + 127) / 128 * d.splits * bh), kThreads, 0, st>>>(d);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+        if (d.splits > 1) {
+            k_cross_sum<T, 0><<<blocks_for(bh * d.rows * d.dim, kThreads), kThreads, 0, st>>>(d);
+            if ((e = hipGetLastError()) != hipSuccess) return e;
+        }
+    } else if (d.rows > 0) {
+        k_cross_delta<T><<<blocks_for(bh * d.rows, 16), kThreads, 0, st>>>(d);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if (d.dk && d.kv_len > 0) {
+        k_cross_dkv<T, KS, MASKED, RAGGED><<<(unsigned)((d.kv_len + 127) / 128 * d.row_splits * bh), kThreads, 0, st>>>(d);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+        if (d.row_splits > 1) {
+            k_cross_sum<T, 1><<<blocks_for(bh * d.kv_len * d.dim, kThreads), kThreads, 0, st>>>(d);
+            if ((e = hipGetLastError()) != hipSuccess) return e;
+            k_cross_sum<T, 2><<<blocks_for(bh * d.kv_len * d.dim, kThreads), kThreads, 0, st>>>(d);
+            e = hipGetLastError();
+        }
+    }
+    return e;
+}
+
+}  // namespace
+
+// Ranges of the split axis: as many as `slots` blocks (what the machine holds at once) allow, each of at
+// least two tiles.
+static void split(int64_t blocks, int64_t slots, int64_t length, int tile, int& n, int& each) {
+    const int64_t tiles = (length + tile - 1) / tile;
+    int64_t want = blocks > 0 ? slots / blocks : 1;
+    if (want > tiles / 2) want = tiles / 2;
+    if (want < 1) want = 1;
+    const int64_t per = tiles > 0 ? (tiles + want - 1) / want : 1;
+    each = (int)(per * tile);
+    n = tiles > 0 ? (int)((tiles + per - 1) / per) : 1;
+}
+
+void cross_plan(CrossDev& d, bool backward_pass) {
+    const int64_t bh = (int64_t)d.batch * d.kv_heads;
+    if (!backward_pass && d.rows <= 32) split(bh, 512, d.kv_len, 128, d.splits, d.split_keys);
+    else split((d.rows + 127) / 128 * bh, 512, d.kv_len, 64, d.splits, d.split_keys);
+    split((d.kv_len + 127) / 128 * bh, d.dim <= 96 ? 512 : 256, (int64_t)d.group * ((d.q_len + 31) / 32), 1, d.row_splits, d.split_tiles);
+}
+
+hipError_t cross_backward(const CrossDev& d, int dtype, hipStream_t st) {
+    return dispatch(d, dtype, [&](auto t, auto ks, auto m, auto r) {
+        return backward<decltype(t), decltype(ks)::value, decltype(m)::value, decltype(r)::value>(d, st);
+    });
+}
+
+}  // namespace pa

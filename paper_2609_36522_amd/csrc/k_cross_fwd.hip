@@ -1,0 +1,330 @@
+// Cross attention, forward, for gfx950 (layout and products: pa_cross.h).
+//
+// One pass over the keys with a running maximum and sum in fp32. Where the rows are too few to fill the
+// machine the keys are split over blocks, whose unnormalised outputs a second kernel joins.
+#include "pa_cross.h"
+
+namespace pa {
+
+namespace {
+
+// Rows fill the block: four waves of 32 rows share stages of 64 keys, double buffered (a stage's loads
+// are in flight during the products of the one before).
+//
+// The accumulator is rescaled only when some row's maximum has grown by a factor of more than 2^kSlack in
+// weight since the last time, so weights reach 2^kSlack, which the element types hold as exactly as 1.
+constexpr float kSlack = 8.0f;
+
+template <class T, int KS, bool MASKED, bool RAGGED>
+__global__ __launch_bounds__(kThreads, 2) void k_cross_fwd(CrossDev d) {
+    constexpr int DP = KS <= 4 ? 64 : 128, DB = (KS + 1) / 2, KEYS = 64, ROWS = 128, NT = 2;
+    typedef typename Vec<T>::v8 v8;
+    __shared__ __align__(16) T tiles[2][2][KEYS * DP];      // [stage parity][K, V]
+    __shared__ __align__(16) float bias[2][MASKED ? KEYS : 4];
+
+    const int row_tiles = (d.rows + ROWS - 1) / ROWS;
+    int id = xcd_order(blockIdx.x, gridDim.x);
+    const int tile = id % row_tiles;
+    id /= row_tiles;
+    const int split = id % d.splits, bh = id / d.splits;
+    const int b = bh / d.kv_heads, hk = bh - b * d.kv_heads;
+    const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6;
+    const int row = tile * ROWS + w * 32 + (lane & 31);
+    const bool valid = row < d.rows;
+    const RowAt ra = row_at(d, hk, valid ? row : 0);
+
+    const int klen = sample_keys(d, b);
+    const int kbeg = split * d.split_keys;
+    const int kend = klen < kbeg + d.split_keys ? klen : kbeg + d.split_keys;
+    const T* kb = static_cast<const T*>(d.k) + b * d.ks[0] + hk * d.ks[2];
+    const T* vb = static_cast<const T*>(d.v) + b * d.vs[0] + hk * d.vs[2];
+    KvStage<T, DP, KEYS, MASKED, kKvKind<MASKED, RAGGED>> st(d);
+    if (kbeg < kend) st.load(d, kb, vb, b, kbeg, kend, tiles[0][0], tiles[0][1]);
+
+    const T* qp = static_cast<const T*>(d.q) + b * d.qs[0] + ra.token * d.qs[1] + ra.head * d.qs[2];
+    v8 q[KS];
+    load_row<T, KS, RAGGED>(q, qp, d.dim, half, valid);
+
+    // Scores in units of 1/f: x f is the exponent of 2. With a mask x is the scaled, biased score.
+    const float f = MASKED ? kLog2e : d.scale * kLog2e;
+    f32x16 acc[DB];
+#pragma unroll
+    for (int i = 0; i < DB; ++i) acc[i] = f32x16{};
+    float m = -INFINITY, l = 0.0f;
+
+    if (kbeg < kend) st.arrive(tiles[0][0], tiles[0][1], bias[0]);
+    __syncthreads();
+    int p = 0;
+    for (int k0 = kbeg; k0 < kend; k0 += KEYS, p ^= 1) {
+        const T* kt = tiles[p][0];
+        const T* vt = tiles[p][1];
+        if (k0 + KEYS < kend) st.load(d, kb, vb, b, k0 + KEYS, kend, tiles[p ^ 1][0], tiles[p ^ 1][1]);
+        f32x16 s[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            s[nt] = f32x16{};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) s[nt] = mma(read_rows<T, DP>(kt, nt * 32 + (lane & 31), ks, half), q[ks], s[nt]);
+        }
+        if constexpr (MASKED) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[nt][r] = fmaf(s[nt][r], d.scale, bias[p][nt * 32 + 8 * (r >> 2) + 4 * half + (r & 3)]);
+        } else if (k0 + KEYS > kend) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (k0 + nt * 32 + 8 * (r >> 2) + 4 * half + (r & 3) >= kend) s[nt][r] = -INFINITY;
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[nt][r]);
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        if (__any((top - m) * f > kSlack)) {
+            const float n = fmaxf(top, m);
+            const float a = __builtin_amdgcn_exp2f((m - (n == -INFINITY ? 0.0f : n)) * f);
+            m = n;
+            l *= a;
+#pragma unroll
+            for (int i = 0; i < DB; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[i][r] *= a;
+        }
+        const float base = m == -INFINITY ? 0.0f : m;       // nothing seen yet: every weight is 0
+        const float mf = base * f;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                // With a mask the difference comes first: x may be near the type's lowest value.
+                const float e = __builtin_amdgcn_exp2f(MASKED ? (s[nt][r] - base) * f : fmaf(s[nt][r], f, -mf));
+                s[nt][r] = e;
+                l += e;
+            }
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const v8 e = pack<T>(s[nt], t);
+#pragma unroll
+                for (int db = 0; db < DB; ++db) acc[db] = mma(read_cols<T, DP>(vt, nt * 32 + t * 16, db, lane), e, acc[db]);
+            }
+        }
+        if (k0 + KEYS < kend) st.arrive(tiles[p ^ 1][0], tiles[p ^ 1][1], bias[p ^ 1]);
+        __syncthreads();
+    }
+    l += __shfl_xor(l, 32, 64);
+    const float m_nat = MASKED || m == -INFINITY ? m : m * d.scale;
+    if (d.splits == 1) {
+        T* op = static_cast<T*>(d.o) + b * d.os[0] + ra.token * d.os[1] + ra.head * d.os[2];
+        store_row<T, DB, RAGGED>(op, d.dim, acc, l == 0.0f ? 0.0f : 1.0f / l, half, valid);   // no key seen: acc is 0
+        if (d.stats && valid && half == 0) {
+            float* sp = d.stats + stat_at(d, b, ra) * 2;
+            sp[0] = m_nat;
+            sp[1] = logf(l);
+        }
+    } else if (valid) {
+        const int64_t at = ((int64_t)split * d.batch * d.kv_heads + bh) * d.rows + row;
+        store_row_f32<DB>(d.part + at * d.dim, d.dim, acc, half);
+        if (half == 0) {
+            d.part_stats[at * 2] = m_nat;
+            d.part_stats[at * 2 + 1] = l;
+        }
+    }
+}
+
+// At most 32 rows: the four waves take 32 keys each of a 128-key tile for the same rows and are joined at
+// the end. Bound by the reading of K and V; two blocks a CU keep 128 KB in flight.
+template <class T, int KS, bool MASKED, bool RAGGED>
+__global__ __launch_bounds__(kThreads, 2) void k_cross_few(CrossDev d) {
+    constexpr int DP = KS <= 4 ? 64 : 128, DB = (KS + 1) / 2, KEYS = 128, ROWS = 32;
+    typedef typename Vec<T>::v8 v8;
+    // K tile, V tile; afterwards the waves' accumulators [4][DP][32] in fp32.
+    __shared__ __align__(16) T tiles[2 * KEYS * DP];
+    __shared__ float bias[MASKED ? KEYS : 1];
+    __shared__ float wave_m[4][32], wave_l[4][32];
+    T* kt = tiles;
+    T* vt = tiles + KEYS * DP;
+
+    const int row_tiles = (d.rows + ROWS - 1) / ROWS;
+    int id = xcd_order(blockIdx.x, gridDim.x);
+    const int tile = id % row_tiles;
+    id /= row_tiles;
+    const int split = id % d.splits, bh = id / d.splits;
+    const int b = bh / d.kv_heads, hk = bh - b * d.kv_heads;
+    const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6;
+    const int row = tile * ROWS + (lane & 31);
+    const bool valid = row < d.rows;
+    const RowAt ra = row_at(d, hk, valid ? row : 0);
+
+    const T* qp = static_cast<const T*>(d.q) + b * d.qs[0] + ra.token * d.qs[1] + ra.head * d.qs[2];
+    v8 q[KS];
+    load_row<T, KS, RAGGED>(q, qp, d.dim, half, valid);
+
+    const int klen = sample_keys(d, b);
+    const int kbeg = split * d.split_keys;
+    const int kend = klen < kbeg + d.split_keys ? klen : kbeg + d.split_keys;
+    const T* kb = static_cast<const T*>(d.k) + b * d.ks[0] + hk * d.ks[2];
+    const T* vb = static_cast<const T*>(d.v) + b * d.vs[0] + hk * d.vs[2];
+
+    // Scores in units of 1/f: x f is the exponent of 2. With a mask x is the scaled, biased score.
+    const float f = MASKED ? kLog2e : d.scale * kLog2e;
+    f32x16 acc[DB];
+#pragma unroll
+    for (int i = 0; i < DB; ++i) acc[i] = f32x16{};
+    float m = -INFINITY, l = 0.0f;
+
+    KvStage<T, DP, KEYS, MASKED, RAGGED ? kRagged : kRegs> st(d);
+    if (kbeg < kend) st.load(d, kb, vb, b, kbeg, kend, kt, vt);
+    for (int k0 = kbeg; k0 < kend; k0 += KEYS) {
+        __syncthreads();
+        st.arrive(kt, vt, bias);
+        __syncthreads();
+        if (k0 + KEYS < kend) st.load(d, kb, vb, b, k0 + KEYS, kend, kt, vt);
+        const int koff = w * 32;
+        f32x16 s = f32x16{};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) s = mma(read_rows<T, DP>(kt, koff + (lane & 31), ks, half), q[ks], s);
+        if constexpr (MASKED) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], d.scale, bias[koff + 8 * (r >> 2) + 4 * half + (r & 3)]);
+        } else if (k0 + KEYS > kend) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (k0 + koff + 8 * (r >> 2) + 4 * half + (r & 3) >= kend) s[r] = -INFINITY;
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[r]);
+        top = fmaxf(fmaxf(top, __shfl_xor(top, 32, 64)), m);
+        const float base = top == -INFINITY ? 0.0f : top;   // nothing seen yet: every weight is 0
+        if (__any(top > m)) {
+            const float a = __builtin_amdgcn_exp2f((m - base) * f);
+            l *= a;
+#pragma unroll
+            for (int i = 0; i < DB; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[i][r] *= a;
+            m = top;
+        }
+        const float mf = base * f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            // With a mask the difference comes first: x may be near the type's lowest value.
+            s[r] = __builtin_amdgcn_exp2f(MASKED ? (s[r] - base) * f : fmaf(s[r], f, -mf));
+            l += s[r];
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const v8 p = pack<T>(s, t);
+#pragma unroll
+            for (int db = 0; db < DB; ++db) acc[db] = mma(read_cols<T, DP>(vt, koff + t * 16, db, lane), p, acc[db]);
+        }
+    }
+    l += __shfl_xor(l, 32, 64);
+    const float m_nat = MASKED || m == -INFINITY ? m : m * d.scale;
+
+    float* wa = reinterpret_cast<float*>(tiles);
+    __syncthreads();
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            wa[(w * DP + db * 32 + 8 * (r >> 2) + 4 * half + (r & 3)) * 32 + (lane & 31)] = acc[db][r];
+    if (half == 0) {
+        wave_m[w][lane] = m_nat;
+        wave_l[w][lane] = l;
+    }
+    __syncthreads();
+    // Thread: row threadIdx % 32, columns threadIdx / 32 + 8 i.
+    const int rr = threadIdx.x & 31, orow = tile * ROWS + rr;
+    if (orow >= d.rows) return;
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = fmaxf(top, wave_m[i][rr]);
+    const float base = top == -INFINITY ? 0.0f : top;
+    float a[4], sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        a[i] = __builtin_amdgcn_exp2f((wave_m[i][rr] - base) * kLog2e);
+        sum += a[i] * wave_l[i][rr];
+    }
+    const RowAt oa = row_at(d, hk, orow);
+    const int64_t at = ((int64_t)split * d.batch * d.kv_heads + bh) * d.rows + orow;
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    T* op = static_cast<T*>(d.o) + b * d.os[0] + oa.token * d.os[1] + oa.head * d.os[2];
+    for (int c = threadIdx.x >> 5; c < d.dim; c += 8) {
+        float o = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o += a[i] * wa[(i * DP + c) * 32 + rr];
+        if (d.splits == 1) op[c] = (T)(o * inv);
+        else d.part[at * d.dim + c] = o;
+    }
+    if (threadIdx.x < 32) {
+        if (d.splits > 1) {
+            d.part_stats[at * 2] = top;
+            d.part_stats[at * 2 + 1] = sum;
+        } else if (d.stats) {
+            float* sp = d.stats + stat_at(d, b, oa) * 2;
+            sp[0] = top;
+            sp[1] = logf(sum);
+        }
+    }
+}
+
+// Joins the key ranges' partial outputs: a wave per row.
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_cross_join(CrossDev d) {
+    const int64_t n = (int64_t)d.batch * d.kv_heads * d.rows;
+    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (at >= n) return;
+    const int lane = threadIdx.x & 63;
+    float top = -INFINITY;
+    for (int s = 0; s < d.splits; ++s) top = fmaxf(top, d.part_stats[(s * n + at) * 2]);
+    const float base = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f, o0 = 0.0f, o1 = 0.0f;
+    for (int s = 0; s < d.splits; ++s) {
+        const float a = __builtin_amdgcn_exp2f((d.part_stats[(s * n + at) * 2] - base) * kLog2e);
+        sum += a * d.part_stats[(s * n + at) * 2 + 1];
+        const float* p = d.part + (s * n + at) * d.dim;
+        if (lane < d.dim) o0 += a * p[lane];
+        if (lane + 64 < d.dim) o1 += a * p[lane + 64];
+    }
+    const int bh = (int)(at / d.rows), b = bh / d.kv_heads;
+    const RowAt ra = row_at(d, bh - b * d.kv_heads, (int)(at - (int64_t)bh * d.rows));
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    T* op = static_cast<T*>(d.o) + b * d.os[0] + ra.token * d.os[1] + ra.head * d.os[2];
+    if (lane < d.dim) op[lane] = (T)(o0 * inv);
+    if (lane + 64 < d.dim) op[lane + 64] = (T)(o1 * inv);
+    if (d.stats && lane == 0) {
+        float* sp = d.stats + stat_at(d, b, ra) * 2;
+        sp[0] = top;
+        sp[1] = logf(sum);
+    }
+}
+
+template <class T, int KS, bool MASKED, bool RAGGED>
+hipError_t forward(const CrossDev& d, hipStream_t st) {
+    const int64_t bh = (int64_t)d.batch * d.kv_heads;
+    if (d.rows <= 32) k_cross_few<T, KS, MASKED, RAGGED><<<(unsigned)(d.splits * bh), kThreads, 0, st>>>(d);
+    else k_cross_fwd<T, KS, MASKED, RAGGED><<<(unsigned)((d.rows + 127) / 128 * d.splits * bh), kThreads, 0, st>>>(d);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || d.splits == 1) return e;
+    k_cross_join<T><<<blocks_for(bh * d.rows, 4), kThreads, 0, st>>>(d);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t cross_forward(const CrossDev& d, int dtype, hipStream_t st) {
+    return dispatch(d, dtype, [&](auto t, auto ks, auto m, auto r) {
+        return forward<decltype(t), decltype(ks)::value, decltype(m)::value, decltype(r)::value>(d, st);
+    });
+}
+
+}  // namespace pa

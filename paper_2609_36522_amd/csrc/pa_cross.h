@@ -1,0 +1,255 @@
+// Cross attention kernels: what the forward and the backward pass share.
+//
+// Rows. The query heads that share a key/value head are rows of one matrix: row = token * group +
+// head in the group, so a shared head's keys and values are read once for all of them, and a
+// single token of a model with shared heads already fills several rows.
+//
+// Products. All use v_mfma_f32_32x32x16 (layouts: pa_mma.h). Scores are computed transposed (S^T = K Q^T: a lane owns a query row, its registers hold
+// keys), so the softmax's maximum and sum are a lane's own plus one exchange with lane l xor 32, and
+// the accumulator, rounded to 16 bits, is already the B operand of the next product over keys
+// (O^T = V^T P^T): its slots 8t .. 8t + 7 are keys 16t + 4 (l/32) + {0..3, 8..11}, an order that the
+// A operand (V^T) follows, read from the row-major tile with transposing LDS loads
+// (read_cols).
+// dk and dv come the other way round (S = Q K^T: a lane owns a key, registers hold rows).
+//
+// Softmax. One pass over the keys with a running maximum and sum in fp32; the accumulator is
+// rescaled only in steps where some row's maximum grew. P and dS are rounded to the element type for
+// their products (the accumulation stays fp32): their rounding errors are independent, so a sum
+// over keys keeps the relative error of one rounding, the size of the output's own.
+#pragma once
+
+#include <math.h>
+
+#include <type_traits>
+
+#include "pa_mma.h"
+
+namespace pa {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr float kLog2e = 1.4426950408889634f;
+
+// Strides below this many elements leave every offset within a tile of 128 rows to 32 bits.
+constexpr int64_t kBufferStride = 1 << 23;
+constexpr uint32_t kBufferBytes = 0x7fffffff, kNowhere = 0x80000000;
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void* p) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, kBufferBytes, 0x00020000);
+}
+
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }   // vmcnt(0)
+
+__device__ __forceinline__ int sample_keys(const CrossDev& d, int b) {
+    if (!d.kv_lens) return d.kv_len;
+    const int n = d.kv_lens[b];
+    return n < 0 ? 0 : n > d.kv_len ? d.kv_len : n;
+}
+
+// Additive bias of a key below the sample's length: 0, the mask's value, or -inf.
+__device__ __forceinline__ float key_bias(const CrossDev& d, int b, int key) {
+    if (d.mask_kind == PA_MASK_NONE) return 0.0f;
+    const int64_t at = b * d.mask_stride + key;
+    if (d.mask_kind == PA_MASK_ADD) return static_cast<const float*>(d.mask)[at];
+    return static_cast<const uint8_t*>(d.mask)[at] ? 0.0f : -INFINITY;
+}
+
+// A tile of ROWS rows, `stride` elements apart, on its way from memory to LDS.
+// KIND 0: buffer loads that write LDS themselves. A wave's 64 lanes fill consecutive 16-byte slots, so
+//   the permutation of a row's pieces is in the addresses that they read.
+// KIND 1: buffer loads into registers (the values can be changed before they are stored).
+// KIND 2: any stride, any head width.
+// With 0 and 1 (head_dim a multiple of 8, strides below kBufferStride) a thread's offset in the tile is
+// the same for every tile; pieces and rows that do not exist get an offset out of the buffer's range,
+// which reads as zero.
+constexpr int kDirect = 0, kRegs = 1, kRagged = 2;
+
+template <class T, int DP, int ROWS, int KIND>
+struct Stage {
+    static constexpr int kPieces = ROWS * (DP / 8) / kThreads, kPerRow = DP / 8, kStep = kThreads / kPerRow;
+    uint4 r[KIND == kDirect ? 1 : kPieces];
+    uint32_t off;
+
+    __device__ __forceinline__ static int row(int i) { return (int)threadIdx.x / kPerRow + i * kStep; }
+    // The thread's piece of its rows. The permutation repeats every 16 rows, and kStep is 16 or 32.
+    __device__ __forceinline__ static int piece() {
+        const int p = (int)threadIdx.x % kPerRow;
+        return KIND == kDirect ? (piece_at<DP>(row(0), p) - row(0) * DP) >> 3 : p;
+    }
+
+    __device__ __forceinline__ Stage(int dim, int64_t stride)
+        : off(piece() * 8 < dim ? (uint32_t)(row(0) * (int)stride + piece() * 8) * 2 : kNowhere) {}
+
+    // Starts the tile at `base`, of which `rows` rows exist, on its way.
+    __device__ __forceinline__ void load(const T* base, int64_t stride, int rows, int dim, T* tile) {
+        if constexpr (KIND == kRagged) {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i)
+                r[i] = __builtin_bit_cast(uint4, load8(base + row(i) * stride, piece() * 8, dim, row(i) < rows));
+        } else {
+            const __amdgpu_buffer_rsrc_t from = buffer_at(base);
+            const int step = kStep * (int)stride * 2;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const uint32_t at = row(i) < rows ? off : kNowhere;
+                if constexpr (KIND == kDirect) {
+                    typedef __attribute__((address_space(3))) void lds_void;
+                    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)(tile + (w * 64 + i * kThreads) * 8), 16, at, i * step, 0, 0);
+                } else {
+                    r[i] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(from, at, i * step, 0));
+                }
+            }
+        }
+    }
+    // The tile is in LDS once every thread has called this and a barrier has passed.
+    __device__ __forceinline__ void arrive(T* tile) const {
+        if constexpr (KIND == kDirect) {
+            wait_loads();
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) *reinterpret_cast<uint4*>(tile + piece_at<DP>(row(i), piece())) = r[i];
+        }
+    }
+};
+
+// Keys and values of a tile; with MASKED zeros where a key is not visible (0 weight times an infinity or
+// a NaN would not be 0), and the keys' biases.
+template <class T, int DP, int KEYS, bool MASKED, int KIND>
+struct KvStage {
+    typedef Stage<T, DP, KEYS, KIND> S;
+    S k, v;
+    float bias, seen[MASKED ? S::kPieces : 1];
+
+    __device__ __forceinline__ KvStage(const CrossDev& d) : k(d.dim, d.ks[1]), v(d.dim, d.vs[1]) {}
+
+    __device__ __forceinline__ void load(const CrossDev& d, const T* kb, const T* vb, int b, int k0, int kend, T* kt, T* vt) {
+        k.load(kb + k0 * d.ks[1], d.ks[1], kend - k0, d.dim, kt);
+        v.load(vb + k0 * d.vs[1], d.vs[1], kend - k0, d.dim, vt);
+        if constexpr (MASKED) {
+            const int key = k0 + (int)threadIdx.x;
+            bias = (int)threadIdx.x < KEYS && key < kend ? key_bias(d, b, key) : -INFINITY;
+#pragma unroll
+            for (int i = 0; i < S::kPieces; ++i) {
+                const int kk = k0 + S::row(i);
+                seen[i] = kk < kend ? key_bias(d, b, kk) : 0.0f;
+            }
+        }
+    }
+    __device__ __forceinline__ void arrive(T* kt, T* vt, float* bt) {
+        if constexpr (MASKED) {
+#pragma unroll
+            for (int i = 0; i < S::kPieces; ++i)
+                if (seen[i] == -INFINITY) k.r[i] = v.r[i] = make_uint4(0, 0, 0, 0);
+            if ((int)threadIdx.x < KEYS) bt[threadIdx.x] = bias;
+        }
+        k.arrive(kt);
+        v.arrive(vt);
+    }
+};
+
+// How a kernel's K and V tiles travel.
+template <bool MASKED, bool RAGGED>
+constexpr int kKvKind = RAGGED ? kRagged : MASKED ? kRegs : kDirect;
+
+// B operands of one row for all reduction steps: elements 16 ks + 8 half .. of the row at p.
+template <class T, int KS, bool RAGGED>
+__device__ __forceinline__ void load_row(typename Vec<T>::v8 (&out)[KS], const T* p, int dim, int half, bool valid) {
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        const int at = ks * 16 + half * 8;
+        if constexpr (RAGGED) {
+            out[ks] = __builtin_bit_cast(typename Vec<T>::v8, load8(p, at, dim, valid));
+        } else {
+            uint4 r = make_uint4(0, 0, 0, 0);
+            if (valid && at < dim) r = __builtin_bit_cast(uint4, *reinterpret_cast<const Pack8<T>*>(p + at));
+            out[ks] = __builtin_bit_cast(typename Vec<T>::v8, r);
+        }
+    }
+}
+
+// Stores a transposed accumulator (lane = row of the output) times f to the row at `out`.
+template <class T, int DB, bool RAGGED>
+__device__ __forceinline__ void store_row(T* out, int dim, const f32x16* acc, float f, int half, bool valid) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const Pack8<T> p = gather8<T>(acc[db], j, f);   // every lane takes part in the exchange
+            const int c = db * 32 + j * 16 + half * 8;
+            if constexpr (RAGGED) {
+                if (valid) store8(out + c, p, dim - c);
+            } else {
+                if (valid && c < dim) *reinterpret_cast<Pack8<T>*>(out + c) = p;
+            }
+        }
+    }
+}
+
+// The same in fp32 without the exchange.
+template <int DB>
+__device__ __forceinline__ void store_row_f32(float* out, int dim, const f32x16* acc, int half) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int c = db * 32 + q * 8 + half * 4;
+            struct __attribute__((packed, aligned(4))) Quad { float v[4]; };
+            if (c + 4 <= dim) {
+                *reinterpret_cast<Quad*>(out + c) = {{acc[db][4 * q], acc[db][4 * q + 1], acc[db][4 * q + 2], acc[db][4 * q + 3]}};
+            } else {
+#pragma unroll
+                for (int i = 0; i < 3; ++i)
+                    if (c + i < dim) out[c + i] = acc[db][4 * q + i];
+            }
+        }
+    }
+}
+
+struct RowAt {
+    int token, head;
+};
+__device__ __forceinline__ RowAt row_at(const CrossDev& d, int hk, int row) {
+    const int token = row / d.group;
+    return {token, hk * d.group + (row - token * d.group)};
+}
+__device__ __forceinline__ int64_t stat_at(const CrossDev& d, int b, RowAt r) {
+    return ((int64_t)b * d.q_heads + r.head) * d.q_len + r.token;
+}
+
+// With a mask, or a scale that is not positive (the largest scaled score is then not the scaled
+// largest product), scores are formed before the maximum is taken.
+inline bool masked(const CrossDev& d) { return d.mask_kind != PA_MASK_NONE || !(d.scale > 0.0f); }
+
+inline bool ragged(const CrossDev& d) {
+    for (const int64_t* p : {d.qs, d.ks, d.vs, d.os, d.dos, d.dqs, d.dks, d.dvs})
+        if (p[1] >= kBufferStride) return true;
+    return d.dim % 8 != 0;
+}
+
+inline unsigned blocks_for(int64_t n, int each) { return (unsigned)((n + each - 1) / each); }
+
+// Calls f(type, reduction steps of 16 over the head, masked, ragged): head widths are padded to 64, 80,
+// 96 or 128, ragged ones to 64 or 128.
+template <class F>
+hipError_t dispatch(const CrossDev& d, int dtype, F f) {
+    const bool m = masked(d), r = ragged(d);
+    auto with = [&](auto t, auto ks) {
+        return m ? f(t, ks, std::true_type{}, std::false_type{}) : f(t, ks, std::false_type{}, std::false_type{});
+    };
+    auto with_ragged = [&](auto t, auto ks) {
+        return m ? f(t, ks, std::true_type{}, std::true_type{}) : f(t, ks, std::false_type{}, std::true_type{});
+    };
+    auto width = [&](auto t) {
+        if (r) return d.dim > 64 ? with_ragged(t, std::integral_constant<int, 8>{}) : with_ragged(t, std::integral_constant<int, 4>{});
+        if (d.dim <= 64) return with(t, std::integral_constant<int, 4>{});
+        if (d.dim <= 80) return with(t, std::integral_constant<int, 5>{});
+        return d.dim <= 96 ? with(t, std::integral_constant<int, 6>{}) : with(t, std::integral_constant<int, 8>{});
+    };
+    return dtype == PA_BF16 ? width((__bf16)0) : width((_Float16)0);
+}
+
+}  // namespace
+
+}  // namespace pa
