@@ -29,19 +29,18 @@ __global__ __launch_bounds__(kThreads) void k_cross_delta(CrossDev d) {
     if (i < n && (threadIdx.x & 15) == 0) d.delta[(b * d.q_heads + h) * d.q_len + t] = s;
 }
 
-// A row's statistics as the backward pass uses them: without a mask hi = log2 of the sum of all
-// weights (lo unused), with one the maximum and the logarithm apart. A row that sees no key has
-// weights 0 whatever its scores.
+// A row's statistics (m, log of the sum) as the backward pass uses them: without a mask hi = log2 of the sum
+// of all weights (lo unused), with one the maximum and the log2 of the sum past it apart. A row that sees
+// no key has weights 0 whatever its scores.
 template <bool MASKED>
-__device__ __forceinline__ void row_stats(const CrossDev& d, int64_t at, float& hi, float& lo) {
-    const float m = d.stats[at * 2], ll = d.stats[at * 2 + 1];
+__device__ __forceinline__ void row_stats(float m, float ll, float& hi, float& lo) {
     const bool empty = ll == -INFINITY;
     hi = MASKED ? (empty ? 0.0f : m) : (empty ? INFINITY : (m + ll) * kLog2e);
-    lo = empty ? INFINITY : ll;
+    lo = empty ? INFINITY : ll * kLog2e;
 }
 template <bool MASKED>
 __device__ __forceinline__ float weight(float s, float scale, float f, float bias, float hi, float lo) {
-    return __builtin_amdgcn_exp2f(MASKED ? ((fmaf(s, scale, bias) - hi) - lo) * kLog2e : fmaf(s, f, -hi));
+    return __builtin_amdgcn_exp2f(MASKED ? fmaf(fmaf(s, scale, bias) - hi, kLog2e, -lo) : fmaf(s, f, -hi));
 }
 
 // dq: the forward pass's tiling; a lane owns a row, K and V tiles pass by. Writes delta for the rows of its
@@ -53,12 +52,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
     __shared__ __align__(16) T tiles[2][2][KEYS * DP];
     __shared__ __align__(16) float bias[2][MASKED ? KEYS : 4];
 
-    const int row_tiles = (d.rows + ROWS - 1) / ROWS;
-    int id = xcd_order(blockIdx.x, gridDim.x);
-    const int tile = id % row_tiles;
-    id /= row_tiles;
-    const int split = id % d.splits, bh = id / d.splits;
-    const int b = bh / d.kv_heads, hk = bh - b * d.kv_heads;
+    const Work wk = work_at(d);
+    const int tile = wk.tile, b = wk.b, hk = wk.hk;
     const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6;
     const int row = tile * ROWS + w * 32 + (lane & 31);
     const bool valid = row < d.rows;
@@ -66,8 +61,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
     const int64_t sat = stat_at(d, b, ra);
 
     const int klen = sample_keys(d, b);
-    const int kbeg = split * d.split_keys;
-    const int kend = klen < kbeg + d.split_keys ? klen : kbeg + d.split_keys;
+    const int kbeg = wk.split * d.split_keys;
+    const int kend = wk.part < 0 || klen < kbeg + d.split_keys ? klen : kbeg + d.split_keys;
     const T* kb = static_cast<const T*>(d.k) + b * d.ks[0] + hk * d.ks[2];
     const T* vb = static_cast<const T*>(d.v) + b * d.vs[0] + hk * d.vs[2];
     KvStage<T, DP, KEYS, MASKED, kKvKind<MASKED, RAGGED>> st(d);
@@ -82,10 +77,10 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) delta = fmaf((float)g[ks][i], (float)q[ks][i], delta);
     delta += __shfl_xor(delta, 32, 64);
-    if (split == 0 && valid && half == 0) d.delta[sat] = delta;
+    if (wk.split == 0 && valid && half == 0) d.delta[sat] = delta;
     load_row<T, KS, RAGGED>(q, static_cast<const T*>(d.q) + b * d.qs[0] + ra.token * d.qs[1] + ra.head * d.qs[2], d.dim, half, valid);
     float hi, lo;
-    row_stats<MASKED>(d, sat, hi, lo);
+    row_stats<MASKED>(d.stats[sat * 2], d.stats[sat * 2 + 1], hi, lo);
     const float f = d.scale * kLog2e;
     f32x16 acc[DB];
 #pragma unroll
@@ -106,13 +101,21 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
                 s = mma(read_rows<T, DP>(kt, nt * 32 + (lane & 31), ks, half), q[ks], s);
                 e = mma(read_rows<T, DP>(vt, nt * 32 + (lane & 31), ks, half), g[ks], e);
             }
-            const bool border = !MASKED && k0 + nt * 32 + 32 > kend;
+            if (!MASKED && k0 + nt * 32 + 32 > kend) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int key = nt * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
-                float x = weight<MASKED>(s[r], d.scale, f, MASKED ? bias[p][key] : 0.0f, hi, lo);
-                if (border && k0 + key >= kend) x = 0.0f;
-                s[r] = x * (e[r] - delta);
+                for (int r = 0; r < 16; ++r)
+                    if (k0 + nt * 32 + 8 * (r >> 2) + 4 * half + (r & 3) >= kend) s[r] = -INFINITY;
+            }
+#pragma unroll
+            for (int g4 = 0; g4 < 4; ++g4) {
+                float4 bv = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if constexpr (MASKED) bv = *reinterpret_cast<const float4*>(&bias[p][nt * 32 + 8 * g4 + 4 * half]);
+                const float bs[4] = {bv.x, bv.y, bv.z, bv.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = 4 * g4 + i;
+                    s[r] = weight<MASKED>(s[r], d.scale, f, bs[i], hi, lo) * (e[r] - delta);
+                }
             }
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
@@ -124,11 +127,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
         if (k0 + KEYS < kend) st.arrive(tiles[p ^ 1][0], tiles[p ^ 1][1], bias[p ^ 1]);
         __syncthreads();
     }
-    if (d.splits == 1) {
+    if (wk.part < 0) {
         T* out = static_cast<T*>(d.dq) + b * d.dqs[0] + ra.token * d.dqs[1] + ra.head * d.dqs[2];
         store_row<T, DB, RAGGED>(out, d.dim, acc, d.scale, half, valid);
     } else if (valid) {
-        const int64_t at = ((int64_t)split * d.batch * d.kv_heads + bh) * d.rows + row;
+        const int64_t at = (int64_t)wk.part * ROWS + (row - tile * ROWS);
         store_row_f32<DB>(d.part + at * d.dim, d.dim, acc, half);
     }
 }
@@ -161,7 +164,7 @@ __global__ __launch_bounds__(kThreads, KS <= 6 ? 2 : 1) void k_cross_dkv(CrossDe
     const T* qb = static_cast<const T*>(d.q) + b * d.qs[0] + (int64_t)hk * d.group * d.qs[2];
     const T* gb = static_cast<const T*>(d.d_o) + b * d.dos[0] + (int64_t)hk * d.group * d.dos[2];
     Stage<T, DP, ROWS, KIND> sq(d.dim, d.qs[1]), sg(d.dim, d.dos[1]);
-    float s_hi = 0.0f, s_lo = 0.0f, s_delta = 0.0f;
+    float s_m = 0.0f, s_l = -INFINITY, s_delta = 0.0f;       // a row that does not exist sees no key
     auto load = [&](int it, int p) {
         const int gh = it / head_tiles, r0 = (it - gh * head_tiles) * ROWS, rows = d.q_len - r0;
         sq.load(qb + gh * d.qs[2] + r0 * d.qs[1], d.qs[1], rows, d.dim, tiles[p][0]);
@@ -169,12 +172,12 @@ __global__ __launch_bounds__(kThreads, KS <= 6 ? 2 : 1) void k_cross_dkv(CrossDe
         if (threadIdx.x < ROWS) {
             if ((int)threadIdx.x < rows) {
                 const int64_t at = stat_at(d, b, {r0 + (int)threadIdx.x, hk * d.group + gh});
-                row_stats<MASKED>(d, at, s_hi, s_lo);
+                s_m = d.stats[at * 2];
+                s_l = d.stats[at * 2 + 1];
                 s_delta = d.delta[at];
             } else {
-                s_hi = MASKED ? 0.0f : INFINITY;
-                s_lo = INFINITY;
-                s_delta = 0.0f;
+                s_m = s_delta = 0.0f;
+                s_l = -INFINITY;
             }
         }
     };
@@ -182,15 +185,17 @@ __global__ __launch_bounds__(kThreads, KS <= 6 ? 2 : 1) void k_cross_dkv(CrossDe
         sq.arrive(tiles[p][0]);
         sg.arrive(tiles[p][1]);
         if (threadIdx.x < ROWS) {
-            stat[p][0][threadIdx.x] = s_hi;
-            stat[p][1][threadIdx.x] = s_lo;
+            float hi, lo;
+            row_stats<MASKED>(s_m, s_l, hi, lo);
+            stat[p][0][threadIdx.x] = hi;
+            stat[p][1][threadIdx.x] = lo;
             stat[p][2][threadIdx.x] = s_delta;
         }
     };
     if (tbeg < tend) load(tbeg, 0);
 
     bool seen = key < klen;
-    float bias = 0.0f;
+    float bias = -INFINITY;                  // of the lane's key
     if (MASKED && seen) {
         bias = key_bias(d, b, key);
         seen = bias != -INFINITY;
@@ -217,12 +222,20 @@ __global__ __launch_bounds__(kThreads, KS <= 6 ? 2 : 1) void k_cross_dkv(CrossDe
             e = mma(read_rows<T, DP>(gt, lane & 31, ks, half), vr[ks], e);
         }
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int rr = 8 * (r >> 2) + 4 * half + (r & 3);
-            float x = weight<MASKED>(s[r], d.scale, f, bias, stat[p][0][rr], MASKED ? stat[p][1][rr] : 0.0f);
-            if (!seen) x = 0.0f;
-            s[r] = x;
-            e[r] = seen ? x * (e[r] - stat[p][2][rr]) : 0.0f;
+        for (int g4 = 0; g4 < 4; ++g4) {
+            float4 st[3];
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (MASKED || i != 1) st[i] = *reinterpret_cast<const float4*>(&stat[p][i][8 * g4 + 4 * half]);
+            const float hi[4] = {st[0].x, st[0].y, st[0].z, st[0].w}, dl[4] = {st[2].x, st[2].y, st[2].z, st[2].w};
+            float lo[4] = {};
+            if constexpr (MASKED) lo[0] = st[1].x, lo[1] = st[1].y, lo[2] = st[1].z, lo[3] = st[1].w;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = 4 * g4 + i;
+                s[r] = weight<MASKED>(s[r], d.scale, f, bias, hi[i], lo[i]);
+                e[r] = s[r] * (e[r] - dl[i]);
+            }
         }
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -235,6 +248,10 @@ __global__ __launch_bounds__(kThreads, KS <= 6 ? 2 : 1) void k_cross_dkv(CrossDe
         }
         if (it + 1 < tend) arrive(p ^ 1);
         __syncthreads();
+    }
+    if (!seen) {                             // the lane's columns held weights of a key of zeros
+#pragma unroll
+        for (int i = 0; i < DB; ++i) ak[i] = av[i] = f32x16{};
     }
     const bool valid = key < d.kv_len;
     if (d.row_splits == 1) {
@@ -249,27 +266,42 @@ __global__ __launch_bounds__(kThreads, KS <= 6 ? 2 : 1) void k_cross_dkv(CrossDe
     }
 }
 
-// Sums of the key ranges' dq (KIND 0) or the row ranges' dk, dv (1, 2), in a fixed order.
-template <class T, int KIND>
-__global__ __launch_bounds__(kThreads) void k_cross_sum(CrossDev d) {
-    const int rows = KIND == 0 ? d.rows : d.kv_len, n_part = KIND == 0 ? d.splits : d.row_splits;
-    const int64_t n = (int64_t)d.batch * d.kv_heads * rows * d.dim;
+// dq of the split row tiles from their key ranges, in a fixed order: 32 lanes of 4 columns per row.
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_cross_sum_dq(CrossDev d) {
+    const int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int rt = (int)(i / d.tile_rows), lr = (int)(i - (int64_t)rt * d.tile_rows), t = d.whole + rt;
+    if (t >= d.tiles) return;
+    const int row_tiles = (d.rows + d.tile_rows - 1) / d.tile_rows, bh = t / row_tiles, row = (t - bh * row_tiles) * d.tile_rows + lr;
+    const int b = bh / d.kv_heads, c = (threadIdx.x & 31) * 4;
+    if (row >= d.rows || c >= d.dim) return;
+    const RowAt a = row_at(d, bh - b * d.kv_heads, row);
+    T* out = static_cast<T*>(d.dq) + b * d.dqs[0] + a.token * d.dqs[1] + a.head * d.dqs[2];
+    const float* p = d.part + ((int64_t)rt * d.splits * d.tile_rows + lr) * d.dim;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (c + e >= d.dim) break;
+        float s = 0.0f;
+        for (int k = 0; k < d.splits; ++k) s += p[(int64_t)k * d.tile_rows * d.dim + c + e];
+        out[c + e] = (T)(s * d.scale);
+    }
+}
+
+// dk (blockIdx.y 0) and dv (1) from their row ranges, in a fixed order.
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_cross_sum_dkv(CrossDev d) {
+    const int64_t n = (int64_t)d.batch * d.kv_heads * d.kv_len * d.dim;
     const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     if (i >= n) return;
-    const float* part = KIND == 0 ? d.part : KIND == 1 ? d.part_dk : d.part_dv;
+    const float* part = blockIdx.y ? d.part_dv : d.part_dk;
     float s = 0.0f;
-    for (int k = 0; k < n_part; ++k) s += part[k * n + i];
+#pragma unroll 4
+    for (int k = 0; k < d.row_splits; ++k) s += part[k * n + i];
     const int c = (int)(i % d.dim);
-    const int64_t r = i / d.dim, bh = r / rows, b = bh / d.kv_heads;
-    const int hk = (int)(bh - b * d.kv_heads), row = (int)(r - bh * rows);
-    if constexpr (KIND == 0) {
-        const RowAt a = row_at(d, hk, row);
-        static_cast<T*>(d.dq)[b * d.dqs[0] + a.token * d.dqs[1] + a.head * d.dqs[2] + c] = (T)(s * d.scale);
-    } else if constexpr (KIND == 1) {
-        static_cast<T*>(d.dk)[b * d.dks[0] + row * d.dks[1] + hk * d.dks[2] + c] = (T)(s * d.scale);
-    } else {
-        static_cast<T*>(d.dv)[b * d.dvs[0] + row * d.dvs[1] + hk * d.dvs[2] + c] = (T)s;
-    }
+    const int64_t r = i / d.dim, bh = r / d.kv_len, b = bh / d.kv_heads;
+    const int hk = (int)(bh - b * d.kv_heads), key = (int)(r - bh * d.kv_len);
+    if (blockIdx.y) static_cast<T*>(d.dv)[b * d.dvs[0] + key * d.dvs[1] + hk * d.dvs[2] + c] = (T)s;
+    else static_cast<T*>(d.dk)[b * d.dks[0] + key * d.dks[1] + hk * d.dks[2] + c] = (T)(s * d.scale);
 }
 
 template <class T, int KS, bool MASKED, bool RAGGED>
@@ -277,10 +309,10 @@ hipError_t backward(const CrossDev& d, hipStream_t st) {
     const int64_t bh = (int64_t)d.batch * d.kv_heads;
     hipError_t e = hipSuccess;
     if (d.dq && d.rows > 0) {
-        k_cross_dq<T, KS, MASKED, RAGGED><<<(unsigned)((d.rows + 127) / 128 * d.splits * bh), kThreads, 0, st>>>(d);
+        k_cross_dq<T, KS, MASKED, RAGGED><<<(unsigned)(d.whole + (d.tiles - d.whole) * d.splits), kThreads, 0, st>>>(d);
         if ((e = hipGetLastError()) != hipSuccess) return e;
-        if (d.splits > 1) {
-            k_cross_sum<T, 0><<<blocks_for(bh * d.rows * d.dim, kThreads), kThreads, 0, st>>>(d);
+        if (d.whole < d.tiles) {
+            k_cross_sum_dq<T><<<blocks_for((int64_t)(d.tiles - d.whole) * d.tile_rows, 8), kThreads, 0, st>>>(d);
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
     } else if (d.rows > 0) {
@@ -291,9 +323,7 @@ hipError_t backward(const CrossDev& d, hipStream_t st) {
         k_cross_dkv<T, KS, MASKED, RAGGED><<<(unsigned)((d.kv_len + 127) / 128 * d.row_splits * bh), kThreads, 0, st>>>(d);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         if (d.row_splits > 1) {
-            k_cross_sum<T, 1><<<blocks_for(bh * d.kv_len * d.dim, kThreads), kThreads, 0, st>>>(d);
-            if ((e = hipGetLastError()) != hipSuccess) return e;
-            k_cross_sum<T, 2><<<blocks_for(bh * d.kv_len * d.dim, kThreads), kThreads, 0, st>>>(d);
+            k_cross_sum_dkv<T><<<dim3(blocks_for(bh * d.kv_len * d.dim, kThreads), 2), kThreads, 0, st>>>(d);
             e = hipGetLastError();
         }
     }
@@ -302,23 +332,35 @@ hipError_t backward(const CrossDev& d, hipStream_t st) {
 
 }  // namespace
 
-// Ranges of the split axis: as many as `slots` blocks (what the machine holds at once) allow, each of at
-// least two tiles.
-static void split(int64_t blocks, int64_t slots, int64_t length, int tile, int& n, int& each) {
-    const int64_t tiles = (length + tile - 1) / tile;
-    int64_t want = blocks > 0 ? slots / blocks : 1;
-    if (want > tiles / 2) want = tiles / 2;
+// Blocks that the machine holds at once: two on each of its 256 CUs.
+constexpr int64_t kSlots = 512;
+
+// Splits `length` tiles of an axis over as many ranges as `room` allows, each of at least two tiles.
+static void split(int64_t room, int64_t length, int& n, int& each) {
+    int64_t want = room < length / 2 ? room : length / 2;
     if (want < 1) want = 1;
-    const int64_t per = tiles > 0 ? (tiles + want - 1) / want : 1;
-    each = (int)(per * tile);
-    n = tiles > 0 ? (int)((tiles + per - 1) / per) : 1;
+    const int64_t per = length > 0 ? (length + want - 1) / want : 1;
+    each = (int)per;
+    n = length > 0 ? (int)((length + per - 1) / per) : 1;
 }
 
+// Row tiles that fill the machine in whole rounds take all keys in one block. The rest, at most half a
+// round, would leave most CUs idle for as long as a whole round takes: they are split over the keys, and
+// their partial results joined. (2304 tokens, 32 heads, 4096 keys: 576 tiles are one round and 64 more.)
 void cross_plan(CrossDev& d, bool backward_pass) {
     const int64_t bh = (int64_t)d.batch * d.kv_heads;
-    if (!backward_pass && d.rows <= 32) split(bh, 512, d.kv_len, 128, d.splits, d.split_keys);
-    else split((d.rows + 127) / 128 * bh, 512, d.kv_len, 64, d.splits, d.split_keys);
-    split((d.kv_len + 127) / 128 * bh, d.dim <= 96 ? 512 : 256, (int64_t)d.group * ((d.q_len + 31) / 32), 1, d.row_splits, d.split_tiles);
+    const int key_tile = !backward_pass && d.rows <= 32 ? 128 : 64;
+    d.tile_rows = !backward_pass && d.rows <= 32 ? 32 : 128;
+    const int64_t tiles = (d.rows + d.tile_rows - 1) / d.tile_rows * bh, rest = tiles % kSlots;
+    d.tiles = (int)tiles;
+    d.whole = (int)tiles;
+    split(rest > 0 ? kSlots / rest : 1, ((int64_t)d.kv_len + key_tile - 1) / key_tile, d.splits, d.split_keys);
+    d.split_keys *= key_tile;
+    if (d.splits > 1) d.whole = (int)(tiles - rest);
+    // dk, dv: one block a CU above a head width of 96.
+    const int64_t key_blocks = ((int64_t)d.kv_len + 127) / 128 * bh;
+    split((d.dim <= 96 ? kSlots : kSlots / 2) / (key_blocks > 0 ? key_blocks : 1), (int64_t)d.group * ((d.q_len + 31) / 32),
+          d.row_splits, d.split_tiles);
 }
 
 hipError_t cross_backward(const CrossDev& d, int dtype, hipStream_t st) {

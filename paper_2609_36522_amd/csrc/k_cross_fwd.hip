@@ -8,6 +8,18 @@ namespace pa {
 
 namespace {
 
+// Scaled scores plus the biases of their 32 keys.
+__device__ __forceinline__ void add_bias(f32x16& s, float scale, const float* bias, int half) {
+#pragma unroll
+    for (int g4 = 0; g4 < 4; ++g4) {
+        const float4 bv = *reinterpret_cast<const float4*>(bias + 8 * g4 + 4 * half);
+        s[4 * g4] = fmaf(s[4 * g4], scale, bv.x);
+        s[4 * g4 + 1] = fmaf(s[4 * g4 + 1], scale, bv.y);
+        s[4 * g4 + 2] = fmaf(s[4 * g4 + 2], scale, bv.z);
+        s[4 * g4 + 3] = fmaf(s[4 * g4 + 3], scale, bv.w);
+    }
+}
+
 // Rows fill the block: four waves of 32 rows share stages of 64 keys, double buffered (a stage's loads
 // are in flight during the products of the one before).
 //
@@ -22,20 +34,16 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_fwd(CrossDev d) {
     __shared__ __align__(16) T tiles[2][2][KEYS * DP];      // [stage parity][K, V]
     __shared__ __align__(16) float bias[2][MASKED ? KEYS : 4];
 
-    const int row_tiles = (d.rows + ROWS - 1) / ROWS;
-    int id = xcd_order(blockIdx.x, gridDim.x);
-    const int tile = id % row_tiles;
-    id /= row_tiles;
-    const int split = id % d.splits, bh = id / d.splits;
-    const int b = bh / d.kv_heads, hk = bh - b * d.kv_heads;
+    const Work wk = work_at(d);
+    const int tile = wk.tile, b = wk.b, hk = wk.hk;
     const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6;
     const int row = tile * ROWS + w * 32 + (lane & 31);
     const bool valid = row < d.rows;
     const RowAt ra = row_at(d, hk, valid ? row : 0);
 
     const int klen = sample_keys(d, b);
-    const int kbeg = split * d.split_keys;
-    const int kend = klen < kbeg + d.split_keys ? klen : kbeg + d.split_keys;
+    const int kbeg = wk.split * d.split_keys;
+    const int kend = wk.part < 0 || klen < kbeg + d.split_keys ? klen : kbeg + d.split_keys;
     const T* kb = static_cast<const T*>(d.k) + b * d.ks[0] + hk * d.ks[2];
     const T* vb = static_cast<const T*>(d.v) + b * d.vs[0] + hk * d.vs[2];
     KvStage<T, DP, KEYS, MASKED, kKvKind<MASKED, RAGGED>> st(d);
@@ -68,9 +76,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_fwd(CrossDev d) {
         }
         if constexpr (MASKED) {
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[nt][r] = fmaf(s[nt][r], d.scale, bias[p][nt * 32 + 8 * (r >> 2) + 4 * half + (r & 3)]);
+            for (int nt = 0; nt < NT; ++nt) add_bias(s[nt], d.scale, bias[p] + nt * 32, half);
         } else if (k0 + KEYS > kend) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
@@ -120,7 +126,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_fwd(CrossDev d) {
     }
     l += __shfl_xor(l, 32, 64);
     const float m_nat = MASKED || m == -INFINITY ? m : m * d.scale;
-    if (d.splits == 1) {
+    if (wk.part < 0) {
         T* op = static_cast<T*>(d.o) + b * d.os[0] + ra.token * d.os[1] + ra.head * d.os[2];
         store_row<T, DB, RAGGED>(op, d.dim, acc, l == 0.0f ? 0.0f : 1.0f / l, half, valid);   // no key seen: acc is 0
         if (d.stats && valid && half == 0) {
@@ -129,7 +135,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_fwd(CrossDev d) {
             sp[1] = logf(l);
         }
     } else if (valid) {
-        const int64_t at = ((int64_t)split * d.batch * d.kv_heads + bh) * d.rows + row;
+        const int64_t at = (int64_t)wk.part * ROWS + (row - tile * ROWS);
         store_row_f32<DB>(d.part + at * d.dim, d.dim, acc, half);
         if (half == 0) {
             d.part_stats[at * 2] = m_nat;
@@ -146,17 +152,13 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_few(CrossDev d) {
     typedef typename Vec<T>::v8 v8;
     // K tile, V tile; afterwards the waves' accumulators [4][DP][32] in fp32.
     __shared__ __align__(16) T tiles[2 * KEYS * DP];
-    __shared__ float bias[MASKED ? KEYS : 1];
+    __shared__ __align__(16) float bias[MASKED ? KEYS : 4];
     __shared__ float wave_m[4][32], wave_l[4][32];
     T* kt = tiles;
     T* vt = tiles + KEYS * DP;
 
-    const int row_tiles = (d.rows + ROWS - 1) / ROWS;
-    int id = xcd_order(blockIdx.x, gridDim.x);
-    const int tile = id % row_tiles;
-    id /= row_tiles;
-    const int split = id % d.splits, bh = id / d.splits;
-    const int b = bh / d.kv_heads, hk = bh - b * d.kv_heads;
+    const Work wk = work_at(d);
+    const int tile = wk.tile, b = wk.b, hk = wk.hk;
     const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6;
     const int row = tile * ROWS + (lane & 31);
     const bool valid = row < d.rows;
@@ -167,8 +169,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_few(CrossDev d) {
     load_row<T, KS, RAGGED>(q, qp, d.dim, half, valid);
 
     const int klen = sample_keys(d, b);
-    const int kbeg = split * d.split_keys;
-    const int kend = klen < kbeg + d.split_keys ? klen : kbeg + d.split_keys;
+    const int kbeg = wk.split * d.split_keys;
+    const int kend = wk.part < 0 || klen < kbeg + d.split_keys ? klen : kbeg + d.split_keys;
     const T* kb = static_cast<const T*>(d.k) + b * d.ks[0] + hk * d.ks[2];
     const T* vb = static_cast<const T*>(d.v) + b * d.vs[0] + hk * d.vs[2];
 
@@ -191,8 +193,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_few(CrossDev d) {
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) s = mma(read_rows<T, DP>(kt, koff + (lane & 31), ks, half), q[ks], s);
         if constexpr (MASKED) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], d.scale, bias[koff + 8 * (r >> 2) + 4 * half + (r & 3)]);
+            add_bias(s, d.scale, bias + koff, half);
         } else if (k0 + KEYS > kend) {
 #pragma unroll
             for (int r = 0; r < 16; ++r)
@@ -255,18 +256,18 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_few(CrossDev d) {
         sum += a[i] * wave_l[i][rr];
     }
     const RowAt oa = row_at(d, hk, orow);
-    const int64_t at = ((int64_t)split * d.batch * d.kv_heads + bh) * d.rows + orow;
+    const int64_t at = (int64_t)wk.part * ROWS + rr;
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     T* op = static_cast<T*>(d.o) + b * d.os[0] + oa.token * d.os[1] + oa.head * d.os[2];
     for (int c = threadIdx.x >> 5; c < d.dim; c += 8) {
         float o = 0.0f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) o += a[i] * wa[(i * DP + c) * 32 + rr];
-        if (d.splits == 1) op[c] = (T)(o * inv);
+        if (wk.part < 0) op[c] = (T)(o * inv);
         else d.part[at * d.dim + c] = o;
     }
     if (threadIdx.x < 32) {
-        if (d.splits > 1) {
+        if (wk.part >= 0) {
             d.part_stats[at * 2] = top;
             d.part_stats[at * 2 + 1] = sum;
         } else if (d.stats) {
@@ -277,31 +278,51 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_few(CrossDev d) {
     }
 }
 
-// Joins the key ranges' partial outputs: a wave per row.
-template <class T>
+// Joins the key ranges of the split row tiles: WPR waves per row (one for a few ranges, four, each taking
+// every fourth range, for many).
+template <class T, int WPR>
 __global__ __launch_bounds__(kThreads) void k_cross_join(CrossDev d) {
-    const int64_t n = (int64_t)d.batch * d.kv_heads * d.rows;
-    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (at >= n) return;
-    const int lane = threadIdx.x & 63;
+    __shared__ float o[WPR == 1 ? 1 : 4][128];
+    const int lane = threadIdx.x & 63, w = WPR == 1 ? 0 : threadIdx.x >> 6;
+    const int i = WPR == 1 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+    const int rt = i / d.tile_rows, lr = i - rt * d.tile_rows, t = d.whole + rt;
+    const int row_tiles = (d.rows + d.tile_rows - 1) / d.tile_rows, bh = t / row_tiles, row = (t - bh * row_tiles) * d.tile_rows + lr;
+    if (row >= d.rows) return;               // the whole block, or (WPR = 1) a wave of a kernel without barriers
+    const int64_t first = (int64_t)rt * d.splits * d.tile_rows + lr;     // partial row of range 0; the next are tile_rows apart
+    const float* ps = d.part_stats + first * 2;
     float top = -INFINITY;
-    for (int s = 0; s < d.splits; ++s) top = fmaxf(top, d.part_stats[(s * n + at) * 2]);
+    for (int s = lane; s < d.splits; s += 64) top = fmaxf(top, ps[(int64_t)s * d.tile_rows * 2]);
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
     const float base = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f, o0 = 0.0f, o1 = 0.0f;
-    for (int s = 0; s < d.splits; ++s) {
-        const float a = __builtin_amdgcn_exp2f((d.part_stats[(s * n + at) * 2] - base) * kLog2e);
-        sum += a * d.part_stats[(s * n + at) * 2 + 1];
-        const float* p = d.part + (s * n + at) * d.dim;
-        if (lane < d.dim) o0 += a * p[lane];
-        if (lane + 64 < d.dim) o1 += a * p[lane + 64];
+    float sum = 0.0f;
+    for (int s = lane; s < d.splits; s += 64)
+        sum += __builtin_amdgcn_exp2f((ps[(int64_t)s * d.tile_rows * 2] - base) * kLog2e) * ps[(int64_t)s * d.tile_rows * 2 + 1];
+    sum = wave_sum_f32(sum);
+    float o0 = 0.0f, o1 = 0.0f;
+    const int c0 = lane < d.dim ? lane : 0, c1 = lane + 64 < d.dim ? lane + 64 : 0;
+#pragma unroll 4
+    for (int s = w; s < d.splits; s += WPR) {
+        const float a = __builtin_amdgcn_exp2f((ps[(int64_t)s * d.tile_rows * 2] - base) * kLog2e);
+        const float* p = d.part + (first + (int64_t)s * d.tile_rows) * d.dim;
+        o0 = fmaf(a, p[c0], o0);
+        o1 = fmaf(a, p[c1], o1);
     }
-    const int bh = (int)(at / d.rows), b = bh / d.kv_heads;
-    const RowAt ra = row_at(d, bh - b * d.kv_heads, (int)(at - (int64_t)bh * d.rows));
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const int b = bh / d.kv_heads;
+    const RowAt ra = row_at(d, bh - b * d.kv_heads, row);
     T* op = static_cast<T*>(d.o) + b * d.os[0] + ra.token * d.os[1] + ra.head * d.os[2];
-    if (lane < d.dim) op[lane] = (T)(o0 * inv);
-    if (lane + 64 < d.dim) op[lane + 64] = (T)(o1 * inv);
-    if (d.stats && lane == 0) {
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    if constexpr (WPR == 1) {
+        if (lane < d.dim) op[lane] = (T)(o0 * inv);
+        if (lane + 64 < d.dim) op[lane + 64] = (T)(o1 * inv);
+    } else {
+        o[w][lane] = o0;
+        o[w][lane + 64] = o1;
+        __syncthreads();
+        const int c = threadIdx.x;
+        if (c < d.dim) op[c] = (T)(((o[0][c] + o[1][c]) + (o[2][c] + o[3][c])) * inv);
+    }
+    if (d.stats && lane == 0 && w == 0) {
         float* sp = d.stats + stat_at(d, b, ra) * 2;
         sp[0] = top;
         sp[1] = logf(sum);
@@ -310,12 +331,14 @@ __global__ __launch_bounds__(kThreads) void k_cross_join(CrossDev d) {
 
 template <class T, int KS, bool MASKED, bool RAGGED>
 hipError_t forward(const CrossDev& d, hipStream_t st) {
-    const int64_t bh = (int64_t)d.batch * d.kv_heads;
-    if (d.rows <= 32) k_cross_few<T, KS, MASKED, RAGGED><<<(unsigned)(d.splits * bh), kThreads, 0, st>>>(d);
-    else k_cross_fwd<T, KS, MASKED, RAGGED><<<(unsigned)((d.rows + 127) / 128 * d.splits * bh), kThreads, 0, st>>>(d);
+    const unsigned blocks = (unsigned)(d.whole + (d.tiles - d.whole) * d.splits);
+    if (d.tile_rows == 32) k_cross_few<T, KS, MASKED, RAGGED><<<blocks, kThreads, 0, st>>>(d);
+    else k_cross_fwd<T, KS, MASKED, RAGGED><<<blocks, kThreads, 0, st>>>(d);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || d.splits == 1) return e;
-    k_cross_join<T><<<blocks_for(bh * d.rows, 4), kThreads, 0, st>>>(d);
+    if (e != hipSuccess || d.whole == d.tiles) return e;
+    const unsigned rows = (unsigned)((d.tiles - d.whole) * d.tile_rows);
+    if (d.splits > 8) k_cross_join<T, 4><<<rows, kThreads, 0, st>>>(d);
+    else k_cross_join<T, 1><<<rows / 4, kThreads, 0, st>>>(d);
     return hipGetLastError();
 }
 

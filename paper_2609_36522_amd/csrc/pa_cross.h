@@ -218,6 +218,32 @@ __device__ __forceinline__ int64_t stat_at(const CrossDev& d, int b, RowAt r) {
     return ((int64_t)b * d.q_heads + r.head) * d.q_len + r.token;
 }
 
+// A block's part of the forward pass or of dq: the first `whole` blocks take a row tile over all keys,
+// the others a key range of a row tile each.
+struct Work {
+    int tile, split, part;           // row tile among those of its kv head, key range, index of the partial result (or -1)
+    int b, hk, bh;
+};
+__device__ __forceinline__ Work work_at(const CrossDev& d) {
+    Work w;
+    const int row_tiles = (d.rows + d.tile_rows - 1) / d.tile_rows;
+    int t;
+    if ((int)blockIdx.x < d.whole) {
+        t = xcd_order(blockIdx.x, d.whole);
+        w.split = 0;
+        w.part = -1;
+    } else {
+        w.part = xcd_order(blockIdx.x - d.whole, gridDim.x - d.whole);
+        t = d.whole + w.part / d.splits;
+        w.split = w.part % d.splits;
+    }
+    w.bh = t / row_tiles;
+    w.tile = t - w.bh * row_tiles;
+    w.b = w.bh / d.kv_heads;
+    w.hk = w.bh - w.b * d.kv_heads;
+    return w;
+}
+
 // With a mask, or a scale that is not positive (the largest scaled score is then not the scaled
 // largest product), scores are formed before the maximum is taken.
 inline bool masked(const CrossDev& d) { return d.mask_kind != PA_MASK_NONE || !(d.scale > 0.0f); }

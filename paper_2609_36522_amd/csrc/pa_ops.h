@@ -29,13 +29,15 @@ struct CrossDev {
     int batch, q_heads, kv_heads, group;   // group: query heads per kv head
     int q_len, kv_len, dim;
     int rows;                        // q_len * group: rows that share a kv head, row = token * group + head in group
-    int splits, split_keys;          // forward, dq: key ranges of split_keys keys (a multiple of the key tile)
+    int whole;                       // forward, dq: row tiles that one block takes over all keys; the others are
+    int splits, split_keys;          // split into key ranges of split_keys keys (a multiple of the key tile)
     int row_splits, split_tiles;     // dk, dv: ranges of split_tiles tiles of 32 tokens of a query head
     float scale;
     int64_t mask_stride;
     int64_t qs[3], ks[3], vs[3], os[3], dos[3], dqs[3], dks[3], dvs[3];   // batch, token, head
-    float* part;                     // partial o, or partial dq: [splits][batch * kv_heads][rows][dim]
-    float* part_stats;               // [splits][batch * kv_heads][rows][2]
+    int tile_rows, tiles;            // rows of a row tile, row tiles of all samples and kv heads
+    float* part;                     // partial o, or partial dq: [split tile][splits][tile_rows][dim]
+    float* part_stats;               // [split tile][splits][tile_rows][2]
     float* delta;                    // [batch][q_heads][q_len]: sum of do * o over the head
     float *part_dk, *part_dv;        // [row_splits][batch * kv_heads][kv_len][dim]
 };

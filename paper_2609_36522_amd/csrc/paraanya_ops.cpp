@@ -145,9 +145,10 @@ size_t cross_layout(pa::CrossDev& d, bool backward, char* ws) {
         return p;
     };
     const size_t rows = (size_t)d.batch * d.kv_heads * d.rows, keys = (size_t)d.batch * d.kv_heads * d.kv_len;
-    if (d.splits > 1) {
-        d.part = take((size_t)d.splits * rows * d.dim);
-        if (!backward) d.part_stats = take((size_t)d.splits * rows * 2);
+    if (d.whole < d.tiles) {
+        const size_t parts = (size_t)(d.tiles - d.whole) * d.splits * d.tile_rows;
+        d.part = take(parts * d.dim);
+        if (!backward) d.part_stats = take(parts * 2);
     }
     if (backward) {
         d.delta = take(rows);
