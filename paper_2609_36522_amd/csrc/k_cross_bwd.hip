@@ -86,7 +86,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
 #pragma unroll
     for (int i = 0; i < DB; ++i) acc[i] = f32x16{};
 
-    if (kbeg < kend) st.arrive(tiles[0][0], tiles[0][1], bias[0]);
+    if (kbeg < kend) st.arrive(tiles[0][0], tiles[0][1], bias[0], d.dim);
     __syncthreads();
     int p = 0;
     for (int k0 = kbeg; k0 < kend; k0 += KEYS, p ^= 1) {
@@ -124,7 +124,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
                 for (int db = 0; db < DB; ++db) acc[db] = mma(read_cols<T, DP>(kt, nt * 32 + t * 16, db, lane), ds, acc[db]);
             }
         }
-        if (k0 + KEYS < kend) st.arrive(tiles[p ^ 1][0], tiles[p ^ 1][1], bias[p ^ 1]);
+        if (k0 + KEYS < kend) st.arrive(tiles[p ^ 1][0], tiles[p ^ 1][1], bias[p ^ 1], d.dim);
         __syncthreads();
     }
     if (wk.part < 0) {
@@ -182,8 +182,8 @@ __global__ __launch_bounds__(kThreads, KS <= 6 ? 2 : 1) void k_cross_dkv(CrossDe
         }
     };
     auto arrive = [&](int p) {
-        sq.arrive(tiles[p][0]);
-        sg.arrive(tiles[p][1]);
+        sq.arrive(tiles[p][0], d.dim);
+        sg.arrive(tiles[p][1], d.dim);
         if (threadIdx.x < ROWS) {
             float hi, lo;
             row_stats<MASKED>(s_m, s_l, hi, lo);

@@ -60,7 +60,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_fwd(CrossDev d) {
     for (int i = 0; i < DB; ++i) acc[i] = f32x16{};
     float m = -INFINITY, l = 0.0f;
 
-    if (kbeg < kend) st.arrive(tiles[0][0], tiles[0][1], bias[0]);
+    if (kbeg < kend) st.arrive(tiles[0][0], tiles[0][1], bias[0], d.dim);
     __syncthreads();
     int p = 0;
     for (int k0 = kbeg; k0 < kend; k0 += KEYS, p ^= 1) {
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_fwd(CrossDev d) {
                 for (int db = 0; db < DB; ++db) acc[db] = mma(read_cols<T, DP>(vt, nt * 32 + t * 16, db, lane), e, acc[db]);
             }
         }
-        if (k0 + KEYS < kend) st.arrive(tiles[p ^ 1][0], tiles[p ^ 1][1], bias[p ^ 1]);
+        if (k0 + KEYS < kend) st.arrive(tiles[p ^ 1][0], tiles[p ^ 1][1], bias[p ^ 1], d.dim);
         __syncthreads();
     }
     l += __shfl_xor(l, 32, 64);
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_few(CrossDev d) {
     if (kbeg < kend) st.load(d, kb, vb, b, kbeg, kend, kt, vt);
     for (int k0 = kbeg; k0 < kend; k0 += KEYS) {
         __syncthreads();
-        st.arrive(kt, vt, bias);
+        st.arrive(kt, vt, bias, d.dim);
         __syncthreads();
         if (k0 + KEYS < kend) st.load(d, kb, vb, b, k0 + KEYS, kend, kt, vt);
         const int koff = w * 32;

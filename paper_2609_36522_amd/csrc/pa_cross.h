@@ -33,13 +33,6 @@ constexpr float kLog2e = 1.4426950408889634f;
 
 // Strides below this many elements leave every offset within a tile of 128 rows to 32 bits.
 constexpr int64_t kBufferStride = 1 << 23;
-constexpr uint32_t kBufferBytes = 0x7fffffff, kNowhere = 0x80000000;
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void* p) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, kBufferBytes, 0x00020000);
-}
-
-__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }   // vmcnt(0)
 
 __device__ __forceinline__ int sample_keys(const CrossDev& d, int b) {
     if (!d.kv_lens) return d.kv_len;
@@ -86,7 +79,7 @@ struct Stage {
         if constexpr (KIND == kRagged) {
 #pragma unroll
             for (int i = 0; i < kPieces; ++i)
-                r[i] = __builtin_bit_cast(uint4, load8(base + row(i) * stride, piece() * 8, dim, row(i) < rows));
+                r[i] = __builtin_bit_cast(uint4, load8_raw(base + row(i) * stride, piece() * 8, dim, row(i) < rows));
         } else {
             const __amdgpu_buffer_rsrc_t from = buffer_at(base);
             const int step = kStep * (int)stride * 2;
@@ -94,9 +87,8 @@ struct Stage {
             for (int i = 0; i < kPieces; ++i) {
                 const uint32_t at = row(i) < rows ? off : kNowhere;
                 if constexpr (KIND == kDirect) {
-                    typedef __attribute__((address_space(3))) void lds_void;
                     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-                    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)(tile + (w * 64 + i * kThreads) * 8), 16, at, i * step, 0, 0);
+                    load_lds(from, tile + (w * 64 + i * kThreads) * 8, at, i * step);
                 } else {
                     r[i] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(from, at, i * step, 0));
                 }
@@ -104,7 +96,12 @@ struct Stage {
         }
     }
     // The tile is in LDS once every thread has called this and a barrier has passed.
-    __device__ __forceinline__ void arrive(T* tile) const {
+    __device__ __forceinline__ void arrive(T* tile, int dim) {
+        if constexpr (KIND == kRagged) {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i)
+                r[i] = __builtin_bit_cast(uint4, fix8(__builtin_bit_cast(Pack8<T>, r[i]), piece() * 8, dim));
+        }
         if constexpr (KIND == kDirect) {
             wait_loads();
         } else {
@@ -137,15 +134,15 @@ struct KvStage {
             }
         }
     }
-    __device__ __forceinline__ void arrive(T* kt, T* vt, float* bt) {
+    __device__ __forceinline__ void arrive(T* kt, T* vt, float* bt, int dim) {
         if constexpr (MASKED) {
 #pragma unroll
             for (int i = 0; i < S::kPieces; ++i)
                 if (seen[i] == -INFINITY) k.r[i] = v.r[i] = make_uint4(0, 0, 0, 0);
             if ((int)threadIdx.x < KEYS) bt[threadIdx.x] = bias;
         }
-        k.arrive(kt);
-        v.arrive(vt);
+        k.arrive(kt, dim);
+        v.arrive(vt, dim);
     }
 };
 
@@ -156,16 +153,22 @@ constexpr int kKvKind = RAGGED ? kRagged : MASKED ? kRegs : kDirect;
 // B operands of one row for all reduction steps: elements 16 ks + 8 half .. of the row at p.
 template <class T, int KS, bool RAGGED>
 __device__ __forceinline__ void load_row(typename Vec<T>::v8 (&out)[KS], const T* p, int dim, int half, bool valid) {
+    typedef typename Vec<T>::v8 v8;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
         const int at = ks * 16 + half * 8;
         if constexpr (RAGGED) {
-            out[ks] = __builtin_bit_cast(typename Vec<T>::v8, load8(p, at, dim, valid));
+            out[ks] = __builtin_bit_cast(v8, load8_raw(p, at, dim, valid));
         } else {
             uint4 r = make_uint4(0, 0, 0, 0);
             if (valid && at < dim) r = __builtin_bit_cast(uint4, *reinterpret_cast<const Pack8<T>*>(p + at));
-            out[ks] = __builtin_bit_cast(typename Vec<T>::v8, r);
+            out[ks] = __builtin_bit_cast(v8, r);
         }
+    }
+    if constexpr (RAGGED) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+            out[ks] = __builtin_bit_cast(v8, fix8(__builtin_bit_cast(Pack8<T>, out[ks]), ks * 16 + half * 8, dim));
     }
 }
 

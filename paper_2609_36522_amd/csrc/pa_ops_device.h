@@ -43,22 +43,34 @@ __device__ __forceinline__ Pack8<T> shift8(Pack8<T> r, int n) {
 }
 
 // Elements at .. at + 7 of a row of len elements, zeros past its end and in an invalid row. A piece
-// that reaches past the end is read as the row's last eight elements and moved down, so that no
-// element outside the row is touched and the load stays one access. len is the same in all lanes.
+// that reaches past the end is read as the row's last eight elements and moved down (fix8), so that no
+// element outside the row is touched and the load stays one access. load8_raw starts the load, fix8
+// waits for it. len is the same in all lanes.
 template <class T>
-__device__ __forceinline__ Pack8<T> load8(const T* row, int at, int len, bool valid = true) {
+__device__ __forceinline__ Pack8<T> load8_raw(const T* row, int at, int len, bool valid = true) {
     Pack8<T> r;
     const int n = valid ? len - at : 0;
-    if (len >= 8) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) r.v[i] = (T)0.0f;
+    for (int i = 0; i < 8; ++i) r.v[i] = (T)0.0f;
+    if (len >= 8) {
         if (n > 0) r = *reinterpret_cast<const Pack8<T>*>(row + (n >= 8 ? at : len - 8));
-        if (len & 7) r = shift8(r, n > 0 && n < 8 ? 8 - n : 0);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) r.v[i] = i < n ? row[at + i] : (T)0.0f;
+        for (int i = 0; i < 7; ++i)
+            if (i < n) r.v[i] = row[at + i];
     }
     return r;
+}
+
+template <class T>
+__device__ __forceinline__ Pack8<T> fix8(const Pack8<T>& r, int at, int len) {
+    if (len < 8 || (len & 7) == 0) return r;
+    return shift8(r, at < len && at + 8 > len ? at + 8 - len : 0);
+}
+
+template <class T>
+__device__ __forceinline__ Pack8<T> load8(const T* row, int at, int len, bool valid = true) {
+    return fix8(load8_raw(row, at, len, valid), at, len);
 }
 
 template <class T>
@@ -71,6 +83,23 @@ __device__ __forceinline__ void store8(T* p, const Pack8<T>& r, int n) {
             if (i < n) p[i] = r.v[i];
     }
 }
+
+// Buffer loads take 32-bit offsets from a base; one at kNowhere is out of the buffer's range and reads as
+// zero.
+constexpr uint32_t kBufferBytes = 0x7fffffff, kNowhere = 0x80000000;
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void* p) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, kBufferBytes, 0x00020000);
+}
+
+// 16 bytes per lane, at `off` + `base_off` of the buffer, into consecutive 16-byte slots of LDS (lds: the
+// wave's first). In LDS once wait_loads has returned.
+__device__ __forceinline__ void load_lds(__amdgpu_buffer_rsrc_t from, void* lds, uint32_t off, int base_off) {
+    typedef __attribute__((address_space(3))) void lds_void;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)lds, 16, off, base_off, 0, 0);
+}
+
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }   // vmcnt(0)
 
 __device__ __forceinline__ float wave_sum_f32(float v) {
 #pragma unroll
