@@ -45,7 +45,7 @@ __device__ __forceinline__ float weight(float s, float scale, float f, float bia
 
 // dq: the forward pass's tiling; a lane owns a row, K and V tiles pass by. Writes delta for the rows of its
 // tile on the way (the first key range does).
-template <class T, int KS, bool MASKED, bool RAGGED>
+template <class T, int KS, bool MASKED, int WIDTH>
 __global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
     constexpr int DP = KS <= 4 ? 64 : 128, DB = (KS + 1) / 2, KEYS = 64, ROWS = 128;
     typedef typename Vec<T>::v8 v8;
@@ -65,12 +65,12 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
     const int kend = wk.part < 0 || klen < kbeg + d.split_keys ? klen : kbeg + d.split_keys;
     const T* kb = static_cast<const T*>(d.k) + b * d.ks[0] + hk * d.ks[2];
     const T* vb = static_cast<const T*>(d.v) + b * d.vs[0] + hk * d.vs[2];
-    KvStage<T, DP, KEYS, MASKED, kKvKind<MASKED, RAGGED>> st(d);
+    KvStage<T, DP, KEYS, MASKED, WIDTH, !MASKED && WIDTH == kWhole> st(d);
     if (kbeg < kend) st.load(d, kb, vb, b, kbeg, kend, tiles[0][0], tiles[0][1]);
 
     v8 q[KS], g[KS];
-    load_row<T, KS, RAGGED>(g, static_cast<const T*>(d.d_o) + b * d.dos[0] + ra.token * d.dos[1] + ra.head * d.dos[2], d.dim, half, valid);
-    load_row<T, KS, RAGGED>(q, static_cast<const T*>(d.o) + b * d.os[0] + ra.token * d.os[1] + ra.head * d.os[2], d.dim, half, valid);
+    load_row<T, KS, WIDTH>(g, static_cast<const T*>(d.d_o) + b * d.dos[0] + ra.token * d.dos[1] + ra.head * d.dos[2], d.dim, half, valid);
+    load_row<T, KS, WIDTH>(q, static_cast<const T*>(d.o) + b * d.os[0] + ra.token * d.os[1] + ra.head * d.os[2], d.dim, half, valid);
     float delta = 0.0f;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
@@ -78,7 +78,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
         for (int i = 0; i < 8; ++i) delta = fmaf((float)g[ks][i], (float)q[ks][i], delta);
     delta += __shfl_xor(delta, 32, 64);
     if (wk.split == 0 && valid && half == 0) d.delta[sat] = delta;
-    load_row<T, KS, RAGGED>(q, static_cast<const T*>(d.q) + b * d.qs[0] + ra.token * d.qs[1] + ra.head * d.qs[2], d.dim, half, valid);
+    load_row<T, KS, WIDTH>(q, static_cast<const T*>(d.q) + b * d.qs[0] + ra.token * d.qs[1] + ra.head * d.qs[2], d.dim, half, valid);
     float hi, lo;
     row_stats<MASKED>(d.stats[sat * 2], d.stats[sat * 2 + 1], hi, lo);
     const float f = d.scale * kLog2e;
@@ -129,7 +129,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
     }
     if (wk.part < 0) {
         T* out = static_cast<T*>(d.dq) + b * d.dqs[0] + ra.token * d.dqs[1] + ra.head * d.dqs[2];
-        store_row<T, DB, RAGGED>(out, d.dim, acc, d.scale, half, valid);
+        store_row<T, DB, WIDTH>(out, d.dim, acc, d.scale, half, valid);
     } else if (valid) {
         const int64_t at = (int64_t)wk.part * ROWS + (row - tile * ROWS);
         store_row_f32<DB>(d.part + at * d.dim, d.dim, acc, half);
@@ -138,10 +138,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
 
 // dk, dv: a wave owns 32 keys (K and V in registers), tiles of 32 tokens of one query head pass by, double
 // buffered; the heads of the group one after the other.
-template <class T, int KS, bool MASKED, bool RAGGED>
+template <class T, int KS, bool MASKED, int WIDTH>
 __global__ __launch_bounds__(kThreads, KS <= 6 ? 2 : 1) void k_cross_dkv(CrossDev d) {
     constexpr int DP = KS <= 4 ? 64 : 128, DB = (KS + 1) / 2, KEYS = 128, ROWS = 32;
-    constexpr int KIND = RAGGED ? kRagged : kDirect;
     typedef typename Vec<T>::v8 v8;
     __shared__ __align__(16) T tiles[2][2][ROWS * DP];       // [parity][q, do]
     __shared__ __align__(16) float stat[2][3][ROWS];         // hi, lo, delta
@@ -163,7 +162,7 @@ __global__ __launch_bounds__(kThreads, KS <= 6 ? 2 : 1) void k_cross_dkv(CrossDe
     if (tile * KEYS >= klen) tend = tbeg;
     const T* qb = static_cast<const T*>(d.q) + b * d.qs[0] + (int64_t)hk * d.group * d.qs[2];
     const T* gb = static_cast<const T*>(d.d_o) + b * d.dos[0] + (int64_t)hk * d.group * d.dos[2];
-    Stage<T, DP, ROWS, KIND> sq(d.dim, d.qs[1]), sg(d.dim, d.dos[1]);
+    Stage<T, DP, ROWS, WIDTH, WIDTH == kWhole> sq(d.dim, d.qs[1]), sg(d.dim, d.dos[1]);
     float s_m = 0.0f, s_l = -INFINITY, s_delta = 0.0f;       // a row that does not exist sees no key
     auto load = [&](int it, int p) {
         const int gh = it / head_tiles, r0 = (it - gh * head_tiles) * ROWS, rows = d.q_len - r0;
@@ -171,10 +170,10 @@ __global__ __launch_bounds__(kThreads, KS <= 6 ? 2 : 1) void k_cross_dkv(CrossDe
         sg.load(gb + gh * d.dos[2] + r0 * d.dos[1], d.dos[1], rows, d.dim, tiles[p][1]);
         if (threadIdx.x < ROWS) {
             if ((int)threadIdx.x < rows) {
-                const int64_t at = stat_at(d, b, {r0 + (int)threadIdx.x, hk * d.group + gh});
-                s_m = d.stats[at * 2];
-                s_l = d.stats[at * 2 + 1];
-                s_delta = d.delta[at];
+                const int64_t sat = stat_at(d, b, {r0 + (int)threadIdx.x, hk * d.group + gh});
+                s_m = d.stats[sat * 2];
+                s_l = d.stats[sat * 2 + 1];
+                s_delta = d.delta[sat];
             } else {
                 s_m = s_delta = 0.0f;
                 s_l = -INFINITY;
@@ -200,9 +199,10 @@ __global__ __launch_bounds__(kThreads, KS <= 6 ? 2 : 1) void k_cross_dkv(CrossDe
         bias = key_bias(d, b, key);
         seen = bias != -INFINITY;
     }
+    const int at = key < d.kv_len ? key : 0;
     v8 kr[KS], vr[KS];
-    load_row<T, KS, RAGGED>(kr, static_cast<const T*>(d.k) + b * d.ks[0] + key * d.ks[1] + hk * d.ks[2], d.dim, half, seen);
-    load_row<T, KS, RAGGED>(vr, static_cast<const T*>(d.v) + b * d.vs[0] + key * d.vs[1] + hk * d.vs[2], d.dim, half, seen);
+    load_row<T, KS, WIDTH>(kr, static_cast<const T*>(d.k) + b * d.ks[0] + at * d.ks[1] + hk * d.ks[2], d.dim, half, seen);
+    load_row<T, KS, WIDTH>(vr, static_cast<const T*>(d.v) + b * d.vs[0] + at * d.vs[1] + hk * d.vs[2], d.dim, half, seen);
     f32x16 ak[DB], av[DB];
 #pragma unroll
     for (int i = 0; i < DB; ++i) ak[i] = av[i] = f32x16{};
@@ -257,12 +257,12 @@ __global__ __launch_bounds__(kThreads, KS <= 6 ? 2 : 1) void k_cross_dkv(CrossDe
     if (d.row_splits == 1) {
         T* ok = static_cast<T*>(d.dk) + b * d.dks[0] + key * d.dks[1] + hk * d.dks[2];
         T* ov = static_cast<T*>(d.dv) + b * d.dvs[0] + key * d.dvs[1] + hk * d.dvs[2];
-        store_row<T, DB, RAGGED>(ok, d.dim, ak, d.scale, half, valid);
-        store_row<T, DB, RAGGED>(ov, d.dim, av, 1.0f, half, valid);
+        store_row<T, DB, WIDTH>(ok, d.dim, ak, d.scale, half, valid);
+        store_row<T, DB, WIDTH>(ov, d.dim, av, 1.0f, half, valid);
     } else if (valid) {
-        const int64_t at = ((int64_t)split * d.batch * d.kv_heads + bh) * d.kv_len + key;
-        store_row_f32<DB>(d.part_dk + at * d.dim, d.dim, ak, half);
-        store_row_f32<DB>(d.part_dv + at * d.dim, d.dim, av, half);
+        const int64_t out = ((int64_t)split * d.batch * d.kv_heads + bh) * d.kv_len + key;
+        store_row_f32<DB>(d.part_dk + out * d.dim, d.dim, ak, half);
+        store_row_f32<DB>(d.part_dv + out * d.dim, d.dim, av, half);
     }
 }
 
@@ -304,12 +304,12 @@ __global__ __launch_bounds__(kThreads) void k_cross_sum_dkv(CrossDev d) {
     else static_cast<T*>(d.dk)[b * d.dks[0] + key * d.dks[1] + hk * d.dks[2] + c] = (T)(s * d.scale);
 }
 
-template <class T, int KS, bool MASKED, bool RAGGED>
+template <class T, int KS, bool MASKED, int WIDTH>
 hipError_t backward(const CrossDev& d, hipStream_t st) {
     const int64_t bh = (int64_t)d.batch * d.kv_heads;
     hipError_t e = hipSuccess;
     if (d.dq && d.rows > 0) {
-        k_cross_dq<T, KS, MASKED, RAGGED><<<(unsigned)(d.whole + (d.tiles - d.whole) * d.splits), kThreads, 0, st>>>(d);
+        k_cross_dq<T, KS, MASKED, WIDTH><<<(unsigned)(d.whole + (d.tiles - d.whole) * d.splits), kThreads, 0, st>>>(d);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         if (d.whole < d.tiles) {
             k_cross_sum_dq<T><<<blocks_for((int64_t)(d.tiles - d.whole) * d.tile_rows, 8), kThreads, 0, st>>>(d);
@@ -320,7 +320,7 @@ hipError_t backward(const CrossDev& d, hipStream_t st) {
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (d.dk && d.kv_len > 0) {
-        k_cross_dkv<T, KS, MASKED, RAGGED><<<(unsigned)((d.kv_len + 127) / 128 * d.row_splits * bh), kThreads, 0, st>>>(d);
+        k_cross_dkv<T, KS, MASKED, WIDTH><<<(unsigned)((d.kv_len + 127) / 128 * d.row_splits * bh), kThreads, 0, st>>>(d);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         if (d.row_splits > 1) {
             k_cross_sum_dkv<T><<<dim3(blocks_for(bh * d.kv_len * d.dim, kThreads), 2), kThreads, 0, st>>>(d);
@@ -364,8 +364,8 @@ void cross_plan(CrossDev& d, bool backward_pass) {
 }
 
 hipError_t cross_backward(const CrossDev& d, int dtype, hipStream_t st) {
-    return dispatch(d, dtype, [&](auto t, auto ks, auto m, auto r) {
-        return backward<decltype(t), decltype(ks)::value, decltype(m)::value, decltype(r)::value>(d, st);
+    return dispatch(d, dtype, [&](auto t, auto ks, auto m, auto wd) {
+        return backward<decltype(t), decltype(ks)::value, decltype(m)::value, decltype(wd)::value>(d, st);
     });
 }
 

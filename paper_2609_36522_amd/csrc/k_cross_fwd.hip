@@ -27,7 +27,7 @@ __device__ __forceinline__ void add_bias(f32x16& s, float scale, const float* bi
 // weight since the last time, so weights reach 2^kSlack, which the element types hold as exactly as 1.
 constexpr float kSlack = 8.0f;
 
-template <class T, int KS, bool MASKED, bool RAGGED>
+template <class T, int KS, bool MASKED, int WIDTH>
 __global__ __launch_bounds__(kThreads, 2) void k_cross_fwd(CrossDev d) {
     constexpr int DP = KS <= 4 ? 64 : 128, DB = (KS + 1) / 2, KEYS = 64, ROWS = 128, NT = 2;
     typedef typename Vec<T>::v8 v8;
@@ -46,12 +46,12 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_fwd(CrossDev d) {
     const int kend = wk.part < 0 || klen < kbeg + d.split_keys ? klen : kbeg + d.split_keys;
     const T* kb = static_cast<const T*>(d.k) + b * d.ks[0] + hk * d.ks[2];
     const T* vb = static_cast<const T*>(d.v) + b * d.vs[0] + hk * d.vs[2];
-    KvStage<T, DP, KEYS, MASKED, kKvKind<MASKED, RAGGED>> st(d);
+    KvStage<T, DP, KEYS, MASKED, WIDTH, !MASKED && WIDTH == kWhole> st(d);
     if (kbeg < kend) st.load(d, kb, vb, b, kbeg, kend, tiles[0][0], tiles[0][1]);
 
     const T* qp = static_cast<const T*>(d.q) + b * d.qs[0] + ra.token * d.qs[1] + ra.head * d.qs[2];
     v8 q[KS];
-    load_row<T, KS, RAGGED>(q, qp, d.dim, half, valid);
+    load_row<T, KS, WIDTH>(q, qp, d.dim, half, valid);
 
     // Scores in units of 1/f: x f is the exponent of 2. With a mask x is the scaled, biased score.
     const float f = MASKED ? kLog2e : d.scale * kLog2e;
@@ -128,7 +128,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_fwd(CrossDev d) {
     const float m_nat = MASKED || m == -INFINITY ? m : m * d.scale;
     if (wk.part < 0) {
         T* op = static_cast<T*>(d.o) + b * d.os[0] + ra.token * d.os[1] + ra.head * d.os[2];
-        store_row<T, DB, RAGGED>(op, d.dim, acc, l == 0.0f ? 0.0f : 1.0f / l, half, valid);   // no key seen: acc is 0
+        store_row<T, DB, WIDTH>(op, d.dim, acc, l == 0.0f ? 0.0f : 1.0f / l, half, valid);   // no key seen: acc is 0
         if (d.stats && valid && half == 0) {
             float* sp = d.stats + stat_at(d, b, ra) * 2;
             sp[0] = m_nat;
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_fwd(CrossDev d) {
 
 // At most 32 rows: the four waves take 32 keys each of a 128-key tile for the same rows and are joined at
 // the end. Bound by the reading of K and V; two blocks a CU keep 128 KB in flight.
-template <class T, int KS, bool MASKED, bool RAGGED>
+template <class T, int KS, bool MASKED, int WIDTH>
 __global__ __launch_bounds__(kThreads, 2) void k_cross_few(CrossDev d) {
     constexpr int DP = KS <= 4 ? 64 : 128, DB = (KS + 1) / 2, KEYS = 128, ROWS = 32;
     typedef typename Vec<T>::v8 v8;
@@ -166,7 +166,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_few(CrossDev d) {
 
     const T* qp = static_cast<const T*>(d.q) + b * d.qs[0] + ra.token * d.qs[1] + ra.head * d.qs[2];
     v8 q[KS];
-    load_row<T, KS, RAGGED>(q, qp, d.dim, half, valid);
+    load_row<T, KS, WIDTH>(q, qp, d.dim, half, valid);
 
     const int klen = sample_keys(d, b);
     const int kbeg = wk.split * d.split_keys;
@@ -181,7 +181,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_few(CrossDev d) {
     for (int i = 0; i < DB; ++i) acc[i] = f32x16{};
     float m = -INFINITY, l = 0.0f;
 
-    KvStage<T, DP, KEYS, MASKED, RAGGED ? kRagged : kRegs> st(d);
+    KvStage<T, DP, KEYS, MASKED, WIDTH, false> st(d);
     if (kbeg < kend) st.load(d, kb, vb, b, kbeg, kend, kt, vt);
     for (int k0 = kbeg; k0 < kend; k0 += KEYS) {
         __syncthreads();
@@ -329,11 +329,11 @@ __global__ __launch_bounds__(kThreads) void k_cross_join(CrossDev d) {
     }
 }
 
-template <class T, int KS, bool MASKED, bool RAGGED>
+template <class T, int KS, bool MASKED, int WIDTH>
 hipError_t forward(const CrossDev& d, hipStream_t st) {
     const unsigned blocks = (unsigned)(d.whole + (d.tiles - d.whole) * d.splits);
-    if (d.tile_rows == 32) k_cross_few<T, KS, MASKED, RAGGED><<<blocks, kThreads, 0, st>>>(d);
-    else k_cross_fwd<T, KS, MASKED, RAGGED><<<blocks, kThreads, 0, st>>>(d);
+    if (d.tile_rows == 32) k_cross_few<T, KS, MASKED, WIDTH><<<blocks, kThreads, 0, st>>>(d);
+    else k_cross_fwd<T, KS, MASKED, WIDTH><<<blocks, kThreads, 0, st>>>(d);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || d.whole == d.tiles) return e;
     const unsigned rows = (unsigned)((d.tiles - d.whole) * d.tile_rows);
@@ -345,8 +345,8 @@ hipError_t forward(const CrossDev& d, hipStream_t st) {
 }  // namespace
 
 hipError_t cross_forward(const CrossDev& d, int dtype, hipStream_t st) {
-    return dispatch(d, dtype, [&](auto t, auto ks, auto m, auto r) {
-        return forward<decltype(t), decltype(ks)::value, decltype(m)::value, decltype(r)::value>(d, st);
+    return dispatch(d, dtype, [&](auto t, auto ks, auto m, auto wd) {
+        return forward<decltype(t), decltype(ks)::value, decltype(m)::value, decltype(wd)::value>(d, st);
     });
 }
 

@@ -45,78 +45,80 @@ __device__ __forceinline__ int request_from(const LoraDev& d, int row) {
     return lo;
 }
 
-// Eight elements at .. of a row of len; without RAGGED len is a multiple of 8, with it the operand is
-// whole after `fixed`.
-template <class T, bool RAGGED>
+// Eight elements at .. of an existing row of len, whole after `fixed`.
+template <class T, int WIDTH>
 __device__ __forceinline__ typename Vec<T>::v8 operand(const T* row, int at, int len, bool valid) {
-    if constexpr (RAGGED) {
-        return __builtin_bit_cast(typename Vec<T>::v8, load8_raw(row, at, len, valid));
-    } else {
-        uint4 r = make_uint4(0, 0, 0, 0);
-        if (valid && at < len) r = __builtin_bit_cast(uint4, *reinterpret_cast<const Pack8<T>*>(row + at));
-        return __builtin_bit_cast(typename Vec<T>::v8, r);
-    }
+    typedef typename Vec<T>::v8 v8;
+    if constexpr (WIDTH == kRagged) return __builtin_bit_cast(v8, load8_raw(row, at, len));
+    if constexpr (WIDTH == kTiny) return __builtin_bit_cast(v8, load8(row, at, len, valid));
+    uint4 r = make_uint4(0, 0, 0, 0);
+    if (valid && at < len) r = __builtin_bit_cast(uint4, *reinterpret_cast<const Pack8<T>*>(row + at));
+    return __builtin_bit_cast(v8, r);
 }
-
-template <class T, bool RAGGED>
-__device__ __forceinline__ typename Vec<T>::v8 fixed(typename Vec<T>::v8 r, int at, int len) {
-    if constexpr (RAGGED) return __builtin_bit_cast(typename Vec<T>::v8, fix8(__builtin_bit_cast(Pack8<T>, r), at, len));
+template <class T, int WIDTH>
+__device__ __forceinline__ typename Vec<T>::v8 fixed(typename Vec<T>::v8 r, int at, int len, bool valid) {
+    if constexpr (WIDTH == kRagged) return __builtin_bit_cast(typename Vec<T>::v8, fix8(__builtin_bit_cast(Pack8<T>, r), at, len, valid));
     return r;
 }
 
-// ROWS rows x 64 columns of a matrix on their way to LDS, THREADS threads. Without RAGGED by loads that
-// write LDS themselves (a wave's lanes fill consecutive 16-byte slots, so the permutation of a row's
-// pieces is in the addresses that they read; what does not exist has an offset out of the buffer's range,
-// which reads as zero), otherwise through registers.
-template <class T, int ROWS, int THREADS, bool RAGGED>
+// ROWS rows x 64 columns of a matrix on their way to LDS, THREADS threads. With kWhole by loads that write
+// LDS themselves (a wave's lanes fill consecutive 16-byte slots, so the permutation of a row's pieces is in
+// the addresses that they read; what does not exist has an offset out of the buffer's range, which reads
+// as zero), otherwise through registers.
+template <class T, int ROWS, int THREADS, int WIDTH>
 struct Stage {
     static constexpr int kPieces = ROWS * 8 / THREADS, kStep = THREADS / 8;
-    uint4 r[RAGGED ? kPieces : 1];
-    uint32_t off[RAGGED ? 1 : kPieces];
-    int piece, row, left;
+    uint4 r[WIDTH == kWhole ? 1 : kPieces];
+    uint32_t off[WIDTH == kWhole ? kPieces : 1];
+    int piece, row, rows, at, len;
 
-    __device__ __forceinline__ Stage(int64_t stride, int rows) {
+    // The matrix's row 0 of this tile exists, and rows - 1 more; rows are n long.
+    __device__ __forceinline__ Stage(int64_t stride, int rows_, int n) : rows(rows_), at(0), len(n) {
         row = (int)threadIdx.x >> 3;
         piece = (int)threadIdx.x & 7;
-        if constexpr (!RAGGED) {
+        if constexpr (WIDTH == kWhole) {
             piece = (piece_at<64>(row, piece) - row * 64) >> 3;     // the same for every kStep (16 or more) rows
 #pragma unroll
             for (int i = 0; i < kPieces; ++i)
                 off[i] = row + i * kStep < rows ? (uint32_t)((row + i * kStep) * (int)stride + piece * 8) * 2 : kNowhere;
         }
     }
-    // The 64 columns at `base` (rows of it exist), `cols` of them left in the row.
-    __device__ __forceinline__ void load(const T* base, int64_t stride, int rows, int cols, T* tile) {
-        if constexpr (RAGGED) {
-            left = cols;
-#pragma unroll
-            for (int i = 0; i < kPieces; ++i)
-                r[i] = __builtin_bit_cast(uint4, load8_raw(base + (row + i * kStep) * stride, piece * 8, cols, row + i * kStep < rows));
-        } else {
-            const __amdgpu_buffer_rsrc_t from = buffer_at(base);
+    // Columns k0 .. of the rows at `base`.
+    __device__ __forceinline__ void load(const T* base, int64_t stride, int k0, T* tile) {
+        if constexpr (WIDTH == kWhole) {
+            const __amdgpu_buffer_rsrc_t from = buffer_at(base + k0);
             const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-            const bool in = piece * 8 < cols;
+            const bool in = k0 + piece * 8 < len;
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i)
-                load_lds(from, tile + (w * 64 + i * THREADS) * 8, in ? off[i] : kNowhere, 0);
+            for (int i = 0; i < kPieces; ++i) load_lds(from, tile + (w * 64 + i * THREADS) * 8, in ? off[i] : kNowhere, 0);
+        } else {
+            at = k0 + piece * 8;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const bool valid = row + i * kStep < rows;
+                const T* p = base + (valid ? row + i * kStep : 0) * stride;
+                r[i] = WIDTH == kRagged ? __builtin_bit_cast(uint4, load8_raw(p, at, len)) : __builtin_bit_cast(uint4, load8(p, at, len, valid));
+            }
         }
     }
     // The tile is in LDS once every thread has called this and a barrier has passed.
-    __device__ __forceinline__ void arrive(T* tile) const {
-        if constexpr (RAGGED) {
-#pragma unroll
-            for (int i = 0; i < kPieces; ++i)
-                *reinterpret_cast<uint4*>(tile + piece_at<64>(row + i * kStep, piece)) =
-                    __builtin_bit_cast(uint4, fix8(__builtin_bit_cast(Pack8<T>, r[i]), piece * 8, left));
-        } else {
+    __device__ __forceinline__ void arrive(T* tile) {
+        if constexpr (WIDTH == kWhole) {
             wait_loads();
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                if constexpr (WIDTH == kRagged)
+                    r[i] = __builtin_bit_cast(uint4, fix8(__builtin_bit_cast(Pack8<T>, r[i]), at, len, row + i * kStep < rows));
+                *reinterpret_cast<uint4*>(tile + piece_at<64>(row + i * kStep, piece)) = r[i];
+            }
         }
     }
 };
 
 // t of 64 rows of one request: block (c, i) takes rows 64 c .. of request i, all of them if the grid is
 // smaller. Of the four waves two take 32 rows each, over half of the reduction; NR 32-row tiles of A.
-template <class T, int NR, bool RAGGED>
+template <class T, int NR, int WIDTH>
 __global__ __launch_bounds__(256) void k_lora_down(LoraDev d) {
     constexpr int ROWS = 64;
     __shared__ __align__(16) T tiles[2][(ROWS + NR * 32) * 64];
@@ -130,14 +132,14 @@ __global__ __launch_bounds__(256) void k_lora_down(LoraDev d) {
     const float s = d.scales ? d.scales[ad] : 1.0f;
     for (int r0 = beg + blockIdx.x * ROWS; r0 < end; r0 += gridDim.x * ROWS) {
         const T* x = static_cast<const T*>(d.x) + (int64_t)r0 * d.x_stride;
-        Stage<T, ROWS, 256, RAGGED> sx(d.x_stride, end - r0);
-        Stage<T, NR * 32, 256, RAGGED> sa(K, d.rank);
+        Stage<T, ROWS, 256, WIDTH> sx(d.x_stride, end - r0, K);
+        Stage<T, NR * 32, 256, WIDTH> sa(K, d.rank, K);
         f32x16 acc[NR];
 #pragma unroll
         for (int n = 0; n < NR; ++n) acc[n] = f32x16{};
         auto load = [&](int k0, int p) {
-            sx.load(x + k0, d.x_stride, end - r0, K - k0, tiles[p]);
-            sa.load(a + k0, K, d.rank, K - k0, tiles[p] + ROWS * 64);
+            sx.load(x, d.x_stride, k0, tiles[p]);
+            sa.load(a, K, k0, tiles[p] + ROWS * 64);
         };
         auto arrive = [&](int p) {
             sx.arrive(tiles[p]);
@@ -187,7 +189,7 @@ __global__ __launch_bounds__(256) void k_lora_down(LoraDev d) {
 
 // The same for requests of few rows: 32 rows a block, 16 / NR waves that take parts of 64 columns in
 // turn, every operand straight from memory, so that one token's reduction is in flight all at once.
-template <class T, int NR, bool RAGGED>
+template <class T, int NR, int WIDTH>
 __global__ __launch_bounds__(1024 / NR) void k_lora_down_few(LoraDev d) {
     constexpr int WAVES = 16 / NR;
     __shared__ float part[WAVES][NR * 32][33];
@@ -209,11 +211,11 @@ __global__ __launch_bounds__(1024 / NR) void k_lora_down_few(LoraDev d) {
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks) {
                 const int k = k0 + ks * 16 + half * 8;
-                xv[ks] = operand<T, RAGGED>(x, k, K, row < end);
+                xv[ks] = operand<T, WIDTH>(x, k, K, row < end);
 #pragma unroll
                 for (int n = 0; n < NR; ++n) {
                     const int r = n * 32 + (lane & 31);
-                    av[ks][n] = operand<T, RAGGED>(a + (int64_t)(r < d.rank ? r : 0) * K, k, K, r < d.rank);
+                    av[ks][n] = operand<T, WIDTH>(a + (int64_t)(r < d.rank ? r : 0) * K, k, K, r < d.rank);
                 }
             }
 #pragma unroll
@@ -221,7 +223,7 @@ __global__ __launch_bounds__(1024 / NR) void k_lora_down_few(LoraDev d) {
 #pragma unroll
                 for (int n = 0; n < NR; ++n) {
                     const int k = k0 + ks * 16 + half * 8;
-                    acc[n] = mma(fixed<T, RAGGED>(av[ks][n], k, K), fixed<T, RAGGED>(xv[ks], k, K), acc[n]);
+                    acc[n] = mma(fixed<T, WIDTH>(av[ks][n], k, K, n * 32 + (lane & 31) < d.rank), fixed<T, WIDTH>(xv[ks], k, K, row < end), acc[n]);
                 }
         }
         __syncthreads();
@@ -243,7 +245,7 @@ __global__ __launch_bounds__(1024 / NR) void k_lora_down_few(LoraDev d) {
 
 // The adapters' part of NM x NX 32 x 32 tiles: features f0 + 32 i + .., rows r0 + 32 j + ..; every
 // `step`-th request from the `first`-th of those that have rows here.
-template <class T, int NM, int NX, bool RAGGED>
+template <class T, int NM, int NX, int WIDTH>
 __device__ __forceinline__ void add_adapters(const LoraDev& d, int f0, int r0, int lane, f32x16 (&acc)[NM][NX], int first = 0, int step = 1) {
     typedef typename Vec<T>::v8 v8;
     const int half = lane >> 5, r1 = r0 + 32 * NX < d.rows ? r0 + 32 * NX : d.rows;
@@ -259,17 +261,17 @@ __device__ __forceinline__ void add_adapters(const LoraDev& d, int f0, int r0, i
 #pragma unroll
             for (int j = 0; j < NX; ++j) {
                 const int row = r0 + j * 32 + (lane & 31);
-                tv[j] = operand<T, false>(static_cast<const T*>(d.t) + (int64_t)row * d.rank_pad, k, d.rank_pad, row >= beg && row < end);
+                tv[j] = operand<T, kWhole>(static_cast<const T*>(d.t) + (int64_t)row * d.rank_pad, k, d.rank_pad, row >= beg && row < end);
             }
 #pragma unroll
             for (int m = 0; m < NM; ++m) {
                 const int f = f0 + m * 32 + (lane & 31);
-                bv[m] = operand<T, RAGGED>(b + (int64_t)f * d.rank, k, d.rank, f < d.out);
+                bv[m] = operand<T, WIDTH == kWhole ? kWhole : kTiny>(b + (int64_t)f * d.rank, k, d.rank, f < d.out);
             }
 #pragma unroll
             for (int m = 0; m < NM; ++m)
 #pragma unroll
-                for (int j = 0; j < NX; ++j) acc[m][j] = mma(fixed<T, RAGGED>(bv[m], k, d.rank), tv[j], acc[m][j]);
+                for (int j = 0; j < NX; ++j) acc[m][j] = mma(bv[m], tv[j], acc[m][j]);
         }
     }
 }
@@ -306,7 +308,7 @@ __device__ __forceinline__ void finish(const LoraDev& d, int f0, int r0, int lan
 // WF x WR waves of NM x NX tiles of 32 x 32 (features x rows) per block. The reduction goes through LDS in
 // parts of 64 columns, double buffered: the next part's loads are in flight during the products of the
 // current one.
-template <class T, int WF, int WR, int NM, int NX, bool RAGGED>
+template <class T, int WF, int WR, int NM, int NX, int WIDTH>
 __global__ __launch_bounds__(64 * WF * WR, 2) void k_lora_tile(LoraDev d) {
     typedef typename Vec<T>::v8 v8;
     constexpr int TF = WF * NM * 32, TR = WR * NX * 32, THREADS = 64 * WF * WR;
@@ -318,11 +320,11 @@ __global__ __launch_bounds__(64 * WF * WR, 2) void k_lora_tile(LoraDev d) {
     const int K = d.in;
     const T* wp = static_cast<const T*>(d.w) + (int64_t)f0 * d.w_stride;
     const T* xp = static_cast<const T*>(d.x) + (int64_t)r0 * d.x_stride;
-    Stage<T, TF, THREADS, RAGGED> sw(d.w_stride, d.out - f0);
-    Stage<T, TR, THREADS, RAGGED> sx(d.x_stride, d.rows - r0);
+    Stage<T, TF, THREADS, WIDTH> sw(d.w_stride, d.out - f0, K);
+    Stage<T, TR, THREADS, WIDTH> sx(d.x_stride, d.rows - r0, K);
     auto load = [&](int k0, int p) {
-        sw.load(wp + k0, d.w_stride, d.out - f0, K - k0, tiles[p]);
-        sx.load(xp + k0, d.x_stride, d.rows - r0, K - k0, tiles[p] + TF * 64);
+        sw.load(wp, d.w_stride, k0, tiles[p]);
+        sx.load(xp, d.x_stride, k0, tiles[p] + TF * 64);
     };
     auto arrive = [&](int p) {
         sw.arrive(tiles[p]);
@@ -357,13 +359,13 @@ __global__ __launch_bounds__(64 * WF * WR, 2) void k_lora_tile(LoraDev d) {
         if (k0 + 64 < K) arrive(p ^ 1);
         __syncthreads();
     }
-    if (d.adapters > 0) add_adapters<T, NM, NX, RAGGED>(d, f0 + fw, r0 + rw, lane, acc);
+    if (d.adapters > 0) add_adapters<T, NM, NX, WIDTH>(d, f0 + fw, r0 + rw, lane, acc);
     finish<T, NM, NX>(d, f0 + fw, r0 + rw, lane, acc);
 }
 
 // Few rows: 32 features x 32 rows per block. W is read once, straight into operand registers; 16 waves
 // take parts of 64 columns in turn, and the requests' adapters in turn, and are joined through LDS.
-template <class T, bool RAGGED>
+template <class T, int WIDTH>
 __global__ __launch_bounds__(1024) void k_lora_rows(LoraDev d) {
     typedef typename Vec<T>::v8 v8;
     __shared__ float part[16][16][64];
@@ -378,16 +380,16 @@ __global__ __launch_bounds__(1024) void k_lora_rows(LoraDev d) {
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) {
             const int k = k0 + ks * 16 + half * 8;
-            wv[ks] = operand<T, RAGGED>(wp, k, K, f < d.out);
-            xv[ks] = operand<T, RAGGED>(xp, k, K, row < d.rows);
+            wv[ks] = operand<T, WIDTH>(wp, k, K, f < d.out);
+            xv[ks] = operand<T, WIDTH>(xp, k, K, row < d.rows);
         }
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) {
             const int k = k0 + ks * 16 + half * 8;
-            acc[0][0] = mma(fixed<T, RAGGED>(wv[ks], k, K), fixed<T, RAGGED>(xv[ks], k, K), acc[0][0]);
+            acc[0][0] = mma(fixed<T, WIDTH>(wv[ks], k, K, f < d.out), fixed<T, WIDTH>(xv[ks], k, K, row < d.rows), acc[0][0]);
         }
     }
-    if (d.adapters > 0) add_adapters<T, 1, 1, RAGGED>(d, f0, r0, lane, acc, w, 16);
+    if (d.adapters > 0) add_adapters<T, 1, 1, WIDTH>(d, f0, r0, lane, acc, w, 16);
 #pragma unroll
     for (int r = 0; r < 16; ++r) part[w][r][lane] = acc[0][0][r];
     __syncthreads();
@@ -404,37 +406,37 @@ __global__ __launch_bounds__(1024) void k_lora_rows(LoraDev d) {
     finish<T, 1, 1>(d, f0, r0, lane, acc);
 }
 
-template <class T, int NR, bool RAGGED>
+template <class T, int NR, int WIDTH>
 void down(const LoraDev& d, hipStream_t st) {
     // Blocks per request: its share of the rows, so that the launch has about rows / 64 (or 32) of them.
     // Requests of fewer than 64 rows on average are latency bound.
     const bool few = d.rows < 64 * d.requests;
     const int per = d.rows / (few ? 32 : 64) / d.requests + 1;
     const dim3 grid((unsigned)(per < 4096 ? per : 4096), (unsigned)d.requests);
-    if (few) k_lora_down_few<T, NR, RAGGED><<<grid, 1024 / NR, 0, st>>>(d);
-    else k_lora_down<T, NR, RAGGED><<<grid, 256, 0, st>>>(d);
+    if (few) k_lora_down_few<T, NR, WIDTH><<<grid, 1024 / NR, 0, st>>>(d);
+    else k_lora_down<T, NR, WIDTH><<<grid, 256, 0, st>>>(d);
 }
 
 int64_t tiles_of(const LoraDev& d, int t) { return (int64_t)((d.out + t - 1) / t) * ((d.rows + t - 1) / t); }
 
 // The largest tile that still gives every CU a block; few rows read W straight from memory.
-template <class T, bool RAGGED>
+template <class T, int WIDTH>
 hipError_t run(const LoraDev& d, hipStream_t st) {
     if (d.adapters > 0) {
-        if (d.rank <= 32)      down<T, 1, RAGGED>(d, st);
-        else if (d.rank <= 64) down<T, 2, RAGGED>(d, st);
-        else                   down<T, 4, RAGGED>(d, st);
+        if (d.rank <= 32)      down<T, 1, WIDTH>(d, st);
+        else if (d.rank <= 64) down<T, 2, WIDTH>(d, st);
+        else                   down<T, 4, WIDTH>(d, st);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     if (d.rows <= 64)
-        k_lora_rows<T, RAGGED><<<dim3((unsigned)((d.out + 31) / 32), (unsigned)((d.rows + 31) / 32)), 1024, 0, st>>>(d);
-    else if (!RAGGED && tiles_of(d, 256) >= kCUs)
-        k_lora_tile<T, 2, 4, 4, 2, false><<<(unsigned)tiles_of(d, 256), 512, 0, st>>>(d);
+        k_lora_rows<T, WIDTH><<<dim3((unsigned)((d.out + 31) / 32), (unsigned)((d.rows + 31) / 32)), 1024, 0, st>>>(d);
+    else if (WIDTH == kWhole && tiles_of(d, 256) >= kCUs)
+        k_lora_tile<T, 2, 4, 4, 2, kWhole><<<(unsigned)tiles_of(d, 256), 512, 0, st>>>(d);
     else if (tiles_of(d, 128) >= kCUs)
-        k_lora_tile<T, 2, 2, 2, 2, RAGGED><<<(unsigned)tiles_of(d, 128), 256, 0, st>>>(d);
+        k_lora_tile<T, 2, 2, 2, 2, WIDTH><<<(unsigned)tiles_of(d, 128), 256, 0, st>>>(d);
     else
-        k_lora_tile<T, 2, 2, 1, 1, RAGGED><<<(unsigned)tiles_of(d, 64), 256, 0, st>>>(d);
+        k_lora_tile<T, 2, 2, 1, 1, WIDTH><<<(unsigned)tiles_of(d, 64), 256, 0, st>>>(d);
     return hipGetLastError();
 }
 
@@ -442,8 +444,11 @@ hipError_t run(const LoraDev& d, hipStream_t st) {
 
 hipError_t lora_linear(const LoraDev& d, int dtype, hipStream_t st) {
     const bool ragged = d.in % 8 != 0 || d.rank % 8 != 0 || d.x_stride >= kBufferStride || d.w_stride >= kBufferStride;
-    if (dtype == PA_BF16) return ragged ? run<__bf16, true>(d, st) : run<__bf16, false>(d, st);
-    return ragged ? run<_Float16, true>(d, st) : run<_Float16, false>(d, st);
+    auto typed = [&](auto t) {
+        typedef decltype(t) T;
+        return d.in < 8 ? run<T, kTiny>(d, st) : ragged ? run<T, kRagged>(d, st) : run<T, kWhole>(d, st);
+    };
+    return dtype == PA_BF16 ? typed((__bf16)0) : typed((_Float16)0);
 }
 
 }  // namespace pa

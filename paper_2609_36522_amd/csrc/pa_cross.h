@@ -49,44 +49,46 @@ __device__ __forceinline__ float key_bias(const CrossDev& d, int b, int key) {
 }
 
 // A tile of ROWS rows, `stride` elements apart, on its way from memory to LDS.
-// KIND 0: buffer loads that write LDS themselves. A wave's 64 lanes fill consecutive 16-byte slots, so
-//   the permutation of a row's pieces is in the addresses that they read.
-// KIND 1: buffer loads into registers (the values can be changed before they are stored).
-// KIND 2: any stride, any head width.
-// With 0 and 1 (head_dim a multiple of 8, strides below kBufferStride) a thread's offset in the tile is
-// the same for every tile; pieces and rows that do not exist get an offset out of the buffer's range,
-// which reads as zero.
-constexpr int kDirect = 0, kRegs = 1, kRagged = 2;
-
-template <class T, int DP, int ROWS, int KIND>
+// WIDTH kWhole (head_dim a multiple of 8, strides below kBufferStride): buffer loads, whose offset in the
+//   tile is a thread's own for all tiles; pieces and rows that do not exist get an offset out of the
+//   buffer's range, which reads as zero. With DIRECT they write LDS themselves: a wave's 64 lanes fill
+//   consecutive 16-byte slots, so the permutation of a row's pieces is in the addresses that they read.
+//   Without it they go through registers, where the values can be changed.
+// Otherwise: any stride, any head width.
+template <class T, int DP, int ROWS, int WIDTH, bool DIRECT>
 struct Stage {
     static constexpr int kPieces = ROWS * (DP / 8) / kThreads, kPerRow = DP / 8, kStep = kThreads / kPerRow;
-    uint4 r[KIND == kDirect ? 1 : kPieces];
+    uint4 r[DIRECT ? 1 : kPieces];
     uint32_t off;
+    int rows;
 
     __device__ __forceinline__ static int row(int i) { return (int)threadIdx.x / kPerRow + i * kStep; }
     // The thread's piece of its rows. The permutation repeats every 16 rows, and kStep is 16 or 32.
     __device__ __forceinline__ static int piece() {
         const int p = (int)threadIdx.x % kPerRow;
-        return KIND == kDirect ? (piece_at<DP>(row(0), p) - row(0) * DP) >> 3 : p;
+        return DIRECT ? (piece_at<DP>(row(0), p) - row(0) * DP) >> 3 : p;
     }
 
     __device__ __forceinline__ Stage(int dim, int64_t stride)
         : off(piece() * 8 < dim ? (uint32_t)(row(0) * (int)stride + piece() * 8) * 2 : kNowhere) {}
 
-    // Starts the tile at `base`, of which `rows` rows exist, on its way.
-    __device__ __forceinline__ void load(const T* base, int64_t stride, int rows, int dim, T* tile) {
-        if constexpr (KIND == kRagged) {
+    // Starts the tile at `base`, of which n (at least 1) rows exist, on its way.
+    __device__ __forceinline__ void load(const T* base, int64_t stride, int n, int dim, T* tile) {
+        rows = n;
+        if constexpr (WIDTH != kWhole) {
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i)
-                r[i] = __builtin_bit_cast(uint4, load8_raw(base + row(i) * stride, piece() * 8, dim, row(i) < rows));
+            for (int i = 0; i < kPieces; ++i) {
+                const T* p = base + (row(i) < rows ? row(i) : 0) * stride;
+                r[i] = WIDTH == kRagged ? __builtin_bit_cast(uint4, load8_raw(p, piece() * 8, dim))
+                                        : __builtin_bit_cast(uint4, load8(p, piece() * 8, dim, row(i) < rows));
+            }
         } else {
             const __amdgpu_buffer_rsrc_t from = buffer_at(base);
             const int step = kStep * (int)stride * 2;
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {
                 const uint32_t at = row(i) < rows ? off : kNowhere;
-                if constexpr (KIND == kDirect) {
+                if constexpr (DIRECT) {
                     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
                     load_lds(from, tile + (w * 64 + i * kThreads) * 8, at, i * step);
                 } else {
@@ -97,12 +99,12 @@ struct Stage {
     }
     // The tile is in LDS once every thread has called this and a barrier has passed.
     __device__ __forceinline__ void arrive(T* tile, int dim) {
-        if constexpr (KIND == kRagged) {
+        if constexpr (WIDTH == kRagged) {
 #pragma unroll
             for (int i = 0; i < kPieces; ++i)
-                r[i] = __builtin_bit_cast(uint4, fix8(__builtin_bit_cast(Pack8<T>, r[i]), piece() * 8, dim));
+                r[i] = __builtin_bit_cast(uint4, fix8(__builtin_bit_cast(Pack8<T>, r[i]), piece() * 8, dim, row(i) < rows));
         }
-        if constexpr (KIND == kDirect) {
+        if constexpr (DIRECT) {
             wait_loads();
         } else {
 #pragma unroll
@@ -113,9 +115,9 @@ struct Stage {
 
 // Keys and values of a tile; with MASKED zeros where a key is not visible (0 weight times an infinity or
 // a NaN would not be 0), and the keys' biases.
-template <class T, int DP, int KEYS, bool MASKED, int KIND>
+template <class T, int DP, int KEYS, bool MASKED, int WIDTH, bool DIRECT>
 struct KvStage {
-    typedef Stage<T, DP, KEYS, KIND> S;
+    typedef Stage<T, DP, KEYS, WIDTH, DIRECT> S;
     S k, v;
     float bias, seen[MASKED ? S::kPieces : 1];
 
@@ -146,34 +148,33 @@ struct KvStage {
     }
 };
 
-// How a kernel's K and V tiles travel.
-template <bool MASKED, bool RAGGED>
-constexpr int kKvKind = RAGGED ? kRagged : MASKED ? kRegs : kDirect;
-
-// B operands of one row for all reduction steps: elements 16 ks + 8 half .. of the row at p.
-template <class T, int KS, bool RAGGED>
+// B operands of one row for all reduction steps: elements 16 ks + 8 half .. of the row at p (which exists
+// also where it is not valid).
+template <class T, int KS, int WIDTH>
 __device__ __forceinline__ void load_row(typename Vec<T>::v8 (&out)[KS], const T* p, int dim, int half, bool valid) {
     typedef typename Vec<T>::v8 v8;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
         const int at = ks * 16 + half * 8;
-        if constexpr (RAGGED) {
-            out[ks] = __builtin_bit_cast(v8, load8_raw(p, at, dim, valid));
+        if constexpr (WIDTH == kRagged) {
+            out[ks] = __builtin_bit_cast(v8, load8_raw(p, at, dim));
+        } else if constexpr (WIDTH == kTiny) {
+            out[ks] = __builtin_bit_cast(v8, load8(p, at, dim, valid));
         } else {
             uint4 r = make_uint4(0, 0, 0, 0);
             if (valid && at < dim) r = __builtin_bit_cast(uint4, *reinterpret_cast<const Pack8<T>*>(p + at));
             out[ks] = __builtin_bit_cast(v8, r);
         }
     }
-    if constexpr (RAGGED) {
+    if constexpr (WIDTH == kRagged) {
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks)
-            out[ks] = __builtin_bit_cast(v8, fix8(__builtin_bit_cast(Pack8<T>, out[ks]), ks * 16 + half * 8, dim));
+            out[ks] = __builtin_bit_cast(v8, fix8(__builtin_bit_cast(Pack8<T>, out[ks]), ks * 16 + half * 8, dim, valid));
     }
 }
 
 // Stores a transposed accumulator (lane = row of the output) times f to the row at `out`.
-template <class T, int DB, bool RAGGED>
+template <class T, int DB, int WIDTH>
 __device__ __forceinline__ void store_row(T* out, int dim, const f32x16* acc, float f, int half, bool valid) {
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
@@ -181,7 +182,7 @@ __device__ __forceinline__ void store_row(T* out, int dim, const f32x16* acc, fl
         for (int j = 0; j < 2; ++j) {
             const Pack8<T> p = gather8<T>(acc[db], j, f);   // every lane takes part in the exchange
             const int c = db * 32 + j * 16 + half * 8;
-            if constexpr (RAGGED) {
+            if constexpr (WIDTH != kWhole) {
                 if (valid) store8(out + c, p, dim - c);
             } else {
                 if (valid && c < dim) *reinterpret_cast<Pack8<T>*>(out + c) = p;
@@ -251,32 +252,34 @@ __device__ __forceinline__ Work work_at(const CrossDev& d) {
 // largest product), scores are formed before the maximum is taken.
 inline bool masked(const CrossDev& d) { return d.mask_kind != PA_MASK_NONE || !(d.scale > 0.0f); }
 
-inline bool ragged(const CrossDev& d) {
+inline int width_of(const CrossDev& d) {
+    if (d.dim < 8) return kTiny;
     for (const int64_t* p : {d.qs, d.ks, d.vs, d.os, d.dos, d.dqs, d.dks, d.dvs})
-        if (p[1] >= kBufferStride) return true;
-    return d.dim % 8 != 0;
+        if (p[1] >= kBufferStride) return kRagged;
+    return d.dim % 8 != 0 ? kRagged : kWhole;
 }
 
 inline unsigned blocks_for(int64_t n, int each) { return (unsigned)((n + each - 1) / each); }
 
-// Calls f(type, reduction steps of 16 over the head, masked, ragged): head widths are padded to 64, 80,
-// 96 or 128, ragged ones to 64 or 128.
+// Calls f(type, reduction steps of 16 over the head, masked, width): head widths are padded to 64, 80, 96 or
+// 128, ragged ones to 64 or 128.
 template <class F>
 hipError_t dispatch(const CrossDev& d, int dtype, F f) {
-    const bool m = masked(d), r = ragged(d);
-    auto with = [&](auto t, auto ks) {
-        return m ? f(t, ks, std::true_type{}, std::false_type{}) : f(t, ks, std::false_type{}, std::false_type{});
+    const bool m = masked(d);
+    const int width = width_of(d);
+    auto with = [&](auto t, auto ks, auto wd) { return m ? f(t, ks, std::true_type{}, wd) : f(t, ks, std::false_type{}, wd); };
+    auto typed = [&](auto t) {
+        const std::integral_constant<int, 4> k4;
+        const std::integral_constant<int, 8> k8;
+        const std::integral_constant<int, kWhole> whole;
+        const std::integral_constant<int, kRagged> rag;
+        if (width == kTiny) return with(t, k4, std::integral_constant<int, kTiny>{});
+        if (width == kRagged) return d.dim > 64 ? with(t, k8, rag) : with(t, k4, rag);
+        if (d.dim <= 64) return with(t, k4, whole);
+        if (d.dim <= 80) return with(t, std::integral_constant<int, 5>{}, whole);
+        return d.dim <= 96 ? with(t, std::integral_constant<int, 6>{}, whole) : with(t, k8, whole);
     };
-    auto with_ragged = [&](auto t, auto ks) {
-        return m ? f(t, ks, std::true_type{}, std::true_type{}) : f(t, ks, std::false_type{}, std::true_type{});
-    };
-    auto width = [&](auto t) {
-        if (r) return d.dim > 64 ? with_ragged(t, std::integral_constant<int, 8>{}) : with_ragged(t, std::integral_constant<int, 4>{});
-        if (d.dim <= 64) return with(t, std::integral_constant<int, 4>{});
-        if (d.dim <= 80) return with(t, std::integral_constant<int, 5>{});
-        return d.dim <= 96 ? with(t, std::integral_constant<int, 6>{}) : with(t, std::integral_constant<int, 8>{});
-    };
-    return dtype == PA_BF16 ? width((__bf16)0) : width((_Float16)0);
+    return dtype == PA_BF16 ? typed((__bf16)0) : typed((_Float16)0);
 }
 
 }  // namespace

@@ -42,18 +42,34 @@ __device__ __forceinline__ Pack8<T> shift8(Pack8<T> r, int n) {
     }
 }
 
-// Elements at .. at + 7 of a row of len elements, zeros past its end and in an invalid row. A piece
-// that reaches past the end is read as the row's last eight elements and moved down (fix8), so that no
-// element outside the row is touched and the load stays one access. load8_raw starts the load, fix8
-// waits for it. len is the same in all lanes.
+// Elements at .. at + 7 of a row of len elements, zeros past its end and in an invalid row. No element
+// outside the row is touched: a piece that reaches past the end is read as the row's last eight elements
+// and moved down. Two halves, so that several loads can be in flight: load8_raw starts the load (without
+// a branch; `row` has to exist even where the result is to be zero), fix8 waits for it. Both need
+// len >= 8; load8 takes any length. len is the same in all lanes.
 template <class T>
-__device__ __forceinline__ Pack8<T> load8_raw(const T* row, int at, int len, bool valid = true) {
+__device__ __forceinline__ Pack8<T> load8_raw(const T* row, int at, int len) {
+    return *reinterpret_cast<const Pack8<T>*>(row + (at + 8 <= len ? at : len - 8));
+}
+
+template <class T>
+__device__ __forceinline__ Pack8<T> fix8(Pack8<T> r, int at, int len, bool valid = true) {
+    const int n = valid ? len - at : 0;
+    if (len & 7) r = shift8(r, n > 0 && n < 8 ? 8 - n : 0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.v[i] = n > 0 ? r.v[i] : (T)0.0f;
+    return r;
+}
+
+template <class T>
+__device__ __forceinline__ Pack8<T> load8(const T* row, int at, int len, bool valid = true) {
     Pack8<T> r;
     const int n = valid ? len - at : 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) r.v[i] = (T)0.0f;
     if (len >= 8) {
-        if (n > 0) r = *reinterpret_cast<const Pack8<T>*>(row + (n >= 8 ? at : len - 8));
+        if (n > 0) r = load8_raw(row, at, len);
+        if (len & 7) r = shift8(r, n > 0 && n < 8 ? 8 - n : 0);
     } else {
 #pragma unroll
         for (int i = 0; i < 7; ++i)
@@ -62,16 +78,9 @@ __device__ __forceinline__ Pack8<T> load8_raw(const T* row, int at, int len, boo
     return r;
 }
 
-template <class T>
-__device__ __forceinline__ Pack8<T> fix8(const Pack8<T>& r, int at, int len) {
-    if (len < 8 || (len & 7) == 0) return r;
-    return shift8(r, at < len && at + 8 > len ? at + 8 - len : 0);
-}
-
-template <class T>
-__device__ __forceinline__ Pack8<T> load8(const T* row, int at, int len, bool valid = true) {
-    return fix8(load8_raw(row, at, len, valid), at, len);
-}
+// How the rows of a kernel's operands are read: rows of a multiple of 8 elements, of any 8 or more, or
+// shorter ones.
+constexpr int kWhole = 0, kRagged = 1, kTiny = 2;
 
 template <class T>
 __device__ __forceinline__ void store8(T* p, const Pack8<T>& r, int n) {
