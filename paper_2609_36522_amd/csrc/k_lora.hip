@@ -34,15 +34,14 @@ __device__ __forceinline__ int adapter_of(const LoraDev& d, int i) {
     return a >= 0 && a < d.adapters ? a : -1;
 }
 
-// First request whose end lies beyond `row` (d.requests if none).
+// First request whose end lies beyond `row` (d.requests if none): a wave looks at 64 requests at a time.
 __device__ __forceinline__ int request_from(const LoraDev& d, int row) {
-    int lo = 0, hi = d.requests;
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (offset_at(d, mid + 1) > row) hi = mid;
-        else lo = mid + 1;
+    const int lane = threadIdx.x & 63;
+    for (int i = 0; i < d.requests; i += 64) {
+        const unsigned long long beyond = __ballot(i + lane < d.requests && offset_at(d, i + lane + 1) > row);
+        if (beyond) return i + __builtin_ctzll(beyond);
     }
-    return lo;
+    return d.requests;
 }
 
 // Eight elements at .. of an existing row of len, whole after `fixed`.
@@ -101,11 +100,9 @@ struct Stage {
             }
         }
     }
-    // The tile is in LDS once every thread has called this and a barrier has passed.
+    // Registers into LDS (kWhole: nothing to do, the loads are waited for by the caller).
     __device__ __forceinline__ void arrive(T* tile) {
-        if constexpr (WIDTH == kWhole) {
-            wait_loads();
-        } else {
+        if constexpr (WIDTH != kWhole) {
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {
                 if constexpr (WIDTH == kRagged)
@@ -117,17 +114,19 @@ struct Stage {
 };
 
 // t of 64 rows of one request: block (c, i) takes rows 64 c .. of request i, all of them if the grid is
-// smaller. Of the four waves two take 32 rows each, over half of the reduction; NR 32-row tiles of A.
+// smaller. Of the four waves two take 32 rows each, over half of the reduction; NR 32-row tiles of A. Bound by
+// the reading of x: three parts of 64 columns are on their way during the products of the current one.
 template <class T, int NR, int WIDTH>
 __global__ __launch_bounds__(256) void k_lora_down(LoraDev d) {
-    constexpr int ROWS = 64;
-    __shared__ __align__(16) T tiles[2][(ROWS + NR * 32) * 64];
-    __shared__ float part[NR * 32][ROWS + 1];
+    constexpr int ROWS = 64, STAGES = WIDTH == kWhole ? 4 : 2, PART = (ROWS + NR * 32) * 64, LOADS = (ROWS + NR * 32) * 8 / 256;
+    static_assert(STAGES * PART * 2 >= NR * 32 * (ROWS + 1) * 4, "the halves of the reduction are joined in the tiles' memory");
+    __shared__ __align__(16) T tiles[STAGES * PART];
+    float (*join)[ROWS + 1] = reinterpret_cast<float (*)[ROWS + 1]>(tiles);
     const int i = blockIdx.y, ad = adapter_of(d, i);
     if (ad < 0) return;
     const int beg = offset_at(d, i), end = offset_at(d, i + 1);
     const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6, rw = w & 1, kw = w >> 1;
-    const int K = d.in;
+    const int K = d.in, parts = (K + 63) / 64;
     const T* a = static_cast<const T*>(d.a) + (int64_t)ad * d.rank * K;
     const float s = d.scales ? d.scales[ad] : 1.0f;
     for (int r0 = beg + blockIdx.x * ROWS; r0 < end; r0 += gridDim.x * ROWS) {
@@ -137,35 +136,45 @@ __global__ __launch_bounds__(256) void k_lora_down(LoraDev d) {
         f32x16 acc[NR];
 #pragma unroll
         for (int n = 0; n < NR; ++n) acc[n] = f32x16{};
-        auto load = [&](int k0, int p) {
-            sx.load(x, d.x_stride, k0, tiles[p]);
-            sa.load(a, K, k0, tiles[p] + ROWS * 64);
+        auto load = [&](int part, int p) {
+            sx.load(x, d.x_stride, part * 64, tiles + p * PART);
+            sa.load(a, K, part * 64, tiles + p * PART + ROWS * 64);
         };
         auto arrive = [&](int p) {
-            sx.arrive(tiles[p]);
-            sa.arrive(tiles[p] + ROWS * 64);
+            sx.arrive(tiles + p * PART);
+            sa.arrive(tiles + p * PART + ROWS * 64);
         };
-        load(0, 0);
+#pragma unroll
+        for (int n = 0; n < STAGES - 1; ++n)
+            if (n < parts) load(n, n);
+        if (parts >= STAGES - 1) wait_loads<(STAGES - 2) * LOADS>();
+        else wait_loads();
         arrive(0);
-        __syncthreads();
-        int p = 0;
-        for (int k0 = 0; k0 < K; k0 += 64, p ^= 1) {
-            if (k0 + 64 < K) load(k0 + 64, p ^ 1);
+        lds_barrier();
+        for (int n = 0; n < parts; ++n) {
+            const T* xt = tiles + n % STAGES * PART;
+            const T* at = xt + ROWS * 64;
+            const int q = (n + STAGES - 1) % STAGES;
+            if (n + STAGES - 1 < parts) load(n + STAGES - 1, q);
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
-                const auto xv = read_rows<T, 64>(tiles[p], rw * 32 + (lane & 31), kw * 2 + ks, half);
+                const auto xv = read_rows<T, 64>(xt, rw * 32 + (lane & 31), kw * 2 + ks, half);
 #pragma unroll
-                for (int n = 0; n < NR; ++n)
-                    acc[n] = mma(read_rows<T, 64>(tiles[p] + ROWS * 64, n * 32 + (lane & 31), kw * 2 + ks, half), xv, acc[n]);
+                for (int m = 0; m < NR; ++m)
+                    acc[m] = mma(read_rows<T, 64>(at, m * 32 + (lane & 31), kw * 2 + ks, half), xv, acc[m]);
             }
-            if (k0 + 64 < K) arrive(p ^ 1);
-            __syncthreads();
+            if (n + 1 < parts) {
+                if (n + STAGES - 1 < parts) wait_loads<(STAGES - 2) * LOADS>();      // the next part is there
+                else wait_loads();
+                arrive(q);
+            }
+            lds_barrier();
         }
         if (kw == 1) {
 #pragma unroll
             for (int n = 0; n < NR; ++n)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) part[n * 32 + 8 * (r >> 2) + 4 * half + (r & 3)][rw * 32 + (lane & 31)] = acc[n][r];
+                for (int r = 0; r < 16; ++r) join[n * 32 + 8 * (r >> 2) + 4 * half + (r & 3)][rw * 32 + (lane & 31)] = acc[n][r];
         }
         __syncthreads();
         if (kw == 0) {
@@ -174,7 +183,7 @@ __global__ __launch_bounds__(256) void k_lora_down(LoraDev d) {
 #pragma unroll
             for (int n = 0; n < NR; ++n) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) acc[n][r] += part[n * 32 + 8 * (r >> 2) + 4 * half + (r & 3)][rw * 32 + (lane & 31)];
+                for (int r = 0; r < 16; ++r) acc[n][r] += join[n * 32 + 8 * (r >> 2) + 4 * half + (r & 3)][rw * 32 + (lane & 31)];
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
                     const Pack8<T> o = gather8<T>(acc[n], q, s);
@@ -244,12 +253,12 @@ __global__ __launch_bounds__(1024 / NR) void k_lora_down_few(LoraDev d) {
 }
 
 // The adapters' part of NM x NX 32 x 32 tiles: features f0 + 32 i + .., rows r0 + 32 j + ..; every
-// `step`-th request from the `first`-th of those that have rows here.
+// `step`-th request from `first`, the first that has rows at r0 or after.
 template <class T, int NM, int NX, int WIDTH>
-__device__ __forceinline__ void add_adapters(const LoraDev& d, int f0, int r0, int lane, f32x16 (&acc)[NM][NX], int first = 0, int step = 1) {
+__device__ __forceinline__ void add_adapters(const LoraDev& d, int f0, int r0, int lane, f32x16 (&acc)[NM][NX], int first, int step = 1) {
     typedef typename Vec<T>::v8 v8;
     const int half = lane >> 5, r1 = r0 + 32 * NX < d.rows ? r0 + 32 * NX : d.rows;
-    for (int i = request_from(d, r0) + first; i < d.requests; i += step) {
+    for (int i = first; i < d.requests; i += step) {
         const int beg = offset_at(d, i), end = offset_at(d, i + 1);
         if (beg >= r1) break;
         const int ad = adapter_of(d, i);
@@ -276,21 +285,27 @@ __device__ __forceinline__ void add_adapters(const LoraDev& d, int f0, int r0, i
     }
 }
 
-// Adds the bias and stores NM x NX tiles.
+// Accumulators that start from the bias.
+template <class T, int NM, int NX>
+__device__ __forceinline__ void start(const LoraDev& d, int f0, int lane, f32x16 (&acc)[NM][NX]) {
+    const int half = lane >> 5;
+#pragma unroll
+    for (int m = 0; m < NM; ++m)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int f = f0 + m * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
+            const float v = d.bias ? (float)static_cast<const T*>(d.bias)[f < d.out ? f : 0] : 0.0f;
+#pragma unroll
+            for (int j = 0; j < NX; ++j) acc[m][j][r] = v;
+        }
+}
+
+// Stores NM x NX tiles.
 template <class T, int NM, int NX>
 __device__ __forceinline__ void finish(const LoraDev& d, int f0, int r0, int lane, f32x16 (&acc)[NM][NX]) {
     const int half = lane >> 5;
 #pragma unroll
     for (int m = 0; m < NM; ++m) {
-        if (d.bias) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int f = f0 + m * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
-                const float bv = f < d.out ? (float)static_cast<const T*>(d.bias)[f] : 0.0f;
-#pragma unroll
-                for (int j = 0; j < NX; ++j) acc[m][j][r] += bv;
-            }
-        }
 #pragma unroll
         for (int j = 0; j < NX; ++j) {
             const int row = r0 + j * 32 + (lane & 31);
@@ -306,60 +321,82 @@ __device__ __forceinline__ void finish(const LoraDev& d, int f0, int r0, int lan
 }
 
 // WF x WR waves of NM x NX tiles of 32 x 32 (features x rows) per block. The reduction goes through LDS in
-// parts of 64 columns, double buffered: the next part's loads are in flight during the products of the
-// current one.
-template <class T, int WF, int WR, int NM, int NX, int WIDTH>
-__global__ __launch_bounds__(64 * WF * WR, 2) void k_lora_tile(LoraDev d) {
+// parts of 64 columns, of which STAGES - 1 are on their way during the products of the current one.
+template <class T, int WF, int WR, int NM, int NX, int STAGES, int WIDTH>
+__global__ __launch_bounds__(64 * WF * WR, NM * NX == 16 ? 1 : 2) void k_lora_tile(LoraDev d) {
     typedef typename Vec<T>::v8 v8;
     constexpr int TF = WF * NM * 32, TR = WR * NX * 32, THREADS = 64 * WF * WR;
-    __shared__ __align__(16) T tiles[2][(TF + TR) * 64];
+    static_assert(WIDTH == kWhole || STAGES == 2, "registers hold one part");
+    __shared__ __align__(16) T tiles[STAGES][(TF + TR) * 64];
     const int f_tiles = (d.out + TF - 1) / TF;
     const int id = xcd_order(blockIdx.x, gridDim.x);
     const int f0 = (id % f_tiles) * TF, r0 = (id / f_tiles) * TR;
     const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6;
-    const int K = d.in;
+    const int K = d.in, parts = (K + 63) / 64;
     const T* wp = static_cast<const T*>(d.w) + (int64_t)f0 * d.w_stride;
     const T* xp = static_cast<const T*>(d.x) + (int64_t)r0 * d.x_stride;
     Stage<T, TF, THREADS, WIDTH> sw(d.w_stride, d.out - f0, K);
     Stage<T, TR, THREADS, WIDTH> sx(d.x_stride, d.rows - r0, K);
-    auto load = [&](int k0, int p) {
-        sw.load(wp, d.w_stride, k0, tiles[p]);
-        sx.load(xp, d.x_stride, k0, tiles[p] + TF * 64);
+    constexpr int LOADS = (TF + TR) * 8 / THREADS;       // a thread's loads of one part
+    auto load = [&](int i, int p) {
+        sw.load(wp, d.w_stride, i * 64, tiles[p]);
+        sx.load(xp, d.x_stride, i * 64, tiles[p] + TF * 64);
     };
     auto arrive = [&](int p) {
         sw.arrive(tiles[p]);
         sx.arrive(tiles[p] + TF * 64);
     };
     f32x16 acc[NM][NX];
-#pragma unroll
-    for (int m = 0; m < NM; ++m)
-#pragma unroll
-        for (int j = 0; j < NX; ++j) acc[m][j] = f32x16{};
     const int fw = (w % WF) * NM * 32, rw = (w / WF) * NX * 32;
-    load(0, 0);
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i)
+        if (i < parts) load(i, i);
+    start<T, NM, NX>(d, f0 + fw, lane, acc);
+    const int first = d.adapters > 0 ? request_from(d, r0 + rw) : 0;
+    if (parts >= STAGES - 1) wait_loads<(STAGES - 2) * LOADS>();
+    else wait_loads();
     arrive(0);
-    __syncthreads();
+    lds_barrier();
     int p = 0;
-    for (int k0 = 0; k0 < K; k0 += 64, p ^= 1) {
-        if (k0 + 64 < K) load(k0 + 64, p ^ 1);
+    for (int i = 0; i < parts; ++i) {
+        int q = p + STAGES - 1;
+        if (q >= STAGES) q -= STAGES;
+        if (i + STAGES - 1 < parts) load(i + STAGES - 1, q);
         const T* wt = tiles[p];
         const T* xt = tiles[p] + TF * 64;
+        // The operands of the next 16 columns are read while those of the current ones are multiplied.
+        v8 a[2][NM], b[2][NX];
+        auto read = [&](int ks) {
+#pragma unroll
+            for (int m = 0; m < NM; ++m) a[ks & 1][m] = read_rows<T, 64>(wt, fw + m * 32 + (lane & 31), ks, half);
+#pragma unroll
+            for (int j = 0; j < NX; ++j) b[ks & 1][j] = read_rows<T, 64>(xt, rw + j * 32 + (lane & 31), ks, half);
+        };
+        read(0);
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) {
-            v8 a[NM], b[NX];
-#pragma unroll
-            for (int m = 0; m < NM; ++m) a[m] = read_rows<T, 64>(wt, fw + m * 32 + (lane & 31), ks, half);
-#pragma unroll
-            for (int j = 0; j < NX; ++j) b[j] = read_rows<T, 64>(xt, rw + j * 32 + (lane & 31), ks, half);
+            if (ks < 3) read(ks + 1);
 #pragma unroll
             for (int m = 0; m < NM; ++m)
 #pragma unroll
-                for (int j = 0; j < NX; ++j) acc[m][j] = mma(a[m], b[j], acc[m][j]);
+                for (int j = 0; j < NX; ++j) acc[m][j] = mma(a[ks & 1][m], b[ks & 1][j], acc[m][j]);
+            if (ks < 3) {
+#pragma unroll
+                for (int g = 0; g < NM + NX; ++g) {
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                      // one LDS read
+                    __builtin_amdgcn_sched_group_barrier(0x008, NM * NX / (NM + NX), 0);     // some products
+                }
+            }
         }
-        if (k0 + 64 < K) arrive(p ^ 1);
-        __syncthreads();
+        if (i + 1 < parts) {
+            if (i + STAGES - 1 < parts) wait_loads<(STAGES - 2) * LOADS>();      // the next part is there
+            else wait_loads();
+            arrive(q);
+        }
+        lds_barrier();
+        if (++p == STAGES) p = 0;
     }
-    if (d.adapters > 0) add_adapters<T, NM, NX, WIDTH>(d, f0 + fw, r0 + rw, lane, acc);
+    if (d.adapters > 0) add_adapters<T, NM, NX, WIDTH>(d, f0 + fw, r0 + rw, lane, acc, first);
     finish<T, NM, NX>(d, f0 + fw, r0 + rw, lane, acc);
 }
 
@@ -374,7 +411,9 @@ __global__ __launch_bounds__(1024) void k_lora_rows(LoraDev d) {
     const int K = d.in, f = f0 + (lane & 31), row = r0 + (lane & 31);
     const T* wp = static_cast<const T*>(d.w) + (int64_t)(f < d.out ? f : 0) * d.w_stride;
     const T* xp = static_cast<const T*>(d.x) + (int64_t)(row < d.rows ? row : 0) * d.x_stride;
+    const int first = d.adapters > 0 ? request_from(d, r0) : 0;
     f32x16 acc[1][1] = {{f32x16{}}};
+    if (w == 0) start<T, 1, 1>(d, f0, lane, acc);
     for (int k0 = w * 64; k0 < K; k0 += 1024) {
         v8 wv[4], xv[4];
 #pragma unroll
@@ -389,7 +428,7 @@ __global__ __launch_bounds__(1024) void k_lora_rows(LoraDev d) {
             acc[0][0] = mma(fixed<T, WIDTH>(wv[ks], k, K, f < d.out), fixed<T, WIDTH>(xv[ks], k, K, row < d.rows), acc[0][0]);
         }
     }
-    if (d.adapters > 0) add_adapters<T, 1, 1, WIDTH>(d, f0, r0, lane, acc, w, 16);
+    if (d.adapters > 0) add_adapters<T, 1, 1, WIDTH>(d, f0, r0, lane, acc, first + w, 16);
 #pragma unroll
     for (int r = 0; r < 16; ++r) part[w][r][lane] = acc[0][0][r];
     __syncthreads();
@@ -432,11 +471,13 @@ hipError_t run(const LoraDev& d, hipStream_t st) {
     if (d.rows <= 64)
         k_lora_rows<T, WIDTH><<<dim3((unsigned)((d.out + 31) / 32), (unsigned)((d.rows + 31) / 32)), 1024, 0, st>>>(d);
     else if (WIDTH == kWhole && tiles_of(d, 256) >= kCUs)
-        k_lora_tile<T, 2, 4, 4, 2, kWhole><<<(unsigned)tiles_of(d, 256), 512, 0, st>>>(d);
+        k_lora_tile<T, 2, 4, 4, 2, 2, kWhole><<<(unsigned)tiles_of(d, 256), 512, 0, st>>>(d);
+    else if (WIDTH == kWhole && (int64_t)((d.out + 255) / 256) * ((d.rows + 127) / 128) >= kCUs)
+        k_lora_tile<T, 4, 2, 2, 2, 3, kWhole><<<(unsigned)((int64_t)((d.out + 255) / 256) * ((d.rows + 127) / 128)), 512, 0, st>>>(d);
     else if (tiles_of(d, 128) >= kCUs)
-        k_lora_tile<T, 2, 2, 2, 2, WIDTH><<<(unsigned)tiles_of(d, 128), 256, 0, st>>>(d);
+        k_lora_tile<T, 2, 2, 2, 2, 2, WIDTH><<<(unsigned)tiles_of(d, 128), 256, 0, st>>>(d);
     else
-        k_lora_tile<T, 2, 2, 1, 1, WIDTH><<<(unsigned)tiles_of(d, 64), 256, 0, st>>>(d);
+        k_lora_tile<T, 2, 2, 1, 1, WIDTH == kWhole ? 4 : 2, WIDTH><<<(unsigned)tiles_of(d, 64), 256, 0, st>>>(d);
     return hipGetLastError();
 }
 

@@ -108,7 +108,16 @@ __device__ __forceinline__ void load_lds(__amdgpu_buffer_rsrc_t from, void* lds,
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)lds, 16, off, base_off, 0, 0);
 }
 
-__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }   // vmcnt(0)
+// Waits until at most N of the wave's loads are in flight (they complete in order).
+template <int N = 0>
+__device__ __forceinline__ void wait_loads() {
+    static_assert(N < 64);
+    __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4 << 14));
+}
+
+// A barrier for data in LDS: the wave's own LDS accesses are done, its loads (those that write LDS included:
+// see wait_loads) stay in flight, where __syncthreads waits for them all.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 __device__ __forceinline__ float wave_sum_f32(float v) {
 #pragma unroll
