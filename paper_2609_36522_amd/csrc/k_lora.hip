@@ -103,9 +103,10 @@ struct Stage {
     // Registers into LDS (kWhole: nothing to do, the loads are waited for by the caller).
     __device__ __forceinline__ void arrive(T* tile) {
         if constexpr (WIDTH != kWhole) {
+            const bool whole = at - piece * 8 + 64 <= len && rows >= ROWS;      // nothing to fix (the same in all lanes)
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {
-                if constexpr (WIDTH == kRagged)
+                if (WIDTH == kRagged && !whole)
                     r[i] = __builtin_bit_cast(uint4, fix8(__builtin_bit_cast(Pack8<T>, r[i]), at, len, row + i * kStep < rows));
                 *reinterpret_cast<uint4*>(tile + piece_at<64>(row + i * kStep, piece)) = r[i];
             }
@@ -448,8 +449,9 @@ __global__ __launch_bounds__(1024) void k_lora_rows(LoraDev d) {
 template <class T, int NR, int WIDTH>
 void down(const LoraDev& d, hipStream_t st) {
     // Blocks per request: its share of the rows, so that the launch has about rows / 64 (or 32) of them.
-    // Requests of fewer than 64 rows on average are latency bound.
-    const bool few = d.rows < 64 * d.requests;
+    // Where those of 64 rows are fewer than the CUs, or requests shorter, latency counts (1999 rows: 42 us in
+    // blocks of 64 rows, 14 in blocks of 32; 8192: 11.8 and 11.6; 32768: 32 and 77).
+    const bool few = d.rows < 64 * kCUs || d.rows < 64 * d.requests;
     const int per = d.rows / (few ? 32 : 64) / d.requests + 1;
     const dim3 grid((unsigned)(per < 4096 ? per : 4096), (unsigned)d.requests);
     if (few) k_lora_down_few<T, NR, WIDTH><<<grid, 1024 / NR, 0, st>>>(d);

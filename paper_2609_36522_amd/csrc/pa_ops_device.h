@@ -56,9 +56,13 @@ template <class T>
 __device__ __forceinline__ Pack8<T> fix8(Pack8<T> r, int at, int len, bool valid = true) {
     const int n = valid ? len - at : 0;
     if (len & 7) r = shift8(r, n > 0 && n < 8 ? 8 - n : 0);
+    struct Words {
+        uint32_t w[2 * sizeof(T)];
+    };
+    Words q = __builtin_bit_cast(Words, r);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r.v[i] = n > 0 ? r.v[i] : (T)0.0f;
-    return r;
+    for (int i = 0; i < (int)(2 * sizeof(T)); ++i) q.w[i] = n > 0 ? q.w[i] : 0;
+    return __builtin_bit_cast(Pack8<T>, q);
 }
 
 template <class T>
