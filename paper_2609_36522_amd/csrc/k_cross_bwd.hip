@@ -9,16 +9,37 @@ namespace pa {
 
 namespace {
 
-// delta = sum of do * o over a head: 16 lanes per row of [batch][q_heads][q_len].
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_cross_delta(CrossDev d) {
+// A row's statistics (m, log of the sum) as the backward pass uses them: without a mask hi = log2 of the sum
+// of all weights (lo unused), with one the maximum and the log2 of the sum past it apart. A row that sees
+// no key has weights 0 whatever its scores.
+template <int MASK>
+__device__ __forceinline__ void row_stats(float m, float ll, float& hi, float& lo) {
+    const bool empty = ll == -INFINITY;
+    hi = MASK ? (empty ? 0.0f : m) : (empty ? INFINITY : (m + ll) * kLog2e);
+    lo = empty ? INFINITY : ll * kLog2e;
+}
+template <int MASK>
+__device__ __forceinline__ float weight(float s, float scale, float f, float bias, float hi, float lo) {
+    return __builtin_amdgcn_exp2f(MASK ? fmaf(fmaf(s, scale, bias) - hi, kLog2e, -lo) : fmaf(s, f, -hi));
+}
+
+// Where dk, dv find the statistics of 32 tokens of a query head: hi, lo and delta, 32 of each.
+__device__ __forceinline__ float* tile_stats(const CrossDev& d, int b, RowAt r) {
+    const int64_t head = (int64_t)b * d.q_heads + r.head, tiles = (d.q_len + 31) / 32;
+    return d.row_stats + (head * tiles + (r.token >> 5)) * 96 + (r.token & 31);
+}
+
+// The rows' statistics where dq, which writes them on its way, is not asked for: 16 lanes per row of
+// [batch][q_len][q_heads].
+template <class T, int MASK>
+__global__ __launch_bounds__(kThreads) void k_cross_stats(CrossDev d) {
     const int64_t n = (int64_t)d.batch * d.q_heads * d.q_len;
     const int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
     const int64_t at = i < n ? i : n - 1;
     const int c = (threadIdx.x & 15) * 8;
-    // Tokens outermost, as the tensors usually lie.
     const int h = (int)(at % d.q_heads);
-    const int64_t bt = at / d.q_heads, t = bt % d.q_len, b = bt / d.q_len;
+    const int64_t bt = at / d.q_heads;
+    const int t = (int)(bt % d.q_len), b = (int)(bt / d.q_len);
     const Pack8<T> po = load8(static_cast<const T*>(d.o) + b * d.os[0] + t * d.os[1] + h * d.os[2], c, d.dim);
     const Pack8<T> pd = load8(static_cast<const T*>(d.d_o) + b * d.dos[0] + t * d.dos[1] + h * d.dos[2], c, d.dim);
     float s = 0.0f;
@@ -26,31 +47,33 @@ __global__ __launch_bounds__(kThreads) void k_cross_delta(CrossDev d) {
     for (int e = 0; e < 8; ++e) s += (float)po.v[e] * (float)pd.v[e];
 #pragma unroll
     for (int off = 8; off >= 1; off >>= 1) s += __shfl_xor(s, off, 64);
-    if (i < n && (threadIdx.x & 15) == 0) d.delta[(b * d.q_heads + h) * d.q_len + t] = s;
+    if (i < n && (threadIdx.x & 15) == 0) {
+        const int64_t sat = stat_at(d, b, {t, h});
+        float hi, lo;
+        row_stats<MASK>(d.stats[sat * 2], d.stats[sat * 2 + 1], hi, lo);
+        float* out = tile_stats(d, b, {t, h});
+        out[0] = hi;
+        out[32] = lo;
+        out[64] = s;
+    }
 }
 
-// A row's statistics (m, log of the sum) as the backward pass uses them: without a mask hi = log2 of the sum
-// of all weights (lo unused), with one the maximum and the log2 of the sum past it apart. A row that sees
-// no key has weights 0 whatever its scores.
-template <bool MASKED>
-__device__ __forceinline__ void row_stats(float m, float ll, float& hi, float& lo) {
-    const bool empty = ll == -INFINITY;
-    hi = MASKED ? (empty ? 0.0f : m) : (empty ? INFINITY : (m + ll) * kLog2e);
-    lo = empty ? INFINITY : ll * kLog2e;
-}
-template <bool MASKED>
-__device__ __forceinline__ float weight(float s, float scale, float f, float bias, float hi, float lo) {
-    return __builtin_amdgcn_exp2f(MASKED ? fmaf(fmaf(s, scale, bias) - hi, kLog2e, -lo) : fmaf(s, f, -hi));
-}
+// dq: the forward pass's tiling; a lane owns a row, K and V tiles pass by.
+//
+// delta, the sum of do * o over the head, equals the sum of P dP over the keys. The first takes the rounded
+// o: its error is one of o's rounding, common to the row's keys, which is lost beside dS's own rounding
+// where many keys share the weight. Up to kExactKeys keys (EXACT) the second is formed in fp32 by a pass of
+// its own over the (few) tiles: the gradients' error at 77 keys is 1.4 instead of 1.6 times the output's
+// rounding.
+constexpr int kExactKeys = 256;
 
-// dq: the forward pass's tiling; a lane owns a row, K and V tiles pass by. Writes delta for the rows of its
-// tile on the way (the first key range does).
-template <class T, int KS, bool MASKED, int WIDTH>
+template <class T, int KS, int MASK, int WIDTH, bool EXACT>
 __global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
     constexpr int DP = KS <= 4 ? 64 : 128, DB = (KS + 1) / 2, KEYS = 64, ROWS = 128;
+    constexpr bool DIRECT = WIDTH == kWhole;
     typedef typename Vec<T>::v8 v8;
     __shared__ __align__(16) T tiles[2][2][KEYS * DP];
-    __shared__ __align__(16) float bias[2][MASKED ? KEYS : 4];
+    __shared__ __align__(16) float bias[2][MASK ? KEYS : 4];
 
     const Work wk = work_at(d);
     const int tile = wk.tile, b = wk.b, hk = wk.hk;
@@ -65,43 +88,60 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
     const int kend = wk.part < 0 || klen < kbeg + d.split_keys ? klen : kbeg + d.split_keys;
     const T* kb = static_cast<const T*>(d.k) + b * d.ks[0] + hk * d.ks[2];
     const T* vb = static_cast<const T*>(d.v) + b * d.vs[0] + hk * d.vs[2];
-    KvStage<T, DP, KEYS, MASKED, WIDTH, !MASKED && WIDTH == kWhole> st(d);
-    if (kbeg < kend) st.load(d, kb, vb, b, kbeg, kend, tiles[0][0], tiles[0][1]);
+    // Tiles of the key range, once or twice.
+    const int n = kend > kbeg ? (kend - kbeg + KEYS - 1) / KEYS : 0, steps = EXACT ? 2 * n : n;
+    auto key_at = [&](int i) { return kbeg + (EXACT && i >= n ? i - n : i) * KEYS; };
+    KvStage<T, DP, KEYS, MASK, WIDTH, DIRECT> st(d);
+    if (steps > 0) {
+        st.load(d, kb, vb, kbeg, kend, tiles[0][0], tiles[0][1]);
+        st.load_mask(d, b, kbeg, kend);
+    }
 
     v8 q[KS], g[KS];
     load_row<T, KS, WIDTH>(g, static_cast<const T*>(d.d_o) + b * d.dos[0] + ra.token * d.dos[1] + ra.head * d.dos[2], d.dim, half, valid);
-    load_row<T, KS, WIDTH>(q, static_cast<const T*>(d.o) + b * d.os[0] + ra.token * d.os[1] + ra.head * d.os[2], d.dim, half, valid);
     float delta = 0.0f;
+    if constexpr (!EXACT) {
+        load_row<T, KS, WIDTH>(q, static_cast<const T*>(d.o) + b * d.os[0] + ra.token * d.os[1] + ra.head * d.os[2], d.dim, half, valid);
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
+        for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) delta = fmaf((float)g[ks][i], (float)q[ks][i], delta);
-    delta += __shfl_xor(delta, 32, 64);
-    if (wk.split == 0 && valid && half == 0) d.delta[sat] = delta;
+            for (int i = 0; i < 8; ++i) delta = fmaf((float)g[ks][i], (float)q[ks][i], delta);
+        delta += __shfl_xor(delta, 32, 64);
+    }
     load_row<T, KS, WIDTH>(q, static_cast<const T*>(d.q) + b * d.qs[0] + ra.token * d.qs[1] + ra.head * d.qs[2], d.dim, half, valid);
     float hi, lo;
-    row_stats<MASKED>(d.stats[sat * 2], d.stats[sat * 2 + 1], hi, lo);
+    row_stats<MASK>(d.stats[sat * 2], d.stats[sat * 2 + 1], hi, lo);
     const float f = d.scale * kLog2e;
     f32x16 acc[DB];
 #pragma unroll
     for (int i = 0; i < DB; ++i) acc[i] = f32x16{};
 
-    if (kbeg < kend) st.arrive(tiles[0][0], tiles[0][1], bias[0], d.dim);
-    __syncthreads();
-    int p = 0;
-    for (int k0 = kbeg; k0 < kend; k0 += KEYS, p ^= 1) {
+    if (DIRECT && steps > 1) {
+        st.load(d, kb, vb, key_at(1), kend, tiles[1][0], tiles[1][1]);
+        wait_loads<decltype(st)::kLoads>();
+    } else {
+        wait_loads();
+    }
+    if (steps > 0) st.arrive(tiles[0][0], tiles[0][1], bias[0], d.dim);
+    if (steps > 1) {
+        if (!DIRECT) st.load(d, kb, vb, key_at(1), kend, tiles[1][0], tiles[1][1]);
+        st.load_mask(d, b, key_at(1), kend);
+    }
+    lds_barrier();
+    for (int i = 0; i < steps; ++i) {
+        const int p = i & 1, k0 = key_at(i);
         const T* kt = tiles[p][0];
         const T* vt = tiles[p][1];
-        if (k0 + KEYS < kend) st.load(d, kb, vb, b, k0 + KEYS, kend, tiles[p ^ 1][0], tiles[p ^ 1][1]);
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
+            if (nt == 1 && k0 + 32 >= kend) break;
             f32x16 s = f32x16{}, e = f32x16{};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 s = mma(read_rows<T, DP>(kt, nt * 32 + (lane & 31), ks, half), q[ks], s);
                 e = mma(read_rows<T, DP>(vt, nt * 32 + (lane & 31), ks, half), g[ks], e);
             }
-            if (!MASKED && k0 + nt * 32 + 32 > kend) {
+            if (!MASK && k0 + nt * 32 + 32 > kend) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     if (k0 + nt * 32 + 8 * (r >> 2) + 4 * half + (r & 3) >= kend) s[r] = -INFINITY;
@@ -109,23 +149,45 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
 #pragma unroll
             for (int g4 = 0; g4 < 4; ++g4) {
                 float4 bv = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                if constexpr (MASKED) bv = *reinterpret_cast<const float4*>(&bias[p][nt * 32 + 8 * g4 + 4 * half]);
+                if constexpr (MASK != kNoMask) bv = *reinterpret_cast<const float4*>(&bias[p][nt * 32 + 8 * g4 + 4 * half]);
                 const float bs[4] = {bv.x, bv.y, bv.z, bv.w};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int r = 4 * g4 + i;
-                    s[r] = weight<MASKED>(s[r], d.scale, f, bs[i], hi, lo) * (e[r] - delta);
+                for (int j = 0; j < 4; ++j) {
+                    const int r = 4 * g4 + j;
+                    s[r] = weight<MASK>(s[r], d.scale, f, bs[j], hi, lo);
                 }
             }
+            if (EXACT && i < n) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const v8 ds = pack<T>(s, t);
+                for (int r = 0; r < 16; ++r) delta = fmaf(s[r], e[r], delta);
+            } else {
 #pragma unroll
-                for (int db = 0; db < DB; ++db) acc[db] = mma(read_cols<T, DP>(kt, nt * 32 + t * 16, db, lane), ds, acc[db]);
+                for (int r = 0; r < 16; ++r) s[r] *= e[r] - delta;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const v8 ds = pack<T>(s, t);
+#pragma unroll
+                    for (int db = 0; db < DB; ++db)
+                        acc[db] = mma(read_cols<T, DP>(kt, nt * 32 + t * 16, db, lane), ds, acc[db]);
+                }
             }
         }
-        if (k0 + KEYS < kend) st.arrive(tiles[p ^ 1][0], tiles[p ^ 1][1], bias[p ^ 1], d.dim);
-        __syncthreads();
+        if (EXACT && i == n - 1) delta += __shfl_xor(delta, 32, 64);
+        if (i + 1 < steps) {
+            wait_loads();
+            st.arrive(tiles[p ^ 1][0], tiles[p ^ 1][1], bias[p ^ 1], d.dim);
+        }
+        lds_barrier();
+        if (i + 2 < steps) {                 // into the buffer that every wave has left
+            st.load(d, kb, vb, key_at(i + 2), kend, tiles[p][0], tiles[p][1]);
+            st.load_mask(d, b, key_at(i + 2), kend);
+        }
+    }
+    if (wk.split == 0 && valid && half == 0) {
+        float* out = tile_stats(d, b, ra);
+        out[0] = hi;
+        out[32] = lo;
+        out[64] = delta;
     }
     if (wk.part < 0) {
         T* out = static_cast<T*>(d.dq) + b * d.dqs[0] + ra.token * d.dqs[1] + ra.head * d.dqs[2];
@@ -136,14 +198,17 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
     }
 }
 
-// dk, dv: a wave owns 32 keys (K and V in registers), tiles of 32 tokens of one query head pass by, double
-// buffered; the heads of the group one after the other.
-template <class T, int KS, bool MASKED, int WIDTH>
+// dk, dv: a wave owns 32 keys (K and V in registers), tiles of 32 tokens of one query head and their
+// statistics pass by, up to three on their way; the heads of the group one after the other.
+template <class T, int KS, int MASK, int WIDTH>
 __global__ __launch_bounds__(kThreads, KS <= 6 ? 2 : 1) void k_cross_dkv(CrossDev d) {
     constexpr int DP = KS <= 4 ? 64 : 128, DB = (KS + 1) / 2, KEYS = 128, ROWS = 32;
+    constexpr bool DIRECT = WIDTH == kWhole;
+    constexpr int STAGES = DIRECT ? 4 : 2;
     typedef typename Vec<T>::v8 v8;
-    __shared__ __align__(16) T tiles[2][2][ROWS * DP];       // [parity][q, do]
-    __shared__ __align__(16) float stat[2][3][ROWS];         // hi, lo, delta
+    typedef Stage<T, DP, ROWS, WIDTH, DIRECT> S;
+    __shared__ __align__(16) T tiles[STAGES][2][ROWS * DP];      // [][q, do]
+    __shared__ __align__(16) float stat[STAGES][4][256];         // [][wave]: wave 0's holds hi, lo, delta, 32 of each
 
     const int key_tiles = (d.kv_len + KEYS - 1) / KEYS;
     int id = xcd_order(blockIdx.x, gridDim.x);
@@ -151,7 +216,7 @@ __global__ __launch_bounds__(kThreads, KS <= 6 ? 2 : 1) void k_cross_dkv(CrossDe
     id /= key_tiles;
     const int split = id % d.row_splits, bh = id / d.row_splits;
     const int b = bh / d.kv_heads, hk = bh - b * d.kv_heads;
-    const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, half = lane >> 5, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int key = tile * KEYS + w * 32 + (lane & 31);
     const int klen = sample_keys(d, b);
 
@@ -162,44 +227,38 @@ __global__ __launch_bounds__(kThreads, KS <= 6 ? 2 : 1) void k_cross_dkv(CrossDe
     if (tile * KEYS >= klen) tend = tbeg;
     const T* qb = static_cast<const T*>(d.q) + b * d.qs[0] + (int64_t)hk * d.group * d.qs[2];
     const T* gb = static_cast<const T*>(d.d_o) + b * d.dos[0] + (int64_t)hk * d.group * d.dos[2];
-    Stage<T, DP, ROWS, WIDTH, WIDTH == kWhole> sq(d.dim, d.qs[1]), sg(d.dim, d.dos[1]);
-    float s_m = 0.0f, s_l = -INFINITY, s_delta = 0.0f;       // a row that does not exist sees no key
+    S sq(d.dim, d.qs[1]), sg(d.dim, d.dos[1]);
+    constexpr int LOADS = 2 * S::kPieces + 1;                    // of a thread for one tile
+    auto rows_of = [&](int it) { return d.q_len - it % head_tiles * ROWS; };
     auto load = [&](int it, int p) {
-        const int gh = it / head_tiles, r0 = (it - gh * head_tiles) * ROWS, rows = d.q_len - r0;
-        sq.load(qb + gh * d.qs[2] + r0 * d.qs[1], d.qs[1], rows, d.dim, tiles[p][0]);
-        sg.load(gb + gh * d.dos[2] + r0 * d.dos[1], d.dos[1], rows, d.dim, tiles[p][1]);
-        if (threadIdx.x < ROWS) {
-            if ((int)threadIdx.x < rows) {
-                const int64_t sat = stat_at(d, b, {r0 + (int)threadIdx.x, hk * d.group + gh});
-                s_m = d.stats[sat * 2];
-                s_l = d.stats[sat * 2 + 1];
-                s_delta = d.delta[sat];
-            } else {
-                s_m = s_delta = 0.0f;
-                s_l = -INFINITY;
-            }
-        }
+        const int gh = it / head_tiles, r0 = (it - gh * head_tiles) * ROWS;
+        sq.load(qb + gh * d.qs[2] + r0 * d.qs[1], d.qs[1], d.q_len - r0, d.dim, tiles[p][0]);
+        sg.load(gb + gh * d.dos[2] + r0 * d.dos[1], d.dos[1], d.q_len - r0, d.dim, tiles[p][1]);
+        // 96 floats: 24 lanes of wave 0 (the other waves fill their own part with zeros, to issue as many loads).
+        load_lds(buffer_at(tile_stats(d, b, {r0, hk * d.group + gh})), stat[p][w], w == 0 && lane < 24 ? lane * 16 : kNowhere, 0);
     };
-    auto arrive = [&](int p) {
+    auto arrive = [&](int it, int p) {
         sq.arrive(tiles[p][0], d.dim);
         sg.arrive(tiles[p][1], d.dim);
-        if (threadIdx.x < ROWS) {
-            float hi, lo;
-            row_stats<MASKED>(s_m, s_l, hi, lo);
-            stat[p][0][threadIdx.x] = hi;
-            stat[p][1][threadIdx.x] = lo;
-            stat[p][2][threadIdx.x] = s_delta;
+        const int i = threadIdx.x;                               // a row that does not exist sees no key
+        if (i < ROWS && i >= rows_of(it)) {
+            stat[p][0][i] = MASK ? 0.0f : INFINITY;
+            stat[p][0][i + 32] = INFINITY;
+            stat[p][0][i + 64] = 0.0f;
         }
     };
-    if (tbeg < tend) load(tbeg, 0);
+#pragma unroll
+    for (int i = 0; i < (DIRECT ? STAGES - 1 : 1); ++i)
+        if (tbeg + i < tend) load(tbeg + i, i);
 
+    const int at = key < d.kv_len ? key : 0;
     bool seen = key < klen;
     float bias = -INFINITY;                  // of the lane's key
-    if (MASKED && seen) {
-        bias = key_bias(d, b, key);
+    if constexpr (MASK != kNoMask) {
+        const float v = mask_bias<MASK>(mask_load<MASK>(d, b, at));
+        bias = seen ? v : -INFINITY;
         seen = bias != -INFINITY;
     }
-    const int at = key < d.kv_len ? key : 0;
     v8 kr[KS], vr[KS];
     load_row<T, KS, WIDTH>(kr, static_cast<const T*>(d.k) + b * d.ks[0] + at * d.ks[1] + hk * d.ks[2], d.dim, half, seen);
     load_row<T, KS, WIDTH>(vr, static_cast<const T*>(d.v) + b * d.vs[0] + at * d.vs[1] + hk * d.vs[2], d.dim, half, seen);
@@ -208,11 +267,13 @@ __global__ __launch_bounds__(kThreads, KS <= 6 ? 2 : 1) void k_cross_dkv(CrossDe
     for (int i = 0; i < DB; ++i) ak[i] = av[i] = f32x16{};
     const float f = d.scale * kLog2e;
 
-    if (tbeg < tend) arrive(0);
-    __syncthreads();
-    int p = 0;
-    for (int it = tbeg; it < tend; ++it, p ^= 1) {
-        if (it + 1 < tend) load(it + 1, p ^ 1);
+    wait_loads();
+    if (tbeg < tend) arrive(tbeg, 0);
+    if (!DIRECT && tbeg + 1 < tend) load(tbeg + 1, 1);
+    lds_barrier();
+    for (int it = tbeg; it < tend; ++it) {
+        const int p = (it - tbeg) % STAGES, p1 = (it + 1 - tbeg) % STAGES;
+        if (DIRECT && it + STAGES - 1 < tend) load(it + STAGES - 1, (it + STAGES - 1 - tbeg) % STAGES);
         const T* qt = tiles[p][0];
         const T* gt = tiles[p][1];
         f32x16 s = f32x16{}, e = f32x16{};
@@ -226,14 +287,14 @@ __global__ __launch_bounds__(kThreads, KS <= 6 ? 2 : 1) void k_cross_dkv(CrossDe
             float4 st[3];
 #pragma unroll
             for (int i = 0; i < 3; ++i)
-                if (MASKED || i != 1) st[i] = *reinterpret_cast<const float4*>(&stat[p][i][8 * g4 + 4 * half]);
+                if (MASK || i != 1) st[i] = *reinterpret_cast<const float4*>(&stat[p][0][i * 32 + 8 * g4 + 4 * half]);
             const float hi[4] = {st[0].x, st[0].y, st[0].z, st[0].w}, dl[4] = {st[2].x, st[2].y, st[2].z, st[2].w};
             float lo[4] = {};
-            if constexpr (MASKED) lo[0] = st[1].x, lo[1] = st[1].y, lo[2] = st[1].z, lo[3] = st[1].w;
+            if constexpr (MASK != kNoMask) lo[0] = st[1].x, lo[1] = st[1].y, lo[2] = st[1].z, lo[3] = st[1].w;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int r = 4 * g4 + i;
-                s[r] = weight<MASKED>(s[r], d.scale, f, bias, hi[i], lo[i]);
+                s[r] = weight<MASK>(s[r], d.scale, f, bias, hi[i], lo[i]);
                 e[r] = s[r] * (e[r] - dl[i]);
             }
         }
@@ -246,8 +307,13 @@ __global__ __launch_bounds__(kThreads, KS <= 6 ? 2 : 1) void k_cross_dkv(CrossDe
                 ak[db] = mma(read_cols<T, DP>(qt, t * 16, db, lane), ds, ak[db]);
             }
         }
-        if (it + 1 < tend) arrive(p ^ 1);
-        __syncthreads();
+        if (it + 1 < tend) {
+            if (DIRECT && it + STAGES - 1 < tend) wait_loads<(STAGES - 2) * LOADS>();    // the next tile is there
+            else wait_loads();
+            arrive(it + 1, p1);
+        }
+        lds_barrier();
+        if (!DIRECT && it + 2 < tend) load(it + 2, p);
     }
     if (!seen) {                             // the lane's columns held weights of a key of zeros
 #pragma unroll
@@ -304,23 +370,25 @@ __global__ __launch_bounds__(kThreads) void k_cross_sum_dkv(CrossDev d) {
     else static_cast<T*>(d.dk)[b * d.dks[0] + key * d.dks[1] + hk * d.dks[2] + c] = (T)(s * d.scale);
 }
 
-template <class T, int KS, bool MASKED, int WIDTH>
+template <class T, int KS, int MASK, int WIDTH>
 hipError_t backward(const CrossDev& d, hipStream_t st) {
     const int64_t bh = (int64_t)d.batch * d.kv_heads;
     hipError_t e = hipSuccess;
     if (d.dq && d.rows > 0) {
-        k_cross_dq<T, KS, MASKED, WIDTH><<<(unsigned)(d.whole + (d.tiles - d.whole) * d.splits), kThreads, 0, st>>>(d);
+        const unsigned blocks = (unsigned)(d.whole + (d.tiles - d.whole) * d.splits);
+        if (d.kv_len <= kExactKeys) k_cross_dq<T, KS, MASK, WIDTH, true><<<blocks, kThreads, 0, st>>>(d);
+        else k_cross_dq<T, KS, MASK, WIDTH, false><<<blocks, kThreads, 0, st>>>(d);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         if (d.whole < d.tiles) {
             k_cross_sum_dq<T><<<blocks_for((int64_t)(d.tiles - d.whole) * d.tile_rows, 8), kThreads, 0, st>>>(d);
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
     } else if (d.rows > 0) {
-        k_cross_delta<T><<<blocks_for(bh * d.rows, 16), kThreads, 0, st>>>(d);
+        k_cross_stats<T, MASK><<<blocks_for(bh * d.rows, 16), kThreads, 0, st>>>(d);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (d.dk && d.kv_len > 0) {
-        k_cross_dkv<T, KS, MASKED, WIDTH><<<(unsigned)((d.kv_len + 127) / 128 * d.row_splits * bh), kThreads, 0, st>>>(d);
+        k_cross_dkv<T, KS, MASK, WIDTH><<<(unsigned)((d.kv_len + 127) / 128 * d.row_splits * bh), kThreads, 0, st>>>(d);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         if (d.row_splits > 1) {
             k_cross_sum_dkv<T><<<dim3(blocks_for(bh * d.kv_len * d.dim, kThreads), 2), kThreads, 0, st>>>(d);
@@ -356,6 +424,7 @@ void cross_plan(CrossDev& d, bool backward_pass) {
     d.whole = (int)tiles;
     split(rest > 0 ? kSlots / rest : 1, ((int64_t)d.kv_len + key_tile - 1) / key_tile, d.splits, d.split_keys);
     d.split_keys *= key_tile;
+    if (backward_pass && d.kv_len <= kExactKeys) d.splits = 1;      // a block sees all keys
     if (d.splits > 1) d.whole = (int)(tiles - rest);
     // dk, dv: one block a CU above a head width of 96.
     const int64_t key_blocks = ((int64_t)d.kv_len + 127) / 128 * bh;
@@ -364,8 +433,8 @@ void cross_plan(CrossDev& d, bool backward_pass) {
 }
 
 hipError_t cross_backward(const CrossDev& d, int dtype, hipStream_t st) {
-    return dispatch(d, dtype, [&](auto t, auto ks, auto m, auto wd) {
-        return backward<decltype(t), decltype(ks)::value, decltype(m)::value, decltype(wd)::value>(d, st);
+    return dispatch(d, dtype, [&](auto t, auto ks, auto mk, auto wd) {
+        return backward<decltype(t), decltype(ks)::value, decltype(mk)::value, decltype(wd)::value>(d, st);
     });
 }
 

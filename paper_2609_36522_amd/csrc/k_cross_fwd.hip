@@ -27,12 +27,12 @@ __device__ __forceinline__ void add_bias(f32x16& s, float scale, const float* bi
 // weight since the last time, so weights reach 2^kSlack, which the element types hold as exactly as 1.
 constexpr float kSlack = 8.0f;
 
-template <class T, int KS, bool MASKED, int WIDTH>
+template <class T, int KS, int MASK, int WIDTH>
 __global__ __launch_bounds__(kThreads, 2) void k_cross_fwd(CrossDev d) {
     constexpr int DP = KS <= 4 ? 64 : 128, DB = (KS + 1) / 2, KEYS = 64, ROWS = 128, NT = 2;
     typedef typename Vec<T>::v8 v8;
     __shared__ __align__(16) T tiles[2][2][KEYS * DP];      // [stage parity][K, V]
-    __shared__ __align__(16) float bias[2][MASKED ? KEYS : 4];
+    __shared__ __align__(16) float bias[2][MASK ? KEYS : 4];
 
     const Work wk = work_at(d);
     const int tile = wk.tile, b = wk.b, hk = wk.hk;
@@ -46,27 +46,41 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_fwd(CrossDev d) {
     const int kend = wk.part < 0 || klen < kbeg + d.split_keys ? klen : kbeg + d.split_keys;
     const T* kb = static_cast<const T*>(d.k) + b * d.ks[0] + hk * d.ks[2];
     const T* vb = static_cast<const T*>(d.v) + b * d.vs[0] + hk * d.vs[2];
-    KvStage<T, DP, KEYS, MASKED, WIDTH, !MASKED && WIDTH == kWhole> st(d);
-    if (kbeg < kend) st.load(d, kb, vb, b, kbeg, kend, tiles[0][0], tiles[0][1]);
+    constexpr bool DIRECT = WIDTH == kWhole;
+    KvStage<T, DP, KEYS, MASK, WIDTH, DIRECT> st(d);
+    if (kbeg < kend) {
+        st.load(d, kb, vb, kbeg, kend, tiles[0][0], tiles[0][1]);
+        st.load_mask(d, b, kbeg, kend);
+    }
 
     const T* qp = static_cast<const T*>(d.q) + b * d.qs[0] + ra.token * d.qs[1] + ra.head * d.qs[2];
     v8 q[KS];
     load_row<T, KS, WIDTH>(q, qp, d.dim, half, valid);
 
     // Scores in units of 1/f: x f is the exponent of 2. With a mask x is the scaled, biased score.
-    const float f = MASKED ? kLog2e : d.scale * kLog2e;
+    const float f = MASK ? kLog2e : d.scale * kLog2e;
     f32x16 acc[DB];
 #pragma unroll
     for (int i = 0; i < DB; ++i) acc[i] = f32x16{};
     float m = -INFINITY, l = 0.0f;
 
+    const bool second = kbeg + KEYS < kend;
+    if (DIRECT && second) {
+        st.load(d, kb, vb, kbeg + KEYS, kend, tiles[1][0], tiles[1][1]);
+        wait_loads<decltype(st)::kLoads>();
+    } else {
+        wait_loads();
+    }
     if (kbeg < kend) st.arrive(tiles[0][0], tiles[0][1], bias[0], d.dim);
-    __syncthreads();
+    if (second) {
+        if (!DIRECT) st.load(d, kb, vb, kbeg + KEYS, kend, tiles[1][0], tiles[1][1]);
+        st.load_mask(d, b, kbeg + KEYS, kend);
+    }
+    lds_barrier();
     int p = 0;
     for (int k0 = kbeg; k0 < kend; k0 += KEYS, p ^= 1) {
         const T* kt = tiles[p][0];
         const T* vt = tiles[p][1];
-        if (k0 + KEYS < kend) st.load(d, kb, vb, b, k0 + KEYS, kend, tiles[p ^ 1][0], tiles[p ^ 1][1]);
         f32x16 s[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -74,7 +88,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_fwd(CrossDev d) {
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) s[nt] = mma(read_rows<T, DP>(kt, nt * 32 + (lane & 31), ks, half), q[ks], s[nt]);
         }
-        if constexpr (MASKED) {
+        if constexpr (MASK != kNoMask) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) add_bias(s[nt], d.scale, bias[p] + nt * 32, half);
         } else if (k0 + KEYS > kend) {
@@ -107,7 +121,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_fwd(CrossDev d) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 // With a mask the difference comes first: x may be near the type's lowest value.
-                const float e = __builtin_amdgcn_exp2f(MASKED ? (s[nt][r] - base) * f : fmaf(s[nt][r], f, -mf));
+                const float e = __builtin_amdgcn_exp2f(MASK ? (s[nt][r] - base) * f : fmaf(s[nt][r], f, -mf));
                 s[nt][r] = e;
                 l += e;
             }
@@ -121,11 +135,18 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_fwd(CrossDev d) {
                 for (int db = 0; db < DB; ++db) acc[db] = mma(read_cols<T, DP>(vt, nt * 32 + t * 16, db, lane), e, acc[db]);
             }
         }
-        if (k0 + KEYS < kend) st.arrive(tiles[p ^ 1][0], tiles[p ^ 1][1], bias[p ^ 1], d.dim);
-        __syncthreads();
+        if (k0 + KEYS < kend) {
+            wait_loads();
+            st.arrive(tiles[p ^ 1][0], tiles[p ^ 1][1], bias[p ^ 1], d.dim);
+        }
+        lds_barrier();
+        if (k0 + 2 * KEYS < kend) {          // into the buffer that every wave has left
+            st.load(d, kb, vb, k0 + 2 * KEYS, kend, tiles[p][0], tiles[p][1]);
+            st.load_mask(d, b, k0 + 2 * KEYS, kend);
+        }
     }
     l += __shfl_xor(l, 32, 64);
-    const float m_nat = MASKED || m == -INFINITY ? m : m * d.scale;
+    const float m_nat = MASK || m == -INFINITY ? m : m * d.scale;
     if (wk.part < 0) {
         T* op = static_cast<T*>(d.o) + b * d.os[0] + ra.token * d.os[1] + ra.head * d.os[2];
         store_row<T, DB, WIDTH>(op, d.dim, acc, l == 0.0f ? 0.0f : 1.0f / l, half, valid);   // no key seen: acc is 0
@@ -146,13 +167,13 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_fwd(CrossDev d) {
 
 // At most 32 rows: the four waves take 32 keys each of a 128-key tile for the same rows and are joined at
 // the end. Bound by the reading of K and V; two blocks a CU keep 128 KB in flight.
-template <class T, int KS, bool MASKED, int WIDTH>
+template <class T, int KS, int MASK, int WIDTH>
 __global__ __launch_bounds__(kThreads, 2) void k_cross_few(CrossDev d) {
     constexpr int DP = KS <= 4 ? 64 : 128, DB = (KS + 1) / 2, KEYS = 128, ROWS = 32;
     typedef typename Vec<T>::v8 v8;
     // K tile, V tile; afterwards the waves' accumulators [4][DP][32] in fp32.
     __shared__ __align__(16) T tiles[2 * KEYS * DP];
-    __shared__ __align__(16) float bias[MASKED ? KEYS : 4];
+    __shared__ __align__(16) float bias[MASK ? KEYS : 4];
     __shared__ float wave_m[4][32], wave_l[4][32];
     T* kt = tiles;
     T* vt = tiles + KEYS * DP;
@@ -175,24 +196,30 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_few(CrossDev d) {
     const T* vb = static_cast<const T*>(d.v) + b * d.vs[0] + hk * d.vs[2];
 
     // Scores in units of 1/f: x f is the exponent of 2. With a mask x is the scaled, biased score.
-    const float f = MASKED ? kLog2e : d.scale * kLog2e;
+    const float f = MASK ? kLog2e : d.scale * kLog2e;
     f32x16 acc[DB];
 #pragma unroll
     for (int i = 0; i < DB; ++i) acc[i] = f32x16{};
     float m = -INFINITY, l = 0.0f;
 
-    KvStage<T, DP, KEYS, MASKED, WIDTH, false> st(d);
-    if (kbeg < kend) st.load(d, kb, vb, b, kbeg, kend, kt, vt);
+    KvStage<T, DP, KEYS, MASK, WIDTH, false> st(d);
+    if (kbeg < kend) {
+        st.load(d, kb, vb, kbeg, kend, kt, vt);
+        st.load_mask(d, b, kbeg, kend);
+    }
     for (int k0 = kbeg; k0 < kend; k0 += KEYS) {
         __syncthreads();
         st.arrive(kt, vt, bias, d.dim);
         __syncthreads();
-        if (k0 + KEYS < kend) st.load(d, kb, vb, b, k0 + KEYS, kend, kt, vt);
+        if (k0 + KEYS < kend) {
+            st.load(d, kb, vb, k0 + KEYS, kend, kt, vt);
+            st.load_mask(d, b, k0 + KEYS, kend);
+        }
         const int koff = w * 32;
         f32x16 s = f32x16{};
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) s = mma(read_rows<T, DP>(kt, koff + (lane & 31), ks, half), q[ks], s);
-        if constexpr (MASKED) {
+        if constexpr (MASK != kNoMask) {
             add_bias(s, d.scale, bias + koff, half);
         } else if (k0 + KEYS > kend) {
 #pragma unroll
@@ -217,7 +244,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_few(CrossDev d) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             // With a mask the difference comes first: x may be near the type's lowest value.
-            s[r] = __builtin_amdgcn_exp2f(MASKED ? (s[r] - base) * f : fmaf(s[r], f, -mf));
+            s[r] = __builtin_amdgcn_exp2f(MASK ? (s[r] - base) * f : fmaf(s[r], f, -mf));
             l += s[r];
         }
 #pragma unroll
@@ -228,7 +255,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_few(CrossDev d) {
         }
     }
     l += __shfl_xor(l, 32, 64);
-    const float m_nat = MASKED || m == -INFINITY ? m : m * d.scale;
+    const float m_nat = MASK || m == -INFINITY ? m : m * d.scale;
 
     float* wa = reinterpret_cast<float*>(tiles);
     __syncthreads();
@@ -329,11 +356,11 @@ __global__ __launch_bounds__(kThreads) void k_cross_join(CrossDev d) {
     }
 }
 
-template <class T, int KS, bool MASKED, int WIDTH>
+template <class T, int KS, int MASK, int WIDTH>
 hipError_t forward(const CrossDev& d, hipStream_t st) {
     const unsigned blocks = (unsigned)(d.whole + (d.tiles - d.whole) * d.splits);
-    if (d.tile_rows == 32) k_cross_few<T, KS, MASKED, WIDTH><<<blocks, kThreads, 0, st>>>(d);
-    else k_cross_fwd<T, KS, MASKED, WIDTH><<<blocks, kThreads, 0, st>>>(d);
+    if (d.tile_rows == 32) k_cross_few<T, KS, MASK, WIDTH><<<blocks, kThreads, 0, st>>>(d);
+    else k_cross_fwd<T, KS, MASK, WIDTH><<<blocks, kThreads, 0, st>>>(d);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || d.whole == d.tiles) return e;
     const unsigned rows = (unsigned)((d.tiles - d.whole) * d.tile_rows);
@@ -345,8 +372,8 @@ hipError_t forward(const CrossDev& d, hipStream_t st) {
 }  // namespace
 
 hipError_t cross_forward(const CrossDev& d, int dtype, hipStream_t st) {
-    return dispatch(d, dtype, [&](auto t, auto ks, auto m, auto wd) {
-        return forward<decltype(t), decltype(ks)::value, decltype(m)::value, decltype(wd)::value>(d, st);
+    return dispatch(d, dtype, [&](auto t, auto ks, auto mk, auto wd) {
+        return forward<decltype(t), decltype(ks)::value, decltype(mk)::value, decltype(wd)::value>(d, st);
     });
 }
 

@@ -40,12 +40,23 @@ __device__ __forceinline__ int sample_keys(const CrossDev& d, int b) {
     return n < 0 ? 0 : n > d.kv_len ? d.kv_len : n;
 }
 
-// Additive bias of a key below the sample's length: 0, the mask's value, or -inf.
-__device__ __forceinline__ float key_bias(const CrossDev& d, int b, int key) {
-    if (d.mask_kind == PA_MASK_NONE) return 0.0f;
-    const int64_t at = b * d.mask_stride + key;
-    if (d.mask_kind == PA_MASK_ADD) return static_cast<const float*>(d.mask)[at];
-    return static_cast<const uint8_t*>(d.mask)[at] ? 0.0f : -INFINITY;
+// The keys' mask. A value is kept as it lies in memory until it is needed, so that its load can be in
+// flight; without a mask (a kernel for masks also takes scales that are not positive) one visible byte
+// stands for all keys.
+constexpr int kNoMask = 0, kBytes = 1, kBiases = 2;
+
+__device__ const uint8_t kVisible = 1;
+
+template <int MASK>
+__device__ __forceinline__ uint32_t mask_load(const CrossDev& d, int b, int key) {
+    if constexpr (MASK == kBiases) return static_cast<const uint32_t*>(d.mask)[b * d.mask_stride + key];
+    const uint8_t* p = d.mask ? static_cast<const uint8_t*>(d.mask) + b * d.mask_stride : &kVisible;
+    return p[d.mask ? key : 0];
+}
+// The additive bias of the key: -inf if it is not visible.
+template <int MASK>
+__device__ __forceinline__ float mask_bias(uint32_t v) {
+    return MASK == kBiases ? __builtin_bit_cast(float, v) : v ? 0.0f : -INFINITY;
 }
 
 // A tile of ROWS rows, `stride` elements apart, on its way from memory to LDS.
@@ -97,51 +108,62 @@ struct Stage {
             }
         }
     }
-    // The tile is in LDS once every thread has called this and a barrier has passed.
+    // Element offset in the tile of what the thread's i-th DIRECT load fills.
+    __device__ __forceinline__ static int slot(int i) { return ((int)threadIdx.x + i * kThreads) * 8; }
+
+    // Registers into LDS (DIRECT: nothing to do, the caller waits for the loads).
     __device__ __forceinline__ void arrive(T* tile, int dim) {
-        if constexpr (WIDTH == kRagged) {
+        if constexpr (!DIRECT) {
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i)
-                r[i] = __builtin_bit_cast(uint4, fix8(__builtin_bit_cast(Pack8<T>, r[i]), piece() * 8, dim, row(i) < rows));
-        }
-        if constexpr (DIRECT) {
-            wait_loads();
-        } else {
-#pragma unroll
-            for (int i = 0; i < kPieces; ++i) *reinterpret_cast<uint4*>(tile + piece_at<DP>(row(i), piece())) = r[i];
+            for (int i = 0; i < kPieces; ++i) {
+                if constexpr (WIDTH == kRagged)
+                    r[i] = __builtin_bit_cast(uint4, fix8(__builtin_bit_cast(Pack8<T>, r[i]), piece() * 8, dim, row(i) < rows));
+                *reinterpret_cast<uint4*>(tile + piece_at<DP>(row(i), piece())) = r[i];
+            }
         }
     }
 };
 
-// Keys and values of a tile; with MASKED zeros where a key is not visible (0 weight times an infinity or
-// a NaN would not be 0), and the keys' biases.
-template <class T, int DP, int KEYS, bool MASKED, int WIDTH, bool DIRECT>
+// Keys and values of a tile of KEYS keys below kend; with a mask zeros where a key is not visible (0 weight
+// times an infinity or a NaN would not be 0), and the keys' biases.
+template <class T, int DP, int KEYS, int MASK, int WIDTH, bool DIRECT>
 struct KvStage {
     typedef Stage<T, DP, KEYS, WIDTH, DIRECT> S;
+    static constexpr int kLoads = 2 * S::kPieces;       // of a thread for one tile (masks not counted)
     S k, v;
-    float bias, seen[MASKED ? S::kPieces : 1];
+    uint32_t bias, seen[MASK ? S::kPieces : 1];
+    int left;
 
     __device__ __forceinline__ KvStage(const CrossDev& d) : k(d.dim, d.ks[1]), v(d.dim, d.vs[1]) {}
 
-    __device__ __forceinline__ void load(const CrossDev& d, const T* kb, const T* vb, int b, int k0, int kend, T* kt, T* vt) {
+    __device__ __forceinline__ void load(const CrossDev& d, const T* kb, const T* vb, int k0, int kend, T* kt, T* vt) {
         k.load(kb + k0 * d.ks[1], d.ks[1], kend - k0, d.dim, kt);
         v.load(vb + k0 * d.vs[1], d.vs[1], kend - k0, d.dim, vt);
-        if constexpr (MASKED) {
-            const int key = k0 + (int)threadIdx.x;
-            bias = (int)threadIdx.x < KEYS && key < kend ? key_bias(d, b, key) : -INFINITY;
+    }
+    __device__ __forceinline__ void load_mask(const CrossDev& d, int b, int k0, int kend) {
+        if constexpr (MASK != kNoMask) {
+            left = kend - k0;
+            const int i0 = (int)threadIdx.x % KEYS;
+            bias = mask_load<MASK>(d, b, k0 + (i0 < left ? i0 : 0));
 #pragma unroll
-            for (int i = 0; i < S::kPieces; ++i) {
-                const int kk = k0 + S::row(i);
-                seen[i] = kk < kend ? key_bias(d, b, kk) : 0.0f;
-            }
+            for (int i = 0; i < S::kPieces; ++i) seen[i] = mask_load<MASK>(d, b, k0 + (S::row(i) < left ? S::row(i) : 0));
         }
     }
+    // The tile is in LDS once every thread has called this (DIRECT: after waiting for its loads) and a
+    // barrier has passed.
     __device__ __forceinline__ void arrive(T* kt, T* vt, float* bt, int dim) {
-        if constexpr (MASKED) {
+        if constexpr (MASK != kNoMask) {
+            if ((int)threadIdx.x < KEYS) bt[threadIdx.x] = (int)threadIdx.x < left ? mask_bias<MASK>(bias) : -INFINITY;
 #pragma unroll
-            for (int i = 0; i < S::kPieces; ++i)
-                if (seen[i] == -INFINITY) k.r[i] = v.r[i] = make_uint4(0, 0, 0, 0);
-            if ((int)threadIdx.x < KEYS) bt[threadIdx.x] = bias;
+            for (int i = 0; i < S::kPieces; ++i) {
+                if (mask_bias<MASK>(seen[i]) != -INFINITY) continue;
+                if constexpr (DIRECT) {
+                    *reinterpret_cast<uint4*>(kt + S::slot(i)) = make_uint4(0, 0, 0, 0);
+                    *reinterpret_cast<uint4*>(vt + S::slot(i)) = make_uint4(0, 0, 0, 0);
+                } else {
+                    k.r[i] = v.r[i] = make_uint4(0, 0, 0, 0);
+                }
+            }
         }
         k.arrive(kt, dim);
         v.arrive(vt, dim);
@@ -250,7 +272,9 @@ __device__ __forceinline__ Work work_at(const CrossDev& d) {
 
 // With a mask, or a scale that is not positive (the largest scaled score is then not the scaled
 // largest product), scores are formed before the maximum is taken.
-inline bool masked(const CrossDev& d) { return d.mask_kind != PA_MASK_NONE || !(d.scale > 0.0f); }
+inline int mask_of(const CrossDev& d) {
+    return d.mask_kind == PA_MASK_ADD ? kBiases : d.mask_kind == PA_MASK_BOOL || !(d.scale > 0.0f) ? kBytes : kNoMask;
+}
 
 inline int width_of(const CrossDev& d) {
     if (d.dim < 8) return kTiny;
@@ -261,13 +285,17 @@ inline int width_of(const CrossDev& d) {
 
 inline unsigned blocks_for(int64_t n, int each) { return (unsigned)((n + each - 1) / each); }
 
-// Calls f(type, reduction steps of 16 over the head, masked, width): head widths are padded to 64, 80, 96 or
+// Calls f(type, reduction steps of 16 over the head, mask, width): head widths are padded to 64, 80, 96 or
 // 128, ragged ones to 64 or 128.
 template <class F>
 hipError_t dispatch(const CrossDev& d, int dtype, F f) {
-    const bool m = masked(d);
+    const int mask = mask_of(d);
     const int width = width_of(d);
-    auto with = [&](auto t, auto ks, auto wd) { return m ? f(t, ks, std::true_type{}, wd) : f(t, ks, std::false_type{}, wd); };
+    auto with = [&](auto t, auto ks, auto wd) {
+        if (mask == kNoMask) return f(t, ks, std::integral_constant<int, kNoMask>{}, wd);
+        if (mask == kBytes) return f(t, ks, std::integral_constant<int, kBytes>{}, wd);
+        return f(t, ks, std::integral_constant<int, kBiases>{}, wd);
+    };
     auto typed = [&](auto t) {
         const std::integral_constant<int, 4> k4;
         const std::integral_constant<int, 8> k8;

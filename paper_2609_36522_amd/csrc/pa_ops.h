@@ -38,7 +38,7 @@ struct CrossDev {
     int tile_rows, tiles;            // rows of a row tile, row tiles of all samples and kv heads
     float* part;                     // partial o, or partial dq: [split tile][splits][tile_rows][dim]
     float* part_stats;               // [split tile][splits][tile_rows][2]
-    float* delta;                    // [batch][q_heads][q_len]: sum of do * o over the head
+    float* row_stats;                // backward: [batch][q_heads][tiles of 32 tokens][3][32]
     float *part_dk, *part_dv;        // [row_splits][batch * kv_heads][kv_len][dim]
 };
 

@@ -144,14 +144,14 @@ size_t cross_layout(pa::CrossDev& d, bool backward, char* ws) {
         used += round256(floats * sizeof(float));
         return p;
     };
-    const size_t rows = (size_t)d.batch * d.kv_heads * d.rows, keys = (size_t)d.batch * d.kv_heads * d.kv_len;
+    const size_t keys = (size_t)d.batch * d.kv_heads * d.kv_len;
     if (d.whole < d.tiles) {
         const size_t parts = (size_t)(d.tiles - d.whole) * d.splits * d.tile_rows;
         d.part = take(parts * d.dim);
         if (!backward) d.part_stats = take(parts * 2);
     }
     if (backward) {
-        d.delta = take(rows);
+        d.row_stats = take((size_t)d.batch * d.q_heads * ((d.q_len + 31) / 32) * 96);
         if (d.row_splits > 1) {
             d.part_dk = take((size_t)d.row_splits * keys * d.dim);
             d.part_dv = take((size_t)d.row_splits * keys * d.dim);
