@@ -41,12 +41,26 @@ __global__ __launch_bounds__(kThreads) void k_norm_fwd(NormDev d) {
     const int N = d.cols;
     const T* x = static_cast<const T*>(d.x) + row * d.x_stride;
     T* y = static_cast<T*>(d.y) + row * d.y_stride;
+    const W* w = static_cast<const W*>(d.w);
+    const W* b = static_cast<const W*>(d.b);
+    Pack8<T> raw[CH];
+    Pack8<W> pw[CH], pb[CH];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) raw[c] = load8_raw(x, (c * TPR + t) * 8, N);
+    if (w) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) pw[c] = load8_raw(w, (c * TPR + t) * 8, N);
+    }
+    if (b) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) pb[c] = load8_raw(b, (c * TPR + t) * 8, N);
+    }
     float v[CH][8];
     float s = 0.0f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int col = (c * TPR + t) * 8;
-        const Pack8<T> p = load8(x, col, N);
+        const Pack8<T> p = fix8(raw[c], col, N);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             v[c][i] = (float)p.v[i];
@@ -70,24 +84,20 @@ __global__ __launch_bounds__(kThreads) void k_norm_fwd(NormDev d) {
         if (d.mean) d.mean[row] = mean;
         if (d.rstd) d.rstd[row] = rstd;
     }
-    const W* w = static_cast<const W*>(d.w);
-    const W* b = static_cast<const W*>(d.b);
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const int col = (c * TPR + t) * 8, n = N - col;
-        if (n <= 0) continue;
-        Pack8<W> pw, pb;
-        if (w) pw = load8(w, col, N);
-        if (b) pb = load8(b, col, N);
+        const int col = (c * TPR + t) * 8;
+        if (w) pw[c] = fix8(pw[c], col, N);
+        if (b) pb[c] = fix8(pb[c], col, N);
         Pack8<T> o;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             float r = (v[c][i] - mean) * rstd;
-            if (w) r *= (float)pw.v[i];
-            if (b) r += (float)pb.v[i];
+            if (w) r *= (float)pw[c].v[i];
+            if (b) r += (float)pb[c].v[i];
             o.v[i] = (T)r;
         }
-        store8(y + col, o, n);
+        store8(y + col, o, N - col);
     }
 }
 
@@ -154,29 +164,47 @@ __global__ __launch_bounds__(kThreads) void k_norm_bwd(NormDev d) {
     const W* w = static_cast<const W*>(d.w);
     float aw[CH][8] = {}, ab[CH][8] = {};
     const float n_f = (float)N;
-    int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * RPB + g; row < d.rows; row += (int64_t)gridDim.x * RPB, turn ^= 1) {
+    Pack8<W> pw[CH];
+    if (w) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) pw[c] = load8_raw(w, (c * TPR + t) * 8, N);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) pw[c] = fix8(pw[c], (c * TPR + t) * 8, N);
+    }
+    // The next row is on its way while a row is worked on.
+    Pack8<T> nx[CH], nd[CH];
+    float n_mean = 0.0f, n_rstd = 0.0f;
+    auto load = [&](int64_t row) {
         const T* x = static_cast<const T*>(d.x) + row * d.x_stride;
         const T* dy = static_cast<const T*>(d.dy) + row * d.y_stride;
-        const float mean = d.mean[row], rstd = d.rstd[row];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            nx[c] = load8_raw(x, (c * TPR + t) * 8, N);
+            nd[c] = load8_raw(dy, (c * TPR + t) * 8, N);
+        }
+        n_mean = d.mean[row];
+        n_rstd = d.rstd[row];
+    };
+    const int64_t step = (int64_t)gridDim.x * RPB;
+    int64_t row = (int64_t)blockIdx.x * RPB + g;
+    if (row < d.rows) load(row);
+    for (int turn = 0; row < d.rows; row += step, turn ^= 1) {
+        const float mean = n_mean, rstd = n_rstd;
         Pack8<T> px[CH], pd[CH];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int col = (c * TPR + t) * 8;
-            px[c] = load8(x, col, N);
-            pd[c] = load8(dy, col, N);
+            px[c] = fix8(nx[c], (c * TPR + t) * 8, N);
+            pd[c] = fix8(nd[c], (c * TPR + t) * 8, N);
         }
+        load(row + step < d.rows ? row + step : row);
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int col = (c * TPR + t) * 8;
-            Pack8<W> pw;
-            if (w) pw = load8(w, col, N);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float dyi = (float)pd[c].v[i];          // 0 past the row
                 const float xh = ((float)px[c].v[i] - mean) * rstd;
-                const float gi = w ? dyi * (float)pw.v[i] : dyi;
+                const float gi = w ? dyi * (float)pw[c].v[i] : dyi;
                 s1 += gi;
                 s2 += gi * xh;
                 aw[c][i] += dyi * xh;
@@ -189,19 +217,16 @@ __global__ __launch_bounds__(kThreads) void k_norm_bwd(NormDev d) {
         T* dx = static_cast<T*>(d.dx) + row * d.dx_stride;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int col = (c * TPR + t) * 8, n = N - col;
-            if (n <= 0) continue;
-            Pack8<W> pw;
-            if (w) pw = load8(w, col, N);
+            const int col = (c * TPR + t) * 8;
             Pack8<T> o;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float dyi = (float)pd[c].v[i];
                 const float xh = ((float)px[c].v[i] - mean) * rstd;
-                const float gi = w ? dyi * (float)pw.v[i] : dyi;
+                const float gi = w ? dyi * (float)pw[c].v[i] : dyi;
                 o.v[i] = (T)(rstd * (gi - s1 - xh * s2));
             }
-            store8(dx + col, o, n);
+            store8(dx + col, o, N - col);
         }
     }
     if (!d.part) return;
@@ -315,6 +340,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_fold(NormDev d) {
     if (!out) return;                        // the whole block
     float a = 0.0f;
     if (col < N)
+#pragma unroll 8
         for (int k = r; k < d.blocks; k += 16) a += d.part[((int64_t)k * 2 + blockIdx.y) * N + col];
     s[r][c] = a;
     __syncthreads();
@@ -330,7 +356,8 @@ template <class T, class W>
 hipError_t fwd(const NormDev& d, hipStream_t st) {
     const int64_t N = d.cols;
     const unsigned wave_rows = (unsigned)((d.rows + 3) / 4), block_rows = (unsigned)d.rows;
-    if (N <= 512)       k_norm_fwd<T, W, 1, 1><<<wave_rows, kThreads, 0, st>>>(d);
+    if (N < 8)          k_norm_fwd_long<T, W><<<block_rows, kThreads, 0, st>>>(d);
+    else if (N <= 512)  k_norm_fwd<T, W, 1, 1><<<wave_rows, kThreads, 0, st>>>(d);
     else if (N <= 1024) k_norm_fwd<T, W, 1, 2><<<wave_rows, kThreads, 0, st>>>(d);
     else if (N <= 2048) k_norm_fwd<T, W, 1, 4><<<wave_rows, kThreads, 0, st>>>(d);
     else if (N <= 4096) k_norm_fwd<T, W, 4, 2><<<block_rows, kThreads, 0, st>>>(d);
@@ -344,11 +371,11 @@ hipError_t bwd(const NormDev& d, hipStream_t st) {
     const int64_t N = d.cols;
     const unsigned nb = (unsigned)d.blocks;
     if (d.rows > 0) {
-        if (N <= 512)       k_norm_bwd<T, W, 1, 1><<<nb, kThreads, 0, st>>>(d);
-        else if (N <= 1024) k_norm_bwd<T, W, 1, 2><<<nb, kThreads, 0, st>>>(d);
-        else if (N <= 2048) k_norm_bwd<T, W, 1, 4><<<nb, kThreads, 0, st>>>(d);
-        else if (N <= 4096) k_norm_bwd<T, W, 4, 2><<<nb, kThreads, 0, st>>>(d);
-        else if (N <= 8192) k_norm_bwd<T, W, 4, 4><<<nb, kThreads, 0, st>>>(d);
+        if (N >= 8 && N <= 512) k_norm_bwd<T, W, 1, 1><<<nb, kThreads, 0, st>>>(d);
+        else if (N >= 8 && N <= 1024) k_norm_bwd<T, W, 1, 2><<<nb, kThreads, 0, st>>>(d);
+        else if (N >= 8 && N <= 2048) k_norm_bwd<T, W, 1, 4><<<nb, kThreads, 0, st>>>(d);
+        else if (N >= 8 && N <= 4096) k_norm_bwd<T, W, 4, 2><<<nb, kThreads, 0, st>>>(d);
+        else if (N >= 8 && N <= 8192) k_norm_bwd<T, W, 4, 4><<<nb, kThreads, 0, st>>>(d);
         else {
             for (int64_t r0 = 0; d.dx && r0 < d.rows; r0 += kLaunchRows) {
                 NormDev c = d;

@@ -123,10 +123,23 @@ __device__ __forceinline__ void wait_loads() {
 // see wait_loads) stay in flight, where __syncthreads waits for them all.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
+// Sum over the wave, in every lane: exchanges within 2, 4, 8 and 16 lanes (DPP), then of 16- and 32-lane
+// halves. The order is fixed.
+template <int CTRL>
+__device__ __forceinline__ float dpp_f32(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
 __device__ __forceinline__ float wave_sum_f32(float v) {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
-    return v;
+    v += dpp_f32<0xB1>(v);        // quad_perm [1, 0, 3, 2]
+    v += dpp_f32<0x4E>(v);        // quad_perm [2, 3, 0, 1]
+    v += dpp_f32<0x141>(v);       // row_half_mirror
+    v += dpp_f32<0x140>(v);       // row_mirror
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto p = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const float h = __builtin_bit_cast(float, (uint32_t)p[0]) + __builtin_bit_cast(float, (uint32_t)p[1]);
+    const uint32_t g = __builtin_bit_cast(uint32_t, h);
+    const auto q = __builtin_amdgcn_permlane32_swap(g, g, false, false);
+    return __builtin_bit_cast(float, (uint32_t)q[0]) + __builtin_bit_cast(float, (uint32_t)q[1]);
 }
 
 }  // namespace pa
