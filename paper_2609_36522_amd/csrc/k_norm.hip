@@ -30,6 +30,13 @@ __device__ __forceinline__ float row_sum(float v, float* lds) {
     return (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
+// A thread's chunk of 8 columns from `col`, once loaded. Only the chunks at the row's end (the same for all
+// threads) need fixing.
+template <class T>
+__device__ __forceinline__ Pack8<T> ready(const Pack8<T>& r, int col, int N, bool last) {
+    return last ? fix8(r, col, N) : r;
+}
+
 // CH chunks of 8 columns per thread, WPR (1 or 4) waves per row.
 template <class T, class W, int WPR, int CH>
 __global__ __launch_bounds__(kThreads) void k_norm_fwd(NormDev d) {
@@ -60,7 +67,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_fwd(NormDev d) {
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int col = (c * TPR + t) * 8;
-        const Pack8<T> p = fix8(raw[c], col, N);
+        const Pack8<T> p = ready(raw[c], col, N, (c + 1) * TPR * 8 > N);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             v[c][i] = (float)p.v[i];
@@ -87,8 +94,8 @@ __global__ __launch_bounds__(kThreads) void k_norm_fwd(NormDev d) {
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int col = (c * TPR + t) * 8;
-        if (w) pw[c] = fix8(pw[c], col, N);
-        if (b) pb[c] = fix8(pb[c], col, N);
+        if (w) pw[c] = ready(pw[c], col, N, (c + 1) * TPR * 8 > N);
+        if (b) pb[c] = ready(pb[c], col, N, (c + 1) * TPR * 8 > N);
         Pack8<T> o;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -169,7 +176,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_bwd(NormDev d) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) pw[c] = load8_raw(w, (c * TPR + t) * 8, N);
 #pragma unroll
-        for (int c = 0; c < CH; ++c) pw[c] = fix8(pw[c], (c * TPR + t) * 8, N);
+        for (int c = 0; c < CH; ++c) pw[c] = ready(pw[c], (c * TPR + t) * 8, N, (c + 1) * TPR * 8 > N);
     }
     // The next row is on its way while a row is worked on.
     Pack8<T> nx[CH], nd[CH];
@@ -193,8 +200,8 @@ __global__ __launch_bounds__(kThreads) void k_norm_bwd(NormDev d) {
         Pack8<T> px[CH], pd[CH];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            px[c] = fix8(nx[c], (c * TPR + t) * 8, N);
-            pd[c] = fix8(nd[c], (c * TPR + t) * 8, N);
+            px[c] = ready(nx[c], (c * TPR + t) * 8, N, (c + 1) * TPR * 8 > N);
+            pd[c] = ready(nd[c], (c * TPR + t) * 8, N, (c + 1) * TPR * 8 > N);
         }
         load(row + step < d.rows ? row + step : row);
         float s1 = 0.0f, s2 = 0.0f;
@@ -359,7 +366,8 @@ hipError_t fwd(const NormDev& d, hipStream_t st) {
     if (N < 8)          k_norm_fwd_long<T, W><<<block_rows, kThreads, 0, st>>>(d);
     else if (N <= 512)  k_norm_fwd<T, W, 1, 1><<<wave_rows, kThreads, 0, st>>>(d);
     else if (N <= 1024) k_norm_fwd<T, W, 1, 2><<<wave_rows, kThreads, 0, st>>>(d);
-    else if (N <= 2048) k_norm_fwd<T, W, 1, 4><<<wave_rows, kThreads, 0, st>>>(d);
+    else if (N <= 2048 && sizeof(T) == 2) k_norm_fwd<T, W, 1, 4><<<wave_rows, kThreads, 0, st>>>(d);
+    else if (N <= 2048) k_norm_fwd<T, W, 4, 1><<<block_rows, kThreads, 0, st>>>(d);
     else if (N <= 4096) k_norm_fwd<T, W, 4, 2><<<block_rows, kThreads, 0, st>>>(d);
     else if (N <= 8192) k_norm_fwd<T, W, 4, 4><<<block_rows, kThreads, 0, st>>>(d);
     else                k_norm_fwd_long<T, W><<<block_rows, kThreads, 0, st>>>(d);
@@ -373,7 +381,7 @@ hipError_t bwd(const NormDev& d, hipStream_t st) {
     if (d.rows > 0) {
         if (N >= 8 && N <= 512) k_norm_bwd<T, W, 1, 1><<<nb, kThreads, 0, st>>>(d);
         else if (N >= 8 && N <= 1024) k_norm_bwd<T, W, 1, 2><<<nb, kThreads, 0, st>>>(d);
-        else if (N >= 8 && N <= 2048) k_norm_bwd<T, W, 1, 4><<<nb, kThreads, 0, st>>>(d);
+        else if (N >= 8 && N <= 2048) k_norm_bwd<T, W, 4, 1><<<nb, kThreads, 0, st>>>(d);
         else if (N >= 8 && N <= 4096) k_norm_bwd<T, W, 4, 2><<<nb, kThreads, 0, st>>>(d);
         else if (N >= 8 && N <= 8192) k_norm_bwd<T, W, 4, 4><<<nb, kThreads, 0, st>>>(d);
         else {
@@ -426,7 +434,7 @@ hipError_t norm_forward(const NormDev& d, int dtype, int param_dtype, hipStream_
 // Blocks of the backward pass: enough to fill the 256 CUs a few times over, no more than there are
 // groups of rows, and fewer partial sums than a quarter of the rows.
 int norm_backward_blocks(int64_t rows, int64_t cols) {
-    const int64_t groups = cols <= 2048 ? (rows + 3) / 4 : rows;
+    const int64_t groups = cols <= 1024 ? (rows + 3) / 4 : rows;
     const int64_t most = 512;
     return (int)(groups < most ? groups : most);
 }
