@@ -10,6 +10,7 @@ workspaces come from torch's allocator on that stream. :func:`layer_norm` and
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import math
 
 import torch
@@ -81,16 +82,19 @@ def _on_device(*tensors):
     """The current stream's handle, once every tensor given is on the current device."""
     dev = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and not (t.is_cuda and t.get_device() == dev):
+        if t is not None and t.get_device() != dev:
             raise ValueError(f"expected tensors on the current CUDA device {dev}")
-    return torch.cuda.current_stream(dev).cuda_stream
+    return torch._C._cuda_getCurrentRawStream(dev)
 
 
-def _workspace(query, p, like):
-    """(tensor or None, bytes) of the scratch memory that a call with these sizes needs."""
+def _size(query, p):
     n = C.c_size_t(0)
     B._check(query(C.byref(p), C.byref(n)))
-    return (torch.empty(n.value, dtype=torch.uint8, device=like.device) if n.value else None), n.value
+    return n.value
+
+
+def _workspace(n, like):
+    return torch.empty(n, dtype=torch.uint8, device=like.device) if n else None
 
 
 def _ptr(t):
@@ -127,6 +131,14 @@ def _norm_args(x, weight, bias):
     return pt
 
 
+@functools.lru_cache(maxsize=256)
+def _norm(M, N, dtype, param_dtype, eps, x_stride, y_stride):
+    """The (constant) description of a norm and the workspace that its backward pass needs."""
+    lib = _library()
+    p = Norm(M, N, dtype, param_dtype, eps, x_stride, y_stride, N)
+    return p, C.byref(p), _size(lib.paraanya_layer_norm_backward_workspace, p)
+
+
 def layer_norm_forward(x, weight=None, bias=None, eps=1e-5):
     """(y, mean, rstd) of the norm over x's last dimension; mean and rstd are fp32, one per row."""
     pt = _norm_args(x, weight, bias)
@@ -134,11 +146,12 @@ def layer_norm_forward(x, weight=None, bias=None, eps=1e-5):
     N = x.shape[-1]
     x2 = _rows(x, N)
     M = x2.shape[0]
+    _, ref, _ = _norm(M, N, _DTYPE[x.dtype], _DTYPE[pt], eps, _stride(x2), N)
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    mean, rstd = torch.empty((2, M), dtype=torch.float32, device=x.device)
-    p = Norm(M, N, _DTYPE[x.dtype], _DTYPE[pt], eps, _stride(x2), N, N)
-    B._check(_library().paraanya_layer_norm(C.byref(p), x2.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(),
-                                            mean.data_ptr(), rstd.data_ptr(), st))
+    mean = torch.empty(M, dtype=torch.float32, device=x.device)
+    rstd = torch.empty(M, dtype=torch.float32, device=x.device)
+    B._check(_LIB.paraanya_layer_norm(ref, x2.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), mean.data_ptr(),
+                                      rstd.data_ptr(), st))
     return y, mean, rstd
 
 
@@ -161,13 +174,13 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, *, param_dtype=None):
         if t.dtype != torch.float32 or t.numel() != M or not t.is_contiguous():
             raise ValueError(f"mean and rstd must be contiguous float32 tensors of {M} elements")
     st = _on_device(x, dy, mean, rstd, weight)
+    _, ref, n = _norm(M, N, _DTYPE[x.dtype], _DTYPE[param_dtype], 0.0, _stride(x2), _stride(dy2))
     dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    dw, db = torch.empty((2, N), dtype=param_dtype, device=x.device)
-    p = Norm(M, N, _DTYPE[x.dtype], _DTYPE[param_dtype], 0.0, _stride(x2), _stride(dy2), N)
-    lib = _library()
-    ws, n = _workspace(lib.paraanya_layer_norm_backward_workspace, p, x)
-    B._check(lib.paraanya_layer_norm_backward(C.byref(p), dy2.data_ptr(), x2.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
-                                              _ptr(weight), dx.data_ptr(), dw.data_ptr(), db.data_ptr(), _ptr(ws), n, st))
+    dw = torch.empty(N, dtype=param_dtype, device=x.device)
+    db = torch.empty(N, dtype=param_dtype, device=x.device)
+    ws = _workspace(n, x)
+    B._check(_LIB.paraanya_layer_norm_backward(ref, dy2.data_ptr(), x2.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+                                               _ptr(weight), dx.data_ptr(), dw.data_ptr(), db.data_ptr(), _ptr(ws), n, st))
     return dx, dw, db
 
 
@@ -200,7 +213,21 @@ def _heads(t, name):
     return t if t.stride(3) == 1 or t.shape[3] == 1 else t.contiguous()
 
 
-def _cross_args(q, k, v, kv_lens, mask, scale, o_stride):
+@functools.lru_cache(maxsize=256)
+def _cross(q_shape, k_shape, dtype, scale, q_stride, k_stride, v_stride, o_stride, mask_kind, mask_stride):
+    """The description of an attention without its kv_lens and mask (to be copied), and the workspaces of its
+    forward and backward pass (which do not depend on them)."""
+    (Bn, Lq, Hq, D), (_, Lk, Hk, _) = q_shape, k_shape
+    p = Cross(Bn, Lq, Lk, Hq, Hk, D, dtype, 1.0 / math.sqrt(D) if scale is None else scale,
+              q_stride[:3], k_stride[:3], v_stride[:3], o_stride[:3])
+    p.mask_kind, p.mask_stride = mask_kind, mask_stride
+    if mask_kind:
+        p.mask = 256          # any address: only the sizes are asked for
+    lib = _library()
+    return p, _size(lib.paraanya_cross_attention_workspace, p), _size(lib.paraanya_cross_attention_backward_workspace, p)
+
+
+def _cross_args(q, k, v, kv_lens, mask, scale, o):
     if q.dtype not in (torch.bfloat16, torch.float16):
         raise ValueError(f"cross attention of {q.dtype} is not built")
     if k.dtype != q.dtype or v.dtype != q.dtype:
@@ -211,21 +238,22 @@ def _cross_args(q, k, v, kv_lens, mask, scale, o_stride):
         raise ValueError("k and v must have one shape, and q's batch and head_dim")
     if Hk < 1 or Hq % Hk:
         raise ValueError("q's heads must be a multiple of k's")
-    p = Cross(Bn, Lq, Lk, Hq, Hk, D, _DTYPE[q.dtype], 1.0 / math.sqrt(D) if scale is None else scale,
-              q.stride()[:3], k.stride()[:3], v.stride()[:3], o_stride)
-    if kv_lens is not None:
-        if kv_lens.dtype != torch.int32 or kv_lens.shape != (Bn,) or not kv_lens.is_contiguous():
-            raise ValueError(f"kv_lens must be a contiguous int32 tensor of {Bn} elements")
-        p.kv_lens = kv_lens.data_ptr()
+    if kv_lens is not None and (kv_lens.dtype != torch.int32 or kv_lens.shape != (Bn,) or not kv_lens.is_contiguous()):
+        raise ValueError(f"kv_lens must be a contiguous int32 tensor of {Bn} elements")
+    kind = PA_MASK_NONE
     if mask is not None:
         if mask.dtype not in (torch.bool, torch.uint8, torch.float32) or mask.shape != (Bn, Lk):
             raise ValueError(f"mask must be a bool, uint8 or float32 tensor of [{Bn}, {Lk}]")
         if mask.stride(1) != 1 and Lk > 1:
             raise ValueError("a mask row's elements must be consecutive")
-        p.mask = mask.data_ptr()
-        p.mask_kind = PA_MASK_ADD if mask.dtype == torch.float32 else PA_MASK_BOOL
-        p.mask_stride = mask.stride(0)
-    return p
+        kind = PA_MASK_ADD if mask.dtype == torch.float32 else PA_MASK_BOOL
+    p, forward, backward = _cross(q.shape, k.shape, _DTYPE[q.dtype], scale, q.stride(), k.stride(), v.stride(), o.stride(),
+                                  kind, mask.stride(0) if kind else 0)
+    if kv_lens is not None or kind:
+        p = Cross.from_buffer_copy(p)
+        p.kv_lens = None if kv_lens is None else kv_lens.data_ptr()
+        p.mask = mask.data_ptr() if kind else None
+    return p, forward, backward
 
 
 def cross_attention_forward(q, k, v, *, kv_lens=None, mask=None, scale=None):
@@ -240,12 +268,11 @@ def cross_attention_forward(q, k, v, *, kv_lens=None, mask=None, scale=None):
     q, k, v = _heads(q, "q"), _heads(k, "k"), _heads(v, "v")
     o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     st = _on_device(q, k, v, kv_lens, mask)
-    p = _cross_args(q, k, v, kv_lens, mask, scale, o.stride()[:3])
+    p, n, _ = _cross_args(q, k, v, kv_lens, mask, scale, o)
     stats = torch.empty((q.shape[0], q.shape[2], q.shape[1], 2), dtype=torch.float32, device=q.device)
-    lib = _library()
-    ws, n = _workspace(lib.paraanya_cross_attention_workspace, p, q)
-    B._check(lib.paraanya_cross_attention(C.byref(p), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
-                                          stats.data_ptr(), _ptr(ws), n, st))
+    ws = _workspace(n, q)
+    B._check(_LIB.paraanya_cross_attention(C.byref(p), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
+                                           stats.data_ptr(), _ptr(ws), n, st))
     return o, stats
 
 
@@ -258,16 +285,15 @@ def cross_attention_backward(do, q, k, v, o, stats, *, kv_lens=None, mask=None, 
     if stats.dtype != torch.float32 or stats.shape != (q.shape[0], q.shape[2], q.shape[1], 2) or not stats.is_contiguous():
         raise ValueError("stats must be the forward pass's")
     st = _on_device(q, k, v, o, do, stats, kv_lens, mask)
-    p = _cross_args(q, k, v, kv_lens, mask, scale, o.stride()[:3])
+    p, _, n = _cross_args(q, k, v, kv_lens, mask, scale, o)
     dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     dk = torch.empty(k.shape, dtype=q.dtype, device=q.device)
     dv = torch.empty(v.shape, dtype=q.dtype, device=q.device)
     g = CrossGrad(do.stride()[:3], dq.stride()[:3], dk.stride()[:3], dv.stride()[:3])
-    lib = _library()
-    ws, n = _workspace(lib.paraanya_cross_attention_backward_workspace, p, q)
-    B._check(lib.paraanya_cross_attention_backward(C.byref(p), C.byref(g), do.data_ptr(), q.data_ptr(), k.data_ptr(),
-                                                   v.data_ptr(), o.data_ptr(), stats.data_ptr(), dq.data_ptr(),
-                                                   dk.data_ptr(), dv.data_ptr(), _ptr(ws), n, st))
+    ws = _workspace(n, q)
+    B._check(_LIB.paraanya_cross_attention_backward(C.byref(p), C.byref(g), do.data_ptr(), q.data_ptr(), k.data_ptr(),
+                                                    v.data_ptr(), o.data_ptr(), stats.data_ptr(), dq.data_ptr(),
+                                                    dk.data_ptr(), dv.data_ptr(), _ptr(ws), n, st))
     return dq, dk, dv
 
 
@@ -292,6 +318,13 @@ def cross_attention(q, k, v, *, kv_lens=None, mask=None, scale=None):
 
 
 # ------------------------------------------------------------------ projection with adapters
+@functools.lru_cache(maxsize=256)
+def _lora(M, K, N, R, E, n, dtype, x_stride, w_stride):
+    """The description of a projection without its offsets, ids and scales (to be copied), and its workspace."""
+    p = Lora(M, K, N, R, E, n, dtype, x_stride, w_stride, N, 256, 256, None)
+    return p, _size(_library().paraanya_lora_linear_workspace, p)
+
+
 def lora_linear(x, weight, a, b, offsets, ids, *, scales=None, bias=None):
     """x W^T + bias + scales[i] (x A_i^T) B_i^T with the adapter i of each row's request.
 
@@ -322,10 +355,10 @@ def lora_linear(x, weight, a, b, offsets, ids, *, scales=None, bias=None):
     x, weight = (t if t.stride(1) == 1 and (t.shape[0] < 2 or t.stride(0) >= K) else t.contiguous() for t in (x, weight))
     st = _on_device(x, weight, a, b, offsets, ids, scales, bias)
     y = torch.empty((M, N), dtype=x.dtype, device=x.device)
-    p = Lora(M, K, N, R, E, n, _DTYPE[x.dtype], _stride(x), _stride(weight), N, offsets.data_ptr(), ids.data_ptr(),
-             _ptr(scales))
-    lib = _library()
-    ws, size = _workspace(lib.paraanya_lora_linear_workspace, p, x)
-    B._check(lib.paraanya_lora_linear(C.byref(p), x.data_ptr(), weight.data_ptr(), _ptr(bias), a.data_ptr(), b.data_ptr(),
-                                      y.data_ptr(), _ptr(ws), size, st))
+    p, size = _lora(M, K, N, R, E, n, _DTYPE[x.dtype], _stride(x), _stride(weight))
+    p = Lora.from_buffer_copy(p)
+    p.offsets, p.ids, p.scales = offsets.data_ptr(), ids.data_ptr(), _ptr(scales)
+    ws = _workspace(size, x)
+    B._check(_LIB.paraanya_lora_linear(C.byref(p), x.data_ptr(), weight.data_ptr(), _ptr(bias), a.data_ptr(), b.data_ptr(),
+                                       y.data_ptr(), _ptr(ws), size, st))
     return y
