@@ -198,6 +198,96 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
     }
 }
 
+// The same for at most 128 keys and a head width of at most 64: all keys' scores and dP stay in registers
+// between the pass that forms delta and the one that uses it.
+constexpr int kShortKeys = 128;
+
+template <class T, int MASK, int WIDTH>
+__global__ __launch_bounds__(kThreads, 2) void k_cross_dq_short(CrossDev d) {
+    constexpr int KS = 4, DP = 64, DB = 2, KEYS = kShortKeys, ROWS = 128, NT = KEYS / 32;
+    constexpr bool DIRECT = WIDTH == kWhole;
+    typedef typename Vec<T>::v8 v8;
+    __shared__ __align__(16) T tiles[2][KEYS * DP];
+    __shared__ __align__(16) float bias[MASK ? KEYS : 4];
+
+    const Work wk = work_at(d);
+    const int tile = wk.tile, b = wk.b, hk = wk.hk;
+    const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6;
+    const int row = tile * ROWS + w * 32 + (lane & 31);
+    const bool valid = row < d.rows;
+    const RowAt ra = row_at(d, hk, valid ? row : 0);
+    const int64_t sat = stat_at(d, b, ra);
+    const int kend = sample_keys(d, b);
+    KvStage<T, DP, KEYS, MASK, WIDTH, DIRECT> st(d);
+    if (kend > 0) {
+        st.load(d, static_cast<const T*>(d.k) + b * d.ks[0] + hk * d.ks[2], static_cast<const T*>(d.v) + b * d.vs[0] + hk * d.vs[2],
+                0, kend, tiles[0], tiles[1]);
+        st.load_mask(d, b, 0, kend);
+    }
+    v8 q[KS], g[KS];
+    load_row<T, KS, WIDTH>(q, static_cast<const T*>(d.q) + b * d.qs[0] + ra.token * d.qs[1] + ra.head * d.qs[2], d.dim, half, valid);
+    load_row<T, KS, WIDTH>(g, static_cast<const T*>(d.d_o) + b * d.dos[0] + ra.token * d.dos[1] + ra.head * d.dos[2], d.dim, half, valid);
+    float hi, lo, delta = 0.0f;
+    row_stats<MASK>(d.stats[sat * 2], d.stats[sat * 2 + 1], hi, lo);
+    const float f = d.scale * kLog2e;
+    wait_loads();
+    if (kend > 0) st.arrive(tiles[0], tiles[1], bias, d.dim);
+    lds_barrier();
+
+    f32x16 s[NT], e[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        if (nt * 32 >= kend) break;
+        s[nt] = e[nt] = f32x16{};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            s[nt] = mma(read_rows<T, DP>(tiles[0], nt * 32 + (lane & 31), ks, half), q[ks], s[nt]);
+            e[nt] = mma(read_rows<T, DP>(tiles[1], nt * 32 + (lane & 31), ks, half), g[ks], e[nt]);
+        }
+        if (!MASK && nt * 32 + 32 > kend) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (nt * 32 + 8 * (r >> 2) + 4 * half + (r & 3) >= kend) s[nt][r] = -INFINITY;
+        }
+#pragma unroll
+        for (int g4 = 0; g4 < 4; ++g4) {
+            float4 bv = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if constexpr (MASK != kNoMask) bv = *reinterpret_cast<const float4*>(&bias[nt * 32 + 8 * g4 + 4 * half]);
+            const float bs[4] = {bv.x, bv.y, bv.z, bv.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int r = 4 * g4 + j;
+                s[nt][r] = weight<MASK>(s[nt][r], d.scale, f, bs[j], hi, lo);
+                delta = fmaf(s[nt][r], e[nt][r], delta);
+            }
+        }
+    }
+    delta += __shfl_xor(delta, 32, 64);
+    f32x16 acc[DB];
+#pragma unroll
+    for (int i = 0; i < DB; ++i) acc[i] = f32x16{};
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        if (nt * 32 >= kend) break;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[nt][r] *= e[nt][r] - delta;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const v8 ds = pack<T>(s[nt], t);
+#pragma unroll
+            for (int db = 0; db < DB; ++db) acc[db] = mma(read_cols<T, DP>(tiles[0], nt * 32 + t * 16, db, lane), ds, acc[db]);
+        }
+    }
+    if (valid && half == 0) {
+        float* out = tile_stats(d, b, ra);
+        out[0] = hi;
+        out[32] = lo;
+        out[64] = delta;
+    }
+    T* out = static_cast<T*>(d.dq) + b * d.dqs[0] + ra.token * d.dqs[1] + ra.head * d.dqs[2];
+    store_row<T, DB, WIDTH>(out, d.dim, acc, d.scale, half, valid);
+}
+
 // dk, dv: a wave owns 32 keys (K and V in registers), tiles of 32 tokens of one query head and their
 // statistics pass by, up to three on their way; the heads of the group one after the other.
 template <class T, int KS, int MASK, int WIDTH>
@@ -266,6 +356,7 @@ __global__ __launch_bounds__(kThreads, KS <= 6 ? 2 : 1) void k_cross_dkv(CrossDe
 #pragma unroll
     for (int i = 0; i < DB; ++i) ak[i] = av[i] = f32x16{};
     const float f = d.scale * kLog2e;
+    const bool busy = tile * KEYS + w * 32 < klen;       // the wave has keys
 
     wait_loads();
     if (tbeg < tend) arrive(tbeg, 0);
@@ -276,35 +367,37 @@ __global__ __launch_bounds__(kThreads, KS <= 6 ? 2 : 1) void k_cross_dkv(CrossDe
         if (DIRECT && it + STAGES - 1 < tend) load(it + STAGES - 1, (it + STAGES - 1 - tbeg) % STAGES);
         const T* qt = tiles[p][0];
         const T* gt = tiles[p][1];
-        f32x16 s = f32x16{}, e = f32x16{};
+        if (busy) {
+            f32x16 s = f32x16{}, e = f32x16{};
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            s = mma(read_rows<T, DP>(qt, lane & 31, ks, half), kr[ks], s);
-            e = mma(read_rows<T, DP>(gt, lane & 31, ks, half), vr[ks], e);
-        }
-#pragma unroll
-        for (int g4 = 0; g4 < 4; ++g4) {
-            float4 st[3];
-#pragma unroll
-            for (int i = 0; i < 3; ++i)
-                if (MASK || i != 1) st[i] = *reinterpret_cast<const float4*>(&stat[p][0][i * 32 + 8 * g4 + 4 * half]);
-            const float hi[4] = {st[0].x, st[0].y, st[0].z, st[0].w}, dl[4] = {st[2].x, st[2].y, st[2].z, st[2].w};
-            float lo[4] = {};
-            if constexpr (MASK != kNoMask) lo[0] = st[1].x, lo[1] = st[1].y, lo[2] = st[1].z, lo[3] = st[1].w;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = 4 * g4 + i;
-                s[r] = weight<MASK>(s[r], d.scale, f, bias, hi[i], lo[i]);
-                e[r] = s[r] * (e[r] - dl[i]);
+            for (int ks = 0; ks < KS; ++ks) {
+                s = mma(read_rows<T, DP>(qt, lane & 31, ks, half), kr[ks], s);
+                e = mma(read_rows<T, DP>(gt, lane & 31, ks, half), vr[ks], e);
             }
-        }
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const v8 pw = pack<T>(s, t), ds = pack<T>(e, t);
+            for (int g4 = 0; g4 < 4; ++g4) {
+                float4 st[3];
 #pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                av[db] = mma(read_cols<T, DP>(gt, t * 16, db, lane), pw, av[db]);
-                ak[db] = mma(read_cols<T, DP>(qt, t * 16, db, lane), ds, ak[db]);
+                for (int i = 0; i < 3; ++i)
+                    if (MASK || i != 1) st[i] = *reinterpret_cast<const float4*>(&stat[p][0][i * 32 + 8 * g4 + 4 * half]);
+                const float hi[4] = {st[0].x, st[0].y, st[0].z, st[0].w}, dl[4] = {st[2].x, st[2].y, st[2].z, st[2].w};
+                float lo[4] = {};
+                if constexpr (MASK != kNoMask) lo[0] = st[1].x, lo[1] = st[1].y, lo[2] = st[1].z, lo[3] = st[1].w;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = 4 * g4 + i;
+                    s[r] = weight<MASK>(s[r], d.scale, f, bias, hi[i], lo[i]);
+                    e[r] = s[r] * (e[r] - dl[i]);
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const v8 pw = pack<T>(s, t), ds = pack<T>(e, t);
+#pragma unroll
+                for (int db = 0; db < DB; ++db) {
+                    av[db] = mma(read_cols<T, DP>(gt, t * 16, db, lane), pw, av[db]);
+                    ak[db] = mma(read_cols<T, DP>(qt, t * 16, db, lane), ds, ak[db]);
+                }
             }
         }
         if (it + 1 < tend) {
@@ -332,42 +425,64 @@ __global__ __launch_bounds__(kThreads, KS <= 6 ? 2 : 1) void k_cross_dkv(CrossDe
     }
 }
 
-// dq of the split row tiles from their key ranges, in a fixed order: 32 lanes of 4 columns per row.
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_cross_sum_dq(CrossDev d) {
-    const int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const int rt = (int)(i / d.tile_rows), lr = (int)(i - (int64_t)rt * d.tile_rows), t = d.whole + rt;
-    if (t >= d.tiles) return;
-    const int row_tiles = (d.rows + d.tile_rows - 1) / d.tile_rows, bh = t / row_tiles, row = (t - bh * row_tiles) * d.tile_rows + lr;
-    const int b = bh / d.kv_heads, c = (threadIdx.x & 31) * 4;
-    if (row >= d.rows || c >= d.dim) return;
-    const RowAt a = row_at(d, bh - b * d.kv_heads, row);
-    T* out = static_cast<T*>(d.dq) + b * d.dqs[0] + a.token * d.dqs[1] + a.head * d.dqs[2];
-    const float* p = d.part + ((int64_t)rt * d.splits * d.tile_rows + lr) * d.dim;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        if (c + e >= d.dim) break;
-        float s = 0.0f;
-        for (int k = 0; k < d.splits; ++k) s += p[(int64_t)k * d.tile_rows * d.dim + c + e];
-        out[c + e] = (T)(s * d.scale);
+// Four consecutive columns from c of the partial results at p, `step` floats apart, summed in order.
+__device__ __forceinline__ float4 sum_parts(const float* p, int64_t step, int n, int c, int dim) {
+    struct __attribute__((packed, aligned(4))) Quad { float v[4]; };
+    const int at = c + 4 <= dim ? c : dim - 4;               // a row's last columns, moved into place below
+    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (dim >= 4) {
+#pragma unroll 4
+        for (int k = 0; k < n; ++k) {
+            const Quad q = *reinterpret_cast<const Quad*>(p + k * step + at);
+            s.x += q.v[0], s.y += q.v[1], s.z += q.v[2], s.w += q.v[3];
+        }
+        for (int m = at; m < c; ++m) s.x = s.y, s.y = s.z, s.z = s.w;
+    } else {
+        for (int k = 0; k < n; ++k) {
+            s.x += p[k * step];
+            if (dim > 1) s.y += p[k * step + 1];
+            if (dim > 2) s.z += p[k * step + 2];
+        }
     }
+    return s;
+}
+template <class T>
+__device__ __forceinline__ void store_quad(T* out, float4 s, float f, int c, int dim) {
+    const float v[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (c + e < dim) out[c + e] = (T)(v[e] * f);
 }
 
-// dk (blockIdx.y 0) and dv (1) from their row ranges, in a fixed order.
+// dq of the split row tiles from their key ranges, in a fixed order; four columns a thread.
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_cross_sum_dq(CrossDev d) {
+    const int quads = (d.dim + 3) / 4;
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x, r = i / quads;
+    const int c = (int)(i - r * quads) * 4;
+    const int rt = (int)(r / d.tile_rows), lr = (int)(r - (int64_t)rt * d.tile_rows), t = d.whole + rt;
+    if (t >= d.tiles) return;
+    const int row_tiles = (d.rows + d.tile_rows - 1) / d.tile_rows, bh = t / row_tiles, row = (t - bh * row_tiles) * d.tile_rows + lr;
+    if (row >= d.rows) return;
+    const int b = bh / d.kv_heads;
+    const RowAt a = row_at(d, bh - b * d.kv_heads, row);
+    const float4 s = sum_parts(d.part + ((int64_t)rt * d.splits * d.tile_rows + lr) * d.dim, (int64_t)d.tile_rows * d.dim, d.splits, c, d.dim);
+    store_quad(static_cast<T*>(d.dq) + b * d.dqs[0] + a.token * d.dqs[1] + a.head * d.dqs[2], s, d.scale, c, d.dim);
+}
+
+// dk (blockIdx.y 0) and dv (1) from their row ranges, in a fixed order; four columns a thread.
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_cross_sum_dkv(CrossDev d) {
-    const int64_t n = (int64_t)d.batch * d.kv_heads * d.kv_len * d.dim;
-    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (i >= n) return;
-    const float* part = blockIdx.y ? d.part_dv : d.part_dk;
-    float s = 0.0f;
-#pragma unroll 4
-    for (int k = 0; k < d.row_splits; ++k) s += part[k * n + i];
-    const int c = (int)(i % d.dim);
-    const int64_t r = i / d.dim, bh = r / d.kv_len, b = bh / d.kv_heads;
+    const int quads = (d.dim + 3) / 4;
+    const int64_t n = (int64_t)d.batch * d.kv_heads * d.kv_len;
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x, r = i / quads;
+    if (r >= n) return;
+    const int c = (int)(i - r * quads) * 4;
+    const float4 s = sum_parts((blockIdx.y ? d.part_dv : d.part_dk) + r * d.dim, n * d.dim, d.row_splits, c, d.dim);
+    const int64_t bh = r / d.kv_len, b = bh / d.kv_heads;
     const int hk = (int)(bh - b * d.kv_heads), key = (int)(r - bh * d.kv_len);
-    if (blockIdx.y) static_cast<T*>(d.dv)[b * d.dvs[0] + key * d.dvs[1] + hk * d.dvs[2] + c] = (T)s;
-    else static_cast<T*>(d.dk)[b * d.dks[0] + key * d.dks[1] + hk * d.dks[2] + c] = (T)(s * d.scale);
+    if (blockIdx.y) store_quad(static_cast<T*>(d.dv) + b * d.dvs[0] + key * d.dvs[1] + hk * d.dvs[2], s, 1.0f, c, d.dim);
+    else store_quad(static_cast<T*>(d.dk) + b * d.dks[0] + key * d.dks[1] + hk * d.dks[2], s, d.scale, c, d.dim);
 }
 
 template <class T, int KS, int MASK, int WIDTH>
@@ -376,11 +491,12 @@ hipError_t backward(const CrossDev& d, hipStream_t st) {
     hipError_t e = hipSuccess;
     if (d.dq && d.rows > 0) {
         const unsigned blocks = (unsigned)(d.whole + (d.tiles - d.whole) * d.splits);
-        if (d.kv_len <= kExactKeys) k_cross_dq<T, KS, MASK, WIDTH, true><<<blocks, kThreads, 0, st>>>(d);
+        if (KS == 4 && d.kv_len <= kShortKeys) k_cross_dq_short<T, MASK, WIDTH><<<blocks, kThreads, 0, st>>>(d);
+        else if (d.kv_len <= kExactKeys) k_cross_dq<T, KS, MASK, WIDTH, true><<<blocks, kThreads, 0, st>>>(d);
         else k_cross_dq<T, KS, MASK, WIDTH, false><<<blocks, kThreads, 0, st>>>(d);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         if (d.whole < d.tiles) {
-            k_cross_sum_dq<T><<<blocks_for((int64_t)(d.tiles - d.whole) * d.tile_rows, 8), kThreads, 0, st>>>(d);
+            k_cross_sum_dq<T><<<blocks_for((int64_t)(d.tiles - d.whole) * d.tile_rows * ((d.dim + 3) / 4), kThreads), kThreads, 0, st>>>(d);
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
     } else if (d.rows > 0) {
@@ -391,7 +507,7 @@ hipError_t backward(const CrossDev& d, hipStream_t st) {
         k_cross_dkv<T, KS, MASK, WIDTH><<<(unsigned)((d.kv_len + 127) / 128 * d.row_splits * bh), kThreads, 0, st>>>(d);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         if (d.row_splits > 1) {
-            k_cross_sum_dkv<T><<<dim3(blocks_for(bh * d.kv_len * d.dim, kThreads), 2), kThreads, 0, st>>>(d);
+            k_cross_sum_dkv<T><<<dim3(blocks_for(bh * d.kv_len * ((d.dim + 3) / 4), kThreads), 2), kThreads, 0, st>>>(d);
             e = hipGetLastError();
         }
     }
