@@ -425,35 +425,6 @@ __global__ __launch_bounds__(kThreads, KS <= 6 ? 2 : 1) void k_cross_dkv(CrossDe
     }
 }
 
-// Four consecutive columns from c of the partial results at p, `step` floats apart, summed in order.
-__device__ __forceinline__ float4 sum_parts(const float* p, int64_t step, int n, int c, int dim) {
-    struct __attribute__((packed, aligned(4))) Quad { float v[4]; };
-    const int at = c + 4 <= dim ? c : dim - 4;               // a row's last columns, moved into place below
-    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (dim >= 4) {
-#pragma unroll 4
-        for (int k = 0; k < n; ++k) {
-            const Quad q = *reinterpret_cast<const Quad*>(p + k * step + at);
-            s.x += q.v[0], s.y += q.v[1], s.z += q.v[2], s.w += q.v[3];
-        }
-        for (int m = at; m < c; ++m) s.x = s.y, s.y = s.z, s.z = s.w;
-    } else {
-        for (int k = 0; k < n; ++k) {
-            s.x += p[k * step];
-            if (dim > 1) s.y += p[k * step + 1];
-            if (dim > 2) s.z += p[k * step + 2];
-        }
-    }
-    return s;
-}
-template <class T>
-__device__ __forceinline__ void store_quad(T* out, float4 s, float f, int c, int dim) {
-    const float v[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (c + e < dim) out[c + e] = (T)(v[e] * f);
-}
-
 // dq of the split row tiles from their key ranges, in a fixed order; four columns a thread.
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_cross_sum_dq(CrossDev d) {
@@ -466,7 +437,7 @@ __global__ __launch_bounds__(kThreads) void k_cross_sum_dq(CrossDev d) {
     if (row >= d.rows) return;
     const int b = bh / d.kv_heads;
     const RowAt a = row_at(d, bh - b * d.kv_heads, row);
-    const float4 s = sum_parts(d.part + ((int64_t)rt * d.splits * d.tile_rows + lr) * d.dim, (int64_t)d.tile_rows * d.dim, d.splits, c, d.dim);
+    const float4 s = sum_parts(d.part + ((int64_t)rt * d.splits * d.tile_rows + lr) * d.dim, (int64_t)d.tile_rows * d.dim, d.splits, c, d.dim, [](int) { return 1.0f; });
     store_quad(static_cast<T*>(d.dq) + b * d.dqs[0] + a.token * d.dqs[1] + a.head * d.dqs[2], s, d.scale, c, d.dim);
 }
 
@@ -478,7 +449,8 @@ __global__ __launch_bounds__(kThreads) void k_cross_sum_dkv(CrossDev d) {
     const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x, r = i / quads;
     if (r >= n) return;
     const int c = (int)(i - r * quads) * 4;
-    const float4 s = sum_parts((blockIdx.y ? d.part_dv : d.part_dk) + r * d.dim, n * d.dim, d.row_splits, c, d.dim);
+    const float4 s = sum_parts((blockIdx.y ? d.part_dv : d.part_dk) + r * d.dim, n * d.dim, d.row_splits, c, d.dim,
+                               [](int) { return 1.0f; });
     const int64_t bh = r / d.kv_len, b = bh / d.kv_heads;
     const int hk = (int)(bh - b * d.kv_heads), key = (int)(r - bh * d.kv_len);
     if (blockIdx.y) store_quad(static_cast<T*>(d.dv) + b * d.dvs[0] + key * d.dvs[1] + hk * d.dvs[2], s, 1.0f, c, d.dim);

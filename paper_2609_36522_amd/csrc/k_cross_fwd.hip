@@ -305,51 +305,85 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_few(CrossDev d) {
     }
 }
 
-// Joins the key ranges of the split row tiles: WPR waves per row (one for a few ranges, four, each taking
-// every fourth range, for many).
-template <class T, int WPR>
-__global__ __launch_bounds__(kThreads) void k_cross_join(CrossDev d) {
-    __shared__ float o[WPR == 1 ? 1 : 4][128];
-    const int lane = threadIdx.x & 63, w = WPR == 1 ? 0 : threadIdx.x >> 6;
-    const int i = WPR == 1 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
-    const int rt = i / d.tile_rows, lr = i - rt * d.tile_rows, t = d.whole + rt;
+// The row of the split row tiles that is i-th among their tile_rows each; false past the last.
+__device__ __forceinline__ bool split_row(const CrossDev& d, int64_t i, int& b, RowAt& ra, int64_t& part) {
+    const int rt = (int)(i / d.tile_rows), lr = (int)(i - (int64_t)rt * d.tile_rows), t = d.whole + rt;
     const int row_tiles = (d.rows + d.tile_rows - 1) / d.tile_rows, bh = t / row_tiles, row = (t - bh * row_tiles) * d.tile_rows + lr;
-    if (row >= d.rows) return;               // the whole block, or (WPR = 1) a wave of a kernel without barriers
-    const int64_t first = (int64_t)rt * d.splits * d.tile_rows + lr;     // partial row of range 0; the next are tile_rows apart
-    const float* ps = d.part_stats + first * 2;
+    if (t >= d.tiles || row >= d.rows) return false;
+    b = bh / d.kv_heads;
+    ra = row_at(d, bh - b * d.kv_heads, row);
+    part = (int64_t)rt * d.splits * d.tile_rows + lr;        // of the first range; the next are tile_rows apart
+    return true;
+}
+
+// Joins a few key ranges (at most kFewParts): four columns a thread, which forms the row's weights itself.
+constexpr int kFewParts = 8;
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_cross_join(CrossDev d) {
+    const int quads = (d.dim + 3) / 4;
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x, r = i / quads;
+    const int c = (int)(i - r * quads) * 4;
+    int b;
+    RowAt ra;
+    int64_t part;
+    if (!split_row(d, r, b, ra, part)) return;
+    const float* ps = d.part_stats + part * 2;
+    const int64_t step = (int64_t)d.tile_rows * 2;
+    float m[kFewParts], top = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kFewParts; ++k) {
+        m[k] = k < d.splits ? ps[k * step] : -INFINITY;
+        top = fmaxf(top, m[k]);
+    }
+    const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+    for (int k = 0; k < kFewParts; ++k)
+        if (k < d.splits) sum = fmaf(__builtin_amdgcn_exp2f((m[k] - base) * kLog2e), ps[k * step + 1], sum);
+    const float4 o = sum_parts(d.part + part * d.dim, (int64_t)d.tile_rows * d.dim, d.splits, c, d.dim,
+                               [&](int k) { return __builtin_amdgcn_exp2f((ps[k * step] - base) * kLog2e); });
+    store_quad(static_cast<T*>(d.o) + b * d.os[0] + ra.token * d.os[1] + ra.head * d.os[2], o, sum == 0.0f ? 0.0f : 1.0f / sum, c, d.dim);
+    if (d.stats && c == 0) {
+        float* sp = d.stats + stat_at(d, b, ra) * 2;
+        sp[0] = top;
+        sp[1] = logf(sum);
+    }
+}
+
+// Joins many: a block per row, its waves take every fourth range.
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_cross_join_many(CrossDev d) {
+    __shared__ float o[4][128];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c = threadIdx.x;
+    int b;
+    RowAt ra;
+    int64_t part;
+    if (!split_row(d, blockIdx.x, b, ra, part)) return;      // the whole block
+    const float* ps = d.part_stats + part * 2;
+    const int64_t step = (int64_t)d.tile_rows * 2;
     float top = -INFINITY;
-    for (int s = lane; s < d.splits; s += 64) top = fmaxf(top, ps[(int64_t)s * d.tile_rows * 2]);
+    for (int s = lane; s < d.splits; s += 64) top = fmaxf(top, ps[s * step]);
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
     const float base = top == -INFINITY ? 0.0f : top;
     float sum = 0.0f;
-    for (int s = lane; s < d.splits; s += 64)
-        sum += __builtin_amdgcn_exp2f((ps[(int64_t)s * d.tile_rows * 2] - base) * kLog2e) * ps[(int64_t)s * d.tile_rows * 2 + 1];
+    for (int s = lane; s < d.splits; s += 64) sum += __builtin_amdgcn_exp2f((ps[s * step] - base) * kLog2e) * ps[s * step + 1];
     sum = wave_sum_f32(sum);
     float o0 = 0.0f, o1 = 0.0f;
     const int c0 = lane < d.dim ? lane : 0, c1 = lane + 64 < d.dim ? lane + 64 : 0;
 #pragma unroll 4
-    for (int s = w; s < d.splits; s += WPR) {
-        const float a = __builtin_amdgcn_exp2f((ps[(int64_t)s * d.tile_rows * 2] - base) * kLog2e);
-        const float* p = d.part + (first + (int64_t)s * d.tile_rows) * d.dim;
+    for (int s = w; s < d.splits; s += 4) {
+        const float a = __builtin_amdgcn_exp2f((ps[s * step] - base) * kLog2e);
+        const float* p = d.part + (part + (int64_t)s * d.tile_rows) * d.dim;
         o0 = fmaf(a, p[c0], o0);
         o1 = fmaf(a, p[c1], o1);
     }
-    const int b = bh / d.kv_heads;
-    const RowAt ra = row_at(d, bh - b * d.kv_heads, row);
+    o[w][lane] = o0;
+    o[w][lane + 64] = o1;
+    __syncthreads();
     T* op = static_cast<T*>(d.o) + b * d.os[0] + ra.token * d.os[1] + ra.head * d.os[2];
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    if constexpr (WPR == 1) {
-        if (lane < d.dim) op[lane] = (T)(o0 * inv);
-        if (lane + 64 < d.dim) op[lane + 64] = (T)(o1 * inv);
-    } else {
-        o[w][lane] = o0;
-        o[w][lane + 64] = o1;
-        __syncthreads();
-        const int c = threadIdx.x;
-        if (c < d.dim) op[c] = (T)(((o[0][c] + o[1][c]) + (o[2][c] + o[3][c])) * inv);
-    }
-    if (d.stats && lane == 0 && w == 0) {
+    if (c < d.dim) op[c] = (T)(((o[0][c] + o[1][c]) + (o[2][c] + o[3][c])) * (sum == 0.0f ? 0.0f : 1.0f / sum));
+    if (d.stats && c == 0) {
         float* sp = d.stats + stat_at(d, b, ra) * 2;
         sp[0] = top;
         sp[1] = logf(sum);
@@ -363,9 +397,9 @@ hipError_t forward(const CrossDev& d, hipStream_t st) {
     else k_cross_fwd<T, KS, MASK, WIDTH><<<blocks, kThreads, 0, st>>>(d);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || d.whole == d.tiles) return e;
-    const unsigned rows = (unsigned)((d.tiles - d.whole) * d.tile_rows);
-    if (d.splits > 8) k_cross_join<T, 4><<<rows, kThreads, 0, st>>>(d);
-    else k_cross_join<T, 1><<<rows / 4, kThreads, 0, st>>>(d);
+    const int64_t rows = (int64_t)(d.tiles - d.whole) * d.tile_rows;
+    if (d.splits > kFewParts) k_cross_join_many<T><<<(unsigned)rows, kThreads, 0, st>>>(d);
+    else k_cross_join<T><<<blocks_for(rows * ((d.dim + 3) / 4), kThreads), kThreads, 0, st>>>(d);
     return hipGetLastError();
 }
 

@@ -270,6 +270,39 @@ __device__ __forceinline__ Work work_at(const CrossDev& d) {
     return w;
 }
 
+// Four consecutive columns from c of the n partial results at p, `step` floats apart, times weight(k), summed
+// in order.
+template <class F>
+__device__ __forceinline__ float4 sum_parts(const float* p, int64_t step, int n, int c, int dim, F weight_of) {
+    struct __attribute__((packed, aligned(4))) Quad { float v[4]; };
+    const int at = c + 4 <= dim ? c : dim - 4;               // a row's last columns, moved into place below
+    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (dim >= 4) {
+#pragma unroll 4
+        for (int k = 0; k < n; ++k) {
+            const Quad q = *reinterpret_cast<const Quad*>(p + k * step + at);
+            const float f = weight_of(k);
+            s.x = fmaf(f, q.v[0], s.x), s.y = fmaf(f, q.v[1], s.y), s.z = fmaf(f, q.v[2], s.z), s.w = fmaf(f, q.v[3], s.w);
+        }
+        for (int m = at; m < c; ++m) s.x = s.y, s.y = s.z, s.z = s.w;
+    } else {
+        for (int k = 0; k < n; ++k) {
+            const float f = weight_of(k);
+            s.x = fmaf(f, p[k * step], s.x);
+            if (dim > 1) s.y = fmaf(f, p[k * step + 1], s.y);
+            if (dim > 2) s.z = fmaf(f, p[k * step + 2], s.z);
+        }
+    }
+    return s;
+}
+template <class T>
+__device__ __forceinline__ void store_quad(T* out, float4 s, float f, int c, int dim) {
+    const float v[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (c + e < dim) out[c + e] = (T)(v[e] * f);
+}
+
 // With a mask, or a scale that is not positive (the largest scaled score is then not the scaled
 // largest product), scores are formed before the maximum is taken.
 inline int mask_of(const CrossDev& d) {
