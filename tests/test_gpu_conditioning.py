@@ -1,0 +1,88 @@
+"""The conditioned block (paper_2609_36522_amd/conditioning.py) on the device: its operators together as a
+program uses them, against the same block in 64 bits. A bound on the result of a chain of roundings is a
+multiple of the element type's: each of the block's roundings (norm, three projections, weights, attention,
+last projection, sum) moves the result by at most about u of its own size."""
+import math
+
+import pytest
+import torch
+
+from paper_2609_36522_amd import conditioning, workloads
+
+pytestmark = pytest.mark.gpu
+
+U = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+
+
+@pytest.fixture(autouse=True)
+def _lib(gpu_lib):
+    return gpu_lib
+
+
+def _exact(blk, h, ctx, lengths, adapters=None, ids=None, leaves=None):
+    """The block in 64 bits; leaves: 64-bit versions of [h, ctx, *parameters]."""
+    p = [t.double() for t in (h, ctx, *blk.parameters())] if leaves is None else leaves
+    H, C, gain, shift, W = p[0], p[1], p[2], p[3], dict(zip(conditioning.PROJECTIONS, p[4:]))
+    B, T, D = H.shape[0], H.shape[1], blk.head_dim
+
+    def project(name, x):
+        y = x @ W[name].T
+        if ids is None:
+            return y
+        add = []
+        for i, a in enumerate(ids.tolist()):
+            t = x[i] @ adapters.a[name][a].double().T @ adapters.b[name][a].double().T if a >= 0 else torch.zeros_like(y[i])
+            add.append(t * float(adapters.scales[a]) if a >= 0 else t)
+        return y + torch.stack(add)
+
+    x = (H - H.mean(-1, keepdim=True)) / torch.sqrt(H.var(-1, unbiased=False, keepdim=True) + blk.eps) * gain + shift
+    q = project("q", x).reshape(B, T, blk.heads, D).transpose(1, 2)
+    G = blk.heads // blk.kv_heads
+    k, v = (project(n, C).reshape(B, -1, blk.kv_heads, D).transpose(1, 2).repeat_interleave(G, 1) for n in ("k", "v"))
+    s = q @ k.transpose(-1, -2) / math.sqrt(D)
+    if lengths is not None:
+        s = s.masked_fill(torch.arange(s.shape[-1], device="cuda") >= lengths[:, None, None, None], -math.inf)
+    o = (torch.softmax(s, -1) @ v).transpose(1, 2).reshape(B, T, blk.hidden)
+    return H + project("o", o)
+
+
+def _inputs(wl, blk, batch, states, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    tokens = wl.latent[1] // 2 * (wl.latent[2] // 2)
+    dt = blk.weight.dtype
+    h = torch.randn((batch, tokens, blk.hidden), generator=g, device="cuda").to(dt)
+    ctx = torch.randn((batch, states, blk.context), generator=g, device="cuda").to(dt)
+    return h, ctx, torch.randn(h.shape, generator=g, device="cuda").to(dt)
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16], ids=["bf16", "f16"])
+@pytest.mark.parametrize("states,kv_heads", [(77, 8), (21, 2)])
+def test_serving_a_batch_of_requests_with_their_own_adapters(states, kv_heads, dt):
+    wl = workloads.SMALL_MLP
+    blk = conditioning.ConditionedBlock(wl.hidden, 384, 8, kv_heads, dtype=dt)
+    h, ctx, _ = _inputs(wl, blk, 4, states, 0)
+    ad = blk.adapters(3, 16)
+    ids = torch.tensor([2, -1, 0, 2], dtype=torch.int32, device="cuda")
+    lengths = torch.tensor([states, 1, states // 2, 13], dtype=torch.int32, device="cuda")
+    y = blk.serve(h, ctx, ad, ids, lengths=lengths)
+    want = _exact(blk, h, ctx, lengths, ad, ids)
+    err, size = (y.double() - want).norm(), (want - h.double()).norm()
+    assert float(err / size) < 8 * U[dt], float(err / size)
+    # Each sample depends on its own request alone.
+    one = blk.serve(h[2:3], ctx[2:3], ad, ids[2:3].contiguous(), lengths=lengths[2:3].contiguous())
+    assert float((one[0].double() - y[2].double()).abs().max()) <= 8 * U[dt] * float(y[2].double().abs().max())
+
+
+def test_training_step_gradients():
+    wl = workloads.SMALL_MLP
+    blk = conditioning.ConditionedBlock(wl.hidden, 256, 8, 4)
+    h, ctx, dy = _inputs(wl, blk, 2, 77, 1)
+    lengths = torch.tensor([77, 40], dtype=torch.int32, device="cuda")
+    leaves = [t.requires_grad_(True) for t in (h, ctx, *blk.parameters())]
+    blk(h, ctx, lengths=lengths).backward(dy)
+    exact = [t.detach().double().requires_grad_(True) for t in leaves]
+    _exact(blk, h, ctx, lengths, leaves=exact).backward(dy.double())
+    for name, got, want in zip(("h", "context", "norm weight", "norm bias", *conditioning.PROJECTIONS), leaves, exact):
+        err = float((got.grad.double() - want.grad).norm() / want.grad.norm())
+        assert err < 12 * U[torch.bfloat16], (name, err)
+    assert not bool(ctx.grad[1, 40:].any())           # states past the prompt's length
