@@ -23,6 +23,12 @@ namespace {
 constexpr int64_t kBufferStride = 1 << 22;
 constexpr int kCUs = 256;
 
+// A width of its own for the tiles: rows of an even number of elements (at least 8) at even addresses and
+// strides, which are read as whole ones are but for the piece that holds the row's end (32768x2044x2048:
+// 492 us as ragged rows, 289 so). It and kWhole are for ranks of a multiple of 8.
+constexpr int kEven = 3;
+constexpr bool direct(int width) { return width == kWhole || width == kEven; }
+
 // Rows of request i, clamped to the matrix.
 __device__ __forceinline__ int offset_at(const LoraDev& d, int i) {
     const int o = d.offsets[i];
@@ -60,22 +66,23 @@ __device__ __forceinline__ typename Vec<T>::v8 fixed(typename Vec<T>::v8 r, int 
     return r;
 }
 
-// ROWS rows x 64 columns of a matrix on their way to LDS, THREADS threads. With kWhole by loads that write
+// ROWS rows x 64 columns of a matrix on their way to LDS, THREADS threads. kWhole and kEven by loads that write
 // LDS themselves (a wave's lanes fill consecutive 16-byte slots, so the permutation of a row's pieces is in
 // the addresses that they read; what does not exist has an offset out of the buffer's range, which reads
-// as zero), otherwise through registers.
+// as zero), otherwise through registers. A piece that holds a row's end is read as the row's last eight
+// elements and moved into place once it is there.
 template <class T, int ROWS, int THREADS, int WIDTH>
 struct Stage {
     static constexpr int kPieces = ROWS * 8 / THREADS, kStep = THREADS / 8;
-    uint4 r[WIDTH == kWhole ? 1 : kPieces];
-    uint32_t off[WIDTH == kWhole ? kPieces : 1];
+    uint4 r[direct(WIDTH) ? 1 : kPieces];
+    uint32_t off[direct(WIDTH) ? kPieces : 1];
     int piece, row, rows, at, len;
 
     // The matrix's row 0 of this tile exists, and rows - 1 more; rows are n long.
     __device__ __forceinline__ Stage(int64_t stride, int rows_, int n) : rows(rows_), at(0), len(n) {
         row = (int)threadIdx.x >> 3;
         piece = (int)threadIdx.x & 7;
-        if constexpr (WIDTH == kWhole) {
+        if constexpr (direct(WIDTH)) {
             piece = (piece_at<64>(row, piece) - row * 64) >> 3;     // the same for every kStep (16 or more) rows
 #pragma unroll
             for (int i = 0; i < kPieces; ++i)
@@ -84,12 +91,21 @@ struct Stage {
     }
     // Columns k0 .. of the rows at `base`.
     __device__ __forceinline__ void load(const T* base, int64_t stride, int k0, T* tile) {
-        if constexpr (WIDTH == kWhole) {
-            const __amdgpu_buffer_rsrc_t from = buffer_at(base + k0);
+        if constexpr (direct(WIDTH)) {
             const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
             const bool in = k0 + piece * 8 < len;
+            if (WIDTH == kEven && k0 + 64 > len) {                  // the rows' last columns
+                at = k0 + piece * 8;
+                const uint32_t col = (at + 8 <= len ? k0 : len - 8 - piece * 8) * 2;
+                const __amdgpu_buffer_rsrc_t from = buffer_at(base);
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) load_lds(from, tile + (w * 64 + i * THREADS) * 8, in ? off[i] : kNowhere, 0);
+                for (int i = 0; i < kPieces; ++i)
+                    load_lds(from, tile + (w * 64 + i * THREADS) * 8, in && off[i] != kNowhere ? off[i] + col : kNowhere, 0);
+            } else {
+                const __amdgpu_buffer_rsrc_t from = buffer_at(base + k0);
+#pragma unroll
+                for (int i = 0; i < kPieces; ++i) load_lds(from, tile + (w * 64 + i * THREADS) * 8, in ? off[i] : kNowhere, 0);
+            }
         } else {
             at = k0 + piece * 8;
 #pragma unroll
@@ -100,9 +116,18 @@ struct Stage {
             }
         }
     }
-    // Registers into LDS (kWhole: nothing to do, the loads are waited for by the caller).
-    __device__ __forceinline__ void arrive(T* tile) {
-        if constexpr (WIDTH != kWhole) {
+    // Registers into LDS; direct loads (which the caller has waited for) are in place but for the rows' last
+    // columns, which the last part's threads move.
+    __device__ __forceinline__ void arrive(T* tile, bool last) {
+        if constexpr (WIDTH == kEven) {
+            if (last && at < len && at + 8 > len) {
+#pragma unroll
+                for (int i = 0; i < kPieces; ++i) {
+                    uint4* slot = reinterpret_cast<uint4*>(tile + (threadIdx.x + i * THREADS) * 8);
+                    *slot = __builtin_bit_cast(uint4, shift8(__builtin_bit_cast(Pack8<T>, *slot), at + 8 - len));
+                }
+            }
+        } else if constexpr (WIDTH != kWhole) {
             const bool whole = at - piece * 8 + 64 <= len && rows >= ROWS;      // nothing to fix (the same in all lanes)
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {
@@ -119,7 +144,7 @@ struct Stage {
 // the reading of x: three parts of 64 columns are on their way during the products of the current one.
 template <class T, int NR, int WIDTH>
 __global__ __launch_bounds__(256) void k_lora_down(LoraDev d) {
-    constexpr int ROWS = 64, STAGES = WIDTH == kWhole ? 4 : 2, PART = (ROWS + NR * 32) * 64, LOADS = (ROWS + NR * 32) * 8 / 256;
+    constexpr int ROWS = 64, STAGES = direct(WIDTH) ? 4 : 2, PART = (ROWS + NR * 32) * 64, LOADS = (ROWS + NR * 32) * 8 / 256;
     static_assert(STAGES * PART * 2 >= NR * 32 * (ROWS + 1) * 4, "the halves of the reduction are joined in the tiles' memory");
     __shared__ __align__(16) T tiles[STAGES * PART];
     float (*join)[ROWS + 1] = reinterpret_cast<float (*)[ROWS + 1]>(tiles);
@@ -141,16 +166,16 @@ __global__ __launch_bounds__(256) void k_lora_down(LoraDev d) {
             sx.load(x, d.x_stride, part * 64, tiles + p * PART);
             sa.load(a, K, part * 64, tiles + p * PART + ROWS * 64);
         };
-        auto arrive = [&](int p) {
-            sx.arrive(tiles + p * PART);
-            sa.arrive(tiles + p * PART + ROWS * 64);
+        auto arrive = [&](int part, int p) {
+            sx.arrive(tiles + p * PART, part == parts - 1);
+            sa.arrive(tiles + p * PART + ROWS * 64, part == parts - 1);
         };
 #pragma unroll
         for (int n = 0; n < STAGES - 1; ++n)
             if (n < parts) load(n, n);
         if (parts >= STAGES - 1) wait_loads<(STAGES - 2) * LOADS>();
         else wait_loads();
-        arrive(0);
+        arrive(0, 0);
         lds_barrier();
         for (int n = 0; n < parts; ++n) {
             const T* xt = tiles + n % STAGES * PART;
@@ -167,7 +192,7 @@ __global__ __launch_bounds__(256) void k_lora_down(LoraDev d) {
             if (n + 1 < parts) {
                 if (n + STAGES - 1 < parts) wait_loads<(STAGES - 2) * LOADS>();      // the next part is there
                 else wait_loads();
-                arrive(q);
+                arrive(n + 1, (n + 1) % STAGES);
             }
             lds_barrier();
         }
@@ -276,7 +301,7 @@ __device__ __forceinline__ void add_adapters(const LoraDev& d, int f0, int r0, i
 #pragma unroll
             for (int m = 0; m < NM; ++m) {
                 const int f = f0 + m * 32 + (lane & 31);
-                bv[m] = operand<T, WIDTH == kWhole ? kWhole : kTiny>(b + (int64_t)f * d.rank, k, d.rank, f < d.out);
+                bv[m] = operand<T, direct(WIDTH) ? kWhole : kTiny>(b + (int64_t)f * d.rank, k, d.rank, f < d.out);
             }
 #pragma unroll
             for (int m = 0; m < NM; ++m)
@@ -327,7 +352,7 @@ template <class T, int WF, int WR, int NM, int NX, int STAGES, int WIDTH>
 __global__ __launch_bounds__(64 * WF * WR, NM * NX == 16 ? 1 : 2) void k_lora_tile(LoraDev d) {
     typedef typename Vec<T>::v8 v8;
     constexpr int TF = WF * NM * 32, TR = WR * NX * 32, THREADS = 64 * WF * WR;
-    static_assert(WIDTH == kWhole || STAGES == 2, "registers hold one part");
+    static_assert(direct(WIDTH) || STAGES == 2, "registers hold one part");
     __shared__ __align__(16) T tiles[STAGES][(TF + TR) * 64];
     const int f_tiles = (d.out + TF - 1) / TF;
     const int id = xcd_order(blockIdx.x, gridDim.x);
@@ -343,9 +368,9 @@ __global__ __launch_bounds__(64 * WF * WR, NM * NX == 16 ? 1 : 2) void k_lora_ti
         sw.load(wp, d.w_stride, i * 64, tiles[p]);
         sx.load(xp, d.x_stride, i * 64, tiles[p] + TF * 64);
     };
-    auto arrive = [&](int p) {
-        sw.arrive(tiles[p]);
-        sx.arrive(tiles[p] + TF * 64);
+    auto arrive = [&](int i, int p) {
+        sw.arrive(tiles[p], i == parts - 1);
+        sx.arrive(tiles[p] + TF * 64, i == parts - 1);
     };
     f32x16 acc[NM][NX];
     const int fw = (w % WF) * NM * 32, rw = (w / WF) * NX * 32;
@@ -356,7 +381,7 @@ __global__ __launch_bounds__(64 * WF * WR, NM * NX == 16 ? 1 : 2) void k_lora_ti
     const int first = d.adapters > 0 ? request_from(d, r0 + rw) : 0;
     if (parts >= STAGES - 1) wait_loads<(STAGES - 2) * LOADS>();
     else wait_loads();
-    arrive(0);
+    arrive(0, 0);
     lds_barrier();
     int p = 0;
     for (int i = 0; i < parts; ++i) {
@@ -392,7 +417,7 @@ __global__ __launch_bounds__(64 * WF * WR, NM * NX == 16 ? 1 : 2) void k_lora_ti
         if (i + 1 < parts) {
             if (i + STAGES - 1 < parts) wait_loads<(STAGES - 2) * LOADS>();      // the next part is there
             else wait_loads();
-            arrive(q);
+            arrive(i + 1, p + 1 == STAGES ? 0 : p + 1);
         }
         lds_barrier();
         if (++p == STAGES) p = 0;
@@ -446,6 +471,9 @@ __global__ __launch_bounds__(1024) void k_lora_rows(LoraDev d) {
     finish<T, 1, 1>(d, f0, r0, lane, acc);
 }
 
+// The kernels that read operands straight from memory take even rows as ragged ones.
+constexpr int in_place(int width) { return width == kEven ? kRagged : width; }
+
 template <class T, int NR, int WIDTH>
 void down(const LoraDev& d, hipStream_t st) {
     // Blocks per request: its share of the rows, so that the launch has about rows / 64 (or 32) of them.
@@ -454,13 +482,13 @@ void down(const LoraDev& d, hipStream_t st) {
     const bool few = d.rows < 64 * kCUs || d.rows < 64 * d.requests;
     const int per = d.rows / (few ? 32 : 64) / d.requests + 1;
     const dim3 grid((unsigned)(per < 4096 ? per : 4096), (unsigned)d.requests);
-    if (few) k_lora_down_few<T, NR, WIDTH><<<grid, 1024 / NR, 0, st>>>(d);
+    if (few) k_lora_down_few<T, NR, in_place(WIDTH)><<<grid, 1024 / NR, 0, st>>>(d);
     else k_lora_down<T, NR, WIDTH><<<grid, 256, 0, st>>>(d);
 }
 
-int64_t tiles_of(const LoraDev& d, int t) { return (int64_t)((d.out + t - 1) / t) * ((d.rows + t - 1) / t); }
+int64_t tiles_of(const LoraDev& d, int f, int r) { return (int64_t)((d.out + f - 1) / f) * ((d.rows + r - 1) / r); }
 
-// The largest tile that still gives every CU a block; few rows read W straight from memory.
+// The largest tile (features x rows) that still gives every CU a block; few rows read W straight from memory.
 template <class T, int WIDTH>
 hipError_t run(const LoraDev& d, hipStream_t st) {
     if (d.adapters > 0) {
@@ -470,26 +498,37 @@ hipError_t run(const LoraDev& d, hipStream_t st) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (d.rows <= 64)
-        k_lora_rows<T, WIDTH><<<dim3((unsigned)((d.out + 31) / 32), (unsigned)((d.rows + 31) / 32)), 1024, 0, st>>>(d);
-    else if (WIDTH == kWhole && tiles_of(d, 256) >= kCUs)
-        k_lora_tile<T, 2, 4, 4, 2, 2, kWhole><<<(unsigned)tiles_of(d, 256), 512, 0, st>>>(d);
-    else if (WIDTH == kWhole && (int64_t)((d.out + 255) / 256) * ((d.rows + 127) / 128) >= kCUs)
-        k_lora_tile<T, 4, 2, 2, 2, 3, kWhole><<<(unsigned)((int64_t)((d.out + 255) / 256) * ((d.rows + 127) / 128)), 512, 0, st>>>(d);
-    else if (tiles_of(d, 128) >= kCUs)
-        k_lora_tile<T, 2, 2, 2, 2, 2, WIDTH><<<(unsigned)tiles_of(d, 128), 256, 0, st>>>(d);
+    if (d.rows <= 64) {
+        k_lora_rows<T, in_place(WIDTH)><<<dim3((unsigned)((d.out + 31) / 32), (unsigned)((d.rows + 31) / 32)), 1024, 0, st>>>(d);
+        return hipGetLastError();
+    }
+    if constexpr (direct(WIDTH)) {
+        if (tiles_of(d, 256, 256) >= kCUs) {
+            k_lora_tile<T, 2, 4, 4, 2, 2, WIDTH><<<(unsigned)tiles_of(d, 256, 256), 512, 0, st>>>(d);
+            return hipGetLastError();
+        }
+        if (tiles_of(d, 256, 128) >= kCUs) {
+            k_lora_tile<T, 4, 2, 2, 2, 3, WIDTH><<<(unsigned)tiles_of(d, 256, 128), 512, 0, st>>>(d);
+            return hipGetLastError();
+        }
+    }
+    if (tiles_of(d, 128, 128) >= kCUs)
+        k_lora_tile<T, 2, 2, 2, 2, 2, WIDTH><<<(unsigned)tiles_of(d, 128, 128), 256, 0, st>>>(d);
     else
-        k_lora_tile<T, 2, 2, 1, 1, WIDTH == kWhole ? 4 : 2, WIDTH><<<(unsigned)tiles_of(d, 64), 256, 0, st>>>(d);
+        k_lora_tile<T, 2, 2, 1, 1, direct(WIDTH) ? 4 : 2, WIDTH><<<(unsigned)tiles_of(d, 64, 64), 256, 0, st>>>(d);
     return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t lora_linear(const LoraDev& d, int dtype, hipStream_t st) {
-    const bool ragged = d.in % 8 != 0 || d.rank % 8 != 0 || d.x_stride >= kBufferStride || d.w_stride >= kBufferStride;
+    const int64_t odd = (int64_t)d.in | d.x_stride | d.w_stride;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(d.x) | reinterpret_cast<uintptr_t>(d.w) | reinterpret_cast<uintptr_t>(d.a);
+    const bool near = d.x_stride < kBufferStride && d.w_stride < kBufferStride && at % 4 == 0 && odd % 2 == 0 && d.rank % 8 == 0;
     auto typed = [&](auto t) {
         typedef decltype(t) T;
-        return d.in < 8 ? run<T, kTiny>(d, st) : ragged ? run<T, kRagged>(d, st) : run<T, kWhole>(d, st);
+        if (d.in < 8) return run<T, kTiny>(d, st);
+        return !near ? run<T, kRagged>(d, st) : d.in % 8 != 0 ? run<T, kEven>(d, st) : run<T, kWhole>(d, st);
     };
     return dtype == PA_BF16 ? typed((__bf16)0) : typed((_Float16)0);
 }

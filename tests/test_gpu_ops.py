@@ -355,6 +355,16 @@ def test_lora_linear(M, K, N, Rk, dt):
     _check_lora(x, w, a, b, cuts, [2, 0, -1, 1, 0], s, bias)
 
 
+@pytest.mark.parametrize("K", [64, 70, 71, 200])
+@pytest.mark.parametrize("M,N", [(8200, 2050), (8200, 1030), (4200, 1030), (1030, 520), (17000, 70)])
+def test_lora_linear_every_tile_size(M, N, K):
+    """Sizes that take the projection's tiles from the largest to the smallest, with rows of whole pieces, of
+    an even and of an odd length, and t's kernel for many rows."""
+    x, w, a, b, s, bias = _lora_case(M, K, N, 24, 3, BF16)
+    cuts = [0, 7, M // 3, M // 3 + 1, M - 5, M]
+    _check_lora(x, w, a, b, cuts, [2, 0, -1, 1, 2], s, bias)
+
+
 @pytest.mark.parametrize("M", [24, 64, 100, 700])
 def test_lora_linear_a_request_per_row(M):
     x, w, a, b, s, bias = _lora_case(M, 264, 136, 16, 11, BF16)
