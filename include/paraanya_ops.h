@@ -97,9 +97,10 @@ typedef struct {
     int64_t mask_stride;         /* elements from a sample's mask row to the next (0 = shared) */
 } pa_cross_t;
 
-/* stats (fp32, [batch][q_heads][q_len][2]; may be NULL) receives for each row the largest score
- * m and log(sum of exp(score - m)) (-inf, -inf for a row that sees no key): the log-sum-exp in
- * two parts, so that scores at the type's lowest value keep their weights in the backward pass. */
+/* stats (fp32, [batch][q_heads][q_len][2]; may be NULL) receives for each row a score m near its
+ * largest (at most log(256) below it) and log(sum of exp(score - m)), for a row that sees no key
+ * (-inf, -inf): the log-sum-exp in two parts, so that scores at the type's lowest value keep their
+ * weights in the backward pass. */
 PA_API int paraanya_cross_attention(const pa_cross_t* p, const void* q, const void* k, const void* v, void* o,
                                     float* stats, void* workspace, size_t workspace_bytes, void* stream);
 PA_API int paraanya_cross_attention_workspace(const pa_cross_t* p, size_t* bytes);

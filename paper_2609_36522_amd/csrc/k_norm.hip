@@ -385,6 +385,8 @@ hipError_t bwd(const NormDev& d, hipStream_t st) {
         else if (N >= 8 && N <= 4096) k_norm_bwd<T, W, 4, 2><<<nb, kThreads, 0, st>>>(d);
         else if (N >= 8 && N <= 8192) k_norm_bwd<T, W, 4, 4><<<nb, kThreads, 0, st>>>(d);
         else {
+            // dx may overwrite dy: the sums over dy come first.
+            if (d.part) k_norm_bwd_long_dw<T, W><<<dim3(nb, (unsigned)((N + 2047) / 2048)), kThreads, 0, st>>>(d);
             for (int64_t r0 = 0; d.dx && r0 < d.rows; r0 += kLaunchRows) {
                 NormDev c = d;
                 c.rows = d.rows - r0 < kLaunchRows ? d.rows - r0 : kLaunchRows;
@@ -395,7 +397,6 @@ hipError_t bwd(const NormDev& d, hipStream_t st) {
                 c.rstd += r0;
                 k_norm_bwd_long_dx<T, W><<<(unsigned)c.rows, kThreads, 0, st>>>(c);
             }
-            if (d.part) k_norm_bwd_long_dw<T, W><<<dim3(nb, (unsigned)((N + 2047) / 2048)), kThreads, 0, st>>>(d);
         }
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;

@@ -263,8 +263,8 @@ def cross_attention_forward(q, k, v, *, kv_lens=None, mask=None, scale=None):
     any strides with consecutive head elements (a stride of 0 repeats); q_heads a multiple of kv_heads.
     ``kv_lens`` (int32, [batch]) is each sample's number of states; ``mask`` [batch, kv_len] admits keys
     (bool or uint8) or is added to their scores (float32, -inf hides a key). ``scale`` defaults to
-    1 / sqrt(head_dim). stats [batch, q_heads, q_len, 2] is what the backward pass needs (the largest
-    score and the logarithm of the sum of exponentials past it; their sum is the log-sum-exp)."""
+    1 / sqrt(head_dim). stats [batch, q_heads, q_len, 2] is what the backward pass needs (a score near
+    the row's largest and the logarithm of the sum of exponentials past it; their sum is the log-sum-exp)."""
     q, k, v = _heads(q, "q"), _heads(k, "k"), _heads(v, "v")
     o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     st = _on_device(q, k, v, kv_lens, mask)

@@ -87,6 +87,32 @@ def test_layer_norm_constant_rows_and_no_rows():
     assert dx.shape == (0, 100) and not dw.any() and not db.any()
 
 
+@pytest.mark.parametrize("N", [96, 1000, 1333, 3000, 9001])
+def test_layer_norm_in_place(N):
+    """y may be x and dx may be dy (C ABI)."""
+    import ctypes as C
+    x, w, b, dy = _norm_case(37, N, BF16)
+    y, mean, rstd = ops.layer_norm_forward(x, w, b)
+    want = ops.layer_norm_backward(dy, x, mean, rstd, w)
+    lib, st = ops._library(), torch.cuda.current_stream().cuda_stream
+    p = ops.Norm(37, N, ops.PA_BF16, ops.PA_BF16, 1e-5, N, N, N)
+    x2, d2 = x.clone(), dy.clone()
+    B._check(lib.paraanya_layer_norm(C.byref(p), x2.data_ptr(), w.data_ptr(), b.data_ptr(), x2.data_ptr(), None, None, st))
+    assert torch.equal(x2, y)
+    n = C.c_size_t(0)
+    B._check(lib.paraanya_layer_norm_backward_workspace(C.byref(p), C.byref(n)))
+    ws = torch.empty(n.value, dtype=torch.uint8, device="cuda")
+    dw, db = torch.empty_like(w), torch.empty_like(b)
+    B._check(lib.paraanya_layer_norm_backward(C.byref(p), d2.data_ptr(), x.data_ptr(), mean.data_ptr(), rstd.data_ptr(), w.data_ptr(),
+                                              d2.data_ptr(), dw.data_ptr(), db.data_ptr(), ws.data_ptr(), n.value, st))
+    assert all(torch.equal(g, t) for g, t in zip((d2, dw, db), want))
+    # Gradients one at a time give the same.
+    only = torch.empty_like(db)
+    B._check(lib.paraanya_layer_norm_backward(C.byref(p), dy.data_ptr(), x.data_ptr(), mean.data_ptr(), rstd.data_ptr(), w.data_ptr(),
+                                              None, None, only.data_ptr(), ws.data_ptr(), n.value, st))
+    assert torch.equal(only, want[2])
+
+
 def test_layer_norm_not_a_number_stays_in_its_row():
     x, w, b, dy = _norm_case(9, 700, BF16)
     x[4, 13] = math.nan
@@ -310,6 +336,27 @@ def test_cross_attention_gradient_against_differences():
         assert abs(got - want) <= 6 * noise + 0.1 * scale * 4, (which, got, want, noise, scale)
 
 
+@pytest.mark.parametrize("Lk", [77, 200, 700])
+def test_cross_attention_gradients_one_at_a_time(Lk):
+    """Through the C ABI dq may be left out (the rows' statistics then come from a kernel of their own), or dk
+    and dv; kept results are the same up to the rounding of o in delta."""
+    import ctypes as C
+    q, k, v, do = _cross_case(2, 70, 4, 2, Lk, 64, BF16)
+    o, stats = ops.cross_attention_forward(q, k, v)
+    dq, dk, dv = ops.cross_attention_backward(do, q, k, v, o, stats)
+    p, _, n = ops._cross_args(q, k, v, None, None, None, o)
+    g = ops.CrossGrad(do.stride()[:3], dq.stride()[:3], dk.stride()[:3], dv.stride()[:3])
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    lib, st = ops._library(), torch.cuda.current_stream().cuda_stream
+    fixed = [t.data_ptr() for t in (do, q, k, v, o, stats)]
+    a, b, c = (torch.full_like(t, math.nan) for t in (dq, dk, dv))
+    B._check(lib.paraanya_cross_attention_backward(C.byref(p), C.byref(g), *fixed, None, b.data_ptr(), c.data_ptr(), ws.data_ptr(), n, st))
+    B._check(lib.paraanya_cross_attention_backward(C.byref(p), C.byref(g), *fixed, a.data_ptr(), None, None, ws.data_ptr(), n, st))
+    ref = R.cross_attention(q, k, v, do)
+    assert torch.equal(a, dq) and torch.equal(c, dv)
+    R.check(b, *ref["dk"], "dk alone")
+
+
 def test_cross_attention_in_autograd():
     q, k, v, do = _cross_case(2, 33, 4, 2, 77, 64, F16)
     lens = torch.tensor([77, 30], dtype=torch.int32, device="cuda")
@@ -326,6 +373,18 @@ def test_cross_attention_offsets_past_32_bits():
     big = torch.empty((1 << 32) + (1 << 20), dtype=BF16, device="cuda")
     k = big.as_strided((2, Lk, 1, D), ((1 << 31), (1 << 31) // 69, D, 1))
     q, kk, v, do = _cross_case(2, 5, 1, 1, Lk, D, BF16)
+    k.copy_(kk)
+    _check_cross(q, k, v, do)
+
+
+@pytest.mark.parametrize("stride", [(1 << 22) + 64, (1 << 23) - 8])
+@pytest.mark.parametrize("Lq", [3, 150])
+def test_cross_attention_tokens_far_apart(Lq, stride):
+    """Token strides of megabytes, below and near the bound up to which offsets in a tile take 32 bits."""
+    Lk, D = 130, 64
+    big = torch.empty((Lk - 1) * stride + D, dtype=F16, device="cuda")
+    q, kk, v, do = _cross_case(1, Lq, 1, 1, Lk, D, F16)
+    k = big.as_strided((1, Lk, 1, D), (0, stride, D, 1))
     k.copy_(kk)
     _check_cross(q, k, v, do)
 
@@ -400,6 +459,18 @@ def test_lora_linear_not_a_number_stays_in_its_row(M):
     y = ops.lora_linear(x, w, a, b, off, torch.tensor([0, 1], dtype=torch.int32, device="cuda"), scales=s, bias=bias)
     bad = torch.isnan(y).any(1)
     assert not bool(bad[:M // 2].any()) and bool(bad[M // 2:].all())
+
+
+def test_lora_linear_rows_far_apart():
+    """Row strides of megabytes: offsets within a tile near 2^31 bytes."""
+    M, K, N = 300, 72, 136
+    x, w, a, b, s, bias = _lora_case(M, K, N, 8, 2, BF16)
+    for stride in ((1 << 22) - 8, (1 << 22) + 8):
+        big = torch.empty((M - 1) * stride + K, dtype=BF16, device="cuda")
+        far = big.as_strided((M, K), (stride, 1))
+        far.copy_(x)
+        _check_lora(far, w, a, b, [0, 100, M], [1, 0], s, bias)
+        del big, far
 
 
 # ------------------------------------------------------------------ all
