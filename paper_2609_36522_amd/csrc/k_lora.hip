@@ -74,12 +74,12 @@ __device__ __forceinline__ typename Vec<T>::v8 fixed(typename Vec<T>::v8 r, int 
 template <class T, int ROWS, int THREADS, int WIDTH>
 struct Stage {
     static constexpr int kPieces = ROWS * 8 / THREADS, kStep = THREADS / 8;
-    uint4 r[direct(WIDTH) ? 1 : kPieces];
+    uint4 r[2][direct(WIDTH) ? 1 : kPieces];         // two sets of registers: parts of two loads in flight
     uint32_t off[direct(WIDTH) ? kPieces : 1];
-    int piece, row, rows, at, len;
+    int piece, row, rows, at[2], len;
 
     // The matrix's row 0 of this tile exists, and rows - 1 more; rows are n long.
-    __device__ __forceinline__ Stage(int64_t stride, int rows_, int n) : rows(rows_), at(0), len(n) {
+    __device__ __forceinline__ Stage(int64_t stride, int rows_, int n) : rows(rows_), at{0, 0}, len(n) {
         row = (int)threadIdx.x >> 3;
         piece = (int)threadIdx.x & 7;
         if constexpr (direct(WIDTH)) {
@@ -90,13 +90,14 @@ struct Stage {
         }
     }
     // Columns k0 .. of the rows at `base`.
+    template <int SET = 0>
     __device__ __forceinline__ void load(const T* base, int64_t stride, int k0, T* tile) {
         if constexpr (direct(WIDTH)) {
             const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
             const bool in = k0 + piece * 8 < len;
             if (WIDTH == kEven && k0 + 64 > len) {                  // the rows' last columns
-                at = k0 + piece * 8;
-                const uint32_t col = (at + 8 <= len ? k0 : len - 8 - piece * 8) * 2;
+                at[0] = k0 + piece * 8;
+                const uint32_t col = (at[0] + 8 <= len ? k0 : len - 8 - piece * 8) * 2;
                 const __amdgpu_buffer_rsrc_t from = buffer_at(base);
 #pragma unroll
                 for (int i = 0; i < kPieces; ++i)
@@ -107,33 +108,35 @@ struct Stage {
                 for (int i = 0; i < kPieces; ++i) load_lds(from, tile + (w * 64 + i * THREADS) * 8, in ? off[i] : kNowhere, 0);
             }
         } else {
-            at = k0 + piece * 8;
+            at[SET] = k0 + piece * 8;
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {
                 const bool valid = row + i * kStep < rows;
                 const T* p = base + (valid ? row + i * kStep : 0) * stride;
-                r[i] = WIDTH == kRagged ? __builtin_bit_cast(uint4, load8_raw(p, at, len)) : __builtin_bit_cast(uint4, load8(p, at, len, valid));
+                r[SET][i] = WIDTH == kRagged ? __builtin_bit_cast(uint4, load8_raw(p, at[SET], len))
+                                             : __builtin_bit_cast(uint4, load8(p, at[SET], len, valid));
             }
         }
     }
     // Registers into LDS; direct loads (which the caller has waited for) are in place but for the rows' last
     // columns, which the last part's threads move.
+    template <int SET = 0>
     __device__ __forceinline__ void arrive(T* tile, bool last) {
         if constexpr (WIDTH == kEven) {
-            if (last && at < len && at + 8 > len) {
+            if (last && at[0] < len && at[0] + 8 > len) {
 #pragma unroll
                 for (int i = 0; i < kPieces; ++i) {
                     uint4* slot = reinterpret_cast<uint4*>(tile + (threadIdx.x + i * THREADS) * 8);
-                    *slot = __builtin_bit_cast(uint4, shift8(__builtin_bit_cast(Pack8<T>, *slot), at + 8 - len));
+                    *slot = __builtin_bit_cast(uint4, shift8(__builtin_bit_cast(Pack8<T>, *slot), at[0] + 8 - len));
                 }
             }
         } else if constexpr (WIDTH != kWhole) {
-            const bool whole = at - piece * 8 + 64 <= len && rows >= ROWS;      // nothing to fix (the same in all lanes)
+            const bool whole = at[SET] - piece * 8 + 64 <= len && rows >= ROWS; // nothing to fix (the same in all lanes)
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {
                 if (WIDTH == kRagged && !whole)
-                    r[i] = __builtin_bit_cast(uint4, fix8(__builtin_bit_cast(Pack8<T>, r[i]), at, len, row + i * kStep < rows));
-                *reinterpret_cast<uint4*>(tile + piece_at<64>(row + i * kStep, piece)) = r[i];
+                    r[SET][i] = __builtin_bit_cast(uint4, fix8(__builtin_bit_cast(Pack8<T>, r[SET][i]), at[SET], len, row + i * kStep < rows));
+                *reinterpret_cast<uint4*>(tile + piece_at<64>(row + i * kStep, piece)) = r[SET][i];
             }
         }
     }
@@ -374,20 +377,7 @@ __global__ __launch_bounds__(64 * WF * WR, NM * NX == 16 ? 1 : 2) void k_lora_ti
     };
     f32x16 acc[NM][NX];
     const int fw = (w % WF) * NM * 32, rw = (w / WF) * NX * 32;
-#pragma unroll
-    for (int i = 0; i < STAGES - 1; ++i)
-        if (i < parts) load(i, i);
-    start<T, NM, NX>(d, f0 + fw, lane, acc);
-    const int first = d.adapters > 0 ? request_from(d, r0 + rw) : 0;
-    if (parts >= STAGES - 1) wait_loads<(STAGES - 2) * LOADS>();
-    else wait_loads();
-    arrive(0, 0);
-    lds_barrier();
-    int p = 0;
-    for (int i = 0; i < parts; ++i) {
-        int q = p + STAGES - 1;
-        if (q >= STAGES) q -= STAGES;
-        if (i + STAGES - 1 < parts) load(i + STAGES - 1, q);
+    auto multiply = [&](int p) {
         const T* wt = tiles[p];
         const T* xt = tiles[p] + TF * 64;
         // The operands of the next 16 columns are read while those of the current ones are multiplied.
@@ -414,13 +404,62 @@ __global__ __launch_bounds__(64 * WF * WR, NM * NX == 16 ? 1 : 2) void k_lora_ti
                 }
             }
         }
-        if (i + 1 < parts) {
-            if (i + STAGES - 1 < parts) wait_loads<(STAGES - 2) * LOADS>();      // the next part is there
-            else wait_loads();
-            arrive(i + 1, p + 1 == STAGES ? 0 : p + 1);
-        }
+    };
+    int first = 0;
+    if constexpr (direct(WIDTH)) {
+#pragma unroll
+        for (int i = 0; i < STAGES - 1; ++i)
+            if (i < parts) load(i, i);
+        start<T, NM, NX>(d, f0 + fw, lane, acc);
+        if (d.adapters > 0) first = request_from(d, r0 + rw);
+        if (parts >= STAGES - 1) wait_loads<(STAGES - 2) * LOADS>();
+        else wait_loads();
+        arrive(0, 0);
         lds_barrier();
-        if (++p == STAGES) p = 0;
+        int p = 0;
+        for (int i = 0; i < parts; ++i) {
+            int q = p + STAGES - 1;
+            if (q >= STAGES) q -= STAGES;
+            if (i + STAGES - 1 < parts) load(i + STAGES - 1, q);
+            multiply(p);
+            if (i + 1 < parts) {
+                if (i + STAGES - 1 < parts) wait_loads<(STAGES - 2) * LOADS>();      // the next part is there
+                else wait_loads();
+                arrive(i + 1, p + 1 == STAGES ? 0 : p + 1);
+            }
+            lds_barrier();
+            if (++p == STAGES) p = 0;
+        }
+    } else {
+        // Registers: part i + 2 is on its way in one set while part i + 1 waits in the other.
+        sw.template load<0>(wp, d.w_stride, 0, nullptr);
+        sx.template load<0>(xp, d.x_stride, 0, nullptr);
+        if (parts > 1) {
+            sw.template load<1>(wp, d.w_stride, 64, nullptr);
+            sx.template load<1>(xp, d.x_stride, 64, nullptr);
+        }
+        start<T, NM, NX>(d, f0 + fw, lane, acc);
+        if (d.adapters > 0) first = request_from(d, r0 + rw);
+        sw.template arrive<0>(tiles[0], parts == 1);
+        sx.template arrive<0>(tiles[0] + TF * 64, parts == 1);
+        __syncthreads();
+        auto step = [&](int i, auto set) {
+            constexpr int A = decltype(set)::value, B = 1 - A;
+            if (i + 2 < parts) {
+                sw.template load<A>(wp, d.w_stride, (i + 2) * 64, nullptr);
+                sx.template load<A>(xp, d.x_stride, (i + 2) * 64, nullptr);
+            }
+            multiply(A);
+            if (i + 1 < parts) {
+                sw.template arrive<B>(tiles[B], i + 1 == parts - 1);
+                sx.template arrive<B>(tiles[B] + TF * 64, i + 1 == parts - 1);
+            }
+            lds_barrier();
+        };
+        for (int i = 0; i < parts; i += 2) {
+            step(i, std::integral_constant<int, 0>{});
+            if (i + 1 < parts) step(i + 1, std::integral_constant<int, 1>{});
+        }
     }
     if (d.adapters > 0) add_adapters<T, NM, NX, WIDTH>(d, f0 + fw, r0 + rw, lane, acc, first);
     finish<T, NM, NX>(d, f0 + fw, r0 + rw, lane, acc);
