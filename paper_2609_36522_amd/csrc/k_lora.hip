@@ -145,6 +145,7 @@ struct Stage {
 // t of 64 rows of one request: block (c, i) takes rows 64 c .. of request i, all of them if the grid is
 // smaller. Of the four waves two take 32 rows each, over half of the reduction; NR 32-row tiles of A. Bound by
 // the reading of x: three parts of 64 columns are on their way during the products of the current one.
+// 32768x2048, rank 64: 32 to 52 us (134 MB, 2.6 to 4.2 TB/s, by what the last-level cache holds of x).
 template <class T, int NR, int WIDTH>
 __global__ __launch_bounds__(256) void k_lora_down(LoraDev d) {
     constexpr int ROWS = 64, STAGES = direct(WIDTH) ? 4 : 2, PART = (ROWS + NR * 32) * 64, LOADS = (ROWS + NR * 32) * 8 / 256;
@@ -226,7 +227,8 @@ __global__ __launch_bounds__(256) void k_lora_down(LoraDev d) {
 }
 
 // The same for requests of few rows: 32 rows a block, 16 / NR waves that take parts of 64 columns in
-// turn, every operand straight from memory, so that one token's reduction is in flight all at once.
+// turn, every operand straight from memory, so that one token's reduction is in flight all at once: 5 us for
+// eight rows of 1024, of which a launch and a chain of two loads are most.
 template <class T, int NR, int WIDTH>
 __global__ __launch_bounds__(1024 / NR) void k_lora_down_few(LoraDev d) {
     constexpr int WAVES = 16 / NR;
@@ -350,7 +352,9 @@ __device__ __forceinline__ void finish(const LoraDev& d, int f0, int r0, int lan
 }
 
 // WF x WR waves of NM x NX tiles of 32 x 32 (features x rows) per block. The reduction goes through LDS in
-// parts of 64 columns, of which STAGES - 1 are on their way during the products of the current one.
+// parts of 64 columns, of which STAGES - 1 are on their way during the products of the current one. Bound by the
+// matrix units and the LDS reads that feed them: 32768x2048x2048, rank 64, 280 to 300 us (980 to 920 TFLOP/s,
+// 1415 for a large library product).
 template <class T, int WF, int WR, int NM, int NX, int STAGES, int WIDTH>
 __global__ __launch_bounds__(64 * WF * WR, NM * NX == 16 ? 1 : 2) void k_lora_tile(LoraDev d) {
     typedef typename Vec<T>::v8 v8;
@@ -466,7 +470,8 @@ __global__ __launch_bounds__(64 * WF * WR, NM * NX == 16 ? 1 : 2) void k_lora_ti
 }
 
 // Few rows: 32 features x 32 rows per block. W is read once, straight into operand registers; 16 waves
-// take parts of 64 columns in turn, and the requests' adapters in turn, and are joined through LDS.
+// take parts of 64 columns in turn, and the requests' adapters in turn, and are joined through LDS. Bound by
+// latency: eight rows of 1024x1024 7 us (2.1 MB).
 template <class T, int WIDTH>
 __global__ __launch_bounds__(1024) void k_lora_rows(LoraDev d) {
     typedef typename Vec<T>::v8 v8;
@@ -527,7 +532,16 @@ void down(const LoraDev& d, hipStream_t st) {
 
 int64_t tiles_of(const LoraDev& d, int f, int r) { return (int64_t)((d.out + f - 1) / f) * ((d.rows + r - 1) / r); }
 
-// The largest tile (features x rows) that still gives every CU a block; few rows read W straight from memory.
+// 256 x 256 tiles (features x rows) where they give every CU a block; 64 x 64 ones where they are few enough
+// for one round of two blocks a CU, or, loaded through registers (where 128 x 128 ones keep too few loads
+// in flight), as long as 128 x 128 ones would not give every CU a block; 128 x 128 ones otherwise. Up to
+// 64 rows W is read straight from memory. Both sides of each rule, with the adapters' first product, in us:
+//   32768x2048x2048, rank 64: 256 x 256 tiles 320, 128 x 128 ones 362
+//   8192x1024x1024, rank 16:  128 x 128 tiles 33.3, 256 x 128 ones of eight waves (not built) 34.4
+//   2048x1024x1024, rank 16:  64 x 64 tiles (512) 17.4, 128 x 128 ones 21.5
+//   1999x1024x1347, rank 24:  128 x 128 tiles 25.4, 64 x 64 ones (704) 30.1
+//   1999x1101x1347, rank 24:  64 x 64 tiles 44, 128 x 128 ones (176) 54; 8192x1101x1024: 75 and 56
+//   8x1024x1024, rank 16, in a graph:  straight from memory 9.5, 64 x 64 tiles 15.2; 64 rows: 10.6 and 14.4
 template <class T, int WIDTH>
 hipError_t run(const LoraDev& d, hipStream_t st) {
     if (d.adapters > 0) {
@@ -546,12 +560,8 @@ hipError_t run(const LoraDev& d, hipStream_t st) {
             k_lora_tile<T, 2, 4, 4, 2, 2, WIDTH><<<(unsigned)tiles_of(d, 256, 256), 512, 0, st>>>(d);
             return hipGetLastError();
         }
-        if (tiles_of(d, 256, 128) >= kCUs) {
-            k_lora_tile<T, 4, 2, 2, 2, 3, WIDTH><<<(unsigned)tiles_of(d, 256, 128), 512, 0, st>>>(d);
-            return hipGetLastError();
-        }
     }
-    if (tiles_of(d, 128, 128) >= kCUs)
+    if (direct(WIDTH) ? tiles_of(d, 64, 64) > 2 * kCUs : tiles_of(d, 128, 128) >= kCUs)
         k_lora_tile<T, 2, 2, 2, 2, 2, WIDTH><<<(unsigned)tiles_of(d, 128, 128), 256, 0, st>>>(d);
     else
         k_lora_tile<T, 2, 2, 1, 1, direct(WIDTH) ? 4 : 2, WIDTH><<<(unsigned)tiles_of(d, 64, 64), 256, 0, st>>>(d);

@@ -1,14 +1,17 @@
 // Layer norm, forward and backward, for gfx950.
 //
-// Forward: a row lives in the registers of one wave (up to 2048 columns) or of one block of four
-// waves, so x is read once and the mean and the sum of squared differences from it are two passes
-// over registers (no cancellation between a sum of squares and a squared sum). Rows too long for
-// that are read three times by one block, from L2 after the first.
+// Forward, y = (x - mean) rstd w + b: a row lives in the registers of one wave or, from 8 columns to
+// 8192, of one block of four waves, so x is read once and the mean and the sum of squared differences
+// from it are two passes over registers (no cancellation between a sum of squares and a squared sum).
+// Rows too long for that are read three times by one block, from L2 after the first.
 //
 // Backward: dx needs two sums over the row (g = dy w; g and g xh), dweight and dbias one sum over
 // all rows for each column. A block walks over rows and keeps its columns' two running sums in
 // registers, so dy and x are read once; the blocks' sums go to `part` and a second kernel adds
-// them in a fixed order. Both passes are bound by memory traffic.
+// them in a fixed order. Both passes are bound by memory traffic: at 32768x1024 in 16 bits 28 to 33 us
+// forward (4.1 to 4.8 TB/s), 39 us backward (5.2 TB/s, part of x and dy still in the last-level
+// cache) and 4 us for the sums' join. Rows at odd addresses take 4-byte or 2-byte pieces of the same
+// lines: 5003x1333 in 32 bits 15 us forward, 20.7 backward.
 #include "pa_ops_device.h"
 
 namespace pa {
@@ -158,7 +161,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_fwd_long(NormDev d) {
     }
 }
 
-// Backward for rows that fit the registers of WPR waves: dx of the block's rows (every
+// Backward, dx = rstd (g - mean(g) - xh mean(g xh)), for rows that fit the registers of WPR waves: dx of the block's rows (every
 // gridDim.x-th group), and the block's sums of dy xh and dy into part[blockIdx.x].
 template <class T, class W, int WPR, int CH>
 __global__ __launch_bounds__(kThreads) void k_norm_bwd(NormDev d) {
@@ -359,6 +362,8 @@ __global__ __launch_bounds__(kThreads) void k_norm_fold(NormDev d) {
     }
 }
 
+// A wave per row while its registers hold it (no barrier, four rows a block in flight), a block per row
+// beyond. 16384x2048: fp32 52 us a wave, 41 a block; bf16 30 a wave, 34 a block.
 template <class T, class W>
 hipError_t fwd(const NormDev& d, hipStream_t st) {
     const int64_t N = d.cols;
@@ -374,6 +379,8 @@ hipError_t fwd(const NormDev& d, hipStream_t st) {
     return hipGetLastError();
 }
 
+// The backward pass holds two rows, the next two and two sums per column, so a row takes a block from
+// 1025 columns on: bf16 16384x2048 55 us a wave, 50 a block; fp32 5003x1333 32 and 26.
 template <class T, class W>
 hipError_t bwd(const NormDev& d, hipStream_t st) {
     const int64_t N = d.cols;
@@ -432,8 +439,8 @@ hipError_t norm_forward(const NormDev& d, int dtype, int param_dtype, hipStream_
     });
 }
 
-// Blocks of the backward pass: enough to fill the 256 CUs a few times over, no more than there are
-// groups of rows, and fewer partial sums than a quarter of the rows.
+// Blocks of the backward pass: two for each of the 256 CUs, as the registers allow, and no more than
+// there are groups of rows. More blocks cost more partial sums to write and join.
 int norm_backward_blocks(int64_t rows, int64_t cols) {
     const int64_t groups = cols <= 1024 ? (rows + 3) / 4 : rows;
     const int64_t most = 512;
