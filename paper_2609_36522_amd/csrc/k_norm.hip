@@ -161,8 +161,8 @@ __global__ __launch_bounds__(kThreads) void k_norm_fwd_long(NormDev d) {
     }
 }
 
-// Backward, dx = rstd (g - mean(g) - xh mean(g xh)), for rows that fit the registers of WPR waves: dx of the block's rows (every
-// gridDim.x-th group), and the block's sums of dy xh and dy into part[blockIdx.x].
+// Backward, dx = rstd (g - mean(g) - xh mean(g xh)), for rows that fit the registers of
+// WPR waves: dx of the block's rows (every gridDim.x-th group), and the block's sums of dy xh and dy into part[blockIdx.x].
 template <class T, class W, int WPR, int CH>
 __global__ __launch_bounds__(kThreads) void k_norm_bwd(NormDev d) {
     constexpr int TPR = 64 * WPR, RPB = 4 / WPR;

@@ -4,8 +4,9 @@
 // head in the group, so a shared head's keys and values are read once for all of them, and a
 // single token of a model with shared heads already fills several rows.
 //
-// Products. All use v_mfma_f32_32x32x16 (layouts: pa_mma.h). Scores are computed transposed (S^T = K Q^T: a lane owns a query row, its registers hold
-// keys), so the softmax's maximum and sum are a lane's own plus one exchange with lane l xor 32, and
+// Products. All use v_mfma_f32_32x32x16 (layouts: pa_mma.h). Scores are computed transposed
+// (S^T = K Q^T: a lane owns a query row, its registers hold keys), so the softmax's maximum and
+// sum are a lane's own plus one exchange with lane l xor 32, and
 // the accumulator, rounded to 16 bits, is already the B operand of the next product over keys
 // (O^T = V^T P^T): its slots 8t .. 8t + 7 are keys 16t + 4 (l/32) + {0..3, 8..11}, an order that the
 // A operand (V^T) follows, read from the row-major tile with transposing LDS loads
