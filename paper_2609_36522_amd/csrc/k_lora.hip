@@ -284,7 +284,10 @@ __global__ __launch_bounds__(1024 / NR) void k_lora_down_few(LoraDev d) {
 }
 
 // The adapters' part of NM x NX 32 x 32 tiles: features f0 + 32 i + .., rows r0 + 32 j + ..; every
-// `step`-th request from `first`, the first that has rows at r0 or after.
+// `step`-th request from `first`, the first that has rows at r0 or after. Where a request has all of the
+// tiles' rows its product goes on in their accumulators. Otherwise 32 rows that it has a part of are carried on
+// in a copy, of which the lanes of its rows (a lane owns a row) are taken: zeros in t for the others would not
+// do, as 0 times an infinity or a NaN in B is a NaN.
 template <class T, int NM, int NX, int WIDTH>
 __device__ __forceinline__ void add_adapters(const LoraDev& d, int f0, int r0, int lane, f32x16 (&acc)[NM][NX], int first, int step = 1) {
     typedef typename Vec<T>::v8 v8;
@@ -295,23 +298,50 @@ __device__ __forceinline__ void add_adapters(const LoraDev& d, int f0, int r0, i
         const int ad = adapter_of(d, i);
         if (ad < 0 || beg >= end) continue;
         const T* b = static_cast<const T*>(d.b) + (int64_t)ad * d.out * d.rank;
-        for (int k0 = 0; k0 < d.rank; k0 += 16) {
-            const int k = k0 + half * 8;
-            v8 tv[NX], bv[NM];
+        auto t_at = [&](int j, int k) {
+            const int row = r0 + j * 32 + (lane & 31);
+            return operand<T, kWhole>(static_cast<const T*>(d.t) + (int64_t)row * d.rank_pad, k, d.rank_pad, row >= beg && row < end);
+        };
+        auto b_at = [&](int m, int k) {
+            const int f = f0 + m * 32 + (lane & 31);
+            return operand<T, direct(WIDTH) ? kWhole : kTiny>(b + (int64_t)f * d.rank, k, d.rank, f < d.out);
+        };
+        if (beg <= r0 && end >= r1) {
+            for (int k0 = 0; k0 < d.rank; k0 += 16) {
+                const int k = k0 + half * 8;
+                v8 tv[NX], bv[NM];
 #pragma unroll
-            for (int j = 0; j < NX; ++j) {
-                const int row = r0 + j * 32 + (lane & 31);
-                tv[j] = operand<T, kWhole>(static_cast<const T*>(d.t) + (int64_t)row * d.rank_pad, k, d.rank_pad, row >= beg && row < end);
-            }
+                for (int j = 0; j < NX; ++j) tv[j] = t_at(j, k);
 #pragma unroll
-            for (int m = 0; m < NM; ++m) {
-                const int f = f0 + m * 32 + (lane & 31);
-                bv[m] = operand<T, direct(WIDTH) ? kWhole : kTiny>(b + (int64_t)f * d.rank, k, d.rank, f < d.out);
+                for (int m = 0; m < NM; ++m) bv[m] = b_at(m, k);
+#pragma unroll
+                for (int m = 0; m < NM; ++m)
+#pragma unroll
+                    for (int j = 0; j < NX; ++j) acc[m][j] = mma(bv[m], tv[j], acc[m][j]);
             }
+            continue;
+        }
+#pragma unroll
+        for (int j = 0; j < NX; ++j) {
+            const int row = r0 + j * 32 + (lane & 31);
+            if (beg >= r0 + j * 32 + 32 || end <= r0 + j * 32) continue;     // the same in all lanes
+            f32x16 sum[NM];
+#pragma unroll
+            for (int m = 0; m < NM; ++m) sum[m] = acc[m][j];
+            for (int k0 = 0; k0 < d.rank; k0 += 16) {
+                const int k = k0 + half * 8;
+                const v8 tv = t_at(j, k);
+                v8 bv[NM];
+#pragma unroll
+                for (int m = 0; m < NM; ++m) bv[m] = b_at(m, k);
+#pragma unroll
+                for (int m = 0; m < NM; ++m) sum[m] = mma(bv[m], tv, sum[m]);
+            }
+            const bool own = row >= beg && row < end;
 #pragma unroll
             for (int m = 0; m < NM; ++m)
 #pragma unroll
-                for (int j = 0; j < NX; ++j) acc[m][j] = mma(bv[m], tv[j], acc[m][j]);
+                for (int r = 0; r < 16; ++r) acc[m][j][r] = own ? sum[m][r] : acc[m][j][r];
         }
     }
 }
