@@ -7,7 +7,9 @@
 // request that has rows in it, with the other requests' rows of t taken as zero. So the adapters cost
 // their own products and no pass over y.
 //
-// t is rounded to the element type for the second product, as its operand has to be.
+// t is rounded to the element type for the second product, as its operand has to be. Its columns past the
+// rank (up to a multiple of 16) are stored as zeros: an infinity in x times the zeros in the place of A's
+// missing rows is a NaN.
 //
 // The products are transposed (a lane owns a row of x, its registers hold output features), so that
 // a lane stores consecutive features.
@@ -216,8 +218,11 @@ __global__ __launch_bounds__(256) void k_lora_down(LoraDev d) {
                 for (int r = 0; r < 16; ++r) acc[n][r] += join[n * 32 + 8 * (r >> 2) + 4 * half + (r & 3)][rw * 32 + (lane & 31)];
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
-                    const Pack8<T> o = gather8<T>(acc[n], q, s);
+                    Pack8<T> o = gather8<T>(acc[n], q, s);
                     const int r = n * 32 + q * 16 + half * 8;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (r + e >= d.rank) o.v[e] = (T)0.0f;
                     if (row < end && r < d.rank_pad) *reinterpret_cast<Pack8<T>*>(t + r) = o;
                 }
             }
@@ -278,7 +283,7 @@ __global__ __launch_bounds__(1024 / NR) void k_lora_down_few(LoraDev d) {
             float v = 0.0f;
 #pragma unroll
             for (int j = 0; j < WAVES; ++j) v += part[j][r][tr];
-            static_cast<T*>(d.t)[(int64_t)(r0 + tr) * d.rank_pad + r] = (T)(v * s);
+            static_cast<T*>(d.t)[(int64_t)(r0 + tr) * d.rank_pad + r] = (T)(r < d.rank ? v * s : 0.0f);
         }
     }
 }

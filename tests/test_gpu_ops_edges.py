@@ -32,3 +32,14 @@ def test_lora_linear_weights_that_are_not_finite_stay_with_their_request(M, K, N
     a[3, Rk - 1, K // 3] = math.inf
     cuts = [0, 1, 3, 7, M // 3, M // 3 + 2, M // 2, M // 2, M - 7, M - 6, M - 2]
     _check_lora(x, w, a, b, cuts, [0, 1, -1, 2, 0, 1, 2, 0, 3, 0], s, bias)
+
+
+@pytest.mark.parametrize("Rk", [1, 5, 8, 20, 24, 100])
+@pytest.mark.parametrize("M,K,N", [(24, 64, 96), (300, 71, 96), (1300, 136, 1400), (17000, 70, 70)])
+def test_lora_linear_a_row_that_is_not_finite(M, K, N, Rk):
+    """An infinity in x, with weights above 0, makes its row infinite (not NaN) and no other."""
+    x, w, a, b, s, bias = _lora_case(M, K, N, Rk, 3, BF16)
+    x[5, K // 2] = math.inf
+    x[M - 3, 0] = -math.inf
+    x[M // 2, 1] = math.nan
+    _check_lora(x, w.abs(), a.abs(), b.abs(), [0, 2, 11, M // 2, M], [0, 1, -1, 2], s, bias)
