@@ -5,7 +5,8 @@ requests.
 Argument marshalling only, as in :mod:`binding`: every product and sum runs in the library's HIP
 kernels. Tensors lie on the current device; kernels run on torch's current stream, outputs and
 workspaces come from torch's allocator on that stream. :func:`layer_norm` and
-:func:`cross_attention` take part in autograd; the ``*_forward`` and ``*_backward`` functions do not.
+:func:`cross_attention` take part in autograd, for first derivatives (a gradient's gradient is refused); the
+``*_forward`` and ``*_backward`` functions do not.
 """
 from __future__ import annotations
 
@@ -14,6 +15,7 @@ import functools
 import math
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as B
 
@@ -193,6 +195,7 @@ class _LayerNorm(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, weight, mean, rstd = ctx.saved_tensors
         dx, dw, db = layer_norm_backward(dy, x, mean, rstd, weight, param_dtype=ctx.param_dtype)
@@ -201,7 +204,7 @@ class _LayerNorm(torch.autograd.Function):
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5):
-    """The norm over x's last dimension, differentiable in x, weight and bias."""
+    """The norm over x's last dimension, differentiable (once) in x, weight and bias."""
     return _LayerNorm.apply(x, weight, bias, eps)
 
 
@@ -306,6 +309,7 @@ class _CrossAttention(torch.autograd.Function):
         return o
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, do):
         q, k, v, o, stats, kv_lens, mask = ctx.saved_tensors
         dq, dk, dv = cross_attention_backward(do, q, k, v, o, stats, kv_lens=kv_lens, mask=mask, scale=ctx.scale)
@@ -313,7 +317,7 @@ class _CrossAttention(torch.autograd.Function):
 
 
 def cross_attention(q, k, v, *, kv_lens=None, mask=None, scale=None):
-    """:func:`cross_attention_forward`'s o, differentiable in q, k and v."""
+    """:func:`cross_attention_forward`'s o, differentiable (once) in q, k and v."""
     return _CrossAttention.apply(q, k, v, kv_lens, mask, scale)
 
 

@@ -216,3 +216,51 @@ def test_cross_attention_formula_against_differences(Hq, Hk):
         e = torch.randn((q, k, v)[which].shape, generator=g, dtype=torch.float64)
         got = _slope(lambda *a: (R.cross_attention(*a, **kw)["o"][0] * do).sum(), (q, k, v), which, e)
         assert abs(got - float((ref[name][0] * e).sum())) < 1e-7, name
+
+
+# ------------------------------------------------------------------ autograd, on formulas in the kernels' place
+def _norm_formula(x, w, b, eps):
+    mean = x.mean(-1)
+    rstd = 1 / torch.sqrt(x.var(-1, unbiased=False) + eps)
+    xh = (x - mean[..., None]) * rstd[..., None]
+    return xh * w + b, mean, rstd
+
+
+def _norm_formula_backward(dy, x, mean, rstd, w, param_dtype=None):
+    xh = (x - mean[..., None]) * rstd[..., None]
+    g = dy * w
+    return (rstd[..., None] * (g - g.mean(-1, keepdim=True) - xh * (g * xh).mean(-1, keepdim=True)), (dy * xh).sum(0), dy.sum(0))
+
+
+def test_layer_norm_refuses_second_derivatives(monkeypatch):
+    """The backward pass has no derivative of its own: a gradient's gradient is refused, not taken as zero."""
+    monkeypatch.setattr(O, "layer_norm_forward", _norm_formula)
+    monkeypatch.setattr(O, "layer_norm_backward", _norm_formula_backward)
+    g = torch.Generator().manual_seed(2)
+    x, w, b = (torch.randn(s, generator=g, dtype=torch.float64).requires_grad_() for s in ((4, 9), (9,), (9,)))
+    loss = O.layer_norm(x, w, b).pow(3).sum() + x.square().sum()
+    want, = torch.autograd.grad(torch.nn.functional.layer_norm(x, (9,), w, b).pow(3).sum() + x.square().sum(), x)
+    grad, = torch.autograd.grad(loss, x, create_graph=True)
+    assert torch.allclose(grad, want)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        grad.square().sum().backward()
+
+
+def test_cross_attention_refuses_second_derivatives(monkeypatch):
+    def formula(q, k, v, *, kv_lens=None, mask=None, scale=None):
+        return R.cross_attention(q, k, v)["o"][0], torch.zeros(1)
+
+    def backward(do, q, k, v, o, stats, *, kv_lens=None, mask=None, scale=None):
+        ref = R.cross_attention(q, k, v, do)
+        return tuple(ref[n][0] for n in ("dq", "dk", "dv"))
+
+    monkeypatch.setitem(R.U, torch.float64, 0.0)
+    monkeypatch.setitem(R.TINY, torch.float64, 0.0)
+    monkeypatch.setattr(O, "cross_attention_forward", formula)
+    monkeypatch.setattr(O, "cross_attention_backward", backward)
+    g = torch.Generator().manual_seed(3)
+    q, k, v = (torch.randn((1, n, 2, 6), generator=g, dtype=torch.float64).requires_grad_() for n in (4, 7, 7))
+    loss = O.cross_attention(q, k, v).pow(3).sum() + q.square().sum()
+    grad, = torch.autograd.grad(loss, q, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        grad.square().sum().backward()
