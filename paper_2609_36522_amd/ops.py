@@ -317,7 +317,10 @@ class _CrossAttention(torch.autograd.Function):
 
 
 def cross_attention(q, k, v, *, kv_lens=None, mask=None, scale=None):
-    """:func:`cross_attention_forward`'s o, differentiable (once) in q, k and v."""
+    """:func:`cross_attention_forward`'s o, differentiable (once) in q, k and v. The mask gets no gradient: one that
+    requires it is refused."""
+    if mask is not None and mask.requires_grad and torch.is_grad_enabled():
+        raise ValueError("cross attention has no gradient for its mask: pass mask.detach()")
     return _CrossAttention.apply(q, k, v, kv_lens, mask, scale)
 
 

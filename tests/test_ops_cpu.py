@@ -264,3 +264,16 @@ def test_cross_attention_refuses_second_derivatives(monkeypatch):
     grad, = torch.autograd.grad(loss, q, create_graph=True)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         grad.square().sum().backward()
+
+
+def test_cross_attention_refuses_a_learned_mask(monkeypatch):
+    """An additive mask gets no gradient: one that asks for it is refused where gradients are recorded."""
+    monkeypatch.setattr(O, "cross_attention_forward", lambda q, k, v, *, kv_lens=None, mask=None, scale=None: (q * 1, torch.zeros(1)))
+    q, k, v = (torch.zeros(1, n, 2, 8, dtype=torch.bfloat16) for n in (3, 5, 5))
+    mask = torch.zeros(1, 5, requires_grad=True)
+    for first in (q, q.clone().requires_grad_()):
+        with pytest.raises(ValueError, match="mask"):
+            O.cross_attention(first, k, v, mask=mask)
+        assert O.cross_attention(first, k, v, mask=mask.detach()).shape == q.shape
+        with torch.no_grad():
+            assert O.cross_attention(first, k, v, mask=mask).shape == q.shape
