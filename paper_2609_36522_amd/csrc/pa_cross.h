@@ -16,7 +16,8 @@
 // Softmax. One pass over the keys with a running maximum and sum in fp32; the accumulator is
 // rescaled only in steps where some row's maximum grew. P and dS are rounded to the element type for
 // their products (the accumulation stays fp32): their rounding errors are independent, so a sum
-// over keys keeps the relative error of one rounding, the size of the output's own.
+// over keys keeps the relative error of one rounding, the size of the output's own. In fp16 that holds for
+// normal numbers only, so dS is brought into their range by powers of two (k_cross_bwd.hip).
 #pragma once
 
 #include <math.h>

@@ -3,8 +3,11 @@ what a kernel's main path takes."""
 import math
 
 import pytest
+import torch
 
-from test_gpu_ops import BF16, _check_lora, _lora_case
+import ops_reference as R
+from paper_2609_36522_amd import ops
+from test_gpu_ops import BF16, F16, _check_lora, _cross_case, _lora_case
 
 pytestmark = pytest.mark.gpu
 
@@ -43,3 +46,48 @@ def test_lora_linear_a_row_that_is_not_finite(M, K, N, Rk):
     x[M - 3, 0] = -math.inf
     x[M // 2, 1] = math.nan
     _check_lora(x, w.abs(), a.abs(), b.abs(), [0, 2, 11, M // 2, M], [0, 1, -1, 2], s, bias)
+
+
+# ------------------------------------------------------------------ cross attention
+def _spread(B_, Lq, H, Lk, D, small, f=8.0, seed=0):
+    """q, k, v with scores of a deviation of 1.5; ``small`` (q or k) is f times smaller than 1, the other larger."""
+    q, k, v, do = _cross_case(B_, Lq, H, H, Lk, D, F16, seed=seed, sharp=1.0)
+    fq, fk = (1.5 / f, f) if small == "q" else (1.5 * f, 1 / f)
+    return (q * fq).to(F16), (k * fk).to(F16), v, do
+
+
+def _grads(q, k, v, do, **kw):
+    o, stats = ops.cross_attention_forward(q, k, v, **kw)
+    ref = R.cross_attention(q, k, v, do, **kw)
+    return dict(zip(("dq", "dk", "dv"), ops.cross_attention_backward(do, q, k, v, o, stats, **kw))), ref
+
+
+def _norm_check(got, want, what):
+    """Independent roundings of dS, of o in delta and of the result itself: each moves the result by about
+    u of its norm, and a result below the type's normal numbers by half their spacing an element."""
+    err, size = float((got.double() - want).norm()), float(want.norm())
+    assert err <= 4 * R.U[F16] * size + R.TINY[F16] * math.sqrt(got.numel()), (what, err / size)
+
+
+@pytest.mark.parametrize("f", [1.0, 1e-2, 1e-3, 2.0 ** -14])
+@pytest.mark.parametrize("Lq,Lk,D", [(150, 77, 64), (150, 200, 64), (150, 200, 128), (150, 4099, 64), (40, 3001, 33), (150, 2000, 96)])
+@pytest.mark.parametrize("name", ["dq", "dk"])
+def test_cross_attention_gradients_of_any_size_in_f16(name, Lq, Lk, D, f):
+    """Incoming gradients far below 1 over many keys: dS is far below fp16's normal numbers, dq or dk is not."""
+    q, k, v, do = _spread(1, Lq, 2, Lk, D, "q" if name == "dq" else "k")
+    do = (f * do).to(F16)
+    got, ref = _grads(q, k, v, do)
+    _norm_check(got[name], ref[name][0], name)
+
+
+@pytest.mark.parametrize("Lk,D", [(3, 128), (3, 64), (140, 64), (300, 64)])
+@pytest.mark.parametrize("name", ["dq", "dk"])
+def test_cross_attention_large_gradients_in_f16(name, Lk, D):
+    """dS beyond fp16's range (two keys take nearly all weight) where dq or dk is not."""
+    q, k, v, do = _spread(1, 20, 2, Lk, D, "k" if name == "dq" else "q", f=64.0)
+    do = (1.5e4 * do).clamp(-6e4, 6e4).to(F16)
+    mask = torch.full((1, Lk), -20.0, device="cuda")
+    mask[0, 0] = mask[0, Lk - 1] = 0.0
+    got, ref = _grads(q, k, v, do, mask=mask)
+    assert bool(torch.isfinite(got[name]).all())
+    _norm_check(got[name], ref[name][0], name)
