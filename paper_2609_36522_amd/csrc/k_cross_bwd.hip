@@ -78,10 +78,25 @@ __device__ __forceinline__ void unscale(f32x16 (&acc)[DB], float power) {
     }
 }
 
-// Where dk, dv find the statistics of 32 tokens of a query head: hi, lo and delta, 32 of each.
+// dk, dv take P itself as an operand, times 2^kLift: a key with little weight has all of its P below fp16's
+// normal numbers (keys of weights around 3e-8: dv off by its own size), while P is at most 1 (and a rounding of
+// the statistics, for which fp16 leaves two more bits).
+template <class T>
+constexpr float kLift = kNarrow<T> ? 14.0f : 0.0f;
+template <class T>
+constexpr float kLifted = kNarrow<T> ? 0x1p14f : 1.0f;
+
+// Where dk, dv find the statistics of 32 tokens of a query head: hi, lo (of lifted weights) and delta, 32 of each.
 __device__ __forceinline__ float* tile_stats(const CrossDev& d, int b, RowAt r) {
     const int64_t head = (int64_t)b * d.q_heads + r.head, tiles = (d.q_len + 31) / 32;
     return d.row_stats + (head * tiles + (r.token >> 5)) * 96 + (r.token & 31);
+}
+template <class T, int MASK>
+__device__ __forceinline__ void put_stats(const CrossDev& d, int b, RowAt r, float hi, float lo, float delta) {
+    float* out = tile_stats(d, b, r);
+    out[0] = MASK ? hi : hi - kLift<T>;
+    out[32] = lo - kLift<T>;
+    out[64] = delta;
 }
 
 // The rows' statistics where dq, which writes them on its way, is not asked for: 16 lanes per row of
@@ -106,10 +121,7 @@ __global__ __launch_bounds__(kThreads) void k_cross_stats(CrossDev d) {
         const int64_t sat = stat_at(d, b, {t, h});
         float hi, lo;
         row_stats<MASK>(d.stats[sat * 2], d.stats[sat * 2 + 1], hi, lo);
-        float* out = tile_stats(d, b, {t, h});
-        out[0] = hi;
-        out[32] = lo;
-        out[64] = s;
+        put_stats<T, MASK>(d, b, {t, h}, hi, lo, s);
     }
 }
 
@@ -241,12 +253,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
             st.load_mask(d, b, key_at(i + 2), kend);
         }
     }
-    if (wk.split == 0 && valid && half == 0) {
-        float* out = tile_stats(d, b, ra);
-        out[0] = hi;
-        out[32] = lo;
-        out[64] = delta;
-    }
+    if (wk.split == 0 && valid && half == 0) put_stats<T, MASK>(d, b, ra, hi, lo, delta);
     unscale<T>(acc, power);
     if (wk.part < 0) {
         T* out = static_cast<T*>(d.dq) + b * d.dqs[0] + ra.token * d.dqs[1] + ra.head * d.dqs[2];
@@ -339,12 +346,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_dq_short(CrossDev d) {
             for (int db = 0; db < DB; ++db) acc[db] = mma(read_cols<T, DP>(tiles[0], nt * 32 + t * 16, db, lane), ds, acc[db]);
         }
     }
-    if (valid && half == 0) {
-        float* out = tile_stats(d, b, ra);
-        out[0] = hi;
-        out[32] = lo;
-        out[64] = delta;
-    }
+    if (valid && half == 0) put_stats<T, MASK>(d, b, ra, hi, lo, delta);
     unscale<T>(acc, power);
     T* out = static_cast<T*>(d.dq) + b * d.dqs[0] + ra.token * d.dqs[1] + ra.head * d.dqs[2];
     store_row<T, DB, WIDTH>(out, d.dim, acc, d.scale, half, valid);
@@ -479,7 +481,8 @@ __global__ __launch_bounds__(kThreads, KS <= 6 ? 2 : 1) void k_cross_dkv(CrossDe
 #pragma unroll
         for (int i = 0; i < DB; ++i) ak[i] = av[i] = f32x16{};
     }
-    unscale<T>(ak, power);
+    unscale<T>(ak, power * kLifted<T>);
+    unscale<T>(av, kLifted<T>);
     const bool valid = key < d.kv_len;
     if (d.row_splits == 1) {
         T* ok = static_cast<T*>(d.dk) + b * d.dks[0] + key * d.dks[1] + hk * d.dks[2];

@@ -17,7 +17,8 @@
 // rescaled only in steps where some row's maximum grew. P and dS are rounded to the element type for
 // their products (the accumulation stays fp32): their rounding errors are independent, so a sum
 // over keys keeps the relative error of one rounding, the size of the output's own. In fp16 that holds for
-// normal numbers only, so dS is brought into their range by powers of two (k_cross_bwd.hip).
+// normal numbers only, so dS, and P where it is dv's operand, are brought into their range by powers of two
+// (k_cross_bwd.hip); the forward pass's weights are relative to the row's largest score.
 #pragma once
 
 #include <math.h>

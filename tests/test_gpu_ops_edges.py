@@ -91,3 +91,19 @@ def test_cross_attention_large_gradients_in_f16(name, Lk, D):
     got, ref = _grads(q, k, v, do, mask=mask)
     assert bool(torch.isfinite(got[name]).all())
     _norm_check(got[name], ref[name][0], name)
+
+
+@pytest.mark.parametrize("Lq,Lk,D", [(64, 120, 64), (64, 4099, 64), (200, 4099, 128), (1, 1000, 40)])
+def test_cross_attention_dv_of_keys_with_little_weight_in_f16(Lq, Lk, D):
+    """Keys with weights around 1e-8 beside ordinary ones, and a gradient that makes their dv an ordinary number:
+    each weight's rounding moves a key's dv by at most u of its terms' magnitudes, as does dv's own."""
+    q, k, v, do = _spread(1, Lq, 2, Lk, D, "k")
+    q = (q / 3).to(F16)
+    do = (1e3 * do).to(F16)
+    mask = torch.zeros(1, Lk, device="cuda")
+    mask[0, 1::2] = math.log(3e-8 * Lk / 2)
+    got, ref = _grads(q, k, v, do, mask=mask)
+    terms = R.cross_attention(q, k, v, do.abs(), mask=mask)["dv"][0]          # P^T |do|
+    err, size = (got["dv"].double() - ref["dv"][0]).norm(dim=-1), terms.norm(dim=-1)
+    bad = err > 4 * R.U[F16] * size + R.TINY[F16] * math.sqrt(D)
+    assert not bool(bad.any()), float((err / size).max())
