@@ -60,34 +60,39 @@ class ConditionedBlock:
     def parameters(self):
         return [self.weight, self.bias, *(self.w[p] for p in PROJECTIONS)]
 
-    def _split(self, t, batch, heads):
-        return t.reshape(batch, -1, heads, self.head_dim)
+    def _split(self, t, heads):
+        return t.reshape(*t.shape[:2], heads, self.head_dim)
 
     @torch.no_grad()
     def serve(self, h, context, adapters: Adapters, ids, *, lengths=None):
         """One pass for a batch of requests; request b (a sample) uses adapter ids[b] (int32, none if
         negative). lengths: int32 [batch], the prompts' states (all of them if None)."""
-        batch, tokens = h.shape[:2]
 
-        def project(p, x):
-            rows = x.shape[1]
-            offsets = torch.arange(0, batch * rows + 1, rows, dtype=torch.int32, device=x.device)
-            y = ops.lora_linear(x.reshape(batch * rows, -1), self.w[p], adapters.a[p], adapters.b[p], offsets, ids, scales=adapters.scales)
-            return y.reshape(batch, rows, -1)
+        def offsets(x):
+            batch, rows = x.shape[:2]
+            if rows == 0:
+                return torch.zeros(batch + 1, dtype=torch.int32, device=x.device)
+            return torch.arange(0, batch * rows + 1, rows, dtype=torch.int32, device=x.device)
+
+        tokens, states = offsets(h), offsets(context)
+
+        def project(p, x, off):
+            y = ops.lora_linear(x.reshape(x.shape[0] * x.shape[1], x.shape[2]), self.w[p], adapters.a[p], adapters.b[p], off, ids,
+                                scales=adapters.scales)
+            return y.reshape(*x.shape[:2], y.shape[1])
 
         x, _, _ = ops.layer_norm_forward(h, self.weight, self.bias, self.eps)
-        q = self._split(project("q", x), batch, self.heads)
-        k = self._split(project("k", context), batch, self.kv_heads)
-        v = self._split(project("v", context), batch, self.kv_heads)
+        q = self._split(project("q", x, tokens), self.heads)
+        k = self._split(project("k", context, states), self.kv_heads)
+        v = self._split(project("v", context, states), self.kv_heads)
         o, _ = ops.cross_attention_forward(q, k, v, kv_lens=lengths)
-        return h + project("o", o.reshape(batch, tokens, self.hidden))
+        return h + project("o", o.reshape(h.shape), tokens)
 
     def __call__(self, h, context, *, lengths=None):
         """The block without adapters, differentiable."""
-        batch, tokens = h.shape[:2]
         x = ops.layer_norm(h, self.weight, self.bias, self.eps)
-        q = self._split(torch.nn.functional.linear(x, self.w["q"]), batch, self.heads)
-        k = self._split(torch.nn.functional.linear(context, self.w["k"]), batch, self.kv_heads)
-        v = self._split(torch.nn.functional.linear(context, self.w["v"]), batch, self.kv_heads)
-        o = ops.cross_attention(q, k, v, kv_lens=lengths).reshape(batch, tokens, self.hidden)
+        q = self._split(torch.nn.functional.linear(x, self.w["q"]), self.heads)
+        k = self._split(torch.nn.functional.linear(context, self.w["k"]), self.kv_heads)
+        v = self._split(torch.nn.functional.linear(context, self.w["v"]), self.kv_heads)
+        o = ops.cross_attention(q, k, v, kv_lens=lengths).reshape(h.shape)
         return h + torch.nn.functional.linear(o, self.w["o"])

@@ -86,3 +86,16 @@ def test_training_step_gradients():
         err = float((got.grad.double() - want.grad).norm() / want.grad.norm())
         assert err < 12 * U[torch.bfloat16], (name, err)
     assert not bool(ctx.grad[1, 40:].any())           # states past the prompt's length
+
+
+def test_a_batch_without_states_tokens_or_requests():
+    """The smallest inputs: attention over no states adds nothing, no tokens or no requests give as many."""
+    wl = workloads.SMALL_MLP
+    blk = conditioning.ConditionedBlock(wl.hidden, 256, 8, 4)
+    h, ctx, _ = _inputs(wl, blk, 3, 9, 2)
+    ad, ids = blk.adapters(2, 16), torch.tensor([1, -1, 0], dtype=torch.int32, device="cuda")
+    none = torch.zeros(3, dtype=torch.int32, device="cuda")
+    for y in (blk.serve(h, ctx[:, :0], ad, ids), blk.serve(h, ctx, ad, ids, lengths=none), blk(h, ctx[:, :0]), blk(h, ctx, lengths=none)):
+        assert torch.equal(y, h)
+    assert blk.serve(h[:, :0], ctx, ad, ids).shape == (3, 0, wl.hidden) == blk(h[:, :0], ctx).shape
+    assert blk.serve(h[:0], ctx[:0], ad, ids[:0]).shape == h[:0].shape == blk(h[:0], ctx[:0]).shape
