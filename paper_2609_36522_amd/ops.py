@@ -221,7 +221,7 @@ def _cross(q_shape, k_shape, dtype, scale, q_stride, k_stride, v_stride, o_strid
     """The description of an attention without its kv_lens and mask (to be copied), and the workspaces of its
     forward and backward pass (which do not depend on them)."""
     (Bn, Lq, Hq, D), (_, Lk, Hk, _) = q_shape, k_shape
-    p = Cross(Bn, Lq, Lk, Hq, Hk, D, dtype, 1.0 / math.sqrt(D) if scale is None else scale,
+    p = Cross(Bn, Lq, Lk, Hq, Hk, D, dtype, 1.0 / math.sqrt(max(D, 1)) if scale is None else scale,
               q_stride[:3], k_stride[:3], v_stride[:3], o_stride[:3])
     p.mask_kind, p.mask_stride = mask_kind, mask_stride
     if mask_kind:

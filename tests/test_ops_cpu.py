@@ -277,3 +277,10 @@ def test_cross_attention_refuses_a_learned_mask(monkeypatch):
         assert O.cross_attention(first, k, v, mask=mask.detach()).shape == q.shape
         with torch.no_grad():
             assert O.cross_attention(first, k, v, mask=mask).shape == q.shape
+
+
+def test_cross_attention_refuses_heads_without_elements():
+    """The default scale of a head width of 0 is no error of its own: the library refuses the width."""
+    q = torch.zeros(1, 2, 2, 0, dtype=torch.bfloat16)
+    with pytest.raises(B.PAError, match="head_dim"):
+        O._cross_args(q, q, q, None, None, None, q)
