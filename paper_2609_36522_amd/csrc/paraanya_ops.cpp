@@ -72,9 +72,10 @@ int check_stride(const int64_t s[3], const char* what) {
     return PA_OK;
 }
 
-// Outputs: distinct elements at distinct addresses need strides that are not 0.
+// Outputs: distinct elements at distinct addresses need strides that are not 0 (one without elements may have any).
 int check_out_stride(const int64_t s[3], int64_t b, int64_t l, int64_t h, int dim, const char* what) {
     if (int rc = check_stride(s, what)) return rc;
+    if (b == 0 || l == 0) return PA_OK;
     if ((b > 1 && s[0] == 0) || (l > 1 && s[1] < dim) || (h > 1 && s[2] < dim))
         return fail(PA_ERR_INVALID_ARG, "cross attention: %s overlaps itself", what);
     return PA_OK;

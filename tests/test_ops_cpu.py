@@ -284,3 +284,15 @@ def test_cross_attention_refuses_heads_without_elements():
     q = torch.zeros(1, 2, 2, 0, dtype=torch.bfloat16)
     with pytest.raises(B.PAError, match="head_dim"):
         O._cross_args(q, q, q, None, None, None, q)
+
+
+@pytest.mark.parametrize("kw", [dict(q_len=0, o_stride=(0, 256, 64)), dict(batch=0, o_stride=(0, 0, 0)),
+                                dict(q_len=0, kv_len=0, o_stride=(0, 0, 0))])
+def test_cross_attention_outputs_without_elements_overlap_nothing(kw):
+    """Strides of an output that has no elements are not looked at: a dense one without tokens has a stride of 0."""
+    lib, p, n = O._library(), _cross(**kw), C.c_size_t(0)
+    assert lib.paraanya_cross_attention_workspace(C.byref(p), C.byref(n)) == B.PA_OK, lib.paraanya_last_error()
+    assert lib.paraanya_cross_attention(C.byref(p), PTR, PTR, PTR, PTR, PTR, PTR, 1 << 30, None) == B.PA_OK
+    none = O.CrossGrad(*[(C.c_int64 * 3)(0, 0, 0)] * 4)
+    if kw.get("batch") == 0:
+        assert lib.paraanya_cross_attention_backward(C.byref(p), C.byref(none), *[PTR] * 10, 1 << 30, None) == B.PA_OK
