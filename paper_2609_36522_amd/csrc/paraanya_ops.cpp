@@ -137,11 +137,11 @@ pa::CrossDev cross_dev(const pa_cross_t* p, bool backward) {
     return d;
 }
 
-// Offsets of the workspace's parts; returns its size.
-size_t cross_layout(pa::CrossDev& d, bool backward, char* ws) {
+// The workspace's parts; returns its size (all that is wanted of a workspace that is not there).
+size_t cross_layout(pa::CrossDev& d, bool backward, void* ws) {
     size_t used = 0;
     auto take = [&](size_t floats) {
-        float* p = reinterpret_cast<float*>(ws + used);
+        float* p = ws ? reinterpret_cast<float*>(static_cast<char*>(ws) + used) : nullptr;
         used += round256(floats * sizeof(float));
         return p;
     };
@@ -280,7 +280,7 @@ int paraanya_cross_attention(const pa_cross_t* p, const void* q, const void* k, 
         if (misaligned(q, 2) || misaligned(k, 2) || misaligned(v, 2) || misaligned(o, 2) || misaligned(stats, 4))
             return fail(PA_ERR_INVALID_ARG, "cross attention: a pointer is not aligned to its element");
         pa::CrossDev d = cross_dev(p, false);
-        if (int rc = check_workspace(workspace, workspace_bytes, cross_layout(d, false, static_cast<char*>(workspace)))) return rc;
+        if (int rc = check_workspace(workspace, workspace_bytes, cross_layout(d, false, workspace))) return rc;
         d.q = q;
         d.k = k;
         d.v = v;
@@ -322,7 +322,7 @@ int paraanya_cross_attention_backward(const pa_cross_t* p, const pa_cross_grad_t
             misaligned(dq, 2) || misaligned(dk, 2) || misaligned(dv, 2) || misaligned(stats, 4))
             return fail(PA_ERR_INVALID_ARG, "cross attention: a pointer is not aligned to its element");
         pa::CrossDev d = cross_dev(p, true);
-        if (int rc = check_workspace(workspace, workspace_bytes, cross_layout(d, true, static_cast<char*>(workspace)))) return rc;
+        if (int rc = check_workspace(workspace, workspace_bytes, cross_layout(d, true, workspace))) return rc;
         d.q = q;
         d.k = k;
         d.v = v;
