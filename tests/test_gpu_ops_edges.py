@@ -1,5 +1,6 @@
 """The operators of include/paraanya_ops.h on the device where a value, a width or a stride is at the edge of
-what a kernel's main path takes."""
+what a kernel's main path takes: values that are not finite in places that belong to somebody else, gradients
+far below or above 1, hidden keys at every head width, strides of any parity."""
 import math
 
 import pytest
@@ -7,7 +8,7 @@ import torch
 
 import ops_reference as R
 from paper_2609_36522_amd import ops
-from test_gpu_ops import BF16, F16, _check_lora, _cross_case, _lora_case
+from test_gpu_ops import BF16, F16, _check_cross, _check_lora, _cross_case, _gen, _lora_case, _randn
 
 pytestmark = pytest.mark.gpu
 
@@ -107,3 +108,63 @@ def test_cross_attention_dv_of_keys_with_little_weight_in_f16(Lq, Lk, D):
     err, size = (got["dv"].double() - ref["dv"][0]).norm(dim=-1), terms.norm(dim=-1)
     bad = err > 4 * R.U[F16] * size + R.TINY[F16] * math.sqrt(D)
     assert not bool(bad.any()), float((err / size).max())
+
+
+@pytest.mark.parametrize("D", [7, 33, 64, 80, 96, 127, 128])
+@pytest.mark.parametrize("Lq,Lk", [(1, 70), (40, 77), (150, 333)])
+def test_cross_attention_hidden_keys_at_every_head_width(Lq, Lk, D):
+    """NaN and infinities past a sample's length and at masked keys, in every layout of a tile."""
+    g = _gen(D)
+    dt = BF16 if D % 2 else F16
+    q, k, v, do = _cross_case(4, Lq, 4, 2, Lk, D, dt, seed=D)
+    lens = torch.tensor([Lk, 1, Lk // 2 + 1, 0], dtype=torch.int32, device="cuda")
+    keep = torch.rand((4, Lk), generator=g, device="cuda") < 0.6
+    keep[2] = False
+    keep[2, Lk // 2] = True
+    past = torch.arange(Lk, device="cuda")[None] >= lens[:, None]
+    k[past], v[past] = math.inf, math.nan
+    _check_cross(q, k, v, do, kv_lens=lens)
+    k[~keep], v[~keep] = math.nan, -math.inf
+    add = torch.where(keep, _randn(g, 4, Lk), -math.inf)
+    for mask in (keep, keep.to(torch.uint8), add):
+        _check_cross(q, k, v, do, mask=mask, kv_lens=lens)
+
+
+@pytest.mark.parametrize("kind", ["none", "bool", "add"])
+@pytest.mark.parametrize("D", [40, 128])
+def test_cross_attention_hidden_keys_of_long_states(kind, D):
+    """Few rows over thousands of keys, split over blocks: ranges that see no key, hidden NaN and infinities."""
+    g = _gen(9)
+    Lk = 5003
+    q, k, v, do = _cross_case(3, 2, 4, 2, Lk, D, F16, seed=9)
+    lens = torch.tensor([Lk, 700, 4000], dtype=torch.int32, device="cuda")
+    keep = torch.rand((3, Lk), generator=g, device="cuda") < 0.7
+    keep[0, 500:3500] = False
+    keep[2, :3900] = False
+    past = torch.arange(Lk, device="cuda")[None] >= lens[:, None]
+    k[past], v[past] = math.nan, math.inf
+    mask = None
+    if kind != "none":
+        k[~keep], v[~keep] = math.inf, math.nan
+        mask = keep if kind == "bool" else torch.where(keep, _randn(g, 3, Lk), -math.inf)
+    _check_cross(q, k, v, do, mask=mask, kv_lens=lens)
+
+
+@pytest.mark.parametrize("D", [8, 40, 64, 80, 128])
+@pytest.mark.parametrize("Lq,Lk", [(1, 300), (40, 77), (150, 130), (150, 400)])
+def test_cross_attention_strides_of_any_parity(Lq, Lk, D):
+    """Tokens, heads and samples an odd number of elements apart, from an odd element on: rows at any address."""
+    q, k, v, do = _cross_case(2, Lq, 4, 2, Lk, D, BF16)
+
+    def apart(t, token, head):
+        B_, L, H, _ = t.shape
+        row = H * (D + head) + token + (H * head + token + 1) % 2
+        wide = torch.zeros(B_ * L * row + 2 * B_ + 64, dtype=t.dtype, device="cuda")
+        view = wide.as_strided(t.shape, (L * row + 1, row, D + head, 1), 1)
+        view.copy_(t)
+        return view
+
+    a = [apart(q, 0, 0), apart(k, 1, 0), apart(v, 2, 3), apart(do, 0, 1)]
+    assert all(t.stride(1) % 2 for t in a[:1])
+    _check_cross(*a)
+    _check_cross(q, apart(k, 5, 0), apart(v, 6, 0), do, mask=torch.rand((2, Lk), generator=_gen(3), device="cuda") < 0.8)
