@@ -391,7 +391,7 @@ __device__ __forceinline__ void finish(const LoraDev& d, int f0, int r0, int lan
 // matrix units and the LDS reads that feed them: 32768x2048x2048, rank 64, 280 to 300 us (980 to 920 TFLOP/s,
 // 1415 for a large library product).
 template <class T, int WF, int WR, int NM, int NX, int STAGES, int WIDTH>
-__global__ __launch_bounds__(64 * WF * WR, NM * NX == 16 ? 1 : 2) void k_lora_tile(LoraDev d) {
+__global__ __launch_bounds__(64 * WF * WR, 2) void k_lora_tile(LoraDev d) {
     typedef typename Vec<T>::v8 v8;
     constexpr int TF = WF * NM * 32, TR = WR * NX * 32, THREADS = 64 * WF * WR;
     static_assert(direct(WIDTH) || STAGES == 2, "registers hold one part");
