@@ -18,6 +18,8 @@
  *   - Strides count elements. Pointers need the alignment of their element type only; 16-byte
  *     alignment of rows is faster.
  *   - Sums, softmax statistics and products are accumulated in fp32 whatever the element type.
+ *     What is rounded to the element type on the way, as the operand of a second product, is said
+ *     at each operator.
  */
 #ifndef PARAANYA_OPS_H
 #define PARAANYA_OPS_H
@@ -74,7 +76,14 @@ PA_API int paraanya_layer_norm_backward_workspace(const pa_norm_t* p, size_t* by
  * visible. PA_MASK_ADD: fp32 per key, added to the scaled score; -inf = not visible (the type's
  * lowest value is a finite bias: a row that has nothing else averages those keys).
  * What an invisible key's k and v hold, infinities and NaN included, has no effect. A row that
- * sees no key gives o = 0 and zero gradients. */
+ * sees no key gives o = 0 and zero gradients.
+ *
+ * Roundings to the element type beside those of the results: the weights (relative to the row's
+ * largest) for their product with v, P for dv, and dS = P (do v^T - delta) for dq and dk. In fp16, P
+ * and dS are scaled by powers of two, so that weights and gradients below its normal numbers, or
+ * beyond its range, keep their digits. delta is formed in fp32 up to kv_len = 256, from the rounded o
+ * above. Errors, root mean square over the result's own: o 1.1 to 1.4 times that of its rounding
+ * alone, gradients 1.3 to 1.65 times. */
 #define PA_MASK_NONE 0
 #define PA_MASK_BOOL 1
 #define PA_MASK_ADD  2
@@ -121,7 +130,8 @@ PA_API int paraanya_cross_attention_backward_workspace(const pa_cross_t* p, size
  * y = x W^T + bias + s_a (x A_a^T) B_a^T for the rows of many requests at once: request i is rows
  * offsets[i] .. offsets[i + 1] - 1 and uses adapter a = ids[i] (a < 0 or >= adapters: none). Rows
  * before offsets[0] and from offsets[requests] on have no adapter. Offsets must not decrease; they
- * are clamped to [0, rows]. Inference only: no gradients. */
+ * are clamped to [0, rows]. Inference only: no gradients. What a request's adapter or rows hold,
+ * infinities and NaN included, has no effect on the rows of others. */
 #define PA_LORA_MAX_RANK 128
 
 typedef struct {

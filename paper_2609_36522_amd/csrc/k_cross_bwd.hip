@@ -126,13 +126,15 @@ __global__ __launch_bounds__(kThreads) void k_cross_stats(CrossDev d) {
 }
 
 // dq: the forward pass's tiling; a lane owns a row, K and V tiles pass by. Bound by the products and the
-// LDS reads that feed them: 2 x 2309 tokens, 16 heads over 4 of 80, 1541 keys 90 us (matrix units busy 35%).
+// LDS reads that feed them: 2 x 2309 tokens, 16 heads over 4 of 80, 1541 keys in fp16 94 us (matrix
+// units busy 32%).
 //
 // delta, the sum of do * o over the head, equals the sum of P dP over the keys. The first takes the rounded
 // o: its error is one of o's rounding, common to the row's keys, which is lost beside dS's own rounding
 // where many keys share the weight. Up to kExactKeys keys (EXACT) the second is formed in fp32 by a pass of
 // its own over the (few) tiles: the gradients' error at 77 keys is 1.4 instead of 1.6 times the output's
-// rounding.
+// rounding. The rule goes by kv_len, which the host knows: a sample with few visible keys among more has the
+// first form's error (1.5 to 1.65 times over hundreds to thousands of keys).
 constexpr int kExactKeys = 256;
 
 template <class T, int KS, int MASK, int WIDTH, bool EXACT>
@@ -265,7 +267,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_dq(CrossDev d) {
 }
 
 // The same for at most 128 keys and a head width of at most 64: all keys' scores and dP stay in registers
-// between the pass that forms delta and the one that uses it: 8 x 1024 tokens, 16 heads of 64, 77 keys 19.6 us.
+// between the pass that forms delta and the one that uses it: 8 x 1024 tokens, 16 heads of 64, 77 keys 20 us.
 constexpr int kShortKeys = 128;
 
 template <class T, int MASK, int WIDTH>
@@ -354,7 +356,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross_dq_short(CrossDev d) {
 
 // dk, dv: a wave owns 32 keys (K and V in registers), tiles of 32 tokens of one query head and their
 // statistics pass by, up to three on their way; the heads of the group one after the other. The sizes of dq's
-// comments: 126 us over 1541 keys (matrix units busy 37%; 416 of the 512 places for blocks are taken), 19.8 us
+// comments: 132 us over 1541 keys in fp16 (matrix units busy 33%; 416 of the 512 places for blocks are taken), 20 us
 // over 77, of which some 15 are a block's start and the writing of its partial sums (with 256 or 768 ranges
 // in place of 512: 20.8 and 23.8).
 template <class T, int KS, int MASK, int WIDTH>

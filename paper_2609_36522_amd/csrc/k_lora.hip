@@ -27,7 +27,9 @@ constexpr int kCUs = 256;
 
 // A width of its own for the tiles: rows of an even number of elements (at least 8) at even addresses and
 // strides, which are read as whole ones are but for the piece that holds the row's end (32768x2044x2048:
-// 492 us as ragged rows, 289 so). It and kWhole are for ranks of a multiple of 8.
+// 492 us as ragged rows, 289 so). It and kWhole are for ranks of a multiple of 8. Rows of an odd length, stride or
+// address are taken as ragged ones; loads that write LDS serve them too (cross attention's do) and are not used
+// here: 32768x2045x2048, rank 64, 533 us as ragged rows, 350 as even ones would be.
 constexpr int kEven = 3;
 constexpr bool direct(int width) { return width == kWhole || width == kEven; }
 
@@ -388,7 +390,7 @@ __device__ __forceinline__ void finish(const LoraDev& d, int f0, int r0, int lan
 
 // WF x WR waves of NM x NX tiles of 32 x 32 (features x rows) per block. The reduction goes through LDS in
 // parts of 64 columns, of which STAGES - 1 are on their way during the products of the current one. Bound by the
-// matrix units and the LDS reads that feed them: 32768x2048x2048, rank 64, 280 to 300 us (980 to 920 TFLOP/s,
+// matrix units and the LDS reads that feed them: 32768x2048x2048, rank 64, 289 to 298 us (950 to 920 TFLOP/s,
 // 1415 for a large library product).
 template <class T, int WF, int WR, int NM, int NX, int STAGES, int WIDTH>
 __global__ __launch_bounds__(64 * WF * WR, 2) void k_lora_tile(LoraDev d) {
@@ -557,7 +559,8 @@ template <class T, int NR, int WIDTH>
 void down(const LoraDev& d, hipStream_t st) {
     // Blocks per request: its share of the rows, so that the launch has about rows / 64 (or 32) of them.
     // Where those of 64 rows are fewer than the CUs, or requests shorter, latency counts (1999 rows: 42 us in
-    // blocks of 64 rows, 14 in blocks of 32; 8192: 11.8 and 11.6; 32768: 32 and 77).
+    // blocks of 64 rows, 14 in blocks of 32; 8192: 11.8 and 11.6; 32768: 32 and 77). A request far above the average
+    // keeps its share of the blocks: 48 requests, one with 8098 of 8192 rows, take 216 us in place of 36.
     const bool few = d.rows < 64 * kCUs || d.rows < 64 * d.requests;
     const int per = d.rows / (few ? 32 : 64) / d.requests + 1;
     const dim3 grid((unsigned)(per < 4096 ? per : 4096), (unsigned)d.requests);
@@ -570,7 +573,8 @@ int64_t tiles_of(const LoraDev& d, int f, int r) { return (int64_t)((d.out + f -
 // 256 x 256 tiles (features x rows) where they give every CU a block; 64 x 64 ones where they are few enough
 // for one round of two blocks a CU, or, loaded through registers (where 128 x 128 ones keep too few loads
 // in flight), as long as 128 x 128 ones would not give every CU a block; 128 x 128 ones otherwise. Up to
-// 64 rows W is read straight from memory. Both sides of each rule, with the adapters' first product, in us:
+// 64 rows W is read straight from memory. Both sides of each rule, with the adapters' first product, in us (taken
+// before the requests of a tile were kept apart, which costs 0 to 1 us on these sizes):
 //   32768x2048x2048, rank 64: 256 x 256 tiles 320, 128 x 128 ones 362
 //   8192x1024x1024, rank 16:  128 x 128 tiles 33.3, 256 x 128 ones of eight waves (not built) 34.4
 //   2048x1024x1024, rank 16:  64 x 64 tiles (512) 17.4, 128 x 128 ones 21.5

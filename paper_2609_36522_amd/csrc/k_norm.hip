@@ -9,8 +9,8 @@
 // all rows for each column. A block walks over rows and keeps its columns' two running sums in
 // registers, so dy and x are read once; the blocks' sums go to `part` and a second kernel adds
 // them in a fixed order. Both passes are bound by memory traffic: at 32768x1024 in 16 bits 28 to 33 us
-// forward (4.1 to 4.8 TB/s), 39 us backward (5.2 TB/s, part of x and dy still in the last-level
-// cache) and 4 us for the sums' join. Rows at odd addresses take 4-byte or 2-byte pieces of the same
+// forward (4.1 to 4.8 TB/s), 39 us backward (5.1 TB/s, part of x and dy still in the last-level
+// cache) and 4.6 us for the sums' join. Rows at odd addresses take 4-byte or 2-byte pieces of the same
 // lines: 5003x1333 in 32 bits 15 us forward, 20.7 backward.
 #include "pa_ops_device.h"
 
@@ -440,7 +440,9 @@ hipError_t norm_forward(const NormDev& d, int dtype, int param_dtype, hipStream_
 }
 
 // Blocks of the backward pass: two for each of the 256 CUs, as the registers allow, and no more than
-// there are groups of rows. More blocks cost more partial sums to write and join.
+// there are groups of rows. More blocks cost more partial sums to write and join (512 rows of 4096 in 16 bits: 12.6 MB
+// of data, 16.8 MB of sums). us with 512, 256 and 128 blocks: 32768x1024 40, 41, 71; 8192x1024 18, 17, 23; 5003x1333
+// 24, 27, 44; but 2048x4096 30, 24, 29 and 512x4096 28, 20, 16 (all in 16 bits).
 int norm_backward_blocks(int64_t rows, int64_t cols) {
     const int64_t groups = cols <= 1024 ? (rows + 3) / 4 : rows;
     const int64_t most = 512;

@@ -57,7 +57,7 @@ hipError_t norm_forward(const NormDev& d, int dtype, int param_dtype, hipStream_
 int norm_backward_blocks(int64_t rows, int64_t cols);
 hipError_t norm_backward(const NormDev& d, int dtype, int param_dtype, hipStream_t st);
 
-// How the forward pass (and dq) splits the keys, and dk, dv the rows: see k_cross.hip.
+// How the forward pass (and dq) splits the keys, and dk, dv the rows: see cross_plan (k_cross_bwd.hip).
 void cross_plan(CrossDev& d, bool backward);
 hipError_t cross_forward(const CrossDev& d, int dtype, hipStream_t st);
 hipError_t cross_backward(const CrossDev& d, int dtype, hipStream_t st);
