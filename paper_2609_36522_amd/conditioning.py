@@ -8,7 +8,7 @@ context]), of which the first ``lengths[b]`` belong to sample b's prompt. Each r
 its own low-rank adapters for the four projections.
 
 :meth:`ConditionedBlock.serve` runs a batch whose requests have adapters of their own (no gradients).
-:meth:`ConditionedBlock.__call__` is the same block without adapters, differentiable in its inputs and
+:meth:`ConditionedBlock.__call__` is the same block without adapters, differentiable (once) in its inputs and
 weights: norm and attention and their backward passes run in the library's kernels, the plain projections
 in torch's.
 """

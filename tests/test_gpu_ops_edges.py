@@ -168,3 +168,25 @@ def test_cross_attention_strides_of_any_parity(Lq, Lk, D):
     assert all(t.stride(1) % 2 for t in a[:1])
     _check_cross(*a)
     _check_cross(q, apart(k, 5, 0), apart(v, 6, 0), do, mask=torch.rand((2, Lk), generator=_gen(3), device="cuda") < 0.8)
+
+
+@pytest.mark.parametrize("kind", ["none", "add"])
+@pytest.mark.parametrize("Lk", [77, 700])
+def test_cross_attention_dk_and_dv_without_dq_in_f16(Lk, kind):
+    """Through the C ABI: the rows' statistics then come from a kernel of their own, which scales P as dq's do."""
+    import ctypes as C
+
+    from paper_2609_36522_amd import binding as B
+    q, k, v, do = _cross_case(2, 70, 4, 2, Lk, 64, F16)
+    mask = None if kind == "none" else _randn(_gen(4), 2, Lk)
+    o, stats = ops.cross_attention_forward(q, k, v, mask=mask)
+    p, _, n = ops._cross_args(q, k, v, None, mask, None, o)
+    dk, dv = torch.empty_like(k), torch.empty_like(v)
+    g = ops.CrossGrad(do.stride()[:3], q.stride()[:3], dk.stride()[:3], dv.stride()[:3])
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    fixed = [t.data_ptr() for t in (do, q, k, v, o, stats)]
+    B._check(ops._library().paraanya_cross_attention_backward(C.byref(p), C.byref(g), *fixed, None, dk.data_ptr(), dv.data_ptr(),
+                                                              ws.data_ptr(), n, torch.cuda.current_stream().cuda_stream))
+    ref = R.cross_attention(q, k, v, do, mask=mask)
+    R.check(dk, *ref["dk"], "dk alone")
+    R.check(dv, *ref["dv"], "dv alone")
