@@ -294,7 +294,7 @@ __global__ __launch_bounds__(1024 / NR) void k_lora_down_few(LoraDev d) {
 // `step`-th request from `first`, the first that has rows at r0 or after. Where a request has all of the
 // tiles' rows its product goes on in their accumulators. Otherwise 32 rows that it has a part of are carried on
 // in a copy, of which the lanes of its rows (a lane owns a row) are taken: zeros in t for the others would not
-// do, as 0 times an infinity or a NaN in B is a NaN. It costs nothing where requests are long, and up to a tenth
+// do, as 0 times an infinity or a NaN in B is a NaN. It costs up to 3% where requests are long, and a tenth
 // where each row is one (256 rows of 1024x1024, rank 16: 28 us with zeros in t, 31 so; sums of their own, added
 // by the request's lanes, 30, but 342 in place of 334 for 32768x2048x2048, rank 64).
 template <class T, int NM, int NX, int WIDTH>
