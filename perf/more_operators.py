@@ -231,7 +231,8 @@ def _plain_feed(s):
 
 def _plain_int8(s):
     x = s["x"].float()
-    scale = x.abs().amax(1) / 127
+    largest = x.abs().amax(1)
+    scale = largest / torch.full_like(largest, 127)        # a quotient: by a number, torch multiplies by its reciprocal
     q = torch.round(x / torch.where(scale == 0, 1.0, scale)[:, None]).clamp(-127, 127)
     y = torch.matmul(q, s["wq"].float().t()) * scale[:, None] * s["ws"]
     if s["bias"] is not None:
