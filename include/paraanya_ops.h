@@ -3,7 +3,8 @@
  *
  * The sampler of paraanya.h evaluates a noise network that sees no prompt. These entry points
  * are what a conditioned network needs beside it: layer norm, cross attention to the states of
- * a prompt encoder, and a shared projection with the low-rank adapters of many requests.
+ * a prompt encoder, a shared projection with the low-rank adapters of many requests, group norm with
+ * an activation, a gated feed-forward block, and a projection in 8-bit integers.
  *
  * Conventions (those of paraanya.h, and)
  *   - Every call is stateless: it checks its arguments (nothing is enqueued when it fails),
@@ -154,6 +155,121 @@ PA_API int paraanya_lora_linear(const pa_lora_t* p, const void* x, const void* w
                                 const void* a, const void* b, void* y, void* workspace,
                                 size_t workspace_bytes, void* stream);
 PA_API int paraanya_lora_linear_workspace(const pa_lora_t* p, size_t* bytes);
+
+/* ------------------------------------------------------------------ group norm
+ * y = act((x - mean) rstd * weight + bias) over a channels-last tensor [batch][pixels][channels]: mean
+ * and v = mean (x - mean)^2 are those of a sample's group (channels / groups consecutive channels, all
+ * pixels), rstd = 1 / sqrt(v + eps). */
+#define PA_ACT_NONE 0
+#define PA_ACT_SILU 1          /* z / (1 + e^-z) */
+#define PA_ACT_GELU 2          /* z Phi(z), the normal distribution's */
+
+#define PA_GROUP_MAX_CHANNELS 4096      /* of one group */
+
+typedef struct {
+    int64_t batch;             /* 0 .. 65535 */
+    int64_t pixels;            /* 0 .. 2^30 */
+    int32_t channels;          /* 1 .. 2^20, a multiple of groups */
+    int32_t groups;            /* >= 1 */
+    int32_t dtype;             /* x, y, dy, dx: PA_F32, PA_BF16 or PA_F16 */
+    int32_t param_dtype;       /* weight, bias, dweight, dbias: dtype or PA_F32 */
+    int32_t activation;        /* PA_ACT_* */
+    int32_t pad;
+    double  eps;               /* >= 0, finite */
+    /* Strides of batch and pixel; a pixel's channels are consecutive. Of inputs a batch stride of 0 repeats a
+     * sample. y_stride: of y (forward) or dy (backward). */
+    int64_t x_stride[2], y_stride[2], dx_stride[2];
+} pa_group_norm_t;
+
+/* weight and bias may be NULL (1 and 0). mean and rstd (fp32, [batch][groups]) are written for the backward
+ * pass; both may be NULL. y may be x (same strides). */
+PA_API int paraanya_group_norm(const pa_group_norm_t* p, const void* x, const void* weight, const void* bias, void* y,
+                               float* mean, float* rstd, void* workspace, size_t workspace_bytes, void* stream);
+PA_API int paraanya_group_norm_workspace(const pa_group_norm_t* p, size_t* bytes);
+
+/* Gradients from dy, the forward's x, weight, bias, mean and rstd: with z the activation's argument,
+ * dz = dy act'(z), g = dz weight, xh = (x - mean) rstd: dx = rstd (g - mean(g) - xh mean(g xh)),
+ * dweight = sum of dz xh, dbias = sum of dz over samples and pixels. Any of dx, dweight, dbias may be NULL (not
+ * computed). dx may be dy or x (same strides). No samples or pixels: zeros in dweight and dbias. */
+PA_API int paraanya_group_norm_backward(const pa_group_norm_t* p, const void* dy, const void* x, const void* weight,
+                                        const void* bias, const float* mean, const float* rstd, void* dx, void* dweight,
+                                        void* dbias, void* workspace, size_t workspace_bytes, void* stream);
+PA_API int paraanya_group_norm_backward_workspace(const pa_group_norm_t* p, size_t* bytes);
+
+/* ------------------------------------------------------------------ gated feed-forward block
+ * h = act(x G^T + bg) * (x U^T + bu), y = h D^T + bd: both projections, the activation and the product in one
+ * kernel, the projection back in a second. h is rounded to the element type as the second product's operand; so are,
+ * for the backward pass, the two projections, and the gradients by them as operands of the gradients of x and of the
+ * weights (in fp16 multiplied by a power of two that brings the largest |dy| to 1 .. 2, so that small gradients
+ * keep their digits). */
+typedef struct {
+    int64_t rows;                /* 0 .. 2^30 */
+    int32_t in_features;         /* K: 1 .. 2^20 */
+    int32_t hidden_features;     /* H: 1 .. 2^20 */
+    int32_t out_features;        /* N: 1 .. 2^20 */
+    int32_t dtype;               /* PA_BF16 or PA_F16, of all tensors */
+    int32_t activation;          /* PA_ACT_* */
+    int32_t alignment;           /* bytes that all pointers to x, the weights and dy are multiples of: 2 .. 16. Rows are
+                                    read in place where it is 16 and strides and lengths are multiples of 8, and copied
+                                    into the workspace otherwise (beyond 64 rows). */
+    int64_t x_stride;            /* row strides: >= K */
+    int64_t gate_stride, up_stride;         /* >= K */
+    int64_t down_stride;         /* >= H */
+    int64_t y_stride;            /* of y (forward) or dy (backward), >= N */
+} pa_feed_t;
+
+/* gate and up [H][K], down [N][H]; biases [H], [H] and [N] or NULL. saved: what the backward pass needs (256-byte
+ * aligned, of the size that paraanya_feed_forward_saved reports; the caller keeps it), or NULL. */
+PA_API int paraanya_feed_forward(const pa_feed_t* p, const void* x, const void* gate, const void* gate_bias, const void* up,
+                                 const void* up_bias, const void* down, const void* down_bias, void* y, void* saved,
+                                 size_t saved_bytes, void* workspace, size_t workspace_bytes, void* stream);
+PA_API int paraanya_feed_forward_saved(const pa_feed_t* p, size_t* bytes);
+PA_API int paraanya_feed_forward_workspace(const pa_feed_t* p, int with_saved, size_t* bytes);
+
+/* Gradients, dense, of the element type: dx [rows][K], dgate and dup [H][K], ddown [N][H], dgate_bias and dup_bias
+ * [H], ddown_bias [N]. Any may be NULL (not computed); a bias's gradient comes with its weight's. No rows: zeros
+ * in the weights' and biases' gradients. */
+typedef struct {
+    void *dx, *dgate, *dup, *ddown, *dgate_bias, *dup_bias, *ddown_bias;
+} pa_feed_grad_t;
+
+PA_API int paraanya_feed_forward_backward(const pa_feed_t* p, const pa_feed_grad_t* g, const void* dy, const void* x,
+                                          const void* gate, const void* up, const void* down, const void* saved,
+                                          size_t saved_bytes, void* workspace, size_t workspace_bytes, void* stream);
+PA_API int paraanya_feed_forward_backward_workspace(const pa_feed_t* p, size_t* bytes);
+
+/* ------------------------------------------------------------------ projection in 8-bit integers
+ * Rows to 8 bits: scale[i] = max |x[i]| / 127 in fp32, q = x / scale rounded to the nearest (even) integer. A row of
+ * zeros has scale 0 and q 0; one that holds an infinity or a NaN has scale NaN and q 0, so that its results are NaN.
+ * q's rows are q_stride bytes apart; bytes from cols up to the next multiple of 16 are written as zeros. */
+typedef struct {
+    int64_t rows;                /* 0 .. 2^40 */
+    int64_t cols;                /* 1 .. 2^20 */
+    int32_t dtype;               /* of x: PA_F32, PA_BF16 or PA_F16 */
+    int32_t pad;
+    int64_t x_stride;            /* >= cols */
+    int64_t q_stride;            /* bytes, a multiple of 16, >= cols; q 16-byte aligned */
+} pa_quantize_t;
+
+PA_API int paraanya_quantize_rows(const pa_quantize_t* p, const void* x, int8_t* q, float* scale, void* stream);
+
+/* y = (xq wq^T) x_scale w_scale + bias: 8-bit products summed in 32-bit integers (exact), then one fp32 product with the
+ * row's scale, one with the channel's, and the bias added. xq [rows][K], wq [N][K] with rows of any
+ * multiple of 16 bytes at 16-byte addresses; bytes past K up to the next multiple of 16 are read and have no effect. */
+typedef struct {
+    int64_t rows;                /* 0 .. 2^30 */
+    int32_t in_features;         /* K: 1 .. PA_INT8_MAX_IN */
+    int32_t out_features;        /* N: 1 .. 2^20 */
+    int32_t dtype;               /* of y and bias: PA_BF16 or PA_F16 */
+    int32_t pad;
+    int64_t x_stride, w_stride;  /* bytes, multiples of 16, >= K */
+    int64_t y_stride;            /* >= N */
+} pa_int8_linear_t;
+
+#define PA_INT8_MAX_IN ((1 << 17) - 1)   /* so many products of at most 128 x 128 stay within 32 bits */
+
+PA_API int paraanya_int8_linear(const pa_int8_linear_t* p, const int8_t* xq, const float* x_scale, const int8_t* wq,
+                                const float* w_scale, const void* bias, void* y, void* stream);
 
 #ifdef __cplusplus
 }

@@ -20,7 +20,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libparaanya.so")
 
 SOURCES = ["paraanya.cpp", "paraanya_parareal.cpp", "host_common.cpp", "k_solver.hip", "k_epsnet.hip", "k_parareal.hip",
-           "paraanya_ops.cpp", "k_norm.hip", "k_cross_fwd.hip", "k_cross_bwd.hip", "k_lora.hip"]
+           "paraanya_ops.cpp", "k_norm.hip", "k_cross_fwd.hip", "k_cross_bwd.hip", "k_lora.hip",
+           "paraanya_block_ops.cpp", "k_group.hip", "k_feed.hip", "k_int8.hip"]
 ARCH = "gfx950"
 
 

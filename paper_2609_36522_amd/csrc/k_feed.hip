@@ -1,0 +1,708 @@
+// A gated feed-forward block, forward and backward, for gfx950: h = act(x G^T + bg) (x U^T + bu),
+// y = h D^T + bd.
+//
+// Forward, two launches. A block of the first takes as many features of G as of U, so that a wave has both
+// projections of a value in the same lane, and stores h (and, for the backward pass, the projections).
+// Backward: dh = dy D with the gate's derivative in its epilogue (dz by the gate's projection, du by the other's);
+// dx = dz G + du U as one reduction over both; the weights' gradients dz^T x, du^T x and dy^T h, reductions
+// over the rows, in one launch, which also sums dz, du and dy over the rows (the biases' gradients) from the
+// operands that pass by.
+#include <type_traits>
+
+#include "pa_act.h"
+#include "pa_gemm.h"
+
+namespace pa {
+
+namespace {
+
+constexpr int kCUs = 256;
+
+template <class T> constexpr bool kScaled = std::is_same_v<T, _Float16>;
+
+// fp16: the power of two that brings the largest |dy| to 1 .. 2 (1 where that is zero or no finite number).
+template <class T>
+__device__ __forceinline__ float gradient_scale(const float* largest) {
+    if constexpr (!kScaled<T>) return 1.0f;
+    const f32x4 v = *reinterpret_cast<const f32x4*>(largest + (threadIdx.x & 63) * 4);
+    float m = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
+#pragma unroll
+    for (int i = 32; i >= 1; i >>= 1) m = fmaxf(m, __shfl_xor(m, i));
+    const int e = (int)(__builtin_bit_cast(uint32_t, m) >> 23);
+    return e == 0 || e == 255 ? 1.0f : __builtin_bit_cast(float, (uint32_t)(254 - e) << 23);
+}
+
+// Partial maxima of |dy|; a NaN among them stays out (it is in every gradient anyway).
+template <class T>
+__global__ __launch_bounds__(256) void k_feed_largest(FeedDev d) {
+    __shared__ float red[4];
+    float m = 0.0f;
+    const int pieces = (d.out + 7) / 8;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)d.rows * pieces; i += 256 * kLargest) {
+        const int64_t row = i / pieces;
+        const Pack8<T> p = load8(static_cast<const T*>(d.dy) + row * d.y_stride, (int)(i - row * pieces) * 8, d.out);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf((float)p.v[e]));
+    }
+#pragma unroll
+    for (int i = 32; i >= 1; i >>= 1) m = fmaxf(m, __shfl_xor(m, i));
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x == 0) d.largest[blockIdx.x] = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+}
+
+// Copies of matrices in whole pieces of 16 bytes, zeros past a row's end.
+struct CopyDev {
+    const void* from[5];
+    void* to[5];
+    int64_t stride[5], first[6];     // first: block of a matrix's first pieces
+    int rows[5], cols[5];
+};
+
+template <class T>
+__global__ __launch_bounds__(256) void k_feed_copy(CopyDev d) {
+    int i = 0;
+    while (blockIdx.x >= d.first[i + 1]) ++i;
+    const int pieces = (d.cols[i] + 7) / 8;
+    const int64_t at = (blockIdx.x - d.first[i]) * 256 + threadIdx.x, row = at / pieces;
+    if (row >= d.rows[i]) return;
+    reinterpret_cast<Pack8<T>*>(d.to[i])[at] =
+        load8(static_cast<const T*>(d.from[i]) + row * d.stride[i], (int)(at - row * pieces) * 8, d.cols[i]);
+}
+
+// Eight values from accumulator registers, zeros from feature `n` on, stored where the row exists.
+template <class T>
+__device__ __forceinline__ void store_padded(T* at, Pack8<T> p, int n) {
+    if (n < 8) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e >= n) p.v[e] = (T)0.0f;
+    }
+    *reinterpret_cast<Pack8<T>*>(at) = p;
+}
+
+template <class X>
+__device__ __forceinline__ void clear(typename X::acc_t (&acc)[X::NM][X::NX], float (&sums)[X::NX]) {
+#pragma unroll
+    for (int m = 0; m < X::NM; ++m)
+#pragma unroll
+        for (int j = 0; j < X::NX; ++j) acc[m][j] = typename X::acc_t{};
+#pragma unroll
+    for (int j = 0; j < X::NX; ++j) sums[j] = 0.0f;
+}
+
+// Adds bias[f0 + ..] to NM tiles' registers.
+template <class T, int NM, int NX>
+__device__ __forceinline__ void add_bias(const void* bias, int f0, int n, int half, f32x16 (&acc)[NM][NX], int m0, int m1) {
+    if (!bias) return;
+#pragma unroll
+    for (int m = m0; m < m1; ++m)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int f = f0 + (m - m0) * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
+            const float v = f < n ? (float)static_cast<const T*>(bias)[f] : 0.0f;
+#pragma unroll
+            for (int j = 0; j < NX; ++j) acc[m][j][r] += v;
+        }
+}
+
+// ------------------------------------------------------------------ forward
+template <class X, int ACT>
+__global__ __launch_bounds__(X::THREADS, 2) void k_feed_gate(FeedDev d, GemmJob job) {
+    typedef typename X::T T;
+    __shared__ __align__(16) char lds[X::BYTES];
+    f32x16 acc[X::NM][X::NX];
+    float sums[X::NX];
+    clear<X>(acc, sums);
+    int f, r;
+    tile_of(job, xcd_order(blockIdx.x, gridDim.x), f, r);
+    X::run(job, f * X::OUT, r * X::TR, 0, (job.len + X::PART - 1) / X::PART, lds, acc, sums);
+    const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6;
+    constexpr int HM = X::NM / 2;
+    const int f0 = f * X::OUT + (w % X::WF) * HM * 32, r0 = r * X::TR + (w / X::WF) * X::NX * 32 + (lane & 31);
+    add_bias<T, X::NM, X::NX>(d.gate_bias, f0, d.hidden, half, acc, 0, HM);
+    add_bias<T, X::NM, X::NX>(d.up_bias, f0, d.hidden, half, acc, HM, X::NM);
+#pragma unroll
+    for (int m = 0; m < HM; ++m) {
+#pragma unroll
+        for (int j = 0; j < X::NX; ++j) {
+            f32x16 h;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) h[i] = activate<ACT>(acc[m][j][i]) * acc[m + HM][j][i];
+            const int row = r0 + j * 32;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const int at = f0 + m * 32 + q * 16 + half * 8;
+                const Pack8<T> ph = gather8<T>(h, q, 1.0f), pg = gather8<T>(acc[m][j], q, 1.0f), pu = gather8<T>(acc[m + HM][j], q, 1.0f);
+                if (row >= d.rows || at >= d.hidden_pad) continue;
+                const int64_t to = (int64_t)row * d.hidden_pad + at;
+                store_padded(static_cast<T*>(d.h) + to, ph, d.hidden - at);
+                if (d.g) {
+                    store_padded(static_cast<T*>(d.g) + to, pg, d.hidden - at);
+                    store_padded(static_cast<T*>(d.u) + to, pu, d.hidden - at);
+                }
+            }
+        }
+    }
+}
+
+// out = R F^T + bias, or its partial sums over ranges of the reduction: [split][rows][feature_pad] in `part`.
+struct PlainDev {
+    const void* bias;
+    void* out;
+    int64_t out_stride;
+    float* part;
+    const float* largest;            // not null: divided by its scale
+    int splits, feature_pad;
+};
+
+template <class X>
+__global__ __launch_bounds__(X::THREADS, 2) void k_feed_plain(PlainDev d, GemmJob job) {
+    typedef typename X::T T;
+    __shared__ __align__(16) char lds[X::BYTES];
+    f32x16 acc[X::NM][X::NX];
+    float sums[X::NX];
+    clear<X>(acc, sums);
+    const int tiles = job.f_tiles * job.r_tiles, id = xcd_order(blockIdx.x, gridDim.x), split = id / tiles;
+    int f, r;
+    tile_of(job, id - split * tiles, f, r);
+    const int parts = (job.len + X::PART - 1) / X::PART * (job.f[1] ? 2 : 1);
+    X::run(job, f * X::TF, r * X::TR, (int)((int64_t)parts * split / d.splits), (int)((int64_t)parts * (split + 1) / d.splits), lds, acc, sums);
+    const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6;
+    const int f0 = f * X::TF + (w % X::WF) * X::NM * 32, r0 = r * X::TR + (w / X::WF) * X::NX * 32 + (lane & 31);
+    if (d.splits == 1) {
+        const float s = d.largest ? 1.0f / gradient_scale<T>(d.largest) : 1.0f;
+        add_bias<T, X::NM, X::NX>(d.bias, f0, job.features, half, acc, 0, X::NM);
+#pragma unroll
+        for (int m = 0; m < X::NM; ++m)
+#pragma unroll
+            for (int j = 0; j < X::NX; ++j)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const int at = f0 + m * 32 + q * 16 + half * 8, row = r0 + j * 32;
+                    const Pack8<T> p = gather8<T>(acc[m][j], q, s);
+                    if (row < job.rows) store8(static_cast<T*>(d.out) + (int64_t)row * d.out_stride + at, p, job.features - at);
+                }
+    } else {
+#pragma unroll
+        for (int m = 0; m < X::NM; ++m)
+#pragma unroll
+            for (int j = 0; j < X::NX; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int at = f0 + m * 32 + q * 8 + half * 4, row = r0 + j * 32;
+                    const f32x4 v = {acc[m][j][4 * q], acc[m][j][4 * q + 1], acc[m][j][4 * q + 2], acc[m][j][4 * q + 3]};
+                    if (row < job.rows && at < d.feature_pad)
+                        *reinterpret_cast<f32x4*>(d.part + ((int64_t)split * job.rows + row) * d.feature_pad + at) = v;
+                }
+    }
+}
+
+// Partial sums joined in order, eight features a thread.
+template <class T>
+__global__ __launch_bounds__(256) void k_feed_join(PlainDev d, int rows, int features) {
+    const int pieces = d.feature_pad / 8;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / pieces;
+    const int at = (int)(i - row * pieces) * 8;
+    if (row >= rows) return;
+    float v[8] = {};
+#pragma unroll 4
+    for (int s = 0; s < d.splits; ++s) {
+        const float* p = d.part + ((int64_t)s * rows + row) * d.feature_pad + at;
+        const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] += a[e];
+            v[4 + e] += b[e];
+        }
+    }
+    const float s = d.largest ? 1.0f / gradient_scale<T>(d.largest) : 1.0f;
+    Pack8<T> o;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        o.v[e] = (T)(v[e] * s + (d.bias && at + e < features ? (float)static_cast<const T*>(d.bias)[at + e] : 0.0f));
+    store8(static_cast<T*>(d.out) + row * d.out_stride + at, o, features - at);
+}
+
+// ------------------------------------------------------------------ few rows
+// 16 features a block, up to 16 NR rows: the weights are read once, straight into operand registers; 16
+// waves take pieces of 32 U elements of the reduction in turn and are joined through LDS in a fixed order.
+template <class T, int U, int NR, int NW, int WIDTH>
+__device__ __forceinline__ void few_rows(const T* const (&wp)[NW], bool f_valid, const T* x, int64_t x_stride, int rows, int len,
+                                         float (*part)[NW][NR][4][64], f32x4 (&out)[NW]) {
+    typedef typename Vec<T>::v8 v8;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    f32x4 acc[NW][NR];
+#pragma unroll
+    for (int n = 0; n < NW; ++n)
+#pragma unroll
+        for (int j = 0; j < NR; ++j) acc[n][j] = f32x4{};
+    for (int k0 = w * 32 * U; k0 < len; k0 += 16 * 32 * U) {
+        v8 wv[NW][U], xv[NR][U];
+#pragma unroll
+        for (int s = 0; s < U; ++s) {
+            const int k = k0 + s * 32 + (lane >> 4) * 8;
+#pragma unroll
+            for (int n = 0; n < NW; ++n) wv[n][s] = operand<T, WIDTH>(wp[n], k, len, f_valid);
+#pragma unroll
+            for (int j = 0; j < NR; ++j) {
+                const int row = j * 16 + (lane & 15);
+                xv[j][s] = operand<T, WIDTH>(x + (row < rows ? row : 0) * x_stride, k, len, row < rows);
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < U; ++s) {
+            const int k = k0 + s * 32 + (lane >> 4) * 8;
+#pragma unroll
+            for (int j = 0; j < NR; ++j) {
+                const v8 b = fixed<T, WIDTH>(xv[j][s], k, len, j * 16 + (lane & 15) < rows);
+#pragma unroll
+                for (int n = 0; n < NW; ++n) acc[n][j] = mma16(fixed<T, WIDTH>(wv[n][s], k, len, f_valid), b, acc[n][j]);
+            }
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NW; ++n)
+#pragma unroll
+        for (int j = 0; j < NR; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) part[w][n][j][r][lane] = acc[n][j][r];
+    __syncthreads();
+    // Wave w < 4 NR sums register w % 4 of row group w / 4.
+#pragma unroll
+    for (int n = 0; n < NW; ++n) out[n] = f32x4{};
+    if (w < 4 * NR) {
+#pragma unroll
+        for (int n = 0; n < NW; ++n) {
+            float v = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v += part[i][n][w >> 2][w & 3][lane];
+            out[n][0] = v;
+        }
+    }
+}
+
+template <class T, int ACT, int NR, int WIDTH>
+__global__ __launch_bounds__(1024) void k_feed_few_gate(FeedDev d) {
+    __shared__ float part[16][2][NR][4][64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, f0 = blockIdx.x * 16, f = f0 + (lane & 15);
+    const bool valid = f < d.hidden;
+    const T* const wp[2] = {static_cast<const T*>(d.gate) + (valid ? f : 0) * d.gate_stride, static_cast<const T*>(d.up) + (valid ? f : 0) * d.up_stride};
+    f32x4 v[2];
+    few_rows<T, 2, NR, 2, WIDTH>(wp, valid, static_cast<const T*>(d.x), d.x_stride, d.rows, d.in, part, v);
+    const int row = (w >> 2) * 16 + (lane & 15), o = f0 + 4 * (lane >> 4) + (w & 3);
+    if (w >= 4 * NR || row >= d.rows || o >= d.hidden_pad) return;
+    const bool in = o < d.hidden;
+    const float g = v[0][0] + (in && d.gate_bias ? (float)static_cast<const T*>(d.gate_bias)[o] : 0.0f);
+    const float u = v[1][0] + (in && d.up_bias ? (float)static_cast<const T*>(d.up_bias)[o] : 0.0f);
+    const int64_t to = (int64_t)row * d.hidden_pad + o;
+    static_cast<T*>(d.h)[to] = (T)(in ? activate<ACT>(g) * u : 0.0f);
+    if (d.g) {
+        static_cast<T*>(d.g)[to] = (T)(in ? g : 0.0f);
+        static_cast<T*>(d.u)[to] = (T)(in ? u : 0.0f);
+    }
+}
+
+template <class T, int NR, int WIDTH>
+__global__ __launch_bounds__(1024) void k_feed_few_down(FeedDev d) {
+    __shared__ float part[16][1][NR][4][64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, f0 = blockIdx.x * 16, f = f0 + (lane & 15);
+    const bool valid = f < d.out;
+    const T* const wp[1] = {static_cast<const T*>(d.down) + (valid ? f : 0) * d.down_stride};
+    f32x4 v[1];
+    few_rows<T, 4, NR, 1, WIDTH>(wp, valid, static_cast<const T*>(d.h), d.hidden_pad, d.rows, d.hidden, part, v);
+    const int row = (w >> 2) * 16 + (lane & 15), o = f0 + 4 * (lane >> 4) + (w & 3);
+    if (w >= 4 * NR || row >= d.rows || o >= d.out) return;
+    static_cast<T*>(d.y)[(int64_t)row * d.y_stride + o] = (T)(v[0][0] + (d.down_bias ? (float)static_cast<const T*>(d.down_bias)[o] : 0.0f));
+}
+
+// ------------------------------------------------------------------ backward
+// dh = dy D, then dz = dh u act'(g) and du = dh act(g) of the saved projections.
+template <class X, int ACT>
+__global__ __launch_bounds__(X::THREADS, 2) void k_feed_grad(FeedDev d, GemmJob job) {
+    typedef typename X::T T;
+    typedef T t4 __attribute__((ext_vector_type(4)));
+    __shared__ __align__(16) char lds[X::BYTES];
+    f32x16 acc[X::NM][X::NX];
+    float sums[X::NX];
+    clear<X>(acc, sums);
+    int f, r;
+    tile_of(job, xcd_order(blockIdx.x, gridDim.x), f, r);
+    const float scale = gradient_scale<T>(d.largest);
+    X::run(job, f * X::TF, r * X::TR, 0, (job.len + X::PART - 1) / X::PART, lds, acc, sums);
+    const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6;
+    const int f0 = f * X::TF + (w % X::WF) * X::NM * 32, r0 = r * X::TR + (w / X::WF) * X::NX * 32 + (lane & 31);
+#pragma unroll
+    for (int m = 0; m < X::NM; ++m) {
+#pragma unroll
+        for (int j = 0; j < X::NX; ++j) {
+            const int row = r0 + j * 32;
+            const int64_t base = (int64_t)(row < d.rows ? row : 0) * d.hidden_pad;
+            f32x16 du;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int at = f0 + m * 32 + q * 8 + half * 4;
+                t4 g = {}, u = {};
+                if (row < d.rows && at < d.hidden_pad) {
+                    g = *reinterpret_cast<const t4*>(static_cast<const T*>(d.g) + base + at);
+                    u = *reinterpret_cast<const t4*>(static_cast<const T*>(d.u) + base + at);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float2 a = activate_grad<ACT>((float)g[e]);
+                    const float dh = acc[m][j][4 * q + e] * scale;
+                    du[4 * q + e] = dh * a.x;
+                    acc[m][j][4 * q + e] = dh * (float)u[e] * a.y;
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const int at = f0 + m * 32 + q * 16 + half * 8;
+                const Pack8<T> pz = gather8<T>(acc[m][j], q, 1.0f), pu = gather8<T>(du, q, 1.0f);
+                if (row >= d.rows || at >= d.hidden_pad) continue;
+                store_padded(static_cast<T*>(d.dz) + base + at, pz, d.hidden - at);
+                store_padded(static_cast<T*>(d.du) + base + at, pu, d.hidden - at);
+            }
+        }
+    }
+}
+
+// The weights' gradients, up to three products in one launch; a split takes a range of the rows.
+struct WeightsDev {
+    GemmJob job[3];
+    void *out[3], *bias[3];          // [rows][features], [rows] (sums over the reduction of R; may be null)
+    const float* largest[3];
+    int64_t part[3];                 // splits > 1: offset of the job's partial sums, [split][rows][feature_pad + 1 piece for the bias]
+    int first[4];
+    int jobs, splits;
+    float* parts;
+};
+
+__device__ __host__ __forceinline__ int padded(int n) { return (n + 7) / 8 * 8; }
+
+template <class X>
+__global__ __launch_bounds__(X::THREADS, 2) void k_feed_weights(WeightsDev d) {
+    typedef typename X::T T;
+    __shared__ __align__(16) char lds[X::BYTES];
+    f32x16 acc[X::NM][X::NX];
+    float sums[X::NX];
+    clear<X>(acc, sums);
+    const int total = d.first[d.jobs], id = xcd_order(blockIdx.x, gridDim.x), split = id / total, tile = id - split * total;
+    int n = 0;
+    while (n + 1 < d.jobs && tile >= d.first[n + 1]) ++n;
+    const GemmJob& job = d.job[n];
+    int f, r;
+    tile_of(job, tile - d.first[n], f, r);
+    const int parts = (job.len + X::PART - 1) / X::PART;
+    X::run(job, f * X::TF, r * X::TR, (int)((int64_t)parts * split / d.splits), (int)((int64_t)parts * (split + 1) / d.splits), lds, acc, sums);
+    const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6;
+    const int f0 = f * X::TF + (w % X::WF) * X::NM * 32, r0 = r * X::TR + (w / X::WF) * X::NX * 32 + (lane & 31);
+    const bool has_sums = d.bias[n] && f == 0 && w % X::WF == 0;
+    if (d.splits == 1) {
+        const float s = d.largest[n] ? 1.0f / gradient_scale<T>(d.largest[n]) : 1.0f;
+#pragma unroll
+        for (int j = 0; j < X::NX; ++j) {
+            const int row = r0 + j * 32;
+            const float sum = sums[j] + __shfl_xor(sums[j], 32);
+            if (has_sums && half == 0 && row < job.rows) static_cast<T*>(d.bias[n])[row] = (T)(sum * s);
+#pragma unroll
+            for (int m = 0; m < X::NM; ++m)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const int at = f0 + m * 32 + q * 16 + half * 8;
+                    const Pack8<T> p = gather8<T>(acc[m][j], q, s);
+                    if (row < job.rows) store8(static_cast<T*>(d.out[n]) + (int64_t)row * job.features + at, p, job.features - at);
+                }
+        }
+    } else {
+        const int pad = padded(job.features) + 8;
+        float* out = d.parts + d.part[n] + (int64_t)split * job.rows * pad;
+#pragma unroll
+        for (int j = 0; j < X::NX; ++j) {
+            const int row = r0 + j * 32;
+            const float sum = sums[j] + __shfl_xor(sums[j], 32);
+            if (has_sums && half == 0 && row < job.rows) out[(int64_t)row * pad + pad - 8] = sum;
+#pragma unroll
+            for (int m = 0; m < X::NM; ++m)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int at = f0 + m * 32 + q * 8 + half * 4;
+                    const f32x4 v = {acc[m][j][4 * q], acc[m][j][4 * q + 1], acc[m][j][4 * q + 2], acc[m][j][4 * q + 3]};
+                    if (row < job.rows && at < pad - 8) *reinterpret_cast<f32x4*>(out + (int64_t)row * pad + at) = v;
+                }
+        }
+    }
+}
+
+// Their partial sums joined in order, eight features a thread; a row's last piece holds its bias's.
+template <class T>
+__global__ __launch_bounds__(256) void k_feed_weights_join(WeightsDev d) {
+    const int n = blockIdx.y;
+    const int rows = d.job[n].rows, features = d.job[n].features, pad = padded(features) + 8, pieces = pad / 8;
+    const float s = d.largest[n] ? 1.0f / gradient_scale<T>(d.largest[n]) : 1.0f;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)rows * pieces; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / pieces;
+        const int at = (int)(i - row * pieces) * 8;
+        if (at == pad - 8) {
+            if (!d.bias[n]) continue;
+            float v = 0.0f;
+            for (int k = 0; k < d.splits; ++k) v += d.parts[d.part[n] + ((int64_t)k * rows + row) * pad + at];
+            static_cast<T*>(d.bias[n])[row] = (T)(v * s);
+            continue;
+        }
+        float v[8] = {};
+#pragma unroll 4
+        for (int k = 0; k < d.splits; ++k) {
+            const float* p = d.parts + d.part[n] + ((int64_t)k * rows + row) * pad + at;
+            const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] += a[e];
+                v[4 + e] += b[e];
+            }
+        }
+        Pack8<T> o;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o.v[e] = (T)(v[e] * s);
+        store8(static_cast<T*>(d.out[n]) + row * features + at, o, features - at);
+    }
+}
+
+// No rows: the gradients of weights and biases are zero.
+template <class T>
+__global__ __launch_bounds__(256) void k_feed_zero(T* p, int64_t n) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = (T)0.0f;
+}
+
+// ------------------------------------------------------------------ launches
+int64_t up_to(int64_t n, int64_t d) { return (n + d - 1) / d; }
+
+#define FEED_TRY(call)                      \
+    do {                                    \
+        const hipError_t e_ = (call);       \
+        if (e_ != hipSuccess) return e_;    \
+    } while (0)
+
+// Tiles of F x R places that cover a job, and whether they give every CU a block.
+template <class X>
+bool tiled(GemmJob& job, int features, int blocks_wanted) {
+    job.f_tiles = (int)up_to(features, X::OUT);
+    job.r_tiles = (int)up_to(job.rows, X::TR);
+    return (int64_t)job.f_tiles * job.r_tiles >= blocks_wanted;
+}
+
+template <class T, bool FCOL, bool RCOL, bool SUMS> using Big = Tile<T, 2, 4, 4, 2, 2, FCOL, RCOL, false, SUMS>;
+template <class T, bool FCOL, bool RCOL, bool SUMS> using Mid = Tile<T, 2, 2, 2, 2, 2, FCOL, RCOL, false, SUMS>;
+template <class T, bool FCOL, bool RCOL, bool SUMS> using Small = Tile<T, 2, 2, 1, 1, 4, FCOL, RCOL, false, SUMS>;
+template <class T> using BigGate = Tile<T, 2, 4, 4, 2, 2, false, false, true>;
+template <class T> using MidGate = Tile<T, 2, 2, 2, 2, 2, false, false, true>;
+template <class T> using SmallGate = Tile<T, 1, 4, 2, 1, 3, false, false, true>;
+
+template <class T, int ACT>
+hipError_t gate(const FeedDev& d, GemmJob job, hipStream_t st) {
+    auto go = [&](auto x) {
+        typedef decltype(x) X;
+        k_feed_gate<X, ACT><<<(unsigned)((int64_t)job.f_tiles * job.r_tiles), X::THREADS, 0, st>>>(d, job);
+        return hipGetLastError();
+    };
+    if (tiled<BigGate<T>>(job, d.hidden, kCUs)) return go(BigGate<T>{});
+    if (tiled<MidGate<T>>(job, d.hidden, kCUs)) return go(MidGate<T>{});
+    tiled<SmallGate<T>>(job, d.hidden, 0);
+    return go(SmallGate<T>{});
+}
+
+template <class T, bool FCOL>
+hipError_t plain(PlainDev p, GemmJob job, hipStream_t st) {
+    auto go = [&](auto x) {
+        typedef decltype(x) X;
+        k_feed_plain<X><<<(unsigned)((int64_t)job.f_tiles * job.r_tiles * p.splits), X::THREADS, 0, st>>>(p, job);
+        return hipGetLastError();
+    };
+    if (tiled<Big<T, FCOL, false, false>>(job, job.features, kCUs)) return go(Big<T, FCOL, false, false>{});
+    if (tiled<Mid<T, FCOL, false, false>>(job, job.features, kCUs)) return go(Mid<T, FCOL, false, false>{});
+    tiled<Small<T, FCOL, false, false>>(job, job.features, 0);
+    FEED_TRY(go(Small<T, FCOL, false, false>{}));
+    if (p.splits > 1) {
+        k_feed_join<T><<<(unsigned)up_to((int64_t)job.rows * (p.feature_pad / 8), 256), 256, 0, st>>>(p, job.rows, job.features);
+        return hipGetLastError();
+    }
+    return hipSuccess;
+}
+
+template <class T, int ACT>
+hipError_t grad(const FeedDev& d, GemmJob job, hipStream_t st) {
+    auto go = [&](auto x) {
+        typedef decltype(x) X;
+        k_feed_grad<X, ACT><<<(unsigned)((int64_t)job.f_tiles * job.r_tiles), X::THREADS, 0, st>>>(d, job);
+        return hipGetLastError();
+    };
+    if (tiled<Big<T, true, false, false>>(job, job.features, kCUs)) return go(Big<T, true, false, false>{});
+    if (tiled<Mid<T, true, false, false>>(job, job.features, kCUs)) return go(Mid<T, true, false, false>{});
+    tiled<Small<T, true, false, false>>(job, job.features, 0);
+    return go(Small<T, true, false, false>{});
+}
+
+template <class T>
+hipError_t weights(WeightsDev w, hipStream_t st) {
+    auto count = [&](auto x) {
+        typedef decltype(x) X;
+        w.first[0] = 0;
+        for (int n = 0; n < w.jobs; ++n) {
+            tiled<X>(w.job[n], w.job[n].features, 0);
+            w.first[n + 1] = w.first[n] + w.job[n].f_tiles * w.job[n].r_tiles;
+        }
+        return w.first[w.jobs];
+    };
+    auto go = [&](auto x) {
+        typedef decltype(x) X;
+        k_feed_weights<X><<<(unsigned)(count(x) * w.splits), X::THREADS, 0, st>>>(w);
+        return hipGetLastError();
+    };
+    if (count(Big<T, true, true, true>{}) * w.splits >= 192) FEED_TRY(go(Big<T, true, true, true>{}));
+    else FEED_TRY(go(Mid<T, true, true, true>{}));
+    if (w.splits > 1) {
+        k_feed_weights_join<T><<<dim3(1024, (unsigned)w.jobs), 256, 0, st>>>(w);
+        return hipGetLastError();
+    }
+    return hipSuccess;
+}
+
+// Copies of what cannot be read in whole pieces; `use` becomes the copy with its stride.
+struct Copies {
+    CopyDev d{};
+    int n = 0;
+    const void* use(const void* from, void* pad, int64_t rows, int cols, int64_t& stride) {
+        if (!pad) return from;
+        d.from[n] = from;
+        d.to[n] = pad;
+        d.stride[n] = stride;
+        d.rows[n] = (int)rows;
+        d.cols[n] = cols;
+        d.first[n + 1] = d.first[n] + up_to(rows * (padded(cols) / 8), 256);
+        ++n;
+        stride = padded(cols);
+        return pad;
+    }
+    template <class T>
+    hipError_t run(hipStream_t st) const {
+        if (n == 0) return hipSuccess;
+        k_feed_copy<T><<<(unsigned)d.first[n], 256, 0, st>>>(d);
+        return hipGetLastError();
+    }
+};
+
+template <class T, int ACT, int WIDTH>
+hipError_t forward_few(const FeedDev& d, hipStream_t st) {
+    const unsigned hb = (unsigned)(d.hidden_pad + 15) / 16, ob = (unsigned)(d.out + 15) / 16;
+    auto go = [&](auto nr) {
+        constexpr int NR = decltype(nr)::value;
+        k_feed_few_gate<T, ACT, NR, WIDTH><<<hb, 1024, 0, st>>>(d);
+        FEED_TRY(hipGetLastError());
+        k_feed_few_down<T, NR, WIDTH><<<ob, 1024, 0, st>>>(d);
+        return hipGetLastError();
+    };
+    if (d.rows <= 16) return go(std::integral_constant<int, 1>{});
+    if (d.rows <= 32) return go(std::integral_constant<int, 2>{});
+    return go(std::integral_constant<int, 4>{});
+}
+
+template <class T, int ACT>
+hipError_t forward(const FeedDev& d, hipStream_t st) {
+    if (feed_few(d.rows)) {
+        const int64_t odd = (int64_t)d.in | d.hidden | d.x_stride | d.gate_stride | d.up_stride | d.down_stride;
+        const uintptr_t at = reinterpret_cast<uintptr_t>(d.x) | reinterpret_cast<uintptr_t>(d.gate) | reinterpret_cast<uintptr_t>(d.up) |
+                             reinterpret_cast<uintptr_t>(d.down);
+        if (d.in < 8 || d.hidden < 8) return forward_few<T, ACT, kTiny>(d, st);
+        return odd % 8 == 0 && at % 16 == 0 ? forward_few<T, ACT, kWhole>(d, st) : forward_few<T, ACT, kRagged>(d, st);
+    }
+    Copies c;
+    int64_t xs = d.x_stride, gs = d.gate_stride, us = d.up_stride, ds = d.down_stride;
+    const void* x = c.use(d.x, d.x_pad, d.rows, d.in, xs);
+    const void* g = c.use(d.gate, d.gate_pad, d.hidden, d.in, gs);
+    const void* u = c.use(d.up, d.up_pad, d.hidden, d.in, us);
+    const void* dn = c.use(d.down, d.down_pad, d.out, d.hidden, ds);
+    FEED_TRY(c.run<T>(st));
+    FEED_TRY((gate<T, ACT>(d, GemmJob{{g, u}, {x, nullptr}, gs, xs, d.hidden, d.rows, d.in, 0, 0}, st)));
+    const PlainDev p{d.down_bias, d.y, d.y_stride, nullptr, nullptr, 1, 0};
+    return plain<T, false>(p, GemmJob{{dn, nullptr}, {d.h, nullptr}, ds, d.hidden_pad, d.out, d.rows, d.hidden, 0, 0}, st);
+}
+
+template <class T>
+hipError_t zero(void* p, int64_t n, hipStream_t st) {
+    if (!p) return hipSuccess;
+    const int64_t blocks = up_to(n, 1024);
+    k_feed_zero<T><<<(unsigned)(blocks < 4096 ? blocks : 4096), 256, 0, st>>>(static_cast<T*>(p), n);
+    return hipGetLastError();
+}
+
+template <class T, int ACT>
+hipError_t backward(const FeedDev& d, hipStream_t st) {
+    if (d.rows == 0) {
+        const int64_t HK = (int64_t)d.hidden * d.in, NH = (int64_t)d.out * d.hidden;
+        FEED_TRY(zero<T>(d.dgate, HK, st));
+        FEED_TRY(zero<T>(d.dup, HK, st));
+        FEED_TRY(zero<T>(d.ddown, NH, st));
+        FEED_TRY(zero<T>(d.dgate_bias, d.hidden, st));
+        FEED_TRY(zero<T>(d.dup_bias, d.hidden, st));
+        return zero<T>(d.ddown_bias, d.out, st);
+    }
+    Copies c;
+    int64_t xs = d.x_stride, gs = d.gate_stride, us = d.up_stride, ds = d.down_stride, ys = d.y_stride;
+    const void* x = c.use(d.x, d.x_pad, d.rows, d.in, xs);
+    const void* g = c.use(d.gate, d.gate_pad, d.hidden, d.in, gs);
+    const void* u = c.use(d.up, d.up_pad, d.hidden, d.in, us);
+    const void* dn = c.use(d.down, d.down_pad, d.out, d.hidden, ds);
+    const void* dy = c.use(d.dy, d.dy_pad, d.rows, d.out, ys);
+    FEED_TRY(c.run<T>(st));
+    const bool through = d.dx || d.dgate || d.dup;
+    if (through) {
+        if (kScaled<T>) {
+            k_feed_largest<T><<<kLargest, 256, 0, st>>>(d);
+            FEED_TRY(hipGetLastError());
+        }
+        FEED_TRY((grad<T, ACT>(d, GemmJob{{dn, nullptr}, {dy, nullptr}, ds, ys, d.hidden, d.rows, d.out, 0, 0}, st)));
+    }
+    const float* largest = kScaled<T> ? d.largest : nullptr;
+    if (d.dx) {
+        const PlainDev p{nullptr, d.dx, d.in, nullptr, largest, 1, 0};
+        FEED_TRY((plain<T, true>(p, GemmJob{{g, u}, {d.dz, d.du}, gs, d.hidden_pad, d.in, d.rows, d.hidden, 0, 0}, st)));
+    }
+    WeightsDev w{};
+    auto add = [&](const void* f, int64_t fs, const void* r, int64_t rs, int rows, int features, void* out, void* bias, const float* l) {
+        if (!out) return;
+        w.job[w.jobs] = GemmJob{{f, nullptr}, {r, nullptr}, fs, rs, features, rows, d.rows, 0, 0};
+        w.out[w.jobs] = out;
+        w.bias[w.jobs] = bias;
+        w.largest[w.jobs++] = l;
+    };
+    add(x, xs, d.dz, d.hidden_pad, d.hidden, d.in, d.dgate, d.dgate_bias, largest);
+    add(x, xs, d.du, d.hidden_pad, d.hidden, d.in, d.dup, d.dup_bias, largest);
+    add(d.h, d.hidden_pad, dy, ys, d.out, d.hidden, d.ddown, d.ddown_bias, nullptr);
+    if (w.jobs == 0) return hipSuccess;
+    w.splits = 1;
+    return weights<T>(w, st);
+}
+
+template <class F>
+hipError_t dispatch(int dtype, int act, F f) {
+    auto typed = [&](auto t) {
+        if (act == PA_ACT_SILU) return f(t, std::integral_constant<int, PA_ACT_SILU>{});
+        if (act == PA_ACT_GELU) return f(t, std::integral_constant<int, PA_ACT_GELU>{});
+        return f(t, std::integral_constant<int, PA_ACT_NONE>{});
+    };
+    return dtype == PA_BF16 ? typed((__bf16)0) : typed((_Float16)0);
+}
+
+}  // namespace
+
+bool feed_few(int64_t rows) { return rows <= 64; }
+
+hipError_t feed_forward(const FeedDev& d, int dtype, int act, hipStream_t st) {
+    return dispatch(dtype, act, [&](auto t, auto a) { return forward<decltype(t), decltype(a)::value>(d, st); });
+}
+
+hipError_t feed_backward(const FeedDev& d, int dtype, int act, hipStream_t st) {
+    return dispatch(dtype, act, [&](auto t, auto a) { return backward<decltype(t), decltype(a)::value>(d, st); });
+}
+
+}  // namespace pa

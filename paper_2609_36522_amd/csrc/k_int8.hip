@@ -1,0 +1,258 @@
+// Projection in 8-bit integers, for gfx950: rows to 8 bits with a scale each, and
+// y = (xq wq^T) x_scale w_scale + bias with the product in 32-bit integers (v_mfma_i32_32x32x32_i8, twice the
+// 16-bit rate).
+#include <type_traits>
+
+#include "pa_gemm.h"
+
+namespace pa {
+
+namespace {
+
+constexpr int kCUs = 256;
+
+// ------------------------------------------------------------------ rows to 8 bits
+// A row's magnitudes are compared as their bit patterns, in which NaN is larger than infinity and that than any
+// number.
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+#pragma unroll
+    for (int i = 32; i >= 1; i >>= 1) {
+        const uint32_t o = __shfl_xor((int)v, i);
+        v = o > v ? o : v;
+    }
+    return v;
+}
+
+template <int WPR>
+__device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t* lds) {
+    v = wave_max_u32(v);
+    if constexpr (WPR == 1) return v;
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    const uint32_t a = lds[0] > lds[1] ? lds[0] : lds[1], b = lds[2] > lds[3] ? lds[2] : lds[3];
+    return a > b ? a : b;
+}
+
+template <class T>
+__device__ __forceinline__ uint32_t largest8(const Pack8<T>& p, uint32_t m) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t b = __builtin_bit_cast(uint32_t, (float)p.v[i]) & 0x7fffffffu;
+        m = b > m ? b : m;
+    }
+    return m;
+}
+
+__device__ __forceinline__ float scale_of(uint32_t m) {
+    return m >= 0x7f800000u ? __builtin_nanf("") : __builtin_bit_cast(float, m) / 127.0f;
+}
+
+// The division is fp32's own (rounded once), so that q is the nearest integer to the fp32 quotient.
+template <class T>
+__device__ __forceinline__ uint2 quantize8(const Pack8<T>& p, float scale) {
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float r = rintf((float)p.v[i] / scale);
+        r = fminf(fmaxf(r, -127.0f), 127.0f);
+        w[i >> 2] |= ((uint32_t)(int)r & 255u) << (8 * (i & 3));
+    }
+    return scale > 0.0f ? make_uint2(w[0], w[1]) : make_uint2(0, 0);    // 0 and NaN: all zero
+}
+
+// WPR (1 or 4) waves per row, CH pieces of 8 columns per thread; CH = 0: rows of any length, read twice.
+template <class T, int WPR, int CH>
+__global__ __launch_bounds__(256) void k_quantize(QuantizeDev d, int64_t row0) {
+    constexpr int TPR = 64 * WPR, RPB = 4 / WPR;
+    __shared__ uint32_t red[4];
+    const int t = threadIdx.x % TPR;
+    const int64_t row = row0 + (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+    if (row >= d.rows) return;               // whole waves (WPR = 1) or none
+    const int N = d.cols, end = (N + 15) / 16 * 16;
+    const T* x = static_cast<const T*>(d.x) + row * d.x_stride;
+    int8_t* q = d.q + row * d.q_stride;
+    uint32_t m = 0;
+    if constexpr (CH > 0) {
+        Pack8<T> p[CH];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) p[c] = load8(x, (c * TPR + t) * 8, N);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) m = largest8(p[c], m);
+        const float s = scale_of(row_max<WPR>(m, red));
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = (c * TPR + t) * 8;
+            if (col < end) *reinterpret_cast<uint2*>(q + col) = quantize8(p[c], s);
+        }
+        if (t == 0) d.scale[row] = s;
+    } else {
+        for (int col = t * 8; col < N; col += TPR * 8) m = largest8(load8(x, col, N), m);
+        const float s = scale_of(row_max<WPR>(m, red));
+        for (int col = t * 8; col < end; col += TPR * 8) *reinterpret_cast<uint2*>(q + col) = quantize8(load8(x, col, N), s);
+        if (t == 0) d.scale[row] = s;
+    }
+}
+
+// ------------------------------------------------------------------ products
+// v x_scale w_scale + bias.
+template <class T>
+__device__ __forceinline__ float scaled(const Int8Dev& d, int v, float xs, int f) {
+    float r = (float)v * xs * d.w_scale[f];
+    if (d.bias) r += (float)static_cast<const T*>(d.bias)[f];
+    return r;
+}
+
+template <class X, class T>
+__global__ __launch_bounds__(X::THREADS, 2) void k_int8_tile(Int8Dev d, GemmJob job) {
+    __shared__ __align__(16) char lds[X::BYTES];
+    i32x16 acc[X::NM][X::NX];
+    float none[X::NX];
+#pragma unroll
+    for (int m = 0; m < X::NM; ++m)
+#pragma unroll
+        for (int j = 0; j < X::NX; ++j) acc[m][j] = i32x16{};
+    int f, r;
+    tile_of(job, xcd_order(blockIdx.x, gridDim.x), f, r);
+    X::run(job, f * X::TF, r * X::TR, 0, (job.len + X::PART - 1) / X::PART, lds, acc, none);
+    const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6;
+    const int f0 = f * X::TF + (w % X::WF) * X::NM * 32, r0 = r * X::TR + (w / X::WF) * X::NX * 32 + (lane & 31);
+    float xs[X::NX];
+#pragma unroll
+    for (int j = 0; j < X::NX; ++j) xs[j] = r0 + j * 32 < d.rows ? d.x_scale[r0 + j * 32] : 0.0f;
+#pragma unroll
+    for (int m = 0; m < X::NM; ++m) {
+        float ws[16], bias[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int at = f0 + m * 32 + 8 * (i >> 2) + 4 * half + (i & 3), c = at < d.out ? at : d.out - 1;
+            ws[i] = d.w_scale[c];
+            bias[i] = d.bias ? (float)static_cast<const T*>(d.bias)[c] : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < X::NX; ++j) {
+            f32x16 v;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = (float)acc[m][j][i] * xs[j] * ws[i] + bias[i];
+            const int row = r0 + j * 32;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const int at = f0 + m * 32 + q * 16 + half * 8;
+                const Pack8<T> p = gather8<T>(v, q, 1.0f);
+                if (row < d.rows) store8(static_cast<T*>(d.y) + (int64_t)row * d.y_stride + at, p, d.out - at);
+            }
+        }
+    }
+}
+
+// Few rows: 16 features x 16 NR rows a block, the weights read once, straight into operand registers; 16 waves
+// take pieces of 64 U bytes in turn and are joined through LDS.
+template <class T, int U, int NR>
+__global__ __launch_bounds__(1024) void k_int8_few(Int8Dev d) {
+    __shared__ int part[16][NR][4][64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, f0 = blockIdx.x * 16, f = f0 + (lane & 15);
+    const int8_t* wp = d.w + (int64_t)(f < d.out ? f : 0) * d.w_stride;
+    i32x4 acc[NR];
+#pragma unroll
+    for (int j = 0; j < NR; ++j) acc[j] = i32x4{};
+    for (int k0 = w * 64 * U; k0 < d.in; k0 += 16 * 64 * U) {
+        i32x4 wv[U], xv[NR][U];
+#pragma unroll
+        for (int s = 0; s < U; ++s) {
+            const int k = k0 + s * 64 + (lane >> 4) * 16;
+            wv[s] = i32x4{};
+            if (k < d.in) wv[s] = *reinterpret_cast<const i32x4*>(wp + k);
+#pragma unroll
+            for (int j = 0; j < NR; ++j) {
+                const int row = j * 16 + (lane & 15);
+                xv[j][s] = i32x4{};
+                if (k < d.in && row < d.rows) xv[j][s] = *reinterpret_cast<const i32x4*>(d.x + row * d.x_stride + k);
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < U; ++s) {
+            const int n = d.in - (k0 + s * 64 + (lane >> 4) * 16);       // bytes of the piece that exist
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int left = n - 4 * i;
+                const uint32_t keep = left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1;
+                wv[s][i] &= (int)keep;
+            }
+#pragma unroll
+            for (int j = 0; j < NR; ++j) acc[j] = mma16(wv[s], xv[j][s], acc[j]);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NR; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) part[w][j][r][lane] = acc[j][r];
+    __syncthreads();
+    const int row = (w >> 2) * 16 + (lane & 15), o = f0 + 4 * (lane >> 4) + (w & 3);
+    if (w >= 4 * NR || row >= d.rows || o >= d.out) return;
+    int v = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v += part[i][w >> 2][w & 3][lane];
+    static_cast<T*>(d.y)[(int64_t)row * d.y_stride + o] = (T)scaled<T>(d, v, d.x_scale[row], o);
+}
+
+template <class X>
+bool tiled(GemmJob& job, int blocks_wanted) {
+    job.f_tiles = (job.features + X::TF - 1) / X::TF;
+    job.r_tiles = (int)(((int64_t)job.rows + X::TR - 1) / X::TR);
+    return (int64_t)job.f_tiles * job.r_tiles >= blocks_wanted;
+}
+
+template <class T>
+hipError_t linear(const Int8Dev& d, hipStream_t st) {
+    if (d.rows <= 64) {
+        const unsigned blocks = (unsigned)((d.out + 15) / 16);
+        if (d.rows <= 16)      k_int8_few<T, 2, 1><<<blocks, 1024, 0, st>>>(d);
+        else if (d.rows <= 32) k_int8_few<T, 2, 2><<<blocks, 1024, 0, st>>>(d);
+        else                   k_int8_few<T, 2, 4><<<blocks, 1024, 0, st>>>(d);
+        return hipGetLastError();
+    }
+    GemmJob job{{d.w, nullptr}, {d.x, nullptr}, d.w_stride, d.x_stride, d.out, d.rows, d.in, 0, 0};
+    auto go = [&](auto x) {
+        typedef decltype(x) X;
+        k_int8_tile<X, T><<<(unsigned)((int64_t)job.f_tiles * job.r_tiles), X::THREADS, 0, st>>>(d, job);
+        return hipGetLastError();
+    };
+    typedef Tile<int8_t, 2, 4, 4, 2, 2, false, false> Big;
+    typedef Tile<int8_t, 2, 2, 2, 2, 2, false, false> Mid;
+    typedef Tile<int8_t, 2, 2, 1, 1, 4, false, false> Small;
+    if (tiled<Big>(job, kCUs)) return go(Big{});
+    if (tiled<Mid>(job, kCUs)) return go(Mid{});
+    tiled<Small>(job, 0);
+    return go(Small{});
+}
+
+template <class T>
+hipError_t quantize(const QuantizeDev& d, hipStream_t st) {
+    for (int64_t r0 = 0; r0 < d.rows; r0 += 1 << 23) {
+        const int64_t n = d.rows - r0 < 1 << 23 ? d.rows - r0 : 1 << 23;
+        const unsigned waves = (unsigned)((n + 3) / 4), blocks = (unsigned)n;
+        QuantizeDev c = d;
+        c.rows = r0 + n;
+        if (d.cols <= 512)       k_quantize<T, 1, 1><<<waves, 256, 0, st>>>(c, r0);
+        else if (d.cols <= 1024) k_quantize<T, 1, 2><<<waves, 256, 0, st>>>(c, r0);
+        else if (d.cols <= 2048) k_quantize<T, 4, 1><<<blocks, 256, 0, st>>>(c, r0);
+        else if (d.cols <= 4096) k_quantize<T, 4, 2><<<blocks, 256, 0, st>>>(c, r0);
+        else if (d.cols <= 8192) k_quantize<T, 4, 4><<<blocks, 256, 0, st>>>(c, r0);
+        else                     k_quantize<T, 4, 0><<<blocks, 256, 0, st>>>(c, r0);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+hipError_t int8_linear(const Int8Dev& d, int dtype, hipStream_t st) {
+    return dtype == PA_BF16 ? linear<__bf16>(d, st) : linear<_Float16>(d, st);
+}
+
+hipError_t quantize_rows(const QuantizeDev& d, int dtype, hipStream_t st) {
+    if (dtype == PA_F32) return quantize<float>(d, st);
+    return dtype == PA_BF16 ? quantize<__bf16>(d, st) : quantize<_Float16>(d, st);
+}
+
+}  // namespace pa

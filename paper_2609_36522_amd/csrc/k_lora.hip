@@ -54,22 +54,6 @@ __device__ __forceinline__ int request_from(const LoraDev& d, int row) {
     return d.requests;
 }
 
-// Eight elements at .. of an existing row of len, whole after `fixed`.
-template <class T, int WIDTH>
-__device__ __forceinline__ typename Vec<T>::v8 operand(const T* row, int at, int len, bool valid) {
-    typedef typename Vec<T>::v8 v8;
-    if constexpr (WIDTH == kRagged) return __builtin_bit_cast(v8, load8_raw(row, at, len));
-    if constexpr (WIDTH == kTiny) return __builtin_bit_cast(v8, load8(row, at, len, valid));
-    uint4 r = make_uint4(0, 0, 0, 0);
-    if (valid && at < len) r = __builtin_bit_cast(uint4, *reinterpret_cast<const Pack8<T>*>(row + at));
-    return __builtin_bit_cast(v8, r);
-}
-template <class T, int WIDTH>
-__device__ __forceinline__ typename Vec<T>::v8 fixed(typename Vec<T>::v8 r, int at, int len, bool valid) {
-    if constexpr (WIDTH == kRagged) return __builtin_bit_cast(typename Vec<T>::v8, fix8(__builtin_bit_cast(Pack8<T>, r), at, len, valid));
-    return r;
-}
-
 // ROWS rows x 64 columns of a matrix on their way to LDS, THREADS threads. kWhole and kEven by loads that write
 // LDS themselves (a wave's lanes fill consecutive 16-byte slots, so the permutation of a row's pieces is in
 // the addresses that they read; what does not exist has an offset out of the buffer's range, which reads

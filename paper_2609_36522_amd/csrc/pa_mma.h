@@ -50,6 +50,22 @@ __device__ __forceinline__ typename Vec<T>::v8 read_cols(const T* tile, int row0
     return __builtin_bit_cast(typename Vec<T>::v8, v);
 }
 
+// Eight elements at .. of an existing row of len, whole after `fixed`.
+template <class T, int WIDTH>
+__device__ __forceinline__ typename Vec<T>::v8 operand(const T* row, int at, int len, bool valid) {
+    typedef typename Vec<T>::v8 v8;
+    if constexpr (WIDTH == kRagged) return __builtin_bit_cast(v8, load8_raw(row, at, len));
+    if constexpr (WIDTH == kTiny) return __builtin_bit_cast(v8, load8(row, at, len, valid));
+    uint4 r = make_uint4(0, 0, 0, 0);
+    if (valid && at < len) r = __builtin_bit_cast(uint4, *reinterpret_cast<const Pack8<T>*>(row + at));
+    return __builtin_bit_cast(v8, r);
+}
+template <class T, int WIDTH>
+__device__ __forceinline__ typename Vec<T>::v8 fixed(typename Vec<T>::v8 r, int at, int len, bool valid) {
+    if constexpr (WIDTH == kRagged) return __builtin_bit_cast(typename Vec<T>::v8, fix8(__builtin_bit_cast(Pack8<T>, r), at, len, valid));
+    return r;
+}
+
 // Registers 8t .. 8t + 7 of an accumulator in the element type: a B operand.
 template <class T>
 __device__ __forceinline__ typename Vec<T>::v8 pack(const f32x16& s, int t) {

@@ -52,6 +52,55 @@ struct LoraDev {
     int64_t x_stride, w_stride, y_stride;
 };
 
+struct GroupDev {
+    const void *x, *dy, *w, *b;
+    void *y, *dx, *dw, *db;
+    float *mean, *rstd;              // [batch][groups]
+    float* part;                     // forward: [batch][groups][chunks][2] mean, sum of squared differences;
+                                     // backward: [batch][chunks][2][channels] sums of dz xh, dz
+    float* sums;                     // backward: [batch][2][channels], the same over all chunks
+    float* means;                    // backward: [batch][groups][2] mean(g), mean(g xh)
+    int64_t xs[2], ys[2], dxs[2];    // batch, pixel
+    int batch, pixels, channels, groups, width;   // width: channels of a group
+    int slab, slabs;                 // channels of a block (whole groups; the last has what is left), blocks over them
+    int chunk, chunks;               // pixels of a block, blocks over them
+    float eps;
+};
+
+struct FeedDev {
+    const void *x, *gate, *up, *down, *dy;      // as given, with their strides
+    int64_t x_stride, gate_stride, up_stride, down_stride, y_stride;
+    const void *gate_bias, *up_bias, *down_bias;
+    void* y;
+    void *g, *u, *h;                 // [rows][hidden_pad] both projections (may be null) and the gated product
+    void *dx, *dgate, *dup, *ddown, *dgate_bias, *dup_bias, *ddown_bias;
+    void *dz, *du;                   // backward: [rows][hidden_pad] gradients by the two projections
+    void *x_pad, *gate_pad, *up_pad, *down_pad, *dy_pad;   // copies in whole pieces of 16 bytes (null: read in place)
+    float* largest;                  // backward in fp16: kLargest partial maxima of |dy|
+    float* part;                     // backward: partial sums of the weights' gradients
+    int rows, in, hidden, out;
+    int in_pad, hidden_pad, out_pad; // multiples of 8
+    int splits;                      // backward: ranges of rows whose weights' gradients are summed apart
+};
+constexpr int kLargest = 256;
+
+struct Int8Dev {
+    const int8_t *x, *w;
+    const float *x_scale, *w_scale;
+    const void* bias;
+    void* y;
+    int rows, in, out;
+    int64_t x_stride, w_stride, y_stride;
+};
+
+struct QuantizeDev {
+    const void* x;
+    int8_t* q;
+    float* scale;
+    int64_t rows, x_stride, q_stride;
+    int cols;
+};
+
 // Launchers return the launch's hipError_t.
 hipError_t norm_forward(const NormDev& d, int dtype, int param_dtype, hipStream_t st);
 int norm_backward_blocks(int64_t rows, int64_t cols);
@@ -63,5 +112,20 @@ hipError_t cross_forward(const CrossDev& d, int dtype, hipStream_t st);
 hipError_t cross_backward(const CrossDev& d, int dtype, hipStream_t st);
 
 hipError_t lora_linear(const LoraDev& d, int dtype, hipStream_t st);
+
+// Fills in slab .. chunks from the sizes. Whether one block takes a slab's pixels in one launch: chunks == 1.
+void group_plan(GroupDev& d, int dtype, bool backward);
+hipError_t group_forward(const GroupDev& d, int dtype, int param_dtype, int act, hipStream_t st);
+hipError_t group_backward(const GroupDev& d, int dtype, int param_dtype, int act, hipStream_t st);
+
+// Whether rows are read straight from memory (no copies in whole pieces).
+bool feed_few(int64_t rows);
+// How many ranges of rows the weights' gradients take.
+int feed_splits(const FeedDev& d);
+hipError_t feed_forward(const FeedDev& d, int dtype, int act, hipStream_t st);
+hipError_t feed_backward(const FeedDev& d, int dtype, int act, hipStream_t st);
+
+hipError_t quantize_rows(const QuantizeDev& d, int dtype, hipStream_t st);
+hipError_t int8_linear(const Int8Dev& d, int dtype, hipStream_t st);
 
 }  // namespace pa

@@ -4,41 +4,13 @@
 #include <math.h>
 #include <stddef.h>
 
-#include "pa_host.h"
-#include "pa_ops.h"
+#include "pa_ops_host.h"
 
-using pa::fail;
-using pa::hip_fail;
+using namespace pa;
 
 namespace {
 
 constexpr int64_t kMaxBlocks = 1 << 23;       // a grid holds fewer than 2^32 threads
-
-size_t round256(size_t n) { return (n + 255) / 256 * 256; }
-
-int element_size(int dtype) { return dtype == PA_F32 ? 4 : 2; }
-
-bool misaligned(const void* p, int size) { return reinterpret_cast<uintptr_t>(p) % size != 0; }
-
-int check_workspace(const void* ws, size_t have, size_t need) {
-    if (need == 0) return PA_OK;
-    if (!ws) return fail(PA_ERR_INVALID_ARG, "workspace is NULL (%zu bytes needed)", need);
-    if (misaligned(ws, 256)) return fail(PA_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
-    if (have < need) return fail(PA_ERR_INVALID_ARG, "workspace of %zu bytes too small: %zu needed", have, need);
-    return PA_OK;
-}
-
-int launched(hipError_t e, const char* what) { return e == hipSuccess ? PA_OK : hip_fail(e, what); }
-
-// No C++ exception (std::bad_alloc of an error text) crosses the C ABI.
-template <class F>
-int guarded(F f) noexcept {
-    try {
-        return f();
-    } catch (...) {
-        return PA_ERR_OOM;
-    }
-}
 
 // ------------------------------------------------------------------ layer norm
 int check_norm(const pa_norm_t* p) {

@@ -1,18 +1,19 @@
 """Operators of a text-conditioned noise network (the C ABI in include/paraanya_ops.h): layer norm,
 cross attention to a prompt encoder's states, a shared projection with the low-rank adapters of many
-requests.
+requests, group norm with an activation, a gated feed-forward block, a projection in 8-bit integers.
 
 Argument marshalling only, as in :mod:`binding`: every product and sum runs in the library's HIP
 kernels. Tensors lie on the current device; kernels run on torch's current stream, outputs and
-workspaces come from torch's allocator on that stream. :func:`layer_norm` and
-:func:`cross_attention` take part in autograd, for first derivatives (a gradient's gradient is refused); the
-``*_forward`` and ``*_backward`` functions do not.
+workspaces come from torch's allocator on that stream. :func:`layer_norm`, :func:`cross_attention`,
+:func:`group_norm` and :func:`feed_forward` take part in autograd, for first derivatives (a gradient's
+gradient is refused); the ``*_forward`` and ``*_backward`` functions do not.
 """
 from __future__ import annotations
 
 import ctypes as C
 import functools
 import math
+from typing import NamedTuple, Optional
 
 import torch
 from torch.autograd.function import once_differentiable
@@ -24,12 +25,21 @@ PA_MASK_NONE, PA_MASK_BOOL, PA_MASK_ADD = 0, 1, 2
 PA_NORM_MAX_COLS = 1 << 20
 PA_LORA_MAX_RANK = 128
 HEAD_DIM_MAX = 128
+PA_ACT_NONE, PA_ACT_SILU, PA_ACT_GELU = 0, 1, 2
+PA_GROUP_MAX_CHANNELS = 4096
+PA_INT8_MAX_IN = (1 << 17) - 1
 
 EXPORTED = ("paraanya_layer_norm", "paraanya_layer_norm_backward", "paraanya_layer_norm_backward_workspace",
             "paraanya_cross_attention", "paraanya_cross_attention_workspace",
             "paraanya_cross_attention_backward", "paraanya_cross_attention_backward_workspace",
-            "paraanya_lora_linear", "paraanya_lora_linear_workspace")
+            "paraanya_lora_linear", "paraanya_lora_linear_workspace",
+            "paraanya_group_norm", "paraanya_group_norm_workspace",
+            "paraanya_group_norm_backward", "paraanya_group_norm_backward_workspace",
+            "paraanya_feed_forward", "paraanya_feed_forward_saved", "paraanya_feed_forward_workspace",
+            "paraanya_feed_forward_backward", "paraanya_feed_forward_backward_workspace",
+            "paraanya_quantize_rows", "paraanya_int8_linear")
 
+_ACT = {None: PA_ACT_NONE, "silu": PA_ACT_SILU, "gelu": PA_ACT_GELU}
 _DTYPE = {torch.float32: PA_F32, torch.bfloat16: PA_BF16, torch.float16: PA_F16}
 
 
@@ -58,6 +68,32 @@ class Lora(C.Structure):
                 ("scales", C.c_void_p)]
 
 
+class GroupNorm(C.Structure):
+    _fields_ = [("batch", C.c_int64), ("pixels", C.c_int64), ("channels", C.c_int32), ("groups", C.c_int32),
+                ("dtype", C.c_int32), ("param_dtype", C.c_int32), ("activation", C.c_int32), ("pad", C.c_int32),
+                ("eps", C.c_double), ("x_stride", C.c_int64 * 2), ("y_stride", C.c_int64 * 2), ("dx_stride", C.c_int64 * 2)]
+
+
+class Feed(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("in_features", C.c_int32), ("hidden_features", C.c_int32), ("out_features", C.c_int32),
+                ("dtype", C.c_int32), ("activation", C.c_int32), ("alignment", C.c_int32), ("x_stride", C.c_int64),
+                ("gate_stride", C.c_int64), ("up_stride", C.c_int64), ("down_stride", C.c_int64), ("y_stride", C.c_int64)]
+
+
+class FeedGrad(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("dx", "dgate", "dup", "ddown", "dgate_bias", "dup_bias", "ddown_bias")]
+
+
+class Quantize(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("dtype", C.c_int32), ("pad", C.c_int32), ("x_stride", C.c_int64),
+                ("q_stride", C.c_int64)]
+
+
+class Int8Linear(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("in_features", C.c_int32), ("out_features", C.c_int32), ("dtype", C.c_int32),
+                ("pad", C.c_int32), ("x_stride", C.c_int64), ("w_stride", C.c_int64), ("y_stride", C.c_int64)]
+
+
 _LIB = None
 
 
@@ -71,11 +107,18 @@ def _library():
         lib.paraanya_cross_attention.argtypes = [P, P, P, P, P, P, P, Z, P]
         lib.paraanya_cross_attention_backward.argtypes = [P, P, P, P, P, P, P, P, P, P, P, P, Z, P]
         lib.paraanya_lora_linear.argtypes = [P, P, P, P, P, P, P, P, Z, P]
+        lib.paraanya_group_norm.argtypes = [P, P, P, P, P, P, P, P, Z, P]
+        lib.paraanya_group_norm_backward.argtypes = [P, P, P, P, P, P, P, P, P, P, P, Z, P]
+        lib.paraanya_feed_forward.argtypes = [P, P, P, P, P, P, P, P, P, P, Z, P, Z, P]
+        lib.paraanya_feed_forward_backward.argtypes = [P, P, P, P, P, P, P, P, Z, P, Z, P]
+        lib.paraanya_quantize_rows.argtypes = [P, P, P, P, P]
+        lib.paraanya_int8_linear.argtypes = [P, P, P, P, P, P, P, P]
         for name in EXPORTED:
             f = getattr(lib, name)
             f.restype = C.c_int
-            if name.endswith("_workspace"):
+            if name.endswith(("_workspace", "_saved")):
                 f.argtypes = [P, C.POINTER(Z)]
+        lib.paraanya_feed_forward_workspace.argtypes = [P, C.c_int, C.POINTER(Z)]
         _LIB = lib
     return _LIB
 
@@ -368,4 +411,307 @@ def lora_linear(x, weight, a, b, offsets, ids, *, scales=None, bias=None):
     ws = _workspace(size, x)
     B._check(_LIB.paraanya_lora_linear(C.byref(p), x.data_ptr(), weight.data_ptr(), _ptr(bias), a.data_ptr(), b.data_ptr(),
                                        y.data_ptr(), _ptr(ws), size, st))
+    return y
+
+
+# ------------------------------------------------------------------ group norm
+def _pixels(t):
+    """A [batch, pixels, channels] view of t with consecutive channels (a copy where its strides allow no view)."""
+    B, Ch = t.shape[0], t.shape[-1]
+    t = t.reshape(B, math.prod(t.shape[1:-1]), Ch)
+    return t if (t.stride(2) == 1 or Ch == 1) and (t.shape[1] < 2 or t.stride(1) >= Ch) else t.contiguous()
+
+
+def _activation(name):
+    if name not in _ACT:
+        raise ValueError(f"activation must be None, 'silu' or 'gelu', not {name!r}")
+    return _ACT[name]
+
+
+def _group_args(x, groups, weight, bias):
+    if x.dtype not in _DTYPE:
+        raise ValueError(f"group norm of {x.dtype} is not built")
+    if x.dim() < 2 or x.shape[-1] < 1:
+        raise ValueError("group norm needs the shape [batch, ..., channels]")
+    if groups < 1 or x.shape[-1] % groups:
+        raise ValueError("channels must be a multiple of groups")
+    return _norm_args(x, weight, bias)
+
+
+@functools.lru_cache(maxsize=256)
+def _group(B_, P, Ch, G, dtype, param_dtype, act, eps, x_stride, y_stride):
+    """The (constant) description of a group norm and the workspaces of its forward and backward pass."""
+    lib = _library()
+    p = GroupNorm(B_, P, Ch, G, dtype, param_dtype, act, 0, eps, x_stride, y_stride, (P * Ch, Ch))
+    return p, C.byref(p), _size(lib.paraanya_group_norm_workspace, p), _size(lib.paraanya_group_norm_backward_workspace, p)
+
+
+def group_norm_forward(x, groups, weight=None, bias=None, eps=1e-5, *, activation=None):
+    """(y, mean, rstd) of the norm over pixels and the channels of each group, followed by an activation.
+
+    x [batch, ..., channels], channels last (of a channels-last image tensor: ``x.permute(0, 2, 3, 1)``, a view), in
+    float32, bf16 or fp16; weight and bias [channels], of x's type or float32. ``activation`` is None, "silu" or
+    "gelu". mean and rstd are fp32, [batch, groups]."""
+    act = _activation(activation)
+    pt = _group_args(x, groups, weight, bias)
+    st = _on_device(x, weight, bias)
+    x3 = _pixels(x)
+    B_, P, Ch = x3.shape
+    _, ref, n, _ = _group(B_, P, Ch, groups, _DTYPE[x.dtype], _DTYPE[pt], act, eps, x3.stride()[:2], (P * Ch, Ch))
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    mean = torch.empty((B_, groups), dtype=torch.float32, device=x.device)
+    rstd = torch.empty((B_, groups), dtype=torch.float32, device=x.device)
+    if P == 0:
+        mean.zero_(), rstd.zero_()
+    ws = _workspace(n, x)
+    B._check(_LIB.paraanya_group_norm(ref, x3.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+                                      _ptr(ws), n, st))
+    return y, mean, rstd
+
+
+def group_norm_backward(dy, x, mean, rstd, weight=None, bias=None, *, activation=None, param_dtype=None):
+    """(dx, dweight, dbias) from the forward pass's x, weight, bias, mean and rstd. dweight and dbias have the
+    parameters' type (``param_dtype``, or x's, where there are none)."""
+    act = _activation(activation)
+    if mean.dim() != 2 or mean.shape[0] != x.shape[0]:
+        raise ValueError("mean and rstd must be [batch, groups]")
+    groups = mean.shape[1]
+    pt = _group_args(x, groups, weight, bias)
+    if weight is None and bias is None and param_dtype is not None:
+        pt = param_dtype
+    if pt not in (x.dtype, torch.float32):
+        raise ValueError("param_dtype must be x's type or float32")
+    if dy.shape != x.shape or dy.dtype != x.dtype:
+        raise ValueError("dy must have x's shape and type")
+    for t in (mean, rstd):
+        if t.dtype != torch.float32 or t.shape != mean.shape or not t.is_contiguous():
+            raise ValueError("mean and rstd must be contiguous float32 tensors of one shape")
+    st = _on_device(x, dy, mean, rstd, weight, bias)
+    x3, dy3 = _pixels(x), _pixels(dy)
+    B_, P, Ch = x3.shape
+    p, _, _, n = _group(B_, P, Ch, groups, _DTYPE[x.dtype], _DTYPE[pt], act, 0.0, x3.stride()[:2], (P * Ch, Ch))
+    p = GroupNorm.from_buffer_copy(p)
+    p.y_stride[:] = dy3.stride()[:2]
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    dw = torch.empty(Ch, dtype=pt, device=x.device)
+    db = torch.empty(Ch, dtype=pt, device=x.device)
+    ws = _workspace(n, x)
+    B._check(_LIB.paraanya_group_norm_backward(C.byref(p), dy3.data_ptr(), x3.data_ptr(), _ptr(weight), _ptr(bias), mean.data_ptr(),
+                                               rstd.data_ptr(), dx.data_ptr(), dw.data_ptr(), db.data_ptr(), _ptr(ws), n, st))
+    return dx, dw, db
+
+
+class _GroupNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, groups, weight, bias, eps, activation):
+        y, mean, rstd = group_norm_forward(x, groups, weight, bias, eps, activation=activation)
+        ctx.save_for_backward(x, weight, bias, mean, rstd)
+        ctx.activation = activation
+        return y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        x, weight, bias, mean, rstd = ctx.saved_tensors
+        dx, dw, db = group_norm_backward(dy, x, mean, rstd, weight, bias, activation=ctx.activation)
+        need = ctx.needs_input_grad
+        return dx if need[0] else None, None, dw if need[2] else None, db if need[3] else None, None, None
+
+
+def group_norm(x, groups, weight=None, bias=None, eps=1e-5, *, activation=None):
+    """:func:`group_norm_forward`'s y, differentiable (once) in x, weight and bias."""
+    return _GroupNorm.apply(x, groups, weight, bias, eps, activation)
+
+
+# ------------------------------------------------------------------ gated feed-forward block
+class FeedGradients(NamedTuple):
+    """Gradients of :func:`feed_forward`'s arguments, of their shapes (None where not asked for)."""
+    x: Optional[torch.Tensor]
+    gate: Optional[torch.Tensor]
+    up: Optional[torch.Tensor]
+    down: Optional[torch.Tensor]
+    gate_bias: Optional[torch.Tensor]
+    up_bias: Optional[torch.Tensor]
+    down_bias: Optional[torch.Tensor]
+
+
+@functools.lru_cache(maxsize=256)
+def _feed(M, K, H, N, dtype, act, alignment, strides):
+    """The (constant) description of a block and the sizes of saved, of the forward pass's workspace without and with it,
+    and of the backward pass's."""
+    lib = _library()
+    p = Feed(M, K, H, N, dtype, act, alignment, *strides)
+    sizes = [_size(lib.paraanya_feed_forward_saved, p)]
+    for with_saved in (0, 1):
+        n = C.c_size_t(0)
+        B._check(lib.paraanya_feed_forward_workspace(C.byref(p), with_saved, C.byref(n)))
+        sizes.append(n.value)
+    return (p, C.byref(p), *sizes, _size(lib.paraanya_feed_forward_backward_workspace, p))
+
+
+def _feed_args(x, gate, up, down, biases, activation, y=None):
+    """(description, x, gate, up, down, y as matrices of consecutive elements, stream)."""
+    if x.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError(f"feed forward of {x.dtype} is not built")
+    act = _activation(activation)
+    if x.dim() < 1 or gate.dim() != 2 or up.dim() != 2 or down.dim() != 2:
+        raise ValueError("expected x [..., K], gate and up [H, K] and down [N, H]")
+    K, (H, N) = x.shape[-1], (gate.shape[0], down.shape[0])
+    if gate.shape != (H, K) or up.shape != (H, K) or down.shape != (N, H) or min(K, H, N) < 1:
+        raise ValueError("x, gate, up and down do not fit together")
+    for t, n in zip(biases, (H, H, N)):
+        if t is not None and (t.shape != (n,) or not t.is_contiguous()):
+            raise ValueError(f"a bias must be contiguous with {n} elements")
+    if any(t is not None and t.dtype != x.dtype for t in (gate, up, down, *biases, y)):
+        raise ValueError("x, the weights, the biases and dy must have one type")
+    if y is not None and y.shape != (*x.shape[:-1], N):
+        raise ValueError("dy must have y's shape")
+    st = _on_device(x, gate, up, down, *biases, y)
+    x, gate, up, down = _rows(x, K), _rows(gate, K), _rows(up, K), _rows(down, H)
+    y = None if y is None else _rows(y, N)
+    given = [t for t in (x, gate, up, down, y) if t is not None]
+    at = functools.reduce(lambda a, t: a | t.data_ptr(), given, 16)
+    d = _feed(x.shape[0], K, H, N, _DTYPE[x.dtype], act, at & -at,
+              (_stride(x), _stride(gate), _stride(up), _stride(down), N if y is None else _stride(y)))
+    return d, x, gate, up, down, y, st
+
+
+def feed_forward_forward(x, gate, up, down, gate_bias=None, up_bias=None, down_bias=None, *, activation="silu", save=True):
+    """(y, saved): (act(x gate^T + gate_bias) * (x up^T + up_bias)) down^T + down_bias.
+
+    x [..., K], gate and up [H, K], down [N, H] (row strides of their own), biases [H], [H], [N], in bf16 or fp16.
+    ``activation`` is "silu", "gelu" or None. saved (opaque; None without ``save``) is what the backward pass
+    needs: both projections and the gated product."""
+    d, x2, g, u, dn, _, st = _feed_args(x, gate, up, down, (gate_bias, up_bias, down_bias), activation)
+    _, ref, keep, plain, with_saved, _ = d
+    y = torch.empty((*x.shape[:-1], down.shape[0]), dtype=x.dtype, device=x.device)
+    saved = torch.empty(keep, dtype=torch.uint8, device=x.device) if save else None
+    n = with_saved if save else plain
+    ws = _workspace(n, x)
+    B._check(_LIB.paraanya_feed_forward(ref, x2.data_ptr(), g.data_ptr(), _ptr(gate_bias), u.data_ptr(), _ptr(up_bias), dn.data_ptr(),
+                                        _ptr(down_bias), y.data_ptr(), _ptr(saved), keep, _ptr(ws), n, st))
+    return y, saved
+
+
+def feed_forward_backward(dy, x, gate, up, down, saved, *, activation="silu", need=(True,) * 7):
+    """:class:`FeedGradients` from dy, the forward pass's inputs and what it saved. ``need`` says which of them
+    are computed (x, gate, up, down and the biases in that order; a bias's comes with its weight's)."""
+    d, x2, g, u, dn, dy2, st = _feed_args(x, gate, up, down, (), activation, dy)
+    p, ref, keep, _, _, n = d
+    if saved.dtype != torch.uint8 or saved.numel() != keep or not saved.is_contiguous():
+        raise ValueError("saved must be the forward pass's")
+    _on_device(saved)
+    H, N = gate.shape[0], down.shape[0]
+    need = list(need)
+    for i in (1, 2, 3):
+        need[i] = need[i] or need[i + 3]
+    shapes = (x.shape, gate.shape, up.shape, down.shape, (H,), (H,), (N,))
+    out = FeedGradients(*(torch.empty(s, dtype=x.dtype, device=x.device) if k else None for s, k in zip(shapes, need)))
+    ws = _workspace(n, x)
+    B._check(_LIB.paraanya_feed_forward_backward(ref, C.byref(FeedGrad(*map(_ptr, out))), dy2.data_ptr(), x2.data_ptr(), g.data_ptr(),
+                                                 u.data_ptr(), dn.data_ptr(), _ptr(saved), keep, _ptr(ws), n, st))
+    return out
+
+
+class _FeedForward(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, gate, up, down, gate_bias, up_bias, down_bias, activation):
+        y, saved = feed_forward_forward(x, gate, up, down, gate_bias, up_bias, down_bias, activation=activation,
+                                        save=any(ctx.needs_input_grad))
+        ctx.save_for_backward(x, gate, up, down, saved)
+        ctx.activation = activation
+        return y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        x, gate, up, down, saved = ctx.saved_tensors
+        need = ctx.needs_input_grad[:7]
+        g = feed_forward_backward(dy, x, gate, up, down, saved, activation=ctx.activation, need=need)
+        return (*(t if k else None for t, k in zip(g, need)), None)
+
+
+def feed_forward(x, gate, up, down, gate_bias=None, up_bias=None, down_bias=None, *, activation="silu"):
+    """:func:`feed_forward_forward`'s y, differentiable (once) in x, the weights and the biases."""
+    return _FeedForward.apply(x, gate, up, down, gate_bias, up_bias, down_bias, activation)
+
+
+# ------------------------------------------------------------------ projection in 8-bit integers
+def _no_gradients(what, *tensors):
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise ValueError(f"{what} has no gradients: call it under torch.no_grad()")
+
+
+@functools.lru_cache(maxsize=256)
+def _quantize(M, K, dtype, x_stride, q_stride):
+    _library()
+    p = Quantize(M, K, dtype, 0, x_stride, q_stride)
+    return p, C.byref(p)
+
+
+def quantize_rows(x):
+    """(q, scale): x's rows as 8-bit integers, scale = max |x| / 127 of each row (float32) and q = x / scale rounded to
+    the nearest integer. x [..., K] in float32, bf16 or fp16. q's rows start at multiples of 16 bytes (so a matrix of
+    weights is quantized by the same call). A row that holds an infinity or a NaN has scale NaN. No gradients."""
+    if x.dtype not in _DTYPE:
+        raise ValueError(f"quantize rows of {x.dtype} is not built")
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError("quantize rows needs at least one column")
+    _no_gradients("quantize rows", x)
+    st = _on_device(x)
+    K = x.shape[-1]
+    x2 = _rows(x, K)
+    M, wide = x2.shape[0], (K + 15) // 16 * 16
+    _, ref = _quantize(M, K, _DTYPE[x.dtype], _stride(x2), wide)
+    q = torch.empty((*x.shape[:-1], wide), dtype=torch.int8, device=x.device)
+    scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    B._check(_LIB.paraanya_quantize_rows(ref, x2.data_ptr(), q.data_ptr(), scale.data_ptr(), st))
+    return q if wide == K else q[..., :K], scale
+
+
+def _int8_rows(t, K):
+    """A [rows, K] view of t whose rows start at multiples of 16 bytes (a copy where it has none)."""
+    t = t.reshape(-1, K)
+    if (t.stride(1) == 1 or K == 1) and t.data_ptr() % 16 == 0 and (t.shape[0] < 2 or (t.stride(0) >= K and t.stride(0) % 16 == 0)):
+        return t
+    out = torch.empty((t.shape[0], (K + 15) // 16 * 16), dtype=torch.int8, device=t.device)[:, :K]
+    return out.copy_(t)
+
+
+def _int8_stride(t):
+    return t.stride(0) if t.shape[0] > 1 else (t.shape[1] + 15) // 16 * 16
+
+
+@functools.lru_cache(maxsize=256)
+def _int8(M, K, N, dtype, x_stride, w_stride):
+    _library()
+    p = Int8Linear(M, K, N, dtype, 0, x_stride, w_stride, N)
+    return p, C.byref(p)
+
+
+def int8_linear(q, scale, weight, weight_scale, bias=None, *, dtype=torch.bfloat16):
+    """(q weight^T) scale weight_scale + bias in ``dtype`` (bf16 or fp16).
+
+    q [..., K] and weight [N, K] are int8 (as :func:`quantize_rows` gives them; rows that do not start at multiples
+    of 16 bytes are copied), scale [...] and weight_scale [N] float32, bias [N] of ``dtype``. The product is summed in
+    32-bit integers. No gradients."""
+    if dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError(f"int8 linear to {dtype} is not built")
+    if q.dtype != torch.int8 or weight.dtype != torch.int8:
+        raise ValueError("q and weight must be int8 tensors")
+    if q.dim() < 1 or weight.dim() != 2 or weight.shape[1] != q.shape[-1] or min(weight.shape) < 1:
+        raise ValueError("expected q [..., K] and weight [N, K]")
+    K, N = q.shape[-1], weight.shape[0]
+    for t, shape, name in ((scale, q.shape[:-1], "scale"), (weight_scale, (N,), "weight_scale")):
+        if t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous float32 tensor of the shape {tuple(shape)}")
+    if bias is not None and (bias.dtype != dtype or bias.shape != (N,) or not bias.is_contiguous()):
+        raise ValueError(f"bias must be contiguous with {N} elements of {dtype}")
+    _no_gradients("int8 linear", scale, weight_scale, bias)
+    st = _on_device(q, scale, weight, weight_scale, bias)
+    q2, w = _int8_rows(q, K), _int8_rows(weight, K)
+    _, ref = _int8(q2.shape[0], K, N, _DTYPE[dtype], _int8_stride(q2), _int8_stride(w))
+    y = torch.empty((*q.shape[:-1], N), dtype=dtype, device=q.device)
+    B._check(_LIB.paraanya_int8_linear(ref, q2.data_ptr(), scale.data_ptr(), w.data_ptr(), weight_scale.data_ptr(), _ptr(bias),
+                                       y.data_ptr(), st))
     return y
