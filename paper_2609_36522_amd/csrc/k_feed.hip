@@ -119,30 +119,27 @@ __global__ __launch_bounds__(X::THREADS, 2) void k_feed_gate(FeedDev d, GemmJob 
     X::run(job, f * X::OUT, r * X::TR, 0, (job.len + X::PART - 1) / X::PART, lds, acc, sums);
     const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6;
     constexpr int HM = X::NM / 2;
-    const int f0 = f * X::OUT + (w % X::WF) * HM * 32, r0 = r * X::TR + (w / X::WF) * X::NX * 32 + (lane & 31);
+    const int f0 = f * X::OUT + (w % X::WF) * HM * 32, r0 = r * X::TR + (w / X::WF) * X::NX * 32;
     add_bias<T, X::NM, X::NX>(d.gate_bias, f0, d.hidden, half, acc, 0, HM);
     add_bias<T, X::NM, X::NX>(d.up_bias, f0, d.hidden, half, acc, HM, X::NM);
+    char* own = lds + w * HM * 2048;
 #pragma unroll
-    for (int m = 0; m < HM; ++m) {
-#pragma unroll
-        for (int j = 0; j < X::NX; ++j) {
-            f32x16 h;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) h[i] = activate<ACT>(acc[m][j][i]) * acc[m + HM][j][i];
-            const int row = r0 + j * 32;
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const int at = f0 + m * 32 + q * 16 + half * 8;
-                const Pack8<T> ph = gather8<T>(h, q, 1.0f), pg = gather8<T>(acc[m][j], q, 1.0f), pu = gather8<T>(acc[m + HM][j], q, 1.0f);
-                if (row >= d.rows || at >= d.hidden_pad) continue;
-                const int64_t to = (int64_t)row * d.hidden_pad + at;
-                store_padded(static_cast<T*>(d.h) + to, ph, d.hidden - at);
-                if (d.g) {
-                    store_padded(static_cast<T*>(d.g) + to, pg, d.hidden - at);
-                    store_padded(static_cast<T*>(d.u) + to, pu, d.hidden - at);
-                }
-            }
+    for (int j = 0; j < X::NX; ++j) {
+        auto store = [&](void* to, auto value) {
+            through_lds<T, HM>(own, lane, value, [&](int row, int at, const Pack8<T>& v) {
+                if (r0 + j * 32 + row < d.rows && f0 + at < d.hidden_pad)
+                    store_padded(static_cast<T*>(to) + (int64_t)(r0 + j * 32 + row) * d.hidden_pad + f0 + at, v, d.hidden - f0 - at);
+            });
+        };
+        if (d.g) {
+            store(d.g, [&](int m, int q) { return gather8<T>(acc[m][j], q, 1.0f); });
+            store(d.u, [&](int m, int q) { return gather8<T>(acc[m + HM][j], q, 1.0f); });
         }
+#pragma unroll
+        for (int m = 0; m < HM; ++m)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[m][j][i] = activate<ACT>(acc[m][j][i]) * acc[m + HM][j][i];
+        store(d.h, [&](int m, int q) { return gather8<T>(acc[m][j], q, 1.0f); });
     }
 }
 
@@ -169,20 +166,17 @@ __global__ __launch_bounds__(X::THREADS, 2) void k_feed_plain(PlainDev d, GemmJo
     const int parts = (job.len + X::PART - 1) / X::PART * (job.f[1] ? 2 : 1);
     X::run(job, f * X::TF, r * X::TR, (int)((int64_t)parts * split / d.splits), (int)((int64_t)parts * (split + 1) / d.splits), lds, acc, sums);
     const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6;
-    const int f0 = f * X::TF + (w % X::WF) * X::NM * 32, r0 = r * X::TR + (w / X::WF) * X::NX * 32 + (lane & 31);
+    const int f0 = f * X::TF + (w % X::WF) * X::NM * 32, r0 = r * X::TR + (w / X::WF) * X::NX * 32;
     if (d.splits == 1) {
         const float s = d.largest ? 1.0f / gradient_scale<T>(d.largest) : 1.0f;
         add_bias<T, X::NM, X::NX>(d.bias, f0, job.features, half, acc, 0, X::NM);
 #pragma unroll
-        for (int m = 0; m < X::NM; ++m)
-#pragma unroll
-            for (int j = 0; j < X::NX; ++j)
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    const int at = f0 + m * 32 + q * 16 + half * 8, row = r0 + j * 32;
-                    const Pack8<T> p = gather8<T>(acc[m][j], q, s);
-                    if (row < job.rows) store8(static_cast<T*>(d.out) + (int64_t)row * d.out_stride + at, p, job.features - at);
-                }
+        for (int j = 0; j < X::NX; ++j)
+            through_lds<T, X::NM>(lds + w * X::NM * 2048, lane, [&](int m, int q) { return gather8<T>(acc[m][j], q, s); },
+                                  [&](int row, int at, const Pack8<T>& v) {
+                                      if (r0 + j * 32 + row < job.rows)
+                                          store8(static_cast<T*>(d.out) + (int64_t)(r0 + j * 32 + row) * d.out_stride + f0 + at, v, job.features - f0 - at);
+                                  });
     } else {
 #pragma unroll
         for (int m = 0; m < X::NM; ++m)
@@ -190,7 +184,7 @@ __global__ __launch_bounds__(X::THREADS, 2) void k_feed_plain(PlainDev d, GemmJo
             for (int j = 0; j < X::NX; ++j)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const int at = f0 + m * 32 + q * 8 + half * 4, row = r0 + j * 32;
+                    const int at = f0 + m * 32 + q * 8 + half * 4, row = r0 + j * 32 + (lane & 31);
                     const f32x4 v = {acc[m][j][4 * q], acc[m][j][4 * q + 1], acc[m][j][4 * q + 2], acc[m][j][4 * q + 3]};
                     if (row < job.rows && at < d.feature_pad)
                         *reinterpret_cast<f32x4*>(d.part + ((int64_t)split * job.rows + row) * d.feature_pad + at) = v;
@@ -289,7 +283,7 @@ __global__ __launch_bounds__(1024) void k_feed_few_gate(FeedDev d) {
     const bool valid = f < d.hidden;
     const T* const wp[2] = {static_cast<const T*>(d.gate) + (valid ? f : 0) * d.gate_stride, static_cast<const T*>(d.up) + (valid ? f : 0) * d.up_stride};
     f32x4 v[2];
-    few_rows<T, 2, NR, 2, WIDTH>(wp, valid, static_cast<const T*>(d.x), d.x_stride, d.rows, d.in, part, v);
+    few_rows<T, NR < 4 ? 2 : 1, NR, 2, WIDTH>(wp, valid, static_cast<const T*>(d.x), d.x_stride, d.rows, d.in, part, v);
     const int row = (w >> 2) * 16 + (lane & 15), o = f0 + 4 * (lane >> 4) + (w & 3);
     if (w >= 4 * NR || row >= d.rows || o >= d.hidden_pad) return;
     const bool in = o < d.hidden;
@@ -310,7 +304,7 @@ __global__ __launch_bounds__(1024) void k_feed_few_down(FeedDev d) {
     const bool valid = f < d.out;
     const T* const wp[1] = {static_cast<const T*>(d.down) + (valid ? f : 0) * d.down_stride};
     f32x4 v[1];
-    few_rows<T, 4, NR, 1, WIDTH>(wp, valid, static_cast<const T*>(d.h), d.hidden_pad, d.rows, d.hidden, part, v);
+    few_rows<T, NR < 4 ? 4 : 2, NR, 1, WIDTH>(wp, valid, static_cast<const T*>(d.h), d.hidden_pad, d.rows, d.hidden, part, v);
     const int row = (w >> 2) * 16 + (lane & 15), o = f0 + 4 * (lane >> 4) + (w & 3);
     if (w >= 4 * NR || row >= d.rows || o >= d.out) return;
     static_cast<T*>(d.y)[(int64_t)row * d.y_stride + o] = (T)(v[0][0] + (d.down_bias ? (float)static_cast<const T*>(d.down_bias)[o] : 0.0f));
@@ -330,39 +324,51 @@ __global__ __launch_bounds__(X::THREADS, 2) void k_feed_grad(FeedDev d, GemmJob 
     tile_of(job, xcd_order(blockIdx.x, gridDim.x), f, r);
     const float scale = gradient_scale<T>(d.largest);
     X::run(job, f * X::TF, r * X::TR, 0, (job.len + X::PART - 1) / X::PART, lds, acc, sums);
-    const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6;
-    const int f0 = f * X::TF + (w % X::WF) * X::NM * 32, r0 = r * X::TR + (w / X::WF) * X::NX * 32 + (lane & 31);
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int f0 = f * X::TF + (w % X::WF) * X::NM * 32, r0 = r * X::TR + (w / X::WF) * X::NX * 32;
+    constexpr int CM = X::NM < 2 ? 1 : 2, P = CM * 4;        // 64 features at a time: 128 bytes of a row
+    char* own = lds + w * CM * 2048;
 #pragma unroll
-    for (int m = 0; m < X::NM; ++m) {
+    for (int j = 0; j < X::NX; ++j) {
 #pragma unroll
-        for (int j = 0; j < X::NX; ++j) {
-            const int row = r0 + j * 32;
-            const int64_t base = (int64_t)(row < d.rows ? row : 0) * d.hidden_pad;
-            f32x16 du;
+        for (int c = 0; c < X::NM; c += CM) {
+            // Both projections, in the order in which they lie, then through LDS to the lanes that hold their places.
+            const int fc = f0 + c * 32;
+            uint4 g[P / 2], u[P / 2];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int at = f0 + m * 32 + q * 8 + half * 4;
-                t4 g = {}, u = {};
-                if (row < d.rows && at < d.hidden_pad) {
-                    g = *reinterpret_cast<const t4*>(static_cast<const T*>(d.g) + base + at);
-                    u = *reinterpret_cast<const t4*>(static_cast<const T*>(d.u) + base + at);
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float2 a = activate_grad<ACT>((float)g[e]);
-                    const float dh = acc[m][j][4 * q + e] * scale;
-                    du[4 * q + e] = dh * a.x;
-                    acc[m][j][4 * q + e] = dh * (float)u[e] * a.y;
+            for (int i = 0; i < P / 2; ++i) {
+                const int at = i * 64 + lane, row = r0 + j * 32 + at / P, col = fc + at % P * 8;
+                g[i] = u[i] = make_uint4(0, 0, 0, 0);
+                if (row < d.rows && col < d.hidden_pad) {
+                    g[i] = *reinterpret_cast<const uint4*>(static_cast<const T*>(d.g) + (int64_t)row * d.hidden_pad + col);
+                    u[i] = *reinterpret_cast<const uint4*>(static_cast<const T*>(d.u) + (int64_t)row * d.hidden_pad + col);
                 }
             }
+            t4 pg[CM][4];
+            f32x16 du[CM];
+            from_lds<CM>(own, lane, g, pg);
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const int at = f0 + m * 32 + q * 16 + half * 8;
-                const Pack8<T> pz = gather8<T>(acc[m][j], q, 1.0f), pu = gather8<T>(du, q, 1.0f);
-                if (row >= d.rows || at >= d.hidden_pad) continue;
-                store_padded(static_cast<T*>(d.dz) + base + at, pz, d.hidden - at);
-                store_padded(static_cast<T*>(d.du) + base + at, pu, d.hidden - at);
-            }
+            for (int m = 0; m < CM; ++m)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float2 a = activate_grad<ACT>((float)pg[m][i >> 2][i & 3]);
+                    const float dh = acc[c + m][j][i] * scale;
+                    du[m][i] = dh * a.x;
+                    acc[c + m][j][i] = dh * a.y;
+                }
+            from_lds<CM>(own, lane, u, pg);
+#pragma unroll
+            for (int m = 0; m < CM; ++m)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[c + m][j][i] *= (float)pg[m][i >> 2][i & 3];
+            auto store = [&](void* to, auto value) {
+                through_lds<T, CM>(own, lane, value, [&](int row, int at, const Pack8<T>& v) {
+                    if (r0 + j * 32 + row < d.rows && fc + at < d.hidden_pad)
+                        store_padded(static_cast<T*>(to) + (int64_t)(r0 + j * 32 + row) * d.hidden_pad + fc + at, v, d.hidden - fc - at);
+                });
+            };
+            store(d.dz, [&](int m, int q) { return gather8<T>(acc[c + m][j], q, 1.0f); });
+            store(d.du, [&](int m, int q) { return gather8<T>(du[m], q, 1.0f); });
         }
     }
 }
@@ -396,30 +402,28 @@ __global__ __launch_bounds__(X::THREADS, 2) void k_feed_weights(WeightsDev d) {
     const int parts = (job.len + X::PART - 1) / X::PART;
     X::run(job, f * X::TF, r * X::TR, (int)((int64_t)parts * split / d.splits), (int)((int64_t)parts * (split + 1) / d.splits), lds, acc, sums);
     const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6;
-    const int f0 = f * X::TF + (w % X::WF) * X::NM * 32, r0 = r * X::TR + (w / X::WF) * X::NX * 32 + (lane & 31);
+    const int f0 = f * X::TF + (w % X::WF) * X::NM * 32, r0 = r * X::TR + (w / X::WF) * X::NX * 32;
     const bool has_sums = d.bias[n] && f == 0 && w % X::WF == 0;
     if (d.splits == 1) {
         const float s = d.largest[n] ? 1.0f / gradient_scale<T>(d.largest[n]) : 1.0f;
 #pragma unroll
         for (int j = 0; j < X::NX; ++j) {
-            const int row = r0 + j * 32;
+            const int own = r0 + j * 32 + (lane & 31);
             const float sum = sums[j] + __shfl_xor(sums[j], 32);
-            if (has_sums && half == 0 && row < job.rows) static_cast<T*>(d.bias[n])[row] = (T)(sum * s);
-#pragma unroll
-            for (int m = 0; m < X::NM; ++m)
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    const int at = f0 + m * 32 + q * 16 + half * 8;
-                    const Pack8<T> p = gather8<T>(acc[m][j], q, s);
-                    if (row < job.rows) store8(static_cast<T*>(d.out[n]) + (int64_t)row * job.features + at, p, job.features - at);
-                }
+            if (has_sums && half == 0 && own < job.rows) static_cast<T*>(d.bias[n])[own] = (T)(sum * s);
+            through_lds<T, X::NM>(lds + w * X::NM * 2048, lane, [&](int m, int q) { return gather8<T>(acc[m][j], q, s); },
+                                  [&](int row, int at, const Pack8<T>& v) {
+                                      if (r0 + j * 32 + row < job.rows)
+                                          store8(static_cast<T*>(d.out[n]) + (int64_t)(r0 + j * 32 + row) * job.features + f0 + at, v,
+                                                 job.features - f0 - at);
+                                  });
         }
     } else {
         const int pad = padded(job.features) + 8;
         float* out = d.parts + d.part[n] + (int64_t)split * job.rows * pad;
 #pragma unroll
         for (int j = 0; j < X::NX; ++j) {
-            const int row = r0 + j * 32;
+            const int row = r0 + j * 32 + (lane & 31);
             const float sum = sums[j] + __shfl_xor(sums[j], 32);
             if (has_sums && half == 0 && row < job.rows) out[(int64_t)row * pad + pad - 8] = sum;
 #pragma unroll

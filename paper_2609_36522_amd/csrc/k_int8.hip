@@ -115,31 +115,38 @@ __global__ __launch_bounds__(X::THREADS, 2) void k_int8_tile(Int8Dev d, GemmJob 
     tile_of(job, xcd_order(blockIdx.x, gridDim.x), f, r);
     X::run(job, f * X::TF, r * X::TR, 0, (job.len + X::PART - 1) / X::PART, lds, acc, none);
     const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6;
-    const int f0 = f * X::TF + (w % X::WF) * X::NM * 32, r0 = r * X::TR + (w / X::WF) * X::NX * 32 + (lane & 31);
+    const int f0 = f * X::TF + (w % X::WF) * X::NM * 32, r0 = r * X::TR + (w / X::WF) * X::NX * 32;
     float xs[X::NX];
 #pragma unroll
-    for (int j = 0; j < X::NX; ++j) xs[j] = r0 + j * 32 < d.rows ? d.x_scale[r0 + j * 32] : 0.0f;
+    for (int j = 0; j < X::NX; ++j) {
+        const int row = r0 + j * 32 + (lane & 31);
+        xs[j] = row < d.rows ? d.x_scale[row] : 0.0f;
+    }
+    constexpr int CM = X::NM < 2 ? 1 : 2;                    // 64 features at a time: 128 bytes of a row
 #pragma unroll
-    for (int m = 0; m < X::NM; ++m) {
-        float ws[16], bias[16];
+    for (int c = 0; c < X::NM; c += CM) {
+        const int fc = f0 + c * 32;
+        float ws[CM][16], bias[CM][16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int at = f0 + m * 32 + 8 * (i >> 2) + 4 * half + (i & 3), c = at < d.out ? at : d.out - 1;
-            ws[i] = d.w_scale[c];
-            bias[i] = d.bias ? (float)static_cast<const T*>(d.bias)[c] : 0.0f;
-        }
+        for (int m = 0; m < CM; ++m)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int at = fc + m * 32 + 8 * (i >> 2) + 4 * half + (i & 3), o = at < d.out ? at : d.out - 1;
+                ws[m][i] = d.w_scale[o];
+                bias[m][i] = d.bias ? (float)static_cast<const T*>(d.bias)[o] : 0.0f;
+            }
 #pragma unroll
         for (int j = 0; j < X::NX; ++j) {
-            f32x16 v;
+            f32x16 v[CM];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = (float)acc[m][j][i] * xs[j] * ws[i] + bias[i];
-            const int row = r0 + j * 32;
+            for (int m = 0; m < CM; ++m)
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const int at = f0 + m * 32 + q * 16 + half * 8;
-                const Pack8<T> p = gather8<T>(v, q, 1.0f);
-                if (row < d.rows) store8(static_cast<T*>(d.y) + (int64_t)row * d.y_stride + at, p, d.out - at);
-            }
+                for (int i = 0; i < 16; ++i) v[m][i] = (float)acc[c + m][j][i] * xs[j] * ws[m][i] + bias[m][i];
+            through_lds<T, CM>(lds + w * CM * 2048, lane, [&](int m, int q) { return gather8<T>(v[m], q, 1.0f); },
+                               [&](int row, int at, const Pack8<T>& p) {
+                                   if (r0 + j * 32 + row < d.rows)
+                                       store8(static_cast<T*>(d.y) + (int64_t)(r0 + j * 32 + row) * d.y_stride + fc + at, p, d.out - fc - at);
+                               });
         }
     }
 }

@@ -42,6 +42,19 @@ __device__ __forceinline__ i32x4 mma16(i32x4 a, i32x4 b, i32x4 c) {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
 }
 
+// load_lds (pa_ops_device.h) without the compiler's own bookkeeping, which takes a transposing LDS load for one that
+// may read what any load in flight writes and has it wait for all of them (dz G + du U of 8192x1024x4096: 263 us so,
+// 158 without). The waits are this file's: wait_loads and a barrier before a buffer is read. The load has no output
+// register; a wait that the compiler places for loads of its own can only become stricter by it.
+__device__ __forceinline__ void load_lds_untracked(const void* from, void* lds, uint32_t off) {
+    typedef __attribute__((address_space(3))) void lds_void;
+    const uint64_t a = reinterpret_cast<uint64_t>(from);
+    const i32x4 rsrc = {(int)(uint32_t)a, (int)((uint32_t)(a >> 32) & 0xffffu), (int)kBufferBytes, 0x00020000};
+    __builtin_assume(lds != nullptr);
+    const uint32_t to = __builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(lds_void*)lds);
+    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(to), "v"(off), "s"(rsrc));
+}
+
 // One product: F and R in one or two segments of `len` reduction elements each (the second follows the
 // first; same strides).
 struct GemmJob {
@@ -55,7 +68,7 @@ struct GemmJob {
 // (piece_at<64>) is in the addresses that are read: a wave's lanes fill consecutive 16-byte slots.
 // A kCol tile is SIZE / 64 tiles of 64 k x 64 columns. UNIT > 0: two matrices, whose rows alternate in
 // groups of UNIT.
-template <class T, int SIZE, int THREADS, bool COL, int UNIT = 0>
+template <class T, int SIZE, int THREADS, bool COL, int UNIT = 0, bool UNTRACKED = false>
 struct Loads {
     static constexpr int kPieces = SIZE * 8 / THREADS, kStep = THREADS / 8, kPer = 16 / sizeof(T);
     static_assert(kPieces * THREADS == SIZE * 8 && (!COL || sizeof(T) == 2));
@@ -80,26 +93,21 @@ struct Loads {
             }
         }
     }
-    // The part at `base` (UNIT: and at `other`), of whose k `left` exist.
-    __device__ __forceinline__ void load(const T* base, const T* other, int left, void* tile) const {
-        constexpr int PART = COL ? 64 : 128 / (int)sizeof(T);
-        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const __amdgpu_buffer_rsrc_t from = buffer_at(base), from2 = buffer_at(UNIT ? other : base);
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int k = COL ? at + (THREADS < 512 ? (i & 1) * 32 : 0) : at;
-            const bool second = UNIT && (i * kStep / (UNIT ? UNIT : 1)) % 2;
-            load_lds(second ? from2 : from, static_cast<char*>(tile) + (w * 64 + i * THREADS) * 16,
-                     left >= PART || k < left ? off[i] : kNowhere, 0);
-        }
+    // The i-th piece of the part at `base` (UNIT: and at `other`), of whose k `left` exist; w: the wave.
+    __device__ __forceinline__ void load(const T* base, const T* other, int left, char* tile, int w, int i) const {
+        const int k = COL && THREADS < 512 ? at + (i & 1) * 32 : at;
+        const bool second = UNIT && (i * kStep / (UNIT ? UNIT : 1)) % 2;
+        const uint32_t at_byte = k < left ? off[i] : kNowhere;
+        if constexpr (UNTRACKED) load_lds_untracked(second ? other : base, tile + (w * 64 + i * THREADS) * 16, at_byte);
+        else load_lds(buffer_at(second ? other : base), tile + (w * 64 + i * THREADS) * 16, at_byte, 0);
     }
     // 8 bits: what of the part lies past the row's end (in a piece that holds it) becomes zero.
-    __device__ __forceinline__ void trim(int left, void* tile) const {
+    __device__ __forceinline__ void trim(int left, char* tile) const {
         const int n = left - at;
         if (n <= 0 || n >= kPer) return;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
-            char* p = static_cast<char*>(tile) + ((int)threadIdx.x + i * THREADS) * 16;
+            char* p = tile + ((int)threadIdx.x + i * THREADS) * 16;
 #pragma unroll
             for (int j = 1; j < 16; ++j)
                 if (j >= n) p[j] = 0;
@@ -153,100 +161,172 @@ struct Tile {
     static constexpr int PART = FCOL || RCOL ? 64 : 128 / (int)sizeof(T);
     static_assert(!(FCOL || RCOL) || sizeof(T) == 2);
     static constexpr int BYTES = STAGES * (TF + TR) * 128;
-    typedef Loads<T, TF, THREADS, FCOL, UNIT> LF;
-    typedef Loads<T, TR, THREADS, RCOL> LR;
+    typedef Loads<T, TF, THREADS, FCOL, UNIT, FCOL || RCOL> LF;
+    typedef Loads<T, TR, THREADS, RCOL, 0, FCOL || RCOL> LR;
+
+    static constexpr int LOADS = LF::kPieces + LR::kPieces;      // a thread's loads of one part
+    static constexpr int HALF = (LOADS + 1) / 2;
 
     // Accumulates parts `first` .. `last` - 1 of the job's tile at feature f0, row r0 into acc (and, SUMS, the
-    // sums over k of the lane's rows of R into sums, of which the other half of the wave has the rest).
+    // sums over k of the lane's rows of R into sums, of which the other half of the wave has the rest). All of the
+    // block's reads of LDS are done when it returns.
+    //
+    // A part is four steps. During a step's products the next step's operands are read, two of them and one load a
+    // product, in the order in which they are written here. Before the last step the next part has to be there and
+    // all waves be done with this one's buffer: its loads are issued then and in the step after.
+    // 32768x2048x8192 in bf16, the times of this loop's forms: loads at the start of a part and a wait at its end
+    // 1010 us, the wait before the last step 927, loads and reads between the products 895; without any loads
+    // 791, without loads and reads 712 (power); four waves of 128 x 128 902, parts of 32 columns 960.
     __device__ __forceinline__ static void run(const GemmJob& job, int f0, int r0, int first, int last, char* lds, acc_t (&acc)[NM][NX],
                                                float (&sums)[NX]) {
         const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int fg = (w % WF) * NM, rg = (w / WF) * NX;
-        const int seg_parts = (job.len + PART - 1) / PART;
+        const int seg_parts = (job.len + PART - 1) / PART, parts = last - first;
         const LF lf(job.f_stride, job.features - f0);
         const LR lr(job.r_stride, job.rows - r0);
-        auto left_of = [&](int part) { return job.len - (part >= seg_parts ? part - seg_parts : part) * PART; };
-        auto load = [&](int part, int p) {
+        // Pieces lo .. hi - 1 of a part into buffer p.
+        auto load = [&](int part, int p, int lo, int hi) {
             const bool second = !GATED && part >= seg_parts;
             const int64_t k0 = (int64_t)(second ? part - seg_parts : part) * PART;
             const int left = job.len - (int)k0;
             const int64_t fo = FCOL ? k0 * job.f_stride + f0 : f0 * job.f_stride + k0;
             const int64_t ro = RCOL ? k0 * job.r_stride + r0 : r0 * job.r_stride + k0;
+            const T* fb = static_cast<const T*>(job.f[second]) + fo;
+            const T* fb2 = GATED ? static_cast<const T*>(job.f[1]) + fo : nullptr;
+            const T* rb = static_cast<const T*>(job.r[second]) + ro;
             char* tile = lds + p * (TF + TR) * 128;
-            lf.load(static_cast<const T*>(job.f[second]) + fo, GATED ? static_cast<const T*>(job.f[1]) + fo : nullptr, left, tile);
-            lr.load(static_cast<const T*>(job.r[second]) + ro, nullptr, left, tile + TF * 128);
+#pragma unroll
+            for (int x = lo; x < hi && x < LOADS; ++x) {
+                if (x < LF::kPieces) lf.load(fb, fb2, left, tile, w, x);
+                else lr.load(rb, nullptr, left, tile + TF * 128, w, x - LF::kPieces);
+            }
         };
+        // 8 bits: the end of the reduction, in the thread's own pieces, once they are there.
         auto arrive = [&](int part, int p) {
             if constexpr (sizeof(T) == 1) {
-                if (left_of(part) < PART) lr.trim(left_of(part), lds + (p * (TF + TR) + TF) * 128);
+                const int left = job.len - part * PART;
+                if (left < PART) lr.trim(left, lds + (p * (TF + TR) + TF) * 128);
             }
         };
-        auto multiply = [&](int p) {
+        // Operands in the order of their use.
+        v a[2][NM], b[2][NX];
+        auto read = [&](int p, int ks, int s, int x) {
             const char* ft = lds + p * (TF + TR) * 128;
             const char* rt = ft + TF * 128;
-            // The operands of the next step are read while those of the current one are multiplied.
-            v a[2][NM], b[2][NX];
-            auto read = [&](int ks) {
+            if (x == 0) a[s][0] = read_operand<T, FCOL>(ft, fg, ks, lane);
+            else if (x <= NX) b[s][x - 1] = read_operand<T, RCOL>(rt, rg + x - 1, ks, lane);
+            else a[s][x - NX] = read_operand<T, FCOL>(ft, fg + x - NX, ks, lane);
+        };
+        // A step's products, reads of step ks of buffer p for the next one, pieces lo .. hi - 1 of a part into buffer q.
+        constexpr int G = NM * NX, READS = NM + NX, AT_ONCE = READS > 2 * G ? READS : 2;
+        auto step = [&](int s, bool next, int p, int ks, int part, int q, int lo, int hi) {
 #pragma unroll
-                for (int m = 0; m < NM; ++m) a[ks & 1][m] = read_operand<T, FCOL>(ft, fg + m, ks, lane);
+            for (int g = 0; g < G; ++g) {
+                if (next) {
 #pragma unroll
-                for (int j = 0; j < NX; ++j) b[ks & 1][j] = read_operand<T, RCOL>(rt, rg + j, ks, lane);
-            };
-            read(0);
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks) {
-                if (ks < 3) read(ks + 1);
-                if constexpr (SUMS) {
-#pragma unroll
-                    for (int j = 0; j < NX; ++j) sums[j] = sum8(b[ks & 1][j], sums[j]);
+                    for (int x = g * AT_ONCE; x < (g + 1) * AT_ONCE && x < READS; ++x) read(p, ks, s ^ 1, x);
                 }
+                if (hi > lo) load(part, q, lo + (hi - lo) * g / G, lo + (hi - lo) * (g + 1) / G);
+                acc[g / NX][g % NX] = mma(a[s][g / NX], b[s][g % NX], acc[g / NX][g % NX]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if constexpr (SUMS) {
 #pragma unroll
-                for (int m = 0; m < NM; ++m)
-#pragma unroll
-                    for (int j = 0; j < NX; ++j) acc[m][j] = mma(a[ks & 1][m], b[ks & 1][j], acc[m][j]);
-                if (ks < 3) {
-                    constexpr int READS = NM * (FCOL ? 2 : 1) + NX * (RCOL ? 2 : 1);
-                    constexpr int EACH = READS > NM * NX ? (READS + NM * NX - 1) / (NM * NX) : 1;
-#pragma unroll
-                    for (int g = 0; g < NM * NX; ++g) {
-                        __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);     // LDS reads
-                        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);        // a product
-                    }
-                }
+                for (int j = 0; j < NX; ++j) sums[j] = sum8(b[s][j], sums[j]);
             }
         };
-        constexpr int LOADS = LF::kPieces + LR::kPieces;      // a thread's loads of one part
-        const int parts = last - first;
 #pragma unroll
         for (int i = 0; i < STAGES - 1; ++i)
-            if (i < parts) load(first + i, i);
+            if (i < parts) load(first + i, i, 0, LOADS);
         if (parts >= STAGES - 1) wait_loads<(STAGES - 2) * LOADS>();
         else wait_loads();
         if (parts > 0) arrive(first, 0);
         lds_barrier();
-        int p = 0;
-        for (int i = 0; i < parts; ++i) {
-            int q = p + STAGES - 1;
-            if (q >= STAGES) q -= STAGES;
-            if (i + STAGES - 1 < parts) load(first + i + STAGES - 1, q);
-            multiply(p);
-            if (i + 1 < parts) {
-                if (i + STAGES - 1 < parts) wait_loads<(STAGES - 2) * LOADS>();      // the next part is there
-                else wait_loads();
-                arrive(first + i + 1, p + 1 == STAGES ? 0 : p + 1);
-            }
+        if (parts <= 0) return;
+#pragma unroll
+        for (int x = 0; x < READS; ++x) read(0, 0, 0, x);
+        if (STAGES - 1 < parts) load(first + STAGES - 1, STAGES - 1, 0, HALF);
+        int p = 0, q = STAGES - 1, i = 0;            // q: the buffer of part i + STAGES - 1, whose second half is to come
+        for (; i + STAGES < parts; ++i) {
+            const int n = p + 1 == STAGES ? 0 : p + 1;
+            step(0, true, p, 1, first + i + STAGES - 1, q, HALF, LOADS);
+            step(1, true, p, 2, 0, 0, 0, 0);
+            step(0, true, p, 3, 0, 0, 0, 0);
+            wait_loads<(STAGES - 2) * LOADS>();
+            arrive(first + i + 1, n);
             lds_barrier();
-            if (++p == STAGES) p = 0;
+            __builtin_amdgcn_sched_barrier(0);
+            step(1, true, n, 0, first + i + STAGES, p, 0, HALF);
+            q = p;
+            p = n;
+        }
+        if (i + STAGES - 1 < parts) load(first + i + STAGES - 1, q, HALF, LOADS);
+        for (; i < parts; ++i) {
+            const int n = p + 1 == STAGES ? 0 : p + 1;
+            step(0, true, p, 1, 0, 0, 0, 0);
+            step(1, true, p, 2, 0, 0, 0, 0);
+            step(0, true, p, 3, 0, 0, 0, 0);
+            wait_loads();
+            if (i + 1 < parts) arrive(first + i + 1, n);
+            lds_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+            step(1, i + 1 < parts, n, 0, 0, 0, 0, 0);
+            p = n;
         }
     }
 };
 
-// The tile of block `id` of a job: groups of 4 row tiles side by side, features before the next group, so that the
-// blocks that run together on an XCD share rows of both operands in its L2.
+// Stores of 32 rows x 32 NM features that a wave has in its accumulators: through LDS, so that consecutive lanes store
+// consecutive features (straight from the registers every row got 32 bytes at a time, and partly written lines cost a
+// quarter of a product of 1024 columns). `lds`: the wave's own NM * 2 KB. value(m, q): eight features (Pack8) from
+// 32 m + 16 q + 8 half; put(row, feature, piece): stores a piece of row 0 .. 31 at feature 0, 8 ..
+template <int P>
+__device__ __forceinline__ int slot_of(int r, int piece) {       // rows of P pieces, whose order is permuted by the row
+    return r * P + (piece ^ (r / (16 / (P < 16 ? P : 16)) % P));
+}
+template <class T, int NM, class F, class S>
+__device__ __forceinline__ void through_lds(char* lds, int lane, F value, S put) {
+    constexpr int P = NM * 4;
+    const int half = lane >> 5, row = lane & 31;
+#pragma unroll
+    for (int m = 0; m < NM; ++m)
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+            *reinterpret_cast<uint4*>(lds + slot_of<P>(row, m * 4 + q * 2 + half) * 16) = __builtin_bit_cast(uint4, value(m, q));
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < P / 2; ++i) {
+        const int at = i * 64 + lane, r = at / P, piece = at % P;
+        put(r, piece * 8, __builtin_bit_cast(Pack8<T>, *reinterpret_cast<const uint4*>(lds + slot_of<P>(r, piece) * 16)));
+    }
+    __builtin_amdgcn_wave_barrier();
+}
+
+// The other way: pieces of 32 rows x 32 NM features, lane after lane in the order in which they lie, to the places of
+// accumulator registers: out[m][q] are features 32 m + 8 q + 4 half .. + 3 of row lane % 32.
+template <int NM, class V>
+__device__ __forceinline__ void from_lds(char* lds, int lane, const uint4 (&in)[NM * 2], V (&out)[NM][4]) {
+    constexpr int P = NM * 4;
+    const int half = lane >> 5, row = lane & 31;
+#pragma unroll
+    for (int i = 0; i < P / 2; ++i) *reinterpret_cast<uint4*>(lds + slot_of<P>((i * 64 + lane) / P, (i * 64 + lane) % P) * 16) = in[i];
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int m = 0; m < NM; ++m)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) out[m][q] = *reinterpret_cast<const V*>(lds + slot_of<P>(row, m * 4 + q) * 16 + half * 8);
+    __builtin_amdgcn_wave_barrier();
+}
+
+// The tile of block `id` of a job: groups of a few row tiles side by side, features before the next group, so that the
+// 32 blocks that run together on an XCD form about a square and share rows of both operands in its L2. us with groups
+// of 2, 4, 6, 8 and 16 row tiles: 32768x16384x2048 (64 feature tiles) 1826, 1904, 1800, 1886, 2325; 32768x2048x8192
+// (8) 895, 895, 926, 927, 1000.
 __device__ __forceinline__ void tile_of(const GemmJob& job, int id, int& f, int& r) {
-    const int per = 4 * job.f_tiles, g = id / per, in = id - g * per, rows = job.r_tiles - g * 4 < 4 ? job.r_tiles - g * 4 : 4;
+    const int group = job.f_tiles > 8 ? 6 : job.f_tiles > 4 ? 4 : 8;
+    const int per = group * job.f_tiles, g = id / per, in = id - g * per, rows = job.r_tiles - g * group < group ? job.r_tiles - g * group : group;
     f = in / rows;
-    r = g * 4 + in - f * rows;
+    r = g * group + in - f * rows;
 }
 
 }  // namespace pa
