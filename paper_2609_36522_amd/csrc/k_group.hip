@@ -1,18 +1,21 @@
 // Group norm with an activation over channels-last tensors, forward and backward, for gfx950.
 //
 // A block takes a run of pixels (a chunk) of one sample and all or a slab of its channels: whole groups, so that
-// memory is read in the order in which it lies. A thread owns 8 consecutive channels of every PP-th pixel; what
+// memory is read in the order in which it lies. A thread owns 8 consecutive channels of every `lanes`-th pixel; what
 // belongs to a channel (weight, bias, its group's statistics) stays in its registers.
 //
-// Statistics: a chunk's values stay in registers, so that its groups' means and then the sums of squared
-// differences from them are two passes over registers (no cancellation between a sum of squares and a squared
-// sum). Chunks are joined by their means' distances from the group's. A slab whose pixels fit one block's registers
-// is done in one launch; otherwise the chunks' statistics go to `part`, and a second launch joins them and
-// normalizes.
+// Statistics: a thread takes a batch of pixels at a time, whose mean and sum of squared differences from it are two
+// passes over registers, and joins them to what it has by the distance of the means; so do threads and then
+// chunks (no cancellation between a sum of squares and a squared sum anywhere). A slab whose pixels fit one
+// block's registers is done in one launch; otherwise the chunks' statistics go to `part`, and a second launch joins
+// them and normalizes.
 //
 // Backward: dx needs two sums over the group (g = dz w; g and g xh), which are sums over its channels of
 // w times the channel's sums of dz and dz xh over pixels; those are dbias and dweight of the sample. So one pass
-// over x and dy gives all sums, a small launch joins them, and a second pass writes dx.
+// over x and dy gives all sums, a small launch joins them, and a second pass writes dx (and joins the samples'
+// sums). Slabs that fit registers take one launch, and one for the samples' sums.
+#include <type_traits>
+
 #include "pa_act.h"
 #include "pa_ops_device.h"
 
@@ -23,233 +26,338 @@ namespace {
 constexpr int kBlock = 512, kWaves = kBlock / 64;
 constexpr int kMaxGroups = 512;          // groups of a slab
 constexpr int kMaxSlab = kBlock * 8;     // channels of a slab
+constexpr int kBatch = 4;                // pixels that a thread takes at a time
 
-// Pixels that a thread's registers hold: 64 (16 bits) or 32 registers of x.
-template <class T> constexpr int kHeld = sizeof(T) == 2 ? 16 : 8;
-int held(int dtype) { return dtype == PA_F32 ? 8 : 16; }
+// a / b of whole numbers below 2^20 by b's reciprocal in fp32: (a + 1/2) / b is at least 1 / (2 b) from a whole number,
+// relative to itself 2^-21, and the product's two roundings are 2^-23.
+__device__ __forceinline__ int divided(int a, float inverse) { return (int)(((float)a + 0.5f) * inverse); }
 
 // The block's place: its sample, channels c0 .. c0 + n - 1 and pixels p0 .. p1 - 1; the thread's piece of 8 channels
-// and its first pixel (pixels beyond the last one where the thread has none).
+// (at c), the slab's group of the first of them and its place in the group, and the first of the thread's pixels.
 struct Place {
-    int b, c0, n, pieces, lanes, c, lane, p0, p1, own;
-    __device__ __forceinline__ explicit Place(const GroupDev& d) {
-        b = blockIdx.z;
-        c0 = blockIdx.y * d.slab;
-        n = d.channels - c0 < d.slab ? d.channels - c0 : d.slab;
+    int b, c0, n, pieces, lanes, c, lane, p0, p1, groups, first, inside;
+    bool own;                            // whether the thread has a piece
+    __device__ __forceinline__ Place(const GroupDev& d, int chunk, int size, int slab, int sample) : b(sample) {
+        c0 = slab * d.slab;
+        const bool last = d.channels - c0 < d.slab;
+        n = last ? d.channels - c0 : d.slab;
+        groups = divided(n, d.per_width);
         pieces = (n + 7) / 8;
-        lanes = kBlock / pieces;             // threads of a piece
-        lane = (int)threadIdx.x / pieces;
+        const float per_pieces = 1.0f / (float)pieces;
+        lanes = divided(kBlock, per_pieces);      // threads of a piece
+        lane = divided((int)threadIdx.x, per_pieces);
         c = ((int)threadIdx.x - lane * pieces) * 8;
-        p0 = (int)blockIdx.x * d.chunk;
-        p1 = d.pixels - p0 < d.chunk ? d.pixels : p0 + d.chunk;
-        own = lane < lanes ? 1 : 0;
+        first = divided(c, d.per_width);
+        inside = c - first * d.width;
+        p0 = chunk * size;
+        p1 = d.pixels - p0 < size ? d.pixels : p0 + size;
+        own = lane < lanes;
+    }
+    // f(i, group within the slab) of the thread's 8 channels; those past the slab count as the last group's.
+    template <class F>
+    __device__ __forceinline__ void each_group(const GroupDev& d, F f) const {
+        int g = first, r = inside;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            f(i, g < groups ? g : groups - 1);
+            if (++r == d.width) {
+                r = 0;
+                ++g;
+            }
+        }
     }
 };
 
-// Row `p` of a tensor at this block's channels.
 template <class T>
-__device__ __forceinline__ const T* row_at(const void* x, const int64_t (&s)[2], const Place& q, int p) {
-    return static_cast<const T*>(x) + q.b * s[0] + p * s[1] + q.c0;
+__device__ __forceinline__ T* row_at(const void* x, const int64_t (&s)[2], const Place& q, int p) {
+    return const_cast<T*>(static_cast<const T*>(x)) + q.b * s[0] + p * s[1] + q.c0;
 }
 
-// A channel's sums over the threads of its piece, then over the channels of each group, in a fixed order:
-// v[8] of every thread -> group[g]. `lds` holds kBlock * 8 floats and kBlock + kMaxSlab after them.
-__device__ __forceinline__ void channel_sums(const Place& q, const float (&v)[8], float* lds, float* channel) {
-    // [lane][channel]
-    const int width = q.pieces * 8;
+// Index of the slab's first group among all samples'.
+__device__ __forceinline__ int64_t group_at(const GroupDev& d, const Place& q) { return (int64_t)q.b * d.groups + divided(q.c0, d.per_width); }
+
+// The thread's piece of an existing pixel: fetch starts the load (slabs of whole pieces, of 8 or more channels, or
+// smaller ones), mend puts a piece that holds the slab's end into place.
+template <class T, int WIDTH>
+__device__ __forceinline__ Pack8<T> fetch(const T* row, const Place& q) {
+    if constexpr (WIDTH == kWhole) return *reinterpret_cast<const Pack8<T>*>(row + q.c);
+    if constexpr (WIDTH == kRagged) return load8_raw(row, q.c, q.n);
+    return load8(row, q.c, q.n);
+}
+template <class T, int WIDTH>
+__device__ __forceinline__ Pack8<T> mend(const Pack8<T>& r, const Place& q) {
+    if constexpr (WIDTH == kRagged) return fix8(r, q.c, q.n);
+    return r;
+}
+
+// R pixels of the thread from `p` on, `lanes` apart; beyond the chunk's last one, which stands in for them, nothing is
+// counted by the callers.
+template <class T, int WIDTH, int R>
+__device__ __forceinline__ void fetch_pixels(const void* x, const int64_t (&s)[2], const Place& q, int p, Pack8<T> (&out)[R]) {
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        const int at = p + k * q.lanes;
+        out[k] = fetch<T, WIDTH>(row_at<T>(x, s, q, at < q.p1 ? at : q.p1 - 1), q);
+    }
+}
+
+// Eight of a parameter's values as they lie in memory, so that their load can be in flight, and as numbers.
+struct Raw {
+    uint4 lo, hi;
+};
+template <int WIDTH>
+__device__ __forceinline__ Raw load_parameters(const GroupDev& d, const void* p, const Place& q) {
+    Raw r{};
+    if (!p) return r;
+    if (d.param_dtype == PA_F32) return __builtin_bit_cast(Raw, fetch<float, WIDTH>(static_cast<const float*>(p) + q.c0, q));
+    r.lo = __builtin_bit_cast(uint4, fetch<__bf16, WIDTH>(static_cast<const __bf16*>(p) + q.c0, q));
+    return r;
+}
+template <int WIDTH>
+__device__ __forceinline__ void numbers(const GroupDev& d, const void* p, const Raw& r, const Place& q, float otherwise, float (&v)[8]) {
+    if (!p) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = otherwise;
+    } else if (d.param_dtype == PA_F32) {
+        const Pack8<float> t = mend<float, WIDTH>(__builtin_bit_cast(Pack8<float>, r), q);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = t.v[i];
+    } else {
+        const Pack8<__bf16> t = mend<__bf16, WIDTH>(__builtin_bit_cast(Pack8<__bf16>, r.lo), q);
+        const Pack8<_Float16> h = __builtin_bit_cast(Pack8<_Float16>, t);
+        const bool bf = d.param_dtype == PA_BF16;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = bf ? (float)t.v[i] : (float)h.v[i];
+    }
+}
+
+// The activation is the same for all: one branch for 8 values.
+__device__ __forceinline__ void activate8(int act, float (&v)[8]) {
+    if (act == PA_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = activate<PA_ACT_SILU>(v[i]);
+    } else if (act == PA_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = activate<PA_ACT_GELU>(v[i]);
+    }
+}
+__device__ __forceinline__ void slope8(int act, float (&v)[8]) {       // its derivative
+    if (act == PA_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = activate_grad<PA_ACT_SILU>(v[i]).y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = activate_grad<PA_ACT_GELU>(v[i]).y;
+    }
+}
+
+// Sums over the threads and channels of each group of the slab, a wave a group, in a fixed order. `lds`: kBlock * 8
+// floats, free before and after.
+__device__ __forceinline__ void group_sums(const GroupDev& d, const Place& q, const float (&v)[8], float* lds, float* group) {
+    const int width = q.pieces * 8, L = d.width;
     if (q.own) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) lds[q.lane * width + q.c + i] = v[i];
     }
     __syncthreads();
-    // Where there are more threads than channels, several take a channel's lanes in turn.
-    const int turns = width < kBlock ? kBlock / width : 1;
-    for (int i = threadIdx.x; i < width * turns; i += kBlock) {
-        const int t = i / width, c = i - t * width;
+    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int total = q.lanes * L;               // at most 4096: value k is channel k % L of lane k / L
+    for (int g = w; g < q.groups; g += kWaves) {
         float s = 0.0f;
-        for (int l = t; l < q.lanes; l += turns) s += lds[l * width + c];
-        channel[i] = s;
-    }
-    __syncthreads();
-    if (turns > 1) {
-        for (int c = threadIdx.x; c < width; c += kBlock) {      // at most one a thread
-            float s = 0.0f;
-            for (int t = 0; t < turns; ++t) s += channel[t * width + c];
-            lds[c] = s;
+        for (int k0 = lane; k0 < total; k0 += 256) {
+            float t[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int k = k0 + 64 * j < total ? k0 + 64 * j : k0;
+                t[j] = lds[k + divided(k, d.per_width) * (width - L) + g * L];
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s += k0 + 64 * j < total ? t[j] : 0.0f;
         }
-        __syncthreads();
-        for (int c = threadIdx.x; c < width; c += kBlock) channel[c] = lds[c];
-        __syncthreads();
-    }
-}
-
-// Sums over each group's channels: a wave a group.
-__device__ __forceinline__ void group_sums(const Place& q, int width, const float* channel, float* group) {
-    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, groups = q.n / width;
-    for (int g = w; g < groups; g += kWaves) {
-        float s = 0.0f;
-        for (int c = lane; c < width; c += 64) s += channel[g * width + c];
         s = wave_sum_f32(s);
         if (lane == 0) group[g] = s;
     }
     __syncthreads();
 }
 
-struct Shared {
-    float lanes[kBlock * 8];
-    float channel[kMaxSlab];
-    float group[2][kMaxGroups];
-};
+// Sum over 16 lanes, in each of them.
+__device__ __forceinline__ float sum16(float v) {
+    v += dpp_f32<0xB1>(v);
+    v += dpp_f32<0x4E>(v);
+    v += dpp_f32<0x141>(v);
+    v += dpp_f32<0x140>(v);
+    return v;
+}
 
-// Means and sums of squared differences of the slab's groups over pixels a .. b - 1 (which the registers hold), in
-// s.group[0] and [1].
-template <class T>
-__device__ __forceinline__ void statistics(const GroupDev& d, const Place& q, const Pack8<T> (&x)[kHeld<T>], int a, int b, Shared& s) {
-    float v[8] = {};
-#pragma unroll
-    for (int k = 0; k < kHeld<T>; ++k) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += (float)x[k].v[i];        // zeros where there is no pixel or channel
-    }
-    channel_sums(q, v, s.lanes, s.channel);
-    group_sums(q, d.width, s.channel, s.group[0]);
-    const float n = (float)(b - a) * (float)d.width;
-    for (int g = threadIdx.x; g < q.n / d.width; g += kBlock) s.group[0][g] /= n;
-    __syncthreads();
-    float mean[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        v[i] = 0.0f;
-        mean[i] = q.own && q.c + i < q.n ? s.group[0][(q.c + i) / d.width] : 0.0f;
-    }
-#pragma unroll
-    for (int k = 0; k < kHeld<T>; ++k) {
-        const bool in = q.own && a + q.lane + k * q.lanes < b;
+// A thread's pixels so far: their number, and each channel's mean and sum of squared differences.
+struct Running {
+    float n = 0.0f, mean[8] = {}, m2[8] = {};
+    template <class T, int R>
+    __device__ __forceinline__ void add(const Pack8<T> (&x)[R], int count) {       // the first `count` of them
+        if (count <= 0) return;
+        const float k = (float)(count < R ? count : R), total = n + k, part = k / total, both = n * part;
+        const float inv = 1.0f / k;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float e = (float)x[k].v[i] - mean[i];
-            v[i] += in && q.c + i < q.n ? e * e : 0.0f;
+            // Relative to the first of them: equal values have exactly their mean.
+            const float x0 = (float)x[0].v[i];
+            float s = 0.0f;
+#pragma unroll
+            for (int r = 1; r < R; ++r) s += r < count ? (float)x[r].v[i] - x0 : 0.0f;
+            const float m = fmaf(s, inv, x0), e = m - mean[i];
+            float q = 0.0f;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float t = (float)x[r].v[i] - m;
+                q += r < count ? t * t : 0.0f;
+            }
+            mean[i] = fmaf(e, part, mean[i]);
+            m2[i] += fmaf(e * e, both, q);
         }
+        n = total;
     }
-    channel_sums(q, v, s.lanes, s.channel);
-    group_sums(q, d.width, s.channel, s.group[1]);
+};
+
+// Pixels of the thread from p to p1.
+__device__ __forceinline__ int pixels_left(const Place& q, int p) {
+    return q.own && p < q.p1 ? (q.p1 - p + q.lanes - 1) / q.lanes : 0;
 }
 
+// Of the slab's groups: a value of each, relative to which means are joined, the sum of differences from it, and the sum of
+// squared differences from the mean.
+struct Groups {
+    float first[kMaxGroups], sum[kMaxGroups], m2[kMaxGroups];
+};
+
+// The groups' statistics over the chunk from every thread's; the mean is first + sum / (values).
+__device__ __forceinline__ void statistics(const GroupDev& d, const Place& q, const Running& r, float* lds, Groups& out) {
+    float v[8];
+    if (q.own && q.lane == 0) {
+        int at = q.inside;
+        q.each_group(d, [&](int i, int g) {
+            if (at == 0 && q.c + i < q.n) out.first[g] = r.mean[i];
+            at = at + 1 == d.width ? 0 : at + 1;
+        });
+    }
+    __syncthreads();
+    q.each_group(d, [&](int i, int g) { v[i] = r.n * (r.mean[i] - out.first[g]); });
+    group_sums(d, q, v, lds, out.sum);
+    const float inv = 1.0f / ((float)(q.p1 - q.p0) * (float)d.width);
+    q.each_group(d, [&](int i, int g) {
+        const float e = r.mean[i] - fmaf(out.sum[g], inv, out.first[g]);
+        v[i] = fmaf(e * e, r.n, r.m2[i]);
+    });
+    group_sums(d, q, v, lds, out.m2);
+}
+
+// act((x - mean) rstd w + b) of one piece (a = rstd w).
 template <class T>
-__device__ __forceinline__ void hold(const GroupDev& d, const Place& q, int a, int b, Pack8<T> (&x)[kHeld<T>]) {
+__device__ __forceinline__ Pack8<T> normalized(const Pack8<T>& x, const float (&mean)[8], const float (&a)[8], const float (&b)[8], int act) {
+    float v[8];
 #pragma unroll
-    for (int k = 0; k < kHeld<T>; ++k) {
-        const int p = a + q.lane + k * q.lanes;
-        x[k] = load8(row_at<T>(d.x, d.xs, q, q.own && p < b ? p : a), q.c, q.n, q.own && p < b);
-    }
-}
-
-template <class W>
-__device__ __forceinline__ void parameters(const void* p, const Place& q, float otherwise, float (&v)[8]) {
-    Pack8<W> r;
-    if (p) r = load8(static_cast<const W*>(p) + q.c0, q.c, q.n, q.own);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = p ? (float)r.v[i] : otherwise;
-}
-
-// act((x - mean) rstd w + b) of one piece.
-template <class T, int ACT>
-__device__ __forceinline__ Pack8<T> normalized(const Pack8<T>& x, const float (&mean)[8], const float (&a)[8], const float (&b)[8]) {
+    for (int i = 0; i < 8; ++i) v[i] = fmaf((float)x.v[i] - mean[i], a[i], b[i]);
+    activate8(act, v);
     Pack8<T> o;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o.v[i] = (T)activate<ACT>(fmaf((float)x.v[i] - mean[i], a[i], b[i]));
+    for (int i = 0; i < 8; ++i) o.v[i] = (T)v[i];
     return o;
 }
 
-// A slab's pixels in one block's registers: statistics and result in one launch.
-template <class T, class W, int ACT>
+// A slab's pixels in one block's registers, R a thread: statistics and result in one launch.
+template <class T, int WIDTH, int R>
 __global__ __launch_bounds__(kBlock) void k_group_whole(GroupDev d) {
-    __shared__ Shared s;
-    const Place q(d);
-    Pack8<T> x[kHeld<T>];
-    hold<T>(d, q, q.p0, q.p1, x);
+    __shared__ float lds[kBlock * 8], group[2][kMaxGroups];
+    __shared__ Groups s;
+    const Place q(d, 0, d.pixels, blockIdx.x, blockIdx.y);
+    Pack8<T> x[R];
+    fetch_pixels<T, WIDTH>(d.x, d.xs, q, q.lane, x);
     float a[8], b[8], mean[8];
-    parameters<W>(d.w, q, 1.0f, a);
-    parameters<W>(d.b, q, 0.0f, b);
-    statistics<T>(d, q, x, q.p0, q.p1, s);
-    const float n = (float)(q.p1 - q.p0) * (float)d.width;
-    for (int g = threadIdx.x; g < q.n / d.width; g += kBlock) {
-        const float rstd = 1.0f / sqrtf(s.group[1][g] / n + d.eps);
-        const int64_t at = (int64_t)q.b * d.groups + q.c0 / d.width + g;
-        if (d.mean) d.mean[at] = s.group[0][g];
+    const Raw rw = load_parameters<WIDTH>(d, d.w, q), rb = load_parameters<WIDTH>(d, d.b, q);
+#pragma unroll
+    for (int k = 0; k < R; ++k) x[k] = mend<T, WIDTH>(x[k], q);
+    const int count = pixels_left(q, q.lane);
+    Running r;
+    r.add(x, count);
+    statistics(d, q, r, lds, s);
+    const float n = (float)d.pixels * (float)d.width;
+    for (int g = threadIdx.x; g < q.groups; g += kBlock) {
+        const float m = fmaf(s.sum[g], 1.0f / n, s.first[g]), rstd = 1.0f / sqrtf(s.m2[g] / n + d.eps);
+        const int64_t at = group_at(d, q) + g;
+        if (d.mean) d.mean[at] = m;
         if (d.rstd) d.rstd[at] = rstd;
-        s.group[1][g] = rstd;
+        group[0][g] = m;
+        group[1][g] = rstd;
     }
     __syncthreads();
+    numbers<WIDTH>(d, d.w, rw, q, 1.0f, a);
+    numbers<WIDTH>(d, d.b, rb, q, 0.0f, b);
+    q.each_group(d, [&](int i, int g) {
+        mean[i] = group[0][g];
+        a[i] *= group[1][g];
+    });
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int g = q.own && q.c + i < q.n ? (q.c + i) / d.width : 0;
-        mean[i] = s.group[0][g];
-        a[i] *= s.group[1][g];
+    for (int k = 0; k < R; ++k)
+        if (k < count) store8(row_at<T>(d.y, d.ys, q, q.lane + k * q.lanes) + q.c, normalized(x[k], mean, a, b, d.act), q.n - q.c);
+}
+
+// Statistics of a chunk. The next batch is on its way while one is worked on.
+template <class T, int WIDTH>
+__global__ __launch_bounds__(kBlock, 4) void k_group_stats(GroupDev d) {
+    __shared__ float lds[kBlock * 8];
+    __shared__ Groups s;
+    const Place q(d, blockIdx.x, d.chunk, blockIdx.y, blockIdx.z);
+    Running r;
+    Pack8<T> x[kBatch], next[kBatch];
+    int p = q.p0 + q.lane, left = pixels_left(q, p);
+    fetch_pixels<T, WIDTH>(d.x, d.xs, q, p, next);
+    while (left > 0) {
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) x[k] = mend<T, WIDTH>(next[k], q);
+        p += kBatch * q.lanes;
+        if (left > kBatch) fetch_pixels<T, WIDTH>(d.x, d.xs, q, p, next);
+        r.add(x, left);
+        left -= kBatch;
     }
-#pragma unroll
-    for (int k = 0; k < kHeld<T>; ++k) {
-        const int p = q.p0 + q.lane + k * q.lanes;
-        if (q.own && p < q.p1)
-            store8(const_cast<T*>(row_at<T>(d.y, d.ys, q, p)) + q.c, normalized<T, ACT>(x[k], mean, a, b), q.n - q.c);
+    statistics(d, q, r, lds, s);
+    const float n = (float)(q.p1 - q.p0) * (float)d.width;
+    for (int g = threadIdx.x; g < q.groups; g += kBlock) {
+        float* out = d.part + ((group_at(d, q) + g) * d.chunks + blockIdx.x) * 2;
+        out[0] = fmaf(s.sum[g], 1.0f / n, s.first[g]);
+        out[1] = s.m2[g];
     }
 }
 
-// Statistics of a chunk, one run of pixels that the registers hold after the other.
-template <class T>
-__global__ __launch_bounds__(kBlock) void k_group_stats(GroupDev d) {
-    __shared__ Shared s;
-    __shared__ float run[2][kMaxGroups];
-    const Place q(d);
-    const int step = q.lanes * kHeld<T>;
-    for (int a = q.p0; a < q.p1; a += step) {
-        const int b = q.p1 - a < step ? q.p1 : a + step;
-        Pack8<T> x[kHeld<T>];
-        hold<T>(d, q, a, b, x);
-        statistics<T>(d, q, x, a, b, s);
-        const float n0 = (float)(a - q.p0) * (float)d.width, n1 = (float)(b - a) * (float)d.width;
-        for (int g = threadIdx.x; g < q.n / d.width; g += kBlock) {
-            float m = s.group[0][g], m2 = s.group[1][g];
-            if (a > q.p0) {
-                const float e = m - run[0][g];
-                m = run[0][g] + e * (n1 / (n0 + n1));
-                m2 = run[1][g] + m2 + e * e * (n0 * n1 / (n0 + n1));
-            }
-            run[0][g] = m;
-            run[1][g] = m2;
-        }
-        __syncthreads();
-    }
-    for (int g = threadIdx.x; g < q.n / d.width; g += kBlock) {
-        float* out = d.part + (((int64_t)q.b * d.groups + q.c0 / d.width + g) * d.chunks + blockIdx.x) * 2;
-        out[0] = run[0][g];
-        out[1] = run[1][g];
-    }
-}
-
-// Joins the chunks' statistics (every block for its own groups, a wave a group) and writes the chunk's results.
-template <class T, class W, int ACT>
-__global__ __launch_bounds__(kBlock) void k_group_apply(GroupDev d) {
+// Joins the chunks' statistics (every block for its own groups, 16 lanes a group) and writes the results of d.spread
+// pixels.
+template <class T, int WIDTH>
+__global__ __launch_bounds__(kBlock, 4) void k_group_apply(GroupDev d) {
     __shared__ float group[2][kMaxGroups];
-    const Place q(d);
+    const Place q(d, blockIdx.x, d.spread, blockIdx.y, blockIdx.z);
+    Pack8<T> next[kBatch];
+    int p = q.p0 + q.lane, left = pixels_left(q, p);
+    fetch_pixels<T, WIDTH>(d.x, d.xs, q, p, next);
     float a[8], b[8], mean[8];
-    parameters<W>(d.w, q, 1.0f, a);
-    parameters<W>(d.b, q, 0.0f, b);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const Raw rw = load_parameters<WIDTH>(d, d.w, q), rb = load_parameters<WIDTH>(d, d.b, q);
+    const int sub = threadIdx.x & 15;
     const float total = (float)d.pixels * (float)d.width, each = (float)d.chunk * (float)d.width;
-    const float rest = total - each * (float)(d.chunks - 1);
-    for (int g = wave; g < q.n / d.width; g += kWaves) {
-        const int64_t at = (int64_t)q.b * d.groups + q.c0 / d.width + g;
-        const float* in = d.part + at * d.chunks * 2;
+    const float rest = (float)(d.pixels - (d.chunks - 1) * d.chunk) * (float)d.width;
+    for (int g0 = 0; g0 < q.groups; g0 += kBlock / 16) {
+        const int g = g0 + ((int)threadIdx.x >> 4);
+        const int64_t at = group_at(d, q) + (g < q.groups ? g : 0);
+        const float2* in = reinterpret_cast<const float2*>(d.part) + at * d.chunks;
+        const float first = in[0].x;
         float m = 0.0f, m2 = 0.0f;
-        for (int k = lane; k < d.chunks; k += 64) m += in[2 * k] * ((k + 1 < d.chunks ? each : rest) / total);
-        m = wave_sum_f32(m);
-        for (int k = lane; k < d.chunks; k += 64) {
-            const float e = in[2 * k] - m;
-            m2 += in[2 * k + 1] + e * e * (k + 1 < d.chunks ? each : rest);
+#pragma unroll 4
+        for (int k = sub; k < d.chunks; k += 16) m += (in[k].x - first) * (k + 1 < d.chunks ? each : rest);
+        m = first + sum16(m) / total;
+#pragma unroll 4
+        for (int k = sub; k < d.chunks; k += 16) {
+            const float2 v = in[k];
+            const float e = v.x - m;
+            m2 += v.y + e * e * (k + 1 < d.chunks ? each : rest);
         }
-        m2 = wave_sum_f32(m2);
-        if (lane == 0) {
+        m2 = sum16(m2);
+        if (sub == 0 && g < q.groups) {
             const float rstd = 1.0f / sqrtf(m2 / total + d.eps);
             group[0][g] = m;
             group[1][g] = rstd;
@@ -260,22 +368,22 @@ __global__ __launch_bounds__(kBlock) void k_group_apply(GroupDev d) {
         }
     }
     __syncthreads();
-    if (!q.own) return;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int g = q.c + i < q.n ? (q.c + i) / d.width : 0;
+    numbers<WIDTH>(d, d.w, rw, q, 1.0f, a);
+    numbers<WIDTH>(d, d.b, rb, q, 0.0f, b);
+    q.each_group(d, [&](int i, int g) {
         mean[i] = group[0][g];
         a[i] *= group[1][g];
-    }
-    for (int p = q.p0 + q.lane; p < q.p1; p += 4 * q.lanes) {
-        Pack8<T> x[4];
+    });
+    while (left > 0) {
+        Pack8<T> x[kBatch];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            x[k] = load8(row_at<T>(d.x, d.xs, q, p + k * q.lanes < q.p1 ? p + k * q.lanes : p), q.c, q.n);
+        for (int k = 0; k < kBatch; ++k) x[k] = mend<T, WIDTH>(next[k], q);
+        if (left > kBatch) fetch_pixels<T, WIDTH>(d.x, d.xs, q, p + kBatch * q.lanes, next);
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (p + k * q.lanes < q.p1)
-                store8(const_cast<T*>(row_at<T>(d.y, d.ys, q, p + k * q.lanes)) + q.c, normalized<T, ACT>(x[k], mean, a, b), q.n - q.c);
+        for (int k = 0; k < kBatch; ++k)
+            if (k < left) store8(row_at<T>(d.y, d.ys, q, p + k * q.lanes) + q.c, normalized(x[k], mean, a, b, d.act), q.n - q.c);
+        p += kBatch * q.lanes;
+        left -= kBatch;
     }
 }
 
@@ -284,66 +392,121 @@ struct Channels {                    // of the thread's 8: group mean, rstd, wei
     float mean[8], rstd[8], w[8], b[8];
 };
 
-template <class W>
+template <int WIDTH>
 __device__ __forceinline__ Channels channels(const GroupDev& d, const Place& q) {
     Channels k;
-    parameters<W>(d.w, q, 1.0f, k.w);
-    parameters<W>(d.b, q, 0.0f, k.b);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int64_t at = (int64_t)q.b * d.groups + (q.c0 + (q.own && q.c + i < q.n ? q.c + i : 0)) / d.width;
-        k.mean[i] = d.mean[at];
-        k.rstd[i] = d.rstd[at];
-    }
+    const Raw rw = load_parameters<WIDTH>(d, d.w, q), rb = load_parameters<WIDTH>(d, d.b, q);
+    const int64_t at = group_at(d, q);
+    q.each_group(d, [&](int i, int g) {
+        k.mean[i] = d.mean[at + g];
+        k.rstd[i] = d.rstd[at + g];
+    });
+    numbers<WIDTH>(d, d.w, rw, q, 1.0f, k.w);
+    numbers<WIDTH>(d, d.b, rb, q, 0.0f, k.b);
     return k;
 }
 
-// {xh, dz} of element i.
-template <int ACT>
-__device__ __forceinline__ float2 through(const Channels& k, float x, float dy, int i) {
-    const float xh = (x - k.mean[i]) * k.rstd[i];
-    return make_float2(xh, ACT == PA_ACT_NONE ? dy : dy * activate_grad<ACT>(fmaf(xh, k.w[i], k.b[i])).y);
+// xh and dz of one piece.
+template <class T>
+__device__ __forceinline__ void through(const Channels& k, const Pack8<T>& x, const Pack8<T>& dy, int act, float (&xh)[8], float (&dz)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        xh[i] = ((float)x.v[i] - k.mean[i]) * k.rstd[i];
+        dz[i] = (float)dy.v[i];
+    }
+    if (act == PA_ACT_NONE) return;
+    float s[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i] = fmaf(xh[i], k.w[i], k.b[i]);
+    slope8(act, s);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dz[i] *= s[i];
+}
+
+// Sums over the block's threads for each channel, in a fixed order: of u into out, of v `channels` after it.
+// `lds`: kBlock * 16 floats.
+__device__ __forceinline__ void channel_sums(const Place& q, const float (&u)[8], const float (&v)[8], float* lds, float* out, int channels) {
+    const int width = q.pieces * 8;
+    float* second = lds + kBlock * 8;
+    if (q.own) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            lds[q.lane * width + q.c + i] = u[i];
+            second[q.lane * width + q.c + i] = v[i];
+        }
+    }
+    __syncthreads();
+    // Where there are twice as many threads as channels, or more, several take a channel's lanes in turn.
+    const float per = 1.0f / (float)width;
+    const int turns = width < kBlock ? divided(kBlock, per) : 1;
+    if (turns > 1) {
+        const int t = divided((int)threadIdx.x, per), c = (int)threadIdx.x - t * width;
+        float a = 0.0f, b = 0.0f;
+        if (t < turns)
+            for (int l = t; l < q.lanes; l += turns) {
+                a += lds[l * width + c];
+                b += second[l * width + c];
+            }
+        __syncthreads();
+        if (t < turns) {
+            lds[t * width + c] = a;
+            second[t * width + c] = b;
+        }
+        __syncthreads();
+    }
+    const int rows = turns > 1 ? turns : q.lanes;
+    for (int c = threadIdx.x; c < q.n; c += kBlock) {
+        float a = 0.0f, b = 0.0f;
+        for (int l = 0; l < rows; ++l) {
+            a += lds[l * width + c];
+            b += second[l * width + c];
+        }
+        out[c] = a;
+        out[channels + c] = b;
+    }
 }
 
 // Sums over a chunk's pixels of dz xh and dz for each channel.
-template <class T, class W, int ACT>
-__global__ __launch_bounds__(kBlock) void k_group_sums(GroupDev d) {
-    __shared__ float lanes[kBlock * 8];
-    __shared__ float channel[kMaxSlab];
-    const Place q(d);
-    const Channels ch = channels<W>(d, q);
+template <class T, int WIDTH>
+__global__ __launch_bounds__(kBlock, 4) void k_group_sums(GroupDev d) {
+    __shared__ float lds[kBlock * 16];
+    const Place q(d, blockIdx.x, d.chunk, blockIdx.y, blockIdx.z);
+    constexpr int R = sizeof(T) == 2 ? 2 : 1;
+    Pack8<T> nx[R], ny[R];
+    int p = q.p0 + q.lane, left = pixels_left(q, p);
+    fetch_pixels<T, WIDTH>(d.x, d.xs, q, p, nx);
+    fetch_pixels<T, WIDTH>(d.dy, d.ys, q, p, ny);
+    const Channels ch = channels<WIDTH>(d, q);
     float sw[8] = {}, sb[8] = {};
-    if (q.own) {
-        for (int p = q.p0 + q.lane; p < q.p1; p += 2 * q.lanes) {
-            Pack8<T> x[2], dy[2];
+    while (left > 0) {
+        Pack8<T> x[R], y[R];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const bool in = p + k * q.lanes < q.p1;
-                x[k] = load8(row_at<T>(d.x, d.xs, q, in ? p + k * q.lanes : p), q.c, q.n);
-                dy[k] = load8(row_at<T>(d.dy, d.ys, q, in ? p + k * q.lanes : p), q.c, q.n);
-            }
+        for (int k = 0; k < R; ++k) {
+            x[k] = mend<T, WIDTH>(nx[k], q);
+            y[k] = mend<T, WIDTH>(ny[k], q);
+        }
+        p += R * q.lanes;
+        if (left > R) {
+            fetch_pixels<T, WIDTH>(d.x, d.xs, q, p, nx);
+            fetch_pixels<T, WIDTH>(d.dy, d.ys, q, p, ny);
+        }
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                if (p + k * q.lanes >= q.p1) continue;
+        for (int k = 0; k < R; ++k) {
+            if (k >= left) break;
+            float xh[8], dz[8];
+            through(ch, x[k], y[k], d.act, xh, dz);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float2 t = through<ACT>(ch, (float)x[k].v[i], (float)dy[k].v[i], i);
-                    sw[i] += t.y * t.x;
-                    sb[i] += t.y;
-                }
+            for (int i = 0; i < 8; ++i) {
+                sw[i] = fmaf(dz[i], xh[i], sw[i]);
+                sb[i] += dz[i];
             }
         }
+        left -= R;
     }
-    float* out = d.part + ((int64_t)q.b * d.chunks + blockIdx.x) * 2 * d.channels + q.c0;
-    channel_sums(q, sw, lanes, channel);
-    for (int c = threadIdx.x; c < q.n; c += kBlock) out[c] = channel[c];
-    __syncthreads();
-    channel_sums(q, sb, lanes, channel);
-    for (int c = threadIdx.x; c < q.n; c += kBlock) out[d.channels + c] = channel[c];
+    channel_sums(q, sw, sb, lds, d.part + ((int64_t)q.b * d.chunks + blockIdx.x) * 2 * d.channels + q.c0, d.channels);
 }
 
-// A sample's group: the channels' sums over the chunks, and from them the means over the group of g xh and g.
-template <class W>
+// A sample's group: the channels' sums over the chunks, and from them the means over the group of g and g xh.
 __global__ __launch_bounds__(256) void k_group_join(GroupDev d) {
     __shared__ float sum[2][256], red[2][4];
     const int g = blockIdx.x, b = blockIdx.y, L = d.width;
@@ -354,12 +517,14 @@ __global__ __launch_bounds__(256) void k_group_join(GroupDev d) {
         const int c = c0 + (L < 256 ? (int)threadIdx.x - t * L : (int)threadIdx.x), ch = g * L + c;
         float v[2] = {};
         const bool own = c < L && (L >= 256 || t < turns);
-        if (own)
+        if (own) {
+#pragma unroll 8
             for (int k = L < 256 ? t : 0; k < d.chunks; k += turns) {
                 const float* in = d.part + ((int64_t)b * d.chunks + k) * 2 * d.channels + ch;
                 v[0] += in[0];
                 v[1] += in[d.channels];
             }
+        }
         sum[0][threadIdx.x] = v[0];
         sum[1][threadIdx.x] = v[1];
         __syncthreads();
@@ -371,7 +536,10 @@ __global__ __launch_bounds__(256) void k_group_join(GroupDev d) {
             float* out = d.sums + (int64_t)b * 2 * d.channels + ch;
             out[0] = v[0];
             out[d.channels] = v[1];
-            const float w = d.w ? (float)static_cast<const W*>(d.w)[ch] : 1.0f;
+            float w = 1.0f;
+            if (d.w)
+                w = d.param_dtype == PA_F32 ? static_cast<const float*>(d.w)[ch]
+                    : d.param_dtype == PA_BF16 ? (float)static_cast<const __bf16*>(d.w)[ch] : (float)static_cast<const _Float16*>(d.w)[ch];
             m[0] += v[1] * w;
             m[1] += v[0] * w;
         }
@@ -388,63 +556,145 @@ __global__ __launch_bounds__(256) void k_group_join(GroupDev d) {
     }
 }
 
-template <class T, class W, int ACT>
-__global__ __launch_bounds__(kBlock) void k_group_dx(GroupDev d) {
-    const Place q(d);
-    if (!q.own) return;
-    Channels ch = channels<W>(d, q);
-    float m1[8], m2[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int64_t at = (int64_t)q.b * d.groups + (q.c0 + (q.c + i < q.n ? q.c + i : 0)) / d.width;
-        m1[i] = d.means[2 * at];
-        m2[i] = d.means[2 * at + 1];
-    }
-    for (int p = q.p0 + q.lane; p < q.p1; p += 2 * q.lanes) {
-        Pack8<T> x[2], dy[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const bool in = p + k * q.lanes < q.p1;
-            x[k] = load8(row_at<T>(d.x, d.xs, q, in ? p + k * q.lanes : p), q.c, q.n);
-            dy[k] = load8(row_at<T>(d.dy, d.ys, q, in ? p + k * q.lanes : p), q.c, q.n);
-        }
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            if (p + k * q.lanes >= q.p1) continue;
-            Pack8<T> o;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float2 t = through<ACT>(ch, (float)x[k].v[i], (float)dy[k].v[i], i);
-                o.v[i] = (T)(ch.rstd[i] * (t.y * ch.w[i] - m1[i] - t.x * m2[i]));
-            }
-            store8(const_cast<T*>(row_at<T>(d.dx, d.dxs, q, p + k * q.lanes)) + q.c, o, q.n - q.c);
-        }
-    }
-}
-
-// dweight (blockIdx.y 0) and dbias from the samples' sums, in order.
-template <class W>
-__global__ __launch_bounds__(256) void k_group_params(GroupDev d) {
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    W* out = static_cast<W*>(blockIdx.y ? d.db : d.dw);
-    if (!out || c >= d.channels) return;
+// dweight and dbias from the samples' sums, in order; `block` of 512 of the 2 x channels values.
+__device__ __forceinline__ void join_samples(const GroupDev& d, int block) {
+    const int64_t i = (int64_t)block * kBlock + threadIdx.x;
+    if (i >= 2 * (int64_t)d.channels) return;
+    const bool second = i >= d.channels;
+    void* out = second ? d.db : d.dw;
+    if (!out) return;
+    const int c = (int)(second ? i - d.channels : i);
     float s = 0.0f;
 #pragma unroll 8
-    for (int b = 0; b < d.batch; ++b) s += d.sums[((int64_t)b * 2 + blockIdx.y) * d.channels + c];
-    out[c] = (W)s;
+    for (int b = 0; b < d.batch; ++b) s += d.sums[(int64_t)b * 2 * d.channels + i];
+    if (d.param_dtype == PA_F32) static_cast<float*>(out)[c] = s;
+    else if (d.param_dtype == PA_BF16) static_cast<__bf16*>(out)[c] = (__bf16)s;
+    else static_cast<_Float16*>(out)[c] = (_Float16)s;
 }
 
+__global__ __launch_bounds__(kBlock) void k_group_params(GroupDev d) { join_samples(d, blockIdx.x); }
+
+// dx of one piece from the means over its channels' groups.
+template <class T>
+__device__ __forceinline__ Pack8<T> gradient(const Channels& ch, const Pack8<T>& x, const Pack8<T>& dy, const float (&m1)[8], const float (&m2)[8], int act) {
+    float xh[8], dz[8];
+    through(ch, x, dy, act, xh, dz);
+    Pack8<T> o;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o.v[i] = (T)(ch.rstd[i] * (dz[i] * ch.w[i] - m1[i] - xh[i] * m2[i]));
+    return o;
+}
+
+// dx of a chunk; the launch's last blocks join the samples' sums (there are `blocks` in front of them).
+template <class T, int WIDTH>
+__global__ __launch_bounds__(kBlock, 4) void k_group_dx(GroupDev d, unsigned blocks) {
+    if (blockIdx.x >= blocks) {
+        join_samples(d, (int)(blockIdx.x - blocks));
+        return;
+    }
+    const int spreads = (int)(blocks / (unsigned)(d.slabs * d.batch)), chunk = (int)(blockIdx.x % spreads), rest = (int)(blockIdx.x / spreads);
+    const Place q(d, chunk, d.spread, rest % d.slabs, rest / d.slabs);
+    constexpr int R = sizeof(T) == 2 ? 2 : 1;
+    Pack8<T> nx[R], ny[R];
+    int p = q.p0 + q.lane, left = pixels_left(q, p);
+    fetch_pixels<T, WIDTH>(d.x, d.xs, q, p, nx);
+    fetch_pixels<T, WIDTH>(d.dy, d.ys, q, p, ny);
+    const Channels ch = channels<WIDTH>(d, q);
+    float m1[8], m2[8];
+    const float2* means = reinterpret_cast<const float2*>(d.means) + group_at(d, q);
+    q.each_group(d, [&](int i, int g) {
+        const float2 v = means[g];
+        m1[i] = v.x;
+        m2[i] = v.y;
+    });
+    while (left > 0) {
+        Pack8<T> x[R], y[R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            x[k] = mend<T, WIDTH>(nx[k], q);
+            y[k] = mend<T, WIDTH>(ny[k], q);
+        }
+        if (left > R) {
+            fetch_pixels<T, WIDTH>(d.x, d.xs, q, p + R * q.lanes, nx);
+            fetch_pixels<T, WIDTH>(d.dy, d.ys, q, p + R * q.lanes, ny);
+        }
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            if (k < left) store8(row_at<T>(d.dx, d.dxs, q, p + k * q.lanes) + q.c, gradient(ch, x[k], y[k], m1, m2, d.act), q.n - q.c);
+            __builtin_amdgcn_sched_barrier(0);           // one pixel's numbers in registers at a time
+        }
+        p += R * q.lanes;
+        left -= R;
+    }
+}
+
+// A slab's pixels of x and dy in one block's registers, R a thread: sums and dx in one launch.
+template <class T, int WIDTH, int R>
+__global__ __launch_bounds__(kBlock) void k_group_bwd_whole(GroupDev d) {
+    __shared__ float lds[kBlock * 16], group[2][kMaxGroups];
+    const Place q(d, 0, d.pixels, blockIdx.x, blockIdx.y);
+    Pack8<T> x[R], y[R];
+    fetch_pixels<T, WIDTH>(d.x, d.xs, q, q.lane, x);
+    fetch_pixels<T, WIDTH>(d.dy, d.ys, q, q.lane, y);
+    const Channels ch = channels<WIDTH>(d, q);
+    const int count = pixels_left(q, q.lane);
+    float sw[8] = {}, sb[8] = {}, v[8];
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        x[k] = mend<T, WIDTH>(x[k], q);
+        y[k] = mend<T, WIDTH>(y[k], q);
+        if (k < count) {
+            float xh[8], dz[8];
+            through(ch, x[k], y[k], d.act, xh, dz);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                sw[i] = fmaf(dz[i], xh[i], sw[i]);
+                sb[i] += dz[i];
+            }
+        }
+    }
+    if (d.dx) {
+        const float inv = 1.0f / ((float)d.pixels * (float)d.width);
+        float m1[8], m2[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = sb[i] * ch.w[i];
+        group_sums(d, q, v, lds, group[0]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = sw[i] * ch.w[i];
+        group_sums(d, q, v, lds, group[1]);
+        q.each_group(d, [&](int i, int g) {
+            m1[i] = group[0][g] * inv;
+            m2[i] = group[1][g] * inv;
+        });
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+            if (k < count) store8(row_at<T>(d.dx, d.dxs, q, q.lane + k * q.lanes) + q.c, gradient(ch, x[k], y[k], m1, m2, d.act), q.n - q.c);
+    }
+    if (d.dw || d.db) channel_sums(q, sw, sb, lds, d.sums + (int64_t)q.b * 2 * d.channels + q.c0, d.channels);
+}
+
+// ------------------------------------------------------------------ launches
+// Pixels of a thread that the one-launch kernels hold.
+constexpr int kHeld = 8;
+
 template <class F>
-hipError_t dispatch(int dtype, int param_dtype, int act, F f) {
-    auto with_act = [&](auto t, auto w) {
-        if (act == PA_ACT_SILU) return f(t, w, std::integral_constant<int, PA_ACT_SILU>{});
-        if (act == PA_ACT_GELU) return f(t, w, std::integral_constant<int, PA_ACT_GELU>{});
-        return f(t, w, std::integral_constant<int, PA_ACT_NONE>{});
+hipError_t dispatch(int dtype, const GroupDev& d, F f) {
+    auto width = [&](auto t) {
+        const int last = d.channels - (d.slabs - 1) * d.slab;
+        if (d.slab % 8 == 0 && last % 8 == 0) return f(t, std::integral_constant<int, kWhole>{});
+        if (d.slab >= 8 && last >= 8) return f(t, std::integral_constant<int, kRagged>{});
+        return f(t, std::integral_constant<int, kTiny>{});
     };
-    const bool pf = param_dtype == PA_F32;
-    if (dtype == PA_F32) return with_act((float)0, (float)0);
-    if (dtype == PA_BF16) return pf ? with_act((__bf16)0, (float)0) : with_act((__bf16)0, (__bf16)0);
-    return pf ? with_act((_Float16)0, (float)0) : with_act((_Float16)0, (_Float16)0);
+    if (dtype == PA_F32) return width((float)0);
+    return dtype == PA_BF16 ? width((__bf16)0) : width((_Float16)0);
+}
+
+// f with the number of a thread's pixels that a slab of one block takes, rounded up to 2 or 8.
+template <class F>
+void held(const GroupDev& d, F f) {
+    const int lanes = kBlock / ((d.slab + 7) / 8);
+    if (d.pixels <= 2 * lanes) f(std::integral_constant<int, 2>{});
+    else f(std::integral_constant<int, kHeld>{});
 }
 
 }  // namespace
@@ -455,6 +705,7 @@ hipError_t dispatch(int dtype, int param_dtype, int act, F f) {
 // as a block can take, in chunks of pixels.
 void group_plan(GroupDev& d, int dtype, bool backward) {
     d.width = d.channels / d.groups;
+    d.per_width = 1.0f / (float)d.width;
     int unit = 1;                                   // groups whose channels make whole pieces
     while (unit < 8 && d.width * unit % 8 != 0) unit *= 2;
     const int most = kMaxSlab / d.width < kMaxGroups ? kMaxSlab / d.width : kMaxGroups;
@@ -466,65 +717,79 @@ void group_plan(GroupDev& d, int dtype, bool backward) {
     };
     const int small = (32 + d.width * unit - 1) / (d.width * unit) * unit;
     slab(small);
-    const int64_t fits = (int64_t)(kBlock / ((d.slab + 7) / 8)) * held(dtype);
+    const int64_t fits = (int64_t)(kBlock / ((d.slab + 7) / 8)) * kHeld;
     const int64_t bytes = (int64_t)d.batch * d.pixels * d.channels * (dtype == PA_F32 ? 4 : 2);
-    if (!backward && d.pixels <= fits && (bytes <= (4 << 20) || (int64_t)d.batch * d.slabs >= 256)) {
+    if (d.pixels <= fits && (bytes <= (4 << 20) || (int64_t)d.batch * d.slabs >= 256)) {
         d.chunk = d.pixels > 0 ? d.pixels : 1;
         d.chunks = 1;
+        d.whole = 1;
         return;
     }
     slab(d.groups);
-    // What the registers hold at a time, fewer where that gives too few blocks, and more beyond 256 chunks a sample.
+    // 512 blocks, two for each CU, as its registers allow, but chunks of two pixels a thread at least, and at most 256 of
+    // them a sample. us with 512, 768, 1024 and 2048 blocks, 32x4096x320: statistics 23, 24, 25, 35, results 33, 33, 34,
+    // 38; 8x4096x640: sums of the backward pass 21, 22, 22, dx 34, 39, 37, 41.
     const int lanes = kBlock / ((d.slab + 7) / 8);
-    const int64_t per = (int64_t)d.batch * d.slabs;
-    int64_t chunk = (int64_t)lanes * (backward ? 8 : held(dtype));
-    while (chunk > lanes * 2 && (d.pixels + chunk - 1) / chunk * per < 512) chunk /= 2;
+    const int64_t per = (int64_t)d.batch * d.slabs, want = (512 + per - 1) / (per > 0 ? per : 1);
+    int64_t chunk = (d.pixels + want - 1) / want;
+    if (chunk < lanes * 2) chunk = lanes * 2;
     if ((d.pixels + chunk - 1) / chunk > 256) chunk = (d.pixels + 255) / 256;
     d.chunk = (int)(chunk < 1 ? 1 : chunk);
     d.chunks = d.pixels > 0 ? (d.pixels + d.chunk - 1) / d.chunk : 1;
+    int64_t spread = (d.pixels + want - 1) / want;
+    if (spread < lanes * 2) spread = lanes * 2;
+    d.spread = (int)spread;
+    d.whole = 0;
 }
 
-hipError_t group_forward(const GroupDev& d, int dtype, int param_dtype, int act, hipStream_t st) {
-    return dispatch(dtype, param_dtype, act, [&](auto t, auto w, auto a) {
+hipError_t group_forward(const GroupDev& d, int dtype, hipStream_t st) {
+    return dispatch(dtype, d, [&](auto t, auto wd) {
         typedef decltype(t) T;
-        typedef decltype(w) W;
-        constexpr int ACT = decltype(a)::value;
-        const dim3 grid((unsigned)d.chunks, (unsigned)d.slabs, (unsigned)d.batch);
-        if (!d.part) {
-            k_group_whole<T, W, ACT><<<grid, kBlock, 0, st>>>(d);
+        constexpr int WIDTH = decltype(wd)::value;
+        if (d.whole) {
+            held(d, [&](auto r) {
+                k_group_whole<T, WIDTH, decltype(r)::value><<<dim3((unsigned)d.slabs, (unsigned)d.batch), kBlock, 0, st>>>(d);
+            });
             return hipGetLastError();
         }
-        k_group_stats<T><<<grid, kBlock, 0, st>>>(d);
+        dim3 grid((unsigned)d.chunks, (unsigned)d.slabs, (unsigned)d.batch);
+        k_group_stats<T, WIDTH><<<grid, kBlock, 0, st>>>(d);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        k_group_apply<T, W, ACT><<<grid, kBlock, 0, st>>>(d);
+        grid.x = (unsigned)((d.pixels + d.spread - 1) / d.spread);
+        k_group_apply<T, WIDTH><<<grid, kBlock, 0, st>>>(d);
         return hipGetLastError();
     });
 }
 
-hipError_t group_backward(const GroupDev& d, int dtype, int param_dtype, int act, hipStream_t st) {
-    return dispatch(dtype, param_dtype, act, [&](auto t, auto w, auto a) {
+hipError_t group_backward(const GroupDev& d, int dtype, hipStream_t st) {
+    return dispatch(dtype, d, [&](auto t, auto wd) {
         typedef decltype(t) T;
-        typedef decltype(w) W;
-        constexpr int ACT = decltype(a)::value;
-        const dim3 grid((unsigned)d.chunks, (unsigned)d.slabs, (unsigned)d.batch);
-        if (d.pixels > 0 && d.batch > 0) {
-            k_group_sums<T, W, ACT><<<grid, kBlock, 0, st>>>(d);
+        constexpr int WIDTH = decltype(wd)::value;
+        const unsigned params = d.dw || d.db ? (unsigned)((2 * (int64_t)d.channels + kBlock - 1) / kBlock) : 0;
+        const bool any = d.batch > 0 && d.pixels > 0;
+        if (any && !d.whole) {
+            k_group_sums<T, WIDTH><<<dim3((unsigned)d.chunks, (unsigned)d.slabs, (unsigned)d.batch), kBlock, 0, st>>>(d);
             hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
-            k_group_join<W><<<dim3((unsigned)d.groups, (unsigned)d.batch), 256, 0, st>>>(d);
+            k_group_join<<<dim3((unsigned)d.groups, (unsigned)d.batch), 256, 0, st>>>(d);
             e = hipGetLastError();
             if (e != hipSuccess) return e;
-            if (d.dx) {
-                k_group_dx<T, W, ACT><<<grid, kBlock, 0, st>>>(d);
-                e = hipGetLastError();
-                if (e != hipSuccess) return e;
-            }
+            const unsigned blocks = d.dx ? (unsigned)((int64_t)((d.pixels + d.spread - 1) / d.spread) * d.slabs * d.batch) : 0;
+            if (blocks + params > 0) k_group_dx<T, WIDTH><<<blocks + params, kBlock, 0, st>>>(d, blocks);
+            return hipGetLastError();
         }
-        if (d.dw || d.db) {
+        if (any) {
+            held(d, [&](auto r) {
+                k_group_bwd_whole<T, WIDTH, decltype(r)::value><<<dim3((unsigned)d.slabs, (unsigned)d.batch), kBlock, 0, st>>>(d);
+            });
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        if (params) {
             GroupDev c = d;
-            if (d.pixels == 0) c.batch = 0;
-            k_group_params<W><<<dim3((unsigned)((d.channels + 255) / 256), 2), 256, 0, st>>>(c);
+            if (!any) c.batch = 0;
+            k_group_params<<<params, kBlock, 0, st>>>(c);
         }
         return hipGetLastError();
     });

@@ -64,6 +64,10 @@ struct GroupDev {
     int batch, pixels, channels, groups, width;   // width: channels of a group
     int slab, slabs;                 // channels of a block (whole groups; the last has what is left), blocks over them
     int chunk, chunks;               // pixels of a block, blocks over them
+    int spread;                      // pixels of a block in the second pass
+    float per_width;                 // 1 / width
+    int whole;                       // a block's registers hold a slab's pixels: no partial sums
+    int param_dtype, act;
     float eps;
 };
 
@@ -113,10 +117,10 @@ hipError_t cross_backward(const CrossDev& d, int dtype, hipStream_t st);
 
 hipError_t lora_linear(const LoraDev& d, int dtype, hipStream_t st);
 
-// Fills in slab .. chunks from the sizes. Whether one block takes a slab's pixels in one launch: chunks == 1.
+// Fills in width and slab .. whole from the sizes.
 void group_plan(GroupDev& d, int dtype, bool backward);
-hipError_t group_forward(const GroupDev& d, int dtype, int param_dtype, int act, hipStream_t st);
-hipError_t group_backward(const GroupDev& d, int dtype, int param_dtype, int act, hipStream_t st);
+hipError_t group_forward(const GroupDev& d, int dtype, hipStream_t st);
+hipError_t group_backward(const GroupDev& d, int dtype, hipStream_t st);
 
 // Whether rows are read straight from memory (no copies in whole pieces).
 bool feed_few(int64_t rows);

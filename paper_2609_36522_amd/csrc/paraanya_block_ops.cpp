@@ -61,6 +61,8 @@ GroupDev group_dev(const pa_group_norm_t* p, bool backward) {
     d.pixels = (int)p->pixels;
     d.channels = p->channels;
     d.groups = p->groups;
+    d.param_dtype = p->param_dtype;
+    d.act = p->activation;
     d.eps = (float)p->eps;
     for (int i = 0; i < 2; ++i) {
         d.xs[i] = p->x_stride[i];
@@ -74,9 +76,9 @@ GroupDev group_dev(const pa_group_norm_t* p, bool backward) {
 size_t group_layout(GroupDev& d, bool backward, void* ws) {
     Parts w(ws);
     if (!backward) {
-        if (d.chunks > 1) d.part = static_cast<float*>(w.take((size_t)d.batch * d.groups * d.chunks * 2 * sizeof(float)));
+        if (!d.whole) d.part = static_cast<float*>(w.take((size_t)d.batch * d.groups * d.chunks * 2 * sizeof(float)));
     } else {
-        d.part = static_cast<float*>(w.take((size_t)d.batch * d.chunks * 2 * d.channels * sizeof(float)));
+        if (!d.whole) d.part = static_cast<float*>(w.take((size_t)d.batch * d.chunks * 2 * d.channels * sizeof(float)));
         d.sums = static_cast<float*>(w.take((size_t)d.batch * 2 * d.channels * sizeof(float)));
         d.means = static_cast<float*>(w.take((size_t)d.batch * d.groups * 2 * sizeof(float)));
     }
@@ -233,7 +235,7 @@ int paraanya_group_norm(const pa_group_norm_t* p, const void* x, const void* wei
         d.y = y;
         d.mean = mean;
         d.rstd = rstd;
-        return launched(group_forward(d, p->dtype, p->param_dtype, p->activation, static_cast<hipStream_t>(stream)), "group norm launch");
+        return launched(group_forward(d, p->dtype, static_cast<hipStream_t>(stream)), "group norm launch");
     });
 }
 
@@ -273,8 +275,7 @@ int paraanya_group_norm_backward(const pa_group_norm_t* p, const void* dy, const
         d.dx = dx;
         d.dw = dweight;
         d.db = dbias;
-        return launched(group_backward(d, p->dtype, p->param_dtype, p->activation, static_cast<hipStream_t>(stream)),
-                        "group norm backward launch");
+        return launched(group_backward(d, p->dtype, static_cast<hipStream_t>(stream)), "group norm backward launch");
     });
 }
 
