@@ -16,8 +16,6 @@ namespace pa {
 
 namespace {
 
-constexpr int kCUs = 256;
-
 template <class T> constexpr bool kScaled = std::is_same_v<T, _Float16>;
 
 // fp16: the power of two that brings the largest |dy| to 1 .. 2 (1 where that is zero or no finite number).
@@ -487,45 +485,72 @@ int64_t up_to(int64_t n, int64_t d) { return (n + d - 1) / d; }
         if (e_ != hipSuccess) return e_;    \
     } while (0)
 
-// Tiles of F x R places that cover a job, and whether they give every CU a block.
-template <class X>
-bool tiled(GemmJob& job, int features, int blocks_wanted) {
-    job.f_tiles = (int)up_to(features, X::OUT);
-    job.r_tiles = (int)up_to(job.rows, X::TR);
-    return (int64_t)job.f_tiles * job.r_tiles >= blocks_wanted;
+// What a product's partial sums cost to write, read and join, in us.
+float join_time(int splits, int64_t values) { return splits < 2 ? 0.0f : 4.0f + (float)values * (float)(8 * splits + 2) / 4.0e6f; }
+
+// The tiles that are expected to take the least time for jobs of features x rows, in `splits` ranges of the reduction each.
+struct Choice {
+    int kind;
+    float time;
+};
+Choice choose(int cols, bool gated, int jobs, const int* features, const int* rows, int parts, int splits) {
+    Choice best{kSmall, 0.0f};
+    for (int k = 0; k < kTileKinds; ++k) {
+        // Gated: half of a tile's features are the output's; the smallest has 64 x 128 places.
+        const int f = kTileCost[k].f / (gated ? 2 : 1), r = gated && k == kSmall ? 128 : kTileCost[k].r;
+        int64_t tiles = 0;
+        for (int n = 0; n < jobs; ++n) tiles += up_to(features[n], f) * up_to(rows[n], r);
+        float t = tile_time(k, cols, tiles * splits, (float)((parts + splits - 1) / splits));
+        if (gated && k == kSmall) t *= 1.7f;
+        if (k == 0 || t < best.time) best = {k, t};
+    }
+    return best;
 }
 
-template <class T, bool FCOL, bool RCOL, bool SUMS> using Big = Tile<T, 2, 4, 4, 2, 2, FCOL, RCOL, false, SUMS>;
-template <class T, bool FCOL, bool RCOL, bool SUMS> using Mid = Tile<T, 2, 2, 2, 2, 2, FCOL, RCOL, false, SUMS>;
-template <class T, bool FCOL, bool RCOL, bool SUMS> using Small = Tile<T, 2, 2, 1, 1, 4, FCOL, RCOL, false, SUMS>;
-template <class T> using BigGate = Tile<T, 2, 4, 4, 2, 2, false, false, true>;
-template <class T> using MidGate = Tile<T, 2, 2, 2, 2, 2, false, false, true>;
-template <class T> using SmallGate = Tile<T, 1, 4, 2, 1, 3, false, false, true>;
+// The number of ranges that makes up for its join, at most 8.
+int choose_splits(int cols, int jobs, const int* features, const int* rows, int parts) {
+    int best = 1;
+    float least = choose(cols, false, jobs, features, rows, parts, 1).time;
+    int64_t values = 0;
+    for (int n = 0; n < jobs; ++n) values += (int64_t)rows[n] * padded(features[n]);
+    for (int s = 2; s <= 8 && 4 * s <= parts; ++s) {
+        const float t = choose(cols, false, jobs, features, rows, parts, s).time + join_time(s, values);
+        if (t < least) {
+            least = t;
+            best = s;
+        }
+    }
+    return best;
+}
+
+int parts_of(int len) { return (len + 63) / 64; }
+
+template <class X>
+void tiled(GemmJob& job) {
+    job.f_tiles = (int)up_to(job.features, X::OUT);
+    job.r_tiles = (int)up_to(job.rows, X::TR);
+}
 
 template <class T, int ACT>
 hipError_t gate(const FeedDev& d, GemmJob job, hipStream_t st) {
-    auto go = [&](auto x) {
+    return with_tile<T, false, false, true, false>(choose(0, true, 1, &job.features, &job.rows, parts_of(job.len), 1).kind, [&](auto x) {
         typedef decltype(x) X;
+        tiled<X>(job);
         k_feed_gate<X, ACT><<<(unsigned)((int64_t)job.f_tiles * job.r_tiles), X::THREADS, 0, st>>>(d, job);
         return hipGetLastError();
-    };
-    if (tiled<BigGate<T>>(job, d.hidden, kCUs)) return go(BigGate<T>{});
-    if (tiled<MidGate<T>>(job, d.hidden, kCUs)) return go(MidGate<T>{});
-    tiled<SmallGate<T>>(job, d.hidden, 0);
-    return go(SmallGate<T>{});
+    });
 }
 
 template <class T, bool FCOL>
 hipError_t plain(PlainDev p, GemmJob job, hipStream_t st) {
-    auto go = [&](auto x) {
+    const int parts = parts_of(job.len) * (job.f[1] ? 2 : 1);
+    p.feature_pad = padded(job.features);
+    FEED_TRY((with_tile<T, FCOL, false, false, false>(choose(FCOL, false, 1, &job.features, &job.rows, parts, p.splits).kind, [&](auto x) {
         typedef decltype(x) X;
+        tiled<X>(job);
         k_feed_plain<X><<<(unsigned)((int64_t)job.f_tiles * job.r_tiles * p.splits), X::THREADS, 0, st>>>(p, job);
         return hipGetLastError();
-    };
-    if (tiled<Big<T, FCOL, false, false>>(job, job.features, kCUs)) return go(Big<T, FCOL, false, false>{});
-    if (tiled<Mid<T, FCOL, false, false>>(job, job.features, kCUs)) return go(Mid<T, FCOL, false, false>{});
-    tiled<Small<T, FCOL, false, false>>(job, job.features, 0);
-    FEED_TRY(go(Small<T, FCOL, false, false>{}));
+    })));
     if (p.splits > 1) {
         k_feed_join<T><<<(unsigned)up_to((int64_t)job.rows * (p.feature_pad / 8), 256), 256, 0, st>>>(p, job.rows, job.features);
         return hipGetLastError();
@@ -535,35 +560,34 @@ hipError_t plain(PlainDev p, GemmJob job, hipStream_t st) {
 
 template <class T, int ACT>
 hipError_t grad(const FeedDev& d, GemmJob job, hipStream_t st) {
-    auto go = [&](auto x) {
+    return with_tile<T, true, false, false, false>(choose(1, false, 1, &job.features, &job.rows, parts_of(job.len), 1).kind, [&](auto x) {
         typedef decltype(x) X;
+        tiled<X>(job);
         k_feed_grad<X, ACT><<<(unsigned)((int64_t)job.f_tiles * job.r_tiles), X::THREADS, 0, st>>>(d, job);
         return hipGetLastError();
-    };
-    if (tiled<Big<T, true, false, false>>(job, job.features, kCUs)) return go(Big<T, true, false, false>{});
-    if (tiled<Mid<T, true, false, false>>(job, job.features, kCUs)) return go(Mid<T, true, false, false>{});
-    tiled<Small<T, true, false, false>>(job, job.features, 0);
-    return go(Small<T, true, false, false>{});
+    });
 }
 
 template <class T>
 hipError_t weights(WeightsDev w, hipStream_t st) {
-    auto count = [&](auto x) {
+    int features[3], rows[3];
+    int64_t at = 0;
+    for (int n = 0; n < w.jobs; ++n) {
+        features[n] = w.job[n].features;
+        rows[n] = w.job[n].rows;
+        w.part[n] = at;
+        at += (int64_t)w.splits * rows[n] * (padded(features[n]) + 8);
+    }
+    FEED_TRY((with_tile<T, true, true, false, true>(choose(2, false, w.jobs, features, rows, parts_of(w.job[0].len), w.splits).kind, [&](auto x) {
         typedef decltype(x) X;
         w.first[0] = 0;
         for (int n = 0; n < w.jobs; ++n) {
-            tiled<X>(w.job[n], w.job[n].features, 0);
+            tiled<X>(w.job[n]);
             w.first[n + 1] = w.first[n] + w.job[n].f_tiles * w.job[n].r_tiles;
         }
-        return w.first[w.jobs];
-    };
-    auto go = [&](auto x) {
-        typedef decltype(x) X;
-        k_feed_weights<X><<<(unsigned)(count(x) * w.splits), X::THREADS, 0, st>>>(w);
+        k_feed_weights<X><<<(unsigned)(w.first[w.jobs] * w.splits), X::THREADS, 0, st>>>(w);
         return hipGetLastError();
-    };
-    if (count(Big<T, true, true, true>{}) * w.splits >= 192) FEED_TRY(go(Big<T, true, true, true>{}));
-    else FEED_TRY(go(Mid<T, true, true, true>{}));
+    })));
     if (w.splits > 1) {
         k_feed_weights_join<T><<<dim3(1024, (unsigned)w.jobs), 256, 0, st>>>(w);
         return hipGetLastError();
@@ -627,7 +651,7 @@ hipError_t forward(const FeedDev& d, hipStream_t st) {
     const void* dn = c.use(d.down, d.down_pad, d.out, d.hidden, ds);
     FEED_TRY(c.run<T>(st));
     FEED_TRY((gate<T, ACT>(d, GemmJob{{g, u}, {x, nullptr}, gs, xs, d.hidden, d.rows, d.in, 0, 0}, st)));
-    const PlainDev p{d.down_bias, d.y, d.y_stride, nullptr, nullptr, 1, 0};
+    const PlainDev p{d.down_bias, d.y, d.y_stride, d.part, nullptr, d.down_splits, 0};
     return plain<T, false>(p, GemmJob{{dn, nullptr}, {d.h, nullptr}, ds, d.hidden_pad, d.out, d.rows, d.hidden, 0, 0}, st);
 }
 
@@ -668,7 +692,7 @@ hipError_t backward(const FeedDev& d, hipStream_t st) {
     }
     const float* largest = kScaled<T> ? d.largest : nullptr;
     if (d.dx) {
-        const PlainDev p{nullptr, d.dx, d.in, nullptr, largest, 1, 0};
+        const PlainDev p{nullptr, d.dx, d.in, d.part, largest, d.dx_splits, 0};
         FEED_TRY((plain<T, true>(p, GemmJob{{g, u}, {d.dz, d.du}, gs, d.hidden_pad, d.in, d.rows, d.hidden, 0, 0}, st)));
     }
     WeightsDev w{};
@@ -683,7 +707,8 @@ hipError_t backward(const FeedDev& d, hipStream_t st) {
     add(x, xs, d.du, d.hidden_pad, d.hidden, d.in, d.dup, d.dup_bias, largest);
     add(d.h, d.hidden_pad, dy, ys, d.out, d.hidden, d.ddown, d.ddown_bias, nullptr);
     if (w.jobs == 0) return hipSuccess;
-    w.splits = 1;
+    w.splits = d.weight_splits;
+    w.parts = d.part;
     return weights<T>(w, st);
 }
 
@@ -700,6 +725,23 @@ hipError_t dispatch(int dtype, int act, F f) {
 }  // namespace
 
 bool feed_few(int64_t rows) { return rows <= 64; }
+
+size_t feed_plan(FeedDev& d, bool backward) {
+    d.down_splits = d.dx_splits = d.weight_splits = 1;
+    if (d.rows == 0 || (!backward && feed_few(d.rows))) return 0;
+    if (!backward) {
+        d.down_splits = choose_splits(0, 1, &d.out, &d.rows, parts_of(d.hidden));
+        return d.down_splits > 1 ? (size_t)d.down_splits * d.rows * padded(d.out) * sizeof(float) : 0;
+    }
+    d.dx_splits = choose_splits(1, 1, &d.in, &d.rows, 2 * parts_of(d.hidden));
+    const int features[3] = {d.in, d.in, d.hidden}, rows[3] = {d.hidden, d.hidden, d.out};
+    d.weight_splits = choose_splits(2, 3, features, rows, parts_of(d.rows));
+    size_t dx = 0, weights = 0;
+    if (d.dx_splits > 1) dx = (size_t)d.dx_splits * d.rows * padded(d.in);
+    if (d.weight_splits > 1)
+        for (int n = 0; n < 3; ++n) weights += (size_t)d.weight_splits * rows[n] * (padded(features[n]) + 8);
+    return (dx > weights ? dx : weights) * sizeof(float);
+}
 
 hipError_t feed_forward(const FeedDev& d, int dtype, int act, hipStream_t st) {
     return dispatch(dtype, act, [&](auto t, auto a) { return forward<decltype(t), decltype(a)::value>(d, st); });

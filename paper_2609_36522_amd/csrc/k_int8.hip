@@ -9,8 +9,6 @@ namespace pa {
 
 namespace {
 
-constexpr int kCUs = 256;
-
 // ------------------------------------------------------------------ rows to 8 bits
 // A row's magnitudes are compared as their bit patterns, in which NaN is larger than infinity and that than any
 // number.
@@ -201,13 +199,6 @@ __global__ __launch_bounds__(1024) void k_int8_few(Int8Dev d) {
     static_cast<T*>(d.y)[(int64_t)row * d.y_stride + o] = (T)scaled<T>(d, v, d.x_scale[row], o);
 }
 
-template <class X>
-bool tiled(GemmJob& job, int blocks_wanted) {
-    job.f_tiles = (job.features + X::TF - 1) / X::TF;
-    job.r_tiles = (int)(((int64_t)job.rows + X::TR - 1) / X::TR);
-    return (int64_t)job.f_tiles * job.r_tiles >= blocks_wanted;
-}
-
 template <class T>
 hipError_t linear(const Int8Dev& d, hipStream_t st) {
     if (d.rows <= 64) {
@@ -218,18 +209,24 @@ hipError_t linear(const Int8Dev& d, hipStream_t st) {
         return hipGetLastError();
     }
     GemmJob job{{d.w, nullptr}, {d.x, nullptr}, d.w_stride, d.x_stride, d.out, d.rows, d.in, 0, 0};
-    auto go = [&](auto x) {
+    // Twice the elements a part at twice the rate: the same rule in parts.
+    int kind = 0;
+    float least = 0.0f;
+    for (int k = 0; k < kTileKinds; ++k) {
+        const int64_t tiles = (int64_t)((d.out + kTileCost[k].f - 1) / kTileCost[k].f) * ((d.rows + (int64_t)kTileCost[k].r - 1) / kTileCost[k].r);
+        const float t = tile_time(k, 0, tiles, (float)((d.in + 127) / 128));
+        if (k == 0 || t < least) {
+            least = t;
+            kind = k;
+        }
+    }
+    return with_tile<int8_t, false, false, false, false>(kind, [&](auto x) {
         typedef decltype(x) X;
+        job.f_tiles = (job.features + X::TF - 1) / X::TF;
+        job.r_tiles = (int)(((int64_t)job.rows + X::TR - 1) / X::TR);
         k_int8_tile<X, T><<<(unsigned)((int64_t)job.f_tiles * job.r_tiles), X::THREADS, 0, st>>>(d, job);
         return hipGetLastError();
-    };
-    typedef Tile<int8_t, 2, 4, 4, 2, 2, false, false> Big;
-    typedef Tile<int8_t, 2, 2, 2, 2, 2, false, false> Mid;
-    typedef Tile<int8_t, 2, 2, 1, 1, 4, false, false> Small;
-    if (tiled<Big>(job, kCUs)) return go(Big{});
-    if (tiled<Mid>(job, kCUs)) return go(Mid{});
-    tiled<Small>(job, 0);
-    return go(Small{});
+    });
 }
 
 template <class T>

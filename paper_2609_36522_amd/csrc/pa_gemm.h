@@ -329,4 +329,44 @@ __device__ __forceinline__ void tile_of(const GemmJob& job, int id, int& f, int&
     r = g * group + in - f * rows;
 }
 
+// ------------------------------------------------------------------ which tiles (host)
+constexpr int kCUs = 256;
+
+enum { kBig, kWide, kMid, kSmall, kTileKinds };
+
+// What a launch of tiles is expected to take, in us: rounds of as many tiles as the CUs hold at once (one of 256 x 256,
+// two of the others a CU), each so much a part of the reduction and so much besides. Measured in bf16 with one and with two tiles
+// on every CU, for two kRow operands, one and no kRow operand. What the rule costs where it is wrong is little: the
+// tiles next to each other in it are. 8192x1024x4096 in us with 256 x 256, 128 x 192 and 128 x 128 tiles: 87, 77, 66;
+// 8192x4096x1024 72, 76, 81; 32768x2048x8192 869, 991, 1050; 9216x1024x8192 without a kRow operand 180, 166, 222.
+struct TileCost {
+    int f, r, at_once;
+    float one[3], all[3], besides;
+};
+constexpr TileCost kTileCost[kTileKinds] = {
+    {256, 256, 1, {1.75f, 1.75f, 1.75f}, {1.75f, 1.75f, 1.75f}, 8.0f},
+    {128, 192, 2, {0.75f, 0.84f, 0.90f}, {1.42f, 1.42f, 1.45f}, 8.0f},
+    {128, 128, 2, {0.63f, 0.70f, 0.75f}, {0.97f, 1.02f, 1.05f}, 7.0f},
+    {64, 64, 2, {0.28f, 0.34f, 0.35f}, {0.39f, 0.44f, 0.49f}, 4.0f},
+};
+
+// cols: operands that are not kRow (0 .. 2).
+inline float tile_time(int kind, int cols, int64_t tiles, float parts) {
+    const TileCost& c = kTileCost[kind];
+    const int64_t slots = (int64_t)kCUs * c.at_once, rounds = tiles / slots, rest = tiles % slots;
+    float t = (float)rounds * (parts * c.all[cols] + c.besides);
+    if (rest > 0) t += parts * (rest <= kCUs ? c.one[cols] : c.all[cols]) + c.besides;
+    return t;
+}
+
+// f(tile type) for a kind.
+template <class T, bool FCOL, bool RCOL, bool GATED, bool SUMS, class F>
+auto with_tile(int kind, F f) {
+    if (kind == kBig) return f(Tile<T, 2, 4, 4, 2, 2, FCOL, RCOL, GATED, SUMS>{});
+    if (kind == kWide) return f(Tile<T, 2, 2, 2, 3, 2, FCOL, RCOL, GATED, SUMS>{});
+    if (kind == kMid) return f(Tile<T, 2, 2, 2, 2, 2, FCOL, RCOL, GATED, SUMS>{});
+    if constexpr (GATED) return f(Tile<T, 1, 4, 2, 1, 3, FCOL, RCOL, GATED, SUMS>{});
+    else return f(Tile<T, 2, 2, 1, 1, 4, FCOL, RCOL, GATED, SUMS>{});
+}
+
 }  // namespace pa

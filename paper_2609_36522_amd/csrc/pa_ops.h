@@ -81,10 +81,10 @@ struct FeedDev {
     void *dz, *du;                   // backward: [rows][hidden_pad] gradients by the two projections
     void *x_pad, *gate_pad, *up_pad, *down_pad, *dy_pad;   // copies in whole pieces of 16 bytes (null: read in place)
     float* largest;                  // backward in fp16: kLargest partial maxima of |dy|
-    float* part;                     // backward: partial sums of the weights' gradients
+    float* part;                     // partial sums of y, or of dx and then of the weights' gradients
     int rows, in, hidden, out;
     int in_pad, hidden_pad, out_pad; // multiples of 8
-    int splits;                      // backward: ranges of rows whose weights' gradients are summed apart
+    int down_splits, dx_splits, weight_splits;   // ranges of a product's reduction that are summed apart
 };
 constexpr int kLargest = 256;
 
@@ -124,8 +124,8 @@ hipError_t group_backward(const GroupDev& d, int dtype, hipStream_t st);
 
 // Whether rows are read straight from memory (no copies in whole pieces).
 bool feed_few(int64_t rows);
-// How many ranges of rows the weights' gradients take.
-int feed_splits(const FeedDev& d);
+// Fills in the splits from the sizes; bytes of `part`.
+size_t feed_plan(FeedDev& d, bool backward);
 hipError_t feed_forward(const FeedDev& d, int dtype, int act, hipStream_t st);
 hipError_t feed_backward(const FeedDev& d, int dtype, int act, hipStream_t st);
 

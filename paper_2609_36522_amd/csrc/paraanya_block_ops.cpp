@@ -171,6 +171,7 @@ size_t feed_layout(const pa_feed_t* p, FeedDev& d, bool backward, bool with_save
         if (!in_place(p, d.hidden, d.down_stride)) d.down_pad = w.take((size_t)d.out * d.hidden_pad * 2);
         if (backward && !in_place(p, d.out, d.y_stride)) d.dy_pad = w.take((size_t)d.rows * d.out_pad * 2);
     }
+    if (const size_t n = feed_plan(d, backward)) d.part = static_cast<float*>(w.take(n));
     return w.used;
 }
 
