@@ -149,7 +149,8 @@ def _ptr(t):
 # ------------------------------------------------------------------ layer norm
 def _rows(t, N):
     """A [rows, N] view of t (a copy where its strides allow no view)."""
-    t = t.reshape(-1, N)
+    if t.dim() != 2:
+        t = t.reshape(-1, N)
     return t if t.stride(1) == 1 and (t.shape[0] < 2 or t.stride(0) >= N) else t.contiguous()
 
 
@@ -418,7 +419,8 @@ def lora_linear(x, weight, a, b, offsets, ids, *, scales=None, bias=None):
 def _pixels(t):
     """A [batch, pixels, channels] view of t with consecutive channels (a copy where its strides allow no view)."""
     B, Ch = t.shape[0], t.shape[-1]
-    t = t.reshape(B, math.prod(t.shape[1:-1]), Ch)
+    if t.dim() != 3:
+        t = t.reshape(B, math.prod(t.shape[1:-1]), Ch)
     return t if (t.stride(2) == 1 or Ch == 1) and (t.shape[1] < 2 or t.stride(1) >= Ch) else t.contiguous()
 
 
@@ -671,7 +673,8 @@ def quantize_rows(x):
 
 def _int8_rows(t, K):
     """A [rows, K] view of t whose rows start at multiples of 16 bytes (a copy where it has none)."""
-    t = t.reshape(-1, K)
+    if t.dim() != 2:
+        t = t.reshape(-1, K)
     if (t.stride(1) == 1 or K == 1) and t.data_ptr() % 16 == 0 and (t.shape[0] < 2 or (t.stride(0) >= K and t.stride(0) % 16 == 0)):
         return t
     out = torch.empty((t.shape[0], (K + 15) // 16 * 16), dtype=torch.int8, device=t.device)[:, :K]
