@@ -494,14 +494,14 @@ struct Choice {
     int kind;
     float time;
 };
-Choice choose(int cols, bool gated, int jobs, const int* features, const int* rows, int parts, int splits) {
+Choice choose(int cols, bool gated, int jobs, const int* features, const int* rows, int parts, int splits, const float* more = nullptr) {
     Choice best{kSmall, 0.0f};
     for (int k = 0; k < kTileKinds; ++k) {
         // Gated: half of a tile's features are the output's; the smallest has 64 x 128 places.
         const int f = kTileCost[k].f / (gated ? 2 : 1), r = gated && k == kSmall ? 128 : kTileCost[k].r;
         int64_t tiles = 0;
         for (int n = 0; n < jobs; ++n) tiles += up_to(features[n], f) * up_to(rows[n], r);
-        float t = tile_time(k, cols, tiles * splits, (float)((parts + splits - 1) / splits));
+        float t = tile_time(k, cols, tiles * splits, (float)((parts + splits - 1) / splits), more ? more[k] : 0.0f);
         if (gated && k == kSmall) t *= 1.7f;
         if (k == 0 || t < best.time) best = {k, t};
     }
@@ -561,7 +561,10 @@ hipError_t plain(PlainDev p, GemmJob job, hipStream_t st) {
 
 template <class T, int ACT>
 hipError_t grad(const FeedDev& d, GemmJob job, hipStream_t st) {
-    return with_tile<T, true, false, false, false>(choose(1, false, 1, &job.features, &job.rows, parts_of(job.len), 1).kind, [&](auto x) {
+    // The gate's derivative takes a wave longer than anything else that follows the products, and two blocks on a CU hide
+    // it behind each other's: 8192x1024x4096 165 us in tiles of 256 x 256, 131 of 128 x 192, 140 of 128 x 128.
+    constexpr float kMore[kTileKinds] = {46.0f, 18.0f, 12.0f, 4.0f};
+    return with_tile<T, true, false, false, false>(choose(1, false, 1, &job.features, &job.rows, parts_of(job.len), 1, kMore).kind, [&](auto x) {
         typedef decltype(x) X;
         tiled<X>(job);
         k_feed_grad<X, ACT><<<(unsigned)((int64_t)job.f_tiles * job.r_tiles), X::THREADS, 0, st>>>(d, job);

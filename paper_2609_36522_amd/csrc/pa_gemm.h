@@ -350,12 +350,12 @@ constexpr TileCost kTileCost[kTileKinds] = {
     {64, 64, 2, {0.28f, 0.34f, 0.35f}, {0.39f, 0.44f, 0.49f}, 4.0f},
 };
 
-// cols: operands that are not kRow (0 .. 2).
-inline float tile_time(int kind, int cols, int64_t tiles, float parts) {
+// cols: operands that are not kRow (0 .. 2); more: what a round of tiles takes besides on top of that.
+inline float tile_time(int kind, int cols, int64_t tiles, float parts, float more = 0.0f) {
     const TileCost& c = kTileCost[kind];
     const int64_t slots = (int64_t)kCUs * c.at_once, rounds = tiles / slots, rest = tiles % slots;
-    float t = (float)rounds * (parts * c.all[cols] + c.besides);
-    if (rest > 0) t += parts * (rest <= kCUs ? c.one[cols] : c.all[cols]) + c.besides;
+    float t = (float)rounds * (parts * c.all[cols] + c.besides + more);
+    if (rest > 0) t += parts * (rest <= kCUs ? c.one[cols] : c.all[cols]) + c.besides + more;
     return t;
 }
 
