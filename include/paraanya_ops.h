@@ -211,7 +211,7 @@ typedef struct {
     int32_t activation;          /* PA_ACT_* */
     int32_t alignment;           /* bytes that all pointers to x, the weights and dy are multiples of: 2 .. 16. Rows are
                                     read in place where it is 16 and strides and lengths are multiples of 8, and copied
-                                    into the workspace otherwise (beyond 64 rows). */
+                                    into the workspace otherwise (beyond 32 rows). */
     int64_t x_stride;            /* row strides: >= K */
     int64_t gate_stride, up_stride;         /* >= K */
     int64_t down_stride;         /* >= H */

@@ -281,7 +281,7 @@ __global__ __launch_bounds__(1024) void k_feed_few_gate(FeedDev d) {
     const bool valid = f < d.hidden;
     const T* const wp[2] = {static_cast<const T*>(d.gate) + (valid ? f : 0) * d.gate_stride, static_cast<const T*>(d.up) + (valid ? f : 0) * d.up_stride};
     f32x4 v[2];
-    few_rows<T, NR < 4 ? 2 : 1, NR, 2, WIDTH>(wp, valid, static_cast<const T*>(d.x), d.x_stride, d.rows, d.in, part, v);
+    few_rows<T, 2, NR, 2, WIDTH>(wp, valid, static_cast<const T*>(d.x), d.x_stride, d.rows, d.in, part, v);
     const int row = (w >> 2) * 16 + (lane & 15), o = f0 + 4 * (lane >> 4) + (w & 3);
     if (w >= 4 * NR || row >= d.rows || o >= d.hidden_pad) return;
     const bool in = o < d.hidden;
@@ -303,7 +303,7 @@ __global__ __launch_bounds__(1024) void k_feed_few_down(FeedDev d) {
     const bool valid = f < d.out && (lane & 15) < FEATURES;
     const T* const wp[1] = {static_cast<const T*>(d.down) + (valid ? f : f0) * d.down_stride};
     f32x4 v[1];
-    few_rows<T, NR == 1 ? 8 : NR < 4 ? 4 : 2, NR, 1, WIDTH>(wp, valid, static_cast<const T*>(d.h), d.hidden_pad, d.rows, d.hidden, part, v);
+    few_rows<T, NR == 1 ? 8 : 4, NR, 1, WIDTH>(wp, valid, static_cast<const T*>(d.h), d.hidden_pad, d.rows, d.hidden, part, v);
     const int row = (w >> 2) * 16 + (lane & 15), in = 4 * (lane >> 4) + (w & 3), o = f0 + in;
     if (w >= 4 * NR || row >= d.rows || in >= FEATURES || o >= d.out) return;
     static_cast<T*>(d.y)[(int64_t)row * d.y_stride + o] = (T)(v[0][0] + (d.down_bias ? (float)static_cast<const T*>(d.down_bias)[o] : 0.0f));
@@ -636,8 +636,7 @@ hipError_t forward_few(const FeedDev& d, hipStream_t st) {
         return hipGetLastError();
     };
     if (d.rows <= 16) return go(std::integral_constant<int, 1>{});
-    if (d.rows <= 32) return go(std::integral_constant<int, 2>{});
-    return go(std::integral_constant<int, 4>{});
+    return go(std::integral_constant<int, 2>{});
 }
 
 template <class T, int ACT>
@@ -730,7 +729,9 @@ hipError_t dispatch(int dtype, int act, F f) {
 
 }  // namespace
 
-bool feed_few(int64_t rows) { return rows <= 64; }
+// us for 17, 32 and 64 rows of 1024x4096, the weights read once straight from memory and in tiles: 17.2 and 21.5, 21.0 and
+// 20.9, 29.8 and 21.6; of 783x2539, where tiles need copies: 22.6 and 28.8 for 24, 34 and 29 for 64.
+bool feed_few(int64_t rows) { return rows <= 32; }
 
 size_t feed_plan(FeedDev& d, bool backward) {
     d.down_splits = d.dx_splits = d.weight_splits = 1;

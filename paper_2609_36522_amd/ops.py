@@ -139,7 +139,7 @@ def _size(query, p):
 
 
 def _workspace(n, like):
-    return torch.empty(n, dtype=torch.uint8, device=like.device) if n else None
+    return like.new_empty(n, dtype=torch.uint8) if n else None
 
 
 def _ptr(t):
@@ -460,9 +460,9 @@ def group_norm_forward(x, groups, weight=None, bias=None, eps=1e-5, *, activatio
     x3 = _pixels(x)
     B_, P, Ch = x3.shape
     _, ref, n, _ = _group(B_, P, Ch, groups, _DTYPE[x.dtype], _DTYPE[pt], act, eps, x3.stride()[:2], (P * Ch, Ch))
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    mean = torch.empty((B_, groups), dtype=torch.float32, device=x.device)
-    rstd = torch.empty((B_, groups), dtype=torch.float32, device=x.device)
+    y = x.new_empty(x.shape)
+    mean = x.new_empty((B_, groups), dtype=torch.float32)
+    rstd = x.new_empty((B_, groups), dtype=torch.float32)
     if P == 0:
         mean.zero_(), rstd.zero_()
     ws = _workspace(n, x)
@@ -494,9 +494,9 @@ def group_norm_backward(dy, x, mean, rstd, weight=None, bias=None, *, activation
     p, _, _, n = _group(B_, P, Ch, groups, _DTYPE[x.dtype], _DTYPE[pt], act, 0.0, x3.stride()[:2], (P * Ch, Ch))
     p = GroupNorm.from_buffer_copy(p)
     p.y_stride[:] = dy3.stride()[:2]
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    dw = torch.empty(Ch, dtype=pt, device=x.device)
-    db = torch.empty(Ch, dtype=pt, device=x.device)
+    dx = x.new_empty(x.shape)
+    dw = x.new_empty(Ch, dtype=pt)
+    db = x.new_empty(Ch, dtype=pt)
     ws = _workspace(n, x)
     B._check(_LIB.paraanya_group_norm_backward(C.byref(p), dy3.data_ptr(), x3.data_ptr(), _ptr(weight), _ptr(bias), mean.data_ptr(),
                                                rstd.data_ptr(), dx.data_ptr(), dw.data_ptr(), db.data_ptr(), _ptr(ws), n, st))
@@ -561,18 +561,20 @@ def _feed_args(x, gate, up, down, biases, activation, y=None):
     K, (H, N) = x.shape[-1], (gate.shape[0], down.shape[0])
     if gate.shape != (H, K) or up.shape != (H, K) or down.shape != (N, H) or min(K, H, N) < 1:
         raise ValueError("x, gate, up and down do not fit together")
+    dt = x.dtype
     for t, n in zip(biases, (H, H, N)):
         if t is not None and (t.shape != (n,) or not t.is_contiguous()):
             raise ValueError(f"a bias must be contiguous with {n} elements")
-    if any(t is not None and t.dtype != x.dtype for t in (gate, up, down, *biases, y)):
+        if t is not None and t.dtype != dt:
+            raise ValueError("x, the weights, the biases and dy must have one type")
+    if gate.dtype != dt or up.dtype != dt or down.dtype != dt or (y is not None and y.dtype != dt):
         raise ValueError("x, the weights, the biases and dy must have one type")
     if y is not None and y.shape != (*x.shape[:-1], N):
         raise ValueError("dy must have y's shape")
     st = _on_device(x, gate, up, down, *biases, y)
     x, gate, up, down = _rows(x, K), _rows(gate, K), _rows(up, K), _rows(down, H)
     y = None if y is None else _rows(y, N)
-    given = [t for t in (x, gate, up, down, y) if t is not None]
-    at = functools.reduce(lambda a, t: a | t.data_ptr(), given, 16)
+    at = 16 | x.data_ptr() | gate.data_ptr() | up.data_ptr() | down.data_ptr() | (0 if y is None else y.data_ptr())
     d = _feed(x.shape[0], K, H, N, _DTYPE[x.dtype], act, at & -at,
               (_stride(x), _stride(gate), _stride(up), _stride(down), N if y is None else _stride(y)))
     return d, x, gate, up, down, y, st
@@ -586,8 +588,8 @@ def feed_forward_forward(x, gate, up, down, gate_bias=None, up_bias=None, down_b
     needs: both projections and the gated product."""
     d, x2, g, u, dn, _, st = _feed_args(x, gate, up, down, (gate_bias, up_bias, down_bias), activation)
     _, ref, keep, plain, with_saved, _ = d
-    y = torch.empty((*x.shape[:-1], down.shape[0]), dtype=x.dtype, device=x.device)
-    saved = torch.empty(keep, dtype=torch.uint8, device=x.device) if save else None
+    y = x.new_empty((*x.shape[:-1], down.shape[0]))
+    saved = x.new_empty(keep, dtype=torch.uint8) if save else None
     n = with_saved if save else plain
     ws = _workspace(n, x)
     B._check(_LIB.paraanya_feed_forward(ref, x2.data_ptr(), g.data_ptr(), _ptr(gate_bias), u.data_ptr(), _ptr(up_bias), dn.data_ptr(),
@@ -608,7 +610,7 @@ def feed_forward_backward(dy, x, gate, up, down, saved, *, activation="silu", ne
     for i in (1, 2, 3):
         need[i] = need[i] or need[i + 3]
     shapes = (x.shape, gate.shape, up.shape, down.shape, (H,), (H,), (N,))
-    out = FeedGradients(*(torch.empty(s, dtype=x.dtype, device=x.device) if k else None for s, k in zip(shapes, need)))
+    out = FeedGradients(*(x.new_empty(s) if k else None for s, k in zip(shapes, need)))
     ws = _workspace(n, x)
     B._check(_LIB.paraanya_feed_forward_backward(ref, C.byref(FeedGrad(*map(_ptr, out))), dy2.data_ptr(), x2.data_ptr(), g.data_ptr(),
                                                  u.data_ptr(), dn.data_ptr(), _ptr(saved), keep, _ptr(ws), n, st))
@@ -640,8 +642,9 @@ def feed_forward(x, gate, up, down, gate_bias=None, up_bias=None, down_bias=None
 
 # ------------------------------------------------------------------ projection in 8-bit integers
 def _no_gradients(what, *tensors):
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
-        raise ValueError(f"{what} has no gradients: call it under torch.no_grad()")
+    for t in tensors:
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{what} has no gradients: call it under torch.no_grad()")
 
 
 @functools.lru_cache(maxsize=256)
@@ -665,8 +668,8 @@ def quantize_rows(x):
     x2 = _rows(x, K)
     M, wide = x2.shape[0], (K + 15) // 16 * 16
     _, ref = _quantize(M, K, _DTYPE[x.dtype], _stride(x2), wide)
-    q = torch.empty((*x.shape[:-1], wide), dtype=torch.int8, device=x.device)
-    scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    q = x.new_empty((*x.shape[:-1], wide), dtype=torch.int8)
+    scale = x.new_empty(x.shape[:-1], dtype=torch.float32)
     B._check(_LIB.paraanya_quantize_rows(ref, x2.data_ptr(), q.data_ptr(), scale.data_ptr(), st))
     return q if wide == K else q[..., :K], scale
 
@@ -705,16 +708,17 @@ def int8_linear(q, scale, weight, weight_scale, bias=None, *, dtype=torch.bfloat
     if q.dim() < 1 or weight.dim() != 2 or weight.shape[1] != q.shape[-1] or min(weight.shape) < 1:
         raise ValueError("expected q [..., K] and weight [N, K]")
     K, N = q.shape[-1], weight.shape[0]
-    for t, shape, name in ((scale, q.shape[:-1], "scale"), (weight_scale, (N,), "weight_scale")):
-        if t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous float32 tensor of the shape {tuple(shape)}")
+    if scale.dtype != torch.float32 or scale.shape != q.shape[:-1] or not scale.is_contiguous():
+        raise ValueError(f"scale must be a contiguous float32 tensor of the shape {tuple(q.shape[:-1])}")
+    if weight_scale.dtype != torch.float32 or weight_scale.shape != (N,) or not weight_scale.is_contiguous():
+        raise ValueError(f"weight_scale must be a contiguous float32 tensor of {N} elements")
     if bias is not None and (bias.dtype != dtype or bias.shape != (N,) or not bias.is_contiguous()):
         raise ValueError(f"bias must be contiguous with {N} elements of {dtype}")
     _no_gradients("int8 linear", scale, weight_scale, bias)
     st = _on_device(q, scale, weight, weight_scale, bias)
     q2, w = _int8_rows(q, K), _int8_rows(weight, K)
     _, ref = _int8(q2.shape[0], K, N, _DTYPE[dtype], _int8_stride(q2), _int8_stride(w))
-    y = torch.empty((*q.shape[:-1], N), dtype=dtype, device=q.device)
+    y = q.new_empty((*q.shape[:-1], N), dtype=dtype)
     B._check(_LIB.paraanya_int8_linear(ref, q2.data_ptr(), scale.data_ptr(), w.data_ptr(), weight_scale.data_ptr(), _ptr(bias),
                                        y.data_ptr(), st))
     return y
