@@ -89,18 +89,18 @@ __device__ __forceinline__ void clear(typename X::acc_t (&acc)[X::NM][X::NX], fl
     for (int j = 0; j < X::NX; ++j) sums[j] = 0.0f;
 }
 
-// Adds bias[f0 + ..] to NM tiles' registers.
-template <class T, int NM, int NX>
-__device__ __forceinline__ void add_bias(const void* bias, int f0, int n, int half, f32x16 (&acc)[NM][NX], int m0, int m1) {
-    if (!bias) return;
+// Adds a value for each feature to tiles m0 .. m0 + N - 1.
+template <int N, int NM, int NX>
+__device__ __forceinline__ void add(const float* per_feature, int half, f32x16 (&acc)[NM][NX], int m0) {
 #pragma unroll
-    for (int m = m0; m < m1; ++m)
+    for (int m = 0; m < N; ++m)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int f = f0 + (m - m0) * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
-            const float v = f < n ? (float)static_cast<const T*>(bias)[f] : 0.0f;
+        for (int q = 0; q < 4; ++q) {
+            const f32x4 v = PerFeature<N>::at(per_feature, m, q, half);
 #pragma unroll
-            for (int j = 0; j < NX; ++j) acc[m][j][r] += v;
+            for (int j = 0; j < NX; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[m0 + m][j][4 * q + i] += v[i];
         }
 }
 
@@ -114,13 +114,19 @@ __global__ __launch_bounds__(X::THREADS, 2) void k_feed_gate(FeedDev d, GemmJob 
     clear<X>(acc, sums);
     int f, r;
     tile_of(job, xcd_order(blockIdx.x, gridDim.x), f, r);
-    X::run(job, f * X::OUT, r * X::TR, 0, (job.len + X::PART - 1) / X::PART, lds, acc, sums);
     const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6;
     constexpr int HM = X::NM / 2;
     const int f0 = f * X::OUT + (w % X::WF) * HM * 32, r0 = r * X::TR + (w / X::WF) * X::NX * 32;
-    add_bias<T, X::NM, X::NX>(d.gate_bias, f0, d.hidden, half, acc, 0, HM);
-    add_bias<T, X::NM, X::NX>(d.up_bias, f0, d.hidden, half, acc, HM, X::NM);
+    const PerFeature<HM> bg(static_cast<const T*>(d.gate_bias), f0, d.hidden, lane), bu(static_cast<const T*>(d.up_bias), f0, d.hidden, lane);
+    X::run(job, f * X::OUT, r * X::TR, 0, (job.len + X::PART - 1) / X::PART, lds, acc, sums);
     char* own = lds + w * HM * 2048;
+    if (d.gate_bias || d.up_bias) {
+        float* per = reinterpret_cast<float*>(lds + X::THREADS / 64 * HM * 2048 + w * 512);
+        bg.put(per, lane);
+        bu.put(per + 64, lane);
+        add<HM>(per, half, acc, 0);
+        add<HM>(per + 64, half, acc, HM);
+    }
 #pragma unroll
     for (int j = 0; j < X::NX; ++j) {
         auto store = [&](void* to, auto value) {
@@ -162,12 +168,17 @@ __global__ __launch_bounds__(X::THREADS, 2) void k_feed_plain(PlainDev d, GemmJo
     int f, r;
     tile_of(job, id - split * tiles, f, r);
     const int parts = (job.len + X::PART - 1) / X::PART * (job.f[1] ? 2 : 1);
-    X::run(job, f * X::TF, r * X::TR, (int)((int64_t)parts * split / d.splits), (int)((int64_t)parts * (split + 1) / d.splits), lds, acc, sums);
     const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6;
     const int f0 = f * X::TF + (w % X::WF) * X::NM * 32, r0 = r * X::TR + (w / X::WF) * X::NX * 32;
+    const PerFeature<X::NM> bias(static_cast<const T*>(d.bias), f0, job.features, lane);
+    X::run(job, f * X::TF, r * X::TR, (int)((int64_t)parts * split / d.splits), (int)((int64_t)parts * (split + 1) / d.splits), lds, acc, sums);
     if (d.splits == 1) {
         const float s = d.largest ? 1.0f / gradient_scale<T>(d.largest) : 1.0f;
-        add_bias<T, X::NM, X::NX>(d.bias, f0, job.features, half, acc, 0, X::NM);
+        if (d.bias) {
+            float* per = reinterpret_cast<float*>(lds + X::THREADS / 64 * X::NM * 2048 + w * 512);
+            bias.put(per, lane);
+            add<X::NM>(per, half, acc, 0);
+        }
 #pragma unroll
         for (int j = 0; j < X::NX; ++j)
             through_lds<T, X::NM>(lds + w * X::NM * 2048, lane, [&](int m, int q) { return gather8<T>(acc[m][j], q, s); },

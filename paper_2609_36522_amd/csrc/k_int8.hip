@@ -133,35 +133,34 @@ __global__ __launch_bounds__(X::THREADS, 2) void k_int8_tile(Int8Dev d, GemmJob 
         for (int j = 0; j < X::NX; ++j) acc[m][j] = i32x16{};
     int f, r;
     tile_of(job, xcd_order(blockIdx.x, gridDim.x), f, r);
-    X::run(job, f * X::TF, r * X::TR, 0, (job.len + X::PART - 1) / X::PART, lds, acc, none);
     const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6;
     const int f0 = f * X::TF + (w % X::WF) * X::NM * 32, r0 = r * X::TR + (w / X::WF) * X::NX * 32;
+    const PerFeature<X::NM> scales(d.w_scale, f0, d.out, lane), biases(static_cast<const T*>(d.bias), f0, d.out, lane);
     float xs[X::NX];
 #pragma unroll
     for (int j = 0; j < X::NX; ++j) {
         const int row = r0 + j * 32 + (lane & 31);
         xs[j] = row < d.rows ? d.x_scale[row] : 0.0f;
     }
+    X::run(job, f * X::TF, r * X::TR, 0, (job.len + X::PART - 1) / X::PART, lds, acc, none);
     constexpr int CM = X::NM < 2 ? 1 : 2;                    // 64 features at a time: 128 bytes of a row
+    float* per = reinterpret_cast<float*>(lds + X::THREADS / 64 * CM * 2048 + w * 1024);
+    scales.put(per, lane);
+    biases.put(per + 128, lane);
 #pragma unroll
     for (int c = 0; c < X::NM; c += CM) {
         const int fc = f0 + c * 32;
-        float ws[CM][16], bias[CM][16];
-#pragma unroll
-        for (int m = 0; m < CM; ++m)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int at = fc + m * 32 + 8 * (i >> 2) + 4 * half + (i & 3), o = at < d.out ? at : d.out - 1;
-                ws[m][i] = d.w_scale[o];
-                bias[m][i] = d.bias ? (float)static_cast<const T*>(d.bias)[o] : 0.0f;
-            }
 #pragma unroll
         for (int j = 0; j < X::NX; ++j) {
             f32x16 v[CM];
 #pragma unroll
             for (int m = 0; m < CM; ++m)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) v[m][i] = (float)acc[c + m][j][i] * xs[j] * ws[m][i] + bias[m][i];
+                for (int q = 0; q < 4; ++q) {
+                    const f32x4 s = PerFeature<X::NM>::at(per, c + m, q, half), b = PerFeature<X::NM>::at(per + 128, c + m, q, half);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[m][4 * q + i] = (float)acc[c + m][j][4 * q + i] * xs[j] * s[i] + b[i];
+                }
             through_lds<T, CM>(lds + w * CM * 2048, lane, [&](int m, int q) { return gather8<T>(v[m], q, 1.0f); },
                                [&](int row, int at, const Pack8<T>& p) {
                                    if (r0 + j * 32 + row < d.rows)

@@ -302,6 +302,34 @@ __device__ __forceinline__ void through_lds(char* lds, int lane, F value, S put)
     __builtin_amdgcn_wave_barrier();
 }
 
+// A value for each of a wave's 32 NM features (biases, scales): loaded before the products, one a lane, and read from LDS
+// after them by the lanes whose registers hold the features. us of the
+// whole product with a load for each register from memory after the products, and so: 8 bits 32768x2048x8192 656, 585;
+// the gated projections of 8192x1024x4096 143, 127.
+template <int NM>
+struct PerFeature {
+    static constexpr int kEach = (NM * 32 + 63) / 64;
+    float v[kEach];
+    template <class T>
+    __device__ __forceinline__ PerFeature(const T* p, int f0, int n, int lane) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int f = f0 + i * 64 + lane;
+            v[i] = p ? (float)p[f < n ? f : n - 1] : 0.0f;
+        }
+    }
+    // lds: the wave's own NM * 128 bytes (256 at least).
+    __device__ __forceinline__ void put(float* lds, int lane) const {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) lds[i * 64 + lane] = v[i];
+        __builtin_amdgcn_wave_barrier();
+    }
+    // Of the features of accumulator registers 4 q .. + 3 of tile m.
+    __device__ __forceinline__ static f32x4 at(const float* lds, int m, int q, int half) {
+        return *reinterpret_cast<const f32x4*>(lds + m * 32 + q * 8 + half * 4);
+    }
+};
+
 // The other way: pieces of 32 rows x 32 NM features, lane after lane in the order in which they lie, to the places of
 // accumulator registers: out[m][q] are features 32 m + 8 q + 4 half .. + 3 of row lane % 32.
 template <int NM, class V>
