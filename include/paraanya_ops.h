@@ -200,10 +200,11 @@ PA_API int paraanya_group_norm_backward_workspace(const pa_group_norm_t* p, size
  * h = act(x G^T + bg) * (x U^T + bu), y = h D^T + bd: both projections, the activation and the product in one
  * kernel, the projection back in a second. h is rounded to the element type as the second product's operand; so are,
  * for the backward pass, the two projections, and the gradients by them as operands of the gradients of x and of the
- * weights (in fp16 multiplied by a power of two that brings the largest |dy| to 1 .. 2, so that small gradients
- * keep their digits). */
+ * weights (in fp16 multiplied by a power of two that brings the largest |dy| to 1/16 .. 1/8, so that small gradients
+ * keep their digits; they may be 2^19 times as large as dy). A gradient's error is so 1.3 to 1.8 times that of rounding the
+ * result alone. */
 typedef struct {
-    int64_t rows;                /* 0 .. 2^30 */
+    int64_t rows;                /* 0 .. 2^30; a matrix has at most 2^34 elements and 2^23 tiles of 64 x 64 */
     int32_t in_features;         /* K: 1 .. 2^20 */
     int32_t hidden_features;     /* H: 1 .. 2^20 */
     int32_t out_features;        /* N: 1 .. 2^20 */
@@ -219,7 +220,8 @@ typedef struct {
 } pa_feed_t;
 
 /* gate and up [H][K], down [N][H]; biases [H], [H] and [N] or NULL. saved: what the backward pass needs (256-byte
- * aligned, of the size that paraanya_feed_forward_saved reports; the caller keeps it), or NULL. */
+ * aligned, of the size that paraanya_feed_forward_saved reports; the caller keeps it), or NULL. Nothing that is written,
+ * here or by the backward pass, may overlap an input. */
 PA_API int paraanya_feed_forward(const pa_feed_t* p, const void* x, const void* gate, const void* gate_bias, const void* up,
                                  const void* up_bias, const void* down, const void* down_bias, void* y, void* saved,
                                  size_t saved_bytes, void* workspace, size_t workspace_bytes, void* stream);
@@ -255,7 +257,8 @@ PA_API int paraanya_quantize_rows(const pa_quantize_t* p, const void* x, int8_t*
 
 /* y = (xq wq^T) x_scale w_scale + bias: 8-bit products summed in 32-bit integers (exact), then one fp32 product with the
  * row's scale, one with the channel's, and the bias added. xq [rows][K], wq [N][K] with rows of any
- * multiple of 16 bytes at 16-byte addresses; bytes past K up to the next multiple of 16 are read and have no effect. */
+ * multiple of 16 bytes at 16-byte addresses; bytes past K up to the next multiple of 16 are read and have no effect.
+ * Neither this nor paraanya_quantize_rows writes into an input. */
 typedef struct {
     int64_t rows;                /* 0 .. 2^30 */
     int32_t in_features;         /* K: 1 .. PA_INT8_MAX_IN */

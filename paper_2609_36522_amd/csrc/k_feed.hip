@@ -18,7 +18,8 @@ namespace {
 
 template <class T> constexpr bool kScaled = std::is_same_v<T, _Float16>;
 
-// fp16: the power of two that brings the largest |dy| to 1 .. 2 (1 where that is zero or no finite number).
+// fp16: the power of two that brings the largest |dy| to 1/16 .. 1/8 (1 where that is zero or no finite number): dz and du
+// may grow to 2^19 times dy before they overflow, and lose digits (2^-25 of absolute error) only below 2^-10 of it.
 template <class T>
 __device__ __forceinline__ float gradient_scale(const float* largest) {
     if constexpr (!kScaled<T>) return 1.0f;
@@ -27,7 +28,7 @@ __device__ __forceinline__ float gradient_scale(const float* largest) {
 #pragma unroll
     for (int i = 32; i >= 1; i >>= 1) m = fmaxf(m, __shfl_xor(m, i));
     const int e = (int)(__builtin_bit_cast(uint32_t, m) >> 23);
-    return e == 0 || e == 255 ? 1.0f : __builtin_bit_cast(float, (uint32_t)(254 - e) << 23);
+    return e == 0 || e == 255 ? 1.0f : __builtin_bit_cast(float, (uint32_t)(250 - e) << 23);
 }
 
 // Partial maxima of |dy|; a NaN among them stays out (it is in every gradient anyway).
@@ -58,11 +59,12 @@ struct CopyDev {
 };
 
 template <class T>
-__global__ __launch_bounds__(256) void k_feed_copy(CopyDev d) {
+__global__ __launch_bounds__(256) void k_feed_copy(CopyDev d, int64_t block0) {
+    const int64_t block = block0 + blockIdx.x;
     int i = 0;
-    while (blockIdx.x >= d.first[i + 1]) ++i;
+    while (block >= d.first[i + 1]) ++i;
     const int pieces = (d.cols[i] + 7) / 8;
-    const int64_t at = (blockIdx.x - d.first[i]) * 256 + threadIdx.x, row = at / pieces;
+    const int64_t at = (block - d.first[i]) * 256 + threadIdx.x, row = at / pieces;
     if (row >= d.rows[i]) return;
     reinterpret_cast<Pack8<T>*>(d.to[i])[at] =
         load8(static_cast<const T*>(d.from[i]) + row * d.stride[i], (int)(at - row * pieces) * 8, d.cols[i]);
@@ -628,9 +630,12 @@ struct Copies {
     }
     template <class T>
     hipError_t run(hipStream_t st) const {
-        if (n == 0) return hipSuccess;
-        k_feed_copy<T><<<(unsigned)d.first[n], 256, 0, st>>>(d);
-        return hipGetLastError();
+        constexpr int64_t most = 1 << 23;            // a grid holds fewer than 2^32 threads
+        for (int64_t b = 0; n > 0 && b < d.first[n]; b += most) {
+            k_feed_copy<T><<<(unsigned)(d.first[n] - b < most ? d.first[n] - b : most), 256, 0, st>>>(d, b);
+            FEED_TRY(hipGetLastError());
+        }
+        return hipSuccess;
     }
 };
 

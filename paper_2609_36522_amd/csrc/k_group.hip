@@ -674,6 +674,8 @@ __global__ __launch_bounds__(kBlock) void k_group_bwd_whole(GroupDev d) {
 }
 
 // ------------------------------------------------------------------ launches
+int64_t parts_of(int64_t n, int64_t size) { return (n + size - 1) / size; }
+
 // Pixels of a thread that the one-launch kernels hold.
 constexpr int kHeld = 8;
 
@@ -735,7 +737,7 @@ void group_plan(GroupDev& d, int dtype, bool backward) {
     if (chunk < lanes * (backward ? 2 : 4)) chunk = lanes * (backward ? 2 : 4);
     if ((d.pixels + chunk - 1) / chunk > 256) chunk = (d.pixels + 255) / 256;
     d.chunk = (int)(chunk < 1 ? 1 : chunk);
-    d.chunks = d.pixels > 0 ? (d.pixels + d.chunk - 1) / d.chunk : 1;
+    d.chunks = d.pixels > 0 ? (int)parts_of(d.pixels, d.chunk) : 1;
     int64_t spread = (d.pixels + want - 1) / want;
     if (spread < lanes * 2) spread = lanes * 2;
     d.spread = (int)spread;
@@ -756,7 +758,7 @@ hipError_t group_forward(const GroupDev& d, int dtype, hipStream_t st) {
         k_group_stats<T, WIDTH><<<grid, kBlock, 0, st>>>(d);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        grid.x = (unsigned)((d.pixels + d.spread - 1) / d.spread);
+        grid.x = (unsigned)parts_of(d.pixels, d.spread);
         k_group_apply<T, WIDTH><<<grid, kBlock, 0, st>>>(d);
         return hipGetLastError();
     });
@@ -775,7 +777,7 @@ hipError_t group_backward(const GroupDev& d, int dtype, hipStream_t st) {
             k_group_join<<<dim3((unsigned)d.groups, (unsigned)d.batch), 256, 0, st>>>(d);
             e = hipGetLastError();
             if (e != hipSuccess) return e;
-            const unsigned blocks = d.dx ? (unsigned)((int64_t)((d.pixels + d.spread - 1) / d.spread) * d.slabs * d.batch) : 0;
+            const unsigned blocks = d.dx ? (unsigned)(parts_of(d.pixels, d.spread) * d.slabs * d.batch) : 0;
             if (blocks + params > 0) k_group_dx<T, WIDTH><<<blocks + params, kBlock, 0, st>>>(d, blocks);
             return hipGetLastError();
         }

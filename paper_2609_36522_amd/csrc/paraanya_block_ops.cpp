@@ -101,12 +101,14 @@ int check_feed(const pa_feed_t* p) {
     if (p->x_stride < p->in_features || p->gate_stride < p->in_features || p->up_stride < p->in_features ||
         p->down_stride < p->hidden_features || p->y_stride < p->out_features)
         return fail(PA_ERR_INVALID_ARG, "feed forward: row strides must be at least the row's length");
-    // Tiles of 64 x 64 of every product, and threads of the copies, fit a grid.
+    // Tiles of 64 x 64 of every product fit a grid.
     const int64_t most = 1ll << 34;
     const int64_t wide = p->in_features > p->hidden_features ? (p->in_features > p->out_features ? p->in_features : p->out_features)
                                                              : (p->hidden_features > p->out_features ? p->hidden_features : p->out_features);
     if (p->rows * wide > most || (int64_t)p->hidden_features * (p->in_features > p->out_features ? p->in_features : p->out_features) > most)
         return fail(PA_ERR_UNSUPPORTED, "feed forward: more than 2^34 elements in a matrix");
+    if ((p->rows + 63) / 64 * ((wide + 63) / 64) > kMaxBlocks)
+        return fail(PA_ERR_UNSUPPORTED, "feed forward: more than 2^23 tiles of 64 x 64 elements in a matrix");
     return PA_OK;
 }
 

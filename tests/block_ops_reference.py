@@ -95,8 +95,9 @@ def feed_forward(x, gate, up, down, biases=(None, None, None), act="silu", dy=No
     ep, eq = ep + u * p.abs() + tiny, eq + u * q.abs() + tiny
     dh, edh = Y @ D, (N + 8) * U32 * (Y.abs() @ D.abs())
     dz, du = dh * q * slope, dh * a
-    # In fp16 they are stored relative to the largest |dy|.
-    small = tiny * (float(Y.abs().max()) if dt == torch.float16 and Y.numel() else 1.0)
+    # In fp16 they are stored times a power of two s with s max |dy| >= 1/16: half of the least spacing over s is at most
+    # 16 max |dy| times it.
+    small = 16 * tiny * (float(Y.abs().max()) if dt == torch.float16 and Y.numel() else 1.0)
     edz = edh * ((q.abs() + eq) * (slope.abs() + CURVE * ep + es)) + dh.abs() * (eq * slope.abs() + (q.abs() + eq) * (CURVE * ep + es)) \
         + (u + 3 * U32) * dz.abs() + small
     edu = edh * (a.abs() + SLOPE * ep + ea) + dh.abs() * (SLOPE * ep + ea) + (u + 2 * U32) * du.abs() + small

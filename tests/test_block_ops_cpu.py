@@ -119,7 +119,8 @@ FEED = dict(rows=200, in_features=64, hidden_features=96, out_features=32, dtype
     (dict(dtype=9), -1, "dtype"), (dict(activation=-1), -1, "activation"), (dict(alignment=3), -1, "alignment"), (dict(alignment=32), -1, "alignment"),
     (dict(x_stride=63), -1, "strides"), (dict(gate_stride=1), -1, "strides"), (dict(up_stride=0), -1, "strides"),
     (dict(down_stride=95), -1, "strides"), (dict(y_stride=31), -1, "strides"),
-    (dict(rows=1 << 30, in_features=64), -6, "elements"), (dict(hidden_features=1 << 20, down_stride=1 << 20, in_features=1 << 20, x_stride=1 << 20,
+    (dict(rows=1 << 30, in_features=64), -6, "elements"),
+    (dict(rows=1 << 30, in_features=16, hidden_features=8, out_features=8), -6, "tiles"), (dict(hidden_features=1 << 20, down_stride=1 << 20, in_features=1 << 20, x_stride=1 << 20,
                                                                 gate_stride=1 << 20, up_stride=1 << 20), -6, "elements"),
 ])
 def test_feed_forward_refuses(kw, code, frag):

@@ -254,6 +254,21 @@ def test_feed_forward_in_fp16_keeps_small_and_large_gradients(M, f):
     _check_feed(*_feed_case(M, 64, 96, 64, F16, f=f))
 
 
+@pytest.mark.parametrize("M", [20, 300])
+def test_feed_forward_in_fp16_with_a_large_gain(M):
+    """dz up to 2^17 times the largest dy: finite in fp16, and to be kept so by the scale."""
+    x, gate, up, down, biases, dy = _feed_case(M, 64, 96, 1024, F16, f=2.0**-12)
+    gate, up, down = (gate.float() / 64).half(), (up.float() * 1024).half(), (down.float() * 2 * math.sqrt(96)).half()
+    ref = R.feed_forward(x, gate, up, down, biases, None, dy)
+    assert float(ref["x"][0].abs().max()) < 65504
+    _, saved = ops.feed_forward_forward(x, gate, up, down, *biases, activation=None)
+    grads = ops.feed_forward_backward(dy, x, gate, up, down, saved, activation=None)
+    for name in ("x", "gate", "up", "gate_bias", "up_bias"):
+        got = getattr(grads, name)
+        assert bool(torch.isfinite(got).all()) or not bool((ref[name][0].abs() < 65504).all()), name
+        check(got, *ref[name], name)
+
+
 def test_feed_forward_not_a_number_stays_in_its_row():
     for M in (20, 150):
         x, gate, up, down, biases, dy = _feed_case(M, 60, 90, 50, BF16)
@@ -455,6 +470,53 @@ def test_captured_calls_replay_on_new_inputs():
             want = call(*held)
             torch.cuda.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(got, want)), (name, k)
+
+
+# ------------------------------------------------------------------ more than 2^31 elements or bytes
+def test_group_norm_offsets_beyond_31_bits():
+    g = _gen(1)
+    w, b = _randn(g, 320, dtype=BF16), _randn(g, 320, dtype=BF16)
+    x = torch.zeros(2250, 3000, 320, dtype=BF16, device="cuda")          # long samples: 2.2e9 elements
+    dy = torch.zeros_like(x)
+    x[-1], dy[-1] = _randn(g, 3000, 320, dtype=BF16), _randn(g, 3000, 320, dtype=BF16)
+    y, mean, rstd = ops.group_norm_forward(x, 32, w, b, activation="silu")
+    got = ops.group_norm_backward(dy, x, mean, rstd, w, b, activation="silu")
+    ref = R.group_norm(x[-1:], 32, w, b, 1e-5, "silu", dy[-1:])
+    for name, t in (("y", y[-1:]), ("dx", got[0][-1:]), ("dw", got[1]), ("db", got[2])):
+        check(t, *ref[name], name)
+    flat = x.view(-1)
+    far = flat.as_strided((1, 64, 320), (0, 34_200_000, 1))
+    far.copy_(_randn(g, 1, 64, 320))
+    check(ops.group_norm_forward(far, 32, w, b)[0], *R.group_norm(far, 32, w, b, 1e-5, None)["y"], "pixels far apart")
+
+
+def test_feed_forward_offsets_beyond_31_bits():
+    """2.3e9 elements in each intermediate; only the last rows have gradients, so that the weights' are theirs."""
+    x, gate, up, down, biases, _ = _feed_case(140_000, 32, 16384, 24, BF16)
+    dy = torch.zeros(140_000, 24, dtype=BF16, device="cuda")
+    dy[-50:] = _randn(_gen(3), 50, 24, dtype=BF16)
+    y, saved = ops.feed_forward_forward(x, gate, up, down, *biases)
+    grads = ops.feed_forward_backward(dy, x, gate, up, down, saved)
+    ref = R.feed_forward(x[-50:], gate, up, down, biases, "silu", dy[-50:])
+    check(y[-50:], *ref["y"], "y")
+    check(grads.x[-50:], *ref["x"], "x")
+    assert not bool(grads.x[:-50].any())
+    for name in ops.FeedGradients._fields[1:]:
+        check(getattr(grads, name), *ref[name], name)
+
+
+def test_8_bit_offsets_beyond_31_bits():
+    g = _gen(5)
+    x = torch.zeros(70_000, 32768, dtype=BF16, device="cuda")
+    x[-40:] = _randn(g, 40, 32768)
+    q, scale = ops.quantize_rows(x)
+    want, s = R.quantize_rows(x[-40:])
+    assert torch.equal(q[-40:], want) and torch.equal(scale[-40:], s)
+    del x
+    wq, ws = ops.quantize_rows(_randn(g, 24, 32768))
+    check(ops.int8_linear(q, scale, wq, ws)[-40:], *R.int8_linear(q[-40:], scale[-40:], wq, ws, None, BF16), "reading far rows")
+    q, s, w, ws, bias = _int8_case(70_000, 24, 32768, BF16)
+    check(ops.int8_linear(q, s, w, ws, bias)[-40:], *R.int8_linear(q[-40:], s[-40:], w, ws, bias, BF16), "writing far rows")
 
 
 def test_a_gradients_gradient_is_refused():
