@@ -108,7 +108,7 @@ __device__ __forceinline__ void add(const float* per_feature, int half, f32x16 (
 
 // ------------------------------------------------------------------ forward
 template <class X, int ACT>
-__global__ __launch_bounds__(X::THREADS, 2) void k_feed_gate(FeedDev d, GemmJob job) {
+__global__ __launch_bounds__(X::THREADS, X::WAVES) void k_feed_gate(FeedDev d, GemmJob job) {
     typedef typename X::T T;
     __shared__ __align__(16) char lds[X::BYTES];
     f32x16 acc[X::NM][X::NX];
@@ -160,7 +160,7 @@ struct PlainDev {
 };
 
 template <class X>
-__global__ __launch_bounds__(X::THREADS, 2) void k_feed_plain(PlainDev d, GemmJob job) {
+__global__ __launch_bounds__(X::THREADS, X::WAVES) void k_feed_plain(PlainDev d, GemmJob job) {
     typedef typename X::T T;
     __shared__ __align__(16) char lds[X::BYTES];
     f32x16 acc[X::NM][X::NX];
@@ -325,7 +325,7 @@ __global__ __launch_bounds__(1024) void k_feed_few_down(FeedDev d) {
 // ------------------------------------------------------------------ backward
 // dh = dy D, then dz = dh u act'(g) and du = dh act(g) of the saved projections.
 template <class X, int ACT>
-__global__ __launch_bounds__(X::THREADS, 2) void k_feed_grad(FeedDev d, GemmJob job) {
+__global__ __launch_bounds__(X::THREADS, X::WAVES) void k_feed_grad(FeedDev d, GemmJob job) {
     typedef typename X::T T;
     typedef T t4 __attribute__((ext_vector_type(4)));
     __shared__ __align__(16) char lds[X::BYTES];
@@ -399,7 +399,7 @@ struct WeightsDev {
 __device__ __host__ __forceinline__ int padded(int n) { return (n + 7) / 8 * 8; }
 
 template <class X>
-__global__ __launch_bounds__(X::THREADS, 2) void k_feed_weights(WeightsDev d) {
+__global__ __launch_bounds__(X::THREADS, X::WAVES) void k_feed_weights(WeightsDev d) {
     typedef typename X::T T;
     __shared__ __align__(16) char lds[X::BYTES];
     f32x16 acc[X::NM][X::NX];
@@ -499,8 +499,8 @@ int64_t up_to(int64_t n, int64_t d) { return (n + d - 1) / d; }
         if (e_ != hipSuccess) return e_;    \
     } while (0)
 
-// What a product's partial sums cost to write, read and join, in us.
-float join_time(int splits, int64_t values) { return splits < 2 ? 0.0f : 4.0f + (float)values * (float)(8 * splits + 2) / 4.0e6f; }
+// What a product's partial sums cost to write, read and join, in us (two of 1999x1100: 7.5).
+float join_time(int splits, int64_t values) { return splits < 2 ? 0.0f : 3.0f + (float)values * (float)(8 * splits + 2) / 9.0e6f; }
 
 // The tiles that are expected to take the least time for jobs of features x rows, in `splits` ranges of the reduction each.
 struct Choice {
@@ -510,7 +510,8 @@ struct Choice {
 Choice choose(int cols, bool gated, int jobs, const int* features, const int* rows, int parts, int splits, const float* more = nullptr) {
     Choice best{kSmall, 0.0f};
     for (int k = 0; k < kTileKinds; ++k) {
-        // Gated: half of a tile's features are the output's; the smallest has 64 x 128 places.
+        // Gated: half of a tile's features are the output's; the smallest has 64 x 128 places, and eight waves need 64 features each.
+        if (gated && k == kTall) continue;
         const int f = kTileCost[k].f / (gated ? 2 : 1), r = gated && k == kSmall ? 128 : kTileCost[k].r;
         int64_t tiles = 0;
         for (int n = 0; n < jobs; ++n) tiles += up_to(features[n], f) * up_to(rows[n], r);
@@ -576,7 +577,7 @@ template <class T, int ACT>
 hipError_t grad(const FeedDev& d, GemmJob job, hipStream_t st) {
     // The gate's derivative takes a wave longer than anything else that follows the products, and two blocks on a CU hide
     // it behind each other's: 8192x1024x4096 165 us in tiles of 256 x 256, 131 of 128 x 192, 140 of 128 x 128.
-    constexpr float kMore[kTileKinds] = {46.0f, 18.0f, 12.0f, 4.0f};
+    constexpr float kMore[kTileKinds] = {46.0f, 24.0f, 18.0f, 12.0f, 12.0f, 4.0f};
     return with_tile<T, true, false, false, false>(choose(1, false, 1, &job.features, &job.rows, parts_of(job.len), 1, kMore).kind, [&](auto x) {
         typedef decltype(x) X;
         tiled<X>(job);

@@ -123,7 +123,7 @@ __device__ __forceinline__ float scaled(const Int8Dev& d, int v, float xs, int f
 }
 
 template <class X, class T>
-__global__ __launch_bounds__(X::THREADS, 2) void k_int8_tile(Int8Dev d, GemmJob job) {
+__global__ __launch_bounds__(X::THREADS, X::WAVES) void k_int8_tile(Int8Dev d, GemmJob job) {
     __shared__ __align__(16) char lds[X::BYTES];
     i32x16 acc[X::NM][X::NX];
     float none[X::NX];

@@ -161,6 +161,7 @@ struct Tile {
     static constexpr int PART = FCOL || RCOL ? 64 : 128 / (int)sizeof(T);
     static_assert(!(FCOL || RCOL) || sizeof(T) == 2);
     static constexpr int BYTES = STAGES * (TF + TR) * 128;
+    static constexpr int WAVES = THREADS == 256 && BYTES > 81920 ? 1 : 2;      // of a SIMD: one block of 8 waves or two of 4, if LDS holds two
     typedef Loads<T, TF, THREADS, FCOL, UNIT, FCOL || RCOL> LF;
     typedef Loads<T, TR, THREADS, RCOL, 0, FCOL || RCOL> LR;
 
@@ -360,21 +361,25 @@ __device__ __forceinline__ void tile_of(const GemmJob& job, int id, int& f, int&
 // ------------------------------------------------------------------ which tiles (host)
 constexpr int kCUs = 256;
 
-enum { kBig, kWide, kMid, kSmall, kTileKinds };
+enum { kBig, kTall, kWide, kMid, kDeep, kSmall, kTileKinds };
 
-// What a launch of tiles is expected to take, in us: rounds of as many tiles as the CUs hold at once (one of 256 x 256,
-// two of the others a CU), each so much a part of the reduction and so much besides. Measured in bf16 with one and with two tiles
-// on every CU, for two kRow operands, one and no kRow operand. What the rule costs where it is wrong is little: the
-// tiles next to each other in it are. 8192x1024x4096 in us with 256 x 256, 128 x 192 and 128 x 128 tiles: 87, 77, 66;
-// 8192x4096x1024 72, 76, 81; 32768x2048x8192 869, 991, 1050; 9216x1024x8192 without a kRow operand 180, 166, 222.
+// What a launch of tiles is expected to take, in us: rounds of as many tiles as the CUs hold at once, each so much a part of
+// the reduction and so much besides. Measured in bf16 with one and with two tiles on every CU, for two kRow operands, one
+// and no kRow operand. Two blocks on a CU hide each other's waits; a CU's only block has LDS for a third stage, which hides
+// the loads'. us with 256 x 256, 256 x 128, 128 x 192, 128 x 128 (two stages), the same (three) and 64 x 64 tiles:
+//   8192x1024x4096         91   64   78   67   76  112        2000x1104x2736          64   39   45   37   27   36
+//   8192x4096x1024         71   77   75   78   88  120        32768x2048x8192        886  966 1025 1093 1168 1763
+//   8192x1024x8192, F kCol 148  127  151  135  146  238       9216x1024x8192, kCol    162  223  164  223  222  283
 struct TileCost {
     int f, r, at_once;
     float one[3], all[3], besides;
 };
 constexpr TileCost kTileCost[kTileKinds] = {
     {256, 256, 1, {1.75f, 1.75f, 1.75f}, {1.75f, 1.75f, 1.75f}, 8.0f},
+    {256, 128, 1, {0.84f, 0.90f, 0.94f}, {0.84f, 0.90f, 0.94f}, 9.0f},
     {128, 192, 2, {0.75f, 0.84f, 0.90f}, {1.42f, 1.42f, 1.45f}, 8.0f},
     {128, 128, 2, {0.63f, 0.70f, 0.75f}, {0.97f, 1.02f, 1.05f}, 7.0f},
+    {128, 128, 1, {0.48f, 0.51f, 0.59f}, {0.48f, 0.51f, 0.59f}, 7.5f},
     {64, 64, 2, {0.28f, 0.34f, 0.35f}, {0.39f, 0.44f, 0.49f}, 4.0f},
 };
 
@@ -391,8 +396,12 @@ inline float tile_time(int kind, int cols, int64_t tiles, float parts, float mor
 template <class T, bool FCOL, bool RCOL, bool GATED, bool SUMS, class F>
 auto with_tile(int kind, F f) {
     if (kind == kBig) return f(Tile<T, 2, 4, 4, 2, 2, FCOL, RCOL, GATED, SUMS>{});
+    if constexpr (!GATED) {
+        if (kind == kTall) return f(Tile<T, 4, 2, 2, 2, 3, FCOL, RCOL, GATED, SUMS>{});
+    }
     if (kind == kWide) return f(Tile<T, 2, 2, 2, 3, 2, FCOL, RCOL, GATED, SUMS>{});
     if (kind == kMid) return f(Tile<T, 2, 2, 2, 2, 2, FCOL, RCOL, GATED, SUMS>{});
+    if (kind == kDeep) return f(Tile<T, 2, 2, 2, 2, 3, FCOL, RCOL, GATED, SUMS>{});
     if constexpr (GATED) return f(Tile<T, 1, 4, 2, 1, 3, FCOL, RCOL, GATED, SUMS>{});
     else return f(Tile<T, 2, 2, 1, 1, 4, FCOL, RCOL, GATED, SUMS>{});
 }
