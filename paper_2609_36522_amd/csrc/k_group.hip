@@ -17,16 +17,24 @@
 #include <type_traits>
 
 #include "pa_act.h"
-#include "pa_ops_device.h"
+#include "pa_mma.h"
 
 namespace pa {
 
 namespace {
 
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
 constexpr int kBlock = 512, kWaves = kBlock / 64;
 constexpr int kMaxGroups = 512;          // groups of a slab
 constexpr int kMaxSlab = kBlock * 8;     // channels of a slab
 constexpr int kBatch = 4;                // pixels that a thread takes at a time
+constexpr int kHeld = 8;                 // pixels that it holds in the one-launch kernels,
+constexpr int kHeldBatch = 7;            // or 2 or 6 (fp32: 3) batches of this
+template <class T> constexpr int kHeldMost = sizeof(T) == 2 ? 42 : 21;      // 168 of a thread's 256 registers: one block a CU
+// Blocks of r pixels a thread, r > kHeld, that share a CU.
+template <class T>
+__device__ __host__ constexpr int held_blocks(int r) { return sizeof(T) == 2 && r <= 2 * kHeldBatch ? 2 : 1; }
 
 // a / b of whole numbers below 2^20 by b's reciprocal in fp32: (a + 1/2) / b is at least 1 / (2 b) from a whole number,
 // relative to itself 2^-21, and the product's two roundings are 2^-23.
@@ -88,6 +96,13 @@ template <class T, int WIDTH>
 __device__ __forceinline__ Pack8<T> mend(const Pack8<T>& r, const Place& q) {
     if constexpr (WIDTH == kRagged) return fix8(r, q.c, q.n);
     return r;
+}
+
+// Stores a piece at channel c of a row.
+template <class T, int WIDTH>
+__device__ __forceinline__ void put(T* row, const Pack8<T>& v, const Place& q) {
+    if constexpr (WIDTH == kWhole) *reinterpret_cast<Pack8<T>*>(row + q.c) = v;
+    else store8(row + q.c, v, q.n - q.c);
 }
 
 // R pixels of the thread from `p` on, `lanes` apart; beyond the chunk's last one, which stands in for them, nothing is
@@ -263,21 +278,51 @@ __device__ __forceinline__ Pack8<T> normalized(const Pack8<T>& x, const float (&
     return o;
 }
 
-// A slab's pixels in one block's registers, R a thread: statistics and result in one launch.
+// The same bits, as far as the compiler knows others: a pixel's 16-bit values stay so between two uses instead of as 32-bit
+// numbers, in twice the registers.
+template <class T>
+__device__ __forceinline__ void keep_packed(Pack8<T>& p) {
+    if constexpr (sizeof(T) == 2) {
+        i32x4 v = __builtin_bit_cast(i32x4, p);
+        asm volatile("" : "+v"(v));
+        p = __builtin_bit_cast(Pack8<T>, v);
+    }
+}
+
+// A slab's pixels in one block's registers, up to R a thread: statistics and result in one launch, x read once. The slabs of
+// a sample are neighbours on an XCD, so that the lines that two of them share are fetched once. Bound by its phases, one
+// after the other where a CU has one block: the loads, then vector instructions (20 a value, silu's included: 27 us) that only
+// the stores overlap. 32x4096x320 in bf16: 45 us, 3.7 TB/s; in two launches 23 + 29.
 template <class T, int WIDTH, int R>
-__global__ __launch_bounds__(kBlock) void k_group_whole(GroupDev d) {
+__global__ __launch_bounds__(kBlock, (R <= kHeld ? 4 : held_blocks<T>(R) * 2)) void k_group_whole(GroupDev d) {
     __shared__ float lds[kBlock * 8], group[2][kMaxGroups];
     __shared__ Groups s;
-    const Place q(d, 0, d.pixels, blockIdx.x, blockIdx.y);
-    Pack8<T> x[R];
-    fetch_pixels<T, WIDTH>(d.x, d.xs, q, q.lane, x);
+    constexpr int N = R % kHeldBatch == 0 ? kHeldBatch : R;          // in batches, of which those that no thread has are left out
+    const int id = xcd_order(blockIdx.x, gridDim.x), sample = id / d.slabs;
+    const Place q(d, 0, d.pixels, id - sample * d.slabs, sample);
+    const int every = divided(d.pixels, 1.0f / (float)q.lanes), any = every + (every * q.lanes < d.pixels);      // a thread's pixels: at least, at most
+    Pack8<T> x[R / N][N];
+#pragma unroll
+    for (int k = 0; k < R / N; ++k) {
+        if (k * N < any) fetch_pixels<T, WIDTH>(d.x, d.xs, q, q.lane + k * N * q.lanes, x[k]);
+        __builtin_amdgcn_sched_barrier(0);               // (addresses and numbers of one batch in registers at a time, here and below)
+    }
     float a[8], b[8], mean[8];
     const Raw rw = load_parameters<WIDTH>(d, d.w, q), rb = load_parameters<WIDTH>(d, d.b, q);
-#pragma unroll
-    for (int k = 0; k < R; ++k) x[k] = mend<T, WIDTH>(x[k], q);
     const int count = pixels_left(q, q.lane);
     Running r;
-    r.add(x, count);
+#pragma unroll
+    for (int k = 0; k < R / N; ++k) {
+        if (k * N >= any) continue;
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[k][i] = mend<T, WIDTH>(x[k][i], q);
+        if ((k + 1) * N <= every) r.add(x[k], N);
+        else r.add(x[k], count - k * N);
+#pragma unroll
+        for (int i = 0; i < N; ++i) keep_packed(x[k][i]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    if (!q.own) r = Running();
     statistics(d, q, r, lds, s);
     const float n = (float)d.pixels * (float)d.width;
     for (int g = threadIdx.x; g < q.groups; g += kBlock) {
@@ -295,9 +340,15 @@ __global__ __launch_bounds__(kBlock) void k_group_whole(GroupDev d) {
         mean[i] = group[0][g];
         a[i] *= group[1][g];
     });
+    if (!q.own) return;
+    T* row = row_at<T>(d.y, d.ys, q, q.lane);
+    const int64_t step = q.lanes * d.ys[1];
 #pragma unroll
-    for (int k = 0; k < R; ++k)
-        if (k < count) store8(row_at<T>(d.y, d.ys, q, q.lane + k * q.lanes) + q.c, normalized(x[k], mean, a, b, d.act), q.n - q.c);
+    for (int k = 0; k < R; ++k) {
+        if (k < every || k < count) put<T, WIDTH>(row, normalized(x[k / N][k % N], mean, a, b, d.act), q);
+        row += step;
+        if (k % 2) __builtin_amdgcn_sched_barrier(0);
+    }
 }
 
 // Statistics of a chunk. The next batch is on its way while one is worked on.
@@ -381,7 +432,7 @@ __global__ __launch_bounds__(kBlock, 4) void k_group_apply(GroupDev d) {
         if (left > kBatch) fetch_pixels<T, WIDTH>(d.x, d.xs, q, p + kBatch * q.lanes, next);
 #pragma unroll
         for (int k = 0; k < kBatch; ++k)
-            if (k < left) store8(row_at<T>(d.y, d.ys, q, p + k * q.lanes) + q.c, normalized(x[k], mean, a, b, d.act), q.n - q.c);
+            if (k < left) put<T, WIDTH>(row_at<T>(d.y, d.ys, q, p + k * q.lanes), normalized(x[k], mean, a, b, d.act), q);
         p += kBatch * q.lanes;
         left -= kBatch;
     }
@@ -620,7 +671,7 @@ __global__ __launch_bounds__(kBlock, 4) void k_group_dx(GroupDev d, unsigned blo
         }
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            if (k < left) store8(row_at<T>(d.dx, d.dxs, q, p + k * q.lanes) + q.c, gradient(ch, x[k], y[k], m1, m2, d.act), q.n - q.c);
+            if (k < left) put<T, WIDTH>(row_at<T>(d.dx, d.dxs, q, p + k * q.lanes), gradient(ch, x[k], y[k], m1, m2, d.act), q);
             __builtin_amdgcn_sched_barrier(0);           // one pixel's numbers in registers at a time
         }
         p += R * q.lanes;
@@ -668,7 +719,7 @@ __global__ __launch_bounds__(kBlock) void k_group_bwd_whole(GroupDev d) {
         });
 #pragma unroll
         for (int k = 0; k < R; ++k)
-            if (k < count) store8(row_at<T>(d.dx, d.dxs, q, q.lane + k * q.lanes) + q.c, gradient(ch, x[k], y[k], m1, m2, d.act), q.n - q.c);
+            if (k < count) put<T, WIDTH>(row_at<T>(d.dx, d.dxs, q, q.lane + k * q.lanes), gradient(ch, x[k], y[k], m1, m2, d.act), q);
     }
     if (d.dw || d.db) channel_sums(q, sw, sb, lds, d.sums + (int64_t)q.b * 2 * d.channels + q.c0, d.channels);
 }
@@ -676,8 +727,6 @@ __global__ __launch_bounds__(kBlock) void k_group_bwd_whole(GroupDev d) {
 // ------------------------------------------------------------------ launches
 int64_t parts_of(int64_t n, int64_t size) { return (n + size - 1) / size; }
 
-// Pixels of a thread that the one-launch kernels hold.
-constexpr int kHeld = 8;
 
 template <class F>
 hipError_t dispatch(int dtype, const GroupDev& d, F f) {
@@ -691,20 +740,19 @@ hipError_t dispatch(int dtype, const GroupDev& d, F f) {
     return dtype == PA_BF16 ? width((__bf16)0) : width((_Float16)0);
 }
 
-// f with the number of a thread's pixels that a slab of one block takes, rounded up to 2 or 8.
-template <class F>
-void held(const GroupDev& d, F f) {
-    const int lanes = kBlock / ((d.slab + 7) / 8);
-    if (d.pixels <= 2 * lanes) f(std::integral_constant<int, 2>{});
-    else f(std::integral_constant<int, kHeld>{});
-}
+// A thread's pixels of a slab of one block.
+int64_t held(const GroupDev& d) { return parts_of(d.pixels, kBlock / ((d.slab + 7) / 8)); }
 
 }  // namespace
 
 // Slabs of whole groups and of whole pieces of 8 channels. The smallest such slab (with at least 32 channels, so that a
-// pixel's piece of it is no smaller than a cache line's sector) if a block's registers hold its pixels, and if the
-// tensor is small enough to be bound by latency or there are slabs for every CU; otherwise as many groups
-// as a block can take, in chunks of pixels.
+// pixel's piece of it is no smaller than a cache line's sector) if a block's registers hold its pixels in one launch; else as
+// many groups as a block can take, in chunks of pixels.
+//
+// One launch or two, us of a bf16 call: 1024 pixels of 640 channels (11 a thread), 16 to 1280 slabs: 15 and 20 (16), 19 and 24
+// (256), 28 and 33 (512), 54 and 54 (1024), 65 and 81 (1280). 4096 pixels of 320 channels (41 a thread, one block a CU): 43
+// and 35 (128 slabs), 44 and 48 (160), 49 and 56 (256), 82 and 76 (288), 86 and 95 (352), 106 and 111 (512): a block a CU
+// pays where two thirds of the CUs and more have one. The backward pass holds x and dy: up to 8 pixels of both.
 void group_plan(GroupDev& d, int dtype, bool backward) {
     d.width = d.channels / d.groups;
     d.per_width = 1.0f / (float)d.width;
@@ -719,9 +767,14 @@ void group_plan(GroupDev& d, int dtype, bool backward) {
     };
     const int small = (32 + d.width * unit - 1) / (d.width * unit) * unit;
     slab(small);
-    const int64_t fits = (int64_t)(kBlock / ((d.slab + 7) / 8)) * kHeld;
-    const int64_t bytes = (int64_t)d.batch * d.pixels * d.channels * (dtype == PA_F32 ? 4 : 2);
-    if (d.pixels <= fits && (bytes <= (4 << 20) || (int64_t)d.batch * d.slabs >= 256)) {
+    const int64_t n = held(d), blocks = (int64_t)d.batch * d.slabs;
+    bool whole = n <= kHeld;
+    if (backward) {
+        whole = whole && (blocks >= 256 || (int64_t)d.batch * d.pixels * d.channels * (dtype == PA_F32 ? 4 : 2) <= 4 << 20);
+    } else if (!whole && d.slab % 8 == 0 && d.channels % 8 == 0 && n <= (dtype == PA_F32 ? kHeldMost<float> : kHeldMost<__bf16>)) {
+        whole = n <= 2 * kHeldBatch || 3 * blocks >= 2 * 256 * parts_of(blocks, 256);
+    }
+    if (whole && blocks < (1 << 23)) {
         d.chunk = d.pixels > 0 ? d.pixels : 1;
         d.chunks = 1;
         d.whole = 1;
@@ -729,7 +782,8 @@ void group_plan(GroupDev& d, int dtype, bool backward) {
     }
     slab(d.groups);
     // 512 blocks, two for each CU, as its registers allow, but chunks of two pixels a thread at least (four where
-    // they come in batches of four: 4x1024x640 statistics 10.6 and 8.2 us), and at most 256 of them a sample. us with 512, 768, 1024 and 2048 blocks, 32x4096x320: statistics 23, 24, 25, 35, results 33, 33, 34,
+    // they come in batches of four: 4x1024x640 statistics 10.6 and 8.2 us), and at most 256 of them a sample. us with 512,
+    // 768, 1024 and 2048 blocks, 32x4096x320: statistics 23, 24, 25, 35, results 33, 33, 34,
     // 38; 8x4096x640: sums of the backward pass 21, 22, 22, dx 34, 39, 37, 41.
     const int lanes = kBlock / ((d.slab + 7) / 8);
     const int64_t per = (int64_t)d.batch * d.slabs, want = (512 + per - 1) / (per > 0 ? per : 1);
@@ -749,9 +803,14 @@ hipError_t group_forward(const GroupDev& d, int dtype, hipStream_t st) {
         typedef decltype(t) T;
         constexpr int WIDTH = decltype(wd)::value;
         if (d.whole) {
-            held(d, [&](auto r) {
-                k_group_whole<T, WIDTH, decltype(r)::value><<<dim3((unsigned)d.slabs, (unsigned)d.batch), kBlock, 0, st>>>(d);
-            });
+            const unsigned blocks = (unsigned)((int64_t)d.slabs * d.batch);
+            const int64_t n = held(d);
+            if (n <= 2) k_group_whole<T, WIDTH, 2><<<blocks, kBlock, 0, st>>>(d);
+            else if (n <= kHeld) k_group_whole<T, WIDTH, kHeld><<<blocks, kBlock, 0, st>>>(d);
+            else if constexpr (WIDTH == kWhole) {
+                if (n <= 2 * kHeldBatch) k_group_whole<T, WIDTH, 2 * kHeldBatch><<<blocks, kBlock, 0, st>>>(d);
+                else k_group_whole<T, WIDTH, kHeldMost<T>><<<blocks, kBlock, 0, st>>>(d);
+            }
             return hipGetLastError();
         }
         dim3 grid((unsigned)d.chunks, (unsigned)d.slabs, (unsigned)d.batch);
@@ -782,9 +841,9 @@ hipError_t group_backward(const GroupDev& d, int dtype, hipStream_t st) {
             return hipGetLastError();
         }
         if (any) {
-            held(d, [&](auto r) {
-                k_group_bwd_whole<T, WIDTH, decltype(r)::value><<<dim3((unsigned)d.slabs, (unsigned)d.batch), kBlock, 0, st>>>(d);
-            });
+            const dim3 grid((unsigned)d.slabs, (unsigned)d.batch);
+            if (held(d) <= 2) k_group_bwd_whole<T, WIDTH, 2><<<grid, kBlock, 0, st>>>(d);
+            else k_group_bwd_whole<T, WIDTH, kHeld><<<grid, kBlock, 0, st>>>(d);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
         }

@@ -111,6 +111,27 @@ def test_group_norm_not_a_number_stays_in_its_group(P):
     assert torch.equal(torch.isnan(dw), want[1, 0])
 
 
+# Slabs enough for a block on most CUs, pixels about what a block's registers hold (8, 14, 21 in fp32 and 42 for each of 128
+# threads, 102 of them for 80 channels in slabs of 40), and about two blocks a CU.
+@pytest.mark.parametrize("dt", [F32, BF16, F16], ids=["f32", "bf16", "f16"])
+@pytest.mark.parametrize("Bn,P,C,G", [
+    (3, 1024, 96, 3), (3, 1025, 96, 3), (2, 1792, 64, 4), (180, 1793, 32, 4), (180, 2100, 32, 1), (180, 2689, 32, 8), (172, 5376, 32, 4),
+    (172, 5377, 32, 4), (90, 4000, 80, 8), (170, 4284, 40, 4), (350, 2500, 32, 2)])
+def test_group_norm_of_many_slabs(Bn, P, C, G, dt):
+    x, w, b, dy = _group_case(Bn, P, C, dt)
+    _check_group(x, G, w, b, dy, "silu")
+    y, mean, rstd = ops.group_norm_forward(x, G, w, b, activation="silu")
+    bad = x.clone()
+    bad[1, P - 1, C // 2] = math.inf
+    z, _, r = ops.group_norm_forward(bad, G, w, b, activation="silu")
+    width = C // G
+    at = C // 2 // width
+    z[1, :, at * width:(at + 1) * width] = y[1, :, at * width:(at + 1) * width]      # the group that has no mean
+    r[1, at] = rstd[1, at]
+    assert torch.equal(z, y) and torch.equal(r, rstd)
+    assert torch.equal(ops.group_norm_forward(x.transpose(0, 1).contiguous().transpose(0, 1), G, w, b, activation="silu")[0], y)
+
+
 def test_group_norm_constant_groups_and_nothing():
     x = torch.full((2, 30, 24), 2.5, device="cuda")
     y, mean, rstd = ops.group_norm_forward(x, 3)
@@ -123,19 +144,19 @@ def test_group_norm_constant_groups_and_nothing():
         assert dx.shape == shape and dw.shape == (24,) and not dw.any() and not db.any()
 
 
-@pytest.mark.parametrize("P", [60, 3000])
-def test_group_norm_in_place(P):
+@pytest.mark.parametrize("Bn,P", [(2, 60), (2, 1500), (2, 3000), (64, 3000)])
+def test_group_norm_in_place(Bn, P):
     """y may be x and dx may be dy (C ABI); gradients one at a time give the same."""
     import ctypes as C
-    x, w, b, dy = _group_case(2, P, 96, BF16)
+    x, w, b, dy = _group_case(Bn, P, 96, BF16)
     y, mean, rstd = ops.group_norm_forward(x, 4, w, b, activation="gelu")
     want = ops.group_norm_backward(dy, x, mean, rstd, w, b, activation="gelu")
     lib, st = ops._library(), torch.cuda.current_stream().cuda_stream
     s = (P * 96, 96)
-    p = ops.GroupNorm(2, P, 96, 4, ops.PA_BF16, ops.PA_BF16, ops.PA_ACT_GELU, 0, 1e-5, s, s, s)
+    p = ops.GroupNorm(Bn, P, 96, 4, ops.PA_BF16, ops.PA_BF16, ops.PA_ACT_GELU, 0, 1e-5, s, s, s)
     n = C.c_size_t(0)
     B._check(lib.paraanya_group_norm_backward_workspace(C.byref(p), C.byref(n)))
-    ws = torch.empty(n.value + (1 << 20), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(n.value + (1 << 22), dtype=torch.uint8, device="cuda")
     x2, d2 = x.clone(), dy.clone()
     B._check(lib.paraanya_group_norm(C.byref(p), x2.data_ptr(), w.data_ptr(), b.data_ptr(), x2.data_ptr(), None, None, ws.data_ptr(),
                                      ws.numel(), st))
