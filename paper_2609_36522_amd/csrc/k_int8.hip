@@ -123,8 +123,8 @@ __device__ __forceinline__ float scaled(const Int8Dev& d, int v, float xs, int f
     return r;
 }
 
-// Bound by the matrix units (busy 45% of the time; the clock is the 16-bit products') and the LDS reads that feed them:
-// 32768x2048x8192 560 to 580 us, 1.9 to 2.0 P operations/s.
+// Bound by the matrix units (busy 54% of the time) and, where a tile's reduction is as short as 16 parts, by the results that
+// follow it: 32768x2048x8192 560 to 580 us, 1.9 to 2.0 P operations/s.
 template <class X, class T>
 __global__ __launch_bounds__(X::THREADS, X::WAVES) void k_int8_tile(Int8Dev d, GemmJob job) {
     __shared__ __align__(16) char lds[X::BYTES];
