@@ -6,7 +6,9 @@ Argument marshalling only, as in :mod:`binding`: every product and sum runs in t
 kernels. Tensors lie on the current device; kernels run on torch's current stream, outputs and
 workspaces come from torch's allocator on that stream. :func:`layer_norm`, :func:`cross_attention`,
 :func:`group_norm` and :func:`feed_forward` take part in autograd, for first derivatives (a gradient's
-gradient is refused); the ``*_forward`` and ``*_backward`` functions do not.
+gradient is refused); the ``*_forward`` and ``*_backward`` functions do not. All may be captured into a graph; while a
+backward pass is captured, no graph of autograd that was built outside may hold the same leaves (torch would accumulate their
+gradients on that graph's stream).
 """
 from __future__ import annotations
 

@@ -493,6 +493,32 @@ def test_captured_calls_replay_on_new_inputs():
             assert all(torch.equal(a, b) for a, b in zip(got, want)), (name, k)
 
 
+def test_captured_training_steps_replay_on_new_inputs():
+    """Forward and backward through autograd in one graph (of leaves that no eager graph holds), replayed among eager steps."""
+    x, w, b, dy = _group_case(2, 700, 96, BF16)
+    _, gate, up, down, biases, _ = _feed_case(1, 96, 200, 96, BF16)
+
+    def step(x, dy):
+        leaves = [t.detach().requires_grad_() for t in (x, w, b, gate, up, down, *biases)]
+        y = ops.feed_forward(ops.group_norm(leaves[0], 4, *leaves[1:3], activation="silu"), *leaves[3:])
+        return (y.detach(), *torch.autograd.grad(y, leaves, dy))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(x, dy)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(x, dy)
+    for k in range(3):
+        x.copy_(x.roll(1, 1)), dy.copy_(dy.roll(k, 1))
+        graph.replay()
+        want = step(x, dy)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), k
+
+
 # ------------------------------------------------------------------ more than 2^31 elements or bytes
 def test_group_norm_offsets_beyond_31_bits():
     g = _gen(1)
