@@ -2,8 +2,8 @@
 // y = h D^T + bd.
 //
 // Forward, two launches. A block of the first takes as many features of G as of U, so that a wave has both
-// projections of a value in the same lane, and stores h (and, for the backward pass, the projections).
-// Backward: dh = dy D with the gate's derivative in its epilogue (dz by the gate's projection, du by the other's);
+// projections of a value in the same lane, and stores h (and, for the backward pass, by what dh gives the gradients by the
+// projections). Backward: dh = dy D with these factors in its epilogue (dz by the gate's projection, du by the other's);
 // dx = dz G + du U as one reduction over both; the weights' gradients dz^T x, du^T x and dy^T h, reductions
 // over the rows, in one launch, which also sums dz, du and dy over the rows (the biases' gradients) from the
 // operands that pass by.
@@ -111,7 +111,7 @@ __device__ __forceinline__ void add(const float* per_feature, int half, f32x16 (
 // Both projections of a tile of rows, which read x once for the two; the activation and the product are formed in the
 // registers that hold them. Bound by the matrix units (the clock falls to 1.64 GHz under them, 77% busy) at long
 // reductions, by what follows the products at short ones: 32768x2048x8192 1720 us (1280 TFLOP/s; the library's product of this
-// size alone 1555), 8192x1024x4096 128 (1070), 145 where the projections are kept for the backward pass.
+// size alone 1555), 8192x1024x4096 128 (1070), 145 to 160 where the factors of the backward pass are formed and kept.
 template <class X, int ACT>
 __global__ __launch_bounds__(X::THREADS, X::WAVES) void k_feed_gate(FeedDev d, GemmJob job) {
     typedef typename X::T T;
@@ -142,14 +142,32 @@ __global__ __launch_bounds__(X::THREADS, X::WAVES) void k_feed_gate(FeedDev d, G
                     store_padded(static_cast<T*>(to) + (int64_t)(r0 + j * 32 + row) * d.hidden_pad + f0 + at, v, d.hidden - f0 - at);
             });
         };
-        if (d.g) {
-            store(d.g, [&](int m, int q) { return gather8<T>(acc[m][j], q, 1.0f); });
-            store(d.u, [&](int m, int q) { return gather8<T>(acc[m + HM][j], q, 1.0f); });
+        if (d.by_z) {
+            Pack8<T> by_z[HM][2];
+#pragma unroll
+            for (int m = 0; m < HM; ++m) {
+                f32x16 v;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float2 a = activate_grad<ACT>(acc[m][j][i]);
+                    v[i] = a.y * acc[m + HM][j][i];
+                    acc[m][j][i] = a.x;
+                }
+#pragma unroll
+                for (int q = 0; q < 2; ++q) by_z[m][q] = gather8<T>(v, q, 1.0f);
+            }
+            store(d.by_z, [&](int m, int q) { return by_z[m][q]; });
+            store(d.by_u, [&](int m, int q) { return gather8<T>(acc[m][j], q, 1.0f); });
+        } else {
+#pragma unroll
+            for (int m = 0; m < HM; ++m)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[m][j][i] = activate<ACT>(acc[m][j][i]);
         }
 #pragma unroll
         for (int m = 0; m < HM; ++m)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[m][j][i] = activate<ACT>(acc[m][j][i]) * acc[m + HM][j][i];
+            for (int i = 0; i < 16; ++i) acc[m][j][i] *= acc[m + HM][j][i];
         store(d.h, [&](int m, int q) { return gather8<T>(acc[m][j], q, 1.0f); });
     }
 }
@@ -309,10 +327,11 @@ __global__ __launch_bounds__(1024) void k_feed_few_gate(FeedDev d) {
     const float g = v[0][0] + (in && d.gate_bias ? (float)static_cast<const T*>(d.gate_bias)[o] : 0.0f);
     const float u = v[1][0] + (in && d.up_bias ? (float)static_cast<const T*>(d.up_bias)[o] : 0.0f);
     const int64_t to = (int64_t)row * d.hidden_pad + o;
-    static_cast<T*>(d.h)[to] = (T)(in ? activate<ACT>(g) * u : 0.0f);
-    if (d.g) {
-        static_cast<T*>(d.g)[to] = (T)(in ? g : 0.0f);
-        static_cast<T*>(d.u)[to] = (T)(in ? u : 0.0f);
+    const float2 a = activate_grad<ACT>(g);
+    static_cast<T*>(d.h)[to] = (T)(in ? a.x * u : 0.0f);
+    if (d.by_z) {
+        static_cast<T*>(d.by_z)[to] = (T)(in ? a.y * u : 0.0f);
+        static_cast<T*>(d.by_u)[to] = (T)(in ? a.x : 0.0f);
     }
 }
 
@@ -331,10 +350,11 @@ __global__ __launch_bounds__(1024) void k_feed_few_down(FeedDev d) {
 }
 
 // ------------------------------------------------------------------ backward
-// dh = dy D, then dz = dh u act'(g) and du = dh act(g) of the saved projections. Bound by what follows the products, which
-// reads and writes as much as it: 8192x1024x4096 130 us, of which the product alone is 73 and 268 MB at the copy rate are 55.
-// (The projections' loads before the products and ahead of each chunk: the same.)
-template <class X, int ACT>
+// dh = dy D, then dz = dh (u act'(g)) and du = dh act(g) by the factors that the forward pass kept. (With g and u kept in their
+// place, each rounded, dx and the weights' gradients are off by 1.8 to 2 times the rounding of a result, so by 1.7; and their
+// activation here took 131 us for 103.) Bound by what follows the products, which reads and writes as much as it:
+// 8192x1024x4096 103 to 108 us, of which the product alone is 73 and 268 MB at the copy rate are 55.
+template <class X>
 __global__ __launch_bounds__(X::THREADS, X::WAVES) void k_feed_grad(FeedDev d, GemmJob job) {
     typedef typename X::T T;
     typedef T t4 __attribute__((ext_vector_type(4)));
@@ -354,43 +374,33 @@ __global__ __launch_bounds__(X::THREADS, X::WAVES) void k_feed_grad(FeedDev d, G
     for (int j = 0; j < X::NX; ++j) {
 #pragma unroll
         for (int c = 0; c < X::NM; c += CM) {
-            // Both projections, in the order in which they lie, then through LDS to the lanes that hold their places.
+            // Both factors, in the order in which they lie, then through LDS to the lanes that hold their places.
             const int fc = f0 + c * 32;
-            uint4 g[P / 2], u[P / 2];
+            uint4 by[2][P / 2];
 #pragma unroll
             for (int i = 0; i < P / 2; ++i) {
                 const int at = i * 64 + lane, row = r0 + j * 32 + at / P, col = fc + at % P * 8;
-                g[i] = u[i] = make_uint4(0, 0, 0, 0);
+                by[0][i] = by[1][i] = make_uint4(0, 0, 0, 0);
                 if (row < d.rows && col < d.hidden_pad) {
-                    g[i] = *reinterpret_cast<const uint4*>(static_cast<const T*>(d.g) + (int64_t)row * d.hidden_pad + col);
-                    u[i] = *reinterpret_cast<const uint4*>(static_cast<const T*>(d.u) + (int64_t)row * d.hidden_pad + col);
+                    by[0][i] = *reinterpret_cast<const uint4*>(static_cast<const T*>(d.by_z) + (int64_t)row * d.hidden_pad + col);
+                    by[1][i] = *reinterpret_cast<const uint4*>(static_cast<const T*>(d.by_u) + (int64_t)row * d.hidden_pad + col);
                 }
             }
-            t4 pg[CM][4];
-            f32x16 du[CM];
-            from_lds<CM>(own, lane, g, pg);
 #pragma unroll
-            for (int m = 0; m < CM; ++m)
+            for (int n = 0; n < 2; ++n) {
+                t4 p[CM][4];
+                from_lds<CM>(own, lane, by[n], p);
+                f32x16 v[CM];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float2 a = activate_grad<ACT>((float)pg[m][i >> 2][i & 3]);
-                    const float dh = acc[c + m][j][i] * scale;
-                    du[m][i] = dh * a.x;
-                    acc[c + m][j][i] = dh * a.y;
-                }
-            from_lds<CM>(own, lane, u, pg);
+                for (int m = 0; m < CM; ++m)
 #pragma unroll
-            for (int m = 0; m < CM; ++m)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) acc[c + m][j][i] *= (float)pg[m][i >> 2][i & 3];
-            auto store = [&](void* to, auto value) {
-                through_lds<T, CM>(own, lane, value, [&](int row, int at, const Pack8<T>& v) {
+                    for (int i = 0; i < 16; ++i) v[m][i] = acc[c + m][j][i] * scale * (float)p[m][i >> 2][i & 3];
+                T* to = static_cast<T*>(n ? d.du : d.dz);
+                through_lds<T, CM>(own, lane, [&](int m, int q) { return gather8<T>(v[m], q, 1.0f); }, [&](int row, int at, const Pack8<T>& o) {
                     if (r0 + j * 32 + row < d.rows && fc + at < d.hidden_pad)
-                        store_padded(static_cast<T*>(to) + (int64_t)(r0 + j * 32 + row) * d.hidden_pad + fc + at, v, d.hidden - fc - at);
+                        store_padded(to + (int64_t)(r0 + j * 32 + row) * d.hidden_pad + fc + at, o, d.hidden - fc - at);
                 });
-            };
-            store(d.dz, [&](int m, int q) { return gather8<T>(acc[c + m][j], q, 1.0f); });
-            store(d.du, [&](int m, int q) { return gather8<T>(du[m], q, 1.0f); });
+            }
         }
     }
 }
@@ -584,15 +594,15 @@ hipError_t plain(PlainDev p, GemmJob job, hipStream_t st) {
     return hipSuccess;
 }
 
-template <class T, int ACT>
+template <class T>
 hipError_t grad(const FeedDev& d, GemmJob job, hipStream_t st) {
-    // The gate's derivative takes a wave longer than anything else that follows the products, and two blocks on a CU hide
-    // it behind each other's: 8192x1024x4096 165 us in tiles of 256 x 256, 131 of 128 x 192, 140 of 128 x 128.
-    constexpr float kMore[kTileKinds] = {46.0f, 24.0f, 18.0f, 12.0f, 12.0f, 4.0f};
+    // What follows the products reads two matrices besides and writes two. 8192x1024x4096: 103 to 108 us in tiles of 256 x 256,
+    // 119 to 128 of 128 x 192.
+    constexpr float kMore[kTileKinds] = {20.0f, 12.0f, 10.0f, 7.0f, 7.0f, 3.0f};
     return with_tile<T, true, false, false, false>(choose(1, false, 1, &job.features, &job.rows, parts_of(job.len), 1, kMore).kind, [&](auto x) {
         typedef decltype(x) X;
         tiled<X>(job);
-        k_feed_grad<X, ACT><<<(unsigned)((int64_t)job.f_tiles * job.r_tiles), X::THREADS, 0, st>>>(d, job);
+        k_feed_grad<X><<<(unsigned)((int64_t)job.f_tiles * job.r_tiles), X::THREADS, 0, st>>>(d, job);
         return hipGetLastError();
     });
 }
@@ -696,7 +706,7 @@ hipError_t zero(void* p, int64_t n, hipStream_t st) {
     return hipGetLastError();
 }
 
-template <class T, int ACT>
+template <class T>
 hipError_t backward(const FeedDev& d, hipStream_t st) {
     if (d.rows == 0) {
         const int64_t HK = (int64_t)d.hidden * d.in, NH = (int64_t)d.out * d.hidden;
@@ -721,7 +731,7 @@ hipError_t backward(const FeedDev& d, hipStream_t st) {
             k_feed_largest<T><<<kLargest, 256, 0, st>>>(d);
             FEED_TRY(hipGetLastError());
         }
-        FEED_TRY((grad<T, ACT>(d, GemmJob{{dn, nullptr}, {dy, nullptr}, ds, ys, d.hidden, d.rows, d.out, 0, 0}, st)));
+        FEED_TRY((grad<T>(d, GemmJob{{dn, nullptr}, {dy, nullptr}, ds, ys, d.hidden, d.rows, d.out, 0, 0}, st)));
     }
     const float* largest = kScaled<T> ? d.largest : nullptr;
     if (d.dx) {
@@ -782,8 +792,8 @@ hipError_t feed_forward(const FeedDev& d, int dtype, int act, hipStream_t st) {
     return dispatch(dtype, act, [&](auto t, auto a) { return forward<decltype(t), decltype(a)::value>(d, st); });
 }
 
-hipError_t feed_backward(const FeedDev& d, int dtype, int act, hipStream_t st) {
-    return dispatch(dtype, act, [&](auto t, auto a) { return backward<decltype(t), decltype(a)::value>(d, st); });
+hipError_t feed_backward(const FeedDev& d, int dtype, hipStream_t st) {
+    return dtype == PA_BF16 ? backward<__bf16>(d, st) : backward<_Float16>(d, st);
 }
 
 }  // namespace pa

@@ -76,7 +76,7 @@ struct FeedDev {
     int64_t x_stride, gate_stride, up_stride, down_stride, y_stride;
     const void *gate_bias, *up_bias, *down_bias;
     void* y;
-    void *g, *u, *h;                 // [rows][hidden_pad] both projections (may be null) and the gated product
+    void *by_z, *by_u, *h;           // [rows][hidden_pad] u act'(g) and act(g), by which dh gives dz and du (may be null), and the gated product
     void *dx, *dgate, *dup, *ddown, *dgate_bias, *dup_bias, *ddown_bias;
     void *dz, *du;                   // backward: [rows][hidden_pad] gradients by the two projections
     void *x_pad, *gate_pad, *up_pad, *down_pad, *dy_pad;   // copies in whole pieces of 16 bytes (null: read in place)
@@ -127,7 +127,7 @@ bool feed_few(int64_t rows);
 // Fills in the splits from the sizes; bytes of `part`.
 size_t feed_plan(FeedDev& d, bool backward);
 hipError_t feed_forward(const FeedDev& d, int dtype, int act, hipStream_t st);
-hipError_t feed_backward(const FeedDev& d, int dtype, int act, hipStream_t st);
+hipError_t feed_backward(const FeedDev& d, int dtype, hipStream_t st);
 
 hipError_t quantize_rows(const QuantizeDev& d, int dtype, hipStream_t st);
 hipError_t int8_linear(const Int8Dev& d, int dtype, hipStream_t st);

@@ -144,8 +144,8 @@ size_t feed_saved(const pa_feed_t* p) { return 3 * round256((size_t)p->rows * pa
 void feed_saved_parts(FeedDev& d, void* saved) {
     Parts w(saved);
     const size_t n = (size_t)d.rows * d.hidden_pad * 2;
-    d.g = w.take(n);
-    d.u = w.take(n);
+    d.by_z = w.take(n);
+    d.by_u = w.take(n);
     d.h = w.take(n);
 }
 
@@ -369,7 +369,7 @@ int paraanya_feed_forward_backward(const pa_feed_t* p, const pa_feed_grad_t* g, 
         d.dgate_bias = g->dgate_bias;
         d.dup_bias = g->dup_bias;
         d.ddown_bias = g->ddown_bias;
-        return launched(feed_backward(d, p->dtype, p->activation, static_cast<hipStream_t>(stream)), "feed forward backward launch");
+        return launched(feed_backward(d, p->dtype, static_cast<hipStream_t>(stream)), "feed forward backward launch");
     });
 }
 

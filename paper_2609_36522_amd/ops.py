@@ -587,7 +587,7 @@ def feed_forward_forward(x, gate, up, down, gate_bias=None, up_bias=None, down_b
 
     x [..., K], gate and up [H, K], down [N, H] (row strides of their own), biases [H], [H], [N], in bf16 or fp16.
     ``activation`` is "silu", "gelu" or None. saved (opaque; None without ``save``) is what the backward pass
-    needs: both projections and the gated product."""
+    needs: the gated product and by what its gradient gives those of the two projections."""
     d, x2, g, u, dn, _, st = _feed_args(x, gate, up, down, (gate_bias, up_bias, down_bias), activation)
     _, ref, keep, plain, with_saved, _ = d
     y = x.new_empty((*x.shape[:-1], down.shape[0]))
