@@ -357,7 +357,7 @@ template <class T, int WIDTH>
 __global__ __launch_bounds__(kBlock, 4) void k_group_stats(GroupDev d) {
     __shared__ float lds[kBlock * 8];
     __shared__ Groups s;
-    const Place q(d, blockIdx.x, d.chunk, blockIdx.y, blockIdx.z);
+    const Place q(d, blockIdx.x, d.chunk, blockIdx.y, d.sample0 + blockIdx.z);
     Running r;
     Pack8<T> x[kBatch], next[kBatch];
     int p = q.p0 + q.lane, left = pixels_left(q, p);
@@ -384,7 +384,7 @@ __global__ __launch_bounds__(kBlock, 4) void k_group_stats(GroupDev d) {
 template <class T, int WIDTH>
 __global__ __launch_bounds__(kBlock, 4) void k_group_apply(GroupDev d) {
     __shared__ float group[2][kMaxGroups];
-    const Place q(d, blockIdx.x, d.spread, blockIdx.y, blockIdx.z);
+    const Place q(d, blockIdx.x, d.spread, blockIdx.y, d.sample0 + blockIdx.z);
     Pack8<T> next[kBatch];
     int p = q.p0 + q.lane, left = pixels_left(q, p);
     fetch_pixels<T, WIDTH>(d.x, d.xs, q, p, next);
@@ -522,7 +522,7 @@ __device__ __forceinline__ void channel_sums(const Place& q, const float (&u)[8]
 template <class T, int WIDTH>
 __global__ __launch_bounds__(kBlock, 4) void k_group_sums(GroupDev d) {
     __shared__ float lds[kBlock * 16];
-    const Place q(d, blockIdx.x, d.chunk, blockIdx.y, blockIdx.z);
+    const Place q(d, blockIdx.x, d.chunk, blockIdx.y, d.sample0 + blockIdx.z);
     constexpr int R = sizeof(T) == 2 ? 2 : 1;
     Pack8<T> nx[R], ny[R];
     int p = q.p0 + q.lane, left = pixels_left(q, p);
@@ -561,7 +561,7 @@ __global__ __launch_bounds__(kBlock, 4) void k_group_sums(GroupDev d) {
 // A sample's group: the channels' sums over the chunks, and from them the means over the group of g and g xh.
 __global__ __launch_bounds__(256) void k_group_join(GroupDev d) {
     __shared__ float sum[2][256], red[2][4];
-    const int g = blockIdx.x, b = blockIdx.y, L = d.width;
+    const int g = blockIdx.x, b = d.sample0 + blockIdx.y, L = d.width;
     // Threads of a channel: the chunks in turn.
     const int turns = L < 256 ? 256 / L : 1, t = (int)threadIdx.x / L, span = L < 256 ? L : 256;
     float m[2] = {};
@@ -637,16 +637,17 @@ __device__ __forceinline__ Pack8<T> gradient(const Channels& ch, const Pack8<T>&
     return o;
 }
 
-// dx of a chunk; the launch's last blocks join the samples' sums (there are `blocks` in front of them). Bound by memory:
+// dx of a chunk (`spreads` of them a sample and slab); the launch's last blocks join the samples' sums (there are `blocks` in
+// front of them). Bound by memory:
 // 8x4096x640 in bf16 27 to 28 us, 126 MB at 4.5 TB/s.
 template <class T, int WIDTH>
-__global__ __launch_bounds__(kBlock, 4) void k_group_dx(GroupDev d, unsigned blocks) {
+__global__ __launch_bounds__(kBlock, 4) void k_group_dx(GroupDev d, unsigned blocks, int spreads) {
     if (blockIdx.x >= blocks) {
         join_samples(d, (int)(blockIdx.x - blocks));
         return;
     }
-    const int spreads = (int)(blocks / (unsigned)(d.slabs * d.batch)), chunk = (int)(blockIdx.x % spreads), rest = (int)(blockIdx.x / spreads);
-    const Place q(d, chunk, d.spread, rest % d.slabs, rest / d.slabs);
+    const int chunk = (int)(blockIdx.x % spreads), rest = (int)(blockIdx.x / spreads);
+    const Place q(d, chunk, d.spread, rest % d.slabs, d.sample0 + rest / d.slabs);
     constexpr int R = sizeof(T) == 2 ? 2 : 1;
     Pack8<T> nx[R], ny[R];
     int p = q.p0 + q.lane, left = pixels_left(q, p);
@@ -729,6 +730,20 @@ __global__ __launch_bounds__(kBlock) void k_group_bwd_whole(GroupDev d) {
 // ------------------------------------------------------------------ launches
 int64_t parts_of(int64_t n, int64_t size) { return (n + size - 1) / size; }
 
+// A launch of so many blocks lasts a millisecond and more: beyond (long batches of many narrow groups) it goes in ranges of the
+// samples, so that no grid comes near 2^32 threads. launch(d, samples) for each range, which begins at d.sample0.
+constexpr int64_t kMaxBlocks = 1 << 20;
+template <class F>
+hipError_t in_ranges(GroupDev d, int64_t blocks_a_sample, F launch) {
+    const int64_t most = blocks_a_sample < kMaxBlocks ? kMaxBlocks / blocks_a_sample : 1;
+    for (int64_t b = 0; b < d.batch; b += most) {
+        d.sample0 = (int)b;
+        launch(d, (unsigned)(d.batch - b < most ? d.batch - b : most));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
 
 template <class F>
 hipError_t dispatch(int dtype, const GroupDev& d, F f) {
@@ -815,13 +830,14 @@ hipError_t group_forward(const GroupDev& d, int dtype, hipStream_t st) {
             }
             return hipGetLastError();
         }
-        dim3 grid((unsigned)d.chunks, (unsigned)d.slabs, (unsigned)d.batch);
-        k_group_stats<T, WIDTH><<<grid, kBlock, 0, st>>>(d);
-        const hipError_t e = hipGetLastError();
+        const unsigned chunks = (unsigned)d.chunks, spreads = (unsigned)parts_of(d.pixels, d.spread), slabs = (unsigned)d.slabs;
+        const hipError_t e = in_ranges(d, (int64_t)chunks * slabs, [&](const GroupDev& c, unsigned n) {
+            k_group_stats<T, WIDTH><<<dim3(chunks, slabs, n), kBlock, 0, st>>>(c);
+        });
         if (e != hipSuccess) return e;
-        grid.x = (unsigned)parts_of(d.pixels, d.spread);
-        k_group_apply<T, WIDTH><<<grid, kBlock, 0, st>>>(d);
-        return hipGetLastError();
+        return in_ranges(d, (int64_t)spreads * slabs, [&](const GroupDev& c, unsigned n) {
+            k_group_apply<T, WIDTH><<<dim3(spreads, slabs, n), kBlock, 0, st>>>(c);
+        });
     });
 }
 
@@ -832,17 +848,23 @@ hipError_t group_backward(const GroupDev& d, int dtype, hipStream_t st) {
         const unsigned params = d.dw || d.db ? (unsigned)((2 * (int64_t)d.channels + kBlock - 1) / kBlock) : 0;
         const bool any = d.batch > 0 && d.pixels > 0;
         if (any && !d.whole) {
-            k_group_sums<T, WIDTH><<<dim3((unsigned)d.chunks, (unsigned)d.slabs, (unsigned)d.batch), kBlock, 0, st>>>(d);
-            hipError_t e = hipGetLastError();
+            const unsigned chunks = (unsigned)d.chunks, slabs = (unsigned)d.slabs, groups = (unsigned)d.groups;
+            hipError_t e = in_ranges(d, (int64_t)chunks * slabs, [&](const GroupDev& c, unsigned n) {
+                k_group_sums<T, WIDTH><<<dim3(chunks, slabs, n), kBlock, 0, st>>>(c);
+            });
             if (e != hipSuccess) return e;
-            k_group_join<<<dim3((unsigned)d.groups, (unsigned)d.batch), 256, 0, st>>>(d);
-            e = hipGetLastError();
+            e = in_ranges(d, groups, [&](const GroupDev& c, unsigned n) { k_group_join<<<dim3(groups, n), 256, 0, st>>>(c); });
             if (e != hipSuccess) return e;
-            const unsigned blocks = d.dx ? (unsigned)(parts_of(d.pixels, d.spread) * d.slabs * d.batch) : 0;
-            if (blocks + params > 0) k_group_dx<T, WIDTH><<<blocks + params, kBlock, 0, st>>>(d, blocks);
-            return hipGetLastError();
-        }
-        if (any) {
+            const unsigned spreads = (unsigned)parts_of(d.pixels, d.spread);
+            if (d.dx) {
+                unsigned with = params;              // the first range's launch joins the samples' sums too
+                return in_ranges(d, (int64_t)spreads * slabs, [&](const GroupDev& c, unsigned n) {
+                    const unsigned blocks = spreads * slabs * n;
+                    k_group_dx<T, WIDTH><<<blocks + with, kBlock, 0, st>>>(c, blocks, (int)spreads);
+                    with = 0;
+                });
+            }
+        } else if (any) {
             const dim3 grid((unsigned)d.slabs, (unsigned)d.batch);
             if (held(d) <= 2) k_group_bwd_whole<T, WIDTH, 2><<<grid, kBlock, 0, st>>>(d);
             else k_group_bwd_whole<T, WIDTH, kHeld><<<grid, kBlock, 0, st>>>(d);

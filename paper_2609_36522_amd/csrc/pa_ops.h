@@ -62,6 +62,7 @@ struct GroupDev {
     float* means;                    // backward: [batch][groups][2] mean(g), mean(g xh)
     int64_t xs[2], ys[2], dxs[2];    // batch, pixel
     int batch, pixels, channels, groups, width;   // width: channels of a group
+    int sample0;                     // a launch's first sample
     int slab, slabs;                 // channels of a block (whole groups; the last has what is left), blocks over them
     int chunk, chunks;               // pixels of a block, blocks over them
     int spread;                      // pixels of a block in the second pass

@@ -1,0 +1,42 @@
+"""Group norm, the feed-forward block and the 8-bit projection on the device where a call is at the edge of what it takes:
+the largest grids, values near the largest numbers, every tile."""
+import pytest
+import torch
+
+import block_ops_reference as R
+from ops_reference import check
+from paper_2609_36522_amd import ops
+
+pytestmark = pytest.mark.gpu
+
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+
+
+@pytest.fixture(autouse=True)
+def _lib(gpu_lib):
+    return gpu_lib
+
+
+def _randn(g, *s, dtype=F32):
+    return torch.randn(s, generator=g, device="cuda", dtype=dtype)
+
+
+# ------------------------------------------------------------------ group norm
+def test_group_norm_in_ranges_of_samples():
+    """8200 samples of 65536 groups: more than 2^20 blocks over the samples in every pass, 2^23 slabs and more, so that each
+    pass takes several launches. Both ends of both ranges' samples, and the parameters' gradients over all of them."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    Bn, P, C = 8200, 2, 65536
+    x, dy = _randn(g, Bn, P, C, dtype=BF16), _randn(g, Bn, P, C, dtype=BF16)
+    w, b = _randn(g, C, dtype=BF16), _randn(g, C, dtype=BF16)
+    y, mean, rstd = ops.group_norm_forward(x, C, w, b, activation="silu")
+    dx, dw, db = ops.group_norm_backward(dy, x, mean, rstd, w, b, activation="silu")
+    cols = torch.tensor([0, 1, 511, 512, 32767, 65024, 65535], device="cuda")
+    at = {n: t[:, :, cols].contiguous() for n, t in (("x", x), ("y", y), ("dy", dy), ("dx", dx))}
+    ref = R.group_norm(at["x"], len(cols), w[cols], b[cols], 1e-5, "silu", at["dy"])
+    for name, got in (("y", at["y"]), ("dx", at["dx"]), ("dw", dw[cols]), ("db", db[cols])):
+        check(got, *ref[name], name)
+    some = [0, 1, 8190, 8191, 8192, 8199]
+    ref = R.group_norm(x[some], C, w, b, 1e-5, "silu", dy[some])
+    check(y[some], *ref["y"], "y of whole samples")
+    check(dx[some], *ref["dx"], "dx of whole samples")
