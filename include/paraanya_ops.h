@@ -159,7 +159,7 @@ PA_API int paraanya_lora_linear_workspace(const pa_lora_t* p, size_t* bytes);
 /* ------------------------------------------------------------------ group norm
  * y = act((x - mean) rstd * weight + bias) over a channels-last tensor [batch][pixels][channels]: mean
  * and v = mean (x - mean)^2 are those of a sample's group (channels / groups consecutive channels, all
- * pixels), rstd = 1 / sqrt(v + eps). */
+ * pixels), rstd = 1 / sqrt(v + eps). In fp32 throughout: a group's sum of (x - mean)^2 has to stay below 2^128. */
 #define PA_ACT_NONE 0
 #define PA_ACT_SILU 1          /* z / (1 + e^-z) */
 #define PA_ACT_GELU 2          /* z Phi(z), the normal distribution's */

@@ -227,7 +227,7 @@ struct Running {
                 q += r < count ? t * t : 0.0f;
             }
             mean[i] = fmaf(e, part, mean[i]);
-            m2[i] += fmaf(e * e, both, q);
+            m2[i] += fmaf(e * both, e, q);          // (e * e alone overflows from 2^64 on, also where there is nothing to join it to)
         }
         n = total;
     }
@@ -260,7 +260,7 @@ __device__ __forceinline__ void statistics(const GroupDev& d, const Place& q, co
     const float inv = 1.0f / ((float)(q.p1 - q.p0) * (float)d.width);
     q.each_group(d, [&](int i, int g) {
         const float e = r.mean[i] - fmaf(out.sum[g], inv, out.first[g]);
-        v[i] = fmaf(e * e, r.n, r.m2[i]);
+        v[i] = fmaf(e * r.n, e, r.m2[i]);           // likewise of a thread without pixels
     });
     group_sums(d, q, v, lds, out.m2);
 }

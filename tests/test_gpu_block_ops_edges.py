@@ -40,3 +40,27 @@ def test_group_norm_in_ranges_of_samples():
     ref = R.group_norm(x[some], C, w, b, 1e-5, "silu", dy[some])
     check(y[some], *ref["y"], "y of whole samples")
     check(dx[some], *ref["dx"], "dx of whole samples")
+
+
+# Fewer pixels than lanes, as many as a block's registers hold (8 and 42 a thread), several chunks.
+@pytest.mark.parametrize("Bn,P,C,G", [(2, 3, 64, 8), (1, 1, 24, 3), (2, 500, 64, 8), (180, 2689, 32, 8), (2, 4000, 64, 8), (3, 3000, 330, 33)])
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+def test_group_norm_of_values_whose_squares_overflow(Bn, P, C, G, dt):
+    """A mean of 2^64 and more, whose square is no number in fp32: with no spread, and with one whose squares are."""
+    g = torch.Generator(device="cuda").manual_seed(P)
+    w, b = _randn(g, C, dtype=dt), _randn(g, C, dtype=dt)
+    x = torch.full((Bn, P, C), 2.0**66, dtype=dt, device="cuda")
+    y, mean, rstd = ops.group_norm_forward(x, G, w, b, activation="silu")
+    assert bool((mean == 2.0**66).all())
+    check(y, *R.group_norm(x, G, w, b, 1e-5, "silu")["y"], "y of a constant")
+    if dt == BF16:
+        # Two neighbours: 2^57 apart, at most 24000 squares of 2^112.
+        x = 2.0**64 * (1 + torch.randint(0, 2, (Bn, P, C), generator=g, device="cuda") / 128)
+    else:
+        x = 2.0**66 * (1 + 1e-4 * _randn(g, Bn, P, C))
+    x, dy = x.to(dt), _randn(g, Bn, P, C, dtype=dt)
+    y, mean, rstd = ops.group_norm_forward(x, G, w, b, activation="silu")
+    dx, dw, db = ops.group_norm_backward(dy, x, mean, rstd, w, b, activation="silu")
+    ref = R.group_norm(x, G, w, b, 1e-5, "silu", dy)
+    for name, got in (("y", y), ("dx", dx), ("dw", dw), ("db", db)):
+        check(got, *ref[name], name)
