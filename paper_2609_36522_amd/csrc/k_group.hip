@@ -146,23 +146,25 @@ __device__ __forceinline__ void numbers(const GroupDev& d, const void* p, const 
     }
 }
 
-// The activation is the same for all: one branch for 8 values.
+// The activation is the same for all: one branch for 8 values. EXACT: of results in fp32.
+template <bool EXACT>
 __device__ __forceinline__ void activate8(int act, float (&v)[8]) {
     if (act == PA_ACT_SILU) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = activate<PA_ACT_SILU>(v[i]);
     } else if (act == PA_ACT_GELU) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = activate<PA_ACT_GELU>(v[i]);
+        for (int i = 0; i < 8; ++i) v[i] = activate<PA_ACT_GELU, EXACT>(v[i]);
     }
 }
+template <bool EXACT>
 __device__ __forceinline__ void slope8(int act, float (&v)[8]) {       // its derivative
     if (act == PA_ACT_SILU) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = activate_grad<PA_ACT_SILU>(v[i]).y;
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = activate_grad<PA_ACT_GELU>(v[i]).y;
+        for (int i = 0; i < 8; ++i) v[i] = activate_grad<PA_ACT_GELU, EXACT>(v[i]).y;
     }
 }
 
@@ -271,7 +273,7 @@ __device__ __forceinline__ Pack8<T> normalized(const Pack8<T>& x, const float (&
     float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = fmaf((float)x.v[i] - mean[i], a[i], b[i]);
-    activate8(act, v);
+    activate8<sizeof(T) == 4>(act, v);
     Pack8<T> o;
 #pragma unroll
     for (int i = 0; i < 8; ++i) o.v[i] = (T)v[i];
@@ -470,7 +472,7 @@ __device__ __forceinline__ void through(const Channels& k, const Pack8<T>& x, co
     float s[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) s[i] = fmaf(xh[i], k.w[i], k.b[i]);
-    slope8(act, s);
+    slope8<sizeof(T) == 4>(act, s);
 #pragma unroll
     for (int i = 0; i < 8; ++i) dz[i] *= s[i];
 }

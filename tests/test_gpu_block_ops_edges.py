@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import block_ops_reference as R
-from ops_reference import check
+from ops_reference import TINY, U, check
 from paper_2609_36522_amd import ops
 
 pytestmark = pytest.mark.gpu
@@ -64,3 +64,49 @@ def test_group_norm_of_values_whose_squares_overflow(Bn, P, C, G, dt):
     ref = R.group_norm(x, G, w, b, 1e-5, "silu", dy)
     for name, got in (("y", y), ("dx", dx), ("dw", dw), ("db", db)):
         check(got, *ref[name], name)
+
+
+def _activation_bounds(act, z, exact):
+    """(value, derivative, bound of each before it is rounded to its type) for an activation of fp32 numbers z. The shares, in
+    units u = 2^-24: an exponential unit's result is off by 2 u of itself, a reciprocal by 2 u, each product or sum by one."""
+    u, a, z = 2.0**-24, z.double().abs(), z.double()
+    if act == "silu":
+        # 2^(-z log2 e): the constant and the product are rounded, |z| u each in the exponential; of p that is its share 1 - p.
+        p, r = torch.sigmoid(z), torch.sigmoid(-z)
+        ep = p * u * (2 * a * r + 2 * r + 4)
+        v, d = z * p, p + z * p * r
+        # v (1 - p) + p: 1 - p is off by ep and a rounding.
+        return v, d, a * ep + u * v.abs() + 2.0**-120, ep + a * r * (ep + u * p) + a * p * (ep + u * r) + u * (p + d.abs()) + 2.0**-120
+    # (torch.special.ndtr loses its digits in the tail.)
+    upper, lower = (torch.special.erfc(t / 2**0.5) / 2 for t in (a, -z))
+    phi = torch.exp(-z * z / 2) / (2 * torch.pi)**0.5
+    v, d = z * lower, lower + z * phi
+    # The density: 0.72 z^2 from two products and a rounded constant, 0.72 ln2 z^2 = z^2 / 2 u each, and 3 more products.
+    ephi = phi * u * (3 + 1.5 * a * a)
+    if not exact:
+        return v, d, 1.5e-7 * a.clamp(min=1) + u * v.abs(), 4e-6 + a * ephi + 2 * u
+    # 2 Q = 2^-P: steps of P's evaluation are rounded (sums of up to 8 times P) and its fit is within 20 u beyond 3; beyond 8 the
+    # result is at most what it is there.
+    eq = upper * u * (4 + 8 * -torch.log2(2 * upper) + 20 * (a > 3)) + 7e-16 * (a > 8)
+    return v, d, a * eq + u * v.abs(), eq + a * ephi + u * (lower + d.abs())
+
+
+@pytest.mark.parametrize("P", [1, 5000])
+@pytest.mark.parametrize("dt", [F32, BF16, F16], ids=["f32", "bf16", "f16"])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_group_norm_activation_and_its_derivative(act, dt, P):
+    """A weight of 0: y is the activation of the bias, and dbias, where dy is 1 in one pixel, its derivative. Parameters
+    in fp32, so that the derivative is not rounded to x's type."""
+    C = 65536 if P == 1 else 2048
+    z = torch.linspace(-14, 14, C, device="cuda")
+    z[: C // 4] = torch.linspace(-1, 1, C // 4, device="cuda") ** 5
+    x = _randn(torch.Generator(device="cuda").manual_seed(1), 1, P, C, dtype=dt)
+    dy = torch.zeros_like(x)
+    dy[0, P // 2] = 1
+    w = torch.zeros_like(z)
+    y, mean, rstd = ops.group_norm_forward(x, 32, w, z, activation=act)
+    _, _, db = ops.group_norm_backward(dy, x, mean, rstd, w, z, activation=act)
+    v, d, ev, ed = _activation_bounds(act, z, dt == F32)
+    for row in (0, P - 1):
+        check(y[0, row], v, ev + (0 if dt == F32 else U[dt]) * v.abs() + TINY[dt], f"{act} in {dt}")
+    check(db, d, ed, f"the derivative of {act} in {dt}")
