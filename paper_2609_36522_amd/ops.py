@@ -638,7 +638,10 @@ class _FeedForward(torch.autograd.Function):
 
 
 def feed_forward(x, gate, up, down, gate_bias=None, up_bias=None, down_bias=None, *, activation="silu"):
-    """:func:`feed_forward_forward`'s y, differentiable (once) in x, the weights and the biases."""
+    """:func:`feed_forward_forward`'s y, differentiable (once) in x, the weights and the biases. Under ``torch.no_grad()``
+    nothing is saved."""
+    if not torch.is_grad_enabled():          # (needs_input_grad tells of the tensors alone)
+        return feed_forward_forward(x, gate, up, down, gate_bias, up_bias, down_bias, activation=activation, save=False)[0]
     return _FeedForward.apply(x, gate, up, down, gate_bias, up_bias, down_bias, activation)
 
 
