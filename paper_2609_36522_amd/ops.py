@@ -473,9 +473,10 @@ def group_norm_forward(x, groups, weight=None, bias=None, eps=1e-5, *, activatio
     return y, mean, rstd
 
 
-def group_norm_backward(dy, x, mean, rstd, weight=None, bias=None, *, activation=None, param_dtype=None):
+def group_norm_backward(dy, x, mean, rstd, weight=None, bias=None, *, activation=None, param_dtype=None, need=(True,) * 3):
     """(dx, dweight, dbias) from the forward pass's x, weight, bias, mean and rstd. dweight and dbias have the
-    parameters' type (``param_dtype``, or x's, where there are none)."""
+    parameters' type (``param_dtype``, or x's, where there are none). ``need`` says which of the three are computed (None in
+    the others' place)."""
     act = _activation(activation)
     if mean.dim() != 2 or mean.shape[0] != x.shape[0]:
         raise ValueError("mean and rstd must be [batch, groups]")
@@ -496,12 +497,12 @@ def group_norm_backward(dy, x, mean, rstd, weight=None, bias=None, *, activation
     p, _, _, n = _group(B_, P, Ch, groups, _DTYPE[x.dtype], _DTYPE[pt], act, 0.0, x3.stride()[:2], (P * Ch, Ch))
     p = GroupNorm.from_buffer_copy(p)
     p.y_stride[:] = dy3.stride()[:2]
-    dx = x.new_empty(x.shape)
-    dw = x.new_empty(Ch, dtype=pt)
-    db = x.new_empty(Ch, dtype=pt)
+    dx = x.new_empty(x.shape) if need[0] else None
+    dw = x.new_empty(Ch, dtype=pt) if need[1] else None
+    db = x.new_empty(Ch, dtype=pt) if need[2] else None
     ws = _workspace(n, x)
     B._check(_LIB.paraanya_group_norm_backward(C.byref(p), dy3.data_ptr(), x3.data_ptr(), _ptr(weight), _ptr(bias), mean.data_ptr(),
-                                               rstd.data_ptr(), dx.data_ptr(), dw.data_ptr(), db.data_ptr(), _ptr(ws), n, st))
+                                               rstd.data_ptr(), _ptr(dx), _ptr(dw), _ptr(db), _ptr(ws), n, st))
     return dx, dw, db
 
 
@@ -517,9 +518,10 @@ class _GroupNorm(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dy):
         x, weight, bias, mean, rstd = ctx.saved_tensors
-        dx, dw, db = group_norm_backward(dy, x, mean, rstd, weight, bias, activation=ctx.activation)
-        need = ctx.needs_input_grad
-        return dx if need[0] else None, None, dw if need[2] else None, db if need[3] else None, None, None
+        need = tuple(ctx.needs_input_grad[i] for i in (0, 2, 3))
+        some = {} if all(need) else {"need": need}
+        dx, dw, db = group_norm_backward(dy, x, mean, rstd, weight, bias, activation=ctx.activation, **some)
+        return dx, None, dw, db, None, None
 
 
 def group_norm(x, groups, weight=None, bias=None, eps=1e-5, *, activation=None):

@@ -110,3 +110,23 @@ def test_group_norm_activation_and_its_derivative(act, dt, P):
     for row in (0, P - 1):
         check(y[0, row], v, ev + (0 if dt == F32 else U[dt]) * v.abs() + TINY[dt], f"{act} in {dt}")
     check(db, d, ed, f"the derivative of {act} in {dt}")
+
+
+@pytest.mark.parametrize("P", [60, 3000])
+def test_group_norm_gradients_one_at_a_time(P):
+    g = torch.Generator(device="cuda").manual_seed(P)
+    x, dy, w, b = (_randn(g, *s, dtype=BF16) for s in ((2, P, 96), (2, P, 96), (96,), (96,)))
+    _, mean, rstd = ops.group_norm_forward(x, 4, w, b, activation="silu")
+    every = ops.group_norm_backward(dy, x, mean, rstd, w, b, activation="silu")
+    for need in ((True, False, False), (False, True, False), (False, False, True), (False, True, True), (True, False, True), (False,) * 3):
+        got = ops.group_norm_backward(dy, x, mean, rstd, w, b, activation="silu", need=need)
+        assert all(a is None if not k else torch.equal(a, e) for a, e, k in zip(got, every, need)), need
+    for i in range(3):
+        leaves = [t.clone().requires_grad_(k == i) for k, t in enumerate((x, w, b))]
+        ops.group_norm(leaves[0], 4, *leaves[1:], activation="silu").backward(dy)
+        assert torch.equal(leaves[i].grad, every[i]) and sum(t.grad is not None for t in leaves) == 1
+    x.requires_grad_()
+    y = ops.group_norm(x, 4, activation="silu")          # no parameters
+    y.backward(dy)
+    _, mean, rstd = ops.group_norm_forward(x.detach(), 4, activation="silu")
+    assert torch.equal(x.grad, ops.group_norm_backward(dy, x.detach(), mean, rstd, activation="silu")[0])
