@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import block_ops_reference as R
+import feed_reference as F
 from ops_reference import TINY, U, check
 from paper_2609_36522_amd import ops
 
@@ -130,3 +131,31 @@ def test_group_norm_gradients_one_at_a_time(P):
     y.backward(dy)
     _, mean, rstd = ops.group_norm_forward(x.detach(), 4, activation="silu")
     assert torch.equal(x.grad, ops.group_norm_backward(dy, x.detach(), mean, rstd, activation="silu")[0])
+
+
+# ------------------------------------------------------------------ feed-forward block
+def _feed(M, K, H, N, dt, act, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x, gate, up, down = (f * _randn(g, *s) for s, f in (((M, K), 1), ((H, K), K**-0.5), ((H, K), K**-0.5), ((N, H), H**-0.5)))
+    biases = tuple((0.2 * _randn(g, n)).to(dt) for n in (H, H, N))
+    args = tuple(t.to(dt) for t in (x, gate, up, down))
+    dy = _randn(g, M, N).to(dt)
+    y, saved = ops.feed_forward_forward(*args, *biases, activation=act)
+    grads = ops.feed_forward_backward(dy, *args, saved, activation=act)
+    ref = F.feed_forward(*args, biases, act, dy)
+    for name, got in (("y", y), *grads._asdict().items()):
+        what = f"{name} of {M}x{K}x{H}x{N} {dt} {act}"
+        want, bound = ref.pop(name)
+        check(got, want, bound, what)
+        if want.numel() >= 1000:
+            off, limit = float((got.double() - want).norm()), F.norm_limit(name, want, dt, M * H)
+            assert off < limit, f"{what}: off by {off / float(want.norm()) / U[dt]:.3f} roundings' size, of {limit / float(want.norm()) / U[dt]:.3f}"
+
+
+# The few-row kernels; sizes in whole pieces, which are read in place.
+@pytest.mark.parametrize("M,K,H,N", [(1, 1000, 3000, 1500), (17, 264, 2048, 1032), (32, 77, 999, 333), (40, 1024, 2048, 512), (2048, 1024, 2048, 1024),
+                                     (1500, 264, 1000, 520)])
+@pytest.mark.parametrize("act", [None, "silu", "gelu"])
+@pytest.mark.parametrize("dt", [BF16, F16], ids=["bf16", "f16"])
+def test_feed_forward_roundings(M, K, H, N, dt, act):
+    _feed(M, K, H, N, dt, act, seed=M + K)
