@@ -7,6 +7,7 @@ import block_ops_reference as R
 import feed_reference as F
 from ops_reference import TINY, U, check
 from paper_2609_36522_amd import ops
+from tile_shapes import FEED_TILES, INT8_TILES
 
 pytestmark = pytest.mark.gpu
 
@@ -152,6 +153,12 @@ def _feed(M, K, H, N, dt, act, seed=0):
             assert off < limit, f"{what}: off by {off / float(want.norm()) / U[dt]:.3f} roundings' size, of {limit / float(want.norm()) / U[dt]:.3f}"
 
 
+@pytest.mark.parametrize("M,K,H,N", FEED_TILES)
+@pytest.mark.parametrize("dt", [BF16, F16], ids=["bf16", "f16"])
+def test_feed_forward_of_every_tile(M, K, H, N, dt):
+    _feed(M, K, H, N, dt, "silu" if M % 2 else "gelu", seed=M)
+
+
 # The few-row kernels; sizes in whole pieces, which are read in place.
 @pytest.mark.parametrize("M,K,H,N", [(1, 1000, 3000, 1500), (17, 264, 2048, 1032), (32, 77, 999, 333), (40, 1024, 2048, 512), (2048, 1024, 2048, 1024),
                                      (1500, 264, 1000, 520)])
@@ -159,3 +166,14 @@ def _feed(M, K, H, N, dt, act, seed=0):
 @pytest.mark.parametrize("dt", [BF16, F16], ids=["bf16", "f16"])
 def test_feed_forward_roundings(M, K, H, N, dt, act):
     _feed(M, K, H, N, dt, act, seed=M + K)
+
+
+# ------------------------------------------------------------------ 8-bit integers
+@pytest.mark.parametrize("M,K,N", INT8_TILES)
+@pytest.mark.parametrize("dt", [BF16, F16], ids=["bf16", "f16"])
+def test_int8_linear_of_every_tile(M, K, N, dt):
+    g = torch.Generator(device="cuda").manual_seed(M)
+    q, w = (torch.randint(-128, 128, s, dtype=torch.int8, device="cuda", generator=g) for s in ((M, K), (N, K)))
+    s, ws = (torch.rand(n, device="cuda", generator=g) / K**0.5 / 50 for n in (M, N))
+    bias = _randn(g, N).to(dt)
+    check(ops.int8_linear(q, s, w, ws, bias, dtype=dt), *R.int8_linear(q, s, w, ws, bias, dt), f"y of {M}x{K}x{N} {dt}")

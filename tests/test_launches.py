@@ -1,5 +1,5 @@
 """What the operators launch, recorded without a GPU (launch_record.py): grids within the limits of a launch at the largest
-sizes that are accepted."""
+sizes that are accepted, and the tiles that the listed sizes of tile_shapes.py take."""
 import math
 import os
 
@@ -8,6 +8,7 @@ import pytest
 import launch_record as L
 from paper_2609_36522_amd import build as B
 from paper_2609_36522_amd import ops as O
+from tile_shapes import FEED_TILES, INT8_TILES
 
 
 @pytest.fixture(scope="module")
@@ -43,3 +44,80 @@ def test_group_norm_grids(recorder, backward, dtype):
         for name, n in blocks.items():
             assert n == params if name == "k_group_params" else n % batch == 0 and n > 0, (call, name, n)
         assert blocks.get("k_group_join", batch * groups) == batch * groups, call
+
+
+# Matrices at the limits of elements (2^34), of tiles (2^23 of 64 x 64) and of a width (2^20).
+FEED_SIZES = [(1 << 29, 1, 1, 1), (1 << 29, 32, 8, 32), (1 << 14, 1 << 20, 1 << 14, 1 << 14), (33, 1 << 14, 1 << 20, 1 << 14), (33, 1 << 20, 1 << 14, 1 << 20),
+              (1 << 14, 8, 1 << 20, 3), ((1 << 14) + 1, 1 << 14, 1 << 20, 1 << 14), (1, 1 << 14, 1 << 20, 1 << 14), (1 << 19, 1 << 15, 1, 1 << 15)]
+
+
+@pytest.mark.parametrize("dtype,alignment", [(O.PA_BF16, 16), (O.PA_F16, 2)])
+def test_feed_forward_grids(recorder, dtype, alignment):
+    calls = [f"feed {b} {' '.join(map(str, s))} {dtype} {O.PA_ACT_SILU} {alignment}" for s in FEED_SIZES for b in (0, 1)]
+    for call, (status, launches) in zip(calls, L.record(recorder, calls)):
+        rows, *widths = map(int, call.split()[2:6])
+        assert status == 0 if rows * max(widths) <= 1 << 34 else (status == -6 and not launches), (call, status)
+        for k in launches:
+            assert math.prod(k.grid) * math.prod(k.block) < 1 << 32 and max(k.grid[1:]) < 1 << 16, (call, k)
+
+
+def test_int8_linear_grids(recorder):
+    sizes = [(1 << 29, 16, 64), (1 << 15, 131071, 1 << 20), (1 << 30, 1, 1), (65, 64, 1 << 20), (1, 64, 1 << 20)]
+    calls = [f"int8 {' '.join(map(str, s))} {O.PA_F16}" for s in sizes]
+    for call, (status, launches) in zip(calls, L.record(recorder, calls)):
+        rows, _, out = map(int, call.split()[1:4])
+        assert status == 0 if -(-rows // 64) * -(-out // 64) <= 1 << 23 else (status == -6 and not launches), (call, status)
+        for k in launches:
+            assert math.prod(k.grid) * math.prod(k.block) < 1 << 32 and max(k.grid[1:]) < 1 << 16, (call, k)
+
+
+# ------------------------------------------------------------------ the tiles that tile_shapes.py is to take
+# Waves over features and over rows, 32-wide tiles a wave of each, stages.
+BIG, TALL, WIDE, MID, DEEP, SMALL = (2, 4, 4, 2, 2), (4, 2, 2, 2, 3), (2, 2, 2, 3, 2), (2, 2, 2, 2, 2), (2, 2, 2, 2, 3), (2, 2, 1, 1, 4)
+GATED_SMALL = (1, 4, 2, 1, 3)
+
+
+def _up(n, d):
+    return -(-n // d)
+
+
+def _taken(launches, joined, product, sizes, parts):
+    """{(product, tile, split)} of a call's launch, if a range of its reduction has 2 x stages + 1 parts or more."""
+    out = set()
+    for k in launches:
+        if k.name != product:
+            continue
+        features, rows = k.tile[0] * k.tile[2] * 32, k.tile[1] * k.tile[3] * 32
+        if k.name == "k_feed_gate":
+            features //= 2
+        ranges, rest = divmod(k.grid[0], sum(_up(f, features) * _up(r, rows) for f, r in sizes))
+        assert rest == 0 and (ranges > 1) == any(j.name == joined for j in launches), k
+        if parts // ranges >= 2 * k.tile[4] + 1:
+            out.add((product, k.tile, ranges > 1))
+    return out
+
+
+def test_listed_sizes_take_every_tile_of_the_feed_forward_block(recorder):
+    for dtype in (O.PA_BF16, O.PA_F16):
+        of_type = set()
+        for M, K, H, N in FEED_TILES:
+            (fs, forward), (bs, backward) = L.record(recorder, [f"feed {b} {M} {K} {H} {N} {dtype} {O.PA_ACT_SILU} 16" for b in (0, 1)])
+            assert fs == 0 and bs == 0
+            of_type |= _taken(forward, None, "k_feed_gate", [(H, M)], _up(K, 64))
+            of_type |= {("y", *t[1:]) for t in _taken(forward, "k_feed_join", "k_feed_plain", [(N, M)], _up(H, 64))}
+            of_type |= _taken(backward, None, "k_feed_grad", [(H, M)], _up(N, 64))
+            of_type |= {("dx", *t[1:]) for t in _taken(backward, "k_feed_join", "k_feed_plain", [(K, M)], 2 * _up(H, 64))}
+            of_type |= _taken(backward, "k_feed_weights_join", "k_feed_weights", [(K, H), (K, H), (H, N)], _up(M, 64))
+        want = {("k_feed_gate", t, False) for t in (BIG, WIDE, MID, DEEP, GATED_SMALL)}
+        want |= {("k_feed_grad", t, False) for t in (BIG, TALL, WIDE, MID, DEEP, SMALL)}
+        want |= {(p, t, s) for p in ("y", "dx", "k_feed_weights") for t in (BIG, TALL, WIDE, MID, DEEP, SMALL) for s in (False, True)}
+        assert of_type == want, (dtype, want - of_type, of_type - want)
+
+
+def test_listed_sizes_take_every_tile_of_the_8_bit_projection(recorder):
+    got = set()
+    for M, K, N in INT8_TILES:
+        (status, launches), = L.record(recorder, [f"int8 {M} {K} {N} {O.PA_BF16}"])
+        assert status == 0
+        got |= _taken(launches, None, "k_int8_tile", [(N, M)], _up(K, 128))
+    assert got == {("k_int8_tile", t, False) for t in (BIG, TALL, WIDE, MID, DEEP, SMALL)}
