@@ -225,7 +225,11 @@ __global__ __launch_bounds__(1024) void k_int8_few(Int8Dev d) {
 
 template <class T>
 hipError_t linear(const Int8Dev& d, hipStream_t st) {
-    if (d.rows <= 64) {
+    // The weights read straight from memory, or tiles: up to 64 rows where a CU has at most one block of 16 features, up to 16
+    // where it has more. us of both for 17, 32, 48 and 64 rows: 1024x4096 3.6, 4.0, 4.6, 5.2 and 5.0 to 5.2; 4096x1024 6.7, 8.0,
+    // 9.6, 12.2 and 11.6 to 11.8; 2048x4096 5.3, 5.9, 7.0, 7.9 and 7.8 to 8.0; 2048x6144 7.2, 8.7, 11.9, 13.8 and 7.9 to 8.2 (16
+    // rows 6.8 and 7.8); 8192x8192 20.8, 27.4, 36.6, 44.6 and 21.8 to 23.1 (16 rows 19.0 and 21.6).
+    if (d.rows <= (d.out <= 16 * kCUs ? 64 : 16)) {
         const unsigned blocks = (unsigned)((d.out + 15) / 16);
         if (d.rows <= 16)      k_int8_few<T, 2, 1><<<blocks, 1024, 0, st>>>(d);
         else if (d.rows <= 32) k_int8_few<T, 2, 2><<<blocks, 1024, 0, st>>>(d);
@@ -233,7 +237,11 @@ hipError_t linear(const Int8Dev& d, hipStream_t st) {
         return hipGetLastError();
     }
     GemmJob job{{d.w, nullptr}, {d.x, nullptr}, d.w_stride, d.x_stride, d.out, d.rows, d.in, 0, 0};
-    // Twice the elements a part at twice the rate: the same rule in parts.
+    // Twice the elements a part at twice the rate: the same rule in parts. us with 256 x 256, 256 x 128, 128 x 192, 128 x 128 (two
+    // stages), the same (three) and 64 x 64 tiles, and what the rule takes:
+    //   32768x2048x8192 574 668 612 677 782 1055, 573       8192x4096x1024   47  39  45  41  47  65,  40
+    //   8192x1024x4096   52  64  56  61  70   81,  52       9216x8192x1024   96 111  85 120 113 141,  85
+    //   1999x1100x1347   23  15  16  14  12   14,  12       1000x2048x2048   27  17  18  16  13  11,  11
     int kind = 0;
     float least = 0.0f;
     for (int k = 0; k < kTileKinds; ++k) {

@@ -169,7 +169,7 @@ def test_feed_forward_roundings(M, K, H, N, dt, act):
 
 
 # ------------------------------------------------------------------ 8-bit integers
-@pytest.mark.parametrize("M,K,N", INT8_TILES)
+@pytest.mark.parametrize("M,K,N", INT8_TILES + [(16, 500, 4111), (17, 500, 4111), (50, 1100, 5000), (64, 129, 4096)])
 @pytest.mark.parametrize("dt", [BF16, F16], ids=["bf16", "f16"])
 def test_int8_linear_of_every_tile(M, K, N, dt):
     g = torch.Generator(device="cuda").manual_seed(M)

@@ -121,3 +121,10 @@ def test_listed_sizes_take_every_tile_of_the_8_bit_projection(recorder):
         assert status == 0
         got |= _taken(launches, None, "k_int8_tile", [(N, M)], _up(K, 128))
     assert got == {("k_int8_tile", t, False) for t in (BIG, TALL, WIDE, MID, DEEP, SMALL)}
+
+
+def test_few_rows_of_the_8_bit_projection(recorder):
+    """Straight from memory where a CU has one block of 16 features, up to 64 rows, and with 16 rows at any width."""
+    calls = [(64, 4096, True), (65, 4096, False), (16, 4097, True), (17, 4097, False), (1, 1 << 20, True), (64, 1, True)]
+    for (rows, out, few), (status, (k,)) in zip(calls, L.record(recorder, [f"int8 {m} 200 {n} {O.PA_F16}" for m, n, _ in calls])):
+        assert status == 0 and k.name == ("k_int8_few" if few else "k_int8_tile"), (rows, out)
