@@ -771,7 +771,13 @@ int64_t held(const GroupDev& d) { return parts_of(d.pixels, kBlock / ((d.slab + 
 // One launch or two, us of a bf16 call: 1024 pixels of 640 channels (11 a thread), 16 to 1280 slabs: 15 and 20 (16), 19 and 24
 // (256), 28 and 33 (512), 54 and 54 (1024), 65 and 81 (1280). 4096 pixels of 320 channels (41 a thread, one block a CU): 43
 // and 35 (128 slabs), 44 and 48 (160), 49 and 56 (256), 82 and 76 (288), 86 and 95 (352), 106 and 111 (512): a block a CU
-// pays where two thirds of the CUs and more have one. The backward pass holds x and dy: up to 8 pixels of both.
+// pays where two thirds of the CUs and more have one.
+//
+// The backward pass holds x and dy: up to 4 pixels of both, or up to 8 where half of the CUs and more have a block. us in one pass
+// and in three launches, 320 channels in slabs of 40: 100 pixels (1 a thread) 8.6 and 12.7 (8 slabs), 9.5 and 13.7 (128), 14.9
+// and 15.1 (320); 400 pixels (4 a thread) 12.4 and 12.9 (8), 15.1 and 14.0 (64), 16.8 and 18.9 (128), 19.0 and 20.9 (192); 800
+// pixels (8 a thread) 16.8 and 13.4 (8), 21.4 and 19.1 (64), 24.3 and 23.4 (128), 27.4 and 31.6 (192); the last in fp32 16.9 and
+// 15.0 (8), 21.2 and 23.4 (64), 24.2 and 27.8 (128), 28.8 and 39.7 (192).
 void group_plan(GroupDev& d, int dtype, bool backward) {
     d.width = d.channels / d.groups;
     d.per_width = 1.0f / (float)d.width;
@@ -789,7 +795,7 @@ void group_plan(GroupDev& d, int dtype, bool backward) {
     const int64_t n = held(d), blocks = (int64_t)d.batch * d.slabs;
     bool whole = n <= kHeld;
     if (backward) {
-        whole = whole && (blocks >= 256 || (int64_t)d.batch * d.pixels * d.channels * (dtype == PA_F32 ? 4 : 2) <= 4 << 20);
+        whole = n <= kHeld / 2 || (whole && blocks >= 128);
     } else if (!whole && d.slab % 8 == 0 && d.channels % 8 == 0 && n <= (dtype == PA_F32 ? kHeldMost<float> : kHeldMost<__bf16>)) {
         whole = n <= 2 * kHeldBatch || 3 * blocks >= 2 * 256 * parts_of(blocks, 256);
     }

@@ -46,6 +46,15 @@ def test_group_norm_grids(recorder, backward, dtype):
         assert blocks.get("k_group_join", batch * groups) == batch * groups, call
 
 
+def test_group_norm_backward_in_one_pass(recorder):
+    """Up to 4 pixels a thread, or up to 8 where half of the CUs have a block (320 channels: 8 slabs of 102 lanes a sample)."""
+    calls = [(1, 408, True), (1, 409, False), (15, 816, False), (16, 816, True), (16, 817, False), (400, 817, False), (400, 816, True)]
+    for (batch, pixels, one), (status, launches) in zip(
+            calls, L.record(recorder, [f"group 1 {b} {p} 320 32 {O.PA_BF16} {O.PA_ACT_SILU}" for b, p, _ in calls])):
+        names = [k.name for k in launches]
+        assert status == 0 and names == (["k_group_bwd_whole", "k_group_params"] if one else ["k_group_sums", "k_group_join", "k_group_dx"]), (batch, pixels)
+
+
 # Matrices at the limits of elements (2^34), of tiles (2^23 of 64 x 64) and of a width (2^20).
 FEED_SIZES = [(1 << 29, 1, 1, 1), (1 << 29, 32, 8, 32), (1 << 14, 1 << 20, 1 << 14, 1 << 14), (33, 1 << 14, 1 << 20, 1 << 14), (33, 1 << 20, 1 << 14, 1 << 20),
               (1 << 14, 8, 1 << 20, 3), ((1 << 14) + 1, 1 << 14, 1 << 20, 1 << 14), (1, 1 << 14, 1 << 20, 1 << 14), (1 << 19, 1 << 15, 1, 1 << 15)]
