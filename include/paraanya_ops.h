@@ -198,11 +198,11 @@ PA_API int paraanya_group_norm_backward_workspace(const pa_group_norm_t* p, size
 
 /* ------------------------------------------------------------------ gated feed-forward block
  * h = act(x G^T + bg) * (x U^T + bu), y = h D^T + bd: both projections, the activation and the product in one
- * kernel, the projection back in a second. h is rounded to the element type as the second product's operand; so are,
- * for the backward pass, u act'(g) and act(g) of the two projections g and u, and the gradients by g and u as operands
- * of those of x and of the weights (in fp16 multiplied by a power of two that brings the largest |dy| to 1/16 .. 1/8, so that small gradients
- * keep their digits; they may be 2^19 times as large as dy). A gradient's error is so 1.3 to 1.8 times that of
- * rounding the result alone. */
+ * kernel, the projection back in a second. h is rounded to the element type as the second product's operand; so are
+ * the gradients by the two projections g and u as operands of those of x and of the weights (in fp16 multiplied by a power
+ * of two that brings the largest |dy| to 1/16 .. 1/8, so that small gradients keep their digits; they may be 2^19 times as
+ * large as dy). u act'(g) and act(g), by which dh gives them, are kept in 24 bits, with fp32's range. An error is so
+ * 1.4 times that of rounding the result alone, of y and of every gradient. In fp16 an h beyond 65504 is infinite. */
 typedef struct {
     int64_t rows;                /* 0 .. 2^30; a matrix has at most 2^34 elements and 2^23 tiles of 64 x 64 */
     int32_t in_features;         /* K: 1 .. 2^20 */

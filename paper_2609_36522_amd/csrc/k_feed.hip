@@ -82,6 +82,26 @@ __device__ __forceinline__ void store_padded(T* at, Pack8<T> p, int n) {
     *reinterpret_cast<Pack8<T>*>(at) = p;
 }
 
+// The factors kept for the backward pass are numbers of 24 bits, the upper three bytes of fp32's four (cut: 2^-15 at most), so
+// that a gradient is rounded to the element type where it is an operand and where it is a result, and nowhere else. (With factors
+// of the element type the gradients were off by 1.73 times the rounding of a result, so by 1.41; and fp16's range ended theirs.)
+// Their upper halves are matrices of their own; a third one has the last byte of both.
+__device__ __forceinline__ uint32_t bits(float v) { return __builtin_bit_cast(uint32_t, v); }
+__device__ __forceinline__ uint32_t last_bytes(float z, float u) { return (bits(z) >> 8 & 0xffu) | (bits(u) & 0xff00u); }
+__device__ __forceinline__ float by_z_of(uint32_t upper, uint32_t last) { return __builtin_bit_cast(float, upper << 16 | (last & 0xffu) << 8); }
+__device__ __forceinline__ float by_u_of(uint32_t upper, uint32_t last) { return __builtin_bit_cast(float, upper << 16 | (last & 0xff00u)); }
+
+// Words of 16 bits, word(i) of accumulator register 8 j + i, to the places of gather8.
+template <class F>
+__device__ __forceinline__ uint4 gather_words(F word) {
+    uint32_t w[2][2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int p = 0; p < 2; ++p) w[q][p] = word(4 * q + 2 * p) | word(4 * q + 2 * p + 1) << 16;
+    return rows8(w);
+}
+
 template <class X>
 __device__ __forceinline__ void clear(typename X::acc_t (&acc)[X::NM][X::NX], float (&sums)[X::NX]) {
 #pragma unroll
@@ -111,7 +131,7 @@ __device__ __forceinline__ void add(const float* per_feature, int half, f32x16 (
 // Both projections of a tile of rows, which read x once for the two; the activation and the product are formed in the
 // registers that hold them. Bound by the matrix units (the clock falls to 1.64 GHz under them, 77% busy) at long
 // reductions, by what follows the products at short ones: 32768x2048x8192 1720 us (1280 TFLOP/s; the library's product of this
-// size alone 1555), 8192x1024x4096 128 (1070), 145 to 160 where the factors of the backward pass are formed and kept.
+// size alone 1555), 8192x1024x4096 128 (1070), 156 to 171 where the factors of the backward pass are formed and kept.
 template <class X, int ACT>
 __global__ __launch_bounds__(X::THREADS, X::WAVES) void k_feed_gate(FeedDev d, GemmJob job) {
     typedef typename X::T T;
@@ -137,13 +157,13 @@ __global__ __launch_bounds__(X::THREADS, X::WAVES) void k_feed_gate(FeedDev d, G
 #pragma unroll
     for (int j = 0; j < X::NX; ++j) {
         auto store = [&](void* to, auto value) {
-            through_lds<T, HM>(own, lane, value, [&](int row, int at, const Pack8<T>& v) {
+            through_lds<uint16_t, HM>(own, lane, value, [&](int row, int at, const Pack8<uint16_t>& v) {
                 if (r0 + j * 32 + row < d.rows && f0 + at < d.hidden_pad)
-                    store_padded(static_cast<T*>(to) + (int64_t)(r0 + j * 32 + row) * d.hidden_pad + f0 + at, v, d.hidden - f0 - at);
+                    store_padded(static_cast<uint16_t*>(to) + (int64_t)(r0 + j * 32 + row) * d.hidden_pad + f0 + at, v, d.hidden - f0 - at);
             });
         };
         if (d.by_z) {
-            Pack8<T> by_z[HM][2];
+            uint4 by_z[HM][2], last[HM][2];
 #pragma unroll
             for (int m = 0; m < HM; ++m) {
                 f32x16 v;
@@ -154,10 +174,14 @@ __global__ __launch_bounds__(X::THREADS, X::WAVES) void k_feed_gate(FeedDev d, G
                     acc[m][j][i] = a.x;
                 }
 #pragma unroll
-                for (int q = 0; q < 2; ++q) by_z[m][q] = gather8<T>(v, q, 1.0f);
+                for (int q = 0; q < 2; ++q) {
+                    by_z[m][q] = gather_words([&](int i) { return bits(v[8 * q + i]) >> 16; });
+                    last[m][q] = gather_words([&](int i) { return last_bytes(v[8 * q + i], acc[m][j][8 * q + i]); });
+                }
             }
             store(d.by_z, [&](int m, int q) { return by_z[m][q]; });
-            store(d.by_u, [&](int m, int q) { return gather8<T>(acc[m][j], q, 1.0f); });
+            store(d.last, [&](int m, int q) { return last[m][q]; });
+            store(d.by_u, [&](int m, int q) { return gather_words([&](int i) { return bits(acc[m][j][8 * q + i]) >> 16; }); });
         } else {
 #pragma unroll
             for (int m = 0; m < HM; ++m)
@@ -330,8 +354,10 @@ __global__ __launch_bounds__(1024) void k_feed_few_gate(FeedDev d) {
     const float2 a = activate_grad<ACT>(g);
     static_cast<T*>(d.h)[to] = (T)(in ? a.x * u : 0.0f);
     if (d.by_z) {
-        static_cast<T*>(d.by_z)[to] = (T)(in ? a.y * u : 0.0f);
-        static_cast<T*>(d.by_u)[to] = (T)(in ? a.x : 0.0f);
+        const float z = in ? a.y * u : 0.0f, value = in ? a.x : 0.0f;
+        d.by_z[to] = (uint16_t)(bits(z) >> 16);
+        d.by_u[to] = (uint16_t)(bits(value) >> 16);
+        d.last[to] = (uint16_t)last_bytes(z, value);
     }
 }
 
@@ -351,13 +377,13 @@ __global__ __launch_bounds__(1024) void k_feed_few_down(FeedDev d) {
 
 // ------------------------------------------------------------------ backward
 // dh = dy D, then dz = dh (u act'(g)) and du = dh act(g) by the factors that the forward pass kept. (With g and u kept in their
-// place, each rounded, dx and the weights' gradients are off by 1.8 to 2 times the rounding of a result, so by 1.7; and their
-// activation here took 131 us for 103.) Bound by what follows the products, which reads and writes as much as it:
-// 8192x1024x4096 103 to 108 us, of which the product alone is 73 and 268 MB at the copy rate are 55.
+// place the activation took 28 us more here.) Bound by what follows the products, which reads and writes as much as it:
+// 8192x1024x4096 120 to 131 us, of which the product alone is 73 and 336 MB at the copy rate are 69. With factors of 16 bits, 67 MB
+// less, 103 to 108.
 template <class X>
 __global__ __launch_bounds__(X::THREADS, X::WAVES) void k_feed_grad(FeedDev d, GemmJob job) {
     typedef typename X::T T;
-    typedef T t4 __attribute__((ext_vector_type(4)));
+    typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
     __shared__ __align__(16) char lds[X::BYTES];
     f32x16 acc[X::NM][X::NX];
     float sums[X::NX];
@@ -376,25 +402,32 @@ __global__ __launch_bounds__(X::THREADS, X::WAVES) void k_feed_grad(FeedDev d, G
         for (int c = 0; c < X::NM; c += CM) {
             // Both factors, in the order in which they lie, then through LDS to the lanes that hold their places.
             const int fc = f0 + c * 32;
-            uint4 by[2][P / 2];
+            uint4 by[3][P / 2];
 #pragma unroll
             for (int i = 0; i < P / 2; ++i) {
                 const int at = i * 64 + lane, row = r0 + j * 32 + at / P, col = fc + at % P * 8;
-                by[0][i] = by[1][i] = make_uint4(0, 0, 0, 0);
+                by[0][i] = by[1][i] = by[2][i] = make_uint4(0, 0, 0, 0);
                 if (row < d.rows && col < d.hidden_pad) {
-                    by[0][i] = *reinterpret_cast<const uint4*>(static_cast<const T*>(d.by_z) + (int64_t)row * d.hidden_pad + col);
-                    by[1][i] = *reinterpret_cast<const uint4*>(static_cast<const T*>(d.by_u) + (int64_t)row * d.hidden_pad + col);
+                    const int64_t from = (int64_t)row * d.hidden_pad + col;
+                    by[0][i] = *reinterpret_cast<const uint4*>(d.by_z + from);
+                    by[1][i] = *reinterpret_cast<const uint4*>(d.by_u + from);
+                    by[2][i] = *reinterpret_cast<const uint4*>(d.last + from);
                 }
             }
+            u16x4 last[CM][4];
+            from_lds<CM>(own, lane, by[2], last);
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
-                t4 p[CM][4];
+                u16x4 p[CM][4];
                 from_lds<CM>(own, lane, by[n], p);
                 f32x16 v[CM];
 #pragma unroll
                 for (int m = 0; m < CM; ++m)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) v[m][i] = acc[c + m][j][i] * scale * (float)p[m][i >> 2][i & 3];
+                    for (int i = 0; i < 16; ++i) {
+                        const uint32_t upper = p[m][i >> 2][i & 3], low = last[m][i >> 2][i & 3];
+                        v[m][i] = acc[c + m][j][i] * scale * (n ? by_u_of(upper, low) : by_z_of(upper, low));
+                    }
                 T* to = static_cast<T*>(n ? d.du : d.dz);
                 through_lds<T, CM>(own, lane, [&](int m, int q) { return gather8<T>(v[m], q, 1.0f); }, [&](int row, int at, const Pack8<T>& o) {
                     if (r0 + j * 32 + row < d.rows && fc + at < d.hidden_pad)
@@ -596,8 +629,10 @@ hipError_t plain(PlainDev p, GemmJob job, hipStream_t st) {
 
 template <class T>
 hipError_t grad(const FeedDev& d, GemmJob job, hipStream_t st) {
-    // What follows the products reads two matrices besides and writes two. 8192x1024x4096: 103 to 108 us in tiles of 256 x 256,
-    // 119 to 128 of 128 x 192.
+    // What follows the products reads three matrices besides and writes two. us with 256 x 256, 256 x 128, 128 x 192, 128 x 128 (two
+    // stages), the same (three) and 64 x 64 tiles, and what the rule takes:
+    //   8192x1024x4096 131 127 128 131 155 183, 131        2048x1024x4096        41 34 35 31 39 46, 34
+    //   4096x1024x4096  59  62  68  65  74  88,  60        1999x1100x2731, fp16  43 29 32 31 40 42, 31
     constexpr float kMore[kTileKinds] = {20.0f, 12.0f, 10.0f, 7.0f, 7.0f, 3.0f};
     return with_tile<T, true, false, false, false>(choose(1, false, 1, &job.features, &job.rows, parts_of(job.len), 1, kMore).kind, [&](auto x) {
         typedef decltype(x) X;

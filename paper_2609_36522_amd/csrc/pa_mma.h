@@ -76,7 +76,12 @@ __device__ __forceinline__ typename Vec<T>::v8 pack(const f32x16& s, int t) {
 }
 
 // Eight consecutive elements per lane from registers 8j .. 8j + 7 (rows 16 j + 4 half + {0..3, 8..11}):
-// lanes below 32 receive rows 16 j .. + 7, the others 16 j + 8 .. + 15.
+// lanes below 32 receive rows 16 j .. + 7, the others 16 j + 8 .. + 15. w: the registers' 16-bit values in pairs.
+__device__ __forceinline__ uint4 rows8(const uint32_t (&w)[2][2]) {
+    const auto x = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
+    const auto y = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
+    return make_uint4(x[0], y[0], x[1], y[1]);
+}
 template <class T>
 __device__ __forceinline__ Pack8<T> gather8(const f32x16& a, int j, float f) {
     typedef T t2 __attribute__((ext_vector_type(2)));
@@ -89,9 +94,7 @@ __device__ __forceinline__ Pack8<T> gather8(const f32x16& a, int j, float f) {
             w[q][p] = __builtin_bit_cast(uint32_t, e);
         }
     }
-    const auto x = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
-    const auto y = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
-    return __builtin_bit_cast(Pack8<T>, make_uint4(x[0], y[0], x[1], y[1]));
+    return __builtin_bit_cast(Pack8<T>, rows8(w));
 }
 
 // Blocks are dealt to the 8 XCDs in turn: gives each XCD a contiguous range of work, so that

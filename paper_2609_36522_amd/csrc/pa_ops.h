@@ -77,7 +77,9 @@ struct FeedDev {
     int64_t x_stride, gate_stride, up_stride, down_stride, y_stride;
     const void *gate_bias, *up_bias, *down_bias;
     void* y;
-    void *by_z, *by_u, *h;           // [rows][hidden_pad] u act'(g) and act(g), by which dh gives dz and du (may be null), and the gated product
+    void* h;                         // [rows][hidden_pad] the gated product
+    uint16_t *by_z, *by_u, *last;    // [rows][hidden_pad] u act'(g) and act(g), by which dh gives dz and du, in 24 bits: their upper
+                                     // halves, and the last byte of both (may be null)
     void *dx, *dgate, *dup, *ddown, *dgate_bias, *dup_bias, *ddown_bias;
     void *dz, *du;                   // backward: [rows][hidden_pad] gradients by the two projections
     void *x_pad, *gate_pad, *up_pad, *down_pad, *dy_pad;   // copies in whole pieces of 16 bytes (null: read in place)

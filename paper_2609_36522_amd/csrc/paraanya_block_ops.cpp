@@ -139,13 +139,14 @@ FeedDev feed_dev(const pa_feed_t* p) {
     return d;
 }
 
-size_t feed_saved(const pa_feed_t* p) { return 3 * round256((size_t)p->rows * pad8(p->hidden_features) * 2); }
+size_t feed_saved(const pa_feed_t* p) { return 4 * round256((size_t)p->rows * pad8(p->hidden_features) * 2); }
 
 void feed_saved_parts(FeedDev& d, void* saved) {
     Parts w(saved);
     const size_t n = (size_t)d.rows * d.hidden_pad * 2;
-    d.by_z = w.take(n);
-    d.by_u = w.take(n);
+    d.by_z = static_cast<uint16_t*>(w.take(n));
+    d.by_u = static_cast<uint16_t*>(w.take(n));
+    d.last = static_cast<uint16_t*>(w.take(n));
     d.h = w.take(n);
 }
 

@@ -1,5 +1,5 @@
-"""The gated feed-forward block in 64 bits with bounds for what its kernels keep: h and the two factors by which dh gives the
-projections' gradients, each rounded to the element type once, and those gradients rounded once more."""
+"""The gated feed-forward block in 64 bits with bounds for what its kernels keep: h, rounded to the element type, the two factors
+by which dh gives the projections' gradients, cut to 24 bits, and those gradients, rounded to the element type."""
 import math
 
 import torch
@@ -7,8 +7,10 @@ import torch
 from block_ops_reference import CURVE, SLOPE, activation
 from ops_reference import TINY, U, U32
 
-# Roundings on the way to a result, its own among them: of h; of a factor and of dz or du; of h.
-ROUNDINGS = {"y": 2, "x": 3, "gate": 3, "up": 3, "down": 2, "gate_bias": 3, "up_bias": 3, "down_bias": 1}
+# Roundings to the element type on the way to a result, its own among them: of h; of dz or du; of h. (The factors' 2^-15 is a
+# sixteenth of fp16's rounding.)
+ROUNDINGS = {"y": 2, "x": 2, "gate": 2, "up": 2, "down": 2, "gate_bias": 2, "up_bias": 2, "down_bias": 1}
+CUT = 2.0 ** -15
 # Of normal numbers and of products of two, a rounding's root mean square over theirs: half a step is 2^e u for a value of
 # 2^e to 2^(e + 1), a third of its square the mean, and 0.4245 u the root of its sum over that of the values' squares.
 ROUNDING = 0.4245
@@ -36,11 +38,11 @@ def feed_forward(x, gate, up, down, biases, act, dy):
         out[name] = (v, 1.01 * e + u * A(v) + tiny)
 
     put("y", h @ D.T + bd, eh @ A(D).T + (H + 8) * U32 * (A(h) @ A(D).T + A(bd)))
-    # The factors, rounded; dz = dh f and du = dh a, rounded. In fp16 both times a power of two s with s max |dy| >= 1/16: half
+    # The factors, cut; dz = dh f and du = dh a, rounded. In fp16 both times a power of two s with s max |dy| >= 1/16: half
     # of the least spacing over s is at most 16 max |dy| times it.
     f = q * slope
-    ef = A(q) * es + eq * (A(slope) + es) + (u + U32) * A(f) + tiny
-    ea = ea + u * A(a) + tiny
+    ef = A(q) * es + eq * (A(slope) + es) + (CUT + U32) * A(f)
+    ea = ea + CUT * A(a)
     small = 16 * tiny * (float(A(Y).max()) if dt == torch.float16 and Y.numel() else 1.0)
     dh, edh = Y @ D, (N + 8) * U32 * (A(Y) @ A(D))
     dz, du = dh * f, dh * a
@@ -61,7 +63,7 @@ def norm_limit(name, want, dt, kept):
     """What the root of the squared errors' sum may be: of independent roundings, with room for their number and for the spread
     of sums of their squares; a result below the type's normal numbers is off by half of their least spacing.
 
-    `kept`: the number of values that h, a factor, dz or du has; each is rounded once, however many results it goes into (one
+    `kept`: the number of values that h, dz or du has; each is rounded once, however many results it goes into (one
     row's go into an outer product), so that a result has no more independent errors than that. The squares summed are of
     products of up to three normal numbers, whose fourth moment is 27 times their second's square, times a rounding's square,
     whose own is 9/5: the sum's deviation is sqrt(27 * 9 / 5 / kept), the root's half of that, 3.5 / sqrt(kept), three times

@@ -168,6 +168,26 @@ def test_feed_forward_roundings(M, K, H, N, dt, act):
     _feed(M, K, H, N, dt, act, seed=M + K)
 
 
+@pytest.mark.parametrize("M", [20, 300])
+def test_feed_forward_in_fp16_with_projections_beyond_its_range(M):
+    """u about 2^17, g about 2^-8: h is a number in fp16, u is not, and dz 2^17 times dy is by its scale. Rows without a
+    gradient stay so."""
+    g = torch.Generator(device="cuda").manual_seed(M)
+    K, H, N = 64, 96, 48
+    x, gate, up, down = (_randn(g, *s) * f for s, f in (((M, K), 4), ((H, K), 2.0**-13), ((H, K), 4096), ((N, H), 0.07)))
+    args = tuple(t.half() for t in (x, gate, up, down))
+    dy = (_randn(g, M, N) * 2.0**-10).half()
+    dy[3] = 0
+    assert float((args[0].double() @ args[2].double().T).abs().median()) > 65504
+    y, saved = ops.feed_forward_forward(*args, activation=None)
+    grads = ops.feed_forward_backward(dy, *args, saved, activation=None)
+    ref = F.feed_forward(*args, (None,) * 3, None, dy)
+    assert all(bool((ref[n][0].abs() < 65504).all()) for n in ("y", "x", "gate", "up", "down"))
+    for name, got in (("y", y), *grads._asdict().items()):
+        check(got, *ref[name], name)
+    assert not bool(grads.x[3].any())
+
+
 # ------------------------------------------------------------------ 8-bit integers
 @pytest.mark.parametrize("M,K,N", INT8_TILES + [(16, 500, 4111), (17, 500, 4111), (50, 1100, 5000), (64, 129, 4096)])
 @pytest.mark.parametrize("dt", [BF16, F16], ids=["bf16", "f16"])
