@@ -131,7 +131,7 @@ __device__ __forceinline__ void add(const float* per_feature, int half, f32x16 (
 // Both projections of a tile of rows, which read x once for the two; the activation and the product are formed in the
 // registers that hold them. Bound by the matrix units (the clock falls to 1.64 GHz under them, 77% busy) at long
 // reductions, by what follows the products at short ones: 32768x2048x8192 1720 us (1280 TFLOP/s; the library's product of this
-// size alone 1555), 8192x1024x4096 128 (1070), 156 to 171 where the factors of the backward pass are formed and kept.
+// size alone 1555), 8192x1024x4096 126 to 141 (1090 to 970), 156 to 174 where the factors of the backward pass are formed and kept.
 template <class X, int ACT>
 __global__ __launch_bounds__(X::THREADS, X::WAVES) void k_feed_gate(FeedDev d, GemmJob job) {
     typedef typename X::T T;
@@ -198,7 +198,7 @@ __global__ __launch_bounds__(X::THREADS, X::WAVES) void k_feed_gate(FeedDev d, G
 
 // out = R F^T + bias, or its partial sums over ranges of the reduction: [split][rows][feature_pad] in `part`: the projection
 // back, and dx. Bound as k_feed_gate is: 32768x8192 to 2048 900 us (1220 TFLOP/s), 8192x4096 to 1024 66 (1040; the library 60),
-// dx of 8192x1024x4096, over both projections, 132 to 144 (the library's product of this size 144).
+// dx of 8192x1024x4096, over both projections, 127 to 144 (the library's product of this size 144).
 struct PlainDev {
     const void* bias;
     void* out;
@@ -439,7 +439,7 @@ __global__ __launch_bounds__(X::THREADS, X::WAVES) void k_feed_grad(FeedDev d, G
 }
 
 // The weights' gradients, up to three products in one launch (alone none fills the CUs); a split takes a range of the rows.
-// Bound by the matrix units on the 192 CUs that have one of its tiles: 8192x1024x4096 235 to 255 us, 206 GFLOP.
+// Bound by the matrix units on the 192 CUs that have one of its tiles: 8192x1024x4096 203 to 255 us, 206 GFLOP.
 struct WeightsDev {
     GemmJob job[3];
     void *out[3], *bias[3];          // [rows][features], [rows] (sums over the reduction of R; may be null)

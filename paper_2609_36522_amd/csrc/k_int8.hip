@@ -124,7 +124,7 @@ __device__ __forceinline__ float scaled(const Int8Dev& d, int v, float xs, int f
 }
 
 // Bound by the matrix units (busy 54% of the time) and, where a tile's reduction is as short as 16 parts, by the results that
-// follow it: 32768x2048x8192 560 to 580 us, 1.9 to 2.0 P operations/s.
+// follow it: 32768x2048x8192 557 to 600 us, 1.8 to 2.0 P operations/s.
 template <class X, class T>
 __global__ __launch_bounds__(X::THREADS, X::WAVES) void k_int8_tile(Int8Dev d, GemmJob job) {
     __shared__ __align__(16) char lds[X::BYTES];
